@@ -269,6 +269,115 @@ mixlora_status_t mixlora_lora_linear_backward(const mixlora_linear_shape_t *shap
                                               void *d_x, int32_t accumulate, void *stream);
 int32_t mixlora_lora_linear_status(const void *workspace, void *stream);
 
+/* Rotary positions on the query and key projections, the step between mixlora_lora_linear_forward and the attention of
+ * a LLaMA-class layer (the paper trains such layers and prints no formula).  The leading rotary_dim values of each head
+ * are taken as rotary_dim / 2 pairs (u, w): value i with value i + rotary_dim / 2 (MIXLORA_ROPE_HALF), or value 2 i with
+ * 2 i + 1 (MIXLORA_ROPE_INTERLEAVED).  Pair i of a token at position p is turned by the angle p * inv_freq[i]:
+ *     u' = amplitude (u cos - w sin),  w' = amplitude (w cos + u sin);
+ * values behind rotary_dim are copied.  Angles are reduced in 64 bits, so positions up to 2^31 - 1 (and negative ones)
+ * keep fp32-exact sines.  mixlora_rope_backward applies the transpose (the same turn backwards) to the gradients.
+ * q [tokens, q_heads, head_dim], k [tokens, k_heads, head_dim] and their outputs are device arrays of shape.dtype whose
+ * tokens lie *_stride elements apart (0: dense), so q and k may be parts of one product's rows; an output is either its
+ * input (same pointer and stride) or does not overlap it.  k_heads = 0 leaves k out (k, k_out ignored).
+ * head_dim <= 512 and the strides are multiples of 8; rotary_dim is even, 2 .. head_dim.  `positions` [tokens] int32, or
+ * NULL for 0 .. tokens - 1; `inv_freq` [rotary_dim / 2] fp64.  Needs no workspace.
+ *
+ * mixlora_rope_frequencies fills inv_freq, once per model.  With w_i = theta^(-2 i / rotary_dim):
+ *   NONE    w_i
+ *   LINEAR  w_i / factor                                       (positions squeezed by factor)
+ *   NTK     w_i of theta * factor^(rotary_dim / (rotary_dim - 2))   (the slowest pair alone is stretched fully)
+ *   PARTS   w_i / factor for pairs that make at most low_turns turns over original_positions, w_i for those that make at
+ *           least high_turns, and in between the two blended linearly in the number of turns.
+ * theta > 0, factor > 0; PARTS: 0 <= low_turns < high_turns, original_positions > 0 (ignored otherwise). */
+#define MIXLORA_ROPE_HALF 0
+#define MIXLORA_ROPE_INTERLEAVED 1
+#define MIXLORA_ROPE_SCALE_NONE 0
+#define MIXLORA_ROPE_SCALE_LINEAR 1
+#define MIXLORA_ROPE_SCALE_NTK 2
+#define MIXLORA_ROPE_SCALE_PARTS 3
+typedef struct {
+  uint32_t struct_size;       /* = sizeof(mixlora_rope_shape_t) */
+  int32_t tokens;
+  int32_t q_heads, k_heads;
+  int32_t head_dim, rotary_dim;
+  int32_t layout;             /* MIXLORA_ROPE_HALF or MIXLORA_ROPE_INTERLEAVED */
+  int32_t dtype;              /* MIXLORA_DTYPE_* */
+  float amplitude;            /* 1 = a pure rotation */
+  int32_t reserved;           /* 0 */
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+} mixlora_rope_shape_t;
+mixlora_status_t mixlora_rope_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor,
+                                          double low_turns, double high_turns, int32_t original_positions,
+                                          double *inv_freq /* device */, void *stream);
+mixlora_status_t mixlora_rope_forward(const mixlora_rope_shape_t *shape /* host */, const void *q, const void *k,
+                                      const int32_t *positions, const double *inv_freq, void *q_out, void *k_out,
+                                      void *stream);
+mixlora_status_t mixlora_rope_backward(const mixlora_rope_shape_t *shape /* host */, const void *d_q_out,
+                                       const void *d_k_out, const int32_t *positions, const double *inv_freq, void *d_q,
+                                       void *d_k, void *stream);
+
+/* Attention between the (rotated) query, key and value projections and the output projection of a layer, over a packed
+ * batch of sequences ("the attention layer" in front of the block of Eq. 5-6).
+ * Sequence b owns the query rows q_off[b] .. q_off[b+1] - 1 and the key rows k_off[b] .. k_off[b+1] - 1, of which the
+ * first k_len[b] are in use (all of them if k_len is NULL): a training batch passes the same offsets twice, a cache of
+ * fixed slots passes multiples of the slot and the used lengths.  With lq, lk the two lengths, key j stands at position
+ * j and query row i at position p_i = lk - lq + i (the last row at the last key).  Row i sees key j < lk when
+ *     j < prefix[b]   or   (causal: j <= p_i)  and  (window > 0: |p_i - j| < window).
+ * For query head h and its key head h / (q_heads / kv_heads):
+ *     s_ij = scale q_i . k_j;   softcap > 0: s <- softcap tanh(s / softcap);   slopes: s <- s - slopes[h] |p_i - j|
+ *     o_i = sum_j e^(s_ij - lse_i) v_j,   lse_i = ln sum_j e^(s_ij)         over the keys that row i sees.
+ * A row that sees nothing gets o = 0 and lse = -inf, and adds nothing to any gradient.  Rows outside every sequence
+ * (behind the last one, behind k_len) are neither read into a result nor written, in outputs and gradients alike, and
+ * may hold anything; an inf or NaN in a row that a sequence does use may reach every row of that sequence and head, also
+ * those whose mask hides it.  Offsets have to ascend and stay inside the tensors; values that do not are clamped on
+ * the device (no access leaves a tensor, the result of such a sequence is unspecified).
+ *
+ * q, o, d_o, d_q [q_rows, q_heads, head_dim]; k, v, d_k, d_v [k_rows, kv_heads, head_dim]; all device arrays of
+ * shape.dtype, 16-byte aligned, rows *_stride elements apart (0: dense; d_q, d_k, d_v have the strides of q, k, v, and
+ * d_o that of o), so q, k, v may be parts of one product's rows.  lse [q_heads, q_rows] fp32.  head_dim <= 128 and the
+ * strides are multiples of 8.  Outputs must not overlap inputs.
+ * max_q_len, max_k_len: upper bounds of lq and lk over the sequences where the caller knows them, else 0.  With
+ * max_q_len > 0 and max_q_len * q_heads / kv_heads <= 64 (a decoding step) the forward call reads the cache once for all
+ * rows that share a key head and splits long caches over the GPU; rows behind a sequence's max_q_len-th are then left
+ * unwritten.  max_k_len only steers that split.
+ *
+ * mixlora_attention_backward takes o and lse as the forward call left them and returns the gradients of <d_o, o> with
+ * respect to q, k and v (sums over shared heads included); scale, softcap, slopes and prefix get none.  Results do not
+ * depend on the order in which blocks run.  The workspace (256-byte aligned, mixlora_attention_workspace_bytes) is
+ * scratch of one call: nothing is kept in it from forward to backward, and calls that may run at the same time need one
+ * each; mixlora_device_status works on it. */
+#define MIXLORA_MAX_HEAD_DIM 128
+typedef struct {
+  uint32_t struct_size;       /* = sizeof(mixlora_attention_shape_t) */
+  int32_t n_seqs;
+  int32_t q_rows, k_rows;     /* rows of q and of k, v; each <= 2^30 */
+  int32_t max_q_len, max_k_len;
+  int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
+  int32_t head_dim;
+  int32_t dtype;              /* MIXLORA_DTYPE_* */
+  int32_t causal;             /* 0 or 1 */
+  int32_t window;             /* 0: none */
+  float scale;                /* > 0 */
+  float softcap;              /* 0: none */
+  int64_t q_stride, k_stride, v_stride, o_stride;
+} mixlora_attention_shape_t;
+typedef struct {
+  const int32_t *q_off, *k_off;   /* [n_seqs + 1] */
+  const int32_t *k_len;           /* [n_seqs] or NULL */
+  const int32_t *prefix;          /* [n_seqs] or NULL */
+  const float *slopes;            /* [q_heads] or NULL */
+} mixlora_attention_mask_t;
+size_t mixlora_attention_workspace_bytes(const mixlora_attention_shape_t *shape /* host */, int for_backward);
+mixlora_status_t mixlora_attention_forward(const mixlora_attention_shape_t *shape /* host */,
+                                           const mixlora_attention_mask_t *mask /* host struct of device ptrs */,
+                                           const void *q, const void *k, const void *v, void *o, float *lse /* or NULL */,
+                                           void *workspace, size_t workspace_bytes, void *stream);
+mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *shape /* host */,
+                                            const mixlora_attention_mask_t *mask /* host struct of device ptrs */,
+                                            const void *q, const void *k, const void *v, const void *o,
+                                            const float *lse, const void *d_o, void *workspace, size_t workspace_bytes,
+                                            void *d_q, void *d_k, void *d_v, void *stream);
+
 /* Device pointers into the workspace, for inspection after a forward call:
  * expert_idx [T, k] (descending logit), gates [T, k], perm [T*k] (slot id at each position
  * of the order "expert ascending, token ascending"), seg_off [N+1] (first position of each

@@ -27,10 +27,20 @@ EXPORTS = ("mixlora_limits", "mixlora_workspace_bytes", "mixlora_ffn_forward", "
            "mixlora_layer_backward", "mixlora_lora_linear_workspace_bytes", "mixlora_lora_linear_forward",
            "mixlora_lora_linear_backward", "mixlora_lora_linear_status", "mixlora_ffn_backward_overlap",
            "mixlora_aux_stats", "mixlora_aux_loss_global", "mixlora_set_option", "mixlora_selftest_wait_timeout",
-           "mixlora_dora_workspace_bytes", "mixlora_dora_ffn_forward", "mixlora_dora_ffn_backward")
+           "mixlora_dora_workspace_bytes", "mixlora_dora_ffn_forward", "mixlora_dora_ffn_backward",
+           "mixlora_rope_frequencies", "mixlora_rope_forward", "mixlora_rope_backward",
+           "mixlora_attention_workspace_bytes", "mixlora_attention_forward", "mixlora_attention_backward")
 
 MIXLORA_OPT_SERIAL = 0
 MIXLORA_OPT_TC_SINGLE = 1
+
+MIXLORA_ROPE_HALF = 0
+MIXLORA_ROPE_INTERLEAVED = 1
+MIXLORA_ROPE_SCALE_NONE = 0
+MIXLORA_ROPE_SCALE_LINEAR = 1
+MIXLORA_ROPE_SCALE_NTK = 2
+MIXLORA_ROPE_SCALE_PARTS = 3
+MIXLORA_MAX_HEAD_DIM = 128
 
 
 class mixlora_linear_shape_t(C.Structure):
@@ -60,6 +70,25 @@ class mixlora_dora_t(C.Structure):
 
 class mixlora_dora_grads_t(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("d_m_gate", "d_m_up", "d_m_down")]
+
+
+class mixlora_rope_shape_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("tokens", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("dtype", C.c_int32),
+                ("amplitude", C.c_float), ("reserved", C.c_int32), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("q_out_stride", C.c_int64), ("k_out_stride", C.c_int64)]
+
+
+class mixlora_attention_shape_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("q_rows", C.c_int32), ("k_rows", C.c_int32),
+                ("max_q_len", C.c_int32), ("max_k_len", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32),
+                ("scale", C.c_float), ("softcap", C.c_float), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("o_stride", C.c_int64)]
+
+
+class mixlora_attention_mask_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_off", "k_off", "k_len", "prefix", "slopes")]
 
 
 class mixlora_limits_t(C.Structure):
@@ -154,6 +183,20 @@ def _load() -> C.CDLL:
                                               C.POINTER(mixlora_dora_t), C.c_void_p, C.c_float, C.c_void_p, C.c_size_t,
                                               C.POINTER(mixlora_grads_t), C.POINTER(mixlora_dora_grads_t), C.c_void_p]
     lib.mixlora_dora_ffn_backward.restype = C.c_int
+    lib.mixlora_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double,
+                                             C.c_int32, C.c_void_p, C.c_void_p]
+    lib.mixlora_rope_frequencies.restype = C.c_int
+    for name in ("mixlora_rope_forward", "mixlora_rope_backward"):
+        getattr(lib, name).argtypes = [C.POINTER(mixlora_rope_shape_t)] + [C.c_void_p] * 7
+        getattr(lib, name).restype = C.c_int
+    lib.mixlora_attention_workspace_bytes.argtypes = [C.POINTER(mixlora_attention_shape_t), C.c_int]
+    lib.mixlora_attention_workspace_bytes.restype = C.c_size_t
+    lib.mixlora_attention_forward.argtypes = ([C.POINTER(mixlora_attention_shape_t), C.POINTER(mixlora_attention_mask_t)] +
+                                              [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p])
+    lib.mixlora_attention_forward.restype = C.c_int
+    lib.mixlora_attention_backward.argtypes = ([C.POINTER(mixlora_attention_shape_t), C.POINTER(mixlora_attention_mask_t)] +
+                                               [C.c_void_p] * 7 + [C.c_size_t] + [C.c_void_p] * 4)
+    lib.mixlora_attention_backward.restype = C.c_int
     lib.mixlora_status_string.argtypes = [C.c_int]
     lib.mixlora_status_string.restype = C.c_char_p
     return lib
@@ -424,3 +467,66 @@ def mixlora_ffn_backward_overlap(shape, params, dy, aux_coef, workspace, grads, 
                                             workspace.numel() if workspace is not None else 0, C.byref(grads),
                                             C.c_void_p(handle) if handle else None, _stream(stream)),
            "mixlora_ffn_backward_overlap")
+
+
+def make_rope_shape(tokens, q_heads, k_heads, head_dim, rotary_dim, layout=MIXLORA_ROPE_HALF, dtype=MIXLORA_DTYPE_BF16,
+                    amplitude=1.0, q_stride=0, k_stride=0, q_out_stride=0, k_out_stride=0) -> mixlora_rope_shape_t:
+    """Strides in elements from token to token; 0 = dense."""
+    return mixlora_rope_shape_t(C.sizeof(mixlora_rope_shape_t), tokens, q_heads, k_heads, head_dim, rotary_dim, layout,
+                                dtype, float(amplitude), 0, q_stride, k_stride, q_out_stride, k_out_stride)
+
+
+def mixlora_rope_frequencies(rotary_dim, theta, scaling, factor, low_turns, high_turns, original_positions, inv_freq,
+                             stream=None) -> None:
+    """Fills inv_freq [rotary_dim / 2] (fp64) with the radians per position of every pair; once per model."""
+    _check(lib.mixlora_rope_frequencies(int(rotary_dim), float(theta), int(scaling), float(factor), float(low_turns),
+                                        float(high_turns), int(original_positions), _ptr(inv_freq), _stream(stream)),
+           "mixlora_rope_frequencies")
+
+
+def mixlora_rope_forward(shape, q, k, positions, inv_freq, q_out, k_out, stream=None) -> None:
+    """q and k turned by their positions (int32 [tokens], or None for 0, 1, ...); outputs may be the inputs."""
+    _check(lib.mixlora_rope_forward(C.byref(shape), _ptr(q), _ptr(k), _ptr(positions), _ptr(inv_freq), _ptr(q_out),
+                                    _ptr(k_out), _stream(stream)), "mixlora_rope_forward")
+
+
+def mixlora_rope_backward(shape, d_q_out, d_k_out, positions, inv_freq, d_q, d_k, stream=None) -> None:
+    _check(lib.mixlora_rope_backward(C.byref(shape), _ptr(d_q_out), _ptr(d_k_out), _ptr(positions), _ptr(inv_freq),
+                                     _ptr(d_q), _ptr(d_k), _stream(stream)), "mixlora_rope_backward")
+
+
+def make_attention_shape(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim, dtype=MIXLORA_DTYPE_BF16, scale=None,
+                         causal=1, window=0, softcap=0.0, max_q_len=0, max_k_len=0, q_stride=0, k_stride=0, v_stride=0,
+                         o_stride=0) -> mixlora_attention_shape_t:
+    """scale None = 1 / sqrt(head_dim); strides in elements from row to row, 0 = dense."""
+    return mixlora_attention_shape_t(C.sizeof(mixlora_attention_shape_t), n_seqs, q_rows, k_rows, max_q_len, max_k_len,
+                                     q_heads, kv_heads, head_dim, dtype, causal, window,
+                                     float(head_dim ** -0.5 if scale is None else scale), float(softcap), q_stride,
+                                     k_stride, v_stride, o_stride)
+
+
+def make_attention_mask(q_off, k_off, k_len=None, prefix=None, slopes=None) -> mixlora_attention_mask_t:
+    """Device arrays: int32 offsets [n_seqs + 1], used key lengths and prefix lengths [n_seqs], fp32 slopes [q_heads].
+    The struct holds their addresses only: keep the tensors alive as long as it is used."""
+    return mixlora_attention_mask_t(_ptr(q_off), _ptr(k_off), _ptr(k_len), _ptr(prefix), _ptr(slopes))
+
+
+def alloc_attention_workspace(shape, for_backward: bool, device="cuda") -> torch.Tensor:
+    n = int(lib.mixlora_attention_workspace_bytes(C.byref(shape), 1 if for_backward else 0))
+    if n == 0:
+        raise MixLoraError(1, "mixlora_attention_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def mixlora_attention_forward(shape, mask, q, k, v, o, lse, workspace, stream=None) -> None:
+    """o = softmax(scores) v over the keys that each row sees; lse [q_heads, q_rows] may be None."""
+    _check(lib.mixlora_attention_forward(C.byref(shape), C.byref(mask), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
+                                         _ptr(workspace), workspace.numel() if workspace is not None else 0,
+                                         _stream(stream)), "mixlora_attention_forward")
+
+
+def mixlora_attention_backward(shape, mask, q, k, v, o, lse, d_o, workspace, d_q, d_k, d_v, stream=None) -> None:
+    _check(lib.mixlora_attention_backward(C.byref(shape), C.byref(mask), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
+                                          _ptr(d_o), _ptr(workspace), workspace.numel() if workspace is not None else 0,
+                                          _ptr(d_q), _ptr(d_k), _ptr(d_v), _stream(stream)),
+           "mixlora_attention_backward")

@@ -1,0 +1,156 @@
+// Shared parts of the attention kernels: arguments, the sequences' geometry, which keys a query sees.
+#pragma once
+
+#include "common.cuh"
+
+namespace mixlora {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct AttnArgs {
+  const void *q, *k, *v;          // [rows, heads, head_dim], `*_stride` elements from row to row
+  const void *o, *d_o;            // backward: the forward's output and its gradient, both with o's stride
+  void* out;                      // forward: o
+  void *dq, *dk, *dv;             // strides of q, k, v
+  float* lse;                     // [q_heads, q_rows], natural logarithm
+  const float* lse2;              // backward: lse in base 2, +inf for rows that see nothing   [q_heads, q_rows]
+  const float* delta;             // backward: sum over head_dim of o * d_o                    [q_heads, q_rows]
+  const int32_t *q_off, *k_off;   // [n_seqs + 1]
+  const int32_t *k_len, *prefix;  // [n_seqs] or NULL
+  const float* slopes;            // [q_heads] or NULL
+  int32_t* status;
+  long long q_stride, k_stride, v_stride, o_stride;
+  int n_seqs, q_rows, k_rows, q_heads, kv_heads, group, head_dim;
+  int causal, window, max_q_len;
+  float scale;                    // multiplies q . k
+  float softcap;                  // > 0: scores become softcap * tanh(score / softcap)
+};
+
+// One sequence: its rows and keys, and the position of its first row (query row i has position shift + i; key j has
+// position j, so that the last row stands at the last key).  Offsets come from device memory and are held inside the
+// tensors whatever they say.
+struct AttnSeq {
+  int q0, lq, k0, lk, shift, prefix;
+};
+
+__device__ __forceinline__ int clamp_int(int v, int lo, int hi) { return min(max(v, lo), hi); }
+
+__device__ __forceinline__ int seq_rows(const int32_t* off, int b, int rows) {
+  const int a = clamp_int(off[b], 0, rows);
+  return clamp_int(off[b + 1], a, rows) - a;
+}
+
+__device__ __forceinline__ AttnSeq load_seq(const AttnArgs& p, int b) {
+  AttnSeq s;
+  s.q0 = clamp_int(p.q_off[b], 0, p.q_rows);
+  s.lq = seq_rows(p.q_off, b, p.q_rows);
+  s.k0 = clamp_int(p.k_off[b], 0, p.k_rows);
+  s.lk = seq_rows(p.k_off, b, p.k_rows);
+  if (p.k_len) s.lk = clamp_int(p.k_len[b], 0, s.lk);
+  s.shift = s.lk - s.lq;
+  s.prefix = p.prefix ? clamp_int(p.prefix[b], 0, s.lk) : 0;
+  return s;
+}
+
+// Finds, with the 32 lanes of one warp, the sequence and the tile in it that tile number `tile` stands for when every
+// sequence has ceil(rows / tile_rows) tiles; false behind the last one.  A sequence's tiles count from its end: under
+// a causal mask the last rows have the most keys, and long work that starts first ends with the rest.
+__device__ __forceinline__ bool find_tile(const int32_t* off, int n_seqs, int rows, int tile_rows, int tile, int* seq,
+                                          int* index) {
+  const int lane = threadIdx.x & 31;
+  for (int base = 0; base < n_seqs; base += 32) {
+    const int b = base + lane;
+    const int n = b < n_seqs ? (seq_rows(off, b, rows) + tile_rows - 1) / tile_rows : 0;
+    int sum = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += up;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, tile < sum);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      const int end = __shfl_sync(0xffffffffu, sum, l);
+      *seq = base + l;
+      *index = end - 1 - tile;
+      return true;
+    }
+    tile -= __shfl_sync(0xffffffffu, sum, 31);
+  }
+  return false;
+}
+
+// Keys that a query at position `pos` sees: [lo, hi) and everything before `prefix`.
+struct RowKeys {
+  int lo, hi, prefix;
+  __device__ __forceinline__ bool sees(int j) const { return (j >= lo && j < hi) || j < prefix; }
+};
+__device__ __forceinline__ RowKeys row_keys(const AttnSeq& s, int causal, int window, int pos) {
+  RowKeys r{0, s.lk, s.prefix};
+  if (causal) r.hi = min(r.hi, pos + 1);
+  if (window) {
+    r.lo = max(0, pos - window + 1);
+    r.hi = (int)min((long long)r.hi, (long long)pos + window);
+  }
+  return r;
+}
+
+// Key tiles (of TILE keys) that the queries at positions [p0, p1] need: tiles [0, pre) and [lo, hi), pre <= lo.
+template <int TILE>
+struct KeyTiles {
+  int pre, lo, hi;
+  __device__ __forceinline__ int count() const { return pre + max(hi - lo, 0); }
+  __device__ __forceinline__ int at(int i) const { return i < pre ? i : lo + i - pre; }
+  __device__ __forceinline__ bool has(int t) const { return t < pre || (t >= lo && t < hi); }
+};
+template <int TILE>
+__device__ __forceinline__ KeyTiles<TILE> key_tiles(const AttnSeq& s, int causal, int window, int p0, int p1) {
+  KeyTiles<TILE> t;
+  const int first = row_keys(s, causal, window, p0).lo, last = max(row_keys(s, causal, window, p1).hi, s.prefix);
+  t.lo = min(first, s.lk) / TILE;
+  t.hi = (max(last, 0) + TILE - 1) / TILE;
+  t.pre = min((s.prefix + TILE - 1) / TILE, t.lo);
+  return t;
+}
+
+// Whether every query at positions [p0, p1] sees every key of [j0, j1).
+__device__ __forceinline__ bool all_seen(const AttnSeq& s, int causal, int window, int p0, int p1, int j0, int j1) {
+  if (j1 > s.lk) return false;
+  if (j1 <= s.prefix) return true;
+  if (causal && j1 - 1 > p0) return false;
+  if (window && (p1 - j0 >= window || j1 - 1 - p0 >= window)) return false;
+  return true;
+}
+
+// Query rows [lo, hi) that may see one of the keys [j0, j1).
+__device__ __forceinline__ void query_rows(const AttnSeq& s, int causal, int window, int j0, int j1, int* lo, int* hi) {
+  *lo = 0;
+  *hi = s.lq;
+  if (j0 < s.prefix) return;
+  if (causal) *lo = clamp_int(j0 - s.shift, 0, s.lq);
+  if (window) {
+    if (!causal) *lo = (int)max((long long)*lo, min((long long)s.lq, (long long)j0 - s.shift - window + 1));
+    *hi = (int)max((long long)*lo, min((long long)s.lq, (long long)j1 - 1 - s.shift + window));
+  }
+}
+
+// tanh from two special-function operations: 1 - 2 / (1 + e^(2x)).  Its absolute error, a few 2^-24, is what counts
+// for a score (the relative one of a small x is bounded by the cap times that).
+__device__ __forceinline__ float tanh_fast(float x) {
+  return 1.f - __fdividef(2.f, 1.f + exp2f(x * (2.f * kLog2e)));
+}
+
+cudaError_t launch_attn_forward_tc(const AttnArgs& p, cudaStream_t st);
+cudaError_t launch_attn_backward_tc(const AttnArgs& p, cudaStream_t st);
+cudaError_t launch_attn_forward_simt(const AttnArgs& p, cudaStream_t st);
+cudaError_t launch_attn_backward_simt(const AttnArgs& p, cudaStream_t st);
+cudaError_t launch_attn_delta(const AttnArgs& p, bool bf16_mode, float* lse2, float* delta, cudaStream_t st);
+
+// Few query rows for each sequence and key head: a split over the keys, joined by a second launch.
+constexpr int kFewRows = 16;                     // rows of a block
+constexpr int kFewRowsMax = 64;                  // rows of a sequence and key head up to which this form is taken
+int attn_few_splits(int n_seqs, int kv_heads, int rows, long long k_rows, int max_k_len);
+cudaError_t launch_attn_few(const AttnArgs& p, bool bf16_mode, int splits, float* part, cudaStream_t st);
+
+}  // namespace mixlora

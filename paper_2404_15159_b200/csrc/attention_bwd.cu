@@ -1,0 +1,636 @@
+// Masked attention, backward, bf16, on the tensor cores.
+//
+//   p_ij  = e^(s_ij - lse_i)                       from the forward's log-sum-exp
+//   dv_j  = sum_i p_ij do_i
+//   ds_ij = p_ij (do_i . v_j - delta_i) c'_ij      delta_i = do_i . o_i;  c' = 1 - tanh^2 of a capped score, else 1
+//   dq_i  = scale sum_j ds_ij k_j                  dk_j = scale sum_i ds_ij q_i
+//
+// Two launches over the same tiles: one owns 128 keys and walks over the query rows that see them (and over the query
+// heads that share the key head) for dk and dv, one owns 128 query rows and walks over their keys for dq.  Scores and
+// p are formed in both: seven products of a tile instead of five, but every gradient is summed by one block in one
+// order, in TMEM, without atomics.
+#include <cuda.h>
+#include <string.h>
+
+#include "attention.cuh"
+#include "tc_ptx.cuh"
+
+namespace mixlora {
+namespace {
+using namespace tc;
+
+constexpr int kTile = 128;
+constexpr int kThreads = 384;                    // two groups of 4 warps on the elements, a load warp, an MMA warp
+constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kTmemCols = 512;
+constexpr int kStages = 2;
+template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
+constexpr uint32_t kRowBytes = 2 * kTile * 4;    // lse and delta of a query tile
+template <int DP> constexpr uint32_t kSmemBytes = (2 + 2 * kStages) * kTileBytes<DP> + kStages * kRowBytes + 1024 + 256;
+
+struct BwdParams {
+  AttnArgs a;
+  CUtensorMap q_map, k_map, v_map, do_map;
+};
+
+struct Ctl {
+  uint32_t bars;
+  volatile int* abort_flag;
+  __device__ __forceinline__ uint32_t full(int s) const { return bars + 8u * s; }
+  __device__ __forceinline__ uint32_t empty(int s) const { return bars + 8u * (kStages + s); }
+  __device__ __forceinline__ uint32_t own() const { return bars + 8u * (2 * kStages); }        // the block's own tiles
+  __device__ __forceinline__ uint32_t s() const { return bars + 8u * (2 * kStages + 1); }      // scores are there
+  __device__ __forceinline__ uint32_t dp() const { return bars + 8u * (2 * kStages + 3); }     // do . v is there
+  __device__ __forceinline__ uint32_t p() const { return bars + 8u * (2 * kStages + 4); }      // p is written
+  __device__ __forceinline__ uint32_t ds() const { return bars + 8u * (2 * kStages + 5); }     // ds is written
+  __device__ __forceinline__ uint32_t acc() const { return bars + 8u * (2 * kStages + 6); }    // the sums are final
+};
+constexpr int kBars = 2 * kStages + 7;
+
+template <int DP>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
+#pragma unroll
+  for (int j = 0; j < DP / 64; ++j) tma_load_3d(dst + j * (kTile * 128), map, bar, j * 64, head, row);
+}
+// Rows [first, 128) of a tile belong to someone else and may hold anything; where they are summed over they have to be
+// finite (their factor is zero).  One warp.
+template <int DP>
+__device__ __forceinline__ void clear_rows(uint32_t tile, int first) {
+  constexpr int NB = DP / 64;
+  for (int i = threadIdx.x & 31; i < (kTile - first) * 8 * NB; i += 32) {
+    const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
+    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(tile + blk * (kTile * 128) + r * 128 + c * 16), "r"(0)
+                 : "memory");
+  }
+}
+// D[128 x 128] = A B^T over DP, both tiles K-major
+template <int DP>
+__device__ __forceinline__ void issue_nt(uint32_t d, uint32_t a, uint32_t b) {
+  const uint32_t idesc = make_idesc(kTile, 0, 0);
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) {
+    const uint32_t off = (k >> 2) * (kTile * 128) + (k & 3) * 32;
+    umma_bf16(d, make_desc_kmajor_rows(a + off, 128), make_desc_kmajor_rows(b + off, 128), idesc, k != 0);
+  }
+}
+// D[128 x DP] += A B, A bf16 [128 x 128] in TMEM (columns 0-31 and 64-95 of its region), B rows = the summed index
+template <int DP>
+__device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint32_t b, bool accumulate) {
+  const uint32_t idesc = make_idesc(DP, 0, 1);
+#pragma unroll
+  for (int k = 0; k < kTile / 16; ++k)
+    umma_bf16_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, make_desc(b + k * 2048, kTile * 128, 1024), idesc, accumulate || k != 0);
+}
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  const __nv_bfloat162 e = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&e);
+}
+template <int DP>
+__device__ __forceinline__ void store_row(uint32_t acc, bool any, float mul, bool mine, bf16* dst, int head_dim) {
+#pragma unroll
+  for (int c = 0; c < DP / 32; ++c) {
+    uint32_t v[32];
+    if (any) {
+      tmem_ld32(acc + c * 32, v);
+      tmem_ld_wait();
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      if (mine && c * 32 + g * 8 < head_dim) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (any) {
+          uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            wp[i] = pack2(__uint_as_float(v[g * 8 + 2 * i]) * mul, __uint_as_float(v[g * 8 + 2 * i + 1]) * mul);
+        }
+        *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = w;
+      }
+  }
+}
+
+// Block setup shared by both kernels: the block's tile, barriers, TMEM.  `loaders`: arrivals that fill a stage.  False:
+// nothing to do.
+__device__ __forceinline__ bool block_begin(const int32_t* off, int n_seqs, int rows, int tile, bool from_end,
+                                            int loaders, const Ctl& c, uint32_t* slot, int* seq, int* index) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* found = reinterpret_cast<volatile int*>(slot + 2);
+  if (warp == 0) {
+    int b = -1, t = 0;
+    if (!find_tile(off, n_seqs, rows, kTile, tile, &b, &t)) b = -1;
+    if (b >= 0 && !from_end) t = (seq_rows(off, b, rows) + kTile - 1) / kTile - 1 - t;
+    if (lane == 0) { found[0] = b; found[1] = t; }
+  }
+  if (threadIdx.x == 32) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(c.full(s), loaders); mbar_init(c.empty(s), 1); }
+    mbar_init(c.own(), 1);
+    mbar_init(c.s(), 1); mbar_init(c.s() + 8u, 1);
+    mbar_init(c.dp(), 1); mbar_init(c.acc(), 1);
+    mbar_init(c.p(), 8); mbar_init(c.ds(), 8);
+    *c.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  *seq = found[0];
+  *index = found[1];
+  if (*seq < 0) return false;
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(slot), kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  return true;
+}
+__device__ __forceinline__ void give_up(const Ctl& c, int32_t* status) {
+  *c.abort_flag = 1;
+  if (status) atomicExch(status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+}
+__device__ __forceinline__ void block_end(const Ctl& c, uint32_t tmem) {
+  tc_fence_before();
+  __syncthreads();
+  if (*c.abort_flag) {
+    for (int i = 0; i < 200; ++i) __nanosleep(5000);         // let copies that may still be in flight land
+  }
+  tc_fence_after();
+  if ((threadIdx.x >> 5) == kMmaWarp) {
+    __syncwarp();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// Scores of half a tile in base 2 less the row's log-sum-exp, and the slope of the cap
+template <bool CAP, bool BIAS>
+struct Score {
+  float mul, cap2, slope2;
+  __device__ __forceinline__ Score(const AttnArgs& a, int head)
+      : mul(CAP ? a.scale / a.softcap : a.scale * kLog2e), cap2(a.softcap * kLog2e),
+        slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
+  __device__ __forceinline__ float prob(float s, float lse2, int distance, float& cap_slope) const {
+    float x = s * mul;
+    if (CAP) {
+      const float t = tanh_fast(x);
+      cap_slope = 1.f - t * t;
+      x = cap2 * t;
+    }
+    if (BIAS) x -= slope2 * fabsf((float)distance);
+    return exp2f(x - lse2);
+  }
+};
+
+// dk, dv of 128 keys of a key head.  TMEM: S^T and dP^T [128 keys x 128 rows] (p^T and ds^T are written over them as
+// bf16 and read from there by the products), dv, dk.  While the element groups work on p the tensor cores form the
+// next dP^T and dk, while they work on ds the next S^T and dv.
+template <int DP, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_constant__ BwdParams p) {
+  constexpr uint32_t TB = kTileBytes<DP>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t k_tile = smem_u32(smem), v_tile = k_tile + TB, ring = k_tile + 2 * TB;
+  float* rows_smem = reinterpret_cast<float*>(smem + (2 + 2 * kStages) * TB);
+  uint8_t* ctl = reinterpret_cast<uint8_t*>(rows_smem) + kStages * kRowBytes;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * kBars);
+  const Ctl c{smem_u32(ctl), reinterpret_cast<volatile int*>(slot + 1)};
+  const AttnArgs& a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int kvh = blockIdx.x % a.kv_heads;
+  int seq, index;
+  // the first keys of a causal sequence are seen by the most rows: long work starts first
+  if (!block_begin(a.k_off, a.n_seqs, a.k_rows, blockIdx.x / a.kv_heads, false, 1 + 32, c, slot, &seq, &index)) return;
+  const uint32_t tmem = *slot;
+  const uint32_t t_s = tmem, t_dp = tmem + kTile, t_dv = tmem + 2 * kTile, t_dk = t_dv + DP;
+  const AttnSeq sq = load_seq(a, seq);
+  const int j0 = index * kTile;
+  const int keys = min(kTile, sq.lk - j0);                   // <= 0: behind the used part of a slot
+  int lo = 0, hi = 0;
+  if (keys > 0) query_rows(sq, a.causal, a.window, j0, j0 + keys, &lo, &hi);
+  lo = lo / kTile * kTile;
+  const int per_head = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
+  const int n = per_head * a.group;
+
+  if (warp == kLoadWarp) {
+    bool ok = true;
+    if (n > 0 && lane == 0) {
+      mbar_expect_tx(c.own(), 2 * TB);
+      load_tile<DP>(k_tile, &p.k_map, c.own(), kvh, sq.k0 + j0);
+      load_tile<DP>(v_tile, &p.v_map, c.own(), kvh, sq.k0 + j0);
+    }
+    for (int i = 0; i < n; ++i) {
+      const int st = i % kStages;
+      if (!__all_sync(0xffffffffu, mbar_wait(c.empty(st), ((i / kStages) & 1u) ^ 1u, c.abort_flag))) { ok = false; break; }
+      const int head = kvh * a.group + i / per_head, i0 = lo + (i % per_head) * kTile;
+      if (lane == 0) {
+        mbar_expect_tx(c.full(st), 2 * TB);
+        load_tile<DP>(ring + st * 2 * TB, &p.q_map, c.full(st), head, sq.q0 + i0);
+        load_tile<DP>(ring + st * 2 * TB + TB, &p.do_map, c.full(st), head, sq.q0 + i0);
+      }
+      float* dst = rows_smem + st * (2 * kTile);
+      const size_t at = (size_t)head * a.q_rows + sq.q0 + i0;
+#pragma unroll
+      for (int x = 0; x < kTile / 32; ++x) {
+        const int r = x * 32 + lane;
+        const bool on = i0 + r < sq.lq;
+        dst[r] = on ? a.lse2[at + r] : INFINITY;
+        dst[kTile + r] = on ? a.delta[at + r] : 0.f;
+      }
+      mbar_arrive(c.full(st));
+    }
+    if (!ok && lane == 0) give_up(c, a.status);
+  } else if (warp == kMmaWarp) {
+    bool ok = n == 0 || mbar_wait(c.own(), 0, c.abort_flag);
+    auto arrived = [&](int i) {                              // tile i of q and do is in shared memory, its tail cleared
+      if (!__all_sync(0xffffffffu, mbar_wait(c.full(i % kStages), (i / kStages) & 1u, c.abort_flag))) return false;
+      const int valid = sq.lq - (lo + (i % per_head) * kTile);
+      if (valid < kTile) {
+        clear_rows<DP>(ring + (i % kStages) * 2 * TB, valid);
+        clear_rows<DP>(ring + (i % kStages) * 2 * TB + TB, valid);
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      tc_fence_after();
+      return true;
+    };
+    ok = __all_sync(0xffffffffu, ok) && (n == 0 || arrived(0));
+    if (ok && n > 0 && lane == 0) {
+      issue_nt<DP>(t_s, k_tile, ring);
+      umma_commit(c.s());
+      issue_nt<DP>(t_dp, v_tile, ring + TB);
+      umma_commit(c.dp());
+    }
+    for (int i = 0; i < n && ok; ++i) {
+      const uint32_t qt = ring + (i % kStages) * 2 * TB, dot = qt + TB;
+      const uint32_t nq = ring + ((i + 1) % kStages) * 2 * TB, ndo = nq + TB;
+      ok = __all_sync(0xffffffffu, mbar_wait(c.p(), i & 1u, c.abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      if (lane == 0) issue_ts<DP>(t_dv, t_s, dot, i > 0);
+      if (i + 1 < n) {
+        ok = arrived(i + 1);
+        if (!ok) break;
+        if (lane == 0) {
+          issue_nt<DP>(t_s, k_tile, nq);
+          umma_commit(c.s());
+        }
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      if (lane == 0) {
+        issue_ts<DP>(t_dk, t_dp, qt, i > 0);
+        umma_commit(c.empty(i % kStages));
+        if (i + 1 < n) {
+          issue_nt<DP>(t_dp, v_tile, ndo);
+          umma_commit(c.dp());
+        } else {
+          umma_commit(c.acc());
+        }
+      }
+    }
+    if (!ok && lane == 0) give_up(c, a.status);
+  } else if (warp < kLoadWarp) {
+    // ---------------- elements: one key per thread, half of the tile's rows per group ----------------
+    const int half = warp >> 2, key = (warp & 3) * 32 + lane, j = j0 + key;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = t_s + lanes + half * 64, dp_addr = t_dp + lanes + half * 64;
+    bool ok = true;
+    for (int i = 0; i < n && ok; ++i) {
+      const int head = kvh * a.group + i / per_head, i0 = lo + (i % per_head) * kTile + half * 64;
+      const Score<CAP, BIAS> score(a, head);
+      const float* lse2 = rows_smem + (i % kStages) * (2 * kTile) + half * 64;
+      const float* delta = lse2 + kTile;
+      const int pos0 = sq.shift + i0;
+      // the tile's rows behind the last see nothing
+      const bool whole = i0 + 64 <= sq.lq && all_seen(sq, a.causal, a.window, pos0, pos0 + 63, j0, j0 + kTile);
+      ok = __all_sync(0xffffffffu, mbar_wait(c.full(i % kStages), (i / kStages) & 1u, c.abort_flag) &&
+                                       mbar_wait(c.s(), i & 1u, c.abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      float pr[64];
+      tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
+      tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
+      tmem_ld_wait();
+#pragma unroll
+      for (int c0 = 0; c0 < 2; ++c0) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int x = 0; x < 32; x += 4) {
+          const float4 ls = *reinterpret_cast<const float4*>(lse2 + c0 * 32 + x);
+          const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = c0 * 32 + x + e;
+            float cs = 1.f;
+            v[e] = score.prob(pr[r], lv[e], pos0 + r - j, cs);
+            if (!whole) {
+              const RowKeys k = row_keys(sq, a.causal, a.window, pos0 + r);
+              if (i0 + r >= sq.lq || !k.sees(j)) v[e] = 0.f;
+            }
+            pr[r] = CAP ? (v[e] == 0.f ? 0.f : v[e] * cs) : v[e];
+          }
+          pk[x / 2] = pack2(v[0], v[1]);
+          pk[x / 2 + 1] = pack2(v[2], v[3]);
+        }
+        tmem_st16(s_addr + c0 * 16, pk);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(c.p());
+      ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), i & 1u, c.abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int c0 = 0; c0 < 2; ++c0) {
+        float dp[32];
+        tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+        tmem_ld_wait();
+        uint32_t pk[16];
+#pragma unroll
+        for (int x = 0; x < 32; x += 4) {
+          const float4 dl = *reinterpret_cast<const float4*>(delta + c0 * 32 + x);
+          const float dv[4] = {dl.x, dl.y, dl.z, dl.w};
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float pv = pr[c0 * 32 + x + e];
+            v[e] = pv * (dp[x + e] - dv[e]);
+            if (!whole && pv == 0.f) v[e] = 0.f;             // rows behind the last may hold anything
+          }
+          pk[x / 2] = pack2(v[0], v[1]);
+          pk[x / 2 + 1] = pack2(v[2], v[3]);
+        }
+        tmem_st16(dp_addr + c0 * 16, pk);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(c.ds());
+    }
+    if (ok && n > 0) {
+      ok = __all_sync(0xffffffffu, mbar_wait(c.acc(), 0, c.abort_flag));
+      tc_fence_after();
+    }
+    if (ok) {
+      const bool mine = key < keys;
+      const size_t row = (size_t)(sq.k0 + (mine ? j : 0));
+      if (half == 0)
+        store_row<DP>(t_dv + lanes, n > 0, 1.f, mine,
+                      reinterpret_cast<bf16*>(a.dv) + row * a.v_stride + (size_t)kvh * a.head_dim, a.head_dim);
+      else
+        store_row<DP>(t_dk + lanes, n > 0, a.scale, mine,
+                      reinterpret_cast<bf16*>(a.dk) + row * a.k_stride + (size_t)kvh * a.head_dim, a.head_dim);
+    } else if (lane == 0) {
+      give_up(c, a.status);
+    }
+  }
+  block_end(c, tmem);
+}
+
+// dq of 128 rows of a head.  TMEM: two S tiles in turn (ds is written over the one it comes from), dP, dq.  The next S
+// runs while the element groups work on this one, and the next dP as soon as this one has been read.
+template <int DP, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_constant__ BwdParams p) {
+  constexpr uint32_t TB = kTileBytes<DP>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t q_tile = smem_u32(smem), do_tile = q_tile + TB, ring = q_tile + 2 * TB;
+  uint8_t* ctl = smem + (2 + 2 * kStages) * TB + kStages * kRowBytes;
+  uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * kBars);
+  const Ctl c{smem_u32(ctl), reinterpret_cast<volatile int*>(slot + 1)};
+  const AttnArgs& a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int head = blockIdx.x % a.q_heads;
+  int seq, index;
+  if (!block_begin(a.q_off, a.n_seqs, a.q_rows, blockIdx.x / a.q_heads, true, 1, c, slot, &seq, &index)) return;
+  const uint32_t tmem = *slot;
+  const uint32_t t_dp = tmem + 2 * kTile, t_dq = tmem + 3 * kTile;
+  const AttnSeq sq = load_seq(a, seq);
+  const int i0 = index * kTile, rows = min(kTile, sq.lq - i0);
+  const int p0 = sq.shift + i0, p1 = p0 + rows - 1;
+  const KeyTiles<kTile> tiles = key_tiles<kTile>(sq, a.causal, a.window, p0, p1);
+  const int n = tiles.count();
+
+  if (warp == kLoadWarp) {
+    if (lane == 0) {
+      const int kvh = head / a.group;
+      bool ok = true;
+      if (n > 0) {
+        mbar_expect_tx(c.own(), 2 * TB);
+        load_tile<DP>(q_tile, &p.q_map, c.own(), head, sq.q0 + i0);
+        load_tile<DP>(do_tile, &p.do_map, c.own(), head, sq.q0 + i0);
+      }
+      for (int i = 0; i < n; ++i) {
+        const int st = i % kStages;
+        if (!mbar_wait(c.empty(st), ((i / kStages) & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
+        mbar_expect_tx(c.full(st), 2 * TB);
+        load_tile<DP>(ring + st * 2 * TB, &p.k_map, c.full(st), kvh, sq.k0 + tiles.at(i) * kTile);
+        load_tile<DP>(ring + st * 2 * TB + TB, &p.v_map, c.full(st), kvh, sq.k0 + tiles.at(i) * kTile);
+      }
+      if (!ok) give_up(c, a.status);
+    }
+  } else if (warp == kMmaWarp) {
+    bool ok = n == 0 || mbar_wait(c.own(), 0, c.abort_flag);
+    auto arrived = [&](int i) {
+      if (!__all_sync(0xffffffffu, mbar_wait(c.full(i % kStages), (i / kStages) & 1u, c.abort_flag))) return false;
+      const int valid = sq.lk - tiles.at(i) * kTile;
+      if (valid < kTile) {
+        clear_rows<DP>(ring + (i % kStages) * 2 * TB, valid);
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      tc_fence_after();
+      return true;
+    };
+    ok = __all_sync(0xffffffffu, ok) && (n == 0 || arrived(0));
+    if (ok && n > 0 && lane == 0) {
+      issue_nt<DP>(tmem, q_tile, ring);
+      umma_commit(c.s());
+      issue_nt<DP>(t_dp, do_tile, ring + TB);
+      umma_commit(c.dp());
+    }
+    for (int i = 0; i < n && ok; ++i) {
+      const uint32_t kt = ring + (i % kStages) * 2 * TB;
+      const uint32_t nk = ring + ((i + 1) % kStages) * 2 * TB;
+      if (i + 1 < n) {
+        ok = arrived(i + 1);
+        if (!ok) break;
+        if (lane == 0) {                                     // over ds of two tiles ago, which its product has read
+          issue_nt<DP>(tmem + ((i + 1) & 1) * kTile, q_tile, nk);
+          umma_commit(c.s() + 8u * ((i + 1) & 1));
+        }
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      if (lane == 0) {
+        if (i + 1 < n) {
+          issue_nt<DP>(t_dp, do_tile, nk + TB);
+          umma_commit(c.dp());
+        }
+        issue_ts<DP>(t_dq, tmem + (i & 1) * kTile, kt, i > 0);
+        umma_commit(c.empty(i % kStages));
+        if (i + 1 == n) umma_commit(c.acc());
+      }
+    }
+    if (!ok && lane == 0) give_up(c, a.status);
+  } else if (warp < kLoadWarp) {
+    // ---------------- elements: one row per thread, half of the tile's keys per group ----------------
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t dp_addr = t_dp + lanes + half * 64;
+    const bool mine = row < rows;
+    const int pos = p0 + row;
+    const size_t at = (size_t)head * a.q_rows + sq.q0 + i0 + (mine ? row : 0);
+    const float lse2 = mine ? a.lse2[at] : INFINITY, delta = mine ? a.delta[at] : 0.f;
+    const Score<CAP, BIAS> score(a, head);
+    const RowKeys keys = row_keys(sq, a.causal, a.window, pos);
+    bool ok = true;
+    for (int i = 0; i < n && ok; ++i) {
+      const int j0 = tiles.at(i) * kTile + half * 64;
+      const bool whole = all_seen(sq, a.causal, a.window, p0, p1, j0, j0 + 64);
+      const uint32_t s_addr = tmem + (i & 1) * kTile + lanes + half * 64;
+      ok = __all_sync(0xffffffffu, mbar_wait(c.s() + 8u * (i & 1), (i >> 1) & 1u, c.abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      float pr[64];
+      tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
+      tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
+      tmem_ld_wait();
+#pragma unroll
+      for (int x = 0; x < 64; ++x) {
+        float cs = 1.f;
+        float v = score.prob(pr[x], lse2, pos - j0 - x, cs);
+        if (CAP) v *= cs;
+        pr[x] = v;
+      }
+      if (!whole) {
+        const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
+#pragma unroll
+        for (int x = 0; x < 64; ++x)
+          if (!((x >= lo && x < hi) || x < pre)) pr[x] = 0.f;
+      }
+      ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), i & 1u, c.abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+#pragma unroll
+      for (int c0 = 0; c0 < 2; ++c0) {
+        float dp[32];
+        tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+        tmem_ld_wait();
+        uint32_t pk[16];
+#pragma unroll
+        for (int x = 0; x < 32; x += 2) {
+          float v[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float pv = pr[c0 * 32 + x + e];
+            v[e] = pv * (dp[x + e] - delta);
+            if (!whole && pv == 0.f) v[e] = 0.f;             // keys behind the last may hold anything
+          }
+          pk[x / 2] = pack2(v[0], v[1]);
+        }
+        tmem_st16(s_addr + c0 * 16, pk);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(c.ds());
+    }
+    if (ok && n > 0) {
+      ok = __all_sync(0xffffffffu, mbar_wait(c.acc(), 0, c.abort_flag));
+      tc_fence_after();
+    }
+    if (ok) {
+      if (half == 0)
+        store_row<DP>(t_dq + lanes, n > 0, a.scale, mine,
+                      reinterpret_cast<bf16*>(a.dq) + (size_t)(sq.q0 + i0 + (mine ? row : 0)) * a.q_stride +
+                          (size_t)head * a.head_dim, a.head_dim);
+    } else if (lane == 0) {
+      give_up(c, a.status);
+    }
+  }
+  block_end(c, tmem);
+}
+
+// delta = sum over the head of o * d_o, and the log-sum-exp in base 2 (+inf, i.e. p = 0, for rows that see nothing):
+// 16 lanes per (row, head), heads fastest so that a warp reads neighbouring memory.
+template <typename T>
+__global__ void __launch_bounds__(256) attn_delta_kernel(AttnArgs a, float* lse2, float* delta) {
+  const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4;
+  const int l = threadIdx.x & 15;
+  const long long total = (long long)a.q_rows * a.q_heads;
+  const bool on = item < total;
+  const long long row = on ? item / a.q_heads : 0;
+  const int head = on ? (int)(item - row * a.q_heads) : 0;
+  const T* o = reinterpret_cast<const T*>(a.o) + row * a.o_stride + (size_t)head * a.head_dim;
+  const T* d = reinterpret_cast<const T*>(a.d_o) + row * a.o_stride + (size_t)head * a.head_dim;
+  constexpr int V = 16 / sizeof(T);
+  float sum = 0.f;
+  if (on)
+    for (int c = l * V; c < a.head_dim; c += 16 * V) {
+      const uint4 x = *reinterpret_cast<const uint4*>(o + c), y = *reinterpret_cast<const uint4*>(d + c);
+      const T* xe = reinterpret_cast<const T*>(&x);
+      const T* ye = reinterpret_cast<const T*>(&y);
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum += (float)xe[e] * (float)ye[e];
+    }
+#pragma unroll
+  for (int f = 8; f >= 1; f >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, f);
+  if (on && l == 0) {
+    const size_t at = (size_t)head * a.q_rows + row;
+    const float z = a.lse[at];
+    delta[at] = sum;
+    lse2[at] = z == -INFINITY ? INFINITY : z * kLog2e;
+  }
+}
+
+template <int DP, bool CAP, bool BIAS>
+cudaError_t launch(const BwdParams& p, unsigned grid_kv, unsigned grid_q, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(attn_bwd_kv_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kSmemBytes<DP>);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(attn_bwd_q_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<DP>);
+  if (e != cudaSuccess) return e;
+  if (grid_kv) {
+    attn_bwd_kv_kernel<DP, CAP, BIAS><<<grid_kv, kThreads, kSmemBytes<DP>, st>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  if (grid_q) attn_bwd_q_kernel<DP, CAP, BIAS><<<grid_q, kThreads, kSmemBytes<DP>, st>>>(p);
+  return cudaGetLastError();
+}
+template <int DP>
+cudaError_t launch_dp(const BwdParams& p, unsigned gk, unsigned gq, cudaStream_t st) {
+  if (p.a.softcap > 0.f) return p.a.slopes ? launch<DP, true, true>(p, gk, gq, st) : launch<DP, true, false>(p, gk, gq, st);
+  return p.a.slopes ? launch<DP, false, true>(p, gk, gq, st) : launch<DP, false, false>(p, gk, gq, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_delta(const AttnArgs& a, bool bf16_mode, float* lse2, float* delta, cudaStream_t st) {
+  const long long blocks = ((long long)a.q_rows * a.q_heads + 15) / 16;
+  if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
+  if (blocks == 0) return cudaSuccess;
+  if (bf16_mode) attn_delta_kernel<bf16><<<(unsigned)blocks, 256, 0, st>>>(a, lse2, delta);
+  else attn_delta_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(a, lse2, delta);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t st) {
+  BwdParams p;
+  memset(&p, 0, sizeof(p));
+  p.a = a;
+  const long long qr = a.q_rows > 0 ? a.q_rows : 1, kr = a.k_rows > 0 ? a.k_rows : 1;   // without rows no tile is loaded
+  if (!tc_encode_heads(&p.q_map, a.q, qr, a.q_heads, a.head_dim, a.q_stride, kTile) ||
+      !tc_encode_heads(&p.do_map, a.d_o, qr, a.q_heads, a.head_dim, a.o_stride, kTile) ||
+      !tc_encode_heads(&p.k_map, a.k, kr, a.kv_heads, a.head_dim, a.k_stride, kTile) ||
+      !tc_encode_heads(&p.v_map, a.v, kr, a.kv_heads, a.head_dim, a.v_stride, kTile))
+    return cudaErrorInvalidValue;
+  const long long gk = a.k_rows ? ((long long)(a.k_rows + kTile - 1) / kTile + a.n_seqs) * a.kv_heads : 0;
+  const long long gq = a.q_rows ? ((long long)(a.q_rows + kTile - 1) / kTile + a.n_seqs) * a.q_heads : 0;
+  if (gk > 0x7fffffffLL || gq > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return a.head_dim <= 64 ? launch_dp<64>(p, (unsigned)gk, (unsigned)gq, st) : launch_dp<128>(p, (unsigned)gk, (unsigned)gq, st);
+}
+
+}  // namespace mixlora

@@ -1,0 +1,490 @@
+// Masked attention for few query rows of each sequence (a decoding step): bound by reading the keys and values once.
+//
+// The rows of a sequence that share a key head (its query heads times the sequence's new tokens) are the
+// 16 rows of one m16n8k16 product, so that every key and value is read once for all of them (more rows go to several
+// blocks, which find the keys in L2).  The keys of a (sequence,
+// key head) are split over several blocks where there are few of those; each leaves (m, l, sum p v) and a second
+// launch joins them in index order.
+#include "attention.cuh"
+
+namespace mixlora {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kStep = 16;                        // keys per step of a warp
+constexpr int kStages = 3;
+
+struct FewParams {
+  AttnArgs a;
+  float* part;                                   // [seq, key head, chunk, split, 16 rows, head_dim + 2]: sum p v, m (base 2), l
+  int splits, rows, chunks;                      // rows = group * max_q_len, in chunks of kFewRows
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// 16 bytes to shared memory; zeros where `on` is false (nothing is read then)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool on) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  const __nv_bfloat162 e = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&e);
+}
+
+// The block's (sequence, key head, split), and the key groups of kStep keys it works on.
+struct Share {
+  AttnSeq sq;
+  int seq, kvh, split, lq;
+  int row0, rows;                                // the block's chunk of the rows
+  KeyTiles<kStep> tiles;
+  int t0, t1;
+};
+__device__ __forceinline__ Share block_share(const FewParams& p) {
+  const AttnArgs& a = p.a;
+  Share w;
+  w.split = blockIdx.x % p.splits;
+  int rest = blockIdx.x / p.splits;
+  w.row0 = rest % p.chunks * kFewRows;
+  w.rows = min(kFewRows, p.rows - w.row0);
+  rest /= p.chunks;
+  w.kvh = rest % a.kv_heads;
+  w.seq = rest / a.kv_heads;
+  w.sq = load_seq(a, w.seq);
+  w.lq = min(w.sq.lq, a.max_q_len);
+  w.t0 = w.t1 = 0;
+  w.tiles = KeyTiles<kStep>{0, 0, 0};
+  if (w.lq > 0) {
+    w.tiles = key_tiles<kStep>(w.sq, a.causal, a.window, w.sq.shift, w.sq.shift + w.lq - 1);
+    const long long n = w.tiles.count();
+    w.t0 = (int)(n * w.split / p.splits);
+    w.t1 = (int)(n * (w.split + 1) / p.splits);
+  }
+  return w;
+}
+
+template <bool CAP, bool BIAS>
+struct ScoreMap {
+  float mul, cap2, scale2;
+  __device__ __forceinline__ explicit ScoreMap(const AttnArgs& a)
+      : mul(CAP ? a.scale / a.softcap : a.scale * kLog2e), cap2(a.softcap * kLog2e), scale2(0.f) {}
+  // score in base 2; `slope2` in base 2 too
+  __device__ __forceinline__ float operator()(float s, float slope2, int distance) const {
+    float x = s * mul;
+    if (CAP) x = cap2 * tanh_fast(x);
+    if (BIAS) x -= slope2 * fabsf((float)distance);
+    return x;
+  }
+};
+
+// Joins the warps' states of a block in warp order and writes the block's result: the rows themselves, or a partial.
+// `st_m`, `st_l` [kWarps][16], `st_o` [kWarps][16][DP] in shared memory.
+template <typename T>
+__device__ __forceinline__ void finish_block(const FewParams& p, const Share& w, const float* st_m, const float* st_l,
+                                             const float* st_o, int dp) {
+  const AttnArgs& a = p.a;
+  const int d = a.head_dim;
+  for (int i = threadIdx.x; i < w.rows * d; i += kWarps * 32) {
+    const int r = i / d, c = i - r * d;
+    const int qi = (w.row0 + r) / a.group, head = w.kvh * a.group + (w.row0 + r - qi * a.group);
+    if (qi >= w.lq) continue;
+    float m = -INFINITY;
+    for (int x = 0; x < kWarps; ++x) m = fmaxf(m, st_m[x * 16 + r]);
+    float l = 0.f, o = 0.f;
+    for (int x = 0; x < kWarps; ++x) {
+      const float f = st_m[x * 16 + r] == -INFINITY ? 0.f : exp2f(st_m[x * 16 + r] - m);
+      l += f * st_l[x * 16 + r];
+      o += f * st_o[(x * 16 + r) * dp + c];
+    }
+    if (p.splits > 1) {
+      const size_t block = (((size_t)w.seq * a.kv_heads + w.kvh) * p.chunks + w.row0 / kFewRows) * p.splits + w.split;
+      float* dst = p.part + (block * kFewRows + r) * (d + 2);
+      dst[c] = o;
+      if (c == 0) { dst[d] = m; dst[d + 1] = l; }
+    } else {
+      const size_t row = (size_t)(w.sq.q0 + qi);
+      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+      T* out = reinterpret_cast<T*>(a.out) + row * a.o_stride + (size_t)head * d + c;
+      if constexpr (sizeof(T) == 2) *out = __float2bfloat16(o * inv);
+      else *out = o * inv;
+      if (c == 0 && a.lse) a.lse[(size_t)head * a.q_rows + row] = (m + log2f(l)) * kLn2;
+    }
+  }
+}
+
+// bf16.  A warp takes every kWarps-th group of 16 keys; K and V of the next groups travel through its own ring of
+// kStages stages in shared memory (16-byte pieces, XORed with the key so that the 8 rows of an ldmatrix fall into
+// different banks).  Keys behind the last one are never read: their rows are filled with zeros.
+template <int DP, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams p) {
+  constexpr int C = DP / 8;                      // 16-byte pieces of a row
+  constexpr int kStageBytes = 2 * kStep * DP * 2;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const AttnArgs& a = p.a;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+  const Share w = block_share(p);
+  const int d = a.head_dim;
+  const uint32_t ring = smem_addr(smem) + warp * kStages * kStageBytes;
+  const bf16* kp = reinterpret_cast<const bf16*>(a.k) + (size_t)w.kvh * d;
+  const bf16* vp = reinterpret_cast<const bf16*>(a.v) + (size_t)w.kvh * d;
+
+  const int first = w.t0 + warp, n = first < w.t1 ? (w.t1 - first + kWarps - 1) / kWarps : 0;
+  auto load = [&](int i) {
+    if (i < n) {
+      const int j0 = w.tiles.at(first + i * kWarps) * kStep;
+      const uint32_t dst = ring + (i % kStages) * kStageBytes;
+#pragma unroll
+      for (int x = 0; x < kStep * C / 32; ++x) {
+        const int idx = x * 32 + lane, r = idx / C, c = idx % C;
+        const bool on = j0 + r < w.sq.lk && c * 8 < d;
+        const size_t row = (size_t)(w.sq.k0 + (on ? j0 + r : 0));
+        const int at = on ? c * 8 : 0;
+        const uint32_t off = (uint32_t)(r * DP * 2 + ((c ^ (r & 7)) << 4));
+        copy16(dst + off, kp + row * a.k_stride + at, on);
+        copy16(dst + kStep * DP * 2 + off, vp + row * a.v_stride + at, on);
+      }
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) load(i);
+
+  // the queries' fragments, straight from memory: rows r = qi * group + head, zeros behind the last
+  uint32_t qf[DP / 16][4];
+  RowKeys keys[2];
+  float slope2[2] = {0.f, 0.f};
+  int pos[2];
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    const int r = w.row0 + g + 8 * hf, qi = r / a.group, hd = w.kvh * a.group + (r - qi * a.group);
+    const bool on = g + 8 * hf < w.rows && qi < w.lq;
+    pos[hf] = w.sq.shift + qi;
+    keys[hf] = on ? row_keys(w.sq, a.causal, a.window, pos[hf]) : RowKeys{0, 0, 0};
+    if (BIAS && on) slope2[hf] = a.slopes[hd] * kLog2e;
+    const bf16* src = reinterpret_cast<const bf16*>(a.q) + (size_t)(w.sq.q0 + (on ? qi : 0)) * a.q_stride + (size_t)hd * d;
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int c = k * 16 + u * 8 + 2 * t;
+        qf[k][hf + 2 * u] = on && c < d ? *reinterpret_cast<const uint32_t*>(src + c) : 0u;
+      }
+  }
+
+  const ScoreMap<CAP, BIAS> score(a);
+  float o[DP / 8][4];
+#pragma unroll
+  for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  for (int i = 0; i < n; ++i) {
+    load(i + kStages - 1);
+    copy_wait<kStages - 1>();
+    __syncwarp();
+    const uint32_t kb = ring + (i % kStages) * kStageBytes, vb = kb + kStep * DP * 2;
+    float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    {
+      // matrices of an ldmatrix: keys 0-7 | 0-7 | 8-15 | 8-15, values 0-7 | 8-15 | 0-7 | 8-15 of the step
+      const int r = (lane & 7) + ((lane >> 4) << 3), hi = (lane >> 3) & 1;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        uint32_t b[4];
+        ldsm4(kb + r * DP * 2 + (((2 * k + hi) ^ (r & 7)) << 4), b);
+        mma16816(s[0], qf[k], b[0], b[1]);
+        mma16816(s[1], qf[k], b[2], b[3]);
+      }
+    }
+    const int j0 = w.tiles.at(first + i * kWarps) * kStep;
+    float mt[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int j = j0 + (x >> 1) * 8 + 2 * t + (x & 1);
+        float& v = s[x >> 1][2 * hf + (x & 1)];
+        v = score(v, slope2[hf], pos[hf] - j);
+        if (!keys[hf].sees(j)) v = -INFINITY;
+        mt[hf] = fmaxf(mt[hf], v);
+      }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      mt[hf] = fmaxf(mt[hf], __shfl_xor_sync(0xffffffffu, mt[hf], 1));
+      mt[hf] = fmaxf(mt[hf], __shfl_xor_sync(0xffffffffu, mt[hf], 2));
+    }
+    // as in the tiled kernel, a row's maximum moves only where it has grown by more than 2^8
+    const bool grown = (mt[0] > m[0] && mt[0] - m[0] > 8.f) || (mt[1] > m[1] && mt[1] - m[1] > 8.f);
+    if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const float mn = fmaxf(m[hf], mt[hf]);
+        const float f = m[hf] == -INFINITY ? 0.f : exp2f(m[hf] - mn);
+        m[hf] = mn;
+        l[hf] *= f;
+#pragma unroll
+        for (int x = 0; x < DP / 8; ++x) { o[x][2 * hf] *= f; o[x][2 * hf + 1] *= f; }
+      }
+    }
+    uint32_t pf[4];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const float base = m[hf] == -INFINITY ? 0.f : m[hf];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float e0 = exp2f(s[u][2 * hf] - base), e1 = exp2f(s[u][2 * hf + 1] - base);
+        l[hf] += e0 + e1;
+        pf[hf + 2 * u] = pack2(e0, e1);
+      }
+    }
+    {
+      // matrices: keys 0-7 | 8-15 | 0-7 | 8-15, values of two neighbouring 8-value pieces
+      const int r = lane & 15, hi = lane >> 4;
+#pragma unroll
+      for (int x = 0; x < DP / 16; ++x) {
+        uint32_t b[4];
+        ldsm4t(vb + r * DP * 2 + (((2 * x + hi) ^ (r & 7)) << 4), b);
+        mma16816(o[2 * x], pf, b[0], b[1]);
+        mma16816(o[2 * x + 1], pf, b[2], b[3]);
+      }
+    }
+    __syncwarp();                                // the stage may be filled again
+  }
+  copy_wait<0>();
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 1);
+    l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 2);
+  }
+  __syncthreads();                               // the rings become the block's exchange
+  float* st_m = reinterpret_cast<float*>(smem);
+  float* st_l = st_m + kWarps * 16;
+  float* st_o = st_l + kWarps * 16;
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf) {
+    const int r = g + 8 * hf;
+    if (t == 0) { st_m[warp * 16 + r] = m[hf]; st_l[warp * 16 + r] = l[hf]; }
+#pragma unroll
+    for (int x = 0; x < DP / 8; ++x)
+      *reinterpret_cast<float2*>(st_o + (warp * 16 + r) * DP + x * 8 + 2 * t) = make_float2(o[x][2 * hf], o[x][2 * hf + 1]);
+  }
+  __syncthreads();
+  finish_block<bf16>(p, w, st_m, st_l, st_o, DP);
+}
+
+// fp32.  LPK lanes hold a key (4 values each); a warp takes 32 / LPK keys at a time, kKeys steps in flight.
+template <int LPK, int ROWS, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kWarps * 32) attn_few_f32_kernel(FewParams p) {
+  constexpr int SUB = 32 / LPK, kKeys = kStep / SUB, DP = LPK * 4;
+  constexpr int kBatch = kKeys < 4 ? kKeys : 4;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const AttnArgs& a = p.a;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int sub = lane / LPK, c = (lane % LPK) * 4;
+  const Share w = block_share(p);
+  const int d = a.head_dim;
+  const bool on_c = c < d;
+  const float* kp = reinterpret_cast<const float*>(a.k) + (size_t)w.kvh * d + (on_c ? c : 0);
+  const float* vp = reinterpret_cast<const float*>(a.v) + (size_t)w.kvh * d + (on_c ? c : 0);
+  const ScoreMap<CAP, BIAS> score(a);
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+
+  float4 q[ROWS], o[ROWS];
+  float m[ROWS], l[ROWS], slope2[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int qi = (w.row0 + r) / a.group, hd = w.kvh * a.group + (w.row0 + r - qi * a.group);
+    const bool on = r < w.rows && qi < w.lq;
+    q[r] = on && on_c ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) +
+                                                          (size_t)(w.sq.q0 + qi) * a.q_stride + (size_t)hd * d + c)
+                      : zero;
+    slope2[r] = BIAS && on ? a.slopes[hd] * kLog2e : 0.f;
+    o[r] = zero;
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+  }
+  for (int tt = w.t0 + warp; tt < w.t1; tt += kWarps) {
+    const int j0 = w.tiles.at(tt) * kStep;
+#pragma unroll
+    for (int b = 0; b < kKeys; b += kBatch) {
+      float4 k[kBatch], v[kBatch];
+#pragma unroll
+      for (int x = 0; x < kBatch; ++x) {
+        const int j = j0 + (b + x) * SUB + sub;
+        const bool on = on_c && j < w.sq.lk;
+        const size_t row = (size_t)(w.sq.k0 + (on ? j : 0));
+        k[x] = on ? *reinterpret_cast<const float4*>(kp + row * a.k_stride) : zero;
+        v[x] = on ? *reinterpret_cast<const float4*>(vp + row * a.v_stride) : zero;
+      }
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const int qi = (w.row0 + r) / a.group;
+        const bool live = r < w.rows && qi < w.lq;
+        const int pos = w.sq.shift + qi;
+        const RowKeys keys = row_keys(w.sq, a.causal, a.window, pos);
+        float s[kBatch], mt = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x)
+          s[x] = q[r].x * k[x].x + q[r].y * k[x].y + q[r].z * k[x].z + q[r].w * k[x].w;
+#pragma unroll
+        for (int f = LPK / 2; f >= 1; f >>= 1)
+#pragma unroll
+          for (int x = 0; x < kBatch; ++x) s[x] += __shfl_xor_sync(0xffffffffu, s[x], f);
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x) {
+          const int j = j0 + (b + x) * SUB + sub;
+          s[x] = live && keys.sees(j) ? score(s[x], slope2[r], pos - j) : -INFINITY;
+          mt = fmaxf(mt, s[x]);
+        }
+        if (mt > m[r]) {                         // the lanes of a key agree
+          const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mt);
+          m[r] = mt;
+          l[r] *= f;
+          o[r].x *= f; o[r].y *= f; o[r].z *= f; o[r].w *= f;
+        }
+        const float base = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+        for (int x = 0; x < kBatch; ++x) {
+          const float e = exp2f(s[x] - base);
+          l[r] += e;
+          o[r].x += e * v[x].x; o[r].y += e * v[x].y; o[r].z += e * v[x].z; o[r].w += e * v[x].w;
+        }
+      }
+    }
+  }
+  float* st_m = reinterpret_cast<float*>(smem);
+  float* st_l = st_m + kWarps * 16;
+  float* st_o = st_l + kWarps * 16;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (SUB == 2) {                              // the warp's two key streams
+      const float mo = __shfl_xor_sync(0xffffffffu, m[r], 16), mn = fmaxf(m[r], mo);
+      const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mn);
+      l[r] *= f;
+      o[r].x *= f; o[r].y *= f; o[r].z *= f; o[r].w *= f;
+      m[r] = mn;
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 16);
+      o[r].x += __shfl_xor_sync(0xffffffffu, o[r].x, 16);
+      o[r].y += __shfl_xor_sync(0xffffffffu, o[r].y, 16);
+      o[r].z += __shfl_xor_sync(0xffffffffu, o[r].z, 16);
+      o[r].w += __shfl_xor_sync(0xffffffffu, o[r].w, 16);
+    }
+    if (lane == 0) { st_m[warp * 16 + r] = m[r]; st_l[warp * 16 + r] = l[r]; }
+    if (sub == 0) *reinterpret_cast<float4*>(st_o + (warp * 16 + r) * DP + c) = o[r];
+  }
+  __syncthreads();
+  finish_block<float>(p, w, st_m, st_l, st_o, DP);
+}
+
+// Joins the splits of a row in index order; one warp per (sequence, query, head).
+template <typename T>
+__global__ void __launch_bounds__(128) attn_few_join_kernel(FewParams p) {
+  const AttnArgs& a = p.a;
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int seq = item / (p.rows * a.kv_heads);
+  if (seq >= a.n_seqs) return;
+  const int rest = item - seq * p.rows * a.kv_heads, kvh = rest / p.rows, r = rest - kvh * p.rows;
+  const int qi = r / a.group, head = kvh * a.group + (r - qi * a.group), d = a.head_dim;
+  const int q0 = clamp_int(a.q_off[seq], 0, a.q_rows);
+  if (qi >= min(seq_rows(a.q_off, seq, a.q_rows), a.max_q_len)) return;
+  const size_t pitch = (size_t)kFewRows * (d + 2);
+  const float* src = p.part + (((size_t)seq * a.kv_heads + kvh) * p.chunks + r / kFewRows) * p.splits * pitch +
+                     (size_t)(r % kFewRows) * (d + 2);
+  float m = -INFINITY;
+  for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, src[s * pitch + d]);
+#pragma unroll
+  for (int f = 16; f >= 1; f >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, f));
+  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < p.splits; ++s) {
+    const float ms = src[s * pitch + d];
+    const float f = ms == -INFINITY ? 0.f : exp2f(ms - m);
+    l += f * src[s * pitch + d + 1];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (lane + 32 * x < d) o[x] += f * src[s * pitch + lane + 32 * x];
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  T* out = reinterpret_cast<T*>(a.out) + (size_t)(q0 + qi) * a.o_stride + (size_t)head * d;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    if (lane + 32 * x < d) {
+      if constexpr (sizeof(T) == 2) out[lane + 32 * x] = __float2bfloat16(o[x] * inv);
+      else out[lane + 32 * x] = o[x] * inv;
+    }
+  if (lane == 0 && a.lse) a.lse[(size_t)head * a.q_rows + q0 + qi] = (m + log2f(l)) * kLn2;
+}
+
+constexpr size_t exchange_bytes(int dp) { return (size_t)kWarps * 16 * (dp + 2) * 4; }
+
+template <int DP, bool CAP, bool BIAS>
+cudaError_t launch_bf16(const FewParams& p, unsigned grid, cudaStream_t st) {
+  constexpr size_t ring = (size_t)kWarps * kStages * 2 * kStep * DP * 2;
+  constexpr size_t smem = ring > exchange_bytes(DP) ? ring : exchange_bytes(DP);
+  cudaError_t e = cudaFuncSetAttribute(attn_few_bf16_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  attn_few_bf16_kernel<DP, CAP, BIAS><<<grid, kWarps * 32, smem, st>>>(p);
+  return cudaGetLastError();
+}
+template <int LPK, int ROWS, bool CAP, bool BIAS>
+cudaError_t launch_f32(const FewParams& p, unsigned grid, cudaStream_t st) {
+  attn_few_f32_kernel<LPK, ROWS, CAP, BIAS><<<grid, kWarps * 32, exchange_bytes(LPK * 4), st>>>(p);
+  return cudaGetLastError();
+}
+template <bool CAP, bool BIAS>
+cudaError_t launch_mode(const FewParams& p, bool bf16_mode, unsigned grid, cudaStream_t st) {
+  const bool narrow = p.a.head_dim <= 64;
+  if (bf16_mode) return narrow ? launch_bf16<64, CAP, BIAS>(p, grid, st) : launch_bf16<128, CAP, BIAS>(p, grid, st);
+  // the rows are registers: as few as hold them
+  if (p.rows <= 1) return narrow ? launch_f32<16, 1, CAP, BIAS>(p, grid, st) : launch_f32<32, 1, CAP, BIAS>(p, grid, st);
+  if (p.rows <= 4) return narrow ? launch_f32<16, 4, CAP, BIAS>(p, grid, st) : launch_f32<32, 4, CAP, BIAS>(p, grid, st);
+  if (p.rows <= 8) return narrow ? launch_f32<16, 8, CAP, BIAS>(p, grid, st) : launch_f32<32, 8, CAP, BIAS>(p, grid, st);
+  return narrow ? launch_f32<16, 16, CAP, BIAS>(p, grid, st) : launch_f32<32, 16, CAP, BIAS>(p, grid, st);
+}
+
+}  // namespace
+
+// Splits of a (sequence, key head): enough blocks for about four rounds of the 2 x 148 that run together (lengths
+// differ, and short pieces even that out), but no piece under 256 keys, and none for the longest length alone.
+int attn_few_splits(int n_seqs, int kv_heads, int rows, long long k_rows, int max_k_len) {
+  const long long pairs = (long long)n_seqs * kv_heads * ((rows + kFewRows - 1) / kFewRows);
+  if (pairs <= 0) return 1;
+  long long longest = max_k_len > 0 ? max_k_len : (k_rows + n_seqs - 1) / n_seqs;
+  if (longest > k_rows) longest = k_rows;
+  long long s = (4 * 2 * 148 + pairs - 1) / pairs;
+  const long long cap = (longest + 255) / 256;
+  if (s > cap) s = cap;
+  if (s > 256) s = 256;
+  return s < 1 ? 1 : (int)s;
+}
+
+cudaError_t launch_attn_few(const AttnArgs& a, bool bf16_mode, int splits, float* part, cudaStream_t st) {
+  const int rows = a.group * a.max_q_len;
+  FewParams p{a, part, splits, rows, (rows + kFewRows - 1) / kFewRows};
+  const long long blocks = (long long)a.n_seqs * a.kv_heads * p.chunks * splits;
+  if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
+  const unsigned grid = (unsigned)blocks;
+  cudaError_t e;
+  if (a.softcap > 0.f) e = a.slopes ? launch_mode<true, true>(p, bf16_mode, grid, st) : launch_mode<true, false>(p, bf16_mode, grid, st);
+  else e = a.slopes ? launch_mode<false, true>(p, bf16_mode, grid, st) : launch_mode<false, false>(p, bf16_mode, grid, st);
+  if (e != cudaSuccess || splits <= 1) return e;
+  const long long items = (long long)a.n_seqs * a.kv_heads * p.rows;
+  const unsigned jg = (unsigned)((items + 3) / 4);
+  if (bf16_mode) attn_few_join_kernel<bf16><<<jg, 128, 0, st>>>(p);
+  else attn_few_join_kernel<float><<<jg, 128, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace mixlora

@@ -1,0 +1,373 @@
+// Masked attention, forward, bf16, on the tensor cores.
+//
+//   s_ij = scale q_i . k_j          capped: s <- c tanh(s / c)          lowered with distance: s <- s - a_h |p_i - p_j|
+//   o_i  = sum_j e^(s_ij - m_i) v_j / l_i,   l_i = sum_j e^(s_ij - m_i),   m_i = a running maximum,   lse_i = m_i + ln l_i
+//
+// over the keys that row i sees.
+#include <cuda.h>
+#include <string.h>
+
+#include "attention.cuh"
+#include "tc_ptx.cuh"
+
+namespace mixlora {
+namespace {
+using namespace tc;
+
+constexpr int kTile = 128;                       // keys per step, and query rows per half of a block's rows
+constexpr int kThreads = 384;                    // two softmax groups of 4 warps; a group with the load and MMA warps
+// A block starts with 168 registers a thread (384 x 168 = 64512); the softmax groups, whose threads hold a row of
+// scores each, take 208 and the third group keeps 88: (2 x 208 + 88) x 128 = 64512.
+constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kTmemCols = 512;
+template <int DP> constexpr int kStages = DP == 128 ? 5 : 8;
+template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
+template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 1024 + 256;
+
+struct FwdParams {
+  AttnArgs a;
+  CUtensorMap q_map, k_map, v_map;
+};
+
+// One block: 256 query rows of a head (two halves of 128, one softmax group each, one row per thread) against the
+// sequence's key tiles.  The load warp streams K and V tiles through a ring; the MMA warp issues, half by half,
+// O += P V and then the next S = Q K^T, so that one half's products run while the other half's group computes its
+// exponentials.  S [128 x 128] sits in TMEM; the group writes P over it as bf16, from where the product reads it: P
+// never touches shared memory.  P is rounded to bf16 (the tensor cores' operand type); the row sums l are taken from
+// the unrounded values in fp32.  The running maximum is only moved (and O rescaled) when a row's maximum grows by more
+// than 2^8: until then e^(s - m) <= 2^8, far from overflow, and the factor cancels in O / l.
+template <int DP, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams p) {
+  constexpr int NS = kStages<DP>;
+  constexpr uint32_t TB = kTileBytes<DP>;
+  constexpr int NB = DP / 64;                    // 64-value blocks of a head in a tile
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  const uint32_t q_base = smem_u32(smem), ring = q_base + 2 * TB;
+  uint8_t* ctl = smem + (2 + NS) * TB;
+  const uint32_t bars = smem_u32(ctl);
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (NS + s); };
+  auto q_bar = [&](int h) { return bars + 8u * (2 * NS + h); };
+  auto s_bar = [&](int h) { return bars + 8u * (2 * NS + 2 + h); };
+  auto p_bar = [&](int h) { return bars + 8u * (2 * NS + 4 + h); };
+  auto o_bar = [&](int h) { return bars + 8u * (2 * NS + 6 + h); };
+  uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * NS + 8));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(slot + 1);
+  volatile int* found = reinterpret_cast<volatile int*>(slot + 2);       // {sequence, tile} or {-1, .}
+
+  const AttnArgs& a = p.a;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int head = blockIdx.x % a.q_heads;
+
+  if (warp == 0) {
+    int b = -1, tile = 0;
+    if (!find_tile(a.q_off, a.n_seqs, a.q_rows, 2 * kTile, blockIdx.x / a.q_heads, &b, &tile)) b = -1;
+    if (lane == 0) { found[0] = b; found[1] = tile; }
+  }
+  if (threadIdx.x == 32) {
+    for (int s = 0; s < NS; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int h = 0; h < 2; ++h) { mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(p_bar(h), 4); mbar_init(o_bar(h), 1); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kLoadWarp && lane == 0) { prefetch_tmap(&p.q_map); prefetch_tmap(&p.k_map); prefetch_tmap(&p.v_map); }
+  __syncthreads();
+  if (found[0] < 0) return;                      // the grid is an upper bound of the tiles there are
+  if (warp == kMmaWarp) {
+    tmem_alloc(smem_u32(slot), kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *slot;
+  const AttnSeq sq = load_seq(a, found[0]);
+  const int r0 = found[1] * 2 * kTile;           // first row of the block in its sequence
+  const int rows = min(2 * kTile, sq.lq - r0);
+  const KeyTiles<kTile> tiles = key_tiles<kTile>(sq, a.causal, a.window, sq.shift + r0, sq.shift + r0 + rows - 1);
+  const int n = tiles.count();
+  // the key tiles that a half needs, among the block's
+  auto half_tiles = [&](int h) {
+    const int hr = min(kTile, rows - h * kTile);
+    if (hr <= 0) return KeyTiles<kTile>{0, 0, 0};
+    const int p0 = sq.shift + r0 + h * kTile;
+    return key_tiles<kTile>(sq, a.causal, a.window, p0, p0 + hr - 1);
+  };
+
+  if (warp >= kLoadWarp) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  if (warp == kLoadWarp) {
+    if (lane == 0) {
+      const int kvh = head / a.group;
+      bool ok = true;
+      for (int h = 0; h < 2; ++h) {
+        if (rows <= h * kTile) break;
+        mbar_expect_tx(q_bar(h), TB);
+        for (int j = 0; j < NB; ++j)
+          tma_load_3d(q_base + h * TB + j * (kTile * 128), &p.q_map, q_bar(h), j * 64, head, sq.q0 + r0 + h * kTile);
+      }
+      for (int i = 0; i < 2 * n && ok; ++i) {    // K and V of a tile in turn
+        const int st = i % NS;
+        if (!mbar_wait(empty_bar(st), ((i / NS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        mbar_expect_tx(full_bar(st), TB);
+        const CUtensorMap* map = (i & 1) ? &p.v_map : &p.k_map;
+        for (int j = 0; j < NB; ++j)
+          tma_load_3d(ring + st * TB + j * (kTile * 128), map, full_bar(st), j * 64, kvh,
+                      sq.k0 + tiles.at(i >> 1) * kTile);
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    const KeyTiles<kTile> need[2] = {half_tiles(0), half_tiles(1)};
+    const uint32_t idesc_s = make_idesc(kTile, 0, 0), idesc_o = make_idesc(DP, 0, 1);
+    int done[2] = {0, 0};
+    bool ok = true;
+    auto wait_slot = [&](int i) { return mbar_wait(full_bar(i % NS), (i / NS) & 1u, abort_flag); };
+    auto issue_s = [&](int h, int it) {
+      const uint32_t kb = ring + ((2 * it) % NS) * TB, qb = q_base + h * TB;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k) {
+        const uint32_t off = (k >> 2) * (kTile * 128) + (k & 3) * 32;
+        umma_bf16(tmem + h * kTile, make_desc_kmajor_rows(qb + off, 128), make_desc_kmajor_rows(kb + off, 128), idesc_s,
+                  k != 0);
+      }
+      umma_commit(s_bar(h));
+    };
+    if (n > 0) ok = wait_slot(0);
+    tc_fence_after();
+    for (int h = 0; h < 2 && ok && n > 0; ++h) {
+      if (need[h].count() == 0) continue;
+      ok = mbar_wait(q_bar(h), 0, abort_flag);
+      tc_fence_after();
+      if (ok && lane == 0 && need[h].has(tiles.at(0))) issue_s(h, 0);
+    }
+    if (ok && n > 0 && lane == 0) umma_commit(empty_bar(0));
+    for (int it = 0; it < n && ok; ++it) {
+      const int vi = 2 * it + 1;
+      if (it + 1 < n) ok = wait_slot(2 * it + 2);
+      ok = ok && wait_slot(vi);
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      const int j0 = tiles.at(it) * kTile;
+      const uint32_t vb = ring + (vi % NS) * TB;
+      if (j0 + kTile > sq.lk) {
+        // rows behind the last key belong to someone else and may hold anything; P is zero there, V has to be finite
+        const int first = sq.lk - j0;
+        for (int i = lane; i < (kTile - first) * 8 * NB; i += 32) {
+          const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
+          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + blk * (kTile * 128) + r * 128 + c * 16), "r"(0)
+                       : "memory");
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      tc_fence_after();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (need[h].has(tiles.at(it))) {
+          ok = mbar_wait(p_bar(h), done[h] & 1u, abort_flag);
+          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+          tc_fence_after();
+          if (lane == 0) {
+#pragma unroll
+            for (int k = 0; k < kTile / 16; ++k)
+              umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + k * 8,
+                           make_desc(vb + k * 2048, kTile * 128, 1024), idesc_o, (done[h] | k) != 0);
+            if (done[h] + 1 == need[h].count()) umma_commit(o_bar(h));
+          }
+          ++done[h];
+        }
+        if (lane == 0) {
+          if (h == 1) umma_commit(empty_bar(vi % NS));
+          if (it + 1 < n) {
+            if (need[h].has(tiles.at(it + 1))) issue_s(h, it + 1);
+            if (h == 1) umma_commit(empty_bar((vi + 1) % NS));
+          }
+        }
+      }
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+    }
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ---------------- softmax: one row per thread ----------------
+    const int h = warp >> 2;
+    const int row = h * kTile + (warp & 3) * 32 + lane;      // in the block
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lanes + h * kTile, o_addr = tmem + lanes + 2 * kTile + h * DP;
+    const KeyTiles<kTile> need = half_tiles(h);
+    const int total = need.count();
+    const int half_rows = clamp_int(rows - h * kTile, 0, kTile);
+    const int p0 = sq.shift + r0 + h * kTile, p1 = p0 + half_rows - 1;
+    const int pos = sq.shift + r0 + row;
+    const RowKeys keys = row_keys(sq, a.causal, a.window, pos);
+    // scores in base 2: exp2 of them is e^s
+    const float mul = CAP ? a.scale / a.softcap : a.scale * kLog2e;
+    const float cap2 = a.softcap * kLog2e;
+    const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
+    constexpr bool kTransformed = CAP || BIAS;               // else the factor goes into the exponent's multiply-add
+    const float to2 = kTransformed ? 1.f : mul;
+    float m = -INFINITY, l = 0.f;                            // m in the scores' units
+    bool ok = true;
+    int cnt = 0;
+    for (int it = 0; it < n && ok; ++it) {
+      const int t = tiles.at(it);
+      if (!need.has(t)) continue;
+      ok = __all_sync(0xffffffffu, mbar_wait(s_bar(h), cnt & 1u, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      float s[kTile];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+      tmem_ld_wait();
+      const int j0 = t * kTile;
+      if (kTransformed) {
+#pragma unroll
+        for (int j = 0; j < kTile; ++j) {
+          float x = s[j] * mul;
+          if (CAP) x = cap2 * tanh_fast(x);
+          if (BIAS) x -= slope2 * fabsf((float)(pos - j0 - j));
+          s[j] = x;
+        }
+      }
+      if (!all_seen(sq, a.causal, a.window, p0, p1, j0, j0 + kTile)) {
+        const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
+#pragma unroll
+        for (int j = 0; j < kTile; ++j)
+          if (!((j >= lo && j < hi) || j < pre)) s[j] = -INFINITY;
+      }
+      float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+      for (int j = 4; j < kTile; ++j) mx[j & 3] = fmaxf(mx[j & 3], s[j]);
+      const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+      // moved where it has grown by more than 2^8 (always at a row's first visible key)
+      const bool grown = mt > m && (mt - m) * to2 > 8.f;
+      if (__any_sync(0xffffffffu, grown)) {
+        const float m_new = fmaxf(m, mt);
+        const float f = m == -INFINITY ? 0.f : exp2f((m - m_new) * to2);
+        m = m_new;
+        l *= f;
+        if (cnt > 0) {                                       // the product before this tile's S has finished
+#pragma unroll
+          for (int c = 0; c < DP / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(o_addr + c * 32, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st32(o_addr + c * 32, o);
+          }
+        }
+      }
+      const float shift = m == -INFINITY ? 0.f : -m * to2;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = c * 32 + 2 * i;
+          const float e0 = exp2f(fmaf(s[j], to2, shift)), e1 = exp2f(fmaf(s[j + 1], to2, shift));
+          sum[i & 3] += e0 + e1;
+          const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
+          pk[i] = *reinterpret_cast<const uint32_t*>(&e);
+        }
+        tmem_st16(s_addr + c * 16, pk);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_bar(h));
+      ++cnt;
+    }
+    if (ok && total > 0) {
+      ok = __all_sync(0xffffffffu, mbar_wait(o_bar(h), 0, abort_flag));
+      tc_fence_after();
+    }
+    if (ok) {
+      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // a row that sees nothing gives zeros
+      const bool mine = row < rows;
+      bf16* dst = reinterpret_cast<bf16*>(a.out) + (size_t)(sq.q0 + r0 + (mine ? row : 0)) * a.o_stride +
+                  (size_t)head * a.head_dim;
+#pragma unroll
+      for (int c = 0; c < DP / 32; ++c) {
+        uint32_t o[32];
+        if (total > 0) {
+          tmem_ld32(o_addr + c * 32, o);
+          tmem_ld_wait();
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          if (mine && c * 32 + g * 8 < a.head_dim) {
+            uint4 w;
+            uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
+              const float y = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
+              const __nv_bfloat162 e = __floats2bfloat162_rn(x, y);
+              wp[i] = *reinterpret_cast<const uint32_t*>(&e);
+            }
+            *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = w;
+          }
+        }
+      }
+      if (a.lse && mine)
+        a.lse[(size_t)head * a.q_rows + sq.q0 + r0 + row] = (m * to2 + log2f(l)) * kLn2;
+    } else if (lane == 0) {
+      *abort_flag = 1;
+      if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    for (int i = 0; i < 200; ++i) __nanosleep(5000);         // let copies that may still be in flight land
+  }
+  tc_fence_after();
+  if (warp == kMmaWarp) {
+    __syncwarp();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+template <int DP, bool CAP, bool BIAS>
+cudaError_t launch(const FwdParams& p, unsigned grid, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(attn_fwd_tc_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kSmemBytes<DP>);
+  if (e != cudaSuccess) return e;
+  attn_fwd_tc_kernel<DP, CAP, BIAS><<<grid, kThreads, kSmemBytes<DP>, st>>>(p);
+  return cudaGetLastError();
+}
+
+template <int DP>
+cudaError_t launch_dp(const FwdParams& p, unsigned grid, cudaStream_t st) {
+  if (p.a.softcap > 0.f) return p.a.slopes ? launch<DP, true, true>(p, grid, st) : launch<DP, true, false>(p, grid, st);
+  return p.a.slopes ? launch<DP, false, true>(p, grid, st) : launch<DP, false, false>(p, grid, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t st) {
+  FwdParams p;
+  memset(&p, 0, sizeof(p));
+  p.a = a;
+  const long long kr = a.k_rows > 0 ? a.k_rows : 1;          // without keys no tile is loaded
+  if (!tc_encode_heads(&p.q_map, a.q, a.q_rows, a.q_heads, a.head_dim, a.q_stride, kTile) ||
+      !tc_encode_heads(&p.k_map, a.k, kr, a.kv_heads, a.head_dim, a.k_stride, kTile) ||
+      !tc_encode_heads(&p.v_map, a.v, kr, a.kv_heads, a.head_dim, a.v_stride, kTile))
+    return cudaErrorInvalidValue;
+  const long long grid = ((long long)(a.q_rows + 2 * kTile - 1) / (2 * kTile) + a.n_seqs) * a.q_heads;
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return a.head_dim <= 64 ? launch_dp<64>(p, (unsigned)grid, st) : launch_dp<128>(p, (unsigned)grid, st);
+}
+
+}  // namespace mixlora

@@ -733,6 +733,19 @@ bool tc_encode_2d(CUtensorMap* map, const void* ptr, long long rows, long long c
   return encode_2d(map, ptr, rows, cols, ld, box_rows, box_cols, swizzle_bytes);
 }
 
+bool tc_encode_heads(CUtensorMap* map, const void* ptr, long long rows, int heads, int head_dim, long long stride,
+                     int box_rows) {
+  EncodeFn fn = get_encode();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
+  cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)stride * 2};
+  cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool tc_gemm_supported(int M, const TcOut* outs, int nout) {
   if (M <= 0 || nout <= 0 || nout > kMaxOut) return false;
   const int nseg = outs[0].nseg;
