@@ -135,10 +135,45 @@ __device__ __forceinline__ void query_rows(const AttnSeq& s, int causal, int win
   }
 }
 
+// 2^x in one special-function operation (within 2^-22 of the value; below 2^-126 it gives zero)
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two fp32 values to an instruction
+__device__ __forceinline__ uint64_t pair2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair2(uint64_t p, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  const __nv_bfloat162 e = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&e);
+}
+
 // tanh from two special-function operations: 1 - 2 / (1 + e^(2x)).  Its absolute error, a few 2^-24, is what counts
 // for a score (the relative one of a small x is bounded by the cap times that).
 __device__ __forceinline__ float tanh_fast(float x) {
-  return 1.f - __fdividef(2.f, 1.f + exp2f(x * (2.f * kLog2e)));
+  return 1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kLog2e)));
 }
 
 cudaError_t launch_attn_forward_tc(const AttnArgs& p, cudaStream_t st);

@@ -25,7 +25,7 @@ constexpr int kLoadWarp = 8, kMmaWarp = 9;
 constexpr int kTmemCols = 512;
 constexpr int kStages = 2;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
-constexpr uint32_t kRowBytes = 2 * kTile * 4;    // lse and delta of a query tile
+constexpr uint32_t kRowBytes = 2 * kTile * 4;    // minus lse and minus delta of a query tile
 template <int DP> constexpr uint32_t kSmemBytes = (2 + 2 * kStages) * kTileBytes<DP> + kStages * kRowBytes + 1024 + 256;
 
 struct BwdParams {
@@ -81,10 +81,6 @@ __device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint32_t b, boo
   for (int k = 0; k < kTile / 16; ++k)
     umma_bf16_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, make_desc(b + k * 2048, kTile * 128, 1024), idesc, accumulate || k != 0);
 }
-__device__ __forceinline__ uint32_t pack2(float x, float y) {
-  const __nv_bfloat162 e = __floats2bfloat162_rn(x, y);
-  return *reinterpret_cast<const uint32_t*>(&e);
-}
 template <int DP>
 __device__ __forceinline__ void store_row(uint32_t acc, bool any, float mul, bool mine, bf16* dst, int head_dim) {
 #pragma unroll
@@ -102,7 +98,7 @@ __device__ __forceinline__ void store_row(uint32_t acc, bool any, float mul, boo
           uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            wp[i] = pack2(__uint_as_float(v[g * 8 + 2 * i]) * mul, __uint_as_float(v[g * 8 + 2 * i + 1]) * mul);
+            wp[i] = bf16x2(__uint_as_float(v[g * 8 + 2 * i]) * mul, __uint_as_float(v[g * 8 + 2 * i + 1]) * mul);
         }
         *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = w;
       }
@@ -160,22 +156,33 @@ __device__ __forceinline__ void block_end(const Ctl& c, uint32_t tmem) {
   }
 }
 
-// Scores of half a tile in base 2 less the row's log-sum-exp, and the slope of the cap
+// p of two neighbouring scores: 2^(score - log-sum-exp), in base 2; with a cap also its slope.  `neg_lse` is minus the
+// log-sum-exp, `d0`, `d1` are the distances.
 template <bool CAP, bool BIAS>
 struct Score {
   float mul, cap2, slope2;
   __device__ __forceinline__ Score(const AttnArgs& a, int head)
       : mul(CAP ? a.scale / a.softcap : a.scale * kLog2e), cap2(a.softcap * kLog2e),
         slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
-  __device__ __forceinline__ float prob(float s, float lse2, int distance, float& cap_slope) const {
-    float x = s * mul;
+  __device__ __forceinline__ void probs(float s0, float s1, uint64_t neg_lse, int d0, int d1, float& p0, float& p1,
+                                        uint64_t& cap_slope) const {
+    uint64_t x;
     if (CAP) {
-      const float t = tanh_fast(x);
-      cap_slope = 1.f - t * t;
-      x = cap2 * t;
+      const float t0 = tanh_fast(s0 * mul), t1 = tanh_fast(s1 * mul);
+      const uint64_t t = pair2(t0, t1);
+      cap_slope = fma2(pair2(-t0, -t1), t, pair2(1.f, 1.f));
+      x = fma2(t, pair2(cap2, cap2), neg_lse);
+    } else {
+      x = fma2(pair2(s0, s1), pair2(mul, mul), neg_lse);
     }
-    if (BIAS) x -= slope2 * fabsf((float)distance);
-    return exp2f(x - lse2);
+    float x0, x1;
+    unpair2(x, x0, x1);
+    if (BIAS) {
+      x0 = fmaf(-slope2, fabsf((float)d0), x0);
+      x1 = fmaf(-slope2, fabsf((float)d1), x1);
+    }
+    p0 = ex2(x0);
+    p1 = ex2(x1);
   }
 };
 
@@ -231,8 +238,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
       for (int x = 0; x < kTile / 32; ++x) {
         const int r = x * 32 + lane;
         const bool on = i0 + r < sq.lq;
-        dst[r] = on ? a.lse2[at + r] : INFINITY;
-        dst[kTile + r] = on ? a.delta[at + r] : 0.f;
+        dst[r] = on ? -a.lse2[at + r] : -INFINITY;
+        dst[kTile + r] = on ? -a.delta[at + r] : 0.f;
       }
       mbar_arrive(c.full(st));
     }
@@ -297,8 +304,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
     for (int i = 0; i < n && ok; ++i) {
       const int head = kvh * a.group + i / per_head, i0 = lo + (i % per_head) * kTile + half * 64;
       const Score<CAP, BIAS> score(a, head);
-      const float* lse2 = rows_smem + (i % kStages) * (2 * kTile) + half * 64;
-      const float* delta = lse2 + kTile;
+      const float* neg_lse = rows_smem + (i % kStages) * (2 * kTile) + half * 64;
+      const float* neg_delta = neg_lse + kTile;
       const int pos0 = sq.shift + i0;
       // the tile's rows behind the last see nothing
       const bool whole = i0 + 64 <= sq.lq && all_seen(sq, a.causal, a.window, pos0, pos0 + 63, j0, j0 + kTile);
@@ -310,28 +317,29 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
       tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
       tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
       tmem_ld_wait();
+      uint64_t cs[CAP ? 32 : 1];
+#pragma unroll
+      for (int x = 0; x < 64; x += 4) {
+        const float4 ls = *reinterpret_cast<const float4*>(neg_lse + x);
+        score.probs(pr[x], pr[x + 1], pair2(ls.x, ls.y), pos0 + x - j, pos0 + x + 1 - j, pr[x], pr[x + 1], cs[CAP ? x / 2 : 0]);
+        score.probs(pr[x + 2], pr[x + 3], pair2(ls.z, ls.w), pos0 + x + 2 - j, pos0 + x + 3 - j, pr[x + 2], pr[x + 3],
+                    cs[CAP ? x / 2 + 1 : 0]);
+      }
+      if (!whole) {
+        // rows that see this key: [r_lo, r_hi), or all where the key lies before the prefix
+        int r_lo = 0, r_hi = 0;
+        if (j < sq.lk) query_rows(sq, a.causal, a.window, j, j + 1, &r_lo, &r_hi);
+        r_lo -= i0;
+        r_hi -= i0;
+#pragma unroll
+        for (int x = 0; x < 64; ++x)
+          if (x < r_lo || x >= r_hi) pr[x] = 0.f;
+      }
 #pragma unroll
       for (int c0 = 0; c0 < 2; ++c0) {
         uint32_t pk[16];
 #pragma unroll
-        for (int x = 0; x < 32; x += 4) {
-          const float4 ls = *reinterpret_cast<const float4*>(lse2 + c0 * 32 + x);
-          const float lv[4] = {ls.x, ls.y, ls.z, ls.w};
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = c0 * 32 + x + e;
-            float cs = 1.f;
-            v[e] = score.prob(pr[r], lv[e], pos0 + r - j, cs);
-            if (!whole) {
-              const RowKeys k = row_keys(sq, a.causal, a.window, pos0 + r);
-              if (i0 + r >= sq.lq || !k.sees(j)) v[e] = 0.f;
-            }
-            pr[r] = CAP ? (v[e] == 0.f ? 0.f : v[e] * cs) : v[e];
-          }
-          pk[x / 2] = pack2(v[0], v[1]);
-          pk[x / 2 + 1] = pack2(v[2], v[3]);
-        }
+        for (int x = 0; x < 16; ++x) pk[x] = bf16x2(pr[c0 * 32 + 2 * x], pr[c0 * 32 + 2 * x + 1]);
         tmem_st16(s_addr + c0 * 16, pk);
       }
       tmem_st_wait();
@@ -346,20 +354,34 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
         float dp[32];
         tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
         tmem_ld_wait();
+        if (!whole) {                                        // rows behind the last may hold anything
+#pragma unroll
+          for (int x = 0; x < 32; ++x)
+            if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+        }
         uint32_t pk[16];
 #pragma unroll
         for (int x = 0; x < 32; x += 4) {
-          const float4 dl = *reinterpret_cast<const float4*>(delta + c0 * 32 + x);
-          const float dv[4] = {dl.x, dl.y, dl.z, dl.w};
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float pv = pr[c0 * 32 + x + e];
-            v[e] = pv * (dp[x + e] - dv[e]);
-            if (!whole && pv == 0.f) v[e] = 0.f;             // rows behind the last may hold anything
+          const float4 dl = *reinterpret_cast<const float4*>(neg_delta + c0 * 32 + x);
+          const float* pv = pr + c0 * 32 + x;
+          uint64_t u = add2(pair2(dp[x], dp[x + 1]), pair2(dl.x, dl.y)), w = add2(pair2(dp[x + 2], dp[x + 3]), pair2(dl.z, dl.w));
+          u = mul2(u, pair2(pv[0], pv[1]));
+          w = mul2(w, pair2(pv[2], pv[3]));
+          if (CAP) {
+            u = mul2(u, cs[c0 * 16 + x / 2]);
+            w = mul2(w, cs[c0 * 16 + x / 2 + 1]);
           }
-          pk[x / 2] = pack2(v[0], v[1]);
-          pk[x / 2 + 1] = pack2(v[2], v[3]);
+          float f0, f1, f2, f3;
+          unpair2(u, f0, f1);
+          unpair2(w, f2, f3);
+          if (CAP && !whole) {                               // the slope of a score that came from anything
+            f0 = pv[0] == 0.f ? 0.f : f0;
+            f1 = pv[1] == 0.f ? 0.f : f1;
+            f2 = pv[2] == 0.f ? 0.f : f2;
+            f3 = pv[3] == 0.f ? 0.f : f3;
+          }
+          pk[x / 2] = bf16x2(f0, f1);
+          pk[x / 2 + 1] = bf16x2(f2, f3);
         }
         tmem_st16(dp_addr + c0 * 16, pk);
       }
@@ -483,7 +505,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
     const bool mine = row < rows;
     const int pos = p0 + row;
     const size_t at = (size_t)head * a.q_rows + sq.q0 + i0 + (mine ? row : 0);
-    const float lse2 = mine ? a.lse2[at] : INFINITY, delta = mine ? a.delta[at] : 0.f;
+    const float nl = mine ? -a.lse2[at] : -INFINITY, nd = mine ? -a.delta[at] : 0.f;
+    const uint64_t neg_lse = pair2(nl, nl), neg_delta = pair2(nd, nd);
     const Score<CAP, BIAS> score(a, head);
     const RowKeys keys = row_keys(sq, a.causal, a.window, pos);
     bool ok = true;
@@ -499,11 +522,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
       tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
       tmem_ld_wait();
 #pragma unroll
-      for (int x = 0; x < 64; ++x) {
-        float cs = 1.f;
-        float v = score.prob(pr[x], lse2, pos - j0 - x, cs);
-        if (CAP) v *= cs;
-        pr[x] = v;
+      for (int x = 0; x < 64; x += 2) {
+        uint64_t cs;
+        score.probs(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
+        if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
       }
       if (!whole) {
         const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
@@ -519,17 +541,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
         float dp[32];
         tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
         tmem_ld_wait();
+        if (!whole) {                                        // keys behind the last may hold anything
+#pragma unroll
+          for (int x = 0; x < 32; ++x)
+            if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+        }
         uint32_t pk[16];
 #pragma unroll
         for (int x = 0; x < 32; x += 2) {
-          float v[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float pv = pr[c0 * 32 + x + e];
-            v[e] = pv * (dp[x + e] - delta);
-            if (!whole && pv == 0.f) v[e] = 0.f;             // keys behind the last may hold anything
-          }
-          pk[x / 2] = pack2(v[0], v[1]);
+          float f0, f1;
+          unpair2(mul2(add2(pair2(dp[x], dp[x + 1]), neg_delta), pair2(pr[c0 * 32 + x], pr[c0 * 32 + x + 1])), f0, f1);
+          pk[x / 2] = bf16x2(f0, f1);
         }
         tmem_st16(s_addr + c0 * 16, pk);
       }

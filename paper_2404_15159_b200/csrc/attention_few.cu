@@ -40,11 +40,6 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack2(float x, float y) {
-  const __nv_bfloat162 e = __floats2bfloat162_rn(x, y);
-  return *reinterpret_cast<const uint32_t*>(&e);
-}
-
 // The block's (sequence, key head, split), and the key groups of kStep keys it works on.
 struct Share {
   AttnSeq sq;
@@ -105,7 +100,7 @@ __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w,
     for (int x = 0; x < kWarps; ++x) m = fmaxf(m, st_m[x * 16 + r]);
     float l = 0.f, o = 0.f;
     for (int x = 0; x < kWarps; ++x) {
-      const float f = st_m[x * 16 + r] == -INFINITY ? 0.f : exp2f(st_m[x * 16 + r] - m);
+      const float f = st_m[x * 16 + r] == -INFINITY ? 0.f : ex2(st_m[x * 16 + r] - m);
       l += f * st_l[x * 16 + r];
       o += f * st_o[(x * 16 + r) * dp + c];
     }
@@ -231,7 +226,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         const float mn = fmaxf(m[hf], mt[hf]);
-        const float f = m[hf] == -INFINITY ? 0.f : exp2f(m[hf] - mn);
+        const float f = m[hf] == -INFINITY ? 0.f : ex2(m[hf] - mn);
         m[hf] = mn;
         l[hf] *= f;
 #pragma unroll
@@ -244,9 +239,9 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
       const float base = m[hf] == -INFINITY ? 0.f : m[hf];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const float e0 = exp2f(s[u][2 * hf] - base), e1 = exp2f(s[u][2 * hf + 1] - base);
+        const float e0 = ex2(s[u][2 * hf] - base), e1 = ex2(s[u][2 * hf + 1] - base);
         l[hf] += e0 + e1;
-        pf[hf + 2 * u] = pack2(e0, e1);
+        pf[hf + 2 * u] = bf16x2(e0, e1);
       }
     }
     {

@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       const bool grown = mt > m && (mt - m) * to2 > 8.f;
       if (__any_sync(0xffffffffu, grown)) {
         const float m_new = fmaxf(m, mt);
-        const float f = m == -INFINITY ? 0.f : exp2f((m - m_new) * to2);
+        const float f = m == -INFINITY ? 0.f : ex2((m - m_new) * to2);
         m = m_new;
         l *= f;
         if (cnt > 0) {                                       // the product before this tile's S has finished
@@ -266,21 +266,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         }
       }
       const float shift = m == -INFINITY ? 0.f : -m * to2;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
+      uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t pk[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = c * 32 + 2 * i;
-          const float e0 = exp2f(fmaf(s[j], to2, shift)), e1 = exp2f(fmaf(s[j + 1], to2, shift));
-          sum[i & 3] += e0 + e1;
-          const __nv_bfloat162 e = __floats2bfloat162_rn(e0, e1);
-          pk[i] = *reinterpret_cast<const uint32_t*>(&e);
+          const uint64_t x = pair2(s[j], s[j + 1]);
+          float e0, e1;
+          unpair2(kTransformed ? add2(x, shift_2) : fma2(x, mul_2, shift_2), e0, e1);
+          e0 = ex2(e0);
+          e1 = ex2(e1);
+          sum[i & 1] = add2(sum[i & 1], pair2(e0, e1));
+          pk[i] = bf16x2(e0, e1);
         }
         tmem_st16(s_addr + c * 16, pk);
       }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      float l0, l1;
+      unpair2(add2(sum[0], sum[1]), l0, l1);
+      l += l0 + l1;
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -312,8 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             for (int i = 0; i < 4; ++i) {
               const float x = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
               const float y = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
-              const __nv_bfloat162 e = __floats2bfloat162_rn(x, y);
-              wp[i] = *reinterpret_cast<const uint32_t*>(&e);
+              wp[i] = bf16x2(x, y);
             }
             *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = w;
           }
