@@ -67,19 +67,21 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int first) {
 template <int DP>
 __device__ __forceinline__ void issue_nt(uint32_t d, uint32_t a, uint32_t b) {
   const uint32_t idesc = make_idesc(kTile, 0, 0);
+  const uint64_t ad = make_desc_kmajor_rows(a, 128), bd = make_desc_kmajor_rows(b, 128);
 #pragma unroll
   for (int k = 0; k < DP / 16; ++k) {
-    const uint32_t off = (k >> 2) * (kTile * 128) + (k & 3) * 32;
-    umma_bf16(d, make_desc_kmajor_rows(a + off, 128), make_desc_kmajor_rows(b + off, 128), idesc, k != 0);
+    const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;          // the address field counts 16 bytes
+    umma_bf16(d, ad + off, bd + off, idesc, k != 0);
   }
 }
 // D[128 x DP] += A B, A bf16 [128 x 128] in TMEM (columns 0-31 and 64-95 of its region), B rows = the summed index
 template <int DP>
 __device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint32_t b, bool accumulate) {
   const uint32_t idesc = make_idesc(DP, 0, 1);
+  const uint64_t bd = make_desc(b, kTile * 128, 1024);
 #pragma unroll
   for (int k = 0; k < kTile / 16; ++k)
-    umma_bf16_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, make_desc(b + k * 2048, kTile * 128, 1024), idesc, accumulate || k != 0);
+    umma_bf16_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, bd + k * (2048 >> 4), idesc, accumulate || k != 0);
 }
 template <int DP>
 __device__ __forceinline__ void store_row(uint32_t acc, bool any, float mul, bool mine, bf16* dst, int head_dim) {

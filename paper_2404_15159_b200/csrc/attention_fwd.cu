@@ -15,36 +15,37 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 128;                       // keys per step, and query rows per half of a block's rows
-constexpr int kThreads = 384;                    // two softmax groups of 4 warps; a group with the load and MMA warps
-// A block starts with 168 registers a thread (384 x 168 = 64512); the softmax groups, whose threads hold a row of
-// scores each, take 208 and the third group keeps 88: (2 x 208 + 88) x 128 = 64512.
-constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 640;                    // four softmax groups of 4 warps; a group with the load and MMA warps
+// A block starts with 96 registers a thread (640 x 96 = 61440); the softmax groups, whose threads hold half a row of
+// scores each, take 112 and the fifth group keeps 32: (4 x 112 + 32) x 128 = 61440.
+constexpr int kLoadWarp = 16, kMmaWarp = 17;
 constexpr int kTmemCols = 512;
 template <int DP> constexpr int kStages = DP == 128 ? 5 : 8;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
-template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 1024 + 256;
+template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 2 * 2 * kTile * 4 + 256;
 
 struct FwdParams {
   AttnArgs a;
   CUtensorMap q_map, k_map, v_map;
 };
 
-// One block: 256 query rows of a head (two halves of 128, one softmax group each, one row per thread) against the
-// sequence's key tiles.  The load warp streams K and V tiles through a ring; the MMA warp issues, half by half,
-// O += P V and then the next S = Q K^T, so that one half's products run while the other half's group computes its
-// exponentials.  S [128 x 128] sits in TMEM; the group writes P over it as bf16, from where the product reads it: P
-// never touches shared memory.  P is rounded to bf16 (the tensor cores' operand type); the row sums l are taken from
-// the unrounded values in fp32.  The running maximum is only moved (and O rescaled) when a row's maximum grows by more
-// than 2^8: until then e^(s - m) <= 2^8, far from overflow, and the factor cancels in O / l.
+// One block: 256 query rows of a head (two halves of 128) against the sequence's key tiles.  The load warp streams K and
+// V tiles through a ring; the MMA warp issues, half by half, O += P V and then the next S = Q K^T, so that one half's
+// products run while the other half's exponentials are computed.  S [128 x 128] sits in TMEM; eight warps take its
+// rows, 64 keys of a row to a thread (two warps to a scheduler and half: one alone is held up by its own latencies),
+// and write P over it as bf16, from where the product reads it: P never touches shared memory.  P is rounded to bf16
+// (the tensor cores' operand type); the row sums l are taken from the unrounded values in fp32.  The running maximum is
+// only moved (and O rescaled) when a row's maximum grows by more than 2^8: until then e^(s - m) <= 2^8, far from
+// overflow, and the factor cancels in O / l.  m is a whole number in base 2, so that a move rescales O and l exactly.
 template <int DP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams p) {
   constexpr int NS = kStages<DP>;
   constexpr uint32_t TB = kTileBytes<DP>;
   constexpr int NB = DP / 64;                    // 64-value blocks of a head in a tile
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle counts from 1024-byte boundaries
   const uint32_t q_base = smem_u32(smem), ring = q_base + 2 * TB;
-  uint8_t* ctl = smem + (2 + NS) * TB;
+  float* exchange = reinterpret_cast<float*>(smem + (2 + NS) * TB);      // [2 column halves][256 rows]
+  uint8_t* ctl = reinterpret_cast<uint8_t*>(exchange + 2 * 2 * kTile);
   const uint32_t bars = smem_u32(ctl);
   auto full_bar = [&](int s) { return bars + 8u * s; };
   auto empty_bar = [&](int s) { return bars + 8u * (NS + s); };
@@ -55,9 +56,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * NS + 8));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(slot + 1);
   volatile int* found = reinterpret_cast<volatile int*>(slot + 2);       // {sequence, tile} or {-1, .}
+  volatile int* stop = reinterpret_cast<volatile int*>(slot + 4);        // [8] a warp of the pair gave up
 
   const AttnArgs& a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int head = blockIdx.x % a.q_heads;
 
   if (warp == 0) {
@@ -67,8 +69,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   }
   if (threadIdx.x == 32) {
     for (int s = 0; s < NS; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int h = 0; h < 2; ++h) { mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(p_bar(h), 4); mbar_init(o_bar(h), 1); }
+    for (int h = 0; h < 2; ++h) { mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(p_bar(h), 8); mbar_init(o_bar(h), 1); }
     *abort_flag = 0;
+    for (int i = 0; i < 8; ++i) stop[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kLoadWarp && lane == 0) { prefetch_tmap(&p.q_map); prefetch_tmap(&p.k_map); prefetch_tmap(&p.v_map); }
@@ -81,7 +84,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *slot;
+  const uint32_t tmem = warp_uniform(*slot);
   const AttnSeq sq = load_seq(a, found[0]);
   const int r0 = found[1] * 2 * kTile;           // first row of the block in its sequence
   const int rows = min(2 * kTile, sq.lq - r0);
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   };
 
   if (warp >= kLoadWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
   if (warp == kLoadWarp) {
     if (lane == 0) {
       const int kvh = head / a.group;
@@ -124,16 +127,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   } else if (warp == kMmaWarp) {
     const KeyTiles<kTile> need[2] = {half_tiles(0), half_tiles(1)};
     const uint32_t idesc_s = make_idesc(kTile, 0, 0), idesc_o = make_idesc(DP, 0, 1);
+    const bool one = elect_one();
     int done[2] = {0, 0};
     bool ok = true;
     auto wait_slot = [&](int i) { return mbar_wait(full_bar(i % NS), (i / NS) & 1u, abort_flag); };
     auto issue_s = [&](int h, int it) {
-      const uint32_t kb = ring + ((2 * it) % NS) * TB, qb = q_base + h * TB;
+      const uint64_t kd = make_desc_kmajor_rows(ring + ((2 * it) % NS) * TB, 128);
+      const uint64_t qd = make_desc_kmajor_rows(q_base + h * TB, 128);
 #pragma unroll
       for (int k = 0; k < DP / 16; ++k) {
-        const uint32_t off = (k >> 2) * (kTile * 128) + (k & 3) * 32;
-        umma_bf16(tmem + h * kTile, make_desc_kmajor_rows(qb + off, 128), make_desc_kmajor_rows(kb + off, 128), idesc_s,
-                  k != 0);
+        const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;      // the address field counts 16 bytes
+        umma_bf16(tmem + h * kTile, qd + off, kd + off, idesc_s, k != 0);
       }
       umma_commit(s_bar(h));
     };
@@ -143,9 +147,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       if (need[h].count() == 0) continue;
       ok = mbar_wait(q_bar(h), 0, abort_flag);
       tc_fence_after();
-      if (ok && lane == 0 && need[h].has(tiles.at(0))) issue_s(h, 0);
+      if (ok && one && need[h].has(tiles.at(0))) issue_s(h, 0);
     }
-    if (ok && n > 0 && lane == 0) umma_commit(empty_bar(0));
+    if (ok && n > 0 && one) umma_commit(empty_bar(0));
     for (int it = 0; it < n && ok; ++it) {
       const int vi = 2 * it + 1;
       if (it + 1 < n) ok = wait_slot(2 * it + 2);
@@ -171,16 +175,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
           ok = mbar_wait(p_bar(h), done[h] & 1u, abort_flag);
           if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
           tc_fence_after();
-          if (lane == 0) {
+          if (one) {
+            const uint64_t vd = make_desc(vb, kTile * 128, 1024);
 #pragma unroll
             for (int k = 0; k < kTile / 16; ++k)
-              umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + k * 8,
-                           make_desc(vb + k * 2048, kTile * 128, 1024), idesc_o, (done[h] | k) != 0);
+              umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + (k >> 2) * 64 + (k & 3) * 8, vd + k * (2048 >> 4), idesc_o,
+                           (done[h] | k) != 0);
             if (done[h] + 1 == need[h].count()) umma_commit(o_bar(h));
           }
           ++done[h];
         }
-        if (lane == 0) {
+        if (one) {
           if (h == 1) umma_commit(empty_bar(vi % NS));
           if (it + 1 < n) {
             if (need[h].has(tiles.at(it + 1))) issue_s(h, it + 1);
@@ -195,12 +200,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     }
   }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    // ---------------- softmax: one row per thread ----------------
-    const int h = warp >> 2;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+    // ---------------- softmax: half a row per thread ----------------
+    const int h = warp >> 3, part = (warp >> 2) & 1;         // which query half, which half of a tile's keys
     const int row = h * kTile + (warp & 3) * 32 + lane;      // in the block
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + h * kTile, o_addr = tmem + lanes + 2 * kTile + h * DP;
+    const uint32_t s_addr = tmem + lanes + h * kTile + part * 64;
+    const uint32_t o_addr = tmem + lanes + 2 * kTile + h * DP + part * (DP / 2);
+    float* mine_max = exchange + part * (2 * kTile) + row;
+    const float* other_max = exchange + (part ^ 1) * (2 * kTile) + row;
+    const int pair_bar = 1 + h * 4 + (warp & 3);             // the two warps that share 32 rows
     const KeyTiles<kTile> need = half_tiles(h);
     const int total = need.count();
     const int half_rows = clamp_int(rows - h * kTile, 0, kTile);
@@ -213,70 +222,77 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
     constexpr bool kTransformed = CAP || BIAS;               // else the factor goes into the exponent's multiply-add
     const float to2 = kTransformed ? 1.f : mul;
-    float m = -INFINITY, l = 0.f;                            // m in the scores' units
+    float m = -INFINITY, l = 0.f;                            // m in base 2; l of this thread's keys
     bool ok = true;
     int cnt = 0;
     for (int it = 0; it < n && ok; ++it) {
       const int t = tiles.at(it);
       if (!need.has(t)) continue;
       ok = __all_sync(0xffffffffu, mbar_wait(s_bar(h), cnt & 1u, abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      float s[kTile];
+      const int j0 = t * kTile + part * 64;
+      float x[64];
+      if (ok) {
+        tc_fence_after();
+        tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+        tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+        tmem_ld_wait();
+        if (kTransformed) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
-      tmem_ld_wait();
-      const int j0 = t * kTile;
-      if (kTransformed) {
-#pragma unroll
-        for (int j = 0; j < kTile; ++j) {
-          float x = s[j] * mul;
-          if (CAP) x = cap2 * tanh_fast(x);
-          if (BIAS) x -= slope2 * fabsf((float)(pos - j0 - j));
-          s[j] = x;
+          for (int j = 0; j < 64; ++j) {
+            x[j] *= mul;
+            if (CAP) x[j] = cap2 * tanh_fast(x[j]);
+            if (BIAS) x[j] = fmaf(-slope2, fabsf((float)(pos - j0 - j)), x[j]);
+          }
         }
-      }
-      if (!all_seen(sq, a.causal, a.window, p0, p1, j0, j0 + kTile)) {
-        const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
+        if (!all_seen(sq, a.causal, a.window, p0, p1, j0, j0 + 64)) {
+          const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
 #pragma unroll
-        for (int j = 0; j < kTile; ++j)
-          if (!((j >= lo && j < hi) || j < pre)) s[j] = -INFINITY;
-      }
-      float mx[4] = {s[0], s[1], s[2], s[3]};
+          for (int j = 0; j < 64; ++j)
+            if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
+        }
+        float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-      for (int j = 4; j < kTile; ++j) mx[j & 3] = fmaxf(mx[j & 3], s[j]);
-      const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      // moved where it has grown by more than 2^8 (always at a row's first visible key)
-      const bool grown = mt > m && (mt - m) * to2 > 8.f;
+        for (int j = 4; j < 64; j += 8) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(fmaxf(mx[e], x[j + e]), x[j + 4 + e < 64 ? j + 4 + e : j + e]);
+        }
+        *mine_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+      } else {
+        stop[pair_bar - 1] = 1;
+      }
+      named_barrier(pair_bar, 64);
+      if (stop[pair_bar - 1]) { ok = false; break; }         // both warps leave in the same tile
+      const float mt = fmaxf(*mine_max, *other_max) * to2;
+      const bool grown = mt > m + 8.f || (mt > m && m == -INFINITY);
       if (__any_sync(0xffffffffu, grown)) {
-        const float m_new = fmaxf(m, mt);
-        const float f = m == -INFINITY ? 0.f : ex2((m - m_new) * to2);
+        // rare after a row's first keys: what there is so far is scaled down, by a power of two, so exactly
+        const float m_new = grown ? ceilf(mt) : m;
+        const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
         m = m_new;
         l *= f;
         if (cnt > 0) {                                       // the product before this tile's S has finished
-#pragma unroll
-          for (int c = 0; c < DP / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32(o_addr + c * 32, o);
+#pragma unroll 1
+          for (int i = 0; i < DP / 32; ++i) {
+            uint32_t o[16];
+            tmem_ld16(o_addr + i * 16, o);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st32(o_addr + c * 32, o);
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st16(o_addr + i * 16, o);
           }
         }
       }
-      const float shift = m == -INFINITY ? 0.f : -m * to2;
+      const float shift = m == -INFINITY ? 0.f : -m;
       const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
       uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         uint32_t pk[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int j = c * 32 + 2 * i;
-          const uint64_t x = pair2(s[j], s[j + 1]);
+          const uint64_t v = pair2(x[c * 32 + 2 * i], x[c * 32 + 2 * i + 1]);
           float e0, e1;
-          unpair2(kTransformed ? add2(x, shift_2) : fma2(x, mul_2, shift_2), e0, e1);
+          unpair2(kTransformed ? add2(v, shift_2) : fma2(v, mul_2, shift_2), e0, e1);
           e0 = ex2(e0);
           e1 = ex2(e1);
           sum[i & 1] = add2(sum[i & 1], pair2(e0, e1));
@@ -297,13 +313,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       ok = __all_sync(0xffffffffu, mbar_wait(o_bar(h), 0, abort_flag));
       tc_fence_after();
     }
+    // every warp of a pair comes here: the row's sum is its two halves'
+    *mine_max = l;
+    named_barrier(pair_bar, 64);
+    l += *other_max;
     if (ok) {
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // a row that sees nothing gives zeros
       const bool mine = row < rows;
+      const int c0 = part * (DP / 2);
       bf16* dst = reinterpret_cast<bf16*>(a.out) + (size_t)(sq.q0 + r0 + (mine ? row : 0)) * a.o_stride +
-                  (size_t)head * a.head_dim;
+                  (size_t)head * a.head_dim + c0;
 #pragma unroll
-      for (int c = 0; c < DP / 32; ++c) {
+      for (int c = 0; c < DP / 64; ++c) {
         uint32_t o[32];
         if (total > 0) {
           tmem_ld32(o_addr + c * 32, o);
@@ -311,21 +332,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          if (mine && c * 32 + g * 8 < a.head_dim) {
+          if (mine && c0 + c * 32 + g * 8 < a.head_dim) {
             uint4 w;
             uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float x = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
-              const float y = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
-              wp[i] = bf16x2(x, y);
+              const float u = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
+              const float v = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
+              wp[i] = bf16x2(u, v);
             }
             *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = w;
           }
         }
       }
-      if (a.lse && mine)
-        a.lse[(size_t)head * a.q_rows + sq.q0 + r0 + row] = (m * to2 + log2f(l)) * kLn2;
+      if (a.lse && mine && part == 0)
+        a.lse[(size_t)head * a.q_rows + sq.q0 + r0 + row] = (m + log2f(l)) * kLn2;
     } else if (lane == 0) {
       *abort_flag = 1;
       if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
