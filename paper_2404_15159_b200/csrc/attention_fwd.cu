@@ -15,14 +15,18 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = 128;                       // keys per step, and query rows per half of a block's rows
-constexpr int kThreads = 640;                    // four softmax groups of 4 warps; a group with the load and MMA warps
-// A block starts with 96 registers a thread (640 x 96 = 61440); the softmax groups, whose threads hold half a row of
-// scores each, take 112 and the fifth group keeps 32: (4 x 112 + 32) x 128 = 61440.
-constexpr int kLoadWarp = 16, kMmaWarp = 17;
+constexpr int kThreads = 384;                    // two softmax groups of 4 warps; a group with the load and MMA warps
+// A block starts with 168 registers a thread (384 x 168 = 64512); the softmax groups, whose threads hold half a row of
+// scores and its exponentials, take 208 and the third group keeps 88: (2 x 208 + 88) x 128 = 64512.
+constexpr int kLoadWarp = 8, kMmaWarp = 9;
 constexpr int kTmemCols = 512;
 template <int DP> constexpr int kStages = DP == 128 ? 5 : 8;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
-template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 2 * 2 * kTile * 4 + 256;
+template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 256;
+
+// Of 8 pairs of exponentials those that go to the fp32 pipes
+constexpr int kPolys = 2;
+template <int N> struct Int { static constexpr int value = N; };
 
 struct FwdParams {
   AttnArgs a;
@@ -31,12 +35,14 @@ struct FwdParams {
 
 // One block: 256 query rows of a head (two halves of 128) against the sequence's key tiles.  The load warp streams K and
 // V tiles through a ring; the MMA warp issues, half by half, O += P V and then the next S = Q K^T, so that one half's
-// products run while the other half's exponentials are computed.  S [128 x 128] sits in TMEM; eight warps take its
-// rows, 64 keys of a row to a thread (two warps to a scheduler and half: one alone is held up by its own latencies),
-// and write P over it as bf16, from where the product reads it: P never touches shared memory.  P is rounded to bf16
-// (the tensor cores' operand type); the row sums l are taken from the unrounded values in fp32.  The running maximum is
-// only moved (and O rescaled) when a row's maximum grows by more than 2^8: until then e^(s - m) <= 2^8, far from
-// overflow, and the factor cancels in O / l.  m is a whole number in base 2, so that a move rescales O and l exactly.
+// products run while the other half's exponentials are computed.  S [128 x 128] sits in TMEM; four warps take its rows,
+// a row to a thread, and write P over it as bf16, from where the product reads it: P never touches shared memory, and
+// its first half is used while the second is computed.  P is rounded to bf16 (the tensor cores' operand type); the row
+// sums l are taken from the unrounded values in fp32.
+// The running maximum m stands for "large enough": p = 2^(s - m) is taken over the m of the tiles before, without
+// waiting for this tile's maximum.  A tile whose p sum up to more than 2^8 raises m for the next one, and only a row's
+// first keys, or p that sum up to more than 2^100 (fp32 and bf16 end at 2^127), are taken again over their own maximum.
+// m is a whole number in base 2, so that raising it rescales O and l exactly.
 template <int DP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams p) {
   constexpr int NS = kStages<DP>;
@@ -44,19 +50,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   constexpr int NB = DP / 64;                    // 64-value blocks of a head in a tile
   extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle counts from 1024-byte boundaries
   const uint32_t q_base = smem_u32(smem), ring = q_base + 2 * TB;
-  float* exchange = reinterpret_cast<float*>(smem + (2 + NS) * TB);      // [2 column halves][256 rows]
-  uint8_t* ctl = reinterpret_cast<uint8_t*>(exchange + 2 * 2 * kTile);
+  uint8_t* ctl = smem + (2 + NS) * TB;
   const uint32_t bars = smem_u32(ctl);
   auto full_bar = [&](int s) { return bars + 8u * s; };
   auto empty_bar = [&](int s) { return bars + 8u * (NS + s); };
   auto q_bar = [&](int h) { return bars + 8u * (2 * NS + h); };
   auto s_bar = [&](int h) { return bars + 8u * (2 * NS + 2 + h); };
   auto p_bar = [&](int h) { return bars + 8u * (2 * NS + 4 + h); };
-  auto o_bar = [&](int h) { return bars + 8u * (2 * NS + 6 + h); };
-  uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * NS + 8));
+  auto o_bar = [&](int h) { return bars + 8u * (2 * NS + 8 + h); };      // p_bar: two pairs, for the two halves of P
+  auto v_bar = [&](int h) { return bars + 8u * (2 * NS + 10 + h); };     // the first half of P has been used
+  uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * NS + 12));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(slot + 1);
   volatile int* found = reinterpret_cast<volatile int*>(slot + 2);       // {sequence, tile} or {-1, .}
-  volatile int* stop = reinterpret_cast<volatile int*>(slot + 4);        // [8] a warp of the pair gave up
 
   const AttnArgs& a = p.a;
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -69,9 +74,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   }
   if (threadIdx.x == 32) {
     for (int s = 0; s < NS; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int h = 0; h < 2; ++h) { mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(p_bar(h), 8); mbar_init(o_bar(h), 1); }
+    for (int h = 0; h < 2; ++h) { mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(p_bar(h), 4); mbar_init(p_bar(h) + 16u, 4); mbar_init(v_bar(h), 1); mbar_init(o_bar(h), 1); }
     *abort_flag = 0;
-    for (int i = 0; i < 8; ++i) stop[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kLoadWarp && lane == 0) { prefetch_tmap(&p.q_map); prefetch_tmap(&p.k_map); prefetch_tmap(&p.v_map); }
@@ -99,7 +103,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   };
 
   if (warp >= kLoadWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == kLoadWarp) {
     if (lane == 0) {
       const int kvh = head / a.group;
@@ -172,17 +176,22 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if (need[h].has(tiles.at(it))) {
-          ok = mbar_wait(p_bar(h), done[h] & 1u, abort_flag);
-          if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-          tc_fence_after();
-          if (one) {
-            const uint64_t vd = make_desc(vb, kTile * 128, 1024);
+          const uint64_t vd = make_desc(vb, kTile * 128, 1024);
 #pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-              umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + (k >> 2) * 64 + (k & 3) * 8, vd + k * (2048 >> 4), idesc_o,
-                           (done[h] | k) != 0);
-            if (done[h] + 1 == need[h].count()) umma_commit(o_bar(h));
+          for (int c = 0; c < 2 && ok; ++c) {                // the two halves of P as they come
+            ok = __all_sync(0xffffffffu, mbar_wait(p_bar(h) + 16u * c, done[h] & 1u, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            if (one) {
+#pragma unroll
+              for (int k = 4 * c; k < 4 * c + 4; ++k)
+                umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + k * 8, vd + k * (2048 >> 4), idesc_o,
+                             (done[h] | k) != 0);
+              if (c == 0) umma_commit(v_bar(h));
+            }
           }
+          if (!ok) break;
+          if (one && done[h] + 1 == need[h].count()) umma_commit(o_bar(h));
           ++done[h];
         }
         if (one) {
@@ -200,16 +209,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     }
   }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-    // ---------------- softmax: half a row per thread ----------------
-    const int h = warp >> 3, part = (warp >> 2) & 1;         // which query half, which half of a tile's keys
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ---------------- softmax: one row per thread ----------------
+    const int h = warp >> 2;
     const int row = h * kTile + (warp & 3) * 32 + lane;      // in the block
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t s_addr = tmem + lanes + h * kTile + part * 64;
-    const uint32_t o_addr = tmem + lanes + 2 * kTile + h * DP + part * (DP / 2);
-    float* mine_max = exchange + part * (2 * kTile) + row;
-    const float* other_max = exchange + (part ^ 1) * (2 * kTile) + row;
-    const int pair_bar = 1 + h * 4 + (warp & 3);             // the two warps that share 32 rows
+    const uint32_t s_addr = tmem + lanes + h * kTile, o_addr = tmem + lanes + 2 * kTile + h * DP;
     const KeyTiles<kTile> need = half_tiles(h);
     const int total = need.count();
     const int half_rows = clamp_int(rows - h * kTile, 0, kTile);
@@ -222,19 +227,42 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
     constexpr bool kTransformed = CAP || BIAS;               // else the factor goes into the exponent's multiply-add
     const float to2 = kTransformed ? 1.f : mul;
-    float m = -INFINITY, l = 0.f;                            // m in base 2; l of this thread's keys
+    float m = -INFINITY, l = 0.f;                            // m in base 2
+    float tile_sum = 0.f;                                    // the last tile's part of l
     bool ok = true;
     int cnt = 0;
+    auto scale_o = [&](float f) {
+#pragma unroll 1
+      for (int i = 0; i < DP / 16; ++i) {
+        uint32_t o[16];
+        tmem_ld16(o_addr + i * 16, o);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+        tmem_st16(o_addr + i * 16, o);
+      }
+    };
     for (int it = 0; it < n && ok; ++it) {
       const int t = tiles.at(it);
       if (!need.has(t)) continue;
+      const bool whole = all_seen(sq, a.causal, a.window, p0, p1, t * kTile, t * kTile + kTile);
       ok = __all_sync(0xffffffffu, mbar_wait(s_bar(h), cnt & 1u, abort_flag));
-      const int j0 = t * kTile + part * 64;
-      float x[64];
-      if (ok) {
-        tc_fence_after();
-        tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
-        tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+      if (!ok) break;
+      tc_fence_after();
+      // S is there, so the products before it have finished and O stands still
+      if (__any_sync(0xffffffffu, tile_sum > 256.f)) {       // the last tile's p had grown: m follows
+        const float k = tile_sum > 256.f ? ceilf(log2f(tile_sum)) : 0.f, f = ex2(-k);
+        m += k;
+        l *= f;
+        scale_o(f);
+      }
+      tile_sum = 0.f;
+#pragma unroll 1
+      for (int c = 0; c < 2 && ok; ++c) {
+        const int j0 = t * kTile + c * 64;
+        float x[64];
+        tmem_ld32(s_addr + c * 64, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+        tmem_ld32(s_addr + c * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
         tmem_ld_wait();
         if (kTransformed) {
 #pragma unroll
@@ -244,87 +272,83 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             if (BIAS) x[j] = fmaf(-slope2, fabsf((float)(pos - j0 - j)), x[j]);
           }
         }
-        if (!all_seen(sq, a.causal, a.window, p0, p1, j0, j0 + 64)) {
+        if (!whole) {
           const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
 #pragma unroll
           for (int j = 0; j < 64; ++j)
             if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
         }
-        float mx[4] = {x[0], x[1], x[2], x[3]};
+        uint32_t pk[32];
+        float sum;
+        bool reset = m == -INFINITY;                         // nothing seen yet; below: p near the end of its range
+        while (true) {
+          if (__any_sync(0xffffffffu, reset)) {
+            float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-        for (int j = 4; j < 64; j += 8) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(fmaxf(mx[e], x[j + e]), x[j + 4 + e < 64 ? j + 4 + e : j + e]);
-        }
-        *mine_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-      } else {
-        stop[pair_bar - 1] = 1;
-      }
-      named_barrier(pair_bar, 64);
-      if (stop[pair_bar - 1]) { ok = false; break; }         // both warps leave in the same tile
-      const float mt = fmaxf(*mine_max, *other_max) * to2;
-      const bool grown = mt > m + 8.f || (mt > m && m == -INFINITY);
-      if (__any_sync(0xffffffffu, grown)) {
-        // rare after a row's first keys: what there is so far is scaled down, by a power of two, so exactly
-        const float m_new = grown ? ceilf(mt) : m;
-        const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
-        m = m_new;
-        l *= f;
-        if (cnt > 0) {                                       // the product before this tile's S has finished
-#pragma unroll 1
-          for (int i = 0; i < DP / 32; ++i) {
-            uint32_t o[16];
-            tmem_ld16(o_addr + i * 16, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st16(o_addr + i * 16, o);
+            for (int j = 4; j < 64; ++j) mx[j & 3] = fmaxf(mx[j & 3], x[j]);
+            const float mt = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * to2);
+            const float m_new = reset ? fmaxf(mt, m) : m;
+            const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
+            m = m_new;
+            l *= f;
+            tile_sum *= f;
+            if (c == 1) {                                    // the first half's P may still be on its way into O
+              ok = __all_sync(0xffffffffu, mbar_wait(v_bar(h), cnt & 1u, abort_flag));
+              if (!ok) break;
+              tc_fence_after();
+            }
+            if (cnt > 0 || c == 1) scale_o(f);
           }
-        }
-      }
-      const float shift = m == -INFINITY ? 0.f : -m;
-      const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
-      uint64_t sum[2] = {0ull, 0ull};
+          const float shift = m == -INFINITY ? 0.f : -m;
+          const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
+          uint64_t acc[2] = {0ull, 0ull};
+          auto exponentials = [&](auto polys) {              // the last `polys` of 8 pairs on the fp32 pipes
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t pk[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint64_t v = pair2(x[c * 32 + 2 * i], x[c * 32 + 2 * i + 1]);
-          float e0, e1;
-          unpair2(kTransformed ? add2(v, shift_2) : fma2(v, mul_2, shift_2), e0, e1);
-          e0 = ex2(e0);
-          e1 = ex2(e1);
-          sum[i & 1] = add2(sum[i & 1], pair2(e0, e1));
-          pk[i] = bf16x2(e0, e1);
+            for (int i = 0; i < 32; ++i) {
+              uint64_t v = pair2(x[2 * i], x[2 * i + 1]);
+              v = kTransformed ? add2(v, shift_2) : fma2(v, mul_2, shift_2);
+              float e0, e1;
+              if ((i & 7) >= 8 - polys.value) {
+                ex2_poly(v, e0, e1);
+              } else {
+                unpair2(v, e0, e1);
+                e0 = ex2(e0);
+                e1 = ex2(e1);
+              }
+              acc[i & 1] = add2(acc[i & 1], pair2(e0, e1));
+              pk[i] = bf16x2(e0, e1);
+            }
+          };
+          if (whole) exponentials(Int<kPolys>());
+          else exponentials(Int<0>());
+          float l0, l1;
+          unpair2(add2(acc[0], acc[1]), l0, l1);
+          sum = l0 + l1;
+          reset = sum > 0x1p100f;
+          if (!__any_sync(0xffffffffu, reset)) break;
         }
-        tmem_st16(s_addr + c * 16, pk);
+        if (!ok) break;
+        tmem_st32(s_addr + c * 32, pk);                      // over scores of the tile's first half
+        l += sum;
+        tile_sum += sum;
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_bar(h) + 16u * c);
       }
-      float l0, l1;
-      unpair2(add2(sum[0], sum[1]), l0, l1);
-      l += l0 + l1;
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_bar(h));
       ++cnt;
     }
     if (ok && total > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(o_bar(h), 0, abort_flag));
       tc_fence_after();
     }
-    // every warp of a pair comes here: the row's sum is its two halves'
-    *mine_max = l;
-    named_barrier(pair_bar, 64);
-    l += *other_max;
     if (ok) {
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // a row that sees nothing gives zeros
       const bool mine = row < rows;
-      const int c0 = part * (DP / 2);
       bf16* dst = reinterpret_cast<bf16*>(a.out) + (size_t)(sq.q0 + r0 + (mine ? row : 0)) * a.o_stride +
-                  (size_t)head * a.head_dim + c0;
+                  (size_t)head * a.head_dim;
 #pragma unroll
-      for (int c = 0; c < DP / 64; ++c) {
+      for (int c = 0; c < DP / 32; ++c) {
         uint32_t o[32];
         if (total > 0) {
           tmem_ld32(o_addr + c * 32, o);
@@ -332,20 +356,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          if (mine && c0 + c * 32 + g * 8 < a.head_dim) {
+          if (mine && c * 32 + g * 8 < a.head_dim) {
             uint4 w;
             uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float u = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
-              const float v = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
-              wp[i] = bf16x2(u, v);
+              const float x = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
+              const float y = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
+              wp[i] = bf16x2(x, y);
             }
             *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = w;
           }
         }
       }
-      if (a.lse && mine && part == 0)
+      if (a.lse && mine)
         a.lse[(size_t)head * a.q_rows + sq.q0 + r0 + row] = (m + log2f(l)) * kLn2;
     } else if (lane == 0) {
       *abort_flag = 1;
