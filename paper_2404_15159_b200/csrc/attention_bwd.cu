@@ -23,10 +23,15 @@ constexpr int kTile = 128;
 constexpr int kThreads = 384;                    // two groups of 4 warps on the elements, a load warp, an MMA warp
 constexpr int kLoadWarp = 8, kMmaWarp = 9;
 constexpr int kTmemCols = 512;
-constexpr int kStages = 2;
+constexpr int kRowWarp = 10;                     // of the key kernel: carries lse and delta
+// The walked tiles come in two streams.  Stream A (q; of the query kernel: k) is read by a tile's first and last product,
+// stream B (do; v) is done earlier: three and two stages, which is what shared memory holds at 128 values a head.
+constexpr int kStagesA = 3, kStagesB = 2;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
-constexpr uint32_t kRowBytes = 2 * kTile * 4;    // minus lse and minus delta of a query tile
-template <int DP> constexpr uint32_t kSmemBytes = (2 + 2 * kStages) * kTileBytes<DP> + kStages * kRowBytes + 1024 + 256;
+constexpr uint32_t kRowBytes = 2 * kTile * 4;    // minus lse and minus delta of a query tile, two stages
+template <int DP> constexpr uint32_t kSmemBytes = (2 + kStagesA + kStagesB) * kTileBytes<DP> + 2 * kRowBytes + 256;
+// Of 8 pairs of exponentials those that go to the fp32 pipes
+constexpr int kPolys = 2;
 
 struct BwdParams {
   AttnArgs a;
@@ -36,16 +41,26 @@ struct BwdParams {
 struct Ctl {
   uint32_t bars;
   volatile int* abort_flag;
-  __device__ __forceinline__ uint32_t full(int s) const { return bars + 8u * s; }
-  __device__ __forceinline__ uint32_t empty(int s) const { return bars + 8u * (kStages + s); }
-  __device__ __forceinline__ uint32_t own() const { return bars + 8u * (2 * kStages); }        // the block's own tiles
-  __device__ __forceinline__ uint32_t s() const { return bars + 8u * (2 * kStages + 1); }      // scores are there
-  __device__ __forceinline__ uint32_t dp() const { return bars + 8u * (2 * kStages + 3); }     // do . v is there
-  __device__ __forceinline__ uint32_t p() const { return bars + 8u * (2 * kStages + 4); }      // p is written
-  __device__ __forceinline__ uint32_t ds() const { return bars + 8u * (2 * kStages + 5); }     // ds is written
-  __device__ __forceinline__ uint32_t acc() const { return bars + 8u * (2 * kStages + 6); }    // the sums are final
+  __device__ __forceinline__ uint32_t full_a(int i) const { return bars + 8u * (i % kStagesA); }
+  __device__ __forceinline__ uint32_t empty_a(int i) const { return bars + 8u * (kStagesA + i % kStagesA); }
+  __device__ __forceinline__ uint32_t full_b(int i) const { return bars + 8u * (2 * kStagesA + i % kStagesB); }
+  __device__ __forceinline__ uint32_t empty_b(int i) const { return bars + 8u * (2 * kStagesA + kStagesB + i % kStagesB); }
+  __device__ __forceinline__ uint32_t at(int k) const { return bars + 8u * (2 * kStagesA + 2 * kStagesB + k); }
+  __device__ __forceinline__ uint32_t own() const { return at(0); }                      // the block's own tiles
+  __device__ __forceinline__ uint32_t s(int k) const { return at(1 + k); }               // scores are there
+  __device__ __forceinline__ uint32_t dp() const { return at(3); }                       // do . v is there
+  __device__ __forceinline__ uint32_t p() const { return at(4); }                        // p is written
+  __device__ __forceinline__ uint32_t ds() const { return at(5); }                       // ds is written
+  __device__ __forceinline__ uint32_t acc() const { return at(6); }                      // the sums are final
+  __device__ __forceinline__ uint32_t rows_full(int i) const { return at(7 + (i & 1)); }
+  __device__ __forceinline__ uint32_t rows_empty(int i) const { return at(9 + (i & 1)); }
+  // waits for use number i / stages of a stage
+  __device__ __forceinline__ bool wait_full_a(int i) const { return mbar_wait(full_a(i), (i / kStagesA) & 1u, abort_flag); }
+  __device__ __forceinline__ bool wait_empty_a(int i) const { return mbar_wait(empty_a(i), ((i / kStagesA) & 1u) ^ 1u, abort_flag); }
+  __device__ __forceinline__ bool wait_full_b(int i) const { return mbar_wait(full_b(i), (i / kStagesB) & 1u, abort_flag); }
+  __device__ __forceinline__ bool wait_empty_b(int i) const { return mbar_wait(empty_b(i), ((i / kStagesB) & 1u) ^ 1u, abort_flag); }
 };
-constexpr int kBars = 2 * kStages + 7;
+constexpr int kBars = 2 * kStagesA + 2 * kStagesB + 11;
 
 template <int DP>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
@@ -107,10 +122,9 @@ __device__ __forceinline__ void store_row(uint32_t acc, bool any, float mul, boo
   }
 }
 
-// Block setup shared by both kernels: the block's tile, barriers, TMEM.  `loaders`: arrivals that fill a stage.  False:
-// nothing to do.
+// Block setup shared by both kernels: the block's tile, barriers, TMEM.  False: nothing to do.
 __device__ __forceinline__ bool block_begin(const int32_t* off, int n_seqs, int rows, int tile, bool from_end,
-                                            int loaders, const Ctl& c, uint32_t* slot, int* seq, int* index) {
+                                            const Ctl& c, uint32_t* slot, int* seq, int* index) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* found = reinterpret_cast<volatile int*>(slot + 2);
   if (warp == 0) {
@@ -120,11 +134,11 @@ __device__ __forceinline__ bool block_begin(const int32_t* off, int n_seqs, int 
     if (lane == 0) { found[0] = b; found[1] = t; }
   }
   if (threadIdx.x == 32) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(c.full(s), loaders); mbar_init(c.empty(s), 1); }
-    mbar_init(c.own(), 1);
-    mbar_init(c.s(), 1); mbar_init(c.s() + 8u, 1);
-    mbar_init(c.dp(), 1); mbar_init(c.acc(), 1);
+    for (int i = 0; i < kStagesA; ++i) { mbar_init(c.full_a(i), 1); mbar_init(c.empty_a(i), 1); }
+    for (int i = 0; i < kStagesB; ++i) { mbar_init(c.full_b(i), 1); mbar_init(c.empty_b(i), 1); }
+    mbar_init(c.own(), 1); mbar_init(c.s(0), 1); mbar_init(c.s(1), 1); mbar_init(c.dp(), 1); mbar_init(c.acc(), 1);
     mbar_init(c.p(), 8); mbar_init(c.ds(), 8);
+    for (int i = 0; i < 2; ++i) { mbar_init(c.rows_full(i), 1); mbar_init(c.rows_empty(i), 8); }
     *c.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -166,6 +180,7 @@ struct Score {
   __device__ __forceinline__ Score(const AttnArgs& a, int head)
       : mul(CAP ? a.scale / a.softcap : a.scale * kLog2e), cap2(a.softcap * kLog2e),
         slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
+  template <bool POLY>
   __device__ __forceinline__ void probs(float s0, float s1, uint64_t neg_lse, int d0, int d1, float& p0, float& p1,
                                         uint64_t& cap_slope) const {
     uint64_t x;
@@ -183,8 +198,12 @@ struct Score {
       x0 = fmaf(-slope2, fabsf((float)d0), x0);
       x1 = fmaf(-slope2, fabsf((float)d1), x1);
     }
-    p0 = ex2(x0);
-    p1 = ex2(x1);
+    if (POLY) {
+      ex2_poly(pair2(x0, x1), p0, p1);
+    } else {
+      p0 = ex2(x0);
+      p1 = ex2(x1);
+    }
   }
 };
 
@@ -194,20 +213,21 @@ struct Score {
 template <int DP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_constant__ BwdParams p) {
   constexpr uint32_t TB = kTileBytes<DP>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  const uint32_t k_tile = smem_u32(smem), v_tile = k_tile + TB, ring = k_tile + 2 * TB;
-  float* rows_smem = reinterpret_cast<float*>(smem + (2 + 2 * kStages) * TB);
-  uint8_t* ctl = reinterpret_cast<uint8_t*>(rows_smem) + kStages * kRowBytes;
+  extern __shared__ __align__(1024) uint8_t smem[];          // the swizzle counts from 1024-byte boundaries
+  const uint32_t k_tile = smem_u32(smem), v_tile = k_tile + TB;
+  auto q_at = [&](int i) { return k_tile + (2 + i % kStagesA) * TB; };
+  auto do_at = [&](int i) { return k_tile + (2 + kStagesA + i % kStagesB) * TB; };
+  float* rows_smem = reinterpret_cast<float*>(smem + (2 + kStagesA + kStagesB) * TB);
+  uint8_t* ctl = reinterpret_cast<uint8_t*>(rows_smem) + 2 * kRowBytes;
   uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * kBars);
   const Ctl c{smem_u32(ctl), reinterpret_cast<volatile int*>(slot + 1)};
   const AttnArgs& a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int kvh = blockIdx.x % a.kv_heads;
   int seq, index;
   // the first keys of a causal sequence are seen by the most rows: long work starts first
-  if (!block_begin(a.k_off, a.n_seqs, a.k_rows, blockIdx.x / a.kv_heads, false, 1 + 32, c, slot, &seq, &index)) return;
-  const uint32_t tmem = *slot;
+  if (!block_begin(a.k_off, a.n_seqs, a.k_rows, blockIdx.x / a.kv_heads, false, c, slot, &seq, &index)) return;
+  const uint32_t tmem = warp_uniform(*slot);
   const uint32_t t_s = tmem, t_dp = tmem + kTile, t_dv = tmem + 2 * kTile, t_dk = t_dv + DP;
   const AttnSeq sq = load_seq(a, seq);
   const int j0 = index * kTile;
@@ -218,83 +238,99 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
   const int per_head = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
   const int n = per_head * a.group;
 
+  auto head_of = [&](int i) { return kvh * a.group + i / per_head; };
+  auto row_of = [&](int i) { return lo + (i % per_head) * kTile; };
+
   if (warp == kLoadWarp) {
-    bool ok = true;
-    if (n > 0 && lane == 0) {
-      mbar_expect_tx(c.own(), 2 * TB);
-      load_tile<DP>(k_tile, &p.k_map, c.own(), kvh, sq.k0 + j0);
-      load_tile<DP>(v_tile, &p.v_map, c.own(), kvh, sq.k0 + j0);
-    }
-    for (int i = 0; i < n; ++i) {
-      const int st = i % kStages;
-      if (!__all_sync(0xffffffffu, mbar_wait(c.empty(st), ((i / kStages) & 1u) ^ 1u, c.abort_flag))) { ok = false; break; }
-      const int head = kvh * a.group + i / per_head, i0 = lo + (i % per_head) * kTile;
-      if (lane == 0) {
-        mbar_expect_tx(c.full(st), 2 * TB);
-        load_tile<DP>(ring + st * 2 * TB, &p.q_map, c.full(st), head, sq.q0 + i0);
-        load_tile<DP>(ring + st * 2 * TB + TB, &p.do_map, c.full(st), head, sq.q0 + i0);
+    if (lane == 0) {
+      bool ok = true;
+      if (n > 0) {
+        mbar_expect_tx(c.own(), 2 * TB);
+        load_tile<DP>(k_tile, &p.k_map, c.own(), kvh, sq.k0 + j0);
+        load_tile<DP>(v_tile, &p.v_map, c.own(), kvh, sq.k0 + j0);
       }
-      float* dst = rows_smem + st * (2 * kTile);
-      const size_t at = (size_t)head * a.q_rows + sq.q0 + i0;
+      for (int i = 0; i < n; ++i) {
+        if (!c.wait_empty_a(i)) { ok = false; break; }
+        mbar_expect_tx(c.full_a(i), TB);
+        load_tile<DP>(q_at(i), &p.q_map, c.full_a(i), head_of(i), sq.q0 + row_of(i));
+        if (!c.wait_empty_b(i)) { ok = false; break; }
+        mbar_expect_tx(c.full_b(i), TB);
+        load_tile<DP>(do_at(i), &p.do_map, c.full_b(i), head_of(i), sq.q0 + row_of(i));
+      }
+      if (!ok) give_up(c, a.status);
+    }
+  } else if (warp == kRowWarp) {
+    bool ok = true;
+    for (int i = 0; i < n; ++i) {
+      float v[2][kTile / 32];
+      const size_t at = (size_t)head_of(i) * a.q_rows + sq.q0 + row_of(i);
 #pragma unroll
       for (int x = 0; x < kTile / 32; ++x) {
-        const int r = x * 32 + lane;
-        const bool on = i0 + r < sq.lq;
-        dst[r] = on ? -a.lse2[at + r] : -INFINITY;
-        dst[kTile + r] = on ? -a.delta[at + r] : 0.f;
+        const bool on = row_of(i) + x * 32 + lane < sq.lq;
+        v[0][x] = on ? -a.lse2[at + x * 32 + lane] : -INFINITY;
+        v[1][x] = on ? -a.delta[at + x * 32 + lane] : 0.f;
       }
-      mbar_arrive(c.full(st));
+      if (!__all_sync(0xffffffffu, mbar_wait(c.rows_empty(i), ((i >> 1) & 1u) ^ 1u, c.abort_flag))) { ok = false; break; }
+      float* dst = rows_smem + (i & 1) * (2 * kTile) + lane;
+#pragma unroll
+      for (int x = 0; x < kTile / 32; ++x) {
+        dst[x * 32] = v[0][x];
+        dst[kTile + x * 32] = v[1][x];
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(c.rows_full(i));
     }
     if (!ok && lane == 0) give_up(c, a.status);
   } else if (warp == kMmaWarp) {
-    bool ok = n == 0 || mbar_wait(c.own(), 0, c.abort_flag);
-    auto arrived = [&](int i) {                              // tile i of q and do is in shared memory, its tail cleared
-      if (!__all_sync(0xffffffffu, mbar_wait(c.full(i % kStages), (i / kStages) & 1u, c.abort_flag))) return false;
-      const int valid = sq.lq - (lo + (i % per_head) * kTile);
+    const bool one = elect_one();
+    bool ok = n == 0 || __all_sync(0xffffffffu, mbar_wait(c.own(), 0, c.abort_flag));
+    // a stream's tile i is in shared memory, its rows behind the last cleared
+    auto tail = [&](int i, uint32_t tile) {
+      const int valid = sq.lq - row_of(i);
       if (valid < kTile) {
-        clear_rows<DP>(ring + (i % kStages) * 2 * TB, valid);
-        clear_rows<DP>(ring + (i % kStages) * 2 * TB + TB, valid);
+        clear_rows<DP>(tile, valid);
         fence_proxy_async_smem();
         __syncwarp();
       }
       tc_fence_after();
+    };
+    auto scores = [&](int i) {
+      if (!__all_sync(0xffffffffu, c.wait_full_a(i))) return false;
+      tail(i, q_at(i));
+      if (one) {
+        issue_nt<DP>(t_s, k_tile, q_at(i));
+        umma_commit(c.s(0));
+      }
       return true;
     };
-    ok = __all_sync(0xffffffffu, ok) && (n == 0 || arrived(0));
-    if (ok && n > 0 && lane == 0) {
-      issue_nt<DP>(t_s, k_tile, ring);
-      umma_commit(c.s());
-      issue_nt<DP>(t_dp, v_tile, ring + TB);
-      umma_commit(c.dp());
-    }
+    auto grads = [&](int i) {
+      if (!__all_sync(0xffffffffu, c.wait_full_b(i))) return false;
+      tail(i, do_at(i));
+      if (one) {
+        issue_nt<DP>(t_dp, v_tile, do_at(i));
+        umma_commit(c.dp());
+      }
+      return true;
+    };
+    ok = ok && (n == 0 || (scores(0) && grads(0)));
     for (int i = 0; i < n && ok; ++i) {
-      const uint32_t qt = ring + (i % kStages) * 2 * TB, dot = qt + TB;
-      const uint32_t nq = ring + ((i + 1) % kStages) * 2 * TB, ndo = nq + TB;
       ok = __all_sync(0xffffffffu, mbar_wait(c.p(), i & 1u, c.abort_flag));
       if (!ok) break;
       tc_fence_after();
-      if (lane == 0) issue_ts<DP>(t_dv, t_s, dot, i > 0);
-      if (i + 1 < n) {
-        ok = arrived(i + 1);
-        if (!ok) break;
-        if (lane == 0) {
-          issue_nt<DP>(t_s, k_tile, nq);
-          umma_commit(c.s());
-        }
+      if (one) {
+        issue_ts<DP>(t_dv, t_s, do_at(i), i > 0);
+        umma_commit(c.empty_b(i));
       }
-      ok = __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
+      ok = i + 1 >= n || scores(i + 1);
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
       if (!ok) break;
       tc_fence_after();
-      if (lane == 0) {
-        issue_ts<DP>(t_dk, t_dp, qt, i > 0);
-        umma_commit(c.empty(i % kStages));
-        if (i + 1 < n) {
-          issue_nt<DP>(t_dp, v_tile, ndo);
-          umma_commit(c.dp());
-        } else {
-          umma_commit(c.acc());
-        }
+      if (one) {
+        issue_ts<DP>(t_dk, t_dp, q_at(i), i > 0);
+        umma_commit(c.empty_a(i));
+        if (i + 1 == n) umma_commit(c.acc());
       }
+      ok = i + 1 >= n || grads(i + 1);
     }
     if (!ok && lane == 0) give_up(c, a.status);
   } else if (warp < kLoadWarp) {
@@ -304,15 +340,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
     const uint32_t s_addr = t_s + lanes + half * 64, dp_addr = t_dp + lanes + half * 64;
     bool ok = true;
     for (int i = 0; i < n && ok; ++i) {
-      const int head = kvh * a.group + i / per_head, i0 = lo + (i % per_head) * kTile + half * 64;
-      const Score<CAP, BIAS> score(a, head);
-      const float* neg_lse = rows_smem + (i % kStages) * (2 * kTile) + half * 64;
+      const int i0 = row_of(i) + half * 64;
+      const Score<CAP, BIAS> score(a, head_of(i));
+      const float* neg_lse = rows_smem + (i & 1) * (2 * kTile) + half * 64;
       const float* neg_delta = neg_lse + kTile;
       const int pos0 = sq.shift + i0;
       // the tile's rows behind the last see nothing
       const bool whole = i0 + 64 <= sq.lq && all_seen(sq, a.causal, a.window, pos0, pos0 + 63, j0, j0 + kTile);
-      ok = __all_sync(0xffffffffu, mbar_wait(c.full(i % kStages), (i / kStages) & 1u, c.abort_flag) &&
-                                       mbar_wait(c.s(), i & 1u, c.abort_flag));
+      ok = __all_sync(0xffffffffu, mbar_wait(c.rows_full(i), (i >> 1) & 1u, c.abort_flag) &&
+                                       mbar_wait(c.s(0), i & 1u, c.abort_flag));
       if (!ok) break;
       tc_fence_after();
       float pr[64];
@@ -323,9 +359,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
 #pragma unroll
       for (int x = 0; x < 64; x += 4) {
         const float4 ls = *reinterpret_cast<const float4*>(neg_lse + x);
-        score.probs(pr[x], pr[x + 1], pair2(ls.x, ls.y), pos0 + x - j, pos0 + x + 1 - j, pr[x], pr[x + 1], cs[CAP ? x / 2 : 0]);
-        score.probs(pr[x + 2], pr[x + 3], pair2(ls.z, ls.w), pos0 + x + 2 - j, pos0 + x + 3 - j, pr[x + 2], pr[x + 3],
-                    cs[CAP ? x / 2 + 1 : 0]);
+        const bool poly = (x / 2 & 7) >= 8 - kPolys;         // known when unrolled
+        if (poly) {
+          score.template probs<true>(pr[x], pr[x + 1], pair2(ls.x, ls.y), pos0 + x - j, pos0 + x + 1 - j, pr[x], pr[x + 1],
+                                     cs[CAP ? x / 2 : 0]);
+          score.template probs<true>(pr[x + 2], pr[x + 3], pair2(ls.z, ls.w), pos0 + x + 2 - j, pos0 + x + 3 - j, pr[x + 2],
+                                     pr[x + 3], cs[CAP ? x / 2 + 1 : 0]);
+        } else {
+          score.template probs<false>(pr[x], pr[x + 1], pair2(ls.x, ls.y), pos0 + x - j, pos0 + x + 1 - j, pr[x], pr[x + 1],
+                                      cs[CAP ? x / 2 : 0]);
+          score.template probs<false>(pr[x + 2], pr[x + 3], pair2(ls.z, ls.w), pos0 + x + 2 - j, pos0 + x + 3 - j, pr[x + 2],
+                                      pr[x + 3], cs[CAP ? x / 2 + 1 : 0]);
+        }
       }
       if (!whole) {
         // rows that see this key: [r_lo, r_hi), or all where the key lies before the prefix
@@ -390,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(c.ds());
+      if (lane == 0) { mbar_arrive(c.ds()); mbar_arrive(c.rows_empty(i)); }
     }
     if (ok && n > 0) {
       ok = __all_sync(0xffffffffu, mbar_wait(c.acc(), 0, c.abort_flag));
@@ -417,18 +462,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
 template <int DP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_constant__ BwdParams p) {
   constexpr uint32_t TB = kTileBytes<DP>;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  const uint32_t q_tile = smem_u32(smem), do_tile = q_tile + TB, ring = q_tile + 2 * TB;
-  uint8_t* ctl = smem + (2 + 2 * kStages) * TB + kStages * kRowBytes;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t q_tile = smem_u32(smem), do_tile = q_tile + TB;
+  auto k_at = [&](int i) { return q_tile + (2 + i % kStagesA) * TB; };
+  auto v_at = [&](int i) { return q_tile + (2 + kStagesA + i % kStagesB) * TB; };
+  uint8_t* ctl = smem + (2 + kStagesA + kStagesB) * TB + 2 * kRowBytes;
   uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * kBars);
   const Ctl c{smem_u32(ctl), reinterpret_cast<volatile int*>(slot + 1)};
   const AttnArgs& a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int head = blockIdx.x % a.q_heads;
   int seq, index;
-  if (!block_begin(a.q_off, a.n_seqs, a.q_rows, blockIdx.x / a.q_heads, true, 1, c, slot, &seq, &index)) return;
-  const uint32_t tmem = *slot;
+  if (!block_begin(a.q_off, a.n_seqs, a.q_rows, blockIdx.x / a.q_heads, true, c, slot, &seq, &index)) return;
+  const uint32_t tmem = warp_uniform(*slot);
   const uint32_t t_dp = tmem + 2 * kTile, t_dq = tmem + 3 * kTile;
   const AttnSeq sq = load_seq(a, seq);
   const int i0 = index * kTile, rows = min(kTile, sq.lq - i0);
@@ -446,55 +492,53 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
         load_tile<DP>(do_tile, &p.do_map, c.own(), head, sq.q0 + i0);
       }
       for (int i = 0; i < n; ++i) {
-        const int st = i % kStages;
-        if (!mbar_wait(c.empty(st), ((i / kStages) & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
-        mbar_expect_tx(c.full(st), 2 * TB);
-        load_tile<DP>(ring + st * 2 * TB, &p.k_map, c.full(st), kvh, sq.k0 + tiles.at(i) * kTile);
-        load_tile<DP>(ring + st * 2 * TB + TB, &p.v_map, c.full(st), kvh, sq.k0 + tiles.at(i) * kTile);
+        if (!c.wait_empty_a(i)) { ok = false; break; }
+        mbar_expect_tx(c.full_a(i), TB);
+        load_tile<DP>(k_at(i), &p.k_map, c.full_a(i), kvh, sq.k0 + tiles.at(i) * kTile);
+        if (!c.wait_empty_b(i)) { ok = false; break; }
+        mbar_expect_tx(c.full_b(i), TB);
+        load_tile<DP>(v_at(i), &p.v_map, c.full_b(i), kvh, sq.k0 + tiles.at(i) * kTile);
       }
       if (!ok) give_up(c, a.status);
     }
   } else if (warp == kMmaWarp) {
-    bool ok = n == 0 || mbar_wait(c.own(), 0, c.abort_flag);
-    auto arrived = [&](int i) {
-      if (!__all_sync(0xffffffffu, mbar_wait(c.full(i % kStages), (i / kStages) & 1u, c.abort_flag))) return false;
+    const bool one = elect_one();
+    bool ok = n == 0 || __all_sync(0xffffffffu, mbar_wait(c.own(), 0, c.abort_flag));
+    auto scores = [&](int i) {                               // over ds of two tiles ago, which its product has read
+      if (!__all_sync(0xffffffffu, c.wait_full_a(i))) return false;
       const int valid = sq.lk - tiles.at(i) * kTile;
       if (valid < kTile) {
-        clear_rows<DP>(ring + (i % kStages) * 2 * TB, valid);
+        clear_rows<DP>(k_at(i), valid);
         fence_proxy_async_smem();
         __syncwarp();
       }
       tc_fence_after();
+      if (one) {
+        issue_nt<DP>(tmem + (i & 1) * kTile, q_tile, k_at(i));
+        umma_commit(c.s(i & 1));
+      }
       return true;
     };
-    ok = __all_sync(0xffffffffu, ok) && (n == 0 || arrived(0));
-    if (ok && n > 0 && lane == 0) {
-      issue_nt<DP>(tmem, q_tile, ring);
-      umma_commit(c.s());
-      issue_nt<DP>(t_dp, do_tile, ring + TB);
-      umma_commit(c.dp());
-    }
-    for (int i = 0; i < n && ok; ++i) {
-      const uint32_t kt = ring + (i % kStages) * 2 * TB;
-      const uint32_t nk = ring + ((i + 1) % kStages) * 2 * TB;
-      if (i + 1 < n) {
-        ok = arrived(i + 1);
-        if (!ok) break;
-        if (lane == 0) {                                     // over ds of two tiles ago, which its product has read
-          issue_nt<DP>(tmem + ((i + 1) & 1) * kTile, q_tile, nk);
-          umma_commit(c.s() + 8u * ((i + 1) & 1));
-        }
+    auto grads = [&](int i) {
+      if (!__all_sync(0xffffffffu, c.wait_full_b(i))) return false;
+      tc_fence_after();
+      if (one) {
+        issue_nt<DP>(t_dp, do_tile, v_at(i));
+        umma_commit(c.dp());
+        umma_commit(c.empty_b(i));
       }
-      ok = __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
+      return true;
+    };
+    ok = ok && (n == 0 || (scores(0) && grads(0)));
+    for (int i = 0; i < n && ok; ++i) {
+      ok = (i + 1 >= n || scores(i + 1)) && __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
       if (!ok) break;
       tc_fence_after();
-      if (lane == 0) {
-        if (i + 1 < n) {
-          issue_nt<DP>(t_dp, do_tile, nk + TB);
-          umma_commit(c.dp());
-        }
-        issue_ts<DP>(t_dq, tmem + (i & 1) * kTile, kt, i > 0);
-        umma_commit(c.empty(i % kStages));
+      ok = i + 1 >= n || grads(i + 1);
+      if (!ok) break;
+      if (one) {
+        issue_ts<DP>(t_dq, tmem + (i & 1) * kTile, k_at(i), i > 0);
+        umma_commit(c.empty_a(i));
         if (i + 1 == n) umma_commit(c.acc());
       }
     }
@@ -516,7 +560,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
       const int j0 = tiles.at(i) * kTile + half * 64;
       const bool whole = all_seen(sq, a.causal, a.window, p0, p1, j0, j0 + 64);
       const uint32_t s_addr = tmem + (i & 1) * kTile + lanes + half * 64;
-      ok = __all_sync(0xffffffffu, mbar_wait(c.s() + 8u * (i & 1), (i >> 1) & 1u, c.abort_flag));
+      ok = __all_sync(0xffffffffu, mbar_wait(c.s(i & 1), (i >> 1) & 1u, c.abort_flag));
       if (!ok) break;
       tc_fence_after();
       float pr[64];
@@ -526,7 +570,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
 #pragma unroll
       for (int x = 0; x < 64; x += 2) {
         uint64_t cs;
-        score.probs(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
+        if ((x / 2 & 7) >= 8 - kPolys)
+          score.template probs<true>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
+        else
+          score.template probs<false>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
         if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
       }
       if (!whole) {
@@ -578,34 +625,54 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
   block_end(c, tmem);
 }
 
-// delta = sum over the head of o * d_o, and the log-sum-exp in base 2 (+inf, i.e. p = 0, for rows that see nothing):
-// 16 lanes per (row, head), heads fastest so that a warp reads neighbouring memory.
+// delta = sum over the head of o * d_o, and the log-sum-exp in base 2 (+inf, i.e. p = 0, for rows that see nothing).
+// Bound by reading o and d_o once: a block takes 8 rows of 32 heads, 16 lanes to a (row, head), with the loads of four
+// of them in flight per lane; the results go through shared memory so that a head's 8 rows are written together.
+constexpr int kDeltaRows = 8, kDeltaHeads = 32;
 template <typename T>
 __global__ void __launch_bounds__(256) attn_delta_kernel(AttnArgs a, float* lse2, float* delta) {
-  const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4;
-  const int l = threadIdx.x & 15;
-  const long long total = (long long)a.q_rows * a.q_heads;
-  const bool on = item < total;
-  const long long row = on ? item / a.q_heads : 0;
-  const int head = on ? (int)(item - row * a.q_heads) : 0;
-  const T* o = reinterpret_cast<const T*>(a.o) + row * a.o_stride + (size_t)head * a.head_dim;
-  const T* d = reinterpret_cast<const T*>(a.d_o) + row * a.o_stride + (size_t)head * a.head_dim;
-  constexpr int V = 16 / sizeof(T);
-  float sum = 0.f;
-  if (on)
-    for (int c = l * V; c < a.head_dim; c += 16 * V) {
-      const uint4 x = *reinterpret_cast<const uint4*>(o + c), y = *reinterpret_cast<const uint4*>(d + c);
-      const T* xe = reinterpret_cast<const T*>(&x);
-      const T* ye = reinterpret_cast<const T*>(&y);
+  constexpr int V = 16 / sizeof(T), ITEMS = 4, CHUNKS = sizeof(T) == 2 ? 1 : 2;   // a head is at most 128 values
+  __shared__ float sums[kDeltaHeads * kDeltaRows];
+  const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int head_blocks = (a.q_heads + kDeltaHeads - 1) / kDeltaHeads;
+  const int row0 = blockIdx.x / head_blocks * kDeltaRows, head0 = blockIdx.x % head_blocks * kDeltaHeads;
+#pragma unroll 1
+  for (int i0 = 0; i0 < kDeltaRows * kDeltaHeads; i0 += 16 * ITEMS) {
+    uint4 x[ITEMS][CHUNKS], y[ITEMS][CHUNKS];
 #pragma unroll
-      for (int e = 0; e < V; ++e) sum += (float)xe[e] * (float)ye[e];
+    for (int n = 0; n < ITEMS; ++n) {
+      const int i = i0 + n * 16 + g, row = row0 + i / kDeltaHeads, head = head0 + i % kDeltaHeads;
+      const size_t at = (size_t)row * a.o_stride + (size_t)head * a.head_dim;
+#pragma unroll
+      for (int k = 0; k < CHUNKS; ++k) {
+        const int c = (k * 16 + l) * V;
+        const bool on = row < a.q_rows && head < a.q_heads && c < a.head_dim;
+        x[n][k] = on ? *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.o) + at + c) : make_uint4(0, 0, 0, 0);
+        y[n][k] = on ? *reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.d_o) + at + c) : make_uint4(0, 0, 0, 0);
+      }
     }
 #pragma unroll
-  for (int f = 8; f >= 1; f >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, f);
-  if (on && l == 0) {
+    for (int n = 0; n < ITEMS; ++n) {
+      const int i = i0 + n * 16 + g;
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < CHUNKS; ++k) {
+        const T* xe = reinterpret_cast<const T*>(&x[n][k]);
+        const T* ye = reinterpret_cast<const T*>(&y[n][k]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum += (float)xe[e] * (float)ye[e];
+      }
+#pragma unroll
+      for (int f = 8; f >= 1; f >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, f);
+      if (l == 0) sums[(i % kDeltaHeads) * kDeltaRows + i / kDeltaHeads] = sum;
+    }
+  }
+  __syncthreads();
+  const int head = head0 + threadIdx.x / kDeltaRows, row = row0 + threadIdx.x % kDeltaRows;
+  if (head < a.q_heads && row < a.q_rows) {
     const size_t at = (size_t)head * a.q_rows + row;
     const float z = a.lse[at];
-    delta[at] = sum;
+    delta[at] = sums[threadIdx.x];
     lse2[at] = z == -INFINITY ? INFINITY : z * kLog2e;
   }
 }
@@ -633,7 +700,7 @@ cudaError_t launch_dp(const BwdParams& p, unsigned gk, unsigned gq, cudaStream_t
 }  // namespace
 
 cudaError_t launch_attn_delta(const AttnArgs& a, bool bf16_mode, float* lse2, float* delta, cudaStream_t st) {
-  const long long blocks = ((long long)a.q_rows * a.q_heads + 15) / 16;
+  const long long blocks = ((long long)a.q_rows + kDeltaRows - 1) / kDeltaRows * ((a.q_heads + kDeltaHeads - 1) / kDeltaHeads);
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
   if (blocks == 0) return cudaSuccess;
   if (bf16_mode) attn_delta_kernel<bf16><<<(unsigned)blocks, 256, 0, st>>>(a, lse2, delta);

@@ -324,11 +324,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
           float l0, l1;
           unpair2(add2(acc[0], acc[1]), l0, l1);
           sum = l0 + l1;
+          tmem_st32(s_addr + c * 32, pk);                    // over scores of the tile's first half
           reset = sum > 0x1p100f;
           if (!__any_sync(0xffffffffu, reset)) break;
         }
         if (!ok) break;
-        tmem_st32(s_addr + c * 32, pk);                      // over scores of the tile's first half
         l += sum;
         tile_sum += sum;
         tmem_st_wait();
