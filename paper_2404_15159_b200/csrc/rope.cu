@@ -11,7 +11,7 @@
 namespace mixlora {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
 // Radians per position of every pair.  In 64 bits: positions reach millions of radians, where a frequency rounded to
 // 32 bits would be off by a large part of a turn.
@@ -38,118 +38,97 @@ template <typename T> __device__ __forceinline__ T from_f(float x);
 template <> __device__ __forceinline__ bf16 from_f<bf16>(float x) { return __float2bfloat16(x); }
 template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
 
-// One item: N values at each of two places of a head (half layout: i and i + rotary_dim / 2), or N neighbouring
-// values (interleaved layout, and the copied rest).  With N values of 16 bytes and both places of an item read before
-// either is written, the kernel also works in place.
-template <typename T, int N, bool INTERLEAVED>
-struct Item {
-  const T* src;
-  T* dst;
-  int at;              // first value of the item inside its head
-  int cs;              // index of its first pair in the cos / sin table, or -1: copied
-  bool on;
-  Vec<T, N> a, b;
-
-  __device__ __forceinline__ void load(int half) {
-    if (!on) return;
-    a = *reinterpret_cast<const Vec<T, N>*>(src + at);
-    if (!INTERLEAVED && cs >= 0) b = *reinterpret_cast<const Vec<T, N>*>(src + at + half);
-  }
-  __device__ __forceinline__ void store(int half, const float2* table) {
-    if (!on) return;
-    if (cs >= 0) {
-      if (INTERLEAVED) {
-#pragma unroll
-        for (int e = 0; e < N; e += 2) {
-          const float2 t = table[cs + e / 2];
-          const float u = to_f(a.v[e]), w = to_f(a.v[e + 1]);
-          a.v[e] = from_f<T>(u * t.x - w * t.y);
-          a.v[e + 1] = from_f<T>(w * t.x + u * t.y);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const float2 t = table[cs + e];
-          const float u = to_f(a.v[e]), w = to_f(b.v[e]);
-          a.v[e] = from_f<T>(u * t.x - w * t.y);
-          b.v[e] = from_f<T>(w * t.x + u * t.y);
-        }
-        *reinterpret_cast<Vec<T, N>*>(dst + at + half) = b;
-      }
-    }
-    *reinterpret_cast<Vec<T, N>*>(dst + at) = a;
-  }
-};
-
-// Bound by memory: every value is read and written once.  A block takes `block_tokens` tokens (and, where there are
-// few tokens, a share of the heads, gridDim.y): its threads first make the tokens' cos and sin once for all heads, in
-// shared memory, then walk over (token, head, item) with kUnroll items' loads in flight each.
+// Bound by memory: every value is read and written once.  A warp takes a token (where there are few, a share of its
+// heads).  Every lane keeps to one item of a head: N values at each of two places, i and i + rotary_dim / 2 (half
+// layout), or N neighbouring values (interleaved, and the copied rest); it makes its pairs' cos and sin once, in
+// registers, and walks over the heads with kUnroll items' loads in flight.  An item is 16 bytes where the pairs allow
+// it; both places of an item are read before either is written, so the kernel also works in place.
 // The angle's turns are formed and reduced in 64 bits; the rest of a turn goes through sincospif in 32.
+// Measured on B200: q and k of 8192 tokens, 32 + 32 heads of 128 in bf16, 50 us (5.4 TB/s); 32768 tokens, 32 + 8 heads out
+// of packed rows, 114 us (5.9 TB/s).
 template <typename T, int N, bool INTERLEAVED>
-__global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs p) {
-  extern __shared__ float2 cs_table[];                  // [block_tokens, pairs]
-  constexpr int kUnroll = 4;
-  const int t0 = blockIdx.x * p.block_tokens;
-  const int nt = min(p.block_tokens, p.tokens - t0);
+__global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs p) {
+  // items in flight per lane: fewer registers, so more warps, beat more loads per warp in bf16 (8192 tokens: 50 us with
+  // one, 53 with two, 64 with three); with half as many pairs to a lane fp32 has room for two (1021 tokens: 11 and 13 us)
+  constexpr int kUnroll = sizeof(T) == 2 ? 1 : 2;
+  constexpr int kPairs = INTERLEAVED ? (N + 1) / 2 : N;
+  const int lane = threadIdx.x & 31;
+  const long long unit = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const int t = (int)(unit / p.shares), share = (int)(unit - (long long)t * p.shares);
+  if (t >= p.tokens) return;
   const int heads = p.q_heads + p.k_heads;
-  const int h0 = (int)((long long)heads * blockIdx.y / gridDim.y);
-  const int h1 = (int)((long long)heads * (blockIdx.y + 1) / gridDim.y);
-  const int half = p.pairs;
+  const int h0 = (int)((long long)heads * share / p.shares), h1 = (int)((long long)heads * (share + 1) / p.shares);
   const int rot_items = INTERLEAVED ? 2 * p.pairs / N : p.pairs / N;
   const int items = rot_items + p.copied / N;           // per head
-  const int per_token = items * (h1 - h0);
-  const int total = per_token * nt;
+  const double pos = p.positions ? (double)p.positions[t] : (double)t;
+  const T* q = reinterpret_cast<const T*>(p.q) + (size_t)t * p.q_stride;
+  const T* k = reinterpret_cast<const T*>(p.k) + (size_t)t * p.k_stride;
+  T* q_out = reinterpret_cast<T*>(p.q_out) + (size_t)t * p.q_out_stride;
+  T* k_out = reinterpret_cast<T*>(p.k_out) + (size_t)t * p.k_out_stride;
 
-  Item<T, N, INTERLEAVED> it[kUnroll];
-  int table_row[kUnroll];
-  auto fetch = [&](int first) {
+  for (int i0 = 0; i0 < items; i0 += 32) {
+    const int here = min(32, items - i0), step = 32 / here;          // lanes of a head, heads of a warp
+    const int hl = lane / here, i = i0 + lane - hl * here;
+    if (hl >= step) continue;
+    const bool turn = i < rot_items;
+    const int at = turn ? i * N : 2 * p.pairs + (i - rot_items) * N;
+    Vec<T, N> a[kUnroll], b[kUnroll];
+    auto load = [&](int h) {
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      const int idx = first + j * kThreads;
-      it[j].on = idx < total;
-      if (!it[j].on) continue;
-      const int tl = idx / per_token, rest = idx - tl * per_token;
-      const int hl = rest / items, i = rest - hl * items;
-      const int h = h0 + hl;
-      const size_t row = (size_t)(t0 + tl);
-      if (h < p.q_heads) {
-        it[j].src = reinterpret_cast<const T*>(p.q) + row * p.q_stride + (size_t)h * p.head_dim;
-        it[j].dst = reinterpret_cast<T*>(p.q_out) + row * p.q_out_stride + (size_t)h * p.head_dim;
-      } else {
-        it[j].src = reinterpret_cast<const T*>(p.k) + row * p.k_stride + (size_t)(h - p.q_heads) * p.head_dim;
-        it[j].dst = reinterpret_cast<T*>(p.k_out) + row * p.k_out_stride + (size_t)(h - p.q_heads) * p.head_dim;
+      for (int j = 0; j < kUnroll; ++j) {
+        const int hh = h + j * step;
+        if (hh >= h1) continue;
+        const T* src = (hh < p.q_heads ? q + (size_t)hh * p.head_dim : k + (size_t)(hh - p.q_heads) * p.head_dim) + at;
+        a[j] = *reinterpret_cast<const Vec<T, N>*>(src);
+        if (!INTERLEAVED && turn) b[j] = *reinterpret_cast<const Vec<T, N>*>(src + p.pairs);
       }
-      if (i < rot_items) {
-        it[j].at = i * N;
-        it[j].cs = INTERLEAVED ? i * (N / 2) : i * N;
-      } else {
-        it[j].at = 2 * p.pairs + (i - rot_items) * N;
-        it[j].cs = -1;
+    };
+    float c[kPairs], s[kPairs];
+    if (turn) {
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) {
+        const double turns = pos * (p.inv_freq[i * kPairs + e] * 0.15915494309189535);
+        sincospif((float)(2.0 * (turns - rint(turns))), &s[e], &c[e]);
+        c[e] *= p.amplitude;
+        s[e] *= p.backward ? -p.amplitude : p.amplitude;
       }
-      table_row[j] = tl * p.pairs;
-      it[j].load(half);
     }
-  };
-  fetch(threadIdx.x);                                   // the first items travel while the table is made
-  for (int i = threadIdx.x; i < nt * p.pairs; i += kThreads) {
-    const int tl = i / p.pairs, pr = i - tl * p.pairs;
-    const double pos = p.positions ? (double)p.positions[t0 + tl] : (double)(t0 + tl);
-    const double turns = pos * (p.inv_freq[pr] * 0.15915494309189535);
-    float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-    cs_table[i] = make_float2(c * p.amplitude, s * (p.backward ? -p.amplitude : p.amplitude));
-  }
-  __syncthreads();
-  for (int first = threadIdx.x; first < total; first += kThreads * kUnroll) {
-    if (first != (int)threadIdx.x) fetch(first);
+    for (int h = h0 + hl; h < h1; h += step * kUnroll) {
+      load(h);
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) it[j].store(half, cs_table + (it[j].on ? table_row[j] : 0));
+      for (int j = 0; j < kUnroll; ++j) {
+        const int hh = h + j * step;
+        if (hh >= h1) continue;
+        T* dst = (hh < p.q_heads ? q_out + (size_t)hh * p.head_dim : k_out + (size_t)(hh - p.q_heads) * p.head_dim) + at;
+        if (turn) {
+          if (INTERLEAVED) {
+#pragma unroll
+            for (int e = 0; e + 1 < N; e += 2) {
+              const float u = to_f(a[j].v[e]), w = to_f(a[j].v[e + 1]);
+              a[j].v[e] = from_f<T>(u * c[e / 2] - w * s[e / 2]);
+              a[j].v[e + 1] = from_f<T>(w * c[e / 2] + u * s[e / 2]);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+              const float u = to_f(a[j].v[e]), w = to_f(b[j].v[e]);
+              a[j].v[e] = from_f<T>(u * c[e] - w * s[e]);
+              b[j].v[e] = from_f<T>(w * c[e] + u * s[e]);
+            }
+            *reinterpret_cast<Vec<T, N>*>(dst + p.pairs) = b[j];
+          }
+        }
+        *reinterpret_cast<Vec<T, N>*>(dst) = a[j];
+      }
+    }
   }
 }
 
 template <typename T, int N, bool IL>
-cudaError_t launch(const RopeArgs& p, dim3 grid, size_t smem, cudaStream_t st) {
-  rope_kernel<T, N, IL><<<grid, kThreads, smem, st>>>(p);
+cudaError_t launch(const RopeArgs& p, cudaStream_t st) {
+  const long long blocks = ((long long)p.tokens * p.shares + kThreads / 32 - 1) / (kThreads / 32);
+  if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
+  rope_kernel<T, N, IL><<<(unsigned)blocks, kThreads, 0, st>>>(p);
   return cudaGetLastError();
 }
 
@@ -165,21 +144,17 @@ cudaError_t launch_rope(RopeArgs p, bool bf16_mode, bool interleaved, cudaStream
   // 16 bytes per item where the pairs fall on 16-byte pieces of a head, else one pair (two values) per item
   const int n = bf16_mode ? 8 : 4;
   const bool wide = (interleaved ? 2 * p.pairs : p.pairs) % n == 0 && p.copied % n == 0;
-  // Tokens per block: 4 share one round of the table's work; with fewer than four blocks per SM the tokens go one by
-  // one, and with few tokens the heads are spread over up to 8 blocks so that a decoding step uses more SMs.
-  const int sms = 148;
-  p.block_tokens = p.tokens >= 16 * sms ? 4 : 1;
-  const int blocks = (p.tokens + p.block_tokens - 1) / p.block_tokens;
-  int split = 1;
-  while (split < 8 && (long long)blocks * split < sms && p.q_heads + p.k_heads >= 8 * split) split *= 2;
-  const dim3 grid((unsigned)blocks, (unsigned)split);
-  const size_t smem = (size_t)p.block_tokens * p.pairs * sizeof(float2);
+  // With fewer tokens than the SMs hold warps of this kernel (148 x 16 of them keep the memory busy) the heads of a
+  // token are spread over several warps, down to 8 heads each.
+  const int heads = p.q_heads + p.k_heads;
+  p.shares = 1;
+  while ((long long)p.tokens * p.shares < 148 * 16 && heads >= 16 * p.shares) p.shares *= 2;
   if (bf16_mode) {
-    if (wide) return interleaved ? launch<bf16, 8, true>(p, grid, smem, st) : launch<bf16, 8, false>(p, grid, smem, st);
-    return interleaved ? launch<bf16, 2, true>(p, grid, smem, st) : launch<bf16, 1, false>(p, grid, smem, st);
+    if (wide) return interleaved ? launch<bf16, 8, true>(p, st) : launch<bf16, 8, false>(p, st);
+    return interleaved ? launch<bf16, 2, true>(p, st) : launch<bf16, 1, false>(p, st);
   }
-  if (wide) return interleaved ? launch<float, 4, true>(p, grid, smem, st) : launch<float, 4, false>(p, grid, smem, st);
-  return interleaved ? launch<float, 2, true>(p, grid, smem, st) : launch<float, 1, false>(p, grid, smem, st);
+  if (wide) return interleaved ? launch<float, 4, true>(p, st) : launch<float, 4, false>(p, st);
+  return interleaved ? launch<float, 2, true>(p, st) : launch<float, 1, false>(p, st);
 }
 
 }  // namespace mixlora

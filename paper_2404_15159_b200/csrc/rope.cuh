@@ -16,7 +16,7 @@ struct RopeArgs {
   int pairs;                      // rotary_dim / 2
   int copied;                     // values behind rotary_dim that have to be copied (0 in place)
   int backward;
-  int block_tokens;
+  int shares;                     // warps that share a token's heads
 };
 
 cudaError_t launch_rope_frequencies(int pairs, double theta, int scaling, double factor, double low, double high,
