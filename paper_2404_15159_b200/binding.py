@@ -222,8 +222,14 @@ def _ptr(t):
     return t.data_ptr()
 
 
+# the current stream's handle without building a Stream object around it (1 us of a call's 5)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 

@@ -202,6 +202,17 @@ __device__ __forceinline__ float tanh_fast(float x) {
   return 1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kLog2e)));
 }
 
+// Lets a kernel use `bytes` of dynamic shared memory: asked of the runtime once per kernel and device.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev >= 0 && dev < 64 && done[dev])) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;      // a race only repeats the call
+  return e;
+}
+
 cudaError_t launch_attn_forward_tc(const AttnArgs& p, cudaStream_t st);
 cudaError_t launch_attn_backward_tc(const AttnArgs& p, cudaStream_t st);
 cudaError_t launch_attn_forward_simt(const AttnArgs& p, cudaStream_t st);
@@ -211,7 +222,8 @@ cudaError_t launch_attn_delta(const AttnArgs& p, bool bf16_mode, float* lse2, fl
 // Few query rows for each sequence and key head: a split over the keys, joined by a second launch.
 constexpr int kFewRows = 16;                     // rows of a block
 constexpr int kFewRowsMax = 64;                  // rows of a sequence and key head up to which this form is taken
-int attn_few_splits(int n_seqs, int kv_heads, int rows, long long k_rows, int max_k_len);
-cudaError_t launch_attn_few(const AttnArgs& p, bool bf16_mode, int splits, float* part, cudaStream_t st);
+struct FewSplits { int count; bool cluster; };   // more than one without a cluster: partials in the workspace
+FewSplits attn_few_splits(int n_seqs, int kv_heads, int rows, long long k_rows, int max_k_len);
+cudaError_t launch_attn_few(const AttnArgs& p, bool bf16_mode, FewSplits splits, float* part, cudaStream_t st);
 
 }  // namespace mixlora

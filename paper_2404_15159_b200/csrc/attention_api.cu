@@ -85,7 +85,7 @@ int few_rows(const mixlora_attention_shape_t& s) {
   const long long rows = (long long)s.max_q_len * (s.q_heads / s.kv_heads);
   return rows > 0 && rows <= kFewRowsMax ? (int)rows : 0;
 }
-int splits_of(const mixlora_attention_shape_t& s) {
+FewSplits splits_of(const mixlora_attention_shape_t& s) {
   return attn_few_splits(s.n_seqs, s.kv_heads, few_rows(s), s.k_rows, s.max_k_len);
 }
 
@@ -95,9 +95,10 @@ AttnLayout attention_layout(const mixlora_attention_shape_t& s, bool backward) {
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
   L.status = take(256);
-  const int rows = few_rows(s), splits = rows ? splits_of(s) : 1;
+  const int rows = few_rows(s);
+  const FewSplits sp = rows ? splits_of(s) : FewSplits{1, false};
   const size_t chunks = (size_t)(rows + kFewRows - 1) / kFewRows;
-  L.part = take(splits > 1 ? (size_t)s.n_seqs * s.kv_heads * chunks * splits * kFewRows * (s.head_dim + 2) * 4 : 0);
+  L.part = take(sp.count > 1 && !sp.cluster ? (size_t)s.n_seqs * s.kv_heads * chunks * sp.count * kFewRows * (s.head_dim + 2) * 4 : 0);
   const size_t per_row = backward ? (size_t)s.q_heads * s.q_rows * 4 : 0;
   L.lse2 = take(per_row);
   L.delta = take(per_row);

@@ -679,10 +679,9 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(AttnArgs a, float* lse2
 
 template <int DP, bool CAP, bool BIAS>
 cudaError_t launch(const BwdParams& p, unsigned grid_kv, unsigned grid_q, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(attn_bwd_kv_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       kSmemBytes<DP>);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(attn_bwd_q_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<DP>);
+  static bool done_kv[64], done_q[64];
+  cudaError_t e = allow_smem(attn_bwd_kv_kernel<DP, CAP, BIAS>, kSmemBytes<DP>, done_kv);
+  if (e == cudaSuccess) e = allow_smem(attn_bwd_q_kernel<DP, CAP, BIAS>, kSmemBytes<DP>, done_q);
   if (e != cudaSuccess) return e;
   if (grid_kv) {
     attn_bwd_kv_kernel<DP, CAP, BIAS><<<grid_kv, kThreads, kSmemBytes<DP>, st>>>(p);

@@ -3,8 +3,7 @@
 // The rows of a sequence that share a key head (its query heads times the sequence's new tokens) are the
 // 16 rows of one m16n8k16 product, so that every key and value is read once for all of them (more rows go to several
 // blocks, which find the keys in L2).  The keys of a (sequence,
-// key head) are split over several blocks where there are few of those; each leaves (m, l, sum p v) and a second
-// launch joins them in index order.
+// key head) are split over several blocks where there are few of those, which join their (m, l, sum p v) in index order.
 #include "attention.cuh"
 
 namespace mixlora {
@@ -14,10 +13,13 @@ constexpr int kWarps = 4;
 constexpr int kStep = 16;                        // keys per step of a warp
 constexpr int kStages = 3;
 
+constexpr int kClusterMax = 8;                   // a cluster's blocks, in every configuration
+
 struct FewParams {
   AttnArgs a;
   float* part;                                   // [seq, key head, chunk, split, 16 rows, head_dim + 2]: sum p v, m (base 2), l
   int splits, rows, chunks;                      // rows = group * max_q_len, in chunks of kFewRows
+  bool cluster;                                  // the splits of a (sequence, key head) are one cluster
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -85,39 +87,101 @@ struct ScoreMap {
   }
 };
 
-// Joins the warps' states of a block in warp order and writes the block's result: the rows themselves, or a partial.
-// `st_m`, `st_l` [kWarps][16], `st_o` [kWarps][16][DP] in shared memory.
+// A row's result: o / l, and the log-sum-exp
 template <typename T>
-__device__ __forceinline__ void finish_block(const FewParams& p, const Share& w, const float* st_m, const float* st_l,
-                                             const float* st_o, int dp) {
+__device__ __forceinline__ void write_result(const FewParams& p, const Share& w, int qi, int head, int c, float o, float l,
+                                             float m) {
+  const AttnArgs& a = p.a;
+  const size_t row = (size_t)(w.sq.q0 + qi);
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  T* out = reinterpret_cast<T*>(a.out) + row * a.o_stride + (size_t)head * a.head_dim + c;
+  if constexpr (sizeof(T) == 2) *out = __float2bfloat16(o * inv);
+  else *out = o * inv;
+  if (c == 0 && a.lse) a.lse[(size_t)head * a.q_rows + row] = (m + log2f(l)) * kLn2;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A value at this shared-memory address in block `rank` of the cluster
+__device__ __forceinline__ float load_from(const float* mine, int rank) {
+  uint32_t addr;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_addr(mine)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// Joins the warps' states of a block in warp order, then the splits in index order: through the cluster's shared memory,
+// or through a partial in the workspace and a second launch.
+// `st_m`, `st_l` [kWarps][16], `st_o` [kWarps][16][DP] in shared memory; the block's own sums go over warp 0's.
+template <typename T>
+__device__ __forceinline__ void finish_block(const FewParams& p, const Share& w, float* st_m, float* st_l, float* st_o,
+                                             int dp) {
   const AttnArgs& a = p.a;
   const int d = a.head_dim;
+  const bool cluster = p.cluster;
+  // a thread owns the same (row, value)s in all passes, but reads every warp's m and l of its rows
+  float keep_m = -INFINITY, keep_l = 0.f;
+  if (threadIdx.x < 16) {
+    float m = -INFINITY, l = 0.f;
+    for (int x = 0; x < kWarps; ++x) m = fmaxf(m, st_m[x * 16 + threadIdx.x]);
+    for (int x = 0; x < kWarps; ++x) {
+      const float mx = st_m[x * 16 + threadIdx.x], f = mx == -INFINITY ? 0.f : ex2(mx - m);
+      l += f * st_l[x * 16 + threadIdx.x];
+    }
+    keep_m = m;
+    keep_l = l;
+  }
   for (int i = threadIdx.x; i < w.rows * d; i += kWarps * 32) {
+    const int r = i / d, c = i - r * d;
+    float m = -INFINITY, o = 0.f;
+    for (int x = 0; x < kWarps; ++x) m = fmaxf(m, st_m[x * 16 + r]);
+    for (int x = 0; x < kWarps; ++x) {
+      const float f = st_m[x * 16 + r] == -INFINITY ? 0.f : ex2(st_m[x * 16 + r] - m);
+      o += f * st_o[(x * 16 + r) * dp + c];
+    }
+    st_o[r * dp + c] = o;
+  }
+  __syncthreads();
+  if (threadIdx.x < 16) { st_m[threadIdx.x] = keep_m; st_l[threadIdx.x] = keep_l; }
+  if (cluster) cluster_sync();
+  else __syncthreads();
+  // the cluster's blocks share the row's values out among themselves
+  const int first = cluster ? w.split : 0, step = cluster ? p.splits : 1;
+  for (int i = threadIdx.x + first * kWarps * 32; i < w.rows * d; i += step * kWarps * 32) {
     const int r = i / d, c = i - r * d;
     const int qi = (w.row0 + r) / a.group, head = w.kvh * a.group + (w.row0 + r - qi * a.group);
     if (qi >= w.lq) continue;
-    float m = -INFINITY;
-    for (int x = 0; x < kWarps; ++x) m = fmaxf(m, st_m[x * 16 + r]);
-    float l = 0.f, o = 0.f;
-    for (int x = 0; x < kWarps; ++x) {
-      const float f = st_m[x * 16 + r] == -INFINITY ? 0.f : ex2(st_m[x * 16 + r] - m);
-      l += f * st_l[x * 16 + r];
-      o += f * st_o[(x * 16 + r) * dp + c];
+    float m = st_m[r], l = st_l[r], o = st_o[r * dp + c];
+    if (cluster) {
+      float ms[kClusterMax];
+      m = -INFINITY;
+#pragma unroll
+      for (int s = 0; s < kClusterMax; ++s) {
+        ms[s] = s < p.splits ? load_from(st_m + r, s) : -INFINITY;
+        m = fmaxf(m, ms[s]);
+      }
+      l = 0.f;
+      o = 0.f;
+#pragma unroll
+      for (int s = 0; s < kClusterMax; ++s)
+        if (s < p.splits && ms[s] != -INFINITY) {
+          const float f = ex2(ms[s] - m);
+          l += f * load_from(st_l + r, s);
+          o += f * load_from(st_o + r * dp + c, s);
+        }
     }
-    if (p.splits > 1) {
+    if (p.splits > 1 && !cluster) {
       const size_t block = (((size_t)w.seq * a.kv_heads + w.kvh) * p.chunks + w.row0 / kFewRows) * p.splits + w.split;
       float* dst = p.part + (block * kFewRows + r) * (d + 2);
       dst[c] = o;
       if (c == 0) { dst[d] = m; dst[d + 1] = l; }
     } else {
-      const size_t row = (size_t)(w.sq.q0 + qi);
-      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-      T* out = reinterpret_cast<T*>(a.out) + row * a.o_stride + (size_t)head * d + c;
-      if constexpr (sizeof(T) == 2) *out = __float2bfloat16(o * inv);
-      else *out = o * inv;
-      if (c == 0 && a.lse) a.lse[(size_t)head * a.q_rows + row] = (m + log2f(l)) * kLn2;
+      write_result<T>(p, w, qi, head, c, o, l, m);
     }
   }
+  if (cluster) cluster_sync();                   // nobody leaves while its shared memory is read
 }
 
 // bf16.  A warp takes every kWarps-th group of 16 keys; K and V of the next groups travel through its own ring of
@@ -424,19 +488,34 @@ __global__ void __launch_bounds__(128) attn_few_join_kernel(FewParams p) {
 
 constexpr size_t exchange_bytes(int dp) { return (size_t)kWarps * 16 * (dp + 2) * 4; }
 
+template <typename K>
+cudaError_t launch_blocks(K kernel, const FewParams& p, unsigned grid, size_t smem, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.splits;             // a (sequence, key head)'s splits are neighbouring blocks
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.cluster ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
 template <int DP, bool CAP, bool BIAS>
 cudaError_t launch_bf16(const FewParams& p, unsigned grid, cudaStream_t st) {
   constexpr size_t ring = (size_t)kWarps * kStages * 2 * kStep * DP * 2;
   constexpr size_t smem = ring > exchange_bytes(DP) ? ring : exchange_bytes(DP);
-  cudaError_t e = cudaFuncSetAttribute(attn_few_bf16_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static bool done[64];
+  cudaError_t e = allow_smem(attn_few_bf16_kernel<DP, CAP, BIAS>, (int)smem, done);
   if (e != cudaSuccess) return e;
-  attn_few_bf16_kernel<DP, CAP, BIAS><<<grid, kWarps * 32, smem, st>>>(p);
-  return cudaGetLastError();
+  return launch_blocks(attn_few_bf16_kernel<DP, CAP, BIAS>, p, grid, smem, st);
 }
 template <int LPK, int ROWS, bool CAP, bool BIAS>
 cudaError_t launch_f32(const FewParams& p, unsigned grid, cudaStream_t st) {
-  attn_few_f32_kernel<LPK, ROWS, CAP, BIAS><<<grid, kWarps * 32, exchange_bytes(LPK * 4), st>>>(p);
-  return cudaGetLastError();
+  return launch_blocks(attn_few_f32_kernel<LPK, ROWS, CAP, BIAS>, p, grid, exchange_bytes(LPK * 4), st);
 }
 template <bool CAP, bool BIAS>
 cudaError_t launch_mode(const FewParams& p, bool bf16_mode, unsigned grid, cudaStream_t st) {
@@ -451,30 +530,38 @@ cudaError_t launch_mode(const FewParams& p, bool bf16_mode, unsigned grid, cudaS
 
 }  // namespace
 
-// Splits of a (sequence, key head): enough blocks for about four rounds of the 2 x 148 that run together (lengths
-// differ, and short pieces even that out), but no piece under 256 keys, and none for the longest length alone.
-int attn_few_splits(int n_seqs, int kv_heads, int rows, long long k_rows, int max_k_len) {
+// Splits of a (sequence, key head), none under 256 keys.  Where the 2 x 148 blocks that run together are not reached
+// without splitting, and are with at most 8, the splits are one cluster and join in the same launch (a call on one
+// sequence of 1024 keys, 32 heads: 8 us, and 10 with a second launch).  Else there are enough for about four rounds of
+// blocks (lengths differ, and short pieces even that out), joined by a second launch (64 sequences of up to 8192 keys:
+// 186 us; clusters, which wait for a free group of SMs, 190).
+FewSplits attn_few_splits(int n_seqs, int kv_heads, int rows, long long k_rows, int max_k_len) {
   const long long pairs = (long long)n_seqs * kv_heads * ((rows + kFewRows - 1) / kFewRows);
-  if (pairs <= 0) return 1;
+  if (pairs <= 0) return FewSplits{1, false};
   long long longest = max_k_len > 0 ? max_k_len : (k_rows + n_seqs - 1) / n_seqs;
   if (longest > k_rows) longest = k_rows;
-  long long s = (4 * 2 * 148 + pairs - 1) / pairs;
-  const long long cap = (longest + 255) / 256;
-  if (s > cap) s = cap;
-  if (s > 256) s = 256;
-  return s < 1 ? 1 : (int)s;
+  const long long cap = longest > 256 ? (longest + 255) / 256 : 1;
+  auto fill = [&](long long blocks) {
+    const long long s = (blocks + pairs - 1) / pairs;
+    return s < cap ? s : cap;
+  };
+  const long long few = fill(2 * 148);
+  if (few <= 1 && pairs < 2 * 148) return FewSplits{1, false};
+  if (few > 1 && few <= kClusterMax) return FewSplits{(int)few, true};
+  const long long many = fill(4 * 2 * 148);
+  return FewSplits{(int)(many < 256 ? many : 256), false};
 }
 
-cudaError_t launch_attn_few(const AttnArgs& a, bool bf16_mode, int splits, float* part, cudaStream_t st) {
+cudaError_t launch_attn_few(const AttnArgs& a, bool bf16_mode, FewSplits splits, float* part, cudaStream_t st) {
   const int rows = a.group * a.max_q_len;
-  FewParams p{a, part, splits, rows, (rows + kFewRows - 1) / kFewRows};
-  const long long blocks = (long long)a.n_seqs * a.kv_heads * p.chunks * splits;
+  FewParams p{a, part, splits.count, rows, (rows + kFewRows - 1) / kFewRows, splits.cluster};
+  const long long blocks = (long long)a.n_seqs * a.kv_heads * p.chunks * p.splits;
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
   const unsigned grid = (unsigned)blocks;
   cudaError_t e;
   if (a.softcap > 0.f) e = a.slopes ? launch_mode<true, true>(p, bf16_mode, grid, st) : launch_mode<true, false>(p, bf16_mode, grid, st);
   else e = a.slopes ? launch_mode<false, true>(p, bf16_mode, grid, st) : launch_mode<false, false>(p, bf16_mode, grid, st);
-  if (e != cudaSuccess || splits <= 1) return e;
+  if (e != cudaSuccess || p.splits == 1 || p.cluster) return e;
   const long long items = (long long)a.n_seqs * a.kv_heads * p.rows;
   const unsigned jg = (unsigned)((items + 3) / 4);
   if (bf16_mode) attn_few_join_kernel<bf16><<<jg, 128, 0, st>>>(p);

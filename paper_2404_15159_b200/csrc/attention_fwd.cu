@@ -391,8 +391,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
 
 template <int DP, bool CAP, bool BIAS>
 cudaError_t launch(const FwdParams& p, unsigned grid, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(attn_fwd_tc_kernel<DP, CAP, BIAS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       kSmemBytes<DP>);
+  static bool done[64];
+  cudaError_t e = allow_smem(attn_fwd_tc_kernel<DP, CAP, BIAS>, kSmemBytes<DP>, done);
   if (e != cudaSuccess) return e;
   attn_fwd_tc_kernel<DP, CAP, BIAS><<<grid, kThreads, kSmemBytes<DP>, st>>>(p);
   return cudaGetLastError();
