@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmixlora.so")
 OBJ_DIR = os.path.join(PKG, "_build")
 SOURCES = ["api.cu", "router.cu", "simt_gemm.cu", "elementwise.cu", "tc_gemm.cu", "static_dispatch.cu", "grouped_swiglu.cu", "dora.cu",
-           "rope.cu", "attention_fwd.cu", "attention_bwd.cu", "attention_few.cu", "attention_simt.cu", "attention_api.cu"]
+           "rope.cu", "attention_plan.cu", "attention_fwd.cu", "attention_bwd.cu", "attention_few.cu", "attention_simt.cu",
+           "attention_api.cu"]
 HEADERS = [os.path.join(CSRC, "common.cuh"), os.path.join(CSRC, "tc_ptx.cuh"),
            os.path.join(CSRC, "rope.cuh"), os.path.join(CSRC, "attention.cuh"), os.path.join(ROOT, "include", "mixlora.h")]
 

@@ -8,6 +8,18 @@ namespace mixlora {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// One sequence: its rows and keys, and the position of its first row (query row i has position shift + i; key j has
+// position j, so that the last row stands at the last key).  Offsets come from device memory and are held inside the
+// tensors whatever they say.
+struct AttnSeq {
+  int q0, lq, k0, lk, shift, prefix;
+};
+// A tile of query rows or keys: its sequence and its first row (key) in it.
+struct alignas(32) AttnTile {
+  AttnSeq sq;
+  int row0, pad;
+};
+
 struct AttnArgs {
   const void *q, *k, *v;          // [rows, heads, head_dim], `*_stride` elements from row to row
   const void *o, *d_o;            // backward: the forward's output and its gradient, both with o's stride
@@ -18,6 +30,8 @@ struct AttnArgs {
   const float* delta;             // backward: sum over head_dim of o * d_o                    [q_heads, q_rows]
   const int32_t *q_off, *k_off;   // [n_seqs + 1]
   const int32_t *k_len, *prefix;  // [n_seqs] or NULL
+  const AttnTile *q_tiles, *k_tiles;  // tensor-core kernels: the planned tiles, longest work first, and their numbers
+  const int32_t *n_q_tiles, *n_k_tiles;
   const float* slopes;            // [q_heads] or NULL
   int32_t* status;
   long long q_stride, k_stride, v_stride, o_stride;
@@ -25,13 +39,6 @@ struct AttnArgs {
   int causal, window, max_q_len;
   float scale;                    // multiplies q . k
   float softcap;                  // > 0: scores become softcap * tanh(score / softcap)
-};
-
-// One sequence: its rows and keys, and the position of its first row (query row i has position shift + i; key j has
-// position j, so that the last row stands at the last key).  Offsets come from device memory and are held inside the
-// tensors whatever they say.
-struct AttnSeq {
-  int q0, lq, k0, lk, shift, prefix;
 };
 
 __device__ __forceinline__ int clamp_int(int v, int lo, int hi) { return min(max(v, lo), hi); }
@@ -196,6 +203,42 @@ __device__ __forceinline__ void ex2_poly(uint64_t x, float& e0, float& e1) {
   e1 = __uint_as_float((__float_as_uint(t1) << 23) + __float_as_uint(y1));
 }
 
+// A block's walk over (tile, head) pairs: rounds over the sorted tiles with the heads fastest, every other round from
+// the other end.  One 32-byte load tells a tile; the next one is fetched while this one is worked on.
+struct TileWalk {
+  const AttnTile* table;
+  int items, heads, round;
+  int4 ahead[2];
+  AttnSeq sq;
+  int row0, head;
+  __device__ __forceinline__ int item(int r) const {
+    return r * (int)gridDim.x + ((r & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x);
+  }
+  __device__ __forceinline__ void fetch(int r) {
+    const long long i = (long long)r * gridDim.x < items ? item(r) : items;
+    if (i < items) {
+      const int4* src = reinterpret_cast<const int4*>(table + i / heads);
+      ahead[0] = src[0];
+      ahead[1] = src[1];
+    }
+  }
+  __device__ __forceinline__ TileWalk(const AttnTile* t, const int32_t* n, int h)
+      : table(t), items(*n * h), heads(h), round(0) { fetch(0); }
+  __device__ __forceinline__ bool next() {
+    if ((long long)round * gridDim.x >= items) return false;
+    const int i = item(round);
+    if (i >= items) {                            // a gap of the last, partial round
+      ++round;
+      return false;
+    }
+    sq = AttnSeq{ahead[0].x, ahead[0].y, ahead[0].z, ahead[0].w, ahead[1].x, ahead[1].y};
+    row0 = ahead[1].z;
+    head = i % heads;
+    fetch(++round);
+    return true;
+  }
+};
+
 // tanh from two special-function operations: 1 - 2 / (1 + e^(2x)).  Its absolute error, a few 2^-24, is what counts
 // for a score (the relative one of a small x is bounded by the cap times that).
 __device__ __forceinline__ float tanh_fast(float x) {
@@ -212,6 +255,17 @@ cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64]) {
   if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;      // a race only repeats the call
   return e;
 }
+
+// Plans the tiles of `tile_rows` query rows (keys: of keys): `table` of `capacity` entries, `first` [n_seqs] scratch.  Also
+// clears the status word.
+struct AttnPlanJob {
+  AttnTile* table;
+  int32_t *count, *first;
+  int tile_rows, capacity, keys;
+};
+cudaError_t launch_attn_plan(const AttnArgs& p, const AttnPlanJob* jobs, int n_jobs, cudaStream_t st);
+int attn_sm_count();
+constexpr int kFwdTile = 256, kBwdTile = 128;
 
 cudaError_t launch_attn_forward_tc(const AttnArgs& p, cudaStream_t st);
 cudaError_t launch_attn_backward_tc(const AttnArgs& p, cudaStream_t st);

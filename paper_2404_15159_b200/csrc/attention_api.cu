@@ -89,7 +89,10 @@ FewSplits splits_of(const mixlora_attention_shape_t& s) {
   return attn_few_splits(s.n_seqs, s.kv_heads, few_rows(s), s.k_rows, s.max_k_len);
 }
 
-struct AttnLayout { size_t status, part, lse2, delta, total; };
+// Tiles of `tile` rows that `rows` rows in n_seqs sequences can have at most
+int tile_capacity(int rows, int n_seqs, int tile) { return (rows + tile - 1) / tile + n_seqs; }
+
+struct AttnLayout { size_t status, part, lse2, delta, q_tiles, k_tiles, q_first, k_first, total; };
 AttnLayout attention_layout(const mixlora_attention_shape_t& s, bool backward) {
   AttnLayout L;
   size_t off = 0;
@@ -102,8 +105,28 @@ AttnLayout attention_layout(const mixlora_attention_shape_t& s, bool backward) {
   const size_t per_row = backward ? (size_t)s.q_heads * s.q_rows * 4 : 0;
   L.lse2 = take(per_row);
   L.delta = take(per_row);
+  // plans of the tensor-core kernels; their tile counts sit in the status block
+  const bool tiled = s.dtype == MIXLORA_DTYPE_BF16 && (backward || !rows);
+  const size_t seqs = tiled ? (size_t)s.n_seqs : 0;
+  L.q_tiles = take(tiled ? (size_t)tile_capacity(s.q_rows, s.n_seqs, backward ? kBwdTile : kFwdTile) * sizeof(AttnTile) : 0);
+  L.k_tiles = take(tiled && backward ? (size_t)tile_capacity(s.k_rows, s.n_seqs, kBwdTile) * sizeof(AttnTile) : 0);
+  L.q_first = take(seqs * 4);
+  L.k_first = take(backward ? seqs * 4 : 0);
   L.total = off;
   return L;
+}
+
+// Fills in the plans' places; returns the number of jobs
+int plan_jobs(const mixlora_attention_shape_t& s, const AttnLayout& L, char* ws, bool backward, AttnArgs* a,
+              AttnPlanJob* jobs) {
+  int32_t* counts = reinterpret_cast<int32_t*>(ws + L.status) + 8;
+  jobs[0] = AttnPlanJob{reinterpret_cast<AttnTile*>(ws + L.q_tiles), counts, reinterpret_cast<int32_t*>(ws + L.q_first),
+                        backward ? kBwdTile : kFwdTile, tile_capacity(s.q_rows, s.n_seqs, backward ? kBwdTile : kFwdTile), 0};
+  jobs[1] = AttnPlanJob{reinterpret_cast<AttnTile*>(ws + L.k_tiles), counts + 1, reinterpret_cast<int32_t*>(ws + L.k_first),
+                        kBwdTile, tile_capacity(s.k_rows, s.n_seqs, kBwdTile), 1};
+  a->q_tiles = jobs[0].table; a->n_q_tiles = jobs[0].count;
+  a->k_tiles = jobs[1].table; a->n_k_tiles = jobs[1].count;
+  return backward ? 2 : 1;
 }
 
 mixlora_status_t attention_args(const mixlora_attention_shape_t* s, const mixlora_attention_mask_t* m, const void* q,
@@ -191,9 +214,16 @@ mixlora_status_t mixlora_attention_forward(const mixlora_attention_shape_t* shap
     MIXLORA_TRY(launch_attn_few(a, bf16_mode, splits_of(*shape), reinterpret_cast<float*>(ws + L.part), cs));
     return MIXLORA_OK;
   }
-  MIXLORA_TRY(cudaMemsetAsync(a.status, 0, 256, cs));
-  if (a.n_seqs == 0 || a.q_rows == 0) return MIXLORA_OK;
-  MIXLORA_TRY(bf16_mode ? launch_attn_forward_tc(a, cs) : launch_attn_forward_simt(a, cs));
+  if (!bf16_mode || a.n_seqs == 0 || a.q_rows == 0) {
+    MIXLORA_TRY(cudaMemsetAsync(a.status, 0, 256, cs));
+    if (a.n_seqs == 0 || a.q_rows == 0) return MIXLORA_OK;
+    MIXLORA_TRY(launch_attn_forward_simt(a, cs));
+    return MIXLORA_OK;
+  }
+  AttnPlanJob jobs[2];
+  const int n_jobs = plan_jobs(*shape, L, ws, false, &a, jobs);
+  MIXLORA_TRY(launch_attn_plan(a, jobs, n_jobs, cs));        // clears the status word
+  MIXLORA_TRY(launch_attn_forward_tc(a, cs));
   return MIXLORA_OK;
 }
 
@@ -218,11 +248,19 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t* sha
   a.lse2 = lse2;
   a.delta = delta;
   a.status = reinterpret_cast<int32_t*>(ws + L.status);
-  MIXLORA_TRY(cudaMemsetAsync(a.status, 0, 256, cs));
-  if (a.n_seqs == 0) return MIXLORA_OK;
   const bool bf16_mode = shape->dtype == MIXLORA_DTYPE_BF16;
+  if (!bf16_mode || a.n_seqs == 0) {
+    MIXLORA_TRY(cudaMemsetAsync(a.status, 0, 256, cs));
+    if (a.n_seqs == 0) return MIXLORA_OK;
+    MIXLORA_TRY(launch_attn_delta(a, bf16_mode, lse2, delta, cs));
+    MIXLORA_TRY(launch_attn_backward_simt(a, cs));
+    return MIXLORA_OK;
+  }
+  AttnPlanJob jobs[2];
+  const int n_jobs = plan_jobs(*shape, L, ws, true, &a, jobs);
+  MIXLORA_TRY(launch_attn_plan(a, jobs, n_jobs, cs));        // clears the status word
   MIXLORA_TRY(launch_attn_delta(a, bf16_mode, lse2, delta, cs));
-  MIXLORA_TRY(bf16_mode ? launch_attn_backward_tc(a, cs) : launch_attn_backward_simt(a, cs));
+  MIXLORA_TRY(launch_attn_backward_tc(a, cs));
   return MIXLORA_OK;
 }
 

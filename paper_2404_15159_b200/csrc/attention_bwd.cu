@@ -21,6 +21,8 @@ using namespace tc;
 
 constexpr int kTile = 128;
 constexpr int kThreads = 384;                    // two groups of 4 warps on the elements, a load warp, an MMA warp
+// A block starts with 168 registers a thread (384 x 168 = 64512); the element groups take 208 and the third group keeps 88:
+// (2 x 208 + 88) x 128 = 64512.
 constexpr int kLoadWarp = 8, kMmaWarp = 9;
 constexpr int kTmemCols = 512;
 constexpr int kRowWarp = 10;                     // of the key kernel: carries lse and delta
@@ -54,13 +56,15 @@ struct Ctl {
   __device__ __forceinline__ uint32_t acc() const { return at(6); }                      // the sums are final
   __device__ __forceinline__ uint32_t rows_full(int i) const { return at(7 + (i & 1)); }
   __device__ __forceinline__ uint32_t rows_empty(int i) const { return at(9 + (i & 1)); }
+  __device__ __forceinline__ uint32_t own_empty() const { return at(11); }               // the own tiles have been used
+  __device__ __forceinline__ uint32_t acc_empty() const { return at(12); }               // the sums have been read
   // waits for use number i / stages of a stage
   __device__ __forceinline__ bool wait_full_a(int i) const { return mbar_wait(full_a(i), (i / kStagesA) & 1u, abort_flag); }
   __device__ __forceinline__ bool wait_empty_a(int i) const { return mbar_wait(empty_a(i), ((i / kStagesA) & 1u) ^ 1u, abort_flag); }
   __device__ __forceinline__ bool wait_full_b(int i) const { return mbar_wait(full_b(i), (i / kStagesB) & 1u, abort_flag); }
   __device__ __forceinline__ bool wait_empty_b(int i) const { return mbar_wait(empty_b(i), ((i / kStagesB) & 1u) ^ 1u, abort_flag); }
 };
-constexpr int kBars = 2 * kStagesA + 2 * kStagesB + 11;
+constexpr int kBars = 2 * kStagesA + 2 * kStagesB + 13;
 
 template <int DP>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
@@ -98,14 +102,21 @@ __device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint32_t b, boo
   for (int k = 0; k < kTile / 16; ++k)
     umma_bf16_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, bd + k * (2048 >> 4), idesc, accumulate || k != 0);
 }
+// One row of the sums to memory; `empty` is told once they have been read (zeros are written where there are none).
 template <int DP>
-__device__ __forceinline__ void store_row(uint32_t acc, bool any, float mul, bool mine, bf16* dst, int head_dim) {
+__device__ __forceinline__ void store_row(uint32_t acc, bool any, uint32_t empty, float mul, bool mine, bf16* dst,
+                                          int head_dim) {
 #pragma unroll
   for (int c = 0; c < DP / 32; ++c) {
     uint32_t v[32];
     if (any) {
       tmem_ld32(acc + c * 32, v);
       tmem_ld_wait();
+      if (c == DP / 32 - 1) {
+        tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
+      }
     }
 #pragma unroll
     for (int g = 0; g < 4; ++g)
@@ -122,38 +133,26 @@ __device__ __forceinline__ void store_row(uint32_t acc, bool any, float mul, boo
   }
 }
 
-// Block setup shared by both kernels: the block's tile, barriers, TMEM.  False: nothing to do.
-__device__ __forceinline__ bool block_begin(const int32_t* off, int n_seqs, int rows, int tile, bool from_end,
-                                            const Ctl& c, uint32_t* slot, int* seq, int* index) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  volatile int* found = reinterpret_cast<volatile int*>(slot + 2);
-  if (warp == 0) {
-    int b = -1, t = 0;
-    if (!find_tile(off, n_seqs, rows, kTile, tile, &b, &t)) b = -1;
-    if (b >= 0 && !from_end) t = (seq_rows(off, b, rows) + kTile - 1) / kTile - 1 - t;
-    if (lane == 0) { found[0] = b; found[1] = t; }
-  }
+// Block setup shared by both kernels: barriers and TMEM, whose address is returned.  `readers`: warps that read the sums.
+__device__ __forceinline__ uint32_t block_begin(const Ctl& c, uint32_t* slot, int readers) {
   if (threadIdx.x == 32) {
     for (int i = 0; i < kStagesA; ++i) { mbar_init(c.full_a(i), 1); mbar_init(c.empty_a(i), 1); }
     for (int i = 0; i < kStagesB; ++i) { mbar_init(c.full_b(i), 1); mbar_init(c.empty_b(i), 1); }
     mbar_init(c.own(), 1); mbar_init(c.s(0), 1); mbar_init(c.s(1), 1); mbar_init(c.dp(), 1); mbar_init(c.acc(), 1);
     mbar_init(c.p(), 8); mbar_init(c.ds(), 8);
     for (int i = 0; i < 2; ++i) { mbar_init(c.rows_full(i), 1); mbar_init(c.rows_empty(i), 8); }
+    mbar_init(c.own_empty(), 1); mbar_init(c.acc_empty(), readers);
     *c.abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  __syncthreads();
-  *seq = found[0];
-  *index = found[1];
-  if (*seq < 0) return false;
-  if (warp == kMmaWarp) {
+  if ((threadIdx.x >> 5) == kMmaWarp) {
     tmem_alloc(smem_u32(slot), kTmemCols);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  return true;
+  return warp_uniform(*slot);
 }
 __device__ __forceinline__ void give_up(const Ctl& c, int32_t* status) {
   *c.abort_flag = 1;
@@ -223,70 +222,81 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
   const Ctl c{smem_u32(ctl), reinterpret_cast<volatile int*>(slot + 1)};
   const AttnArgs& a = p.a;
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const int kvh = blockIdx.x % a.kv_heads;
-  int seq, index;
-  // the first keys of a causal sequence are seen by the most rows: long work starts first
-  if (!block_begin(a.k_off, a.n_seqs, a.k_rows, blockIdx.x / a.kv_heads, false, c, slot, &seq, &index)) return;
-  const uint32_t tmem = warp_uniform(*slot);
+  const uint32_t tmem = block_begin(c, slot, 8);
   const uint32_t t_s = tmem, t_dp = tmem + kTile, t_dv = tmem + 2 * kTile, t_dk = t_dv + DP;
-  const AttnSeq sq = load_seq(a, seq);
-  const int j0 = index * kTile;
-  const int keys = min(kTile, sq.lk - j0);                   // <= 0: behind the used part of a slot
-  int lo = 0, hi = 0;
-  if (keys > 0) query_rows(sq, a.causal, a.window, j0, j0 + keys, &lo, &hi);
-  lo = lo / kTile * kTile;
-  const int per_head = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
-  const int n = per_head * a.group;
-
-  auto head_of = [&](int i) { return kvh * a.group + i / per_head; };
+  TileWalk w(a.k_tiles, a.n_k_tiles, a.kv_heads);            // w.head is the key head
+  // of the tile at hand: the query tiles of a head that see it, from row `lo`, and the steps over all heads that share it
+  int lo = 0, per_head = 0;
+  auto steps = [&] {
+    int hi;
+    query_rows(w.sq, a.causal, a.window, w.row0, min(w.row0 + kTile, w.sq.lk), &lo, &hi);
+    lo = lo / kTile * kTile;
+    per_head = hi > lo ? (hi - lo + kTile - 1) / kTile : 0;
+    return per_head * a.group;
+  };
+  auto head_of = [&](int i) { return w.head * a.group + i / per_head; };
   auto row_of = [&](int i) { return lo + (i % per_head) * kTile; };
 
+  // In every role `at` counts the steps of the tiles before: stages and barrier phases go on from tile to tile.
+  if (warp >= kLoadWarp) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == kLoadWarp) {
     if (lane == 0) {
       bool ok = true;
-      if (n > 0) {
+      int at = 0, used = 0;                                  // used: tiles whose keys have been loaded
+      while (ok && w.next()) {
+        const int n = steps();
+        if (n == 0) continue;
+        if (!mbar_wait(c.own_empty(), (used & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
+        ++used;
         mbar_expect_tx(c.own(), 2 * TB);
-        load_tile<DP>(k_tile, &p.k_map, c.own(), kvh, sq.k0 + j0);
-        load_tile<DP>(v_tile, &p.v_map, c.own(), kvh, sq.k0 + j0);
-      }
-      for (int i = 0; i < n; ++i) {
-        if (!c.wait_empty_a(i)) { ok = false; break; }
-        mbar_expect_tx(c.full_a(i), TB);
-        load_tile<DP>(q_at(i), &p.q_map, c.full_a(i), head_of(i), sq.q0 + row_of(i));
-        if (!c.wait_empty_b(i)) { ok = false; break; }
-        mbar_expect_tx(c.full_b(i), TB);
-        load_tile<DP>(do_at(i), &p.do_map, c.full_b(i), head_of(i), sq.q0 + row_of(i));
+        load_tile<DP>(k_tile, &p.k_map, c.own(), w.head, w.sq.k0 + w.row0);
+        load_tile<DP>(v_tile, &p.v_map, c.own(), w.head, w.sq.k0 + w.row0);
+        for (int i = 0; i < n; ++i, ++at) {
+          if (!c.wait_empty_a(at)) { ok = false; break; }
+          mbar_expect_tx(c.full_a(at), TB);
+          load_tile<DP>(q_at(at), &p.q_map, c.full_a(at), head_of(i), w.sq.q0 + row_of(i));
+          if (!c.wait_empty_b(at)) { ok = false; break; }
+          mbar_expect_tx(c.full_b(at), TB);
+          load_tile<DP>(do_at(at), &p.do_map, c.full_b(at), head_of(i), w.sq.q0 + row_of(i));
+        }
       }
       if (!ok) give_up(c, a.status);
     }
   } else if (warp == kRowWarp) {
     bool ok = true;
-    for (int i = 0; i < n; ++i) {
-      float v[2][kTile / 32];
-      const size_t at = (size_t)head_of(i) * a.q_rows + sq.q0 + row_of(i);
+    int at = 0;
+    while (ok && w.next()) {
+      const int n = steps();
+      for (int i = 0; i < n; ++i, ++at) {
+        float v[2][kTile / 32];
+        const size_t first = (size_t)head_of(i) * a.q_rows + w.sq.q0 + row_of(i);
 #pragma unroll
-      for (int x = 0; x < kTile / 32; ++x) {
-        const bool on = row_of(i) + x * 32 + lane < sq.lq;
-        v[0][x] = on ? -a.lse2[at + x * 32 + lane] : -INFINITY;
-        v[1][x] = on ? -a.delta[at + x * 32 + lane] : 0.f;
-      }
-      if (!__all_sync(0xffffffffu, mbar_wait(c.rows_empty(i), ((i >> 1) & 1u) ^ 1u, c.abort_flag))) { ok = false; break; }
-      float* dst = rows_smem + (i & 1) * (2 * kTile) + lane;
+        for (int x = 0; x < kTile / 32; ++x) {
+          const bool on = row_of(i) + x * 32 + lane < w.sq.lq;
+          v[0][x] = on ? -a.lse2[first + x * 32 + lane] : -INFINITY;
+          v[1][x] = on ? -a.delta[first + x * 32 + lane] : 0.f;
+        }
+        ok = __all_sync(0xffffffffu, mbar_wait(c.rows_empty(at), ((at >> 1) & 1u) ^ 1u, c.abort_flag));
+        if (!ok) break;
+        float* dst = rows_smem + (at & 1) * (2 * kTile) + lane;
 #pragma unroll
-      for (int x = 0; x < kTile / 32; ++x) {
-        dst[x * 32] = v[0][x];
-        dst[kTile + x * 32] = v[1][x];
+        for (int x = 0; x < kTile / 32; ++x) {
+          dst[x * 32] = v[0][x];
+          dst[kTile + x * 32] = v[1][x];
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c.rows_full(at));
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(c.rows_full(i));
     }
     if (!ok && lane == 0) give_up(c, a.status);
   } else if (warp == kMmaWarp) {
     const bool one = elect_one();
-    bool ok = n == 0 || __all_sync(0xffffffffu, mbar_wait(c.own(), 0, c.abort_flag));
+    bool ok = true;
+    int at = 0, used = 0;
     // a stream's tile i is in shared memory, its rows behind the last cleared
     auto tail = [&](int i, uint32_t tile) {
-      const int valid = sq.lq - row_of(i);
+      const int valid = w.sq.lq - row_of(i);
       if (valid < kTile) {
         clear_rows<DP>(tile, valid);
         fence_proxy_async_smem();
@@ -295,164 +305,178 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
       tc_fence_after();
     };
     auto scores = [&](int i) {
-      if (!__all_sync(0xffffffffu, c.wait_full_a(i))) return false;
-      tail(i, q_at(i));
+      if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
+      tail(i, q_at(at + i));
       if (one) {
-        issue_nt<DP>(t_s, k_tile, q_at(i));
+        issue_nt<DP>(t_s, k_tile, q_at(at + i));
         umma_commit(c.s(0));
       }
       return true;
     };
     auto grads = [&](int i) {
-      if (!__all_sync(0xffffffffu, c.wait_full_b(i))) return false;
-      tail(i, do_at(i));
+      if (!__all_sync(0xffffffffu, c.wait_full_b(at + i))) return false;
+      tail(i, do_at(at + i));
       if (one) {
-        issue_nt<DP>(t_dp, v_tile, do_at(i));
+        issue_nt<DP>(t_dp, v_tile, do_at(at + i));
         umma_commit(c.dp());
       }
       return true;
     };
-    ok = ok && (n == 0 || (scores(0) && grads(0)));
-    for (int i = 0; i < n && ok; ++i) {
-      ok = __all_sync(0xffffffffu, mbar_wait(c.p(), i & 1u, c.abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      if (one) {
-        issue_ts<DP>(t_dv, t_s, do_at(i), i > 0);
-        umma_commit(c.empty_b(i));
+    while (ok && w.next()) {
+      const int n = steps();
+      if (n == 0) continue;
+      ok = __all_sync(0xffffffffu, mbar_wait(c.own(), used & 1u, c.abort_flag)) && scores(0) && grads(0) &&
+           __all_sync(0xffffffffu, mbar_wait(c.acc_empty(), (used & 1u) ^ 1u, c.abort_flag));
+      ++used;
+      for (int i = 0; i < n && ok; ++i) {
+        ok = __all_sync(0xffffffffu, mbar_wait(c.p(), (at + i) & 1u, c.abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        if (one) {
+          issue_ts<DP>(t_dv, t_s, do_at(at + i), i > 0);
+          umma_commit(c.empty_b(at + i));
+        }
+        ok = i + 1 >= n || scores(i + 1);
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(c.ds(), (at + i) & 1u, c.abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        if (one) {
+          issue_ts<DP>(t_dk, t_dp, q_at(at + i), i > 0);
+          umma_commit(c.empty_a(at + i));
+          if (i + 1 == n) { umma_commit(c.acc()); umma_commit(c.own_empty()); }
+        }
+        ok = i + 1 >= n || grads(i + 1);
       }
-      ok = i + 1 >= n || scores(i + 1);
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      if (one) {
-        issue_ts<DP>(t_dk, t_dp, q_at(i), i > 0);
-        umma_commit(c.empty_a(i));
-        if (i + 1 == n) umma_commit(c.acc());
-      }
-      ok = i + 1 >= n || grads(i + 1);
+      at += n;
     }
     if (!ok && lane == 0) give_up(c, a.status);
-  } else if (warp < kLoadWarp) {
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---------------- elements: one key per thread, half of the tile's rows per group ----------------
-    const int half = warp >> 2, key = (warp & 3) * 32 + lane, j = j0 + key;
+    const int half = warp >> 2, key = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = t_s + lanes + half * 64, dp_addr = t_dp + lanes + half * 64;
     bool ok = true;
-    for (int i = 0; i < n && ok; ++i) {
-      const int i0 = row_of(i) + half * 64;
-      const Score<CAP, BIAS> score(a, head_of(i));
-      const float* neg_lse = rows_smem + (i & 1) * (2 * kTile) + half * 64;
-      const float* neg_delta = neg_lse + kTile;
-      const int pos0 = sq.shift + i0;
-      // the tile's rows behind the last see nothing
-      const bool whole = i0 + 64 <= sq.lq && all_seen(sq, a.causal, a.window, pos0, pos0 + 63, j0, j0 + kTile);
-      ok = __all_sync(0xffffffffu, mbar_wait(c.rows_full(i), (i >> 1) & 1u, c.abort_flag) &&
-                                       mbar_wait(c.s(0), i & 1u, c.abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      float pr[64];
-      tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
-      tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
-      tmem_ld_wait();
-      uint64_t cs[CAP ? 32 : 1];
-#pragma unroll
-      for (int x = 0; x < 64; x += 4) {
-        const float4 ls = *reinterpret_cast<const float4*>(neg_lse + x);
-        const bool poly = (x / 2 & 7) >= 8 - kPolys;         // known when unrolled
-        if (poly) {
-          score.template probs<true>(pr[x], pr[x + 1], pair2(ls.x, ls.y), pos0 + x - j, pos0 + x + 1 - j, pr[x], pr[x + 1],
-                                     cs[CAP ? x / 2 : 0]);
-          score.template probs<true>(pr[x + 2], pr[x + 3], pair2(ls.z, ls.w), pos0 + x + 2 - j, pos0 + x + 3 - j, pr[x + 2],
-                                     pr[x + 3], cs[CAP ? x / 2 + 1 : 0]);
-        } else {
-          score.template probs<false>(pr[x], pr[x + 1], pair2(ls.x, ls.y), pos0 + x - j, pos0 + x + 1 - j, pr[x], pr[x + 1],
-                                      cs[CAP ? x / 2 : 0]);
-          score.template probs<false>(pr[x + 2], pr[x + 3], pair2(ls.z, ls.w), pos0 + x + 2 - j, pos0 + x + 3 - j, pr[x + 2],
-                                      pr[x + 3], cs[CAP ? x / 2 + 1 : 0]);
-        }
-      }
-      if (!whole) {
-        // rows that see this key: [r_lo, r_hi), or all where the key lies before the prefix
-        int r_lo = 0, r_hi = 0;
-        if (j < sq.lk) query_rows(sq, a.causal, a.window, j, j + 1, &r_lo, &r_hi);
-        r_lo -= i0;
-        r_hi -= i0;
-#pragma unroll
-        for (int x = 0; x < 64; ++x)
-          if (x < r_lo || x >= r_hi) pr[x] = 0.f;
-      }
-#pragma unroll
-      for (int c0 = 0; c0 < 2; ++c0) {
-        uint32_t pk[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) pk[x] = bf16x2(pr[c0 * 32 + 2 * x], pr[c0 * 32 + 2 * x + 1]);
-        tmem_st16(s_addr + c0 * 16, pk);
-      }
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(c.p());
-      ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), i & 1u, c.abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-#pragma unroll
-      for (int c0 = 0; c0 < 2; ++c0) {
-        float dp[32];
-        tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+    int at = 0, used = 0;
+    while (ok && w.next()) {
+      const int n = steps(), j0 = w.row0, j = j0 + key, keys = min(kTile, w.sq.lk - j0);
+      for (int i = 0; i < n && ok; ++i, ++at) {
+        const int i0 = row_of(i) + half * 64;
+        const Score<CAP, BIAS> score(a, head_of(i));
+        const float* neg_lse = rows_smem + (at & 1) * (2 * kTile) + half * 64;
+        const float* neg_delta = neg_lse + kTile;
+        const int pos0 = w.sq.shift + i0;
+        // the tile's rows behind the last see nothing
+        const bool whole = i0 + 64 <= w.sq.lq && all_seen(w.sq, a.causal, a.window, pos0, pos0 + 63, j0, j0 + kTile);
+        ok = __all_sync(0xffffffffu, mbar_wait(c.rows_full(at), (at >> 1) & 1u, c.abort_flag) &&
+                                         mbar_wait(c.s(0), at & 1u, c.abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        float pr[64];
+        tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
+        tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
         tmem_ld_wait();
-        if (!whole) {                                        // rows behind the last may hold anything
-#pragma unroll
-          for (int x = 0; x < 32; ++x)
-            if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+        // rows that see this key: [r_lo, r_hi), or all where the key lies before the prefix
+        int r_lo = 0, r_hi = 64;
+        if (!whole) {
+          r_hi = 0;
+          if (j < w.sq.lk) query_rows(w.sq, a.causal, a.window, j, j + 1, &r_lo, &r_hi);
+          r_lo -= i0;
+          r_hi -= i0;
         }
-        uint32_t pk[16];
 #pragma unroll
-        for (int x = 0; x < 32; x += 4) {
-          const float4 dl = *reinterpret_cast<const float4*>(neg_delta + c0 * 32 + x);
-          const float* pv = pr + c0 * 32 + x;
-          uint64_t u = add2(pair2(dp[x], dp[x + 1]), pair2(dl.x, dl.y)), w = add2(pair2(dp[x + 2], dp[x + 3]), pair2(dl.z, dl.w));
-          u = mul2(u, pair2(pv[0], pv[1]));
-          w = mul2(w, pair2(pv[2], pv[3]));
-          if (CAP) {
-            u = mul2(u, cs[c0 * 16 + x / 2]);
-            w = mul2(w, cs[c0 * 16 + x / 2 + 1]);
+        for (int c0 = 0; c0 < 2; ++c0) {
+          uint64_t cs[CAP ? 16 : 1];
+          float* pc = pr + c0 * 32;
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) {
+            const float4 ls = *reinterpret_cast<const float4*>(neg_lse + c0 * 32 + x);
+            const int d0 = pos0 + c0 * 32 + x - j;
+            uint64_t& cs0 = cs[CAP ? x / 2 : 0];
+            uint64_t& cs1 = cs[CAP ? x / 2 + 1 : 0];
+            if ((x / 2 & 7) >= 8 - kPolys) {                   // known when unrolled
+              score.template probs<true>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1, pc[x], pc[x + 1], cs0);
+              score.template probs<true>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2, d0 + 3, pc[x + 2], pc[x + 3], cs1);
+            } else {
+              score.template probs<false>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1, pc[x], pc[x + 1], cs0);
+              score.template probs<false>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2, d0 + 3, pc[x + 2], pc[x + 3], cs1);
+            }
           }
-          float f0, f1, f2, f3;
-          unpair2(u, f0, f1);
-          unpair2(w, f2, f3);
-          if (CAP && !whole) {                               // the slope of a score that came from anything
-            f0 = pv[0] == 0.f ? 0.f : f0;
-            f1 = pv[1] == 0.f ? 0.f : f1;
-            f2 = pv[2] == 0.f ? 0.f : f2;
-            f3 = pv[3] == 0.f ? 0.f : f3;
+          if (!whole) {
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (c0 * 32 + x < r_lo || c0 * 32 + x >= r_hi) pc[x] = 0.f;
           }
-          pk[x / 2] = bf16x2(f0, f1);
-          pk[x / 2 + 1] = bf16x2(f2, f3);
+          uint32_t pk[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) pk[x] = bf16x2(pc[2 * x], pc[2 * x + 1]);
+          tmem_st16(s_addr + c0 * 16, pk);
+          if (CAP) {                                           // from here on p times the cap's slope
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+              float f0, f1;
+              unpair2(mul2(pair2(pc[x], pc[x + 1]), cs[x / 2]), f0, f1);
+              pc[x] = !whole && pc[x] == 0.f ? 0.f : f0;       // a hidden score's slope may be anything
+              pc[x + 1] = !whole && pc[x + 1] == 0.f ? 0.f : f1;
+            }
+          }
         }
-        tmem_st16(dp_addr + c0 * 16, pk);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c.p());
+        ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), at & 1u, c.abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int c0 = 0; c0 < 2; ++c0) {
+          float dp[32];
+          tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+          tmem_ld_wait();
+          if (!whole) {                                        // rows behind the last may hold anything
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+          }
+          uint32_t pk[16];
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) {
+            const float4 dl = *reinterpret_cast<const float4*>(neg_delta + c0 * 32 + x);
+            const float* pv = pr + c0 * 32 + x;
+            uint64_t u = add2(pair2(dp[x], dp[x + 1]), pair2(dl.x, dl.y)), v = add2(pair2(dp[x + 2], dp[x + 3]), pair2(dl.z, dl.w));
+            u = mul2(u, pair2(pv[0], pv[1]));
+            v = mul2(v, pair2(pv[2], pv[3]));
+            float f0, f1, f2, f3;
+            unpair2(u, f0, f1);
+            unpair2(v, f2, f3);
+            pk[x / 2] = bf16x2(f0, f1);
+            pk[x / 2 + 1] = bf16x2(f2, f3);
+          }
+          tmem_st16(dp_addr + c0 * 16, pk);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(c.ds()); mbar_arrive(c.rows_empty(at)); }
       }
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) { mbar_arrive(c.ds()); mbar_arrive(c.rows_empty(i)); }
+      if (ok && n > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(c.acc(), used & 1u, c.abort_flag));
+        ++used;
+        tc_fence_after();
+      }
+      if (ok) {
+        const bool mine = key < keys;
+        const size_t row = (size_t)(w.sq.k0 + (mine ? j : 0));
+        if (half == 0)
+          store_row<DP>(t_dv + lanes, n > 0, c.acc_empty(), 1.f, mine,
+                        reinterpret_cast<bf16*>(a.dv) + row * a.v_stride + (size_t)w.head * a.head_dim, a.head_dim);
+        else
+          store_row<DP>(t_dk + lanes, n > 0, c.acc_empty(), a.scale, mine,
+                        reinterpret_cast<bf16*>(a.dk) + row * a.k_stride + (size_t)w.head * a.head_dim, a.head_dim);
+      }
     }
-    if (ok && n > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait(c.acc(), 0, c.abort_flag));
-      tc_fence_after();
-    }
-    if (ok) {
-      const bool mine = key < keys;
-      const size_t row = (size_t)(sq.k0 + (mine ? j : 0));
-      if (half == 0)
-        store_row<DP>(t_dv + lanes, n > 0, 1.f, mine,
-                      reinterpret_cast<bf16*>(a.dv) + row * a.v_stride + (size_t)kvh * a.head_dim, a.head_dim);
-      else
-        store_row<DP>(t_dk + lanes, n > 0, a.scale, mine,
-                      reinterpret_cast<bf16*>(a.dk) + row * a.k_stride + (size_t)kvh * a.head_dim, a.head_dim);
-    } else if (lane == 0) {
-      give_up(c, a.status);
-    }
+    if (!ok && lane == 0) give_up(c, a.status);
   }
   block_end(c, tmem);
 }
@@ -471,156 +495,178 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
   const Ctl c{smem_u32(ctl), reinterpret_cast<volatile int*>(slot + 1)};
   const AttnArgs& a = p.a;
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const int head = blockIdx.x % a.q_heads;
-  int seq, index;
-  if (!block_begin(a.q_off, a.n_seqs, a.q_rows, blockIdx.x / a.q_heads, true, c, slot, &seq, &index)) return;
-  const uint32_t tmem = warp_uniform(*slot);
+  const uint32_t tmem = block_begin(c, slot, 4);
   const uint32_t t_dp = tmem + 2 * kTile, t_dq = tmem + 3 * kTile;
-  const AttnSeq sq = load_seq(a, seq);
-  const int i0 = index * kTile, rows = min(kTile, sq.lq - i0);
-  const int p0 = sq.shift + i0, p1 = p0 + rows - 1;
-  const KeyTiles<kTile> tiles = key_tiles<kTile>(sq, a.causal, a.window, p0, p1);
-  const int n = tiles.count();
+  TileWalk w(a.q_tiles, a.n_q_tiles, a.q_heads);
+  auto rows_of = [&] { return min(kTile, w.sq.lq - w.row0); };
+  auto tiles_of = [&] {
+    const int p0 = w.sq.shift + w.row0;
+    return key_tiles<kTile>(w.sq, a.causal, a.window, p0, p0 + rows_of() - 1);
+  };
 
+  if (warp >= kLoadWarp) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == kLoadWarp) {
     if (lane == 0) {
-      const int kvh = head / a.group;
       bool ok = true;
-      if (n > 0) {
+      int at = 0, used = 0;
+      while (ok && w.next()) {
+        const KeyTiles<kTile> tiles = tiles_of();
+        const int n = tiles.count(), kvh = w.head / a.group;
+        if (n == 0) continue;
+        if (!mbar_wait(c.own_empty(), (used & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
+        ++used;
         mbar_expect_tx(c.own(), 2 * TB);
-        load_tile<DP>(q_tile, &p.q_map, c.own(), head, sq.q0 + i0);
-        load_tile<DP>(do_tile, &p.do_map, c.own(), head, sq.q0 + i0);
-      }
-      for (int i = 0; i < n; ++i) {
-        if (!c.wait_empty_a(i)) { ok = false; break; }
-        mbar_expect_tx(c.full_a(i), TB);
-        load_tile<DP>(k_at(i), &p.k_map, c.full_a(i), kvh, sq.k0 + tiles.at(i) * kTile);
-        if (!c.wait_empty_b(i)) { ok = false; break; }
-        mbar_expect_tx(c.full_b(i), TB);
-        load_tile<DP>(v_at(i), &p.v_map, c.full_b(i), kvh, sq.k0 + tiles.at(i) * kTile);
+        load_tile<DP>(q_tile, &p.q_map, c.own(), w.head, w.sq.q0 + w.row0);
+        load_tile<DP>(do_tile, &p.do_map, c.own(), w.head, w.sq.q0 + w.row0);
+        for (int i = 0; i < n; ++i, ++at) {
+          if (!c.wait_empty_a(at)) { ok = false; break; }
+          mbar_expect_tx(c.full_a(at), TB);
+          load_tile<DP>(k_at(at), &p.k_map, c.full_a(at), kvh, w.sq.k0 + tiles.at(i) * kTile);
+          if (!c.wait_empty_b(at)) { ok = false; break; }
+          mbar_expect_tx(c.full_b(at), TB);
+          load_tile<DP>(v_at(at), &p.v_map, c.full_b(at), kvh, w.sq.k0 + tiles.at(i) * kTile);
+        }
       }
       if (!ok) give_up(c, a.status);
     }
   } else if (warp == kMmaWarp) {
     const bool one = elect_one();
-    bool ok = n == 0 || __all_sync(0xffffffffu, mbar_wait(c.own(), 0, c.abort_flag));
+    bool ok = true;
+    int at = 0, used = 0;
+    KeyTiles<kTile> tiles;
     auto scores = [&](int i) {                               // over ds of two tiles ago, which its product has read
-      if (!__all_sync(0xffffffffu, c.wait_full_a(i))) return false;
-      const int valid = sq.lk - tiles.at(i) * kTile;
+      if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
+      const int valid = w.sq.lk - tiles.at(i) * kTile;
       if (valid < kTile) {
-        clear_rows<DP>(k_at(i), valid);
+        clear_rows<DP>(k_at(at + i), valid);
         fence_proxy_async_smem();
         __syncwarp();
       }
       tc_fence_after();
       if (one) {
-        issue_nt<DP>(tmem + (i & 1) * kTile, q_tile, k_at(i));
-        umma_commit(c.s(i & 1));
+        issue_nt<DP>(tmem + ((at + i) & 1) * kTile, q_tile, k_at(at + i));
+        umma_commit(c.s((at + i) & 1));
       }
       return true;
     };
     auto grads = [&](int i) {
-      if (!__all_sync(0xffffffffu, c.wait_full_b(i))) return false;
+      if (!__all_sync(0xffffffffu, c.wait_full_b(at + i))) return false;
       tc_fence_after();
       if (one) {
-        issue_nt<DP>(t_dp, do_tile, v_at(i));
+        issue_nt<DP>(t_dp, do_tile, v_at(at + i));
         umma_commit(c.dp());
-        umma_commit(c.empty_b(i));
+        umma_commit(c.empty_b(at + i));
       }
       return true;
     };
-    ok = ok && (n == 0 || (scores(0) && grads(0)));
-    for (int i = 0; i < n && ok; ++i) {
-      ok = (i + 1 >= n || scores(i + 1)) && __all_sync(0xffffffffu, mbar_wait(c.ds(), i & 1u, c.abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      ok = i + 1 >= n || grads(i + 1);
-      if (!ok) break;
-      if (one) {
-        issue_ts<DP>(t_dq, tmem + (i & 1) * kTile, k_at(i), i > 0);
-        umma_commit(c.empty_a(i));
-        if (i + 1 == n) umma_commit(c.acc());
+    while (ok && w.next()) {
+      tiles = tiles_of();
+      const int n = tiles.count();
+      if (n == 0) continue;
+      ok = __all_sync(0xffffffffu, mbar_wait(c.own(), used & 1u, c.abort_flag)) && scores(0) && grads(0) &&
+           __all_sync(0xffffffffu, mbar_wait(c.acc_empty(), (used & 1u) ^ 1u, c.abort_flag));
+      ++used;
+      for (int i = 0; i < n && ok; ++i) {
+        ok = (i + 1 >= n || scores(i + 1)) && __all_sync(0xffffffffu, mbar_wait(c.ds(), (at + i) & 1u, c.abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        ok = i + 1 >= n || grads(i + 1);
+        if (!ok) break;
+        if (one) {
+          issue_ts<DP>(t_dq, tmem + ((at + i) & 1) * kTile, k_at(at + i), i > 0);
+          umma_commit(c.empty_a(at + i));
+          if (i + 1 == n) { umma_commit(c.acc()); umma_commit(c.own_empty()); }
+        }
       }
+      at += n;
     }
     if (!ok && lane == 0) give_up(c, a.status);
-  } else if (warp < kLoadWarp) {
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---------------- elements: one row per thread, half of the tile's keys per group ----------------
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t dp_addr = t_dp + lanes + half * 64;
-    const bool mine = row < rows;
-    const int pos = p0 + row;
-    const size_t at = (size_t)head * a.q_rows + sq.q0 + i0 + (mine ? row : 0);
-    const float nl = mine ? -a.lse2[at] : -INFINITY, nd = mine ? -a.delta[at] : 0.f;
-    const uint64_t neg_lse = pair2(nl, nl), neg_delta = pair2(nd, nd);
-    const Score<CAP, BIAS> score(a, head);
-    const RowKeys keys = row_keys(sq, a.causal, a.window, pos);
     bool ok = true;
-    for (int i = 0; i < n && ok; ++i) {
-      const int j0 = tiles.at(i) * kTile + half * 64;
-      const bool whole = all_seen(sq, a.causal, a.window, p0, p1, j0, j0 + 64);
-      const uint32_t s_addr = tmem + (i & 1) * kTile + lanes + half * 64;
-      ok = __all_sync(0xffffffffu, mbar_wait(c.s(i & 1), (i >> 1) & 1u, c.abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      float pr[64];
-      tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
-      tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
-      tmem_ld_wait();
-#pragma unroll
-      for (int x = 0; x < 64; x += 2) {
-        uint64_t cs;
-        if ((x / 2 & 7) >= 8 - kPolys)
-          score.template probs<true>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
-        else
-          score.template probs<false>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
-        if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
-      }
-      if (!whole) {
-        const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
-#pragma unroll
-        for (int x = 0; x < 64; ++x)
-          if (!((x >= lo && x < hi) || x < pre)) pr[x] = 0.f;
-      }
-      ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), i & 1u, c.abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-#pragma unroll
-      for (int c0 = 0; c0 < 2; ++c0) {
-        float dp[32];
-        tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+    int at = 0, used = 0;
+    while (ok && w.next()) {
+      const KeyTiles<kTile> tiles = tiles_of();
+      const int n = tiles.count(), rows = rows_of();
+      const int p0 = w.sq.shift + w.row0, p1 = p0 + rows - 1, pos = p0 + row;
+      const bool mine = row < rows;
+      const size_t place = (size_t)w.head * a.q_rows + w.sq.q0 + w.row0 + (mine ? row : 0);
+      const float nl = mine ? -a.lse2[place] : -INFINITY, nd = mine ? -a.delta[place] : 0.f;
+      const uint64_t neg_lse = pair2(nl, nl), neg_delta = pair2(nd, nd);
+      const Score<CAP, BIAS> score(a, w.head);
+      const RowKeys keys = row_keys(w.sq, a.causal, a.window, pos);
+      for (int i = 0; i < n && ok; ++i, ++at) {
+        const int j0 = tiles.at(i) * kTile + half * 64;
+        const bool whole = all_seen(w.sq, a.causal, a.window, p0, p1, j0, j0 + 64);
+        const uint32_t s_addr = tmem + (at & 1) * kTile + lanes + half * 64;
+        ok = __all_sync(0xffffffffu, mbar_wait(c.s(at & 1), (at >> 1) & 1u, c.abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        float pr[64];
+        tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
+        tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
         tmem_ld_wait();
-        if (!whole) {                                        // keys behind the last may hold anything
 #pragma unroll
-          for (int x = 0; x < 32; ++x)
-            if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+        for (int x = 0; x < 64; x += 2) {
+          uint64_t cs;
+          if ((x / 2 & 7) >= 8 - kPolys)
+            score.template probs<true>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
+          else
+            score.template probs<false>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
+          if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
         }
-        uint32_t pk[16];
+        if (!whole) {
+          const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
 #pragma unroll
-        for (int x = 0; x < 32; x += 2) {
-          float f0, f1;
-          unpair2(mul2(add2(pair2(dp[x], dp[x + 1]), neg_delta), pair2(pr[c0 * 32 + x], pr[c0 * 32 + x + 1])), f0, f1);
-          pk[x / 2] = bf16x2(f0, f1);
+          for (int x = 0; x < 64; ++x)
+            if (!((x >= lo && x < hi) || x < pre)) pr[x] = 0.f;
         }
-        tmem_st16(s_addr + c0 * 16, pk);
+        ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), at & 1u, c.abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int c0 = 0; c0 < 2; ++c0) {
+          float dp[32];
+          tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+          tmem_ld_wait();
+          if (!whole) {                                        // keys behind the last may hold anything
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+          }
+          uint32_t pk[16];
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) {
+            float f0, f1;
+            unpair2(mul2(add2(pair2(dp[x], dp[x + 1]), neg_delta), pair2(pr[c0 * 32 + x], pr[c0 * 32 + x + 1])), f0, f1);
+            pk[x / 2] = bf16x2(f0, f1);
+          }
+          tmem_st16(s_addr + c0 * 16, pk);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c.ds());
       }
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(c.ds());
+      if (ok && n > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(c.acc(), used & 1u, c.abort_flag));
+        ++used;
+        tc_fence_after();
+      }
+      if (ok) {
+        if (half == 0)
+          store_row<DP>(t_dq + lanes, n > 0, c.acc_empty(), a.scale, mine,
+                        reinterpret_cast<bf16*>(a.dq) + (size_t)(w.sq.q0 + w.row0 + (mine ? row : 0)) * a.q_stride +
+                            (size_t)w.head * a.head_dim, a.head_dim);
+      }
     }
-    if (ok && n > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait(c.acc(), 0, c.abort_flag));
-      tc_fence_after();
-    }
-    if (ok) {
-      if (half == 0)
-        store_row<DP>(t_dq + lanes, n > 0, a.scale, mine,
-                      reinterpret_cast<bf16*>(a.dq) + (size_t)(sq.q0 + i0 + (mine ? row : 0)) * a.q_stride +
-                          (size_t)head * a.head_dim, a.head_dim);
-    } else if (lane == 0) {
-      give_up(c, a.status);
-    }
+    if (!ok && lane == 0) give_up(c, a.status);
   }
   block_end(c, tmem);
 }
@@ -717,9 +763,12 @@ cudaError_t launch_attn_backward_tc(const AttnArgs& a, cudaStream_t st) {
       !tc_encode_heads(&p.k_map, a.k, kr, a.kv_heads, a.head_dim, a.k_stride, kTile) ||
       !tc_encode_heads(&p.v_map, a.v, kr, a.kv_heads, a.head_dim, a.v_stride, kTile))
     return cudaErrorInvalidValue;
-  const long long gk = a.k_rows ? ((long long)(a.k_rows + kTile - 1) / kTile + a.n_seqs) * a.kv_heads : 0;
-  const long long gq = a.q_rows ? ((long long)(a.q_rows + kTile - 1) / kTile + a.n_seqs) * a.q_heads : 0;
-  if (gk > 0x7fffffffLL || gq > 0x7fffffffLL) return cudaErrorInvalidValue;
+  long long gk = a.k_rows ? ((long long)(a.k_rows + kBwdTile - 1) / kBwdTile + a.n_seqs) * a.kv_heads : 0;
+  long long gq = a.q_rows ? ((long long)(a.q_rows + kBwdTile - 1) / kBwdTile + a.n_seqs) * a.q_heads : 0;
+  if (gk > 0x7fff0000LL || gq > 0x7fff0000LL) return cudaErrorInvalidValue;
+  const int sms = attn_sm_count();                           // one block per SM, which walks over the tiles
+  if (gk > sms) gk = sms;
+  if (gq > sms) gq = sms;
   return a.head_dim <= 64 ? launch_dp<64>(p, (unsigned)gk, (unsigned)gq, st) : launch_dp<128>(p, (unsigned)gk, (unsigned)gq, st);
 }
 

@@ -22,7 +22,7 @@ constexpr int kLoadWarp = 8, kMmaWarp = 9;
 constexpr int kTmemCols = 512;
 template <int DP> constexpr int kStages = DP == 128 ? 5 : 8;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
-template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 256;
+template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 320;
 
 // Of 8 pairs of exponentials those that go to the fp32 pipes
 constexpr int kPolys = 2;
@@ -33,7 +33,8 @@ struct FwdParams {
   CUtensorMap q_map, k_map, v_map;
 };
 
-// One block: 256 query rows of a head (two halves of 128) against the sequence's key tiles.  The load warp streams K and
+// One block per SM walks over (256 query rows, head) pairs, longest first: two halves of 128 rows against the sequence's
+// key tiles.  The load warp runs ahead into the next pair's Q and K while this one's results are written.  It streams K and
 // V tiles through a ring; the MMA warp issues, half by half, O += P V and then the next S = Q K^T, so that one half's
 // products run while the other half's exponentials are computed.  S [128 x 128] sits in TMEM; four warps take its rows,
 // a row to a thread, and write P over it as bf16, from where the product reads it: P never touches shared memory, and
@@ -56,31 +57,26 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   auto empty_bar = [&](int s) { return bars + 8u * (NS + s); };
   auto q_bar = [&](int h) { return bars + 8u * (2 * NS + h); };
   auto s_bar = [&](int h) { return bars + 8u * (2 * NS + 2 + h); };
-  auto p_bar = [&](int h) { return bars + 8u * (2 * NS + 4 + h); };
-  auto o_bar = [&](int h) { return bars + 8u * (2 * NS + 8 + h); };      // p_bar: two pairs, for the two halves of P
+  auto p_bar = [&](int h) { return bars + 8u * (2 * NS + 4 + h); };      // and 16 bytes on, for the second half of P
+  auto o_bar = [&](int h) { return bars + 8u * (2 * NS + 8 + h); };
   auto v_bar = [&](int h) { return bars + 8u * (2 * NS + 10 + h); };     // the first half of P has been used
-  uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * NS + 12));
+  auto q_empty_bar = [&](int h) { return bars + 8u * (2 * NS + 12 + h); };
+  auto o_empty_bar = [&](int h) { return bars + 8u * (2 * NS + 14 + h); };
+  uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * NS + 16));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(slot + 1);
-  volatile int* found = reinterpret_cast<volatile int*>(slot + 2);       // {sequence, tile} or {-1, .}
 
   const AttnArgs& a = p.a;
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const int head = blockIdx.x % a.q_heads;
-
-  if (warp == 0) {
-    int b = -1, tile = 0;
-    if (!find_tile(a.q_off, a.n_seqs, a.q_rows, 2 * kTile, blockIdx.x / a.q_heads, &b, &tile)) b = -1;
-    if (lane == 0) { found[0] = b; found[1] = tile; }
-  }
   if (threadIdx.x == 32) {
     for (int s = 0; s < NS; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int h = 0; h < 2; ++h) { mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(p_bar(h), 4); mbar_init(p_bar(h) + 16u, 4); mbar_init(v_bar(h), 1); mbar_init(o_bar(h), 1); }
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(o_bar(h), 1); mbar_init(v_bar(h), 1);
+      mbar_init(p_bar(h), 4); mbar_init(p_bar(h) + 16u, 4); mbar_init(q_empty_bar(h), 1); mbar_init(o_empty_bar(h), 4);
+    }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kLoadWarp && lane == 0) { prefetch_tmap(&p.q_map); prefetch_tmap(&p.k_map); prefetch_tmap(&p.v_map); }
-  __syncthreads();
-  if (found[0] < 0) return;                      // the grid is an upper bound of the tiles there are
   if (warp == kMmaWarp) {
     tmem_alloc(smem_u32(slot), kTmemCols);
     tmem_relinquish();
@@ -89,39 +85,48 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = warp_uniform(*slot);
-  const AttnSeq sq = load_seq(a, found[0]);
-  const int r0 = found[1] * 2 * kTile;           // first row of the block in its sequence
-  const int rows = min(2 * kTile, sq.lq - r0);
-  const KeyTiles<kTile> tiles = key_tiles<kTile>(sq, a.causal, a.window, sq.shift + r0, sq.shift + r0 + rows - 1);
-  const int n = tiles.count();
-  // the key tiles that a half needs, among the block's
+  TileWalk w(a.q_tiles, a.n_q_tiles, a.q_heads);
+  // of the tile at hand: its rows, its key tiles, and those of them that a half of the rows needs
+  auto rows_of = [&] { return min(2 * kTile, w.sq.lq - w.row0); };
+  auto tiles_of = [&] {
+    const int p0 = w.sq.shift + w.row0;
+    return key_tiles<kTile>(w.sq, a.causal, a.window, p0, p0 + rows_of() - 1);
+  };
   auto half_tiles = [&](int h) {
-    const int hr = min(kTile, rows - h * kTile);
+    const int hr = min(kTile, rows_of() - h * kTile);
     if (hr <= 0) return KeyTiles<kTile>{0, 0, 0};
-    const int p0 = sq.shift + r0 + h * kTile;
-    return key_tiles<kTile>(sq, a.causal, a.window, p0, p0 + hr - 1);
+    const int p0 = w.sq.shift + w.row0 + h * kTile;
+    return key_tiles<kTile>(w.sq, a.causal, a.window, p0, p0 + hr - 1);
   };
 
   if (warp >= kLoadWarp) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == kLoadWarp) {
     if (lane == 0) {
-      const int kvh = head / a.group;
       bool ok = true;
-      for (int h = 0; h < 2; ++h) {
-        if (rows <= h * kTile) break;
-        mbar_expect_tx(q_bar(h), TB);
-        for (int j = 0; j < NB; ++j)
-          tma_load_3d(q_base + h * TB + j * (kTile * 128), &p.q_map, q_bar(h), j * 64, head, sq.q0 + r0 + h * kTile);
-      }
-      for (int i = 0; i < 2 * n && ok; ++i) {    // K and V of a tile in turn
-        const int st = i % NS;
-        if (!mbar_wait(empty_bar(st), ((i / NS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-        mbar_expect_tx(full_bar(st), TB);
-        const CUtensorMap* map = (i & 1) ? &p.v_map : &p.k_map;
-        for (int j = 0; j < NB; ++j)
-          tma_load_3d(ring + st * TB + j * (kTile * 128), map, full_bar(st), j * 64, kvh,
-                      sq.k0 + tiles.at(i >> 1) * kTile);
+      int used = 0, q_used[2] = {0, 0};          // ring slots and Q halves that have been filled
+      while (ok && w.next()) {
+        const int kvh = w.head / a.group;
+        const KeyTiles<kTile> tiles = tiles_of();
+        const int n = tiles.count();
+        for (int h = 0; h < 2; ++h) {
+          if (half_tiles(h).count() == 0) continue;
+          if (!mbar_wait(q_empty_bar(h), (q_used[h] & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          ++q_used[h];
+          mbar_expect_tx(q_bar(h), TB);
+          for (int j = 0; j < NB; ++j)
+            tma_load_3d(q_base + h * TB + j * (kTile * 128), &p.q_map, q_bar(h), j * 64, w.head,
+                        w.sq.q0 + w.row0 + h * kTile);
+        }
+        for (int i = 0; i < 2 * n && ok; ++i, ++used) {      // K and V of a tile in turn
+          const int st = used % NS;
+          if (!mbar_wait(empty_bar(st), ((used / NS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          mbar_expect_tx(full_bar(st), TB);
+          const CUtensorMap* map = (i & 1) ? &p.v_map : &p.k_map;
+          for (int j = 0; j < NB; ++j)
+            tma_load_3d(ring + st * TB + j * (kTile * 128), map, full_bar(st), j * 64, kvh,
+                        w.sq.k0 + tiles.at(i >> 1) * kTile);
+        }
       }
       if (!ok) {
         *abort_flag = 1;
@@ -129,79 +134,97 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       }
     }
   } else if (warp == kMmaWarp) {
-    const KeyTiles<kTile> need[2] = {half_tiles(0), half_tiles(1)};
     const uint32_t idesc_s = make_idesc(kTile, 0, 0), idesc_o = make_idesc(DP, 0, 1);
     const bool one = elect_one();
-    int done[2] = {0, 0};
+    int base = 0;                                // ring slots of the tiles before
+    int q_used[2] = {0, 0}, done[2] = {0, 0};    // Q halves, and P tiles of a half, over all tiles
     bool ok = true;
-    auto wait_slot = [&](int i) { return mbar_wait(full_bar(i % NS), (i / NS) & 1u, abort_flag); };
-    auto issue_s = [&](int h, int it) {
-      const uint64_t kd = make_desc_kmajor_rows(ring + ((2 * it) % NS) * TB, 128);
-      const uint64_t qd = make_desc_kmajor_rows(q_base + h * TB, 128);
-#pragma unroll
-      for (int k = 0; k < DP / 16; ++k) {
-        const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;      // the address field counts 16 bytes
-        umma_bf16(tmem + h * kTile, qd + off, kd + off, idesc_s, k != 0);
-      }
-      umma_commit(s_bar(h));
+    auto wait_slot = [&](int i) {
+      return __all_sync(0xffffffffu, mbar_wait(full_bar(i % NS), (i / NS) & 1u, abort_flag)) != 0;
     };
-    if (n > 0) ok = wait_slot(0);
-    tc_fence_after();
-    for (int h = 0; h < 2 && ok && n > 0; ++h) {
-      if (need[h].count() == 0) continue;
-      ok = mbar_wait(q_bar(h), 0, abort_flag);
-      tc_fence_after();
-      if (ok && one && need[h].has(tiles.at(0))) issue_s(h, 0);
-    }
-    if (ok && n > 0 && one) umma_commit(empty_bar(0));
-    for (int it = 0; it < n && ok; ++it) {
-      const int vi = 2 * it + 1;
-      if (it + 1 < n) ok = wait_slot(2 * it + 2);
-      ok = ok && wait_slot(vi);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-      const int j0 = tiles.at(it) * kTile;
-      const uint32_t vb = ring + (vi % NS) * TB;
-      if (j0 + kTile > sq.lk) {
-        // rows behind the last key belong to someone else and may hold anything; P is zero there, V has to be finite
-        const int first = sq.lk - j0;
-        for (int i = lane; i < (kTile - first) * 8 * NB; i += 32) {
-          const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
-          asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + blk * (kTile * 128) + r * 128 + c * 16), "r"(0)
-                       : "memory");
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-      }
-      tc_fence_after();
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (need[h].has(tiles.at(it))) {
-          const uint64_t vd = make_desc(vb, kTile * 128, 1024);
-#pragma unroll
-          for (int c = 0; c < 2 && ok; ++c) {                // the two halves of P as they come
-            ok = __all_sync(0xffffffffu, mbar_wait(p_bar(h) + 16u * c, done[h] & 1u, abort_flag));
-            if (!ok) break;
-            tc_fence_after();
-            if (one) {
-#pragma unroll
-              for (int k = 4 * c; k < 4 * c + 4; ++k)
-                umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + k * 8, vd + k * (2048 >> 4), idesc_o,
-                             (done[h] | k) != 0);
-              if (c == 0) umma_commit(v_bar(h));
-            }
-          }
-          if (!ok) break;
-          if (one && done[h] + 1 == need[h].count()) umma_commit(o_bar(h));
-          ++done[h];
-        }
+    while (ok && w.next()) {
+      const KeyTiles<kTile> tiles = tiles_of();
+      const KeyTiles<kTile> need[2] = {half_tiles(0), half_tiles(1)};
+      const int n = tiles.count();
+      int left[2] = {need[0].count(), need[1].count()};      // S tiles still to be issued
+      int nth[2] = {0, 0};
+      auto issue_s = [&](int h, int it) {
+        const uint64_t kd = make_desc_kmajor_rows(ring + ((base + 2 * it) % NS) * TB, 128);
+        const uint64_t qd = make_desc_kmajor_rows(q_base + h * TB, 128);
         if (one) {
-          if (h == 1) umma_commit(empty_bar(vi % NS));
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k) {
+            const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;  // the address field counts 16 bytes
+            umma_bf16(tmem + h * kTile, qd + off, kd + off, idesc_s, k != 0);
+          }
+          umma_commit(s_bar(h));
+          if (left[h] == 1) umma_commit(q_empty_bar(h));
+        }
+        --left[h];
+      };
+      if (n > 0) ok = wait_slot(base);
+      tc_fence_after();
+      for (int h = 0; h < 2 && ok && n > 0; ++h) {
+        if (left[h] == 0) continue;
+        ok = __all_sync(0xffffffffu, mbar_wait(q_bar(h), q_used[h] & 1u, abort_flag));
+        ++q_used[h];
+        tc_fence_after();
+        if (ok && need[h].has(tiles.at(0))) issue_s(h, 0);
+      }
+      if (ok && n > 0 && one) umma_commit(empty_bar(base % NS));
+      for (int it = 0; it < n && ok; ++it) {
+        const int vi = base + 2 * it + 1;
+        if (it + 1 < n) ok = wait_slot(vi + 1);
+        ok = ok && wait_slot(vi);
+        if (!ok) break;
+        const int j0 = tiles.at(it) * kTile;
+        const uint32_t vb = ring + (vi % NS) * TB;
+        if (j0 + kTile > w.sq.lk) {
+          // rows behind the last key belong to someone else and may hold anything; P is zero there, V has to be finite
+          const int first = w.sq.lk - j0;
+          for (int i = lane; i < (kTile - first) * 8 * NB; i += 32) {
+            const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
+            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + blk * (kTile * 128) + r * 128 + c * 16),
+                         "r"(0)
+                         : "memory");
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        const uint64_t vd = make_desc(vb, kTile * 128, 1024);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (!ok) break;
+          if (need[h].has(tiles.at(it))) {
+            // the first product of a tile overwrites O, which the tile before has to have been read out of
+            if (nth[h] == 0)
+              ok = __all_sync(0xffffffffu, mbar_wait(o_empty_bar(h), (q_used[h] & 1u), abort_flag));
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {                    // the two halves of P as they come
+              ok = ok && __all_sync(0xffffffffu, mbar_wait(p_bar(h) + 16u * c, done[h] & 1u, abort_flag));
+              if (!ok) break;
+              tc_fence_after();
+              if (one) {
+#pragma unroll
+                for (int k = 4 * c; k < 4 * c + 4; ++k)
+                  umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + k * 8, vd + k * (2048 >> 4), idesc_o,
+                               (nth[h] | k) != 0);
+                if (c == 0) umma_commit(v_bar(h));
+              }
+            }
+            if (!ok) break;
+            ++done[h];
+            if (++nth[h] == need[h].count() && one) umma_commit(o_bar(h));
+          }
+          if (one && h == 1) umma_commit(empty_bar(vi % NS));
           if (it + 1 < n) {
             if (need[h].has(tiles.at(it + 1))) issue_s(h, it + 1);
-            if (h == 1) umma_commit(empty_bar((vi + 1) % NS));
+            if (one && h == 1) umma_commit(empty_bar((vi + 1) % NS));
           }
         }
       }
+      base += 2 * n;
     }
     if (!ok && lane == 0) {
       *abort_flag = 1;
@@ -215,22 +238,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     const int row = h * kTile + (warp & 3) * 32 + lane;      // in the block
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lanes + h * kTile, o_addr = tmem + lanes + 2 * kTile + h * DP;
-    const KeyTiles<kTile> need = half_tiles(h);
-    const int total = need.count();
-    const int half_rows = clamp_int(rows - h * kTile, 0, kTile);
-    const int p0 = sq.shift + r0 + h * kTile, p1 = p0 + half_rows - 1;
-    const int pos = sq.shift + r0 + row;
-    const RowKeys keys = row_keys(sq, a.causal, a.window, pos);
     // scores in base 2: exp2 of them is e^s
     const float mul = CAP ? a.scale / a.softcap : a.scale * kLog2e;
     const float cap2 = a.softcap * kLog2e;
-    const float slope2 = BIAS ? a.slopes[head] * kLog2e : 0.f;
     constexpr bool kTransformed = CAP || BIAS;               // else the factor goes into the exponent's multiply-add
     const float to2 = kTransformed ? 1.f : mul;
-    float m = -INFINITY, l = 0.f;                            // m in base 2
-    float tile_sum = 0.f;                                    // the last tile's part of l
     bool ok = true;
-    int cnt = 0;
+    int cnt = 0;                                             // tiles of this half so far, over all row tiles
+    int o_used = 0;
     auto scale_o = [&](float f) {
 #pragma unroll 1
       for (int i = 0; i < DP / 16; ++i) {
@@ -242,136 +257,156 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         tmem_st16(o_addr + i * 16, o);
       }
     };
-    for (int it = 0; it < n && ok; ++it) {
-      const int t = tiles.at(it);
-      if (!need.has(t)) continue;
-      const bool whole = all_seen(sq, a.causal, a.window, p0, p1, t * kTile, t * kTile + kTile);
-      ok = __all_sync(0xffffffffu, mbar_wait(s_bar(h), cnt & 1u, abort_flag));
-      if (!ok) break;
-      tc_fence_after();
-      // S is there, so the products before it have finished and O stands still
-      if (__any_sync(0xffffffffu, tile_sum > 256.f)) {       // the last tile's p had grown: m follows
-        const float k = tile_sum > 256.f ? ceilf(log2f(tile_sum)) : 0.f, f = ex2(-k);
-        m += k;
-        l *= f;
-        scale_o(f);
-      }
-      tile_sum = 0.f;
-#pragma unroll 1
-      for (int c = 0; c < 2 && ok; ++c) {
-        const int j0 = t * kTile + c * 64;
-        float x[64];
-        tmem_ld32(s_addr + c * 64, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
-        tmem_ld32(s_addr + c * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
-        tmem_ld_wait();
-        if (kTransformed) {
-#pragma unroll
-          for (int j = 0; j < 64; ++j) {
-            x[j] *= mul;
-            if (CAP) x[j] = cap2 * tanh_fast(x[j]);
-            if (BIAS) x[j] = fmaf(-slope2, fabsf((float)(pos - j0 - j)), x[j]);
-          }
-        }
-        if (!whole) {
-          const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
-#pragma unroll
-          for (int j = 0; j < 64; ++j)
-            if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
-        }
-        uint32_t pk[32];
-        float sum;
-        bool reset = m == -INFINITY;                         // nothing seen yet; below: p near the end of its range
-        while (true) {
-          if (__any_sync(0xffffffffu, reset)) {
-            float mx[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-            for (int j = 4; j < 64; ++j) mx[j & 3] = fmaxf(mx[j & 3], x[j]);
-            const float mt = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * to2);
-            const float m_new = reset ? fmaxf(mt, m) : m;
-            const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
-            m = m_new;
-            l *= f;
-            tile_sum *= f;
-            if (c == 1) {                                    // the first half's P may still be on its way into O
-              ok = __all_sync(0xffffffffu, mbar_wait(v_bar(h), cnt & 1u, abort_flag));
-              if (!ok) break;
-              tc_fence_after();
-            }
-            if (cnt > 0 || c == 1) scale_o(f);
-          }
-          const float shift = m == -INFINITY ? 0.f : -m;
-          const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
-          uint64_t acc[2] = {0ull, 0ull};
-          auto exponentials = [&](auto polys) {              // the last `polys` of 8 pairs on the fp32 pipes
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              uint64_t v = pair2(x[2 * i], x[2 * i + 1]);
-              v = kTransformed ? add2(v, shift_2) : fma2(v, mul_2, shift_2);
-              float e0, e1;
-              if ((i & 7) >= 8 - polys.value) {
-                ex2_poly(v, e0, e1);
-              } else {
-                unpair2(v, e0, e1);
-                e0 = ex2(e0);
-                e1 = ex2(e1);
-              }
-              acc[i & 1] = add2(acc[i & 1], pair2(e0, e1));
-              pk[i] = bf16x2(e0, e1);
-            }
-          };
-          if (whole) exponentials(Int<kPolys>());
-          else exponentials(Int<0>());
-          float l0, l1;
-          unpair2(add2(acc[0], acc[1]), l0, l1);
-          sum = l0 + l1;
-          tmem_st32(s_addr + c * 32, pk);                    // over scores of the tile's first half
-          reset = sum > 0x1p100f;
-          if (!__any_sync(0xffffffffu, reset)) break;
-        }
+    while (ok && w.next()) {
+      const KeyTiles<kTile> tiles = tiles_of(), need = half_tiles(h);
+      const int n = tiles.count(), total = need.count(), rows = rows_of();
+      const int half_rows = clamp_int(rows - h * kTile, 0, kTile);
+      const int p0 = w.sq.shift + w.row0 + h * kTile, p1 = p0 + half_rows - 1;
+      const int pos = w.sq.shift + w.row0 + row;
+      const RowKeys keys = row_keys(w.sq, a.causal, a.window, pos);
+      const float slope2 = BIAS ? a.slopes[w.head] * kLog2e : 0.f;
+      float m = -INFINITY, l = 0.f;                            // m in base 2
+      float tile_sum = 0.f;                                    // the last tile's part of l
+      int nth = 0;
+      for (int it = 0; it < n && ok; ++it) {
+        const int t = tiles.at(it);
+        if (!need.has(t)) continue;
+        const bool whole = all_seen(w.sq, a.causal, a.window, p0, p1, t * kTile, t * kTile + kTile);
+        ok = __all_sync(0xffffffffu, mbar_wait(s_bar(h), cnt & 1u, abort_flag));
         if (!ok) break;
-        l += sum;
-        tile_sum += sum;
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_bar(h) + 16u * c);
-      }
-      ++cnt;
-    }
-    if (ok && total > 0) {
-      ok = __all_sync(0xffffffffu, mbar_wait(o_bar(h), 0, abort_flag));
-      tc_fence_after();
-    }
-    if (ok) {
-      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // a row that sees nothing gives zeros
-      const bool mine = row < rows;
-      bf16* dst = reinterpret_cast<bf16*>(a.out) + (size_t)(sq.q0 + r0 + (mine ? row : 0)) * a.o_stride +
-                  (size_t)head * a.head_dim;
-#pragma unroll
-      for (int c = 0; c < DP / 32; ++c) {
-        uint32_t o[32];
-        if (total > 0) {
-          tmem_ld32(o_addr + c * 32, o);
-          tmem_ld_wait();
+        tc_fence_after();
+        // S is there, so the products before it have finished and O stands still
+        if (__any_sync(0xffffffffu, tile_sum > 256.f)) {       // the last tile's p had grown: m follows
+          const float k = tile_sum > 256.f ? ceilf(log2f(tile_sum)) : 0.f, f = ex2(-k);
+          m += k;
+          l *= f;
+          scale_o(f);
         }
+        tile_sum = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < 2 && ok; ++c) {
+          const int j0 = t * kTile + c * 64;
+          float x[64];
+          tmem_ld32(s_addr + c * 64, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+          tmem_ld32(s_addr + c * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+          tmem_ld_wait();
+          if (kTransformed) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          if (mine && c * 32 + g * 8 < a.head_dim) {
-            uint4 w;
-            uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float x = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
-              const float y = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
-              wp[i] = bf16x2(x, y);
+            for (int j = 0; j < 64; ++j) {
+              x[j] *= mul;
+              if (CAP) x[j] = cap2 * tanh_fast(x[j]);
+              if (BIAS) x[j] = fmaf(-slope2, fabsf((float)(pos - j0 - j)), x[j]);
             }
-            *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = w;
+          }
+          if (!whole) {
+            const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+              if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
+          }
+          uint32_t pk[32];
+          float sum;
+          bool reset = m == -INFINITY;                         // nothing seen yet; below: p near the end of its range
+          while (true) {
+            if (__any_sync(0xffffffffu, reset)) {
+              float mx[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+              for (int j = 4; j < 64; ++j) mx[j & 3] = fmaxf(mx[j & 3], x[j]);
+              const float mt = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * to2);
+              const float m_new = reset ? fmaxf(mt, m) : m;
+              const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
+              m = m_new;
+              l *= f;
+              tile_sum *= f;
+              if (c == 1) {                                    // the first half's P may still be on its way into O
+                ok = __all_sync(0xffffffffu, mbar_wait(v_bar(h), cnt & 1u, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+              }
+              if (nth > 0 || c == 1) scale_o(f);
+            }
+            const float shift = m == -INFINITY ? 0.f : -m;
+            const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
+            uint64_t acc[2] = {0ull, 0ull};
+            auto exponentials = [&](auto polys) {              // the last `polys` of 8 pairs on the fp32 pipes
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                uint64_t v = pair2(x[2 * i], x[2 * i + 1]);
+                v = kTransformed ? add2(v, shift_2) : fma2(v, mul_2, shift_2);
+                float e0, e1;
+                if ((i & 7) >= 8 - polys.value) {
+                  ex2_poly(v, e0, e1);
+                } else {
+                  unpair2(v, e0, e1);
+                  e0 = ex2(e0);
+                  e1 = ex2(e1);
+                }
+                acc[i & 1] = add2(acc[i & 1], pair2(e0, e1));
+                pk[i] = bf16x2(e0, e1);
+              }
+            };
+            if (whole) exponentials(Int<kPolys>());
+            else exponentials(Int<0>());
+            float l0, l1;
+            unpair2(add2(acc[0], acc[1]), l0, l1);
+            sum = l0 + l1;
+            tmem_st32(s_addr + c * 32, pk);                    // over scores of the tile's first half
+            reset = sum > 0x1p100f;
+            if (!__any_sync(0xffffffffu, reset)) break;
+          }
+          if (!ok) break;
+          l += sum;
+          tile_sum += sum;
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_bar(h) + 16u * c);
+        }
+        ++cnt;
+        ++nth;
+      }
+      if (ok && total > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(o_bar(h), o_used & 1u, abort_flag));
+        ++o_used;
+        tc_fence_after();
+      }
+      if (ok && rows > h * kTile) {
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // a row that sees nothing gives zeros
+        const bool mine = row < rows;
+        bf16* dst = reinterpret_cast<bf16*>(a.out) + (size_t)(w.sq.q0 + w.row0 + (mine ? row : 0)) * a.o_stride +
+                    (size_t)w.head * a.head_dim;
+#pragma unroll
+        for (int c = 0; c < DP / 32; ++c) {
+          uint32_t o[32];
+          if (total > 0) {
+            tmem_ld32(o_addr + c * 32, o);
+            tmem_ld_wait();
+            if (c == DP / 32 - 1) {                            // O may be written again
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(o_empty_bar(h));
+            }
+          }
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            if (mine && c * 32 + g * 8 < a.head_dim) {
+              uint4 v;
+              uint32_t* wp = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float x = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
+                const float y = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
+                wp[i] = bf16x2(x, y);
+              }
+              *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = v;
+            }
           }
         }
+        if (a.lse && mine)
+          a.lse[(size_t)w.head * a.q_rows + w.sq.q0 + w.row0 + row] = (m + log2f(l)) * kLn2;
       }
-      if (a.lse && mine)
-        a.lse[(size_t)head * a.q_rows + sq.q0 + r0 + row] = (m + log2f(l)) * kLn2;
-    } else if (lane == 0) {
+    }
+    if (!ok && lane == 0) {
       *abort_flag = 1;
       if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
     }
@@ -415,8 +450,10 @@ cudaError_t launch_attn_forward_tc(const AttnArgs& a, cudaStream_t st) {
       !tc_encode_heads(&p.k_map, a.k, kr, a.kv_heads, a.head_dim, a.k_stride, kTile) ||
       !tc_encode_heads(&p.v_map, a.v, kr, a.kv_heads, a.head_dim, a.v_stride, kTile))
     return cudaErrorInvalidValue;
-  const long long grid = ((long long)(a.q_rows + 2 * kTile - 1) / (2 * kTile) + a.n_seqs) * a.q_heads;
-  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  const long long most = ((long long)(a.q_rows + kFwdTile - 1) / kFwdTile + a.n_seqs) * a.q_heads;
+  if (most > 0x7fff0000LL) return cudaErrorInvalidValue;
+  const int sms = attn_sm_count();
+  const long long grid = most < sms ? most : sms;            // one block per SM, which walks over the tiles
   return a.head_dim <= 64 ? launch_dp<64>(p, (unsigned)grid, st) : launch_dp<128>(p, (unsigned)grid, st);
 }
 
