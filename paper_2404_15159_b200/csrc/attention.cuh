@@ -245,6 +245,31 @@ __device__ __forceinline__ float tanh_fast(float x) {
   return 1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kLog2e)));
 }
 
+// x <- tanh(x * mul) for a thread's scores.  Where none of a warp's lies above 3/4, as with scores well below the cap, on
+// the fp32 pipes: the odd polynomial of degree 11 with the least absolute error there (7e-8 in fp32; fitted for this
+// purpose by linear programming), 2.5 times as fast as two special-function operations a value.
+template <int N>
+__device__ __forceinline__ void tanh_all(float (&x)[N], float mul) {
+  float mx[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < N; ++j) mx[j & 1] = fmaxf(mx[j & 1], fabsf(x[j]));
+  if (__any_sync(0xffffffffu, fmaxf(mx[0], mx[1]) * mul > 0.75f)) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = tanh_fast(x[j] * mul);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+      const uint64_t u = mul2(pair2(x[j], x[j + 1]), pair2(mul, mul)), t = mul2(u, u);
+      uint64_t y = fma2(t, pair2(-0.004493420943617821f, -0.004493420943617821f), pair2(0.019237183034420013f, 0.019237183034420013f));
+      y = fma2(y, t, pair2(-0.053149230778217316f, -0.053149230778217316f));
+      y = fma2(y, t, pair2(0.13320578634738922f, 0.13320578634738922f));
+      y = fma2(y, t, pair2(-0.33332470059394836f, -0.33332470059394836f));
+      y = fma2(y, t, pair2(0.9999998211860657f, 0.9999998211860657f));
+      unpair2(mul2(y, u), x[j], x[j + 1]);
+    }
+  }
+}
+
 // Lets a kernel use `bytes` of dynamic shared memory: asked of the runtime once per kernel and device.
 template <typename K>
 cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64]) {

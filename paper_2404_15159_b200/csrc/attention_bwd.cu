@@ -171,31 +171,29 @@ __device__ __forceinline__ void block_end(const Ctl& c, uint32_t tmem) {
   }
 }
 
-// p of two neighbouring scores: 2^(score - log-sum-exp), in base 2; with a cap also its slope.  `neg_lse` is minus the
-// log-sum-exp, `d0`, `d1` are the distances.
+// p of two neighbouring scores: 2^(score - log-sum-exp), in base 2; with a cap the scores are tanh already, and the slope
+// comes back too.  `neg_lse` is minus the log-sum-exp, `d0`, `d1` are the distances.
 template <bool CAP, bool BIAS>
 struct Score {
-  float mul, cap2, slope2;
+  float mul, factor, slope2;
   __device__ __forceinline__ Score(const AttnArgs& a, int head)
-      : mul(CAP ? a.scale / a.softcap : a.scale * kLog2e), cap2(a.softcap * kLog2e),
+      : mul(a.scale / a.softcap), factor(CAP ? a.softcap * kLog2e : a.scale * kLog2e),
         slope2(BIAS ? a.slopes[head] * kLog2e : 0.f) {}
+  template <int N>
+  __device__ __forceinline__ void cap(float (&s)[N]) const {
+    if (CAP) tanh_all(s, mul);
+  }
   template <bool POLY>
-  __device__ __forceinline__ void probs(float s0, float s1, uint64_t neg_lse, int d0, int d1, float& p0, float& p1,
+  __device__ __forceinline__ void probs(float s0, float s1, uint64_t neg_lse, float d0, float d1, float& p0, float& p1,
                                         uint64_t& cap_slope) const {
-    uint64_t x;
-    if (CAP) {
-      const float t0 = tanh_fast(s0 * mul), t1 = tanh_fast(s1 * mul);
-      const uint64_t t = pair2(t0, t1);
-      cap_slope = fma2(pair2(-t0, -t1), t, pair2(1.f, 1.f));
-      x = fma2(t, pair2(cap2, cap2), neg_lse);
-    } else {
-      x = fma2(pair2(s0, s1), pair2(mul, mul), neg_lse);
-    }
+    const uint64_t s = pair2(s0, s1);
+    if (CAP) cap_slope = fma2(pair2(-s0, -s1), s, pair2(1.f, 1.f));
+    const uint64_t x = fma2(s, pair2(factor, factor), neg_lse);
     float x0, x1;
     unpair2(x, x0, x1);
     if (BIAS) {
-      x0 = fmaf(-slope2, fabsf((float)d0), x0);
-      x1 = fmaf(-slope2, fabsf((float)d1), x1);
+      x0 = fmaf(-slope2, fabsf(d0), x0);
+      x1 = fmaf(-slope2, fabsf(d1), x1);
     }
     if (POLY) {
       ex2_poly(pair2(x0, x1), p0, p1);
@@ -385,6 +383,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
           r_lo -= i0;
           r_hi -= i0;
         }
+        const float d = (float)(pos0 - j);
+        score.cap(pr);
 #pragma unroll
         for (int c0 = 0; c0 < 2; ++c0) {
           uint64_t cs[CAP ? 16 : 1];
@@ -392,15 +392,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
 #pragma unroll
           for (int x = 0; x < 32; x += 4) {
             const float4 ls = *reinterpret_cast<const float4*>(neg_lse + c0 * 32 + x);
-            const int d0 = pos0 + c0 * 32 + x - j;
+            const float d0 = d + (float)(c0 * 32 + x);
             uint64_t& cs0 = cs[CAP ? x / 2 : 0];
             uint64_t& cs1 = cs[CAP ? x / 2 + 1 : 0];
             if ((x / 2 & 7) >= 8 - kPolys) {                   // known when unrolled
-              score.template probs<true>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1, pc[x], pc[x + 1], cs0);
-              score.template probs<true>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2, d0 + 3, pc[x + 2], pc[x + 3], cs1);
+              score.template probs<true>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1.f, pc[x], pc[x + 1], cs0);
+              score.template probs<true>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
             } else {
-              score.template probs<false>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1, pc[x], pc[x + 1], cs0);
-              score.template probs<false>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2, d0 + 3, pc[x + 2], pc[x + 3], cs1);
+              score.template probs<false>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1.f, pc[x], pc[x + 1], cs0);
+              score.template probs<false>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
             }
           }
           if (!whole) {
@@ -612,13 +612,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
         tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
         tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
         tmem_ld_wait();
+        const float d = (float)(pos - j0);
+        score.cap(pr);
 #pragma unroll
         for (int x = 0; x < 64; x += 2) {
           uint64_t cs;
           if ((x / 2 & 7) >= 8 - kPolys)
-            score.template probs<true>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
+            score.template probs<true>(pr[x], pr[x + 1], neg_lse, d - x, d - (x + 1), pr[x], pr[x + 1], cs);
           else
-            score.template probs<false>(pr[x], pr[x + 1], neg_lse, pos - j0 - x, pos - j0 - x - 1, pr[x], pr[x + 1], cs);
+            score.template probs<false>(pr[x], pr[x + 1], neg_lse, d - x, d - (x + 1), pr[x], pr[x + 1], cs);
           if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
         }
         if (!whole) {

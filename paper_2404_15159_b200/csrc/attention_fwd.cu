@@ -290,13 +290,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
           tmem_ld32(s_addr + c * 64, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
           tmem_ld32(s_addr + c * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
           tmem_ld_wait();
-          if (kTransformed) {
+          if (CAP) {
+            tanh_all(x, mul);
 #pragma unroll
-            for (int j = 0; j < 64; ++j) {
-              x[j] *= mul;
-              if (CAP) x[j] = cap2 * tanh_fast(x[j]);
-              if (BIAS) x[j] = fmaf(-slope2, fabsf((float)(pos - j0 - j)), x[j]);
-            }
+            for (int j = 0; j < 64; j += 2) unpair2(mul2(pair2(x[j], x[j + 1]), pair2(cap2, cap2)), x[j], x[j + 1]);
+          }
+          if (BIAS) {
+            const float d = (float)(pos - j0);
+#pragma unroll
+            for (int j = 0; j < 64; ++j) x[j] = fmaf(-slope2, fabsf(d - (float)j), CAP ? x[j] : x[j] * mul);
           }
           if (!whole) {
             const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
