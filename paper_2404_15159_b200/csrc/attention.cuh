@@ -177,32 +177,6 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&e);
 }
 
-// 2^x of two values on the fp32 pipes, for the share of a tile's exponentials that the special-function unit (16 a cycle
-// and SM) would be late with.  x = n + f with n whole (rounded by adding and taking away 1.5 * 2^23) and |f| <= 1/2; 2^f
-// by the polynomial of degree 4 with the least relative error there (2.7e-6, fitted for this purpose by linear
-// programming; p itself is rounded to 2^-8 afterwards), n added to the exponent.  x is held inside
-// [-126, 127], so keys that are hidden (-inf) must not come here.  A NaN gives a value near the largest.
-__device__ __forceinline__ void ex2_poly(uint64_t x, float& e0, float& e1) {
-  float x0, x1;
-  unpair2(x, x0, x1);
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x0) : "f"(-126.f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x1) : "f"(-126.f));
-  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x0) : "f"(127.f));
-  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x1) : "f"(127.f));
-  x = pair2(x0, x1);
-  const uint64_t t = add2(x, pair2(12582912.f, 12582912.f));
-  const uint64_t f = fma2(add2(t, pair2(-12582912.f, -12582912.f)), pair2(-1.f, -1.f), x);
-  uint64_t y = fma2(f, pair2(0.00957053154706955f, 0.00957053154706955f), pair2(0.05591866374015808f, 0.05591866374015808f));
-  y = fma2(y, f, pair2(0.24024735391139984f, 0.24024735391139984f));
-  y = fma2(y, f, pair2(0.6931216716766357f, 0.6931216716766357f));
-  y = fma2(y, f, pair2(0.9999992847442627f, 0.9999992847442627f));
-  float t0, t1, y0, y1;
-  unpair2(t, t0, t1);
-  unpair2(y, y0, y1);
-  e0 = __uint_as_float((__float_as_uint(t0) << 23) + __float_as_uint(y0));
-  e1 = __uint_as_float((__float_as_uint(t1) << 23) + __float_as_uint(y1));
-}
-
 // A block's walk over (tile, head) pairs: rounds over the sorted tiles with the heads fastest, every other round from
 // the other end.  One 32-byte load tells a tile; the next one is fetched while this one is worked on.
 struct TileWalk {

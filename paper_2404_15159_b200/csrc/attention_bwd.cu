@@ -32,8 +32,6 @@ constexpr int kStagesA = 3, kStagesB = 2;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
 constexpr uint32_t kRowBytes = 2 * kTile * 4;    // minus lse and minus delta of a query tile, two stages
 template <int DP> constexpr uint32_t kSmemBytes = (2 + kStagesA + kStagesB) * kTileBytes<DP> + 2 * kRowBytes + 256;
-// Of 8 pairs of exponentials those that go to the fp32 pipes
-constexpr int kPolys = 2;
 
 struct BwdParams {
   AttnArgs a;
@@ -102,17 +100,25 @@ __device__ __forceinline__ void issue_ts(uint32_t d, uint32_t a, uint32_t b, boo
   for (int k = 0; k < kTile / 16; ++k)
     umma_bf16_ts(d, a + (k >> 2) * 64 + (k & 3) * 8, bd + k * (2048 >> 4), idesc, accumulate || k != 0);
 }
-// One row of the sums to memory; `empty` is told once they have been read (zeros are written where there are none).
-template <int DP>
-__device__ __forceinline__ void store_row(uint32_t acc, bool any, uint32_t empty, float mul, bool mine, bf16* dst,
-                                          int head_dim) {
+// 64 zeros of p or ds
+__device__ __forceinline__ void store_zeros(uint32_t addr) {
+  uint32_t z[16];
 #pragma unroll
-  for (int c = 0; c < DP / 32; ++c) {
+  for (int i = 0; i < 16; ++i) z[i] = 0;
+  tmem_st16(addr, z);
+  tmem_st16(addr + 16, z);
+}
+// N values of a row of the sums to memory, those before `valid`; `empty` is told once they have been read (zeros are written where there are none).
+template <int N>
+__device__ __forceinline__ void store_row(uint32_t acc, bool any, uint32_t empty, float mul, bool mine, bf16* dst,
+                                          int valid) {
+#pragma unroll
+  for (int c = 0; c < N / 32; ++c) {
     uint32_t v[32];
     if (any) {
       tmem_ld32(acc + c * 32, v);
       tmem_ld_wait();
-      if (c == DP / 32 - 1) {
+      if (c == N / 32 - 1) {
         tc_fence_before();
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(empty);
@@ -120,7 +126,7 @@ __device__ __forceinline__ void store_row(uint32_t acc, bool any, uint32_t empty
     }
 #pragma unroll
     for (int g = 0; g < 4; ++g)
-      if (mine && c * 32 + g * 8 < head_dim) {
+      if (mine && c * 32 + g * 8 < valid) {
         uint4 w = make_uint4(0, 0, 0, 0);
         if (any) {
           uint32_t* wp = reinterpret_cast<uint32_t*>(&w);
@@ -183,7 +189,6 @@ struct Score {
   __device__ __forceinline__ void cap(float (&s)[N]) const {
     if (CAP) tanh_all(s, mul);
   }
-  template <bool POLY>
   __device__ __forceinline__ void probs(float s0, float s1, uint64_t neg_lse, float d0, float d1, float& p0, float& p1,
                                         uint64_t& cap_slope) const {
     const uint64_t s = pair2(s0, s1);
@@ -195,12 +200,8 @@ struct Score {
       x0 = fmaf(-slope2, fabsf(d0), x0);
       x1 = fmaf(-slope2, fabsf(d1), x1);
     }
-    if (POLY) {
-      ex2_poly(pair2(x0, x1), p0, p1);
-    } else {
-      p0 = ex2(x0);
-      p1 = ex2(x1);
-    }
+    p0 = ex2(x0);
+    p1 = ex2(x1);
   }
 };
 
@@ -365,24 +366,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
         const float* neg_lse = rows_smem + (at & 1) * (2 * kTile) + half * 64;
         const float* neg_delta = neg_lse + kTile;
         const int pos0 = w.sq.shift + i0;
-        // the tile's rows behind the last see nothing
-        const bool whole = i0 + 64 <= w.sq.lq && all_seen(w.sq, a.causal, a.window, pos0, pos0 + 63, j0, j0 + kTile);
+        // the rows of these 64 that see this key: [r_lo, r_hi); what that comes to for the warp's keys: all, some (hidden
+        // ones become zeros), or nothing
+        int r_lo = 0, r_hi = 0;
+        if (j < w.sq.lk) query_rows(w.sq, a.causal, a.window, j, j + 1, &r_lo, &r_hi);
+        r_lo -= i0;
+        r_hi -= i0;
+        const bool whole = __all_sync(0xffffffffu, r_lo <= 0 && r_hi >= 64);
+        const bool none = __all_sync(0xffffffffu, min(r_hi, 64) <= max(r_lo, 0));
         ok = __all_sync(0xffffffffu, mbar_wait(c.rows_full(at), (at >> 1) & 1u, c.abort_flag) &&
                                          mbar_wait(c.s(0), at & 1u, c.abort_flag));
         if (!ok) break;
         tc_fence_after();
         float pr[64];
+        if (none) {
+          store_zeros(s_addr);
+        } else {
         tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
         tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
         tmem_ld_wait();
-        // rows that see this key: [r_lo, r_hi), or all where the key lies before the prefix
-        int r_lo = 0, r_hi = 64;
-        if (!whole) {
-          r_hi = 0;
-          if (j < w.sq.lk) query_rows(w.sq, a.causal, a.window, j, j + 1, &r_lo, &r_hi);
-          r_lo -= i0;
-          r_hi -= i0;
-        }
         const float d = (float)(pos0 - j);
         score.cap(pr);
 #pragma unroll
@@ -395,13 +397,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
             const float d0 = d + (float)(c0 * 32 + x);
             uint64_t& cs0 = cs[CAP ? x / 2 : 0];
             uint64_t& cs1 = cs[CAP ? x / 2 + 1 : 0];
-            if ((x / 2 & 7) >= 8 - kPolys) {                   // known when unrolled
-              score.template probs<true>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1.f, pc[x], pc[x + 1], cs0);
-              score.template probs<true>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
-            } else {
-              score.template probs<false>(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1.f, pc[x], pc[x + 1], cs0);
-              score.template probs<false>(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
-            }
+            score.probs(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1.f, pc[x], pc[x + 1], cs0);
+            score.probs(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
           }
           if (!whole) {
 #pragma unroll
@@ -422,6 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
             }
           }
         }
+        }
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -429,6 +427,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
         ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), at & 1u, c.abort_flag));
         if (!ok) break;
         tc_fence_after();
+        if (none) {
+          store_zeros(dp_addr);
+        } else {
 #pragma unroll
         for (int c0 = 0; c0 < 2; ++c0) {
           float dp[32];
@@ -454,6 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
             pk[x / 2 + 1] = bf16x2(f2, f3);
           }
           tmem_st16(dp_addr + c0 * 16, pk);
+        }
         }
         tmem_st_wait();
         tc_fence_before();
@@ -594,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
     while (ok && w.next()) {
       const KeyTiles<kTile> tiles = tiles_of();
       const int n = tiles.count(), rows = rows_of();
-      const int p0 = w.sq.shift + w.row0, p1 = p0 + rows - 1, pos = p0 + row;
+      const int pos = w.sq.shift + w.row0 + row;
       const bool mine = row < rows;
       const size_t place = (size_t)w.head * a.q_rows + w.sq.q0 + w.row0 + (mine ? row : 0);
       const float nl = mine ? -a.lse2[place] : -INFINITY, nd = mine ? -a.delta[place] : 0.f;
@@ -603,12 +605,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
       const RowKeys keys = row_keys(w.sq, a.causal, a.window, pos);
       for (int i = 0; i < n && ok; ++i, ++at) {
         const int j0 = tiles.at(i) * kTile + half * 64;
-        const bool whole = all_seen(w.sq, a.causal, a.window, p0, p1, j0, j0 + 64);
+        // what the warp's rows see of these 64 keys: all, some (hidden ones become zeros), or nothing
+        const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
+        const bool whole = __all_sync(0xffffffffu, (lo <= 0 && hi >= 64) || pre >= 64);
+        const bool none = __all_sync(0xffffffffu, min(hi, 64) <= max(lo, 0) && pre <= 0);
         const uint32_t s_addr = tmem + (at & 1) * kTile + lanes + half * 64;
         ok = __all_sync(0xffffffffu, mbar_wait(c.s(at & 1), (at >> 1) & 1u, c.abort_flag));
         if (!ok) break;
         tc_fence_after();
         float pr[64];
+        if (!none) {
         tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
         tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
         tmem_ld_wait();
@@ -617,21 +623,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
 #pragma unroll
         for (int x = 0; x < 64; x += 2) {
           uint64_t cs;
-          if ((x / 2 & 7) >= 8 - kPolys)
-            score.template probs<true>(pr[x], pr[x + 1], neg_lse, d - x, d - (x + 1), pr[x], pr[x + 1], cs);
-          else
-            score.template probs<false>(pr[x], pr[x + 1], neg_lse, d - x, d - (x + 1), pr[x], pr[x + 1], cs);
+          score.probs(pr[x], pr[x + 1], neg_lse, d - x, d - (x + 1), pr[x], pr[x + 1], cs);
           if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
         }
         if (!whole) {
-          const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
 #pragma unroll
           for (int x = 0; x < 64; ++x)
             if (!((x >= lo && x < hi) || x < pre)) pr[x] = 0.f;
         }
+        }
         ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), at & 1u, c.abort_flag));
         if (!ok) break;
         tc_fence_after();
+        if (none) {
+          store_zeros(s_addr);
+        } else {
 #pragma unroll
         for (int c0 = 0; c0 < 2; ++c0) {
           float dp[32];
@@ -650,6 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
             pk[x / 2] = bf16x2(f0, f1);
           }
           tmem_st16(s_addr + c0 * 16, pk);
+        }
         }
         tmem_st_wait();
         tc_fence_before();

@@ -18,15 +18,11 @@ constexpr int kTile = 128;                       // keys per step, and query row
 constexpr int kThreads = 384;                    // two softmax groups of 4 warps; a group with the load and MMA warps
 // A block starts with 168 registers a thread (384 x 168 = 64512); the softmax groups, whose threads hold half a row of
 // scores and its exponentials, take 208 and the third group keeps 88: (2 x 208 + 88) x 128 = 64512.
-constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kLoadWarp = 8, kMmaWarp = 9;       // and 10: one for each query half
 constexpr int kTmemCols = 512;
 template <int DP> constexpr int kStages = DP == 128 ? 5 : 8;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
 template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 320;
-
-// Of 8 pairs of exponentials those that go to the fp32 pipes
-constexpr int kPolys = 2;
-template <int N> struct Int { static constexpr int value = N; };
 
 struct FwdParams {
   AttnArgs a;
@@ -64,16 +60,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   auto o_empty_bar = [&](int h) { return bars + 8u * (2 * NS + 14 + h); };
   uint32_t* slot = reinterpret_cast<uint32_t*>(ctl + 8 * (2 * NS + 16));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(slot + 1);
+  volatile int* turns = reinterpret_cast<volatile int*>(slot + 2);       // [2] tiles of both halves that each has reached
 
   const AttnArgs& a = p.a;
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (threadIdx.x == 32) {
-    for (int s = 0; s < NS; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int s = 0; s < NS; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 2); }
     for (int h = 0; h < 2; ++h) {
       mbar_init(q_bar(h), 1); mbar_init(s_bar(h), 1); mbar_init(o_bar(h), 1); mbar_init(v_bar(h), 1);
       mbar_init(p_bar(h), 4); mbar_init(p_bar(h) + 16u, 4); mbar_init(q_empty_bar(h), 1); mbar_init(o_empty_bar(h), 4);
     }
     *abort_flag = 0;
+    turns[0] = turns[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kLoadWarp && lane == 0) { prefetch_tmap(&p.q_map); prefetch_tmap(&p.k_map); prefetch_tmap(&p.v_map); }
@@ -133,95 +131,100 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
       }
     }
-  } else if (warp == kMmaWarp) {
+  } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+    const int h = warp - kMmaWarp;
     const uint32_t idesc_s = make_idesc(kTile, 0, 0), idesc_o = make_idesc(DP, 0, 1);
+    const uint32_t t_s = tmem + h * kTile, t_o = tmem + 2 * kTile + h * DP;
     const bool one = elect_one();
     int base = 0;                                // ring slots of the tiles before
-    int q_used[2] = {0, 0}, done[2] = {0, 0};    // Q halves, and P tiles of a half, over all tiles
+    int q_used = 0, done = 0;                    // tiles of Q, and of P, so far
+    int both = 0;                                // tiles so far that both halves need
     bool ok = true;
+    // Where both halves walk over the same keys they take turns, the first one first: left alone they fall into step, with
+    // both at their exponentials and then both at the tensor cores.  A hint only: the wait is short and may be given up.
+    auto take_turn = [&](bool first_of_tile) {
+      for (int i = 0; i < 256; ++i)
+        if (h == 0 ? first_of_tile || turns[1] >= both : turns[0] > both) break;
+    };
+    // Every slot is waited for and given back, also where this half needs nothing of it: a slot is free when both halves
+    // have said so once.
     auto wait_slot = [&](int i) {
       return __all_sync(0xffffffffu, mbar_wait(full_bar(i % NS), (i / NS) & 1u, abort_flag)) != 0;
     };
     while (ok && w.next()) {
-      const KeyTiles<kTile> tiles = tiles_of();
-      const KeyTiles<kTile> need[2] = {half_tiles(0), half_tiles(1)};
-      const int n = tiles.count();
-      int left[2] = {need[0].count(), need[1].count()};      // S tiles still to be issued
-      int nth[2] = {0, 0};
-      auto issue_s = [&](int h, int it) {
-        const uint64_t kd = make_desc_kmajor_rows(ring + ((base + 2 * it) % NS) * TB, 128);
-        const uint64_t qd = make_desc_kmajor_rows(q_base + h * TB, 128);
-        if (one) {
+      const KeyTiles<kTile> tiles = tiles_of(), need = half_tiles(h), other = half_tiles(h ^ 1);
+      const int n = tiles.count(), total = need.count();
+      int issued = 0, nth = 0;
+      auto scores = [&](int it) {                // S of tile `it`, whose K is there
+        if (need.has(tiles.at(it))) {
+          ++issued;
+          if (one) {
+            const uint64_t kd = make_desc_kmajor_rows(ring + ((base + 2 * it) % NS) * TB, 128);
+            const uint64_t qd = make_desc_kmajor_rows(q_base + h * TB, 128);
 #pragma unroll
-          for (int k = 0; k < DP / 16; ++k) {
-            const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;  // the address field counts 16 bytes
-            umma_bf16(tmem + h * kTile, qd + off, kd + off, idesc_s, k != 0);
+            for (int k = 0; k < DP / 16; ++k) {
+              const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;  // the address field counts 16 bytes
+              umma_bf16(t_s, qd + off, kd + off, idesc_s, k != 0);
+            }
+            umma_commit(s_bar(h));
+            if (issued == total) umma_commit(q_empty_bar(h));
           }
-          umma_commit(s_bar(h));
-          if (left[h] == 1) umma_commit(q_empty_bar(h));
         }
-        --left[h];
+        if (one) umma_commit(empty_bar((base + 2 * it) % NS));
       };
-      if (n > 0) ok = wait_slot(base);
-      tc_fence_after();
-      for (int h = 0; h < 2 && ok && n > 0; ++h) {
-        if (left[h] == 0) continue;
-        ok = __all_sync(0xffffffffu, mbar_wait(q_bar(h), q_used[h] & 1u, abort_flag));
-        ++q_used[h];
-        tc_fence_after();
-        if (ok && need[h].has(tiles.at(0))) issue_s(h, 0);
+      if (total > 0) {
+        ok = __all_sync(0xffffffffu, mbar_wait(q_bar(h), q_used & 1u, abort_flag));
+        ++q_used;
       }
-      if (ok && n > 0 && one) umma_commit(empty_bar(base % NS));
+      ok = ok && (n == 0 || wait_slot(base));
+      tc_fence_after();
+      if (ok && n > 0) scores(0);
       for (int it = 0; it < n && ok; ++it) {
         const int vi = base + 2 * it + 1;
-        if (it + 1 < n) ok = wait_slot(vi + 1);
-        ok = ok && wait_slot(vi);
+        ok = (it + 1 >= n || wait_slot(vi + 1)) && wait_slot(vi);
         if (!ok) break;
-        const int j0 = tiles.at(it) * kTile;
-        const uint32_t vb = ring + (vi % NS) * TB;
-        if (j0 + kTile > w.sq.lk) {
-          // rows behind the last key belong to someone else and may hold anything; P is zero there, V has to be finite
-          const int first = w.sq.lk - j0;
-          for (int i = lane; i < (kTile - first) * 8 * NB; i += 32) {
-            const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
-            asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + blk * (kTile * 128) + r * 128 + c * 16),
-                         "r"(0)
-                         : "memory");
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-        tc_fence_after();
-        const uint64_t vd = make_desc(vb, kTile * 128, 1024);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (!ok) break;
-          if (need[h].has(tiles.at(it))) {
-            // the first product of a tile overwrites O, which the tile before has to have been read out of
-            if (nth[h] == 0)
-              ok = __all_sync(0xffffffffu, mbar_wait(o_empty_bar(h), (q_used[h] & 1u), abort_flag));
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {                    // the two halves of P as they come
-              ok = ok && __all_sync(0xffffffffu, mbar_wait(p_bar(h) + 16u * c, done[h] & 1u, abort_flag));
-              if (!ok) break;
-              tc_fence_after();
-              if (one) {
-#pragma unroll
-                for (int k = 4 * c; k < 4 * c + 4; ++k)
-                  umma_bf16_ts(tmem + 2 * kTile + h * DP, tmem + h * kTile + k * 8, vd + k * (2048 >> 4), idesc_o,
-                               (nth[h] | k) != 0);
-                if (c == 0) umma_commit(v_bar(h));
-              }
+        if (need.has(tiles.at(it))) {
+          const int j0 = tiles.at(it) * kTile;
+          const uint32_t vb = ring + (vi % NS) * TB;
+          if (j0 + kTile > w.sq.lk) {
+            // rows behind the last key belong to someone else and may hold anything; P is zero there, V has to be finite
+            // (both halves' warps clear them, with the same zeros)
+            const int first = w.sq.lk - j0;
+            for (int i = lane; i < (kTile - first) * 8 * NB; i += 32) {
+              const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
+              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + blk * (kTile * 128) + r * 128 + c * 16),
+                           "r"(0)
+                           : "memory");
             }
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          // the first product of a tile overwrites O, which the tile before has to have been read out of
+          if (nth == 0) ok = __all_sync(0xffffffffu, mbar_wait(o_empty_bar(h), q_used & 1u, abort_flag));
+          const uint64_t vd = make_desc(vb, kTile * 128, 1024);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {                      // the two halves of P as they come
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(p_bar(h) + 16u * c, done & 1u, abort_flag));
             if (!ok) break;
-            ++done[h];
-            if (++nth[h] == need[h].count() && one) umma_commit(o_bar(h));
+            if (c == 0 && other.has(tiles.at(it))) take_turn(nth == 0);
+            tc_fence_after();
+            if (one) {
+#pragma unroll
+              for (int k = 4 * c; k < 4 * c + 4; ++k)
+                umma_bf16_ts(t_o, t_s + k * 8, vd + k * (2048 >> 4), idesc_o, (nth | k) != 0);
+              if (c == 0) umma_commit(v_bar(h));
+            }
           }
-          if (one && h == 1) umma_commit(empty_bar(vi % NS));
-          if (it + 1 < n) {
-            if (need[h].has(tiles.at(it + 1))) issue_s(h, it + 1);
-            if (one && h == 1) umma_commit(empty_bar((vi + 1) % NS));
-          }
+          if (!ok) break;
+          ++done;
+          if (++nth == total && one) umma_commit(o_bar(h));
+        }
+        if (one) umma_commit(empty_bar(vi % NS));
+        tc_fence_after();
+        if (it + 1 < n) scores(it + 1);
+        if (need.has(tiles.at(it)) && other.has(tiles.at(it))) {
+          ++both;
+          if (one) turns[h] = both;
         }
       }
       base += 2 * n;
@@ -260,8 +263,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     while (ok && w.next()) {
       const KeyTiles<kTile> tiles = tiles_of(), need = half_tiles(h);
       const int n = tiles.count(), total = need.count(), rows = rows_of();
-      const int half_rows = clamp_int(rows - h * kTile, 0, kTile);
-      const int p0 = w.sq.shift + w.row0 + h * kTile, p1 = p0 + half_rows - 1;
       const int pos = w.sq.shift + w.row0 + row;
       const RowKeys keys = row_keys(w.sq, a.causal, a.window, pos);
       const float slope2 = BIAS ? a.slopes[w.head] * kLog2e : 0.f;
@@ -271,7 +272,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       for (int it = 0; it < n && ok; ++it) {
         const int t = tiles.at(it);
         if (!need.has(t)) continue;
-        const bool whole = all_seen(w.sq, a.causal, a.window, p0, p1, t * kTile, t * kTile + kTile);
         ok = __all_sync(0xffffffffu, mbar_wait(s_bar(h), cnt & 1u, abort_flag));
         if (!ok) break;
         tc_fence_after();
@@ -286,6 +286,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
 #pragma unroll 1
         for (int c = 0; c < 2 && ok; ++c) {
           const int j0 = t * kTile + c * 64;
+          // what the warp's rows see of these keys: all, some (then hidden scores become -inf), or nothing
+          const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
+          const bool whole = __all_sync(0xffffffffu, (lo <= 0 && hi >= 64) || pre >= 64);
+          if (__all_sync(0xffffffffu, min(hi, 64) <= max(lo, 0) && pre <= 0)) {
+            uint32_t zero[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) zero[i] = 0;
+            tmem_st32(s_addr + c * 32, zero);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_bar(h) + 16u * c);
+            continue;
+          }
           float x[64];
           tmem_ld32(s_addr + c * 64, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
           tmem_ld32(s_addr + c * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
@@ -301,7 +315,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             for (int j = 0; j < 64; ++j) x[j] = fmaf(-slope2, fabsf(d - (float)j), CAP ? x[j] : x[j] * mul);
           }
           if (!whole) {
-            const int lo = keys.lo - j0, hi = keys.hi - j0, pre = keys.prefix - j0;
 #pragma unroll
             for (int j = 0; j < 64; ++j)
               if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
@@ -330,25 +343,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             const float shift = m == -INFINITY ? 0.f : -m;
             const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
             uint64_t acc[2] = {0ull, 0ull};
-            auto exponentials = [&](auto polys) {              // the last `polys` of 8 pairs on the fp32 pipes
 #pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                uint64_t v = pair2(x[2 * i], x[2 * i + 1]);
-                v = kTransformed ? add2(v, shift_2) : fma2(v, mul_2, shift_2);
-                float e0, e1;
-                if ((i & 7) >= 8 - polys.value) {
-                  ex2_poly(v, e0, e1);
-                } else {
-                  unpair2(v, e0, e1);
-                  e0 = ex2(e0);
-                  e1 = ex2(e1);
-                }
-                acc[i & 1] = add2(acc[i & 1], pair2(e0, e1));
-                pk[i] = bf16x2(e0, e1);
-              }
-            };
-            if (whole) exponentials(Int<kPolys>());
-            else exponentials(Int<0>());
+            for (int i = 0; i < 32; ++i) {
+              uint64_t v = pair2(x[2 * i], x[2 * i + 1]);
+              v = kTransformed ? add2(v, shift_2) : fma2(v, mul_2, shift_2);
+              float e0, e1;
+              unpair2(v, e0, e1);
+              e0 = ex2(e0);
+              e1 = ex2(e1);
+              acc[i & 1] = add2(acc[i & 1], pair2(e0, e1));
+              pk[i] = bf16x2(e0, e1);
+            }
             float l0, l1;
             unpair2(add2(acc[0], acc[1]), l0, l1);
             sum = l0 + l1;
@@ -392,13 +397,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             if (mine && c * 32 + g * 8 < a.head_dim) {
-              uint4 v;
-              uint32_t* wp = reinterpret_cast<uint32_t*>(&v);
+              uint4 v = make_uint4(0, 0, 0, 0);
+              if (total > 0) {
+                uint32_t* vp = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float x = total > 0 ? __uint_as_float(o[g * 8 + 2 * i]) * inv : 0.f;
-                const float y = total > 0 ? __uint_as_float(o[g * 8 + 2 * i + 1]) * inv : 0.f;
-                wp[i] = bf16x2(x, y);
+                for (int i = 0; i < 4; ++i)
+                  vp[i] = bf16x2(__uint_as_float(o[g * 8 + 2 * i]) * inv, __uint_as_float(o[g * 8 + 2 * i + 1]) * inv);
               }
               *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = v;
             }
