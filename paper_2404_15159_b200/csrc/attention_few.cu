@@ -112,12 +112,12 @@ __device__ __forceinline__ float load_from(const float* mine, int rank) {
   return v;
 }
 
-// Joins the warps' states of a block in warp order, then the splits in index order: through the cluster's shared memory,
+// Joins the states of a block's warps in order, then the splits in index order: through the cluster's shared memory,
 // or through a partial in the workspace and a second launch.
-// `st_m`, `st_l` [kWarps][16], `st_o` [kWarps][16][DP] in shared memory; the block's own sums go over warp 0's.
+// `st_m`, `st_l` [states][16], `st_o` [states][16][DP] in shared memory; the block's own sums go over the first state's.
 template <typename T>
 __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w, float* st_m, float* st_l, float* st_o,
-                                             int dp) {
+                                             int dp, int states) {
   const AttnArgs& a = p.a;
   const int d = a.head_dim;
   const bool cluster = p.cluster;
@@ -125,8 +125,8 @@ __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w,
   float keep_m = -INFINITY, keep_l = 0.f;
   if (threadIdx.x < 16) {
     float m = -INFINITY, l = 0.f;
-    for (int x = 0; x < kWarps; ++x) m = fmaxf(m, st_m[x * 16 + threadIdx.x]);
-    for (int x = 0; x < kWarps; ++x) {
+    for (int x = 0; x < states; ++x) m = fmaxf(m, st_m[x * 16 + threadIdx.x]);
+    for (int x = 0; x < states; ++x) {
       const float mx = st_m[x * 16 + threadIdx.x], f = mx == -INFINITY ? 0.f : ex2(mx - m);
       l += f * st_l[x * 16 + threadIdx.x];
     }
@@ -136,8 +136,8 @@ __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w,
   for (int i = threadIdx.x; i < w.rows * d; i += kWarps * 32) {
     const int r = i / d, c = i - r * d;
     float m = -INFINITY, o = 0.f;
-    for (int x = 0; x < kWarps; ++x) m = fmaxf(m, st_m[x * 16 + r]);
-    for (int x = 0; x < kWarps; ++x) {
+    for (int x = 0; x < states; ++x) m = fmaxf(m, st_m[x * 16 + r]);
+    for (int x = 0; x < states; ++x) {
       const float f = st_m[x * 16 + r] == -INFINITY ? 0.f : ex2(st_m[x * 16 + r] - m);
       o += f * st_o[(x * 16 + r) * dp + c];
     }
@@ -340,29 +340,87 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
       *reinterpret_cast<float2*>(st_o + (warp * 16 + r) * DP + x * 8 + 2 * t) = make_float2(o[x][2 * hf], o[x][2 * hf + 1]);
   }
   __syncthreads();
-  finish_block<bf16>(p, w, st_m, st_l, st_o, DP);
+  finish_block<bf16>(p, w, st_m, st_l, st_o, DP, kWarps);
 }
 
-// fp32.  LPK lanes hold a key (4 values each); a warp takes 32 / LPK keys at a time, kKeys steps in flight.
+// Where a value of a batch ends up when the M partial sums of LPK lanes are added up: every step of the exchange halves the
+// values a lane keeps (the upper half in lanes with that bit set) until one is left, later steps only add.
+template <int LPK, int M>
+struct Spread {
+  static constexpr int kOwn = M > LPK ? M / LPK : 1;         // values of a lane in the end
+  // the lane (of LPK) that ends up with value `idx`, and which of its values it is
+  static __host__ __device__ constexpr int lane_of(int idx) {
+    int lane = 0, cur = M;
+    for (int off = LPK / 2; off >= 1; off >>= 1)
+      if (cur > 1) {
+        cur >>= 1;
+        if (idx & cur) lane |= off;
+      }
+    return lane;
+  }
+  static __device__ __forceinline__ int first_of(int lane) {
+    int idx = 0, cur = M;
+#pragma unroll
+    for (int off = LPK / 2; off >= 1; off >>= 1)
+      if (cur > 1) {
+        cur >>= 1;
+        if (lane & off) idx |= cur;
+      }
+    return idx;
+  }
+  static __device__ __forceinline__ void add_up(float (&v)[M], int lane) {
+    int cur = M;
+#pragma unroll
+    for (int off = LPK / 2; off >= 1; off >>= 1) {
+      if (cur > 1) {
+        cur >>= 1;
+        const bool up = lane & off;
+#pragma unroll
+        for (int k = 0; k < M / 2; ++k)
+          if (k < cur) {
+            const float send = up ? v[k] : v[k + cur], keep = up ? v[k + cur] : v[k];
+            v[k] = keep + __shfl_xor_sync(0xffffffffu, send, off);
+          }
+      } else {
+        v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+      }
+    }
+  }
+  // over the lanes that hold the four keys of a row (values 4 r .. 4 r + 3)
+  template <typename F>
+  static __device__ __forceinline__ float over_keys(float v, F f) {
+    int cur = M;
+#pragma unroll
+    for (int off = LPK / 2; off >= 1; off >>= 1)
+      if (cur > 1) {
+        cur >>= 1;
+        if (cur < 4) v = f(v, __shfl_xor_sync(0xffffffffu, v, off));
+      }
+    return v;
+  }
+};
+
+// fp32.  LPK lanes hold a key (4 values each), and four keys at a time; their ROWS x 4 scores are summed so that every
+// lane ends up with its own share of them, whose exponentials it takes once and hands back to the others.  The cap goes
+// through tanhf: this is the check mode.
 template <int LPK, int ROWS, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kWarps * 32) attn_few_f32_kernel(FewParams p) {
-  constexpr int SUB = 32 / LPK, kKeys = kStep / SUB, DP = LPK * 4;
-  constexpr int kBatch = kKeys < 4 ? kKeys : 4;
+  constexpr int SUB = 32 / LPK, DP = LPK * 4, M = 4 * ROWS;
+  using S = Spread<LPK, M>;
+  constexpr int OWN = S::kOwn;
   extern __shared__ __align__(128) uint8_t smem[];
   const AttnArgs& a = p.a;
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int sub = lane / LPK, c = (lane % LPK) * 4;
+  const int sub = lane / LPK, sl = lane % LPK, c = sl * 4;
   const Share w = block_share(p);
   const int d = a.head_dim;
   const bool on_c = c < d;
   const float* kp = reinterpret_cast<const float*>(a.k) + (size_t)w.kvh * d + (on_c ? c : 0);
   const float* vp = reinterpret_cast<const float*>(a.v) + (size_t)w.kvh * d + (on_c ? c : 0);
-  const ScoreMap<CAP, BIAS> score(a);
   const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
 
   float4 q[ROWS], o[ROWS];
-  float m[ROWS], l[ROWS], slope2[ROWS];
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     const int qi = (w.row0 + r) / a.group, hd = w.kvh * a.group + (w.row0 + r - qi * a.group);
@@ -370,82 +428,91 @@ __global__ void __launch_bounds__(kWarps * 32) attn_few_f32_kernel(FewParams p) 
     q[r] = on && on_c ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.q) +
                                                           (size_t)(w.sq.q0 + qi) * a.q_stride + (size_t)hd * d + c)
                       : zero;
-    slope2[r] = BIAS && on ? a.slopes[hd] * kLog2e : 0.f;
     o[r] = zero;
-    m[r] = -INFINITY;
-    l[r] = 0.f;
   }
+  // this lane's row, the first of its keys, and the row's running maximum and part of the sum
+  const int own = S::first_of(sl), own_r = own >> 2, own_x = own & 3;
+  const int qi = (w.row0 + own_r) / a.group, hd = w.kvh * a.group + (w.row0 + own_r - qi * a.group);
+  const bool live = own_r < w.rows && qi < w.lq;
+  const int pos = w.sq.shift + qi;
+  const RowKeys keys = live ? row_keys(w.sq, a.causal, a.window, pos) : RowKeys{0, 0, 0};
+  const float slope2 = BIAS && live ? a.slopes[hd] * kLog2e : 0.f;
+  float m = -INFINITY, l = 0.f;
+  auto larger = [](float x, float y) { return fmaxf(x, y); };
+  auto sum = [](float x, float y) { return x + y; };
+
   for (int tt = w.t0 + warp; tt < w.t1; tt += kWarps) {
     const int j0 = w.tiles.at(tt) * kStep;
 #pragma unroll
-    for (int b = 0; b < kKeys; b += kBatch) {
-      float4 k[kBatch], v[kBatch];
+    for (int b = 0; b < kStep / (4 * SUB); ++b) {
+      const int jb = j0 + (b * SUB + sub) * 4;   // this group of lanes' four keys
+      float4 k[4], v[4];
 #pragma unroll
-      for (int x = 0; x < kBatch; ++x) {
-        const int j = j0 + (b + x) * SUB + sub;
-        const bool on = on_c && j < w.sq.lk;
-        const size_t row = (size_t)(w.sq.k0 + (on ? j : 0));
+      for (int x = 0; x < 4; ++x) {
+        const bool on = on_c && jb + x < w.sq.lk;
+        const size_t row = (size_t)(w.sq.k0 + (on ? jb + x : 0));
         k[x] = on ? *reinterpret_cast<const float4*>(kp + row * a.k_stride) : zero;
         v[x] = on ? *reinterpret_cast<const float4*>(vp + row * a.v_stride) : zero;
       }
+      float s[M];
 #pragma unroll
-      for (int r = 0; r < ROWS; ++r) {
-        const int qi = (w.row0 + r) / a.group;
-        const bool live = r < w.rows && qi < w.lq;
-        const int pos = w.sq.shift + qi;
-        const RowKeys keys = row_keys(w.sq, a.causal, a.window, pos);
-        float s[kBatch], mt = -INFINITY;
+      for (int r = 0; r < ROWS; ++r)
 #pragma unroll
-        for (int x = 0; x < kBatch; ++x)
-          s[x] = q[r].x * k[x].x + q[r].y * k[x].y + q[r].z * k[x].z + q[r].w * k[x].w;
+        for (int x = 0; x < 4; ++x)
+          s[4 * r + x] = fmaf(q[r].w, k[x].w, fmaf(q[r].z, k[x].z, fmaf(q[r].y, k[x].y, q[r].x * k[x].x)));
+      S::add_up(s, sl);
+      float mt = -INFINITY;
 #pragma unroll
-        for (int f = LPK / 2; f >= 1; f >>= 1)
+      for (int i = 0; i < OWN; ++i) {
+        const int j = jb + own_x + i;
+        float y = s[i] * a.scale;
+        if (CAP) y = a.softcap * tanhf(y / a.softcap);
+        y *= kLog2e;
+        if (BIAS) y -= slope2 * fabsf((float)(pos - j));
+        s[i] = keys.sees(j) ? y : -INFINITY;
+        mt = fmaxf(mt, s[i]);
+      }
+      mt = S::over_keys(mt, larger);
+      const bool grown = mt > m + 8.f || (mt > m && m == -INFINITY);
+      if (__any_sync(0xffffffffu, grown)) {
+        const float m_new = grown ? mt : m, f = m == -INFINITY ? 0.f : exp2f(m - m_new);
+        m = m_new;
+        l *= f;
 #pragma unroll
-          for (int x = 0; x < kBatch; ++x) s[x] += __shfl_xor_sync(0xffffffffu, s[x], f);
-#pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-          const int j = j0 + (b + x) * SUB + sub;
-          s[x] = live && keys.sees(j) ? score(s[x], slope2[r], pos - j) : -INFINITY;
-          mt = fmaxf(mt, s[x]);
-        }
-        if (mt > m[r]) {                         // the lanes of a key agree
-          const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mt);
-          m[r] = mt;
-          l[r] *= f;
-          o[r].x *= f; o[r].y *= f; o[r].z *= f; o[r].w *= f;
-        }
-        const float base = m[r] == -INFINITY ? 0.f : m[r];
-#pragma unroll
-        for (int x = 0; x < kBatch; ++x) {
-          const float e = exp2f(s[x] - base);
-          l[r] += e;
-          o[r].x += e * v[x].x; o[r].y += e * v[x].y; o[r].z += e * v[x].z; o[r].w += e * v[x].w;
+        for (int r = 0; r < ROWS; ++r) {
+          const float fr = __shfl_sync(0xffffffffu, f, sub * LPK + S::lane_of(4 * r));
+          o[r].x *= fr; o[r].y *= fr; o[r].z *= fr; o[r].w *= fr;
         }
       }
-    }
-  }
-  float* st_m = reinterpret_cast<float*>(smem);
-  float* st_l = st_m + kWarps * 16;
-  float* st_o = st_l + kWarps * 16;
+      const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    if (SUB == 2) {                              // the warp's two key streams
-      const float mo = __shfl_xor_sync(0xffffffffu, m[r], 16), mn = fmaxf(m[r], mo);
-      const float f = m[r] == -INFINITY ? 0.f : exp2f(m[r] - mn);
-      l[r] *= f;
-      o[r].x *= f; o[r].y *= f; o[r].z *= f; o[r].w *= f;
-      m[r] = mn;
-      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 16);
-      o[r].x += __shfl_xor_sync(0xffffffffu, o[r].x, 16);
-      o[r].y += __shfl_xor_sync(0xffffffffu, o[r].y, 16);
-      o[r].z += __shfl_xor_sync(0xffffffffu, o[r].z, 16);
-      o[r].w += __shfl_xor_sync(0xffffffffu, o[r].w, 16);
+      for (int i = 0; i < OWN; ++i) {
+        s[i] = exp2f(s[i] - base);
+        l += s[i];
+      }
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float e = __shfl_sync(0xffffffffu, s[(4 * r + x) % OWN], sub * LPK + S::lane_of(4 * r + x));
+          o[r].x = fmaf(e, v[x].x, o[r].x);
+          o[r].y = fmaf(e, v[x].y, o[r].y);
+          o[r].z = fmaf(e, v[x].z, o[r].z);
+          o[r].w = fmaf(e, v[x].w, o[r].w);
+        }
     }
-    if (lane == 0) { st_m[warp * 16 + r] = m[r]; st_l[warp * 16 + r] = l[r]; }
-    if (sub == 0) *reinterpret_cast<float4*>(st_o + (warp * 16 + r) * DP + c) = o[r];
   }
+  constexpr int kStates = kWarps * SUB;
+  float* st_m = reinterpret_cast<float*>(smem);
+  float* st_l = st_m + kStates * 16;
+  float* st_o = st_l + kStates * 16;
+  const int state = warp * SUB + sub;
+  l = S::over_keys(l, sum);
+  if (own_x == 0) { st_m[state * 16 + own_r] = m; st_l[state * 16 + own_r] = l; }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) *reinterpret_cast<float4*>(st_o + (state * 16 + r) * DP + c) = o[r];
   __syncthreads();
-  finish_block<float>(p, w, st_m, st_l, st_o, DP);
+  finish_block<float>(p, w, st_m, st_l, st_o, DP, kStates);
 }
 
 // Joins the splits of a row in index order; one warp per (sequence, query, head).
@@ -486,7 +553,7 @@ __global__ void __launch_bounds__(128) attn_few_join_kernel(FewParams p) {
   if (lane == 0 && a.lse) a.lse[(size_t)head * a.q_rows + q0 + qi] = (m + log2f(l)) * kLn2;
 }
 
-constexpr size_t exchange_bytes(int dp) { return (size_t)kWarps * 16 * (dp + 2) * 4; }
+constexpr size_t exchange_bytes(int dp, int states) { return (size_t)states * 16 * (dp + 2) * 4; }
 
 template <typename K>
 cudaError_t launch_blocks(K kernel, const FewParams& p, unsigned grid, size_t smem, cudaStream_t st) {
@@ -507,7 +574,7 @@ cudaError_t launch_blocks(K kernel, const FewParams& p, unsigned grid, size_t sm
 template <int DP, bool CAP, bool BIAS>
 cudaError_t launch_bf16(const FewParams& p, unsigned grid, cudaStream_t st) {
   constexpr size_t ring = (size_t)kWarps * kStages * 2 * kStep * DP * 2;
-  constexpr size_t smem = ring > exchange_bytes(DP) ? ring : exchange_bytes(DP);
+  constexpr size_t smem = ring > exchange_bytes(DP, kWarps) ? ring : exchange_bytes(DP, kWarps);
   static bool done[64];
   cudaError_t e = allow_smem(attn_few_bf16_kernel<DP, CAP, BIAS>, (int)smem, done);
   if (e != cudaSuccess) return e;
@@ -515,7 +582,7 @@ cudaError_t launch_bf16(const FewParams& p, unsigned grid, cudaStream_t st) {
 }
 template <int LPK, int ROWS, bool CAP, bool BIAS>
 cudaError_t launch_f32(const FewParams& p, unsigned grid, cudaStream_t st) {
-  return launch_blocks(attn_few_f32_kernel<LPK, ROWS, CAP, BIAS>, p, grid, exchange_bytes(LPK * 4), st);
+  return launch_blocks(attn_few_f32_kernel<LPK, ROWS, CAP, BIAS>, p, grid, exchange_bytes(LPK * 4, kWarps * (32 / LPK)), st);
 }
 template <bool CAP, bool BIAS>
 cudaError_t launch_mode(const FewParams& p, bool bf16_mode, unsigned grid, cudaStream_t st) {
