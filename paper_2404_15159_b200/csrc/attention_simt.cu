@@ -20,6 +20,27 @@ __device__ __forceinline__ void load_rows(float* dst, const float* src, long lon
     *reinterpret_cast<float4*>(dst + r * kPitch<DP> + c) = v;
   }
 }
+// The same in two steps, so that a tile's loads travel while the one before is worked on.
+template <int DP>
+struct RowsAhead {
+  static constexpr int kPer = kT * (DP / 4) / kThreads;
+  float4 v[kPer];
+  __device__ __forceinline__ void fetch(const float* src, long long stride, int valid, int head_dim) {
+#pragma unroll
+    for (int n = 0; n < kPer; ++n) {
+      const int i = n * kThreads + threadIdx.x, r = i / (DP / 4), c = (i % (DP / 4)) * 4;
+      v[n] = r < valid && c < head_dim ? *reinterpret_cast<const float4*>(src + (size_t)r * stride + c)
+                                       : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  __device__ __forceinline__ void put(float* dst) const {
+#pragma unroll
+    for (int n = 0; n < kPer; ++n) {
+      const int i = n * kThreads + threadIdx.x, r = i / (DP / 4), c = (i % (DP / 4)) * 4;
+      *reinterpret_cast<float4*>(dst + r * kPitch<DP> + c) = v[n];
+    }
+  }
+};
 // acc[i][c] = A[4 ty + i] . B[tx + 16 c]
 template <int DP>
 __device__ __forceinline__ void dot_tile(const float* A, const float* B, int ty, int tx, float (&acc)[4][4]) {
@@ -196,6 +217,14 @@ template <int DP>
 __device__ __forceinline__ void grad_tile(const AttnArgs& a, const AttnSeq& sq, int head, float slope2, int i0, int j0,
                                           const float* qs, const float* dos, const float* ks, const float* vs, float* ps,
                                           float* dss, int ty, int tx) {
+  float row_lse[4], row_delta[4];                // on their way during the products
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i0 + 4 * ty + i;
+    const size_t at = (size_t)head * a.q_rows + sq.q0 + (r < sq.lq ? r : 0);
+    row_lse[i] = r < sq.lq ? a.lse2[at] : INFINITY;
+    row_delta[i] = r < sq.lq ? a.delta[at] : 0.f;
+  }
   float s[4][4], dp[4][4];
   dot_tile<DP>(qs, ks, ty, tx, s);
   dot_tile<DP>(dos, vs, ty, tx, dp);
@@ -204,8 +233,7 @@ __device__ __forceinline__ void grad_tile(const AttnArgs& a, const AttnSeq& sq, 
     const int r = i0 + 4 * ty + i, pos = sq.shift + r;
     const bool on = r < sq.lq;
     const RowKeys keys = row_keys(sq, a.causal, a.window, pos);
-    const size_t at = (size_t)head * a.q_rows + sq.q0 + (on ? r : 0);
-    const float lse2 = on ? a.lse2[at] : INFINITY, delta = on ? a.delta[at] : 0.f;
+    const float lse2 = row_lse[i], delta = row_delta[i];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const int j = j0 + tx + 16 * c;
@@ -221,8 +249,7 @@ __device__ __forceinline__ void grad_tile(const AttnArgs& a, const AttnSeq& sq, 
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_simt_kernel(AttnArgs a) {
-  extern __shared__ __align__(16) float smem_f[];
+__device__ __forceinline__ void bwd_kv_block(const AttnArgs& a, int block, float* smem_f) {
   float* ks = smem_f;
   float* vs = ks + kT * kPitch<DP>;
   float* qs = vs + kT * kPitch<DP>;
@@ -230,9 +257,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_simt_kernel(AttnArgs 
   float* ps = dos + kT * kPitch<DP>;
   float* dss = ps + kT * kPitchP;
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  const int kvh = blockIdx.x % a.kv_heads, d = a.head_dim;
+  const int kvh = block % a.kv_heads, d = a.head_dim;
   int seq, index;
-  if (!block_tile(a.k_off, a.n_seqs, a.k_rows, blockIdx.x / a.kv_heads, &seq, &index)) return;
+  if (!block_tile(a.k_off, a.n_seqs, a.k_rows, block / a.kv_heads, &seq, &index)) return;
   const AttnSeq sq = load_seq(a, seq);
   const int j0 = index * kT, keys = min(kT, sq.lk - j0);
   if (keys <= 0) return;                         // behind the used part of a slot
@@ -246,20 +273,26 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_simt_kernel(AttnArgs 
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) dk[i][c] = dv[i][c] = 0.f;
-  for (int g = 0; g < a.group; ++g) {
-    const int head = kvh * a.group + g;
-    const float slope2 = a.slopes ? a.slopes[head] * kLog2e : 0.f;
-    for (int i0 = lo / kT * kT; i0 < hi; i0 += kT) {
-      const size_t row = (size_t)(sq.q0 + i0);
-      load_rows<DP>(qs, reinterpret_cast<const float*>(a.q) + row * a.q_stride + (size_t)head * d, a.q_stride, sq.lq - i0, d);
-      load_rows<DP>(dos, reinterpret_cast<const float*>(a.d_o) + row * a.o_stride + (size_t)head * d, a.o_stride, sq.lq - i0, d);
-      __syncthreads();
-      grad_tile<DP>(a, sq, head, slope2, i0, j0, qs, dos, ks, vs, ps, dss, ty, tx);
-      __syncthreads();
-      sum_tile<DP, false>(ps, dos, ty, tx, dv);
-      sum_tile<DP, false>(dss, qs, ty, tx, dk);
-      __syncthreads();
-    }
+  const int first = lo / kT * kT, per_head = hi > first ? (hi - first + kT - 1) / kT : 0, n = per_head * a.group;
+  RowsAhead<DP> nq, ndo;
+  auto fetch = [&](int i) {
+    const int head = kvh * a.group + i / per_head, i0 = first + (i % per_head) * kT;
+    const size_t row = (size_t)(sq.q0 + i0);
+    nq.fetch(reinterpret_cast<const float*>(a.q) + row * a.q_stride + (size_t)head * d, a.q_stride, sq.lq - i0, d);
+    ndo.fetch(reinterpret_cast<const float*>(a.d_o) + row * a.o_stride + (size_t)head * d, a.o_stride, sq.lq - i0, d);
+  };
+  if (n > 0) fetch(0);
+  for (int i = 0; i < n; ++i) {
+    const int head = kvh * a.group + i / per_head, i0 = first + (i % per_head) * kT;
+    nq.put(qs);
+    ndo.put(dos);
+    __syncthreads();
+    if (i + 1 < n) fetch(i + 1);
+    grad_tile<DP>(a, sq, head, a.slopes ? a.slopes[head] * kLog2e : 0.f, i0, j0, qs, dos, ks, vs, ps, dss, ty, tx);
+    __syncthreads();
+    sum_tile<DP, false>(ps, dos, ty, tx, dv);
+    sum_tile<DP, false>(dss, qs, ty, tx, dk);
+    __syncthreads();
   }
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, mul[4] = {a.scale, a.scale, a.scale, a.scale};
   store_rows<DP>(reinterpret_cast<float*>(a.dv) + krow * a.v_stride + (size_t)kvh * d, a.v_stride, keys, d, ty, tx, dv, one);
@@ -267,17 +300,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_simt_kernel(AttnArgs 
 }
 
 template <int DP>
-__global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_simt_kernel(AttnArgs a) {
-  extern __shared__ __align__(16) float smem_f[];
+__device__ __forceinline__ void bwd_q_block(const AttnArgs& a, int block, float* smem_f) {
   float* qs = smem_f;
   float* dos = qs + kT * kPitch<DP>;
   float* ks = dos + kT * kPitch<DP>;
   float* vs = ks + kT * kPitch<DP>;
   float* dss = vs + kT * kPitch<DP>;
   const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
-  const int head = blockIdx.x % a.q_heads, kvh = head / a.group, d = a.head_dim;
+  const int head = block % a.q_heads, kvh = head / a.group, d = a.head_dim;
   int seq, index;
-  if (!block_tile(a.q_off, a.n_seqs, a.q_rows, blockIdx.x / a.q_heads, &seq, &index)) return;
+  if (!block_tile(a.q_off, a.n_seqs, a.q_rows, block / a.q_heads, &seq, &index)) return;
   const AttnSeq sq = load_seq(a, seq);
   const int i0 = index * kT, rows = min(kT, sq.lq - i0), p0 = sq.shift + i0;
   const KeyTiles<kT> tiles = key_tiles<kT>(sq, a.causal, a.window, p0, p0 + rows - 1);
@@ -290,13 +322,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_simt_kernel(AttnArgs a
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) dq[i][c] = 0.f;
-  for (int it = 0; it < tiles.count(); ++it) {
+  const int n = tiles.count();
+  RowsAhead<DP> nk, nv;
+  auto fetch = [&](int it) {
     const int j0 = tiles.at(it) * kT, valid = min(kT, sq.lk - j0);
     const size_t krow = (size_t)(sq.k0 + j0);
-    load_rows<DP>(ks, reinterpret_cast<const float*>(a.k) + krow * a.k_stride + (size_t)kvh * d, a.k_stride, valid, d);
-    load_rows<DP>(vs, reinterpret_cast<const float*>(a.v) + krow * a.v_stride + (size_t)kvh * d, a.v_stride, valid, d);
+    nk.fetch(reinterpret_cast<const float*>(a.k) + krow * a.k_stride + (size_t)kvh * d, a.k_stride, valid, d);
+    nv.fetch(reinterpret_cast<const float*>(a.v) + krow * a.v_stride + (size_t)kvh * d, a.v_stride, valid, d);
+  };
+  if (n > 0) fetch(0);
+  for (int it = 0; it < n; ++it) {
+    nk.put(ks);
+    nv.put(vs);
     __syncthreads();
-    grad_tile<DP>(a, sq, head, slope2, i0, j0, qs, dos, ks, vs, nullptr, dss, ty, tx);
+    if (it + 1 < n) fetch(it + 1);
+    grad_tile<DP>(a, sq, head, slope2, i0, tiles.at(it) * kT, qs, dos, ks, vs, nullptr, dss, ty, tx);
     __syncthreads();
     sum_tile<DP, true>(dss, ks, ty, tx, dq);
     __syncthreads();
@@ -305,15 +345,30 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_simt_kernel(AttnArgs a
   store_rows<DP>(reinterpret_cast<float*>(a.dq) + row * a.q_stride + (size_t)head * d, a.q_stride, rows, d, ty, tx, dq, mul);
 }
 
+// dk, dv and dq in one launch: the key blocks, which are fewer and longer, start first.
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1) attn_bwd_simt_kernel(AttnArgs a, int key_blocks) {
+  extern __shared__ __align__(16) float smem_f[];
+  if ((int)blockIdx.x < key_blocks) bwd_kv_block<DP>(a, blockIdx.x, smem_f);
+  else bwd_q_block<DP>(a, blockIdx.x - key_blocks, smem_f);
+}
+
 template <int DP> constexpr int bytes(int rows, int tiles) { return 4 * (rows * kT * kPitch<DP> + tiles * kT * kPitchP); }
 
-template <typename K>
-cudaError_t run(K kernel, long long grid, int smem, const AttnArgs& a, cudaStream_t st) {
-  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
-  if (grid == 0) return cudaSuccess;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  kernel<<<(unsigned)grid, kThreads, smem, st>>>(a);
+template <int DP>
+cudaError_t forward(const AttnArgs& a, long long grid, cudaStream_t st) {
+  static bool done[64];
+  cudaError_t e = allow_smem(attn_fwd_simt_kernel<DP>, bytes<DP>(2, 1), done);
+  if (e != cudaSuccess || grid == 0) return e;
+  attn_fwd_simt_kernel<DP><<<(unsigned)grid, kThreads, bytes<DP>(2, 1), st>>>(a);
+  return cudaGetLastError();
+}
+template <int DP>
+cudaError_t backward(const AttnArgs& a, long long key_blocks, long long row_blocks, cudaStream_t st) {
+  static bool done[64];
+  cudaError_t e = allow_smem(attn_bwd_simt_kernel<DP>, bytes<DP>(4, 2), done);
+  if (e != cudaSuccess || key_blocks + row_blocks == 0) return e;
+  attn_bwd_simt_kernel<DP><<<(unsigned)(key_blocks + row_blocks), kThreads, bytes<DP>(4, 2), st>>>(a, (int)key_blocks);
   return cudaGetLastError();
 }
 long long tiles_of(int rows, int n_seqs, int heads) {
@@ -324,18 +379,14 @@ long long tiles_of(int rows, int n_seqs, int heads) {
 
 cudaError_t launch_attn_forward_simt(const AttnArgs& a, cudaStream_t st) {
   const long long grid = tiles_of(a.q_rows, a.n_seqs, a.q_heads);
-  return a.head_dim <= 64 ? run(attn_fwd_simt_kernel<64>, grid, bytes<64>(2, 1), a, st)
-                          : run(attn_fwd_simt_kernel<128>, grid, bytes<128>(2, 1), a, st);
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return a.head_dim <= 64 ? forward<64>(a, grid, st) : forward<128>(a, grid, st);
 }
 
 cudaError_t launch_attn_backward_simt(const AttnArgs& a, cudaStream_t st) {
   const long long gk = tiles_of(a.k_rows, a.n_seqs, a.kv_heads), gq = tiles_of(a.q_rows, a.n_seqs, a.q_heads);
-  const bool narrow = a.head_dim <= 64;
-  cudaError_t e = narrow ? run(attn_bwd_kv_simt_kernel<64>, gk, bytes<64>(4, 2), a, st)
-                         : run(attn_bwd_kv_simt_kernel<128>, gk, bytes<128>(4, 2), a, st);
-  if (e != cudaSuccess) return e;
-  return narrow ? run(attn_bwd_q_simt_kernel<64>, gq, bytes<64>(4, 1), a, st)
-                : run(attn_bwd_q_simt_kernel<128>, gq, bytes<128>(4, 1), a, st);
+  if (gk + gq > 0x7fffffffLL) return cudaErrorInvalidValue;
+  return a.head_dim <= 64 ? backward<64>(a, gk, gq, st) : backward<128>(a, gk, gq, st);
 }
 
 }  // namespace mixlora
