@@ -322,7 +322,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
           uint32_t pk[32];
           float sum;
           bool reset = m == -INFINITY;                         // nothing seen yet; below: p near the end of its range
-          while (true) {
+#pragma unroll 1
+          for (int attempt = 0; attempt < 2; ++attempt) {      // over their own maximum p are at most about 1
             if (__any_sync(0xffffffffu, reset)) {
               float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll

@@ -308,3 +308,92 @@ def test_two_streams_with_a_workspace_each():
             B.mixlora_attention_forward(shape, mask, t["q"], t["k"], t["v"], o, None, ws, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o, _ in work)
+
+
+@TYPES
+def test_many_short_sequences(bf16):
+    # more sequences than the planning block has threads, empty ones among them
+    lens = [(i * 7) % 4 for i in range(2600)]
+    c = Case(lens, hq=2, hk=1, dim=16, seed=41, bf16=bf16, tail=1)
+    c.check(c.run())
+
+
+def test_decoding_step_in_a_captured_graph():
+    import torch
+    from paper_2404_15159_b200 import binding as B
+    for slots, slot in ((1, 2000), (40, 700)):        # joined inside a cluster; through partials and a second launch
+        c = Case([1] * slots, k_lens=[slot] * slots, k_len=[slot - 3 * (i % 50) for i in range(slots)], hq=32, hk=8, dim=128,
+                 seed=50 + slots)
+        t = c.to_gpu()
+        shape = c.shape(B, t, max_q_len=1, max_k_len=slot)
+        mask = B.make_attention_mask(t["q_off"], t["k_off"], t["k_len"])
+        ws, o, lse = B.alloc_attention_workspace(shape, False), torch.empty_like(t["q"]), torch.empty(32, c.rows, device="cuda")
+        step = lambda: B.mixlora_attention_forward(shape, mask, t["q"], t["k"], t["v"], o, lse, ws)  # noqa: E731
+        step()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                step()
+        torch.cuda.synchronize()
+        # the next step: every sequence one key shorter, another query
+        t["k_len"] -= 1
+        t["q"].copy_(t["q"].flip(1))
+        c.k_len = [n - 1 for n in c.k_len]
+        c.q = c.q[:, ::-1]
+        o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(dict(o=o.double().cpu().numpy(), lse=lse.double().cpu().numpy()), backward=False)
+
+
+@pytest.mark.parametrize("few", [True, False])
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "fp32"])
+def test_offsets_beyond_32_bits(few, bf16):
+    # the one sequence lies behind 2^31 elements of a cache (and, in bf16, behind 2^32 bytes of it)
+    import torch
+    from paper_2404_15159_b200 import binding as B
+    hk, dim, lk, lq = 8, 128, 300, (2 if few else 70)
+    far = 2 ** 31 // (hk * dim) + 5
+    act = torch.bfloat16 if bf16 else torch.float32
+    c = Case([lq], k_lens=[lk], hq=8, hk=hk, dim=dim, seed=61, bf16=bf16)
+    t = c.to_gpu()
+    big = [torch.empty(far + lk, hk, dim, dtype=act, device="cuda") for _ in range(2)]
+    for x, n in zip(big, "kv"):
+        x[far:] = t[n]
+    off = torch.tensor([far, far + lk], dtype=torch.int32, device="cuda")
+    shape = B.make_attention_shape(1, lq, far + lk, 8, hk, dim, B.MIXLORA_DTYPE_BF16 if bf16 else B.MIXLORA_DTYPE_FP32,
+                                   max_q_len=lq if few else 0, max_k_len=lk)
+    ws = B.alloc_attention_workspace(shape, not few)
+    mask = B.make_attention_mask(t["q_off"], off)
+    o, lse = torch.empty_like(t["q"]), torch.empty(8, lq, device="cuda")
+    B.mixlora_attention_forward(shape, mask, t["q"], big[0], big[1], o, lse, ws)
+    got = dict(o=o, lse=lse)
+    if not few:
+        grads = [torch.empty_like(t["q"]), torch.empty_like(big[0]), torch.empty_like(big[1])]
+        B.mixlora_attention_backward(shape, mask, t["q"], big[0], big[1], o, lse, t["d_o"], ws, *grads)
+        got.update(d_q=grads[0], d_k=grads[1][far:], d_v=grads[2][far:])
+    torch.cuda.synchronize()
+    c.check({n: x.double().cpu().numpy() for n, x in got.items()}, backward=not few)
+
+
+@pytest.mark.parametrize("size", [1e3, 1e6, 1e15])
+def test_scores_of_any_size_end(size):
+    # up to scores whose neighbours in fp32 lie further apart than its exponents reach: the call still ends
+    import torch
+    from paper_2404_15159_b200 import binding as B
+    n = 200
+    x = torch.zeros(n, 1, 64, dtype=torch.bfloat16, device="cuda")
+    x[:, 0, 0] = size
+    v = torch.ones_like(x)
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    shape = B.make_attention_shape(1, n, n, 1, 1, 64)
+    ws = B.alloc_attention_workspace(shape, True)
+    o, lse = torch.empty_like(x), torch.empty(1, n, device="cuda")
+    mask = B.make_attention_mask(off, off)
+    B.mixlora_attention_forward(shape, mask, x, x, v, o, lse, ws)
+    B.mixlora_attention_backward(shape, mask, x, x, v, o, lse, v, ws, *(torch.empty_like(x) for _ in range(3)))
+    assert B.mixlora_device_status(ws) == 0
+    if size <= 1e3:                                   # equal scores: every row is the mean of ones
+        assert (o == 1).all()
