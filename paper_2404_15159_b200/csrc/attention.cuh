@@ -148,6 +148,9 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The two values of a bf16 pair
+__device__ __forceinline__ float bf16_lo(uint32_t p) { return __uint_as_float(p << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
 // Two fp32 values to an instruction
 __device__ __forceinline__ uint64_t pair2(float lo, float hi) {
   uint64_t r;

@@ -101,7 +101,7 @@ AttnLayout attention_layout(const mixlora_attention_shape_t& s, bool backward) {
   const int rows = few_rows(s);
   const FewSplits sp = rows ? splits_of(s) : FewSplits{1, false};
   const size_t chunks = (size_t)(rows + kFewRows - 1) / kFewRows;
-  L.part = take(sp.count > 1 && !sp.cluster ? (size_t)s.n_seqs * s.kv_heads * chunks * sp.count * kFewRows * (s.head_dim + 2) * 4 : 0);
+  L.part = take(sp.count > 1 && !sp.cluster ? (size_t)s.n_seqs * s.kv_heads * chunks * sp.count * kFewRows * (s.head_dim + 3) * 4 : 0);
   const size_t per_row = backward ? (size_t)s.q_heads * s.q_rows * 4 : 0;
   L.lse2 = take(per_row);
   L.delta = take(per_row);

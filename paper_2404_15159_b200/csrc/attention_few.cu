@@ -17,7 +17,7 @@ constexpr int kClusterMax = 8;                   // a cluster's blocks, in every
 
 struct FewParams {
   AttnArgs a;
-  float* part;                                   // [seq, key head, chunk, split, 16 rows, head_dim + 2]: sum p v, m (base 2), l
+  float* part;                                   // [seq, key head, chunk, split, 16 rows, head_dim + 3]: sum p v, m (base 2), sum p as taken and as rounded
   int splits, rows, chunks;                      // rows = group * max_q_len, in chunks of kFewRows
   bool cluster;                                  // the splits of a (sequence, key head) are one cluster
 };
@@ -87,13 +87,13 @@ struct ScoreMap {
   }
 };
 
-// A row's result: o / l, and the log-sum-exp
+// A row's result: o over the sum of the p it was made with, and the log-sum-exp
 template <typename T>
 __device__ __forceinline__ void write_result(const FewParams& p, const Share& w, int qi, int head, int c, float o, float l,
-                                             float m) {
+                                             float u, float m) {
   const AttnArgs& a = p.a;
   const size_t row = (size_t)(w.sq.q0 + qi);
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const float inv = l > 0.f || l != l ? 1.f / u : 0.f;
   T* out = reinterpret_cast<T*>(a.out) + row * a.o_stride + (size_t)head * a.head_dim + c;
   if constexpr (sizeof(T) == 2) *out = __float2bfloat16(o * inv);
   else *out = o * inv;
@@ -114,24 +114,26 @@ __device__ __forceinline__ float load_from(const float* mine, int rank) {
 
 // Joins the states of a block's warps in order, then the splits in index order: through the cluster's shared memory,
 // or through a partial in the workspace and a second launch.
-// `st_m`, `st_l` [states][16], `st_o` [states][16][DP] in shared memory; the block's own sums go over the first state's.
+// `st_m`, `st_l`, `st_u` [states][16], `st_o` [states][16][DP] in shared memory; the block's own sums go over the first state's.
 template <typename T>
-__device__ __forceinline__ void finish_block(const FewParams& p, const Share& w, float* st_m, float* st_l, float* st_o,
-                                             int dp, int states) {
+__device__ __forceinline__ void finish_block(const FewParams& p, const Share& w, float* st_m, float* st_l, float* st_u,
+                                             float* st_o, int dp, int states) {
   const AttnArgs& a = p.a;
   const int d = a.head_dim;
   const bool cluster = p.cluster;
   // a thread owns the same (row, value)s in all passes, but reads every warp's m and l of its rows
-  float keep_m = -INFINITY, keep_l = 0.f;
+  float keep_m = -INFINITY, keep_l = 0.f, keep_u = 0.f;
   if (threadIdx.x < 16) {
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, l = 0.f, u = 0.f;
     for (int x = 0; x < states; ++x) m = fmaxf(m, st_m[x * 16 + threadIdx.x]);
     for (int x = 0; x < states; ++x) {
       const float mx = st_m[x * 16 + threadIdx.x], f = mx == -INFINITY ? 0.f : ex2(mx - m);
       l += f * st_l[x * 16 + threadIdx.x];
+      u += f * st_u[x * 16 + threadIdx.x];
     }
     keep_m = m;
     keep_l = l;
+    keep_u = u;
   }
   for (int i = threadIdx.x; i < w.rows * d; i += kWarps * 32) {
     const int r = i / d, c = i - r * d;
@@ -144,7 +146,7 @@ __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w,
     st_o[r * dp + c] = o;
   }
   __syncthreads();
-  if (threadIdx.x < 16) { st_m[threadIdx.x] = keep_m; st_l[threadIdx.x] = keep_l; }
+  if (threadIdx.x < 16) { st_m[threadIdx.x] = keep_m; st_l[threadIdx.x] = keep_l; st_u[threadIdx.x] = keep_u; }
   if (cluster) cluster_sync();
   else __syncthreads();
   // the cluster's blocks share the row's values out among themselves
@@ -153,7 +155,7 @@ __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w,
     const int r = i / d, c = i - r * d;
     const int qi = (w.row0 + r) / a.group, head = w.kvh * a.group + (w.row0 + r - qi * a.group);
     if (qi >= w.lq) continue;
-    float m = st_m[r], l = st_l[r], o = st_o[r * dp + c];
+    float m = st_m[r], l = st_l[r], u = st_u[r], o = st_o[r * dp + c];
     if (cluster) {
       float ms[kClusterMax];
       m = -INFINITY;
@@ -162,23 +164,23 @@ __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w,
         ms[s] = s < p.splits ? load_from(st_m + r, s) : -INFINITY;
         m = fmaxf(m, ms[s]);
       }
-      l = 0.f;
-      o = 0.f;
+      l = u = o = 0.f;
 #pragma unroll
       for (int s = 0; s < kClusterMax; ++s)
         if (s < p.splits && ms[s] != -INFINITY) {
           const float f = ex2(ms[s] - m);
           l += f * load_from(st_l + r, s);
+          u += f * load_from(st_u + r, s);
           o += f * load_from(st_o + r * dp + c, s);
         }
     }
     if (p.splits > 1 && !cluster) {
       const size_t block = (((size_t)w.seq * a.kv_heads + w.kvh) * p.chunks + w.row0 / kFewRows) * p.splits + w.split;
-      float* dst = p.part + (block * kFewRows + r) * (d + 2);
+      float* dst = p.part + (block * kFewRows + r) * (d + 3);
       dst[c] = o;
-      if (c == 0) { dst[d] = m; dst[d + 1] = l; }
+      if (c == 0) { dst[d] = m; dst[d + 1] = l; dst[d + 2] = u; }
     } else {
-      write_result<T>(p, w, qi, head, c, o, l, m);
+      write_result<T>(p, w, qi, head, c, o, l, u, m);
     }
   }
   if (cluster) cluster_sync();                   // nobody leaves while its shared memory is read
@@ -249,7 +251,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
   float o[DP / 8][4];
 #pragma unroll
   for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, used[2] = {0.f, 0.f};   // sums of p as taken and as rounded
   for (int i = 0; i < n; ++i) {
     load(i + kStages - 1);
     copy_wait<kStages - 1>();
@@ -293,6 +295,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
         const float f = m[hf] == -INFINITY ? 0.f : ex2(m[hf] - mn);
         m[hf] = mn;
         l[hf] *= f;
+        used[hf] *= f;
 #pragma unroll
         for (int x = 0; x < DP / 8; ++x) { o[x][2 * hf] *= f; o[x][2 * hf + 1] *= f; }
       }
@@ -306,6 +309,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
         const float e0 = ex2(s[u][2 * hf] - base), e1 = ex2(s[u][2 * hf + 1] - base);
         l[hf] += e0 + e1;
         pf[hf + 2 * u] = bf16x2(e0, e1);
+        used[hf] += bf16_lo(pf[hf + 2 * u]) + bf16_hi(pf[hf + 2 * u]);
       }
     }
     {
@@ -326,21 +330,24 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
   for (int hf = 0; hf < 2; ++hf) {
     l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 1);
     l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 2);
+    used[hf] += __shfl_xor_sync(0xffffffffu, used[hf], 1);
+    used[hf] += __shfl_xor_sync(0xffffffffu, used[hf], 2);
   }
   __syncthreads();                               // the rings become the block's exchange
   float* st_m = reinterpret_cast<float*>(smem);
   float* st_l = st_m + kWarps * 16;
-  float* st_o = st_l + kWarps * 16;
+  float* st_u = st_l + kWarps * 16;
+  float* st_o = st_u + kWarps * 16;
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf) {
     const int r = g + 8 * hf;
-    if (t == 0) { st_m[warp * 16 + r] = m[hf]; st_l[warp * 16 + r] = l[hf]; }
+    if (t == 0) { st_m[warp * 16 + r] = m[hf]; st_l[warp * 16 + r] = l[hf]; st_u[warp * 16 + r] = used[hf]; }
 #pragma unroll
     for (int x = 0; x < DP / 8; ++x)
       *reinterpret_cast<float2*>(st_o + (warp * 16 + r) * DP + x * 8 + 2 * t) = make_float2(o[x][2 * hf], o[x][2 * hf + 1]);
   }
   __syncthreads();
-  finish_block<bf16>(p, w, st_m, st_l, st_o, DP, kWarps);
+  finish_block<bf16>(p, w, st_m, st_l, st_u, st_o, DP, kWarps);
 }
 
 // Where a value of a batch ends up when the M partial sums of LPK lanes are added up: every step of the exchange halves the
@@ -505,14 +512,15 @@ __global__ void __launch_bounds__(kWarps * 32) attn_few_f32_kernel(FewParams p) 
   constexpr int kStates = kWarps * SUB;
   float* st_m = reinterpret_cast<float*>(smem);
   float* st_l = st_m + kStates * 16;
-  float* st_o = st_l + kStates * 16;
+  float* st_u = st_l + kStates * 16;              // p is used as taken
+  float* st_o = st_u + kStates * 16;
   const int state = warp * SUB + sub;
   l = S::over_keys(l, sum);
-  if (own_x == 0) { st_m[state * 16 + own_r] = m; st_l[state * 16 + own_r] = l; }
+  if (own_x == 0) st_m[state * 16 + own_r] = m, st_l[state * 16 + own_r] = l, st_u[state * 16 + own_r] = l;
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) *reinterpret_cast<float4*>(st_o + (state * 16 + r) * DP + c) = o[r];
   __syncthreads();
-  finish_block<float>(p, w, st_m, st_l, st_o, DP, kStates);
+  finish_block<float>(p, w, st_m, st_l, st_u, st_o, DP, kStates);
 }
 
 // Joins the splits of a row in index order; one warp per (sequence, query, head).
@@ -526,23 +534,24 @@ __global__ void __launch_bounds__(128) attn_few_join_kernel(FewParams p) {
   const int qi = r / a.group, head = kvh * a.group + (r - qi * a.group), d = a.head_dim;
   const int q0 = clamp_int(a.q_off[seq], 0, a.q_rows);
   if (qi >= min(seq_rows(a.q_off, seq, a.q_rows), a.max_q_len)) return;
-  const size_t pitch = (size_t)kFewRows * (d + 2);
+  const size_t pitch = (size_t)kFewRows * (d + 3);
   const float* src = p.part + (((size_t)seq * a.kv_heads + kvh) * p.chunks + r / kFewRows) * p.splits * pitch +
-                     (size_t)(r % kFewRows) * (d + 2);
+                     (size_t)(r % kFewRows) * (d + 3);
   float m = -INFINITY;
   for (int s = lane; s < p.splits; s += 32) m = fmaxf(m, src[s * pitch + d]);
 #pragma unroll
   for (int f = 16; f >= 1; f >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, f));
-  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f, u = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   for (int s = 0; s < p.splits; ++s) {
     const float ms = src[s * pitch + d];
     const float f = ms == -INFINITY ? 0.f : exp2f(ms - m);
     l += f * src[s * pitch + d + 1];
+    u += f * src[s * pitch + d + 2];
 #pragma unroll
     for (int x = 0; x < 4; ++x)
       if (lane + 32 * x < d) o[x] += f * src[s * pitch + lane + 32 * x];
   }
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const float inv = l > 0.f || l != l ? 1.f / u : 0.f;
   T* out = reinterpret_cast<T*>(a.out) + (size_t)(q0 + qi) * a.o_stride + (size_t)head * d;
 #pragma unroll
   for (int x = 0; x < 4; ++x)
@@ -553,7 +562,7 @@ __global__ void __launch_bounds__(128) attn_few_join_kernel(FewParams p) {
   if (lane == 0 && a.lse) a.lse[(size_t)head * a.q_rows + q0 + qi] = (m + log2f(l)) * kLn2;
 }
 
-constexpr size_t exchange_bytes(int dp, int states) { return (size_t)states * 16 * (dp + 2) * 4; }
+constexpr size_t exchange_bytes(int dp, int states) { return (size_t)states * 16 * (dp + 3) * 4; }
 
 template <typename K>
 cudaError_t launch_blocks(K kernel, const FewParams& p, unsigned grid, size_t smem, cudaStream_t st) {

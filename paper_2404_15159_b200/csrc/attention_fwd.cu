@@ -266,7 +266,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       const int pos = w.sq.shift + w.row0 + row;
       const RowKeys keys = row_keys(w.sq, a.causal, a.window, pos);
       const float slope2 = BIAS ? a.slopes[w.head] * kLog2e : 0.f;
-      float m = -INFINITY, l = 0.f;                            // m in base 2
+      // m in base 2; the sums of p as taken, for the log-sum-exp, and as rounded, by which O is divided: the weights that
+      // the product uses then sum to one, and a row with one large weight keeps its value
+      float m = -INFINITY, l = 0.f, l_used = 0.f;
       float tile_sum = 0.f;                                    // the last tile's part of l
       int nth = 0;
       for (int it = 0; it < n && ok; ++it) {
@@ -280,6 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
           const float k = tile_sum > 256.f ? ceilf(log2f(tile_sum)) : 0.f, f = ex2(-k);
           m += k;
           l *= f;
+          l_used *= f;
           scale_o(f);
         }
         tile_sum = 0.f;
@@ -320,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
               if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
           }
           uint32_t pk[32];
-          float sum;
+          float sum, sum_used;
           bool reset = m == -INFINITY;                         // nothing seen yet; below: p near the end of its range
 #pragma unroll 1
           for (int attempt = 0; attempt < 2; ++attempt) {      // over their own maximum p are at most about 1
@@ -333,6 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
               const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
               m = m_new;
               l *= f;
+              l_used *= f;
               tile_sum *= f;
               if (c == 1) {                                    // the first half's P may still be on its way into O
                 ok = __all_sync(0xffffffffu, mbar_wait(v_bar(h), cnt & 1u, abort_flag));
@@ -343,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             }
             const float shift = m == -INFINITY ? 0.f : -m;
             const uint64_t mul_2 = pair2(to2, to2), shift_2 = pair2(shift, shift);
-            uint64_t acc[2] = {0ull, 0ull};
+            uint64_t acc[2] = {0ull, 0ull}, used[2] = {0ull, 0ull};
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
               uint64_t v = pair2(x[2 * i], x[2 * i + 1]);
@@ -354,16 +358,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
               e1 = ex2(e1);
               acc[i & 1] = add2(acc[i & 1], pair2(e0, e1));
               pk[i] = bf16x2(e0, e1);
+              used[i & 1] = add2(used[i & 1], pair2(bf16_lo(pk[i]), bf16_hi(pk[i])));
             }
             float l0, l1;
             unpair2(add2(acc[0], acc[1]), l0, l1);
             sum = l0 + l1;
+            unpair2(add2(used[0], used[1]), l0, l1);
+            sum_used = l0 + l1;
             tmem_st32(s_addr + c * 32, pk);                    // over scores of the tile's first half
             reset = sum > 0x1p100f;
             if (!__any_sync(0xffffffffu, reset)) break;
           }
           if (!ok) break;
           l += sum;
+          l_used += sum_used;
           tile_sum += sum;
           tmem_st_wait();
           tc_fence_before();
@@ -379,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         tc_fence_after();
       }
       if (ok && rows > h * kTile) {
-        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;   // a row that sees nothing gives zeros
+        const float inv = l > 0.f || l != l ? 1.f / l_used : 0.f;   // a row that sees nothing gives zeros
         const bool mine = row < rows;
         bf16* dst = reinterpret_cast<bf16*>(a.out) + (size_t)(w.sq.q0 + w.row0 + (mine ? row : 0)) * a.o_stride +
                     (size_t)w.head * a.head_dim;

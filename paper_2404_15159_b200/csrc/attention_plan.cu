@@ -41,7 +41,7 @@ __device__ __forceinline__ int block_sum(int v, int* warp_sums, int* total) {
 
 __global__ void __launch_bounds__(kThreads) attn_plan_kernel(AttnArgs a, AttnPlanJob job0, AttnPlanJob job1) {
   const AttnPlanJob job = blockIdx.x == 0 ? job0 : job1;
-  __shared__ int warp_sums[32], levels[kLevels];
+  __shared__ int warp_sums[32], levels[kLevels], first_near[kThreads];
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
   for (int i = threadIdx.x; i < kLevels; i += kThreads) levels[i] = 0;
   int total = 0;
@@ -54,21 +54,25 @@ __global__ void __launch_bounds__(kThreads) attn_plan_kernel(AttnArgs a, AttnPla
     }
     int sum;
     const int upto = block_sum(n, warp_sums, &sum);
-    if (b < a.n_seqs) job.first[b] = total + upto - n;
+    if (b < a.n_seqs) {
+      job.first[b] = total + upto - n;
+      if (b0 == 0) first_near[b] = upto - n;
+    }
     total += sum;
   }
   __syncthreads();                               // `first` is read by other threads of this block
+  const int* first = a.n_seqs <= kThreads ? first_near : job.first;
   total = min(total, job.capacity);              // offsets that overlap could ask for more
   // the tile with number i: its sequence is the last one that starts at or before it and has tiles
   auto tile = [&](int i, AttnTile* t) {
     int lo = 0, hi = a.n_seqs - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (job.first[mid] <= i) lo = mid;
+      if (first[mid] <= i) lo = mid;
       else hi = mid - 1;
     }
     t->sq = load_seq(a, lo);
-    t->row0 = (i - job.first[lo]) * job.tile_rows;
+    t->row0 = (i - first[lo]) * job.tile_rows;
     const AttnSeq& s = t->sq;
     int work;
     if (job.keys) {
@@ -81,15 +85,24 @@ __global__ void __launch_bounds__(kThreads) attn_plan_kernel(AttnArgs a, AttnPla
     }
     return kLevels - 1 - min(work, kLevels - 1);
   };
-  AttnTile t;
-  for (int i = threadIdx.x; i < total; i += kThreads) atomicAdd(&levels[tile(i, &t)], 1);
+  AttnTile t;                                    // a thread's first tile is kept for the second pass
+  int level = 0;
+  if ((int)threadIdx.x < total) {
+    level = tile(threadIdx.x, &t);
+    atomicAdd(&levels[level], 1);
+  }
+  for (int i = threadIdx.x + kThreads; i < total; i += kThreads) {
+    AttnTile u;
+    atomicAdd(&levels[tile(i, &u)], 1);
+  }
   __syncthreads();
   int sum;
   const int mine = levels[threadIdx.x], upto = block_sum(mine, warp_sums, &sum);
   levels[threadIdx.x] = upto - mine;
   __syncthreads();
   for (int i = threadIdx.x; i < total; i += kThreads) {
-    const int at = atomicAdd(&levels[tile(i, &t)], 1);
+    if (i >= kThreads) level = tile(i, &t);
+    const int at = atomicAdd(&levels[level], 1);
     int4* dst = reinterpret_cast<int4*>(job.table + at);
     dst[0] = make_int4(t.sq.q0, t.sq.lq, t.sq.k0, t.sq.lk);
     dst[1] = make_int4(t.sq.shift, t.sq.prefix, t.row0, 0);
