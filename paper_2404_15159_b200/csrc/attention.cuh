@@ -258,6 +258,27 @@ cudaError_t allow_smem(K kernel, int bytes, bool (&done)[64]) {
   return e;
 }
 
+// Launches of one call follow each other closely: a kernel launched with launch_behind() may start, and set itself up, as
+// soon as every block of the kernel before it has begun (let_next_start), and waits for that kernel's end and results
+// with wait_for_last before it touches anything that the call's kernels share.  Saves 2 to 3 us a launch.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename... Params, typename... Args>
+cudaError_t launch_behind(void (*kernel)(Params...), unsigned grid, unsigned block, size_t smem, cudaStream_t st,
+                          const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
 // Plans the tiles of `tile_rows` query rows (keys: of keys): `table` of `capacity` entries, `first` [n_seqs] scratch.  Also
 // clears the status word.
 struct AttnPlanJob {

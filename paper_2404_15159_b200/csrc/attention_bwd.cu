@@ -223,6 +223,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t tmem = block_begin(c, slot, 8);
   const uint32_t t_s = tmem, t_dp = tmem + kTile, t_dv = tmem + 2 * kTile, t_dk = t_dv + DP;
+  let_next_start();
+  wait_for_last();                               // the plan, and delta
   TileWalk w(a.k_tiles, a.n_k_tiles, a.kv_heads);            // w.head is the key head
   // of the tile at hand: the query tiles of a head that see it, from row `lo`, and the steps over all heads that share it
   int lo = 0, per_head = 0;
@@ -499,6 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
   const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const uint32_t tmem = block_begin(c, slot, 4);
   const uint32_t t_dp = tmem + 2 * kTile, t_dq = tmem + 3 * kTile;
+  wait_for_last();
   TileWalk w(a.q_tiles, a.n_q_tiles, a.q_heads);
   auto rows_of = [&] { return min(kTile, w.sq.lq - w.row0); };
   auto tiles_of = [&] {
@@ -688,6 +691,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) attn_delta_kernel(AttnArgs a, float* lse2, float* delta) {
   constexpr int V = 16 / sizeof(T), ITEMS = 4, CHUNKS = sizeof(T) == 2 ? 1 : 2;   // a head is at most 128 values
   __shared__ float sums[kDeltaHeads * kDeltaRows];
+  let_next_start();
   const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
   const int head_blocks = (a.q_heads + kDeltaHeads - 1) / kDeltaHeads;
   const int row0 = blockIdx.x / head_blocks * kDeltaRows, head0 = blockIdx.x % head_blocks * kDeltaHeads;
@@ -730,6 +734,7 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(AttnArgs a, float* lse2
     delta[at] = sums[threadIdx.x];
     lse2[at] = z == -INFINITY ? INFINITY : z * kLog2e;
   }
+  wait_for_last();                               // not needed here, but what comes behind this kernel needs the plan too
 }
 
 template <int DP, bool CAP, bool BIAS>
@@ -738,12 +743,10 @@ cudaError_t launch(const BwdParams& p, unsigned grid_kv, unsigned grid_q, cudaSt
   cudaError_t e = allow_smem(attn_bwd_kv_kernel<DP, CAP, BIAS>, kSmemBytes<DP>, done_kv);
   if (e == cudaSuccess) e = allow_smem(attn_bwd_q_kernel<DP, CAP, BIAS>, kSmemBytes<DP>, done_q);
   if (e != cudaSuccess) return e;
-  if (grid_kv) {
-    attn_bwd_kv_kernel<DP, CAP, BIAS><<<grid_kv, kThreads, kSmemBytes<DP>, st>>>(p);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-  }
-  if (grid_q) attn_bwd_q_kernel<DP, CAP, BIAS><<<grid_q, kThreads, kSmemBytes<DP>, st>>>(p);
-  return cudaGetLastError();
+  if (grid_kv) e = launch_behind(attn_bwd_kv_kernel<DP, CAP, BIAS>, grid_kv, kThreads, kSmemBytes<DP>, st, p);
+  if (e == cudaSuccess && grid_q)
+    e = launch_behind(attn_bwd_q_kernel<DP, CAP, BIAS>, grid_q, kThreads, kSmemBytes<DP>, st, p);
+  return e;
 }
 template <int DP>
 cudaError_t launch_dp(const BwdParams& p, unsigned gk, unsigned gq, cudaStream_t st) {
@@ -757,8 +760,8 @@ cudaError_t launch_attn_delta(const AttnArgs& a, bool bf16_mode, float* lse2, fl
   const long long blocks = ((long long)a.q_rows + kDeltaRows - 1) / kDeltaRows * ((a.q_heads + kDeltaHeads - 1) / kDeltaHeads);
   if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
   if (blocks == 0) return cudaSuccess;
-  if (bf16_mode) attn_delta_kernel<bf16><<<(unsigned)blocks, 256, 0, st>>>(a, lse2, delta);
-  else attn_delta_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(a, lse2, delta);
+  if (bf16_mode) return launch_behind(attn_delta_kernel<bf16>, (unsigned)blocks, 256, 0, st, a, lse2, delta);
+  attn_delta_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(a, lse2, delta);
   return cudaGetLastError();
 }
 

@@ -195,6 +195,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
   constexpr int kStageBytes = 2 * kStep * DP * 2;
   extern __shared__ __align__(128) uint8_t smem[];
   const AttnArgs& a = p.a;
+  let_next_start();
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
@@ -417,6 +418,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn_few_f32_kernel(FewParams p) 
   constexpr int OWN = S::kOwn;
   extern __shared__ __align__(128) uint8_t smem[];
   const AttnArgs& a = p.a;
+  let_next_start();
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int sub = lane / LPK, sl = lane % LPK, c = sl * 4;
@@ -527,6 +529,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn_few_f32_kernel(FewParams p) 
 template <typename T>
 __global__ void __launch_bounds__(128) attn_few_join_kernel(FewParams p) {
   const AttnArgs& a = p.a;
+  wait_for_last();
   const int item = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int seq = item / (p.rows * a.kv_heads);
   if (seq >= a.n_seqs) return;
@@ -640,9 +643,8 @@ cudaError_t launch_attn_few(const AttnArgs& a, bool bf16_mode, FewSplits splits,
   if (e != cudaSuccess || p.splits == 1 || p.cluster) return e;
   const long long items = (long long)a.n_seqs * a.kv_heads * p.rows;
   const unsigned jg = (unsigned)((items + 3) / 4);
-  if (bf16_mode) attn_few_join_kernel<bf16><<<jg, 128, 0, st>>>(p);
-  else attn_few_join_kernel<float><<<jg, 128, 0, st>>>(p);
-  return cudaGetLastError();
+  return bf16_mode ? launch_behind(attn_few_join_kernel<bf16>, jg, 128, 0, st, p)
+                   : launch_behind(attn_few_join_kernel<float>, jg, 128, 0, st, p);
 }
 
 }  // namespace mixlora

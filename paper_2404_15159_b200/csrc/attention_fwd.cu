@@ -83,6 +83,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = warp_uniform(*slot);
+  wait_for_last();                               // the plan
   TileWalk w(a.q_tiles, a.n_q_tiles, a.q_heads);
   // of the tile at hand: its rows, its key tiles, and those of them that a half of the rows needs
   auto rows_of = [&] { return min(2 * kTile, w.sq.lq - w.row0); };
@@ -444,8 +445,7 @@ cudaError_t launch(const FwdParams& p, unsigned grid, cudaStream_t st) {
   static bool done[64];
   cudaError_t e = allow_smem(attn_fwd_tc_kernel<DP, CAP, BIAS>, kSmemBytes<DP>, done);
   if (e != cudaSuccess) return e;
-  attn_fwd_tc_kernel<DP, CAP, BIAS><<<grid, kThreads, kSmemBytes<DP>, st>>>(p);
-  return cudaGetLastError();
+  return launch_behind(attn_fwd_tc_kernel<DP, CAP, BIAS>, grid, kThreads, kSmemBytes<DP>, st, p);
 }
 
 template <int DP>

@@ -40,6 +40,7 @@ __device__ __forceinline__ int block_sum(int v, int* warp_sums, int* total) {
 }
 
 __global__ void __launch_bounds__(kThreads) attn_plan_kernel(AttnArgs a, AttnPlanJob job0, AttnPlanJob job1) {
+  let_next_start();
   const AttnPlanJob job = blockIdx.x == 0 ? job0 : job1;
   __shared__ int warp_sums[32], levels[kLevels], first_near[kThreads];
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) *a.status = 0;
