@@ -269,7 +269,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       const float slope2 = BIAS ? a.slopes[w.head] * kLog2e : 0.f;
       // m in base 2; the sums of p as taken, for the log-sum-exp, and as rounded, by which O is divided: the weights that
       // the product uses then sum to one, and a row with one large weight keeps its value
-      float m = -INFINITY, l = 0.f, l_used = 0.f;
+      // Scores capped at up to 2^96 either way need no maximum at all: 2^s stays inside the range of fp32 and bf16.
+      const bool bounded = CAP && !BIAS && cap2 <= 96.f;
+      float m = bounded ? 0.f : -INFINITY, l = 0.f, l_used = 0.f;
       float tile_sum = 0.f;                                    // the last tile's part of l
       int nth = 0;
       for (int it = 0; it < n && ok; ++it) {
@@ -279,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         if (!ok) break;
         tc_fence_after();
         // S is there, so the products before it have finished and O stands still
-        if (__any_sync(0xffffffffu, tile_sum > 256.f)) {       // the last tile's p had grown: m follows
+        if (!bounded && __any_sync(0xffffffffu, tile_sum > 256.f)) {       // the last tile's p had grown: m follows
           const float k = tile_sum > 256.f ? ceilf(log2f(tile_sum)) : 0.f, f = ex2(-k);
           m += k;
           l *= f;
@@ -319,9 +321,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             for (int j = 0; j < 64; ++j) x[j] = fmaf(-slope2, fabsf(d - (float)j), CAP ? x[j] : x[j] * mul);
           }
           if (!whole) {
+            if (__all_sync(0xffffffffu, lo <= 0 && pre <= 0)) {  // the usual case: rows or keys end here
 #pragma unroll
-            for (int j = 0; j < 64; ++j)
-              if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
+              for (int j = 0; j < 64; ++j)
+                if (j >= hi) x[j] = -INFINITY;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 64; ++j)
+                if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
+            }
           }
           uint32_t pk[32];
           float sum, sum_used;
