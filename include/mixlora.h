@@ -358,7 +358,7 @@ typedef struct {
   int32_t causal;             /* 0 or 1 */
   int32_t window;             /* 0: none */
   float scale;                /* > 0 */
-  float softcap;              /* 0: none */
+  float softcap;              /* 0: none; scale / softcap has to be finite */
   int64_t q_stride, k_stride, v_stride, o_stride;
 } mixlora_attention_shape_t;
 typedef struct {

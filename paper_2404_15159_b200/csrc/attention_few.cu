@@ -104,6 +104,7 @@ __device__ __forceinline__ void write_result(const FewParams& p, const Share& w,
   if (c == 0 && a.lse) a.lse[(size_t)head * a.q_rows + row] = (m + log2f(l)) * kLn2;
 }
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }

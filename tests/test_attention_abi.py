@@ -76,7 +76,7 @@ def attention(B, drop=(), ws=PTR, ws_bytes=1 << 40, mask_edit=None, at=None, **e
     (dict(q_heads=3), INVALID), (dict(head_dim=0), INVALID), (dict(head_dim=60), UNSUPPORTED), (dict(head_dim=136), UNSUPPORTED),
     (dict(dtype=2), INVALID), (dict(causal=2), INVALID), (dict(window=-1), INVALID), (dict(scale=0.0), INVALID),
     (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID), (dict(softcap=-1.0), INVALID),
-    (dict(softcap=float("nan")), INVALID), (dict(q_stride=8), INVALID), (dict(k_stride=-128), INVALID),
+    (dict(softcap=float("nan")), INVALID), (dict(softcap=1e-42, scale=1e3), INVALID), (dict(q_stride=8), INVALID), (dict(k_stride=-128), INVALID),
     (dict(v_stride=132), UNSUPPORTED), (dict(o_stride=260), UNSUPPORTED), (dict(q_rows=2 ** 30 + 1), UNSUPPORTED),
     (dict(k_rows=2 ** 30 + 1), UNSUPPORTED)])
 def test_attention_shape_refusals(B, edit, status):
