@@ -74,8 +74,8 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
 #pragma unroll
   for (int j = 0; j < DP / 64; ++j) tma_load_3d(dst + j * (kTile * 128), map, bar, j * 64, head, row);
 }
-// Rows [first, 128) of a tile belong to someone else and may hold anything; where they are summed over they have to be
-// finite (their factor is zero).  One warp.
+// Rows [first, 128) of a tile belong to someone else and may hold anything; as the summed index of a product, and as the
+// columns of scores and dP, they have to be finite (p and ds are zero there).  One warp.
 template <int DP>
 __device__ __forceinline__ void clear_rows(uint32_t tile, int first) {
   constexpr int NB = DP / 64;
@@ -387,19 +387,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
                                          mbar_wait(c.s(0), at & 1u, c.abort_flag));
         if (!ok) break;
         tc_fence_after();
-        float pr[64];
+        float pr[2][32];
         if (none) {
           store_zeros(s_addr);
         } else {
-          tmem_ld32(s_addr, *reinterpret_cast<uint32_t(*)[32]>(&pr[0]));
-          tmem_ld32(s_addr + 32, *reinterpret_cast<uint32_t(*)[32]>(&pr[32]));
-          tmem_ld_wait();
           const float d = (float)(pos0 - j);
-          score.cap(pr);
 #pragma unroll
           for (int c0 = 0; c0 < 2; ++c0) {
             uint64_t cs[CAP ? 16 : 1];
-            float* pc = pr + c0 * 32;
+            float (&pc)[32] = pr[c0];
+            tmem_ld32(s_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&pc[0]));
+            tmem_ld_wait();
+            score.cap(pc);
 #pragma unroll
             for (int x = 0; x < 32; x += 4) {
               const float4 ls = *reinterpret_cast<const float4*>(neg_lse + c0 * 32 + x);
@@ -429,8 +428,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
               for (int x = 0; x < 32; x += 2) {
                 float f0, f1;
                 unpair2(mul2(pair2(pc[x], pc[x + 1]), cs[x / 2]), f0, f1);
-                pc[x] = !whole && pc[x] == 0.f ? 0.f : f0;       // a hidden score's slope may be anything
-                pc[x + 1] = !whole && pc[x + 1] == 0.f ? 0.f : f1;
+                pc[x] = f0;
+                pc[x + 1] = f1;
               }
             }
           }
@@ -450,16 +449,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
             float dp[32];
             tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
             tmem_ld_wait();
-            if (!whole) {                                        // rows behind the last may hold anything
-#pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
-            }
             uint32_t pk[16];
 #pragma unroll
             for (int x = 0; x < 32; x += 4) {
               const float4 dl = *reinterpret_cast<const float4*>(neg_delta + c0 * 32 + x);
-              const float* pv = pr + c0 * 32 + x;
+              const float* pv = pr[c0] + x;
               uint64_t u = add2(pair2(dp[x], dp[x + 1]), pair2(dl.x, dl.y)), v = add2(pair2(dp[x + 2], dp[x + 3]), pair2(dl.z, dl.w));
               u = mul2(u, pair2(pv[0], pv[1]));
               v = mul2(v, pair2(pv[2], pv[3]));
@@ -553,15 +547,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
       bool ok = true;
       int at = 0, used = 0;
       KeyTiles<kTile> tiles;
-      auto scores = [&](int i) {                               // over ds of two tiles ago, which its product has read
-        if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
+      // a stream's tile i is in shared memory, its keys behind the last cleared
+      auto tail = [&](int i, uint32_t tile) {
         const int valid = w.sq.lk - tiles.at(i) * kTile;
         if (valid < kTile) {
-          clear_rows<DP>(k_at(at + i), valid);
+          clear_rows<DP>(tile, valid);
           fence_proxy_async_smem();
           __syncwarp();
         }
         tc_fence_after();
+      };
+      auto scores = [&](int i) {                               // over ds of two tiles ago, which its product has read
+        if (!__all_sync(0xffffffffu, c.wait_full_a(at + i))) return false;
+        tail(i, k_at(at + i));
         if (one) {
           issue_nt<DP>(tmem + ((at + i) & 1) * kTile, q_tile, k_at(at + i));
           umma_commit(c.s((at + i) & 1));
@@ -570,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
       };
       auto grads = [&](int i) {
         if (!__all_sync(0xffffffffu, c.wait_full_b(at + i))) return false;
-        tc_fence_after();
+        tail(i, v_at(at + i));
         if (one) {
           issue_nt<DP>(t_dp, do_tile, v_at(at + i));
           umma_commit(c.dp());
@@ -665,11 +663,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
             float dp[32];
             tmem_ld32(dp_addr + c0 * 32, *reinterpret_cast<uint32_t(*)[32]>(&dp[0]));
             tmem_ld_wait();
-            if (!whole) {                                        // keys behind the last may hold anything
-#pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (pr[c0 * 32 + x] == 0.f) dp[x] = 0.f;
-            }
             uint32_t pk[16];
 #pragma unroll
             for (int x = 0; x < 32; x += 2) {
