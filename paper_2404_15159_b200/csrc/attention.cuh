@@ -133,6 +133,13 @@ __device__ __forceinline__ void query_rows(const AttnSeq& s, int causal, int win
   }
 }
 
+// Bits 0 to n - 1, of 32
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : (1u << max(n, 0)) - 1u; }
+// Of 32 keys from j0: those that `lo`, `hi` and `prefix`, counted from j0, leave visible
+__device__ __forceinline__ uint32_t seen_bits(int lo, int hi, int prefix) {
+  return (low_bits(hi) & ~low_bits(lo)) | low_bits(prefix);
+}
+
 // 2^x in one special-function operation (within 2^-22 of the value; below 2^-126 it gives zero)
 __device__ __forceinline__ float ex2(float x) {
   float y;

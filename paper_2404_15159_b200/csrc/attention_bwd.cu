@@ -382,7 +382,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
         r_hi -= i0;
         const bool whole = __all_sync(0xffffffffu, r_lo <= 0 && r_hi >= 64);
         const bool none = __all_sync(0xffffffffu, min(r_hi, 64) <= max(r_lo, 0));
-        const bool to_end = __all_sync(0xffffffffu, r_hi >= 64);
         ok = __all_sync(0xffffffffu, mbar_wait(c.rows_full(at), (at >> 1) & 1u, c.abort_flag) &&
                                          mbar_wait(c.s(0), at & 1u, c.abort_flag));
         if (!ok) break;
@@ -409,15 +408,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_kv_kernel(const __grid_c
               score.probs(pc[x + 2], pc[x + 3], pair2(ls.z, ls.w), d0 + 2.f, d0 + 3.f, pc[x + 2], pc[x + 3], cs1);
             }
             if (!whole) {
-              if (to_end) {                                      // the usual case: rows from the key's own on
+              const uint32_t seen = seen_bits(r_lo - c0 * 32, r_hi - c0 * 32, 0);
 #pragma unroll
-                for (int x = 0; x < 32; ++x)
-                  if (c0 * 32 + x < r_lo) pc[x] = 0.f;
-              } else {
-#pragma unroll
-                for (int x = 0; x < 32; ++x)
-                  if (c0 * 32 + x < r_lo || c0 * 32 + x >= r_hi) pc[x] = 0.f;
-              }
+              for (int x = 0; x < 32; ++x)
+                if (!(seen & (1u << x))) pc[x] = 0.f;
             }
             uint32_t pk[16];
 #pragma unroll
@@ -641,14 +635,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_bwd_q_kernel(const __grid_co
             if (CAP) unpair2(mul2(pair2(pr[x], pr[x + 1]), cs), pr[x], pr[x + 1]);
           }
           if (!whole) {
-            if (__all_sync(0xffffffffu, lo <= 0 && pre <= 0)) {  // the usual case: rows or keys end here
 #pragma unroll
-              for (int x = 0; x < 64; ++x)
-                if (x >= hi) pr[x] = 0.f;
-            } else {
+            for (int b = 0; b < 64; b += 32) {
+              const uint32_t seen = seen_bits(lo - b, hi - b, pre - b);
 #pragma unroll
-              for (int x = 0; x < 64; ++x)
-                if (!((x >= lo && x < hi) || x < pre)) pr[x] = 0.f;
+              for (int x = 0; x < 32; ++x)
+                if (!(seen & (1u << x))) pr[b + x] = 0.f;
             }
           }
         }

@@ -329,15 +329,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
 #pragma unroll
             for (int j = 0; j < 64; ++j) x[j] = fmaf(-slope2, fabsf(d - (float)j), CAP ? x[j] : x[j] * mul);
           }
-          if (!whole) {
-            if (__all_sync(0xffffffffu, lo <= 0 && pre <= 0)) {  // the usual case: rows or keys end here
+          if (!whole) {                                        // a bit and a selection a score, whatever the mask
 #pragma unroll
-              for (int j = 0; j < 64; ++j)
-                if (j >= hi) x[j] = -INFINITY;
-            } else {
+            for (int b = 0; b < 64; b += 32) {
+              const uint32_t seen = seen_bits(lo - b, hi - b, pre - b);
 #pragma unroll
-              for (int j = 0; j < 64; ++j)
-                if (!((j >= lo && j < hi) || j < pre)) x[j] = -INFINITY;
+              for (int j = 0; j < 32; ++j)
+                if (!(seen & (1u << j))) x[b + j] = -INFINITY;
             }
           }
           uint32_t pk[32];
