@@ -152,6 +152,16 @@ def test_masks(mask, bf16):
 
 
 @TYPES
+@pytest.mark.parametrize("mask", [dict(), dict(causal=False), dict(window=210), dict(prefix=[500, 100]),
+                                  dict(prefix=[140, 0], window=70, softcap=8.0), dict(causal=False, window=150)], ids=str)
+def test_distance_over_many_tiles(mask, bf16):
+    # the scores rise or fall by up to hundreds from tile to tile, in either direction, under every kind of mask
+    c = Case([601, 300], k_lens=[601, 450], hq=4, hk=4, dim=96, seed=21, bf16=bf16, tail=4,
+             slopes=[1.0, 0.03, -0.5, 0.0], **mask)
+    c.check(c.run())
+
+
+@TYPES
 @pytest.mark.parametrize("hq,hk", [(1, 1), (8, 1), (6, 2), (5, 5)])
 def test_shared_heads(hq, hk, bf16):
     c = Case([200, 141], hq=hq, hk=hk, dim=64, seed=hq, bf16=bf16)
