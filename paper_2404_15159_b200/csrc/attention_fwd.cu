@@ -263,6 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     bool ok = true;
     int cnt = 0;                                             // tiles of this half so far, over all row tiles
     int o_used = 0;
+    // Waits for its stores too: a tile may rescale O twice, and only that wait orders a load behind a store.
     auto scale_o = [&](float f) {
 #pragma unroll 1
       for (int i = 0; i < DP / 16; ++i) {
@@ -273,6 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
         tmem_st16(o_addr + i * 16, o);
       }
+      tmem_st_wait();
     };
     while (ok && w.next()) {
       const KeyTiles<kTile> tiles = tiles_of(), need = half_tiles(h);
@@ -388,6 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             tmem_st32(s_addr + c * 32, pk);                    // over scores of the tile's first half
             reset = sum > 0x1p100f;
             if (!__any_sync(0xffffffffu, reset)) break;
+            tmem_st_wait();                                    // the next attempt writes the same columns
           }
           if (!ok) break;
           l += sum;
