@@ -1,5 +1,6 @@
 """Masked attention at the edges of its range: scores that jump within a tile, capped scores of every size, values that
 are very large or small, what lies outside the sequences.  Cases, oracle and bounds as in test_gpu_attention.py."""
+import numpy as np
 import pytest
 
 from paper_2404_15159_b200 import synth
@@ -21,4 +22,53 @@ def test_rows_of_a_warp_rescale_at_different_places(mask, dim):
     c.k[:, :, :2] = 0.0
     c.k[grow, :, 0], c.k[jump, :, 1] = 4.5, 50.0
     c.q = synth.round_to_bf16(c.q)                   # as the GPU gets them
+    c.check(c.run())
+
+
+def parts(c, got, b):
+    """What a run gives for sequence b: its rows and its used keys."""
+    rows = slice(c.q_off[b], c.q_off[b + 1])
+    keys = slice(c.k_off[b], c.k_off[b] + (c.k_off[b + 1] - c.k_off[b] if c.k_len is None else c.k_len[b]))
+    return {n: x[:, rows] if n == "lse" else x[keys] if n in ("d_k", "d_v") else x[rows] for n, x in got.items()}
+
+
+def same(a, b):
+    assert all(np.array_equal(a[n], b[n]) for n in a), [n for n in a if not np.array_equal(a[n], b[n])]
+
+
+@pytest.mark.parametrize("q_len", [0, 2])
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("slopes", [None, [0.25, 0.0]], ids=str)
+def test_capped_scores_are_the_same_whatever_lies_outside(slopes, bf16, q_len):
+    # zeros, values whose scores lie far above the cap, and NaN: behind the used keys, and in rows of no sequence
+    lens, slots, used = ([40, 150, 1], [70, 200, 130], [50, 150, 129]) if q_len == 0 else ([q_len] * 3, [70, 200, 130], [50, 150, 129])
+    runs = []
+    for fill in (0.0, 1000.0, np.nan):
+        c = Case(lens, k_lens=slots, k_len=used, hq=2, hk=2, dim=64, seed=81, bf16=bf16, tail=70, softcap=6.0, slopes=slopes)
+        for x in (c.q, c.k, c.v, c.d_o):
+            x[np.isnan(x)] = fill
+        runs.append(c.run(backward=q_len == 0, max_q_len=q_len))
+    for got in runs[1:]:
+        for b in range(3):
+            same(parts(c, runs[0], b), parts(c, got, b))
+
+
+@pytest.mark.parametrize("slopes", [None, [0.25, 0.0]], ids=str)
+def test_capped_scores_are_the_same_whatever_the_neighbours_hold(slopes):
+    runs = []
+    for amp in (1.0, 64.0):
+        c = Case([75, 140, 200], hq=2, hk=2, dim=64, seed=82, softcap=6.0, slopes=slopes)
+        for x in (c.q, c.k, c.v, c.d_o):
+            x[:75] *= amp
+            x[215:] *= amp
+        runs.append(c.run())
+    same(parts(c, runs[0], 1), parts(c, runs[1], 1))
+    assert not np.array_equal(parts(c, runs[0], 0)["o"], parts(c, runs[1], 0)["o"])
+
+
+@pytest.mark.parametrize("amp", [0.2, 3.0, 30.0])
+@pytest.mark.parametrize("mask", [dict(), dict(slopes=[0.25, 0.0]), dict(window=70, prefix=[20, 0])], ids=str)
+def test_scores_below_around_and_far_above_the_cap(mask, amp):
+    # amp 0.2: the polynomial alone; 3: both forms in a warp; 30: most scores at the cap
+    c = Case([190, 300], hq=2, hk=2, dim=96, seed=83, amp=amp, softcap=4.0, **mask)
     c.check(c.run())
