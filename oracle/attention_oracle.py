@@ -58,15 +58,16 @@ def visible(lq, lk, causal=True, window=0, prefix=0):
 
 
 def attention(q, k, v, q_off, k_off, k_len=None, prefix=None, slopes=None, scale=None, causal=True, window=0,
-              softcap=0.0, d_o=None, p_step=0.0, out_step=2.0 ** -24):
+              softcap=0.0, d_o=None, p_step=0.0, out_step=2.0 ** -24, cap_rel=None):
     """Outputs and, with d_o, gradients, as a dict; `bound` holds for each how far a kernel may be off that forms scores
     and sums in fp32, rounds p and ds relatively by `p_step`, and its outputs (o before the backward pass too) by
     `out_step`.  Rows outside every sequence are NaN in both.
 
     The bounds: a score is a sum of D products in fp32, off by at most (D + 4) 2^-24 sum |q k| scale (the last factors'
-    roundings included), a cap or a distance adds a few 2^-22 of its size; p is off relatively by twice the row's
-    largest score error (its own and, through the sum, the others'), by n 2^-24 for the sum of n terms and by a few
-    2^-22 for the exponential: together `rel`.  fp32 (and bf16, which has its range) ends at 2^-126: a p, a ds, a product
+    roundings included), a cap or a distance adds a few 2^-22 of its size (with `cap_rel` a cap adds that part of the
+    score instead: for caps far above the scores); p is off relatively by twice the row's largest score error (its own
+    and, through the sum, the others'), by n 2^-24 for the sum of n terms and by a few 2^-22 for the exponential:
+    together `rel`.  fp32 (and bf16, which has its range) ends at 2^-126: a p, a ds, a product
     of theirs or an output below that may become zero, which is off by at most 2^-126 itself (`TINY`) and by
     that times the other factor in the sums it enters.  Everything below is the product rule over those."""
     hq, hk, dim = q.shape[1], k.shape[1], q.shape[2]
@@ -96,7 +97,7 @@ def attention(q, k, v, q_off, k_off, k_len=None, prefix=None, slopes=None, scale
                 t = np.tanh(s / softcap)
                 cap = 1.0 - t * t
                 s = softcap * t
-                err = err + softcap * 2.0 ** -20
+                err = err + (softcap * 2.0 ** -20 if cap_rel is None else cap_rel * np.abs(s))
             if slopes is not None:
                 s = s - float(slopes[h]) * dist
                 err = err + 2.0 ** -22 * np.abs(s)

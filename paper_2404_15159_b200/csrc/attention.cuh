@@ -233,6 +233,12 @@ __device__ __forceinline__ uint64_t tanh_poly(uint64_t u) {
   return mul2(y, u);
 }
 
+__device__ __forceinline__ float tanh_one(float x) {
+  float p, unused;
+  unpair2(tanh_poly(pair2(x, 0.f)), p, unused);
+  return fabsf(x) > kTanhPoly ? tanh_fast(x) : p;
+}
+
 // x <- tanh(x * mul) for a thread's scores.  What a value becomes depends on itself alone: the values of a warp only decide
 // together whether any of them needs the special functions, so hidden keys and rows of other sequences change nothing.
 // Where one does the warp computes both forms of every value (4096 rows, 16 heads of 128: forward 86 us without any, 119

@@ -79,13 +79,13 @@ __device__ __forceinline__ Share block_share(const FewParams& p) {
 
 template <bool CAP, bool BIAS>
 struct ScoreMap {
-  float mul, cap2, scale2;
+  float mul, cap2;
   __device__ __forceinline__ explicit ScoreMap(const AttnArgs& a)
-      : mul(CAP ? a.scale / a.softcap : a.scale * kLog2e), cap2(a.softcap * kLog2e), scale2(0.f) {}
+      : mul(CAP ? a.scale / a.softcap : a.scale * kLog2e), cap2(a.softcap * kLog2e) {}
   // score in base 2; `slope2` in base 2 too
   __device__ __forceinline__ float operator()(float s, float slope2, int distance) const {
     float x = s * mul;
-    if (CAP) x = cap2 * tanh_fast(x);
+    if (CAP) x = cap2 * tanh_one(x);
     if (BIAS) x -= slope2 * fabsf((float)distance);
     return x;
   }

@@ -72,3 +72,14 @@ def test_scores_below_around_and_far_above_the_cap(mask, amp):
     # amp 0.2: the polynomial alone; 3: both forms in a warp; 30: most scores at the cap
     c = Case([190, 300], hq=2, hk=2, dim=96, seed=83, amp=amp, softcap=4.0, **mask)
     c.check(c.run())
+
+
+@pytest.mark.parametrize("few", [True, False])
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("softcap", [200.0, 1e4, 1e8, 1e30])
+def test_caps_far_above_the_scores(softcap, bf16, few):
+    # A capped score is cap2 tanh(x mul): the three factors' and two products' roundings are 5 half steps of 2^-24, the
+    # polynomial is off by 2.6e-7 (4.4 of 2^-24) and rounds 3 times more at its end: 2^-20 of the score covers them.
+    c = Case([2, 1, 2] if few else [60, 1, 130], k_lens=[700, 300, 130], k_len=[700, 256, 130], hq=4, hk=2, dim=128, seed=84,
+             bf16=bf16, softcap=softcap, cap_rel=2.0 ** -20)
+    c.check(c.run(backward=not few, max_q_len=2 if few else 0), backward=not few)
