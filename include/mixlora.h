@@ -357,8 +357,8 @@ typedef struct {
   int32_t dtype;              /* MIXLORA_DTYPE_* */
   int32_t causal;             /* 0 or 1 */
   int32_t window;             /* 0: none */
-  float scale;                /* > 0 */
-  float softcap;              /* 0: none; scale / softcap has to be finite */
+  float scale;                /* > 0; scale * log2(e) has to be finite in fp32 */
+  float softcap;              /* 0: none; else scale / softcap and softcap * log2(e) have to be normal fp32 numbers */
   int64_t q_stride, k_stride, v_stride, o_stride;
 } mixlora_attention_shape_t;
 typedef struct {

@@ -68,7 +68,10 @@ mixlora_status_t check_attention(const mixlora_attention_shape_t* s) {
     return MIXLORA_ERR_INVALID_ARG;
   if (s->q_heads % s->kv_heads) return MIXLORA_ERR_INVALID_ARG;
   if (!isfinite(s->scale) || s->scale <= 0.f || !isfinite(s->softcap) || s->softcap < 0.f) return MIXLORA_ERR_INVALID_ARG;
-  if (s->softcap > 0.f && !isfinite(s->scale / s->softcap)) return MIXLORA_ERR_INVALID_ARG;
+  // the factors that the kernels form of them, in fp32: none may overflow, and a cap's may not lose bits below the normal
+  // range, since a large number multiplies what is left
+  if (!isfinite(s->scale * kLog2e)) return MIXLORA_ERR_INVALID_ARG;
+  if (s->softcap > 0.f && (!isnormal(s->scale / s->softcap) || !isnormal(s->softcap * kLog2e))) return MIXLORA_ERR_INVALID_ARG;
   const long long strides[] = {stride_of(s->q_stride, s->q_heads, s->head_dim), stride_of(s->k_stride, s->kv_heads, s->head_dim),
                                stride_of(s->v_stride, s->kv_heads, s->head_dim), stride_of(s->o_stride, s->q_heads, s->head_dim)};
   for (long long v : strides)
