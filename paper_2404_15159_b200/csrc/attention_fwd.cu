@@ -20,6 +20,7 @@ constexpr int kThreads = 384;                    // two softmax groups of 4 warp
 // their exponentials, take 208 and the third group keeps 88: (2 x 208 + 88) x 128 = 64512.
 constexpr int kLoadWarp = 8, kMmaWarp = 9;       // and 10: one for each query half
 constexpr int kTmemCols = 512;
+constexpr float kRaise = 0x1p16f, kRetake = 0x1p24f;         // sums of p that move the running maximum, see below
 template <int DP> constexpr int kStages = DP == 128 ? 5 : 8;
 template <int DP> constexpr uint32_t kTileBytes = kTile * DP * 2;
 template <int DP> constexpr uint32_t kSmemBytes = (2 + kStages<DP>) * kTileBytes<DP> + 320;
@@ -40,8 +41,10 @@ struct FwdParams {
 // sums of the unrounded values in fp32; O is divided by the sum of the rounded ones.
 //
 // The running maximum m stands for "large enough": p = 2^(s - m) is taken over the m of the tiles before, without
-// waiting for this tile's maximum.  A tile whose p sum up to more than 2^8 raises m for the next one, and only a row's
-// first keys, or p that sum up to more than 2^100 (fp32 and bf16 end at 2^127), are taken again over their own maximum.
+// waiting for this tile's maximum.  A tile whose p sum up to more than 2^16 raises m for the next one, and only a row's
+// first keys, or p of 64 keys that sum up to more than 2^24, are taken again over their own maximum.  Scores capped at up to
+// 2^96 either way (no distance term) start from m = 0 instead, unless a row's first p sum up to less than 2^-24.  So O stays
+// below 2^40 |v| (2^23 tiles of 2^16, one of 2^24) and a row's largest p above 2^-30, which leaves v from 2^-80 to 2^80.
 // m is a whole number in base 2, so that raising it rescales O and l exactly.
 //
 // A 128 x 128 tile costs 1024 cycles of the special-function unit (16 exponentials a cycle) and, at 128 values a head,
@@ -284,9 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       const float slope2 = BIAS ? a.slopes[w.head] * kLog2e : 0.f;
       // m in base 2; the sums of p as taken, for the log-sum-exp, and as rounded, by which O is divided: the weights that
       // the product uses then sum to one, and a row with one large weight keeps its value
-      // Scores capped at up to 2^96 either way need no maximum at all: 2^s stays inside the range of fp32 and bf16.
-      const bool bounded = CAP && !BIAS && cap2 <= 96.f;
-      float m = bounded ? 0.f : -INFINITY, l = 0.f, l_used = 0.f;
+      float m = CAP && !BIAS && cap2 <= 96.f ? 0.f : -INFINITY, l = 0.f, l_used = 0.f;
       float tile_sum = 0.f;                                    // the last tile's part of l
       int nth = 0;
       for (int it = 0; it < n && ok; ++it) {
@@ -296,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
         if (!ok) break;
         tc_fence_after();
         // S is there, so the products before it have finished and O stands still
-        if (!bounded && __any_sync(0xffffffffu, tile_sum > 256.f)) {       // the last tile's p had grown: m follows
-          const float k = tile_sum > 256.f ? ceilf(log2f(tile_sum)) : 0.f, f = ex2(-k);
+        if (__any_sync(0xffffffffu, tile_sum > kRaise)) {      // the last tile's p had grown: m follows
+          const float k = tile_sum > kRaise ? ceilf(log2f(tile_sum)) : 0.f, f = ex2(-k);
           m += k;
           l *= f;
           l_used *= f;
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
           }
           uint32_t pk[32];
           float sum, sum_used;
-          bool reset = m == -INFINITY;                         // nothing seen yet; below: p near the end of its range
+          bool reset = m == -INFINITY;                         // nothing seen yet; below: p far from one
 #pragma unroll 1
           for (int attempt = 0; attempt < 2; ++attempt) {      // over their own maximum p are at most about 1
             if (__any_sync(0xffffffffu, reset)) {
@@ -354,8 +355,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
 #pragma unroll
               for (int j = 4; j < 64; ++j) mx[j & 3] = fmaxf(mx[j & 3], x[j]);
               const float mt = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * to2);
-              const float m_new = reset ? fmaxf(mt, m) : m;
-              const float f = m == -INFINITY ? 0.f : ex2(m - m_new);
+              const float m_new = !reset ? m : l == 0.f ? mt : fmaxf(mt, m);
+              const float f = l == 0.f ? 0.f : ex2(m - m_new);     // where l is 0, O is
               m = m_new;
               l *= f;
               l_used *= f;
@@ -388,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             unpair2(add2(used[0], used[1]), l0, l1);
             sum_used = l0 + l1;
             tmem_st32(s_addr + c * 32, pk);                    // over scores of the tile's first half
-            reset = sum > 0x1p100f;
+            reset = sum > kRetake || (l == 0.f && sum > 0.f && sum < 1.f / kRetake);
             if (!__any_sync(0xffffffffu, reset)) break;
             tmem_st_wait();                                    // the next attempt writes the same columns
           }

@@ -83,3 +83,22 @@ def test_caps_far_above_the_scores(softcap, bf16, few):
     c = Case([2, 1, 2] if few else [60, 1, 130], k_lens=[700, 300, 130], k_len=[700, 256, 130], hq=4, hk=2, dim=128, seed=84,
              bf16=bf16, softcap=softcap, cap_rel=2.0 ** -20)
     c.check(c.run(backward=not few, max_q_len=2 if few else 0), backward=not few)
+
+
+@pytest.mark.parametrize("few", [True, False])
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("v_size", [2.0 ** 80, 1.0, 2.0 ** -80], ids=["2^80", "1", "2^-80"])
+@pytest.mark.parametrize("softcap,slopes", [(0.0, None), (0.0, [0.01, 0.0]), (60.0, None), (66.5, None), (67.0, None),
+                                            (100.0, None), (60.0, [0.01, 0.0])], ids=str)
+def test_small_and_large_values_under_rising_scores(softcap, slopes, v_size, bf16, few):
+    # first scores of about 0 (-90 with a distance term, or minus the cap), then, for rows that see them, some of +60 and one
+    # of +90: rows' weights jump by 2^86, or by 2^170 and more, and nothing of v may be lost on the way
+    c = Case([2] if few else [300], k_lens=[300], hq=2, hk=2, dim=64, seed=85, bf16=bf16, softcap=softcap, slopes=slopes,
+             causal=not few)
+    c.q[:, :, 0] = 16.0                               # times a key's 1: a score of 2
+    c.k[:, :, 0] = -200.0 if softcap else -45.0 if slopes else 0.0
+    c.k[100:110, :, 0], c.k[210, :, 0] = 30.0, 45.0
+    c.v *= v_size
+    got = c.run(backward=not few, max_q_len=2 if few else 0)
+    c.check(got, backward=not few)
+    assert (np.abs(got["o"]).max(axis=(1, 2)) > v_size / 64).all()
