@@ -274,8 +274,9 @@ int32_t mixlora_lora_linear_status(const void *workspace, void *stream);
  * are taken as rotary_dim / 2 pairs (u, w): value i with value i + rotary_dim / 2 (MIXLORA_ROPE_HALF), or value 2 i with
  * 2 i + 1 (MIXLORA_ROPE_INTERLEAVED).  Pair i of a token at position p is turned by the angle p * inv_freq[i]:
  *     u' = amplitude (u cos - w sin),  w' = amplitude (w cos + u sin);
- * values behind rotary_dim are copied.  Angles are reduced in 64 bits, so positions up to 2^31 - 1 (and negative ones)
- * keep fp32-exact sines.  mixlora_rope_backward applies the transpose (the same turn backwards) to the gradients.
+ * values behind rotary_dim are copied.  Angles are reduced in 64 bits with what their products round off, so sines and
+ * cosines are within 2^-22 at every position (as long as |p * inv_freq[i]| < 2^48).  mixlora_rope_backward applies the
+ * transpose (the same turn backwards) to the gradients.
  * q [tokens, q_heads, head_dim], k [tokens, k_heads, head_dim] and their outputs are device arrays of shape.dtype whose
  * tokens lie *_stride elements apart (0: dense), so q and k may be parts of one product's rows; an output is either its
  * input (same pointer and stride) or does not overlap it.  k_heads = 0 leaves k out (k, k_out ignored).
