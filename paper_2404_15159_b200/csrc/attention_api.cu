@@ -156,8 +156,9 @@ mixlora_status_t attention_args(const mixlora_attention_shape_t* s, const mixlor
   a->n_seqs = s->n_seqs; a->q_rows = s->q_rows; a->k_rows = s->k_rows;
   a->q_heads = s->q_heads; a->kv_heads = s->kv_heads; a->group = s->q_heads / s->kv_heads; a->head_dim = s->head_dim;
   a->causal = s->causal; a->max_q_len = s->max_q_len;
-  // distances stay below q_rows + k_rows: a window that wide hides nothing
-  a->window = (long long)s->window > (long long)s->q_rows + s->k_rows ? 0 : s->window;
+  // a row is at most lk - 1 behind and lq - 1 before a key: a window that wide hides nothing, and with those below 2^30 no
+  // position less a window leaves 32 bits
+  a->window = s->window >= s->q_rows && s->window >= s->k_rows ? 0 : s->window;
   a->scale = s->scale; a->softcap = s->softcap;
   return MIXLORA_OK;
 }

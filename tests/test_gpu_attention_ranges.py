@@ -102,3 +102,23 @@ def test_small_and_large_values_under_rising_scores(softcap, slopes, v_size, bf1
     got = c.run(backward=not few, max_q_len=2 if few else 0)
     c.check(got, backward=not few)
     assert (np.abs(got["o"]).max(axis=(1, 2)) > v_size / 64).all()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 30])
+def test_widest_window_over_the_most_rows(window):
+    # 2^30 rows stand up to 2^30 - 1 before their one key: position less window would leave 32 bits
+    import torch
+    from paper_2404_15159_b200 import binding as B
+    rows = 2 ** 30
+    x = torch.zeros(rows, 1, 8, dtype=torch.bfloat16, device="cuda")
+    x[0] = torch.arange(8, device="cuda")
+    o = torch.full_like(x, 100.0)
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    shape = B.make_attention_shape(1, rows, rows, 1, 1, 8, causal=0, window=window)
+    ws = B.alloc_attention_workspace(shape, False)
+    mask = B.make_attention_mask(off, off, k_len=torch.ones(1, dtype=torch.int32, device="cuda"))
+    B.mixlora_attention_forward(shape, mask, x, x, x, o, None, ws)
+    assert B.mixlora_device_status(ws) == 0
+    assert all(bool((part == x[0]).all()) for part in o.split(2 ** 27))
+    del x, o, ws
+    torch.cuda.empty_cache()
