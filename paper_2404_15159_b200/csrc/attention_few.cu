@@ -194,7 +194,13 @@ __device__ __forceinline__ void finish_block(const FewParams& p, const Share& w,
 // bf16.  A warp takes every kWarps-th group of 16 keys; K and V of the next groups travel through its own ring of
 // kStages stages in shared memory (16-byte pieces, XORed with the key so that the 8 rows of an ldmatrix fall into
 // different banks).  Keys behind the last one are never read: their rows are filled with zeros.
-template <int DP, bool CAP, bool BIAS>
+//
+// p goes into its product in bf16, and o is divided by the sum of the rounded p.  With at most 8 rows (TWO) rows 8 to 15 of
+// the product are empty and take what the rounding left of rows 0 to 7, again in bf16: p then keeps 16 bits, and both halves
+// of the result are added up at the end (64 sequences of up to 8192 keys, 4 rows: the same 213 us as with p rounded once,
+// the error against 64 bits 0.0024 -> 0.0017, which is the output's own rounding).  More rows would need a second product
+// (16 rows 231 -> 249 us, 32 rows 351 -> 418), so there a weight is rounded once, by half a step, 2^-8 of itself.
+template <int DP, bool CAP, bool BIAS, bool TWO>
 __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams p) {
   constexpr int C = DP / 8;                      // 16-byte pieces of a row
   constexpr int kStageBytes = 2 * kStep * DP * 2;
@@ -278,7 +284,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
     const int j0 = w.tiles.at(first + i * kWarps) * kStep;
     float mt[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
+    for (int hf = 0; hf < 2; ++hf) {
+      if (hf && TWO) break;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int j = j0 + (x >> 1) * 8 + 2 * t + (x & 1);
@@ -287,35 +294,38 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
         if (!keys[hf].sees(j)) v = -INFINITY;
         mt[hf] = fmaxf(mt[hf], v);
       }
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
       mt[hf] = fmaxf(mt[hf], __shfl_xor_sync(0xffffffffu, mt[hf], 1));
       mt[hf] = fmaxf(mt[hf], __shfl_xor_sync(0xffffffffu, mt[hf], 2));
     }
     // as in the tiled kernel, a row's maximum moves only where it has grown by more than 2^8
     const bool grown = (mt[0] > m[0] && mt[0] - m[0] > 8.f) || (mt[1] > m[1] && mt[1] - m[1] > 8.f);
     if (__any_sync(0xffffffffu, grown)) {
+      float f[2];
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         const float mn = fmaxf(m[hf], mt[hf]);
-        const float f = m[hf] == -INFINITY ? 0.f : ex2(m[hf] - mn);
+        f[hf] = m[hf] == -INFINITY ? 0.f : ex2(m[hf] - mn);
         m[hf] = mn;
-        l[hf] *= f;
-        used[hf] *= f;
+        l[hf] *= f[hf];
+        used[hf] *= f[hf];
+        if (hf && TWO) f[1] = f[0];
 #pragma unroll
-        for (int x = 0; x < DP / 8; ++x) { o[x][2 * hf] *= f; o[x][2 * hf + 1] *= f; }
+        for (int x = 0; x < DP / 8; ++x) { o[x][2 * hf] *= f[hf]; o[x][2 * hf + 1] *= f[hf]; }
       }
     }
     uint32_t pf[4];
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
+      if (hf && TWO) break;
       const float base = m[hf] == -INFINITY ? 0.f : m[hf];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const float e0 = ex2(s[u][2 * hf] - base), e1 = ex2(s[u][2 * hf + 1] - base);
         l[hf] += e0 + e1;
-        pf[hf + 2 * u] = bf16x2(e0, e1);
-        used[hf] += bf16_lo(pf[hf + 2 * u]) + bf16_hi(pf[hf + 2 * u]);
+        const uint32_t r = bf16x2(e0, e1);
+        pf[hf + 2 * u] = r;
+        if (TWO) pf[1 + 2 * u] = bf16x2(e0 - bf16_lo(r), e1 - bf16_hi(r));
+        else used[hf] += bf16_lo(r) + bf16_hi(r);
       }
     }
     {
@@ -338,6 +348,11 @@ __global__ void __launch_bounds__(kWarps * 32, 2) attn_few_bf16_kernel(FewParams
     l[hf] += __shfl_xor_sync(0xffffffffu, l[hf], 2);
     used[hf] += __shfl_xor_sync(0xffffffffu, used[hf], 1);
     used[hf] += __shfl_xor_sync(0xffffffffu, used[hf], 2);
+  }
+  if (TWO) {
+    used[0] = l[0];
+#pragma unroll
+    for (int x = 0; x < DP / 8; ++x) { o[x][0] += o[x][2]; o[x][1] += o[x][3]; }
   }
   __syncthreads();                               // the rings become the block's exchange
   float* st_m = reinterpret_cast<float*>(smem);
@@ -588,14 +603,14 @@ cudaError_t launch_blocks(K kernel, const FewParams& p, unsigned grid, size_t sm
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <int DP, bool CAP, bool BIAS>
+template <int DP, bool CAP, bool BIAS, bool TWO>
 cudaError_t launch_bf16(const FewParams& p, unsigned grid, cudaStream_t st) {
   constexpr size_t ring = (size_t)kWarps * kStages * 2 * kStep * DP * 2;
   constexpr size_t smem = ring > exchange_bytes(DP, kWarps) ? ring : exchange_bytes(DP, kWarps);
   static bool done[64];
-  cudaError_t e = allow_smem(attn_few_bf16_kernel<DP, CAP, BIAS>, (int)smem, done);
+  cudaError_t e = allow_smem(attn_few_bf16_kernel<DP, CAP, BIAS, TWO>, (int)smem, done);
   if (e != cudaSuccess) return e;
-  return launch_blocks(attn_few_bf16_kernel<DP, CAP, BIAS>, p, grid, smem, st);
+  return launch_blocks(attn_few_bf16_kernel<DP, CAP, BIAS, TWO>, p, grid, smem, st);
 }
 template <int LPK, int ROWS, bool CAP, bool BIAS>
 cudaError_t launch_f32(const FewParams& p, unsigned grid, cudaStream_t st) {
@@ -604,7 +619,9 @@ cudaError_t launch_f32(const FewParams& p, unsigned grid, cudaStream_t st) {
 template <bool CAP, bool BIAS>
 cudaError_t launch_mode(const FewParams& p, bool bf16_mode, unsigned grid, cudaStream_t st) {
   const bool narrow = p.a.head_dim <= 64;
-  if (bf16_mode) return narrow ? launch_bf16<64, CAP, BIAS>(p, grid, st) : launch_bf16<128, CAP, BIAS>(p, grid, st);
+  if (bf16_mode && p.rows <= 8)
+    return narrow ? launch_bf16<64, CAP, BIAS, true>(p, grid, st) : launch_bf16<128, CAP, BIAS, true>(p, grid, st);
+  if (bf16_mode) return narrow ? launch_bf16<64, CAP, BIAS, false>(p, grid, st) : launch_bf16<128, CAP, BIAS, false>(p, grid, st);
   // the rows are registers: as few as hold them
   if (p.rows <= 1) return narrow ? launch_f32<16, 1, CAP, BIAS>(p, grid, st) : launch_f32<32, 1, CAP, BIAS>(p, grid, st);
   if (p.rows <= 4) return narrow ? launch_f32<16, 4, CAP, BIAS>(p, grid, st) : launch_f32<32, 4, CAP, BIAS>(p, grid, st);

@@ -122,3 +122,20 @@ def test_widest_window_over_the_most_rows(window):
     assert all(bool((part == x[0]).all()) for part in o.split(2 ** 27))
     del x, o, ws
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("seqs,q_len,hq", [(1, 1, 2), (40, 1, 4), (3, 2, 8)])
+def test_few_rows_keep_weights_beyond_bf16(seqs, q_len, hq, bf16):
+    # Up to 8 rows a key head.  Values that come in pairs v, -v whose weights differ by a few per cent, so that o is a small
+    # part of sum p |v|: weights rounded once to bf16 would be off by 2^-8 of that sum.  They go in as two bf16 values, off by
+    # half a step of the second, 2^-16; the output's own rounding is 2^-8 of o itself.
+    from oracle import attention_oracle as orc
+    c = Case([q_len] * seqs, k_lens=[64] * seqs, hq=hq, hk=2, dim=16, seed=86, bf16=bf16, causal=False, amp=0.5)
+    c.k[1::2] = synth.round_to_bf16(c.k[0::2] + 0.03 * np.random.default_rng(5).standard_normal(c.k[0::2].shape))
+    c.v[1::2] = -c.v[0::2]
+    got = c.run(backward=False, max_q_len=q_len)
+    want = orc.attention(c.q, c.k, c.v, c.q_off, c.k_off, causal=False, p_step=2.0 ** -16, out_step=0.0)
+    bound = want["bound"]["o"] + (2.0 ** -8 if bf16 else 2.0 ** -24) * (np.abs(want["o"]) + want["bound"]["o"])
+    assert (np.abs(got["o"] - want["o"]) <= bound).all()
+    assert (np.abs(got["lse"] - want["lse"]) <= want["bound"]["lse"]).all()
