@@ -262,6 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
     const float mul = CAP ? a.scale / a.softcap : a.scale * kLog2e;
     const float cap2 = a.softcap * kLog2e;
     constexpr bool kTransformed = CAP || BIAS;               // else the factor goes into the exponent's multiply-add
+    constexpr bool kGuessed = CAP && !BIAS;                  // m may start from 0
     const float to2 = kTransformed ? 1.f : mul;
     bool ok = true;
     int cnt = 0;                                             // tiles of this half so far, over all row tiles
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
       const float slope2 = BIAS ? a.slopes[w.head] * kLog2e : 0.f;
       // m in base 2; the sums of p as taken, for the log-sum-exp, and as rounded, by which O is divided: the weights that
       // the product uses then sum to one, and a row with one large weight keeps its value
-      float m = CAP && !BIAS && cap2 <= 96.f ? 0.f : -INFINITY, l = 0.f, l_used = 0.f;
+      float m = kGuessed && cap2 <= 96.f ? 0.f : -INFINITY, l = 0.f, l_used = 0.f;
       float tile_sum = 0.f;                                    // the last tile's part of l
       int nth = 0;
       for (int it = 0; it < n && ok; ++it) {
@@ -355,8 +356,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
 #pragma unroll
               for (int j = 4; j < 64; ++j) mx[j & 3] = fmaxf(mx[j & 3], x[j]);
               const float mt = ceilf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * to2);
-              const float m_new = !reset ? m : l == 0.f ? mt : fmaxf(mt, m);
-              const float f = l == 0.f ? 0.f : ex2(m - m_new);     // where l is 0, O is
+              const bool none = kGuessed ? l == 0.f : m == -INFINITY;   // nothing seen before: l and O are zero
+              const float m_new = !reset ? m : kGuessed && none ? mt : fmaxf(mt, m);
+              const float f = none ? 0.f : ex2(m - m_new);
               m = m_new;
               l *= f;
               l_used *= f;
@@ -389,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_c
             unpair2(add2(used[0], used[1]), l0, l1);
             sum_used = l0 + l1;
             tmem_st32(s_addr + c * 32, pk);                    // over scores of the tile's first half
-            reset = sum > kRetake || (l == 0.f && sum > 0.f && sum < 1.f / kRetake);
+            reset = sum > kRetake || (kGuessed && l == 0.f && sum > 0.f && sum < 1.f / kRetake);
             if (!__any_sync(0xffffffffu, reset)) break;
             tmem_st_wait();                                    // the next attempt writes the same columns
           }
