@@ -327,8 +327,9 @@ mixlora_status_t mixlora_rope_backward(const mixlora_rope_shape_t *shape /* host
  * For query head h and its key head h / (q_heads / kv_heads):
  *     s_ij = scale q_i . k_j;   softcap > 0: s <- softcap tanh(s / softcap);   slopes: s <- s - slopes[h] |p_i - j|
  *     o_i = sum_j e^(s_ij - lse_i) v_j,   lse_i = ln sum_j e^(s_ij)         over the keys that row i sees.
- * Magnitudes of v between 2^-80 and 2^80 keep o's relative precision whatever the scores are; larger ones may overflow
- * where o itself does not, smaller ones may become zero.
+ * Scores are formed in fp32, so a weight is off by about 2^-22 of its row's largest |s|; where that is above 2^20 no
+ * result is promised.  Magnitudes of v between 2^-80 and 2^80 keep o's relative precision whatever the weights are; larger
+ * ones may overflow where o itself does not, smaller ones may become zero.
  * A row that sees nothing gets o = 0 and lse = -inf, and adds nothing to any gradient.  Rows outside every sequence
  * (behind the last one, behind k_len) are neither read into a result nor written, in outputs and gradients alike, and
  * may hold anything; an inf or NaN in a row that a sequence does use may reach every row of that sequence and head, also

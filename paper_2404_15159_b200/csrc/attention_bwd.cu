@@ -13,7 +13,7 @@
 //
 // A tile of dk / dv is 2048 cycles of the tensor pipe at 128 values a head and takes about 3100, one of dq 1536 and about
 // 2200: what is left over is the chain from a product to the elements and back.  Measured: 8192 rows in 4 documents, 32 / 8
-// heads of 128, causal: delta 32 us, dk and dv 290 us, dq 223 us in short bursts (0.9 PFLOP/s of the seven products).
+// heads of 128, causal: delta 32 us, dk and dv 304 us, dq 250 us (0.87 PFLOP/s of the seven products).
 #include <cuda.h>
 #include <string.h>
 

@@ -5,8 +5,9 @@
 // the keys in L2).  mma.sync and not tcgen05: a tile of 128 rows would hold 1 to 16, and the product takes a few per cent
 // of the time that the keys take to arrive.  The keys of a (sequence, key head) are split over several blocks where there
 // are few of those, which join their (m, l, sum p v) in index order.
-// Measured: 64 sequences in slots of 8192 keys, 32 / 8 heads of 128, 1.21 GB: 185 us (6.5 TB/s) and 5 us for the join; one
-// sequence of 1000 keys, 32 heads: 8 us; fp32, 7 sequences of 4 tokens and up to 2000 keys, 16 / 8 heads of 64: 18 us.
+// Measured: 64 sequences in slots of 8192 keys, 32 / 8 heads of 128, 1.21 GB: 184 us (6.6 TB/s) and 5 us for the join; one
+// sequence of 1000 keys, 32 heads: 8 us; fp32, 7 sequences of 4 tokens and up to 2000 keys, 16 / 8 heads of 64: 18 us, where
+// no load is under way while a step is computed.
 #include "attention.cuh"
 
 namespace mixlora {

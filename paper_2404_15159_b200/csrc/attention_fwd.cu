@@ -50,8 +50,8 @@ struct FwdParams {
 // A 128 x 128 tile costs 1024 cycles of the special-function unit (16 exponentials a cycle) and, at 128 values a head,
 // 1024 of the tensor pipe; a half's chain of waiting for S, reading it, exponentials, P, product and next S takes about
 // 3300, so the pipes are active for about half of the time each.  Measured: one sequence of 8192 rows, 32 heads of 128,
-// causal, 519 us (1.06 PFLOP/s) in short bursts and 600 us under the power cap (1.58 GHz); 24 documents in 5003 rows,
-// 32 / 8 heads of 64, capped, 58 us.
+// causal, 523 us (1.05 PFLOP/s) alone and 605 to 625 one after another, where the power cap takes the clock to 1.58 GHz; 24
+// documents in 5003 rows, 32 / 8 heads of 64, capped, 59 us.
 template <int DP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams p) {
   constexpr int NS = kStages<DP>;

@@ -60,7 +60,7 @@ __device__ __forceinline__ double rest_of_turns(double pos, double freq) {
 template <typename T, int N, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs p) {
   // items in flight per lane: fewer registers, so more warps, beat more loads per warp in bf16 (8192 tokens: 50 us with
-  // one, 53 with two, 64 with three); with half as many pairs to a lane fp32 has room for two (1021 tokens: 11 and 13 us)
+  // one, 53 with two, 64 with three); with half as many pairs to a lane fp32 has room for two (1021 tokens, which L2 holds: 11 and 13 us; 19 out of memory)
   constexpr int kUnroll = sizeof(T) == 2 ? 1 : 2;
   constexpr int kPairs = INTERLEAVED ? (N + 1) / 2 : N;
   const int lane = threadIdx.x & 31;
