@@ -382,6 +382,68 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
                                             const float *lse, const void *d_o, void *workspace, size_t workspace_bytes,
                                             void *d_q, void *d_k, void *d_v, void *stream);
 
+/* Losses at the end of a MixLoRA model: from the last hidden states (after the final norm) and the frozen output head to a
+ * loss and the gradient towards the hidden states, which mixlora_layer_backward of the last layer takes as dh (the paper
+ * trains with the language-model loss and prints no formula).  Logits are formed a tile at a time and never kept.
+ *     z_tv = cap(scale x_t . w_v) / temperature,   cap(y) = softcap tanh(y / softcap), or y where softcap = 0
+ *     lse_t = ln sum_v e^(z_tv),   p_tv = e^(z_tv - lse_t)
+ * mixlora_head_loss, with one label y_t a token:
+ *     loss_t = lse_t - z_ty + z_loss lse_t^2
+ * A token whose label is outside [0, vocab) (-1, -100, ...) is left out.
+ * mixlora_head_distill, with the logits u_tk that a teacher gave to teacher_top columns c_tk:
+ *     without teacher_lse   q_tk = e^(u_tk / temperature) / sum_k e^(u_tk / temperature)
+ *                           loss_t = sum_k q_tk (ln q_tk - ln p_tc) + z_loss lse_t^2
+ *     with teacher_lse [T] (ln of the sum of e^(u / temperature) over the teacher's whole vocabulary)
+ *                           q_tk = e^(u_tk / temperature - teacher_lse_t), and what they leave over, r_t = 1 - sum_k q_tk
+ *                           (0 where the sum is above 1 or every column is listed), counts as one more class:
+ *                           loss_t = sum_k q_tk (ln q_tk - ln p_tc) + r_t (ln r_t - ln(1 - sum_k p_tc)) + z_loss lse_t^2
+ * Entries whose column is outside [0, vocab) are dropped (a shorter list ends in -1), entries of the same column are added
+ * up, their order is free; a token without any entry (without teacher_lse: without any logit above -inf) is left out.
+ * Divergences carry no factor temperature^2; a caller that wants it puts it into the weights.
+ *
+ * Outputs: loss [T] and lse [T] (may be NULL), 0 for tokens that are left out; totals [2] (may be NULL) = {sum_t weight_t
+ * loss_t, sum_t weight_t} over the others, in an order that does not change; d_x [T, d] (NULL: loss only, about a third of
+ * the time) = the gradient of sum_t weight_t loss_t / normalizer, 0 for tokens that are left out.  weights [T] fp32 or NULL
+ * (all 1); `normalizer` is a device scalar, or NULL for this call's own sum of weights (data-parallel shards pass the sum
+ * over all shards); where it is 0 the gradient is 0.  w gets no gradient.
+ *
+ * x, d_x [T, d], w [vocab, d] of shape.dtype, 16-byte aligned, rows *_stride elements apart (0: dense); d_x must not
+ * overlap an input.  d_model and the strides are multiples of 8.  Tokens that are left out cost nothing in the products.
+ * Logits are sums in fp32.  Factors of the gradient's product are rounded once to shape.dtype (relatively, after all
+ * differences have been taken, so that a confident token's small gradient keeps its precision); where a row's listed
+ * columns hold more than 2^70 times the weight of all others, the others' part of the gradient may become zero.  Results
+ * do not depend on the order in which blocks run.
+ * An inf or NaN in a token's x makes its own loss and gradient NaN (and totals[0]), no other token's; one in w reaches every
+ * token.  Tokens that are left out may hold anything.
+ * The workspace (256-byte aligned, mixlora_head_workspace_bytes) is scratch of one call: whatever the batch, about 1.2 GB at
+ * most beside a few numbers a token and the teacher's entries; calls that may run at the same time need one each;
+ * mixlora_device_status works on it. */
+#define MIXLORA_MAX_TEACHER_TOP 256
+typedef struct {
+  uint32_t struct_size;       /* = sizeof(mixlora_head_shape_t) */
+  int32_t tokens;             /* T, up to 2^24 */
+  int32_t d_model;            /* up to 65536 */
+  int32_t vocab;              /* up to 2^20 */
+  int32_t teacher_top;        /* entries a token of mixlora_head_distill, up to MIXLORA_MAX_TEACHER_TOP; 0 for labels */
+  int32_t dtype;              /* MIXLORA_DTYPE_* */
+  float scale;                /* > 0 */
+  float softcap;              /* 0: none */
+  float temperature;          /* > 0 */
+  float z_loss;               /* >= 0 */
+  int32_t reserved;           /* 0 */
+  int64_t x_stride, w_stride, d_x_stride;
+} mixlora_head_shape_t;
+size_t mixlora_head_workspace_bytes(const mixlora_head_shape_t *shape /* host */, int with_gradient);
+mixlora_status_t mixlora_head_loss(const mixlora_head_shape_t *shape /* host */, const void *x, const void *w,
+                                   const int32_t *labels, const float *weights, const float *normalizer, float *loss,
+                                   float *lse, float *totals, void *d_x, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+mixlora_status_t mixlora_head_distill(const mixlora_head_shape_t *shape /* host */, const void *x, const void *w,
+                                      const int32_t *teacher_index, const float *teacher_logit,
+                                      const float *teacher_lse, const float *weights, const float *normalizer,
+                                      float *loss, float *lse, float *totals, void *d_x, void *workspace,
+                                      size_t workspace_bytes, void *stream);
+
 /* Device pointers into the workspace, for inspection after a forward call:
  * expert_idx [T, k] (descending logit), gates [T, k], perm [T*k] (slot id at each position
  * of the order "expert ascending, token ascending"), seg_off [N+1] (first position of each

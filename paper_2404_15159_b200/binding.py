@@ -29,7 +29,8 @@ EXPORTS = ("mixlora_limits", "mixlora_workspace_bytes", "mixlora_ffn_forward", "
            "mixlora_aux_stats", "mixlora_aux_loss_global", "mixlora_set_option", "mixlora_selftest_wait_timeout",
            "mixlora_dora_workspace_bytes", "mixlora_dora_ffn_forward", "mixlora_dora_ffn_backward",
            "mixlora_rope_frequencies", "mixlora_rope_forward", "mixlora_rope_backward",
-           "mixlora_attention_workspace_bytes", "mixlora_attention_forward", "mixlora_attention_backward")
+           "mixlora_attention_workspace_bytes", "mixlora_attention_forward", "mixlora_attention_backward",
+           "mixlora_head_workspace_bytes", "mixlora_head_loss", "mixlora_head_distill")
 
 MIXLORA_OPT_SERIAL = 0
 MIXLORA_OPT_TC_SINGLE = 1
@@ -41,6 +42,7 @@ MIXLORA_ROPE_SCALE_LINEAR = 1
 MIXLORA_ROPE_SCALE_NTK = 2
 MIXLORA_ROPE_SCALE_PARTS = 3
 MIXLORA_MAX_HEAD_DIM = 128
+MIXLORA_MAX_TEACHER_TOP = 256
 
 
 class mixlora_linear_shape_t(C.Structure):
@@ -89,6 +91,13 @@ class mixlora_attention_shape_t(C.Structure):
 
 class mixlora_attention_mask_t(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q_off", "k_off", "k_len", "prefix", "slopes")]
+
+
+class mixlora_head_shape_t(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("tokens", C.c_int32), ("d_model", C.c_int32), ("vocab", C.c_int32),
+                ("teacher_top", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("softcap", C.c_float),
+                ("temperature", C.c_float), ("z_loss", C.c_float), ("reserved", C.c_int32), ("x_stride", C.c_int64),
+                ("w_stride", C.c_int64), ("d_x_stride", C.c_int64)]
 
 
 class mixlora_limits_t(C.Structure):
@@ -197,6 +206,12 @@ def _load() -> C.CDLL:
     lib.mixlora_attention_backward.argtypes = ([C.POINTER(mixlora_attention_shape_t), C.POINTER(mixlora_attention_mask_t)] +
                                                [C.c_void_p] * 7 + [C.c_size_t] + [C.c_void_p] * 4)
     lib.mixlora_attention_backward.restype = C.c_int
+    lib.mixlora_head_workspace_bytes.argtypes = [C.POINTER(mixlora_head_shape_t), C.c_int]
+    lib.mixlora_head_workspace_bytes.restype = C.c_size_t
+    lib.mixlora_head_loss.argtypes = ([C.POINTER(mixlora_head_shape_t)] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p])
+    lib.mixlora_head_loss.restype = C.c_int
+    lib.mixlora_head_distill.argtypes = ([C.POINTER(mixlora_head_shape_t)] + [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p])
+    lib.mixlora_head_distill.restype = C.c_int
     lib.mixlora_status_string.argtypes = [C.c_int]
     lib.mixlora_status_string.restype = C.c_char_p
     return lib
@@ -536,3 +551,36 @@ def mixlora_attention_backward(shape, mask, q, k, v, o, lse, d_o, workspace, d_q
                                           _ptr(d_o), _ptr(workspace), workspace.numel() if workspace is not None else 0,
                                           _ptr(d_q), _ptr(d_k), _ptr(d_v), _stream(stream)),
            "mixlora_attention_backward")
+
+
+def make_head_shape(tokens, d_model, vocab, dtype=MIXLORA_DTYPE_BF16, teacher_top=0, scale=1.0, softcap=0.0,
+                    temperature=1.0, z_loss=0.0, x_stride=0, w_stride=0, d_x_stride=0) -> mixlora_head_shape_t:
+    """teacher_top: entries a token of mixlora_head_distill, 0 for mixlora_head_loss; strides in elements from row to row,
+    0 = dense."""
+    return mixlora_head_shape_t(C.sizeof(mixlora_head_shape_t), tokens, d_model, vocab, teacher_top, dtype, float(scale),
+                                float(softcap), float(temperature), float(z_loss), 0, x_stride, w_stride, d_x_stride)
+
+
+def alloc_head_workspace(shape, with_gradient: bool, device="cuda") -> torch.Tensor:
+    n = int(lib.mixlora_head_workspace_bytes(C.byref(shape), 1 if with_gradient else 0))
+    if n == 0:
+        raise MixLoraError(1, "mixlora_head_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def mixlora_head_loss(shape, x, w, labels, weights, normalizer, loss, lse, totals, d_x, workspace, stream=None) -> None:
+    """Cross entropy of the head's logits x w^T with int32 labels [T] (outside [0, vocab): left out), and its gradient d_x
+    (None: loss only).  weights [T], normalizer (device scalar), lse [T] and totals [2] may be None."""
+    _check(lib.mixlora_head_loss(C.byref(shape), _ptr(x), _ptr(w), _ptr(labels), _ptr(weights), _ptr(normalizer), _ptr(loss),
+                                 _ptr(lse), _ptr(totals), _ptr(d_x), _ptr(workspace),
+                                 workspace.numel() if workspace is not None else 0, _stream(stream)), "mixlora_head_loss")
+
+
+def mixlora_head_distill(shape, x, w, teacher_index, teacher_logit, teacher_lse, weights, normalizer, loss, lse, totals, d_x,
+                         workspace, stream=None) -> None:
+    """Divergence of the head's distribution from a teacher's top logits (int32 columns and fp32 logits [T, teacher_top],
+    teacher_lse [T] or None), and its gradient d_x (None: loss only)."""
+    _check(lib.mixlora_head_distill(C.byref(shape), _ptr(x), _ptr(w), _ptr(teacher_index), _ptr(teacher_logit),
+                                    _ptr(teacher_lse), _ptr(weights), _ptr(normalizer), _ptr(loss), _ptr(lse), _ptr(totals),
+                                    _ptr(d_x), _ptr(workspace), workspace.numel() if workspace is not None else 0,
+                                    _stream(stream)), "mixlora_head_distill")

@@ -1,0 +1,470 @@
+// What the head's losses do once a row: which rows count, a teacher's lists, and the join of a row's tiles.
+//
+// All of it is small beside the products (8192 rows of 32000 columns: TODO us of TODO), so what can lose bits by
+// cancellation is done in 64 bits: probabilities of a teacher, log-sum-exps, gradients towards listed columns.
+#include <math.h>
+
+#include "head.cuh"
+
+namespace mixlora {
+namespace {
+
+constexpr double kLn2d = 0.69314718055994530942, kLog2ed = 1.44269504088896340736;
+constexpr int kListThreads = 128;
+constexpr int kScanThreads = 1024, kScanEach = 8;
+constexpr int kRowThreads = 256;
+
+template <typename T> __device__ __forceinline__ T warp_sum(T v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return v;
+}
+__device__ __forceinline__ double warp_max(double v) {
+#pragma unroll
+  for (int d = 16; d; d >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, d));
+  return v;
+}
+
+// A teacher's entries of one token, a warp each: columns ascending, an entry outside the vocabulary dropped, entries of the
+// same column added up; their probabilities and what they leave over.  An entry's place is the number of entries before
+// it, counted by comparing it with all (at most 256 x 256 / 32 steps of a warp).
+__global__ void __launch_bounds__(kListThreads) head_lists_kernel(HeadArgs p) {
+  let_next_start();
+  extern __shared__ char smem[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x * (kListThreads / 32) + warp;
+  if (t >= p.tokens) return;
+  const int top = p.top, each = (top + 31) / 32;
+  double* prob = reinterpret_cast<double*>(smem) + (size_t)warp * 2 * top;      // by entry, then by place
+  int* col = reinterpret_cast<int*>(reinterpret_cast<double*>(smem) + (size_t)(kListThreads / 32) * 2 * top) + (size_t)warp * 2 * top;
+  const int32_t* index = p.t_index + (size_t)t * top;
+  const float* logit = p.t_logit + (size_t)t * top;
+  double most = -INFINITY;
+  for (int k = lane; k < top; k += 32) {
+    const int c = index[k];
+    const bool in = c >= 0 && c < p.vocab;
+    col[k] = in ? c : kHeadNone;
+    const double z = (double)logit[k] / (double)p.temperature;
+    prob[k] = z;
+    if (in) most = fmax(most, z);
+  }
+  most = warp_max(most);
+  const bool whole = p.t_lse != nullptr;
+  // without the teacher's sum a list of nothing but -inf says nothing; with it, it says that these are not chosen
+  const double from = whole ? (double)p.t_lse[t] : most;
+  __syncwarp();
+  for (int k = lane; k < top; k += 32) {
+    const int c = col[k];
+    int place = 0;
+    for (int j = 0; j < top; ++j) place += col[j] < c || (col[j] == c && j < k);
+    col[top + place] = c;
+    prob[top + place] = c == kHeadNone || (most == -INFINITY && !isnan(prob[k])) ? 0.0 : exp(prob[k] - from);
+  }
+  __syncwarp();
+  // first entries of their column, in order: 32 places at a time
+  double sum = 0.0;
+  int n = 0;
+  for (int i = 0; i < each; ++i) {
+    const int k = i * 32 + lane;
+    const int c = k < top ? col[top + k] : kHeadNone;
+    const bool lead = c != kHeadNone && (k == 0 || col[top + k - 1] != c);
+    double q = 0.0;
+    if (lead)
+      for (int j = k; j < top && col[top + j] == c; ++j) q += prob[top + j];
+    const unsigned leads = __ballot_sync(0xffffffffu, lead);
+    const int at = n + __popc(leads & ((1u << lane) - 1u));
+    if (lead) {
+      col[at] = c;              // at <= k: that place has been read, col[.. top) is free since the sort
+      prob[at] = q;
+    }
+    sum += lead ? q : 0.0;
+    n += __popc(leads);
+  }
+  sum = warp_sum(sum);
+  __syncwarp();
+  if (!whole && sum == 0.0) n = 0;
+  for (int k = lane; k < top; k += 32) {
+    p.list_out[(size_t)t * top + k] = k < n ? col[k] : kHeadNone;
+    p.list_q[(size_t)t * top + k] = k < n ? (whole ? prob[k] : prob[k] / sum) : 0.0;
+  }
+  if (lane == 0) {
+    p.list_n[t] = n;
+    // a list of every column leaves nothing over, whatever its sum was rounded to; a sum that is no number says so
+    p.rest_q[t] = whole && n < p.vocab ? (sum >= 1.0 ? 0.0 : 1.0 - sum) : 0.0;
+  }
+}
+
+// Numbers the counted rows and adds up their weights: one block, 8192 tokens a turn.  Rows that are left out get their
+// zeroes here, and the counters of the call are cleared.
+__global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
+  let_next_start();
+  wait_for_last();
+  __shared__ int warp_n[32];
+  __shared__ double warp_w[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int i = threadIdx.x; i < kHeadCounters; i += kScanThreads) p.counters[i] = 0;
+  int base = 0;
+  double weight = 0.0;
+  for (int t0 = 0; t0 < p.tokens; t0 += kScanThreads * kScanEach) {
+    const int first = t0 + threadIdx.x * kScanEach;
+    unsigned in = 0;
+#pragma unroll
+    for (int j = 0; j < kScanEach; ++j) {
+      const int t = first + j;
+      if (t >= p.tokens) break;
+      const bool ok = p.labels ? p.labels[t] >= 0 && p.labels[t] < p.vocab : p.list_n[t] > 0;
+      in |= (unsigned)ok << j;
+      if (ok) {
+        weight += p.weights ? (double)p.weights[t] : 1.0;
+      } else {
+        p.loss[t] = 0.f;
+        if (p.lse) p.lse[t] = 0.f;
+      }
+    }
+    const int n = __popc(in);
+    int upto = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += up;
+    }
+    if (lane == 31) warp_n[warp] = upto;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int i = 0; i < kScanThreads / 32; ++i) {
+      if (i < warp) before += warp_n[i];
+      all += warp_n[i];
+    }
+    int row = base + before + upto - n;
+#pragma unroll
+    for (int j = 0; j < kScanEach; ++j) {
+      const int t = first + j;
+      if (t >= p.tokens) break;
+      const bool ok = in >> j & 1;
+      p.token_row[t] = ok ? row : -1;
+      if (ok) p.row_token[row++] = t;
+    }
+    base += all;
+    __syncthreads();
+  }
+  weight = warp_sum(weight);
+  if (lane == 0) warp_w[warp] = weight;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double sum = 0.0;
+    for (int i = 0; i < kScanThreads / 32; ++i) sum += warp_w[i];
+    const double norm = p.normalizer ? (double)p.normalizer[0] : sum;
+    p.state->status = 0;
+    p.state->counted = base;
+    p.state->joined = 0;
+    p.state->weight = (float)sum;
+    p.state->each = norm == 0.0 ? 0.f : (float)(1.0 / norm);
+  }
+}
+
+// Where tokens are left out: the counted rows of this piece side by side (the products then pass over nothing else), and
+// zeroes for the gradients of the others.  A warp a token.
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) head_gather_kernel(HeadArgs p, int zeroes) {
+  let_next_start();
+  wait_for_last();
+  if (p.state->counted == p.tokens) return;
+  const int lane = threadIdx.x & 31;
+  const int t = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  if (t >= p.tokens) return;
+  const int row = p.token_row[t] - p.piece0;
+  const bool left_out = row + p.piece0 < 0;
+  if (left_out ? !(zeroes && p.d_x) : (row < 0 || row >= p.piece || !p.x_rows)) return;
+  constexpr int kEach = 16 / sizeof(T);
+  const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.x) + (size_t)t * p.x_stride);
+  uint4* dst = left_out ? reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.d_x) + (size_t)t * p.dx_stride)
+                        : reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.x_rows) + (size_t)row * p.d);
+  for (int i = lane; i < p.d / kEach; i += 32) dst[i] = left_out ? make_uint4(0, 0, 0, 0) : src[i];
+}
+
+// One row's loss and, with a gradient, what its columns need, by one warp.  lr: log-sum-exp of the columns that are not
+// listed; r_others: their R (-inf where there is none).  `z` holds the listed logits and gets the places' values G_k / A.
+struct RowResult { double r, weighted; float scale; };
+__device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, int n, double lr, double r_others, float* z) {
+  const int lane = threadIdx.x & 31;
+  const double* q = p.labels ? nullptr : p.list_q + (size_t)token * p.top;
+  const double rest = p.labels ? 0.0 : p.rest_q[token];
+  double most = -INFINITY;
+  for (int k = lane; k < n; k += 32) most = fmax(most, (double)z[k]);
+  most = warp_max(most);
+  const double from = fmax(most, lr);
+  double sum = 0.0;
+  for (int k = lane; k < n; k += 32) sum += exp((double)z[k] - from);
+  sum = warp_sum(sum);
+  const double lse = from + log(sum + exp(lr - from));
+  double loss = 0.0;
+  for (int k = lane; k < n; k += 32) {
+    const double zk = (double)z[k];
+    if (!q) {
+      const double gap = lr - zk;
+      loss = fmax(gap, 0.0) + log1p(exp(-fabs(gap)));
+    } else if (!(q[k] == 0.0)) {
+      loss += q[k] * (log(q[k]) - (zk - lse));
+    }
+  }
+  loss = warp_sum(loss);
+  if (!(rest == 0.0)) loss += rest * (log(rest) - (lr - lse));
+  loss += (double)p.z_loss * lse * lse;
+  // what the target sums up to: 1 but where a teacher's entries exceed it, or name every column and stay below
+  double mass = 1.0;
+  if (q) {
+    mass = 0.0;
+    for (int k = lane; k < n; k += 32) mass += q[k];
+    mass = warp_sum(mass) + rest;
+  }
+  const double curl = 2.0 * (double)p.z_loss * lse, share = mass + curl;
+  const double weight = p.weights ? (double)p.weights[token] : 1.0;
+  if (lane == 0) {
+    p.loss[token] = (float)loss;
+    if (p.lse) p.lse[token] = (float)lse;
+  }
+  RowResult out{0.0, weight * (double)(float)loss, 0.f};
+  if (!p.d_x) return out;
+  const double r = fmax(r_others, 100.0 * rint(most * kLog2ed / 100.0));
+  const double u = exp(r * kLn2d - lse), s = exp(lr - r * kLn2d);
+  const double part = rest > 0.0 && s > 0x1p-100 ? rest / s : 0.0;
+  double a = share * u - part;
+  // nothing below what the 32-bit sums behind u and s can tell from zero, so that G_k / A stays in range
+  const double least = 0x1p-30 * fmax(u, part);
+  if (fabs(a) < least) a = a < 0.0 ? -least : least;
+  for (int k = lane; k < n; k += 32) {
+    const double zk = (double)z[k], pk = exp(zk - lse);
+    double g = q ? share * pk - q[k] : curl * pk - 1.0 / (1.0 + exp(zk - lr));
+    if (p.softcap > 0.f) {
+      const double tk = zk * (double)p.temperature / (double)p.softcap;
+      g *= (1.0 - tk) * (1.0 + tk);
+    }
+    z[k] = (float)(g / a);
+  }
+  out.r = r;
+  out.scale = (float)(a * ((double)p.scale / (double)p.temperature) * weight * (double)p.state->each);
+  return out;
+}
+
+// Sum of every block's weighted losses, by the block that comes last, in the blocks' order.
+__device__ __forceinline__ void add_totals(const HeadArgs& p, int block, double mine, double* warp_w) {
+  __shared__ int last;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    p.loss_part[block] = mine;
+    __threadfence();
+    last = atomicAdd(&p.state->joined, 1) == p.join_blocks - 1;
+  }
+  __syncthreads();
+  if (!last || !p.totals) return;
+  __threadfence();
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < p.join_blocks; i += kRowThreads) sum += __ldcg(p.loss_part + i);
+  sum = warp_sum(sum);
+  if (lane == 0) warp_w[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0.0;
+    for (int i = 0; i < kRowThreads / 32; ++i) sum += warp_w[i];
+    p.totals[0] = (float)sum;
+    p.totals[1] = p.state->weight;
+  }
+}
+
+// Joins a row's tiles: 32 rows a block, first a row per lane and an eighth of the tiles per warp, then a warp per row.
+__global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
+  constexpr int kWarps = kRowThreads / 32, kRows = kHeadRowsPerBlock;
+  let_next_start();
+  wait_for_last();
+  __shared__ float r_of[kWarps][kRows], s_of[kWarps][kRows], r_row[kRows];
+  __shared__ double warp_w[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row0 = blockIdx.x * kRows, rows = head_rows_here(p) - row0;
+  double weighted = 0.0;
+  if (rows > 0) {
+    const float2* stats = p.stats + row0;
+    float r = -INFINITY, s = 0.f;
+    if (lane < rows) {
+      for (int i = warp; i < p.col_tiles; i += kWarps) {
+        const float2 v = stats[(size_t)i * p.piece + lane];
+        if (v.y == 0.f) continue;
+        if (v.x > r) { s = s * exp2f(r - v.x) + v.y; r = v.x; }
+        else s += v.y * exp2f(v.x - r);
+      }
+    }
+    r_of[warp][lane] = r;
+    s_of[warp][lane] = s;
+    __syncthreads();
+    for (int i = warp; i < min(rows, kRows); i += kWarps) {
+      const int token = p.row_token[p.piece0 + row0 + i];
+      float ro = -INFINITY, so = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float rv = r_of[w][i], sv = s_of[w][i];
+        if (sv == 0.f) continue;
+        if (rv > ro) { so = so * exp2f(ro - rv) + sv; ro = rv; }
+        else so += sv * exp2f(rv - ro);
+      }
+      const double lr = so == 0.f ? -INFINITY : (double)ro * kLn2d + log((double)so);
+      const RowResult res = finish_row(p, token, p.labels ? 1 : p.list_n[token], lr, (double)ro,
+                                       p.z_listed + (size_t)(row0 + i) * p.top);
+      if (lane == 0) {
+        weighted += res.weighted;
+        r_row[i] = (float)res.r;
+        if (p.d_x) p.row_scale[row0 + i] = res.scale;
+      }
+    }
+    if (p.d_x) {
+      __syncthreads();
+      bf16* e = reinterpret_cast<bf16*>(p.e) + (size_t)row0 * p.pitch;
+      for (int i = warp; i < p.col_tiles; i += kWarps) {
+        float by = 0.f;
+        if (lane < rows) {
+          const float2 v = stats[(size_t)i * p.piece + lane];
+          by = v.y == 0.f ? 0.f : v.x - r_row[lane];
+        }
+        unsigned todo = __ballot_sync(0xffffffffu, by < 0.f);
+        while (todo) {
+          const int l = __ffs(todo) - 1;
+          todo &= todo - 1;
+          const float f = exp2f(__shfl_sync(0xffffffffu, by, l));
+          const int c = i * kHeadTile + lane * 8;
+          if (c >= p.pitch) continue;
+          uint4* at = reinterpret_cast<uint4*>(e + (size_t)l * p.pitch + c);
+          uint4 v = *at;
+          __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 w = __bfloat1622float2(h[j]);
+            h[j] = __floats2bfloat162_rn(w.x * f, w.y * f);
+          }
+          *at = v;
+        }
+        __syncwarp();
+      }
+      __syncthreads();
+      for (int i = warp; i < min(rows, kRows); i += kWarps) {
+        const int token = p.row_token[p.piece0 + row0 + i];
+        const int n = p.labels ? 1 : p.list_n[token];
+        for (int k = lane; k < n; k += 32)
+          e[(size_t)i * p.pitch + p.list[(size_t)token * p.top + k]] =
+              __float2bfloat16(p.z_listed[(size_t)(row0 + i) * p.top + k]);
+      }
+    }
+  }
+  if (lane == 0) warp_w[warp] = weighted;
+  __syncthreads();
+  double mine = 0.0;
+  if (threadIdx.x == 0)
+    for (int i = 0; i < kWarps; ++i) mine += warp_w[i];
+  __syncthreads();
+  add_totals(p, p.piece0 / kRows + blockIdx.x, mine, warp_w);
+}
+
+// The fp32 mode's rows: a block a row, whose logits (x . w, as the product left them) become the gradient's factors.
+__global__ void __launch_bounds__(kRowThreads) head_join_f32_kernel(HeadArgs p) {
+  constexpr int kWarps = kRowThreads / 32;
+  let_next_start();
+  wait_for_last();
+  __shared__ float warp_m[kWarps];
+  __shared__ double warp_w[kWarps], row_r;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x;
+  double weighted = 0.0;
+  if (row < head_rows_here(p)) {
+    float* e = reinterpret_cast<float*>(p.e) + (size_t)row * p.pitch;
+    float* z = p.z_listed + (size_t)row * p.top;
+    const int token = p.row_token[p.piece0 + row];
+    const int n = p.labels ? 1 : p.list_n[token];
+    const int32_t* list = p.list + (size_t)token * p.top;
+    // the listed logits leave the row
+    if (warp == 0) {
+      for (int k = lane; k < n; k += 32) {
+        const float raw = e[list[k]] * p.logit_factor;
+        z[k] = p.softcap > 0.f ? tanhf(raw) * p.cap_out : raw;
+        e[list[k]] = -INFINITY;
+      }
+    }
+    __syncthreads();
+    float m = -INFINITY;
+    for (int c = threadIdx.x; c < p.vocab; c += kRowThreads) m = fmaxf(m, e[c]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    if (lane == 0) warp_m[warp] = m;
+    __syncthreads();
+    m = warp_m[0];
+    for (int i = 1; i < kWarps; ++i) m = fmaxf(m, warp_m[i]);
+    m *= p.logit_factor;
+    if (p.softcap > 0.f) m = tanhf(m) * p.cap_out;
+    if (m == -INFINITY) m = 0.f;
+    double sum = 0.0;
+    for (int c = threadIdx.x; c < p.vocab; c += kRowThreads) {
+      float v = e[c] * p.logit_factor, slope = 1.f;
+      const bool gone = e[c] == -INFINITY;
+      if (p.softcap > 0.f) {
+        const float t = tanhf(v);
+        v = t * p.cap_out;
+        slope = (1.f - t) * (1.f + t);
+      }
+      const float ex = gone ? 0.f : expf(v - m);
+      sum += (double)ex;
+      if (p.d_x) e[c] = ex * slope;
+    }
+    sum = warp_sum(sum);
+    if (lane == 0) warp_w[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+      sum = 0.0;
+      for (int i = 0; i < kWarps; ++i) sum += warp_w[i];
+      // R of the others is their largest logit here (no tiles have to agree on one), as a power of two
+      const double lr = sum == 0.0 ? -INFINITY : (double)m + log(sum);
+      const RowResult res = finish_row(p, token, n, lr, sum == 0.0 ? -INFINITY : (double)m * kLog2ed, z);
+      if (lane == 0) {
+        weighted = res.weighted;
+        row_r = res.r;
+        if (p.d_x) p.row_scale[row] = res.scale;
+      }
+    }
+    __syncthreads();
+    if (p.d_x) {
+      // e is over e^m, the row over 2^R
+      const double by = (double)m * kLog2ed - row_r;
+      if (by < 0.0) {
+        const float f = (float)exp2(by);
+        for (int c = threadIdx.x; c < p.vocab; c += kRowThreads) e[c] *= f;
+      }
+      __syncthreads();
+      if (warp == 0)
+        for (int k = lane; k < n; k += 32) e[list[k]] = z[k];
+    }
+  }
+  __syncthreads();
+  add_totals(p, p.piece0 + blockIdx.x, weighted, warp_w);
+}
+
+}  // namespace
+
+cudaError_t launch_head_lists(const HeadArgs& p, cudaStream_t st) {
+  constexpr int kWarps = kListThreads / 32;
+  const size_t smem = (size_t)kWarps * 2 * p.top * (sizeof(double) + sizeof(int));   // 24 KB at 256 entries
+  head_lists_kernel<<<(p.tokens + kWarps - 1) / kWarps, kListThreads, smem, st>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st) {
+  if (!first) return launch_behind(head_scan_kernel, 1, kScanThreads, 0, st, p);
+  head_scan_kernel<<<1, kScanThreads, 0, st>>>(p);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_head_gather(const HeadArgs& p, bool bf16_mode, bool first_piece, cudaStream_t st) {
+  const unsigned blocks = (unsigned)((p.tokens + kRowThreads / 32 - 1) / (kRowThreads / 32));
+  return bf16_mode ? launch_behind(head_gather_kernel<bf16>, blocks, kRowThreads, 0, st, p, first_piece ? 1 : 0)
+                   : launch_behind(head_gather_kernel<float>, blocks, kRowThreads, 0, st, p, first_piece ? 1 : 0);
+}
+
+cudaError_t launch_head_join(const HeadArgs& p, bool bf16_mode, cudaStream_t st) {
+  if (!bf16_mode) return launch_behind(head_join_f32_kernel, (unsigned)p.piece, kRowThreads, 0, st, p);
+  return launch_behind(head_join_kernel, (unsigned)((p.piece + kHeadRowsPerBlock - 1) / kHeadRowsPerBlock), kRowThreads, 0, st, p);
+}
+
+}  // namespace mixlora
