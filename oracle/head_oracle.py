@@ -48,7 +48,7 @@ def label_rows(labels, vocab):
 def head(x, w, target, named, rest, counted, scale=1.0, softcap=0.0, temperature=1.0, z_loss=0.0, weights=None,
          normalizer=None, p_step=0.0, out_step=2.0 ** -24, gradient=True):
     """Outputs, and in `bound` how far off a kernel may be that sums logits in fp32 and rounds the factors of the gradient's
-    product relatively by `p_step` and d_x by `out_step`.
+    product relatively by `p_step` (those that are not listed up to twice) and d_x by `out_step`.
 
     A logit is a sum of d products, each addition off by at most 2^-23 (nearest or truncated) of what is summed, and a few
     roundings; a cap adds 2^-21 of the logit (tanh) and passes the rest on.  `far` is a row's largest such error.  A
@@ -114,7 +114,8 @@ def head(x, w, target, named, rest, counted, scale=1.0, softcap=0.0, temperature
         g_err = torch.where(one_hot[:, None] & named, tight, g_err)
         g_err = g_err * (slope + slope_err) + g.abs() * slope_err
         g = g * slope
-        g_err = g_err + p_step * (g.abs() + g_err) + 2.0 ** -60 * p.max(1, keepdim=True).values + TINY
+        # a column that is not listed is rounded itself, and its row's factor may be moved by as much again
+        g_err = g_err + torch.where(named, p_step, 2 * p_step + p_step ** 2) * (g.abs() + g_err) + 2.0 ** -60 * p.max(1, keepdim=True).values + TINY
         d_x = each[:, None] * (g @ w)
         size = g.abs() @ w.abs()
         b = each.abs()[:, None] * (g_err @ w.abs() + (v + 32) * 2.0 ** -23 * (size + g_err @ w.abs()))

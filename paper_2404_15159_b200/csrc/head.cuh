@@ -1,9 +1,9 @@
 // Shared parts of the losses on the output head: arguments, and how a row's exponentials are held.
 //
-// Logits z_v = (capped) scale x . w_v / temperature of a row are formed 256 columns at a time and turned into
+// Logits z_v = (capped) scale x . w_v / temperature of a row are formed 128 columns at a time and turned into
 // exponentials at once.  A row's `listed` columns (its label, or the teacher's entries) are left out of them and kept as
 // fp32 logits: a sum or a difference that a confident row makes small is then never taken of nearly equal numbers.
-//   tile of 256 columns   R = 100 rint(log2(e) max z / 100) over its columns that are not listed, S = sum 2^(z log2(e) - R)
+//   128 columns           R = 100 rint(log2(e) max z / 100) over its columns that are not listed, S = sum 2^(z log2(e) - R)
 //   gradient              E_v = 2^(z_v log2(e) - R) (1 - (z_v temperature / softcap)^2), one rounding to bf16
 // R is a multiple of 100, so tiles of a row nearly always share it, and where they do not (logits 35 apart or more) the
 // row is brought to the largest one by powers of two, which round nothing.  With the row's R and
@@ -17,7 +17,8 @@
 
 namespace mixlora {
 
-constexpr int kHeadTile = 256;               // rows and columns of a tile
+constexpr int kHeadTile = 256;               // rows and columns of a tile of the products
+constexpr int kHeadCols = 128;               // columns that share R and S
 constexpr float kHeadStep = 100.f;           // R's step, in powers of two
 constexpr int kHeadNone = 0x7fffffff;        // no column (ends a row's list)
 constexpr int kHeadMaxShares = 16;           // CTA pairs that share one tile's reduction
@@ -60,7 +61,7 @@ struct HeadArgs {
   double* loss_part;              // sum of weight * loss for each block of the joining kernel
   void* x_rows;                   // [piece, d] the counted rows of x, where some tokens are left out
   float* z_listed;                // [piece, top] logits of the listed columns
-  float2* stats;                  // [column tiles, piece] (R, S)
+  float2* stats;                  // [col_tiles, piece] (R, S)
   void* e;                        // [piece, pitch]
   float* row_scale;               // [piece]
   float* part;                    // partial tiles of a split reduction

@@ -43,11 +43,11 @@ mixlora_status_t check_head(const mixlora_head_shape_t* s) {
 }
 
 // Counted rows are worked on in pieces, as many as keep a piece's exponentials (fp32 mode: logits) within 512 MiB: enough
-// for whole rounds of tiles, and the same whatever the batch.  Without a gradient bf16 keeps two numbers for 256 columns,
+// for whole rounds of tiles, and the same whatever the batch.  Without a gradient bf16 keeps two numbers for 128 columns,
 // and the copy of the rows of x is what counts.
 int piece_rows(const mixlora_head_shape_t& s, bool gradient) {
   const bool bf16_mode = s.dtype == MIXLORA_DTYPE_BF16;
-  long long row = bf16_mode ? (gradient ? (long long)s.vocab * 2 : (long long)((s.vocab + kHeadTile - 1) / kHeadTile) * 8)
+  long long row = bf16_mode ? (gradient ? (long long)s.vocab * 2 : (long long)((s.vocab + kHeadCols - 1) / kHeadCols) * 8)
                             : (long long)s.vocab * 4;
   if (bf16_mode && row < 2LL * s.d_model) row = 2LL * s.d_model;
   long long rows = (512LL << 20) / row / kHeadTile * kHeadTile;
@@ -68,7 +68,7 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   L.piece = piece_rows(s, gradient);
   L.pieces = (s.tokens + L.piece - 1) / L.piece;
   L.pitch = (s.vocab + 7) / 8 * 8;
-  L.col_tiles = (s.vocab + kHeadTile - 1) / kHeadTile;
+  L.col_tiles = (s.vocab + kHeadCols - 1) / kHeadCols;
   const int per_block = bf16_mode ? kHeadRowsPerBlock : 1;
   L.join_blocks = L.pieces * (L.piece / per_block);
   size_t off = 0;

@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kRowThreads) head_gather_kernel(HeadArgs p, in
 // One row's loss and, with a gradient, what its columns need, by one warp.  lr: log-sum-exp of the columns that are not
 // listed; r_others: their R (-inf where there is none).  `z` holds the listed logits and gets the places' values G_k / A.
 struct RowResult { double r, weighted; float scale; };
-__device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, int n, double lr, double r_others, float* z) {
+__device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, int n, double lr, double r_others, float* z, bool rounds) {
   const int lane = threadIdx.x & 31;
   const double* q = p.labels ? nullptr : p.list_q + (size_t)token * p.top;
   const double rest = p.labels ? 0.0 : p.rest_q[token];
@@ -232,6 +232,7 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
   // nothing below what the 32-bit sums behind u and s can tell from zero, so that G_k / A stays in range
   const double least = 0x1p-30 * fmax(u, part);
   if (fabs(a) < least) a = a < 0.0 ? -least : least;
+  double largest = 0.0;
   for (int k = lane; k < n; k += 32) {
     const double zk = (double)z[k], pk = exp(zk - lse);
     double g = q ? share * pk - q[k] : curl * pk - 1.0 / (1.0 + exp(zk - lr));
@@ -239,8 +240,21 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
       const double tk = zk * (double)p.temperature / (double)p.softcap;
       g *= (1.0 - tk) * (1.0 + tk);
     }
-    z[k] = (float)(g / a);
+    z[k] = (float)g;
+    if (fabs(g) > fabs(largest)) largest = (double)(float)g;
   }
+  if (rounds) {
+    // the largest listed factor, most of the gradient where the others' are spread out, is made one that rounding keeps: A
+    // takes up the difference
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+      const double other = __shfl_xor_sync(0xffffffffu, largest, d);
+      if (fabs(other) > fabs(largest) || (fabs(other) == fabs(largest) && other > largest)) largest = other;
+    }
+    const double near = (double)__bfloat162float(__float2bfloat16((float)(largest / a)));
+    if (fabs(near) > 0x1p-100 && fabs(near) < 0x1p120) a = largest / near;
+  }
+  for (int k = lane; k < n; k += 32) z[k] = (float)((double)z[k] / a);
   out.r = r;
   out.scale = (float)(a * ((double)p.scale / (double)p.temperature) * weight * (double)p.state->each);
   return out;
@@ -307,7 +321,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
       }
       const double lr = so == 0.f ? -INFINITY : (double)ro * kLn2d + log((double)so);
       const RowResult res = finish_row(p, token, p.labels ? 1 : p.list_n[token], lr, (double)ro,
-                                       p.z_listed + (size_t)(row0 + i) * p.top);
+                                       p.z_listed + (size_t)(row0 + i) * p.top, true);
       if (lane == 0) {
         weighted += res.weighted;
         r_row[i] = (float)res.r;
@@ -328,13 +342,13 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
           const int l = __ffs(todo) - 1;
           todo &= todo - 1;
           const float f = exp2f(__shfl_sync(0xffffffffu, by, l));
-          const int c = i * kHeadTile + lane * 8;
+          const int c = i * kHeadCols + lane * 4;
           if (c >= p.pitch) continue;
-          uint4* at = reinterpret_cast<uint4*>(e + (size_t)l * p.pitch + c);
-          uint4 v = *at;
+          uint2* at = reinterpret_cast<uint2*>(e + (size_t)l * p.pitch + c);
+          uint2 v = *at;
           __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 2; ++j) {
             const float2 w = __bfloat1622float2(h[j]);
             h[j] = __floats2bfloat162_rn(w.x * f, w.y * f);
           }
@@ -417,7 +431,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_f32_kernel(HeadArgs p) 
       for (int i = 0; i < kWarps; ++i) sum += warp_w[i];
       // R of the others is their largest logit here (no tiles have to agree on one), as a power of two
       const double lr = sum == 0.0 ? -INFINITY : (double)m + log(sum);
-      const RowResult res = finish_row(p, token, n, lr, sum == 0.0 ? -INFINITY : (double)m * kLog2ed, z);
+      const RowResult res = finish_row(p, token, n, lr, sum == 0.0 ? -INFINITY : (double)m * kLog2ed, z, false);
       if (lane == 0) {
         weighted = res.weighted;
         row_r = res.r;

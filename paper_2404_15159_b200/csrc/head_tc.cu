@@ -4,8 +4,8 @@
 //   grad     E [rows, vocab] . w [vocab, d]  times the row's A scale / temperature weight / normalizer, to the row's token
 //
 // Pairs of CTAs work on 256 x 256 tiles (cta_group::2, 128 rows of the accumulator and half of B's columns each), one
-// persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the products, warps 2 to 5 turn the finished
-// accumulator into its result while the other one is filled.  The number of rows is read on the device: tokens without a
+// persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the products, the other warps turn a finished
+// accumulator into its result while the second one is filled.  The number of rows is read on the device: tokens without a
 // label take no part.
 #include <cuda.h>
 #include <math.h>
@@ -19,7 +19,11 @@ namespace {
 using namespace tc;
 constexpr int kBK = 64, kUmmaK = 16, kTile = kHeadTile;
 constexpr int kStages = 6;
-constexpr int kThreads = 192;
+// warps that take finished accumulators: the logits need two for each quarter of the rows, 128 columns a thread
+constexpr int result_warps(bool to_x) { return to_x ? 4 : 8; }
+constexpr int threads_of(bool to_x) { return 64 + 32 * result_warps(to_x); }
+// k-blocks of a logit that the tensor core adds up before the sum is taken on in registers (see logits_rows)
+constexpr int kSpan = 4;
 constexpr uint32_t kABytes = 128 * kBK * 2, kBBytes = 128 * kBK * 2, kStageBytes = kABytes + kBBytes;
 constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 + 256;
 constexpr uint32_t kTmemCols = 512;
@@ -91,30 +95,30 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// One row of a finished tile of logits: its 256 columns are read twice from TMEM, once for the largest, once for the
-// exponentials.  `dead` marks, a bit a column, what is listed or behind the vocabulary.
+// One row of 128 logits, in registers, by one thread: the listed ones are put aside, the others become exponentials.
 template <bool GRAD, bool CAP>
-__device__ __forceinline__ void logits_row(const HeadArgs& p, uint32_t tmem, int n0, int row, bool live) {
+__device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCols], int n0, int row, bool live) {
+  constexpr int kChunks = kHeadCols / 32;
   const int token = live ? p.row_token[p.piece0 + row] : 0;
   const int32_t* list = p.list + (size_t)token * p.top;
-  // the first listed column that this tile may hold
-  int first = 0;
+  // the first listed column that may be among these
+  int at = 0;
   if (live) {
     int hi = p.top;
-    while (first < hi) {
-      const int mid = (first + hi) >> 1;
-      if (list[mid] < n0) first = mid + 1;
+    while (at < hi) {
+      const int mid = (at + hi) >> 1;
+      if (list[mid] < n0) at = mid + 1;
       else hi = mid;
     }
   }
-  float* z = p.z_listed + (size_t)row * p.top + first;
-  int at, next;
-  auto begin = [&] {
-    at = first;
-    next = live && at < p.top ? list[at] : kHeadNone;
-  };
-  // of the 32 columns from `col`, those that are listed; called with ascending columns
-  auto named_in = [&](int col) {
+  float* z = p.z_listed + (size_t)row * p.top + at;
+  const float factor = p.logit_factor, cap_out = p.cap_out, to2 = p.to2;
+  int next = live && at < p.top ? list[at] : kHeadNone;
+  uint32_t dead[kChunks];       // a bit for each column that is listed or behind the vocabulary
+  float most = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const int col = n0 + 32 * c;
     uint32_t named = 0;
     while (next < col + 32) {
       named |= 1u << (next - col);
@@ -122,76 +126,58 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, uint32_t tmem, int
       next = at < p.top ? list[at] : kHeadNone;
     }
     __syncwarp();
-    return named;
-  };
-  auto behind = [&](int col) { return p.vocab - col >= 32 ? 0u : ~((1u << max(p.vocab - col, 0)) - 1u); };
-  begin();
-  float most = -INFINITY;
-#pragma unroll 1
-  for (int c = 0; c < kTile; c += 32) {
-    const uint32_t dead = named_in(n0 + c) | behind(n0 + c);
-    uint32_t v[32];
-    tmem_ld32(tmem + c, v);
-    tmem_ld_wait();
-    if (__any_sync(0xffffffffu, dead)) {
-#pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (!(dead >> j & 1)) most = fmaxf(most, __uint_as_float(v[j]));
-    } else {
-#pragma unroll
-      for (int j = 0; j < 32; ++j) most = fmaxf(most, __uint_as_float(v[j]));
-    }
-  }
-  most *= p.logit_factor;
-  if (CAP) most = tanhf(most) * p.cap_out;
-  const float r = most == -INFINITY ? 0.f : kHeadStep * rintf(most * (1.4426950408889634f / kHeadStep));
-  const float factor = p.logit_factor, cap_out = p.cap_out, to2 = p.to2;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  bf16* e = reinterpret_cast<bf16*>(p.e) + (size_t)row * p.pitch + n0;
-  begin();
-#pragma unroll 1
-  for (int c = 0; c < kTile; c += 32) {
-    const uint32_t named = named_in(n0 + c), dead = named | behind(n0 + c);
-    const bool any = __any_sync(0xffffffffu, dead);
-    uint32_t v[32];
-    tmem_ld32(tmem + c, v);
-    tmem_ld_wait();
-    if (any && named) {
+    if (named) {
 #pragma unroll
       for (int j = 0; j < 32; ++j)
         if (named >> j & 1) {
-          const float raw = __uint_as_float(v[j]) * factor;
+          const float raw = x[32 * c + j] * factor;
           *z++ = CAP ? tanhf(raw) * cap_out : raw;
         }
     }
     __syncwarp();
+    dead[c] = named | (p.vocab - col >= 32 ? 0u : ~((1u << max(p.vocab - col, 0)) - 1u));
+    if (__any_sync(0xffffffffu, dead[c])) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (!(dead[c] >> j & 1)) most = fmaxf(most, x[32 * c + j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) most = fmaxf(most, x[32 * c + j]);
+    }
+  }
+  most *= factor;
+  if (CAP) most = tanhf(most) * cap_out;
+  const float r = most == -INFINITY ? 0.f : kHeadStep * rintf(most * (1.4426950408889634f / kHeadStep));
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  bf16* e = reinterpret_cast<bf16*>(p.e) + (size_t)row * p.pitch + n0;
+#pragma unroll
+  for (int c = 0; c < kChunks; ++c) {
+    const bool any = __any_sync(0xffffffffu, dead[c]);
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-      const float raw = __uint_as_float(v[j]);
+      float& v = x[32 * c + j];
       float ex, slope = 1.f;
       if (CAP) {
-        const float t = tanhf(raw * factor);
+        const float t = tanhf(v * factor);
         ex = exp2_fast(fmaf(t, to2, -r));
         slope = (1.f - t) * (1.f + t);
       } else {
-        ex = exp2_fast(fmaf(raw, to2, -r));
+        ex = exp2_fast(fmaf(v, to2, -r));
       }
-      if (any && (dead >> j & 1)) ex = 0.f;
+      if (any && (dead[c] >> j & 1)) ex = 0.f;
       sum[j & 3] += ex;
-      v[j] = __float_as_uint(CAP ? ex * slope : ex);
+      v = CAP ? ex * slope : ex;
     }
     if (GRAD && live) {
 #pragma unroll
-      for (int j = 0; j < 32; j += 8)
-        if (n0 + c + j < p.pitch)
-          *reinterpret_cast<uint4*>(e + c + j) =
-              make_uint4(pack_bf16(__uint_as_float(v[j]), __uint_as_float(v[j + 1])),
-                         pack_bf16(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])),
-                         pack_bf16(__uint_as_float(v[j + 4]), __uint_as_float(v[j + 5])),
-                         pack_bf16(__uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])));
+      for (int j = 32 * c; j < 32 * c + 32; j += 8)
+        if (n0 + j < p.pitch)
+          *reinterpret_cast<uint4*>(e + j) = make_uint4(pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
+                                                        pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
     }
   }
-  if (live) p.stats[(size_t)(n0 / kTile) * p.piece + row] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+  if (live && n0 < p.vocab)
+    p.stats[(size_t)(n0 / kHeadCols) * p.piece + row] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
 }
 
 // 32 columns of one row of d_x
@@ -209,7 +195,7 @@ __device__ __forceinline__ void grad_chunk(const HeadArgs& p, bf16* out, float b
 enum { kLogits = 0, kLogitsGrad = 1, kLogitsCap = 2, kLogitsCapGrad = 3, kGrad = 4 };
 
 template <int MODE>
-__global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_constant__ HeadArgs p,
+__global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(const __grid_constant__ HeadArgs p,
                                                               const __grid_constant__ HeadMaps maps) {
   constexpr bool kToX = MODE == kGrad;                    // the second product: B is [K, N]
   extern __shared__ uint8_t smem_raw[];
@@ -229,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
   let_next_start();
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 8); }   // 4 warps of each CTA
+    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * result_warps(kToX)); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tmap(&maps.a); prefetch_tmap(&maps.a_rows); prefetch_tmap(&maps.b);
@@ -248,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
   const int rows = head_rows_here(p);
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const Plan plan = kToX ? make_plan(rows, (p.d + kTile - 1) / kTile, (p.vocab + kBK - 1) / kBK, pairs, p.part_items, true)
-                         : make_plan(rows, p.col_tiles, (p.d + kBK - 1) / kBK, pairs, 0, false);
+                         : make_plan(rows, (p.vocab + kTile - 1) / kTile, (p.d + kBK - 1) / kBK, pairs, 0, false);
 
   if (warp == 0) {
     // ---------------- loads (both CTAs, each its own halves) ----------------
@@ -288,27 +274,30 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       const uint32_t idesc = make_idesc_m(256, kTile, 0, kToX ? 1 : 0);
       uint32_t it = 0, count = 0;
       bool ok = true;
-      for (int i = pair; i < plan.items && ok; i += pairs, ++count) {
+      for (int i = pair; i < plan.items && ok; i += pairs) {
         const Item t = item_at(plan, i);
-        const uint32_t buf = count & 1u, use = count >> 1;
-        if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t acc = tmem_base + buf * kTile;
-        for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
-          const int st = it % kStages;
-          if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
+        for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += kToX ? plan.k_blocks : kSpan, ++count) {
+          const int k1 = kToX ? t.kb1 : min(k0 + kSpan, t.kb1);
+          const uint32_t buf = count & 1u, use = count >> 1;
+          if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t a_addr = smem_base + st * kStageBytes, b_addr = a_addr + kABytes;
+          const uint32_t acc = tmem_base + buf * kTile;
+          for (int kb = k0; kb < k1; ++kb, ++it) {
+            const int st = it % kStages;
+            if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t a_addr = smem_base + st * kStageBytes, b_addr = a_addr + kABytes;
 #pragma unroll
-          for (int k = 0; k < kBK / kUmmaK; ++k) {
-            const uint64_t ad = make_desc(a_addr + k * (kUmmaK * 2), 16, 1024);
-            const uint64_t bd = kToX ? make_desc(b_addr + k * (kUmmaK * 128), kBK * 128, 1024)
-                                     : make_desc(b_addr + k * (kUmmaK * 2), 16, 1024);
-            umma_bf16_pair(acc, ad, bd, idesc, kb > t.kb0 || k > 0);
+            for (int k = 0; k < kBK / kUmmaK; ++k) {
+              const uint64_t ad = make_desc(a_addr + k * (kUmmaK * 2), 16, 1024);
+              const uint64_t bd = kToX ? make_desc(b_addr + k * (kUmmaK * 128), kBK * 128, 1024)
+                                       : make_desc(b_addr + k * (kUmmaK * 2), 16, 1024);
+              umma_bf16_pair(acc, ad, bd, idesc, kb > k0 || k > 0);
+            }
+            umma_commit_pair(empty_bar(st), 3);
           }
-          umma_commit_pair(empty_bar(st), 3);
+          if (ok) umma_commit_pair(tfull_bar(buf), 3);
         }
-        if (ok) umma_commit_pair(tfull_bar(buf), 3);
       }
       if (!ok) {
         *abort_flag = 1;
@@ -320,17 +309,43 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
     const int q = warp & 3;
     uint32_t count = 0;
     bool ok = true;
-    for (int i = pair; i < plan.items; i += pairs, ++count) {
+    for (int i = pair; i < plan.items && ok; i += pairs) {
       const Item t = item_at(plan, i);
-      const uint32_t buf = count & 1u, use = count >> 1;
-      if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
-      tc_fence_after();
       const int row = t.m0 + (int)rank * 128 + q * 32 + lane;
       const bool live = row < rows;
-      const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile;
       if constexpr (!kToX) {
-        logits_row<(MODE & 1) != 0, (MODE & 2) != 0>(p, acc, t.n0, row, live);
+        // The tensor core cuts off what a sum has behind its 24 bits, at every step of 16 products: over a whole row that
+        // is a few 2^-20 of the logit, always towards zero.  So a sum starts anew every kSpan k-blocks, and the parts are
+        // added here, rounded to nearest.
+        const int half = (warp - 2) >> 2;
+        float x[kHeadCols];
+#pragma unroll
+        for (int j = 0; j < kHeadCols; ++j) x[j] = 0.f;
+        for (int k0 = 0; k0 < plan.k_blocks; k0 += kSpan, ++count) {
+          const uint32_t buf = count & 1u, use = count >> 1;
+          if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile + half * kHeadCols;
+#pragma unroll
+          for (int c = 0; c < kHeadCols; c += 32) {
+            uint32_t v[32];
+            tmem_ld32(acc + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[c + j] += __uint_as_float(v[j]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(buf), 0));
+        }
+        if (!ok) break;
+        logits_row<(MODE & 1) != 0, (MODE & 2) != 0>(p, x, t.n0 + half * kHeadCols, row, live);
       } else {
+        const uint32_t buf = count & 1u, use = count >> 1;
+        ++count;
+        if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile;
         float by = 0.f;
         bf16* out = nullptr;
         if (live) {
@@ -402,10 +417,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
           tmem_ld_wait();
           if (live) grad_chunk(p, out, by, t.n0 + c, v);
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(buf), 0));
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(buf), 0));
     }
     if (!ok && lane == 0) {
       *abort_flag = 1;
@@ -432,7 +447,7 @@ cudaError_t launch(const HeadArgs& p, const HeadMaps& maps, long long most_items
   cudaError_t e = allow_smem(head_tc_kernel<MODE>, kSmemBytes, done);
   if (e != cudaSuccess) return e;
   const int pairs = (int)(most_items < head_pairs() ? (most_items > 0 ? most_items : 1) : head_pairs());
-  return launch_behind_in_clusters(2, head_tc_kernel<MODE>, (unsigned)(2 * pairs), kThreads, kSmemBytes, st, p, maps);
+  return launch_behind_in_clusters(2, head_tc_kernel<MODE>, (unsigned)(2 * pairs), threads_of(MODE == kGrad), kSmemBytes, st, p, maps);
 }
 
 }  // namespace
@@ -454,7 +469,7 @@ cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st) {
       !tc_encode_2d(&m.a_rows, p.x_rows, p.piece, p.d, p.d, 128, kBK) ||
       !tc_encode_2d(&m.b, p.w, p.vocab, p.d, p.w_stride, 128, kBK))
     return cudaErrorInvalidValue;
-  const long long items = (long long)((p.piece + kTile - 1) / kTile) * p.col_tiles;
+  const long long items = (long long)((p.piece + kTile - 1) / kTile) * ((p.vocab + kTile - 1) / kTile);
   if (p.softcap > 0.f) return p.d_x ? launch<kLogitsCapGrad>(p, m, items, st) : launch<kLogitsCap>(p, m, items, st);
   return p.d_x ? launch<kLogitsGrad>(p, m, items, st) : launch<kLogits>(p, m, items, st);
 }
