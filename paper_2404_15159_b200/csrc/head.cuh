@@ -25,7 +25,7 @@ constexpr int kHeadMaxShares = 16;           // CTA pairs that share one tile's 
 constexpr int kHeadMaxItems = 222;           // shares under way: three rounds of 74 CTA pairs
 constexpr int kHeadCounters = 1024;          // one for each epilogue warp of a split tile (73 tiles of 8 warps at most)
 constexpr int kHeadSimtShares = 296;         // the same of the fp32 kernel's 128 x 128 tiles, two blocks an SM
-constexpr int kHeadRowsPerBlock = 32;        // rows that a block of the joining kernel takes
+constexpr int kHeadRowsPerBlock = 8;         // rows that a block of the joining kernel takes
 
 // What the kernels of a call leave for one another beside the arrays
 struct HeadState {
@@ -61,7 +61,7 @@ struct HeadArgs {
   double* loss_part;              // sum of weight * loss for each block of the joining kernel
   void* x_rows;                   // [piece, d] the counted rows of x, where some tokens are left out
   float* z_listed;                // [piece, top] logits of the listed columns
-  float2* stats;                  // [col_tiles, piece] (R, S)
+  float2* stats;                  // [piece, col_tiles] (R, S)
   void* e;                        // [piece, pitch]
   float* row_scale;               // [piece]
   float* part;                    // partial tiles of a split reduction

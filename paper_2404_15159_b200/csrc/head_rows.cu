@@ -12,7 +12,7 @@ namespace {
 constexpr double kLn2d = 0.69314718055994530942, kLog2ed = 1.44269504088896340736;
 constexpr int kListThreads = 128;
 constexpr int kScanThreads = 1024, kScanEach = 8;
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 32 * kHeadRowsPerBlock;
 
 template <typename T> __device__ __forceinline__ T warp_sum(T v) {
 #pragma unroll
@@ -285,85 +285,73 @@ __device__ __forceinline__ void add_totals(const HeadArgs& p, int block, double 
   }
 }
 
-// Joins a row's tiles: 32 rows a block, first a row per lane and an eighth of the tiles per warp, then a warp per row.
+// Joins a row's tiles, a warp a row: sums over the tiles' R and S, the row's loss, and for a gradient its exponentials at one
+// R with the listed columns' factors in their places.
 __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
-  constexpr int kWarps = kRowThreads / 32, kRows = kHeadRowsPerBlock;
+  constexpr int kWarps = kRowThreads / 32, kAhead = 8;
   let_next_start();
   wait_for_last();
-  __shared__ float r_of[kWarps][kRows], s_of[kWarps][kRows], r_row[kRows];
   __shared__ double warp_w[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row0 = blockIdx.x * kRows, rows = head_rows_here(p) - row0;
+  const int row = blockIdx.x * kWarps + warp;
   double weighted = 0.0;
-  if (rows > 0) {
-    const float2* stats = p.stats + row0;
+  if (row < head_rows_here(p)) {
+    const float2* stats = p.stats + (size_t)row * p.col_tiles;
+    const int token = p.row_token[p.piece0 + row];
+    const int n = p.labels ? 1 : p.list_n[token];
+    float* z = p.z_listed + (size_t)row * p.top;
     float r = -INFINITY, s = 0.f;
-    if (lane < rows) {
-      for (int i = warp; i < p.col_tiles; i += kWarps) {
-        const float2 v = stats[(size_t)i * p.piece + lane];
-        if (v.y == 0.f) continue;
-        if (v.x > r) { s = s * exp2f(r - v.x) + v.y; r = v.x; }
-        else s += v.y * exp2f(v.x - r);
-      }
-    }
-    r_of[warp][lane] = r;
-    s_of[warp][lane] = s;
-    __syncthreads();
-    for (int i = warp; i < min(rows, kRows); i += kWarps) {
-      const int token = p.row_token[p.piece0 + row0 + i];
-      float ro = -INFINITY, so = 0.f;
+    auto add = [&](float r2, float s2) {           // a sum of nothing has no say in R
+      const float most = s2 == 0.f ? r : (s == 0.f ? r2 : fmaxf(r, r2));
+      s = (s == 0.f ? 0.f : s * exp2f(r - most)) + (s2 == 0.f ? 0.f : s2 * exp2f(r2 - most));
+      r = most;
+    };
+    for (int i0 = lane; i0 < p.col_tiles; i0 += 32 * kAhead) {
+      float2 v[kAhead];
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float rv = r_of[w][i], sv = s_of[w][i];
-        if (sv == 0.f) continue;
-        if (rv > ro) { so = so * exp2f(ro - rv) + sv; ro = rv; }
-        else so += sv * exp2f(rv - ro);
-      }
-      const double lr = so == 0.f ? -INFINITY : (double)ro * kLn2d + log((double)so);
-      const RowResult res = finish_row(p, token, p.labels ? 1 : p.list_n[token], lr, (double)ro,
-                                       p.z_listed + (size_t)(row0 + i) * p.top, true);
-      if (lane == 0) {
-        weighted += res.weighted;
-        r_row[i] = (float)res.r;
-        if (p.d_x) p.row_scale[row0 + i] = res.scale;
-      }
+      for (int j = 0; j < kAhead; ++j) v[j] = i0 + 32 * j < p.col_tiles ? stats[i0 + 32 * j] : make_float2(0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) add(v[j].x, v[j].y);
     }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+      const float r2 = __shfl_xor_sync(0xffffffffu, r, d), s2 = __shfl_xor_sync(0xffffffffu, s, d);
+      add(r2, s2);
+    }
+    const double lr = s == 0.f ? -INFINITY : (double)r * kLn2d + log((double)s);
+    const RowResult res = finish_row(p, token, n, lr, s == 0.f ? -INFINITY : (double)r, z, true);
+    if (lane == 0) weighted = res.weighted;
     if (p.d_x) {
-      __syncthreads();
-      bf16* e = reinterpret_cast<bf16*>(p.e) + (size_t)row0 * p.pitch;
-      for (int i = warp; i < p.col_tiles; i += kWarps) {
+      if (lane == 0) p.row_scale[row] = res.scale;
+      bf16* e = reinterpret_cast<bf16*>(p.e) + (size_t)row * p.pitch;
+      for (int i0 = 0; i0 < p.col_tiles; i0 += 32) {
         float by = 0.f;
-        if (lane < rows) {
-          const float2 v = stats[(size_t)i * p.piece + lane];
-          by = v.y == 0.f ? 0.f : v.x - r_row[lane];
+        if (i0 + lane < p.col_tiles) {
+          const float2 v = stats[i0 + lane];
+          if (v.y != 0.f) by = v.x - (float)res.r;
         }
         unsigned todo = __ballot_sync(0xffffffffu, by < 0.f);
         while (todo) {
           const int l = __ffs(todo) - 1;
           todo &= todo - 1;
           const float f = exp2f(__shfl_sync(0xffffffffu, by, l));
-          const int c = i * kHeadCols + lane * 4;
-          if (c >= p.pitch) continue;
-          uint2* at = reinterpret_cast<uint2*>(e + (size_t)l * p.pitch + c);
-          uint2 v = *at;
-          __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+          const int c = (i0 + l) * kHeadCols + lane * 4;
+          if (c < p.pitch) {
+            uint2* at = reinterpret_cast<uint2*>(e + c);
+            uint2 v = *at;
+            __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float2 w = __bfloat1622float2(h[j]);
-            h[j] = __floats2bfloat162_rn(w.x * f, w.y * f);
+            for (int j = 0; j < 2; ++j) {
+              const float2 w = __bfloat1622float2(h[j]);
+              h[j] = __floats2bfloat162_rn(w.x * f, w.y * f);
+            }
+            *at = v;
           }
-          *at = v;
         }
-        __syncwarp();
       }
-      __syncthreads();
-      for (int i = warp; i < min(rows, kRows); i += kWarps) {
-        const int token = p.row_token[p.piece0 + row0 + i];
-        const int n = p.labels ? 1 : p.list_n[token];
-        for (int k = lane; k < n; k += 32)
-          e[(size_t)i * p.pitch + p.list[(size_t)token * p.top + k]] =
-              __float2bfloat16(p.z_listed[(size_t)(row0 + i) * p.top + k]);
-      }
+      __syncwarp();
+      const int32_t* list = p.list + (size_t)token * p.top;
+      for (int k = lane; k < n; k += 32) e[list[k]] = __float2bfloat16(z[k]);
     }
   }
   if (lane == 0) warp_w[warp] = weighted;
@@ -372,7 +360,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
   if (threadIdx.x == 0)
     for (int i = 0; i < kWarps; ++i) mine += warp_w[i];
   __syncthreads();
-  add_totals(p, p.piece0 / kRows + blockIdx.x, mine, warp_w);
+  add_totals(p, p.piece0 / kWarps + blockIdx.x, mine, warp_w);
 }
 
 // The fp32 mode's rows: a block a row, whose logits (x . w, as the product left them) become the gradient's factors.

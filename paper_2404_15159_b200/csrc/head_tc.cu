@@ -23,7 +23,7 @@ constexpr int kStages = 6;
 constexpr int result_warps(bool to_x) { return to_x ? 4 : 8; }
 constexpr int threads_of(bool to_x) { return 64 + 32 * result_warps(to_x); }
 // k-blocks of a logit that the tensor core adds up before the sum is taken on in registers (see logits_rows)
-constexpr int kSpan = 4;
+constexpr int kSpan = 16;
 constexpr uint32_t kABytes = 128 * kBK * 2, kBBytes = 128 * kBK * 2, kStageBytes = kABytes + kBBytes;
 constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 + 256;
 constexpr uint32_t kTmemCols = 512;
@@ -177,7 +177,7 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     }
   }
   if (live && n0 < p.vocab)
-    p.stats[(size_t)(n0 / kHeadCols) * p.piece + row] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+    p.stats[(size_t)row * p.col_tiles + n0 / kHeadCols] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
 }
 
 // 32 columns of one row of d_x
