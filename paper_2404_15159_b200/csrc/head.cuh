@@ -20,6 +20,7 @@ namespace mixlora {
 constexpr int kHeadTile = 256;               // rows and columns of a tile of the products
 constexpr int kHeadCols = 128;               // columns that share R and S
 constexpr float kHeadStep = 100.f;           // R's step, in powers of two
+constexpr int kHeadFewTokens = 64;
 constexpr int kHeadNone = 0x7fffffff;        // no column (ends a row's list)
 constexpr int kHeadMaxShares = 16;           // CTA pairs that share one tile's reduction
 constexpr int kHeadMaxItems = 222;           // shares under way: three rounds of 74 CTA pairs
@@ -70,8 +71,13 @@ struct HeadArgs {
   int pitch, col_tiles;
   int join_blocks;                // of the joining kernel, over all pieces
   int part_items;                 // that `part` has room for
+  int few;                        // rows are tokens, those that are left out among them
 };
 
+// Entries of a token's list, 0 where it is left out
+__device__ __forceinline__ int head_entries(const HeadArgs& p, int token) {
+  return p.labels ? (p.labels[token] >= 0 && p.labels[token] < p.vocab) : p.list_n[token];
+}
 __device__ __forceinline__ int head_rows_here(const HeadArgs& p) {
   return min(max(p.state->counted - p.piece0, 0), p.piece);
 }
@@ -82,6 +88,7 @@ cudaError_t launch_head_gather(const HeadArgs& p, bool bf16_mode, bool first_pie
 cudaError_t launch_head_join(const HeadArgs& p, bool bf16_mode, cudaStream_t st);      // loss, lse, totals; E finished, row_scale
 cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st);    // stats, z_listed, E
 cudaError_t launch_head_grad_tc(const HeadArgs& p, cudaStream_t st);      // d_x
+cudaError_t launch_head_logits_few(const HeadArgs& p, bool first, cudaStream_t st);   // the same for up to kHeadFewTokens; clears the state
 cudaError_t launch_head_logits_simt(const HeadArgs& p, cudaStream_t st);
 cudaError_t launch_head_grad_simt(const HeadArgs& p, cudaStream_t st);
 int head_pairs();                                                         // CTA pairs of this GPU

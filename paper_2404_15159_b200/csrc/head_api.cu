@@ -159,6 +159,13 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   a.join_blocks = L.join_blocks; a.part_items = L.part_items;
 
   if (!c.labels) MIXLORA_TRY(launch_head_lists(a, st));
+  if (bf16_mode && s->tokens <= kHeadFewTokens) {
+    a.few = 1;
+    MIXLORA_TRY(launch_head_logits_few(a, c.labels != nullptr, st));
+    MIXLORA_TRY(launch_head_join(a, true, st));
+    if (gradient) MIXLORA_TRY(launch_head_grad_tc(a, st));
+    return MIXLORA_OK;
+  }
   MIXLORA_TRY(launch_head_scan(a, c.labels != nullptr, st));
   for (int i = 0; i < L.pieces; ++i) {
     a.piece0 = i * L.piece;

@@ -1,0 +1,277 @@
+// Logits of a few tokens (up to 64; bf16): bound by reading the head once.
+//
+// The roles of the operands are turned around: 128 columns of the vocabulary are the rows of a tensor-core tile, the tokens
+// its columns (16, 32 or 64), so that no part of a tile is empty and the head streams through shared memory at the rate of
+// the memory.  One persistent CTA an SM; warp 0 loads (128 reduction elements a stage, so that 256 bytes of each row are
+// asked for at once), warp 1 issues the products, warps 2 to 5 add up the spans (see the kernel for many tokens) and pass
+// the tile through shared memory, and warps 2 to 9 then work on a token each, four neighbouring columns a lane.
+// Rows are tokens here: those that are left out pass through the product too, and the joining kernel drops them.
+#include <cuda.h>
+#include <math.h>
+
+#include "head.cuh"
+#include "tc_ptx.cuh"
+
+namespace mixlora {
+namespace {
+
+using namespace tc;
+constexpr int kWarps = 8, kThreads = 64 + 32 * kWarps, kBK = 64, kUmmaK = 16;
+constexpr int kSpan = 8;                                  // stages of 128 reduction elements
+constexpr uint32_t kABytes = 2 * 128 * kBK * 2;
+template <int NC> struct Few {
+  static constexpr uint32_t kBBytes = 2 * NC * kBK * 2, kStage = kABytes + kBBytes;
+  static constexpr int kStages = NC == 16 ? 6 : (NC == 32 ? 5 : 4);
+  static constexpr uint32_t kTurn = NC * kHeadCols * 4;   // the finished tile, [token][column]
+  static constexpr uint32_t kSmem = kStages * kStage + kTurn + 1024 + 256;
+};
+struct alignas(64) FewMaps { CUtensorMap w, x; };
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <int NC, bool GRAD, bool CAP>
+__global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_constant__ HeadArgs p,
+                                                               const __grid_constant__ FewMaps maps) {
+  using F = Few<NC>;
+  constexpr int kStages = F::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* turn = reinterpret_cast<float*>(smem + kStages * F::kStage);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * F::kStage + F::kTurn);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* give_up = abort_flag + 1;                 // one of the result warps waited in vain
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (kStages + s); };
+  auto tfull_bar = [&](int b) { return bar_base + 8u * (2 * kStages + b); };
+  auto tempty_bar = [&](int b) { return bar_base + 8u * (2 * kStages + 2 + b); };
+
+  let_next_start();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 4); }
+    *abort_flag = 0;
+    *give_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_tmap(&maps.w); prefetch_tmap(&maps.x);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), 2 * NC);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  wait_for_last();
+  // what the scan leaves for the later kernels of a call with many tokens
+  if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < kHeadCounters; i += kThreads) p.counters[i] = 0;
+    if (threadIdx.x == 0) {
+      p.state->status = 0;
+      p.state->counted = p.tokens;
+      p.state->joined = 0;
+    }
+  }
+
+  const int steps = (p.d + 2 * kBK - 1) / (2 * kBK);
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
+        for (int s = 0; s < steps; ++s, ++it) {
+          const int st = it % kStages;
+          if (!mbar_wait(empty_bar(st), ((it / kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          const uint32_t a_dst = smem_base + st * F::kStage, b_dst = a_dst + kABytes;
+          mbar_expect_tx(full_bar(st), F::kStage);
+          const int k = s * 2 * kBK;
+          tma_load_2d(a_dst, &maps.w, full_bar(st), k, tile * kHeadCols);
+          tma_load_2d(a_dst + kABytes / 2, &maps.w, full_bar(st), k + kBK, tile * kHeadCols);
+          tma_load_2d(b_dst, &maps.x, full_bar(st), k, 0);
+          tma_load_2d(b_dst + F::kBBytes / 2, &maps.x, full_bar(st), k + kBK, 0);
+        }
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicExch(&p.state->status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = make_idesc(NC, 0, 0);
+      uint32_t it = 0, count = 0;
+      bool ok = true;
+      for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
+        for (int s0 = 0; s0 < steps && ok; s0 += kSpan, ++count) {
+          const uint32_t buf = count & 1u, use = count >> 1;
+          if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t acc = tmem_base + buf * NC;
+          for (int s = s0; s < min(s0 + kSpan, steps); ++s, ++it) {
+            const int st = it % kStages;
+            if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t a_addr = smem_base + st * F::kStage, b_addr = a_addr + kABytes;
+#pragma unroll
+            for (int k = 0; k < 2 * kBK / kUmmaK; ++k) {
+              const uint32_t half = k / (kBK / kUmmaK), in = k % (kBK / kUmmaK);
+              umma_bf16(acc, make_desc(a_addr + half * (kABytes / 2) + in * (kUmmaK * 2), 16, 1024),
+                        make_desc(b_addr + half * (F::kBBytes / 2) + in * (kUmmaK * 2), 16, 1024), idesc, s > s0 || k > 0);
+            }
+            umma_commit(empty_bar(st));
+          }
+          if (ok) umma_commit(tfull_bar(buf));
+        }
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicExch(&p.state->status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+      }
+    }
+  } else {
+    const int q = warp & 3;
+    const float factor = p.logit_factor, cap_out = p.cap_out, to2 = p.to2;
+    uint32_t count = 0;
+    bool ok = true;
+    for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
+      float x[NC];
+      if (warp < 6) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) x[j] = 0.f;
+        for (int s0 = 0; s0 < steps; s0 += kSpan, ++count) {
+          const uint32_t buf = count & 1u, use = count >> 1;
+          if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * NC;
+#pragma unroll
+          for (int c = 0; c < NC; c += 16) {
+            uint32_t v[16];
+            tmem_ld16(acc + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[c + j] += __uint_as_float(v[j]);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(tempty_bar(buf));
+        }
+      }
+      // the warps meet whether a wait ran out or not, and leave together
+      if (!ok) *give_up = 1;
+      named_barrier(1, 32 * kWarps);                      // the tile before has been read
+      ok = *give_up == 0;
+      if (warp < 6) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) turn[j * kHeadCols + q * 32 + lane] = x[j];
+      }
+      named_barrier(1, 32 * kWarps);
+      if (!ok) break;
+      const int n0 = tile * kHeadCols, col = n0 + lane * 4;
+      for (int t = warp - 2; t < min(NC, p.tokens); t += kWarps) {
+        const float4 f = *reinterpret_cast<const float4*>(turn + t * kHeadCols + lane * 4);
+        float v[4] = {f.x, f.y, f.z, f.w};
+        uint32_t dead = 0;                                // of this lane's columns: listed, or behind the vocabulary
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dead |= col + j >= p.vocab ? 1u << j : 0u;
+        const int32_t* list = p.list + (size_t)t * p.top;
+        for (int k0 = 0; k0 < p.top; k0 += 32) {
+          const int c = k0 + lane < p.top ? list[k0 + lane] : kHeadNone;
+          unsigned hit = __ballot_sync(0xffffffffu, c >= n0 && c < n0 + kHeadCols && c < p.vocab);
+          while (hit) {
+            const int l = __ffs(hit) - 1, at = __shfl_sync(0xffffffffu, c, l) - n0;
+            hit &= hit - 1;
+            if (at >> 2 == lane) {
+              const int j = at & 3;
+              const float raw = (j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3]) * factor;
+              p.z_listed[(size_t)t * p.top + k0 + l] = CAP ? tanhf(raw) * cap_out : raw;
+              dead |= 1u << j;
+            }
+          }
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (!(dead >> j & 1)) most = fmaxf(most, v[j]);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        most *= factor;
+        if (CAP) most = tanhf(most) * cap_out;
+        const float r = most == -INFINITY ? 0.f : kHeadStep * rintf(most * (1.4426950408889634f / kHeadStep));
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float ex, slope = 1.f;
+          if (CAP) {
+            const float th = tanhf(v[j] * factor);
+            ex = exp2_fast(fmaf(th, to2, -r));
+            slope = (1.f - th) * (1.f + th);
+          } else {
+            ex = exp2_fast(fmaf(v[j], to2, -r));
+          }
+          if (dead >> j & 1) ex = 0.f;
+          sum += ex;
+          v[j] = CAP ? ex * slope : ex;
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) p.stats[(size_t)t * p.col_tiles + tile] = make_float2(r, sum);
+        if (GRAD && col < p.pitch) {
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), up = __floats2bfloat162_rn(v[2], v[3]);
+          *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(p.e) + (size_t)t * p.pitch + col) =
+              make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&up));
+        }
+      }
+    }
+    if (!ok && lane == 0) {
+      *abort_flag = 1;
+      atomicExch(&p.state->status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+    }
+  }
+
+  __syncthreads();
+  if (*abort_flag) {
+    for (int i = 0; i < 200; ++i) __nanosleep(5000);      // let copies that may still be in flight land
+  }
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem_base, 2 * NC);
+  }
+}
+
+template <int NC, bool GRAD, bool CAP>
+cudaError_t launch(const HeadArgs& p, bool first, cudaStream_t st) {
+  FewMaps m;
+  if (!tc_encode_2d(&m.w, p.w, p.vocab, p.d, p.w_stride, kHeadCols, kBK) ||
+      !tc_encode_2d(&m.x, p.x, p.tokens, p.d, p.x_stride, NC, kBK))
+    return cudaErrorInvalidValue;
+  static bool done[64] = {false};
+  cudaError_t e = allow_smem(head_few_kernel<NC, GRAD, CAP>, Few<NC>::kSmem, done);
+  if (e != cudaSuccess) return e;
+  const int sms = 2 * head_pairs(), grid = p.col_tiles < sms ? p.col_tiles : sms;
+  if (!first) return launch_behind(head_few_kernel<NC, GRAD, CAP>, (unsigned)grid, kThreads, Few<NC>::kSmem, st, p, m);
+  head_few_kernel<NC, GRAD, CAP><<<grid, kThreads, Few<NC>::kSmem, st>>>(p, m);
+  return cudaGetLastError();
+}
+template <int NC>
+cudaError_t launch_for(const HeadArgs& p, bool first, cudaStream_t st) {
+  if (p.softcap > 0.f) return p.d_x ? launch<NC, true, true>(p, first, st) : launch<NC, false, true>(p, first, st);
+  return p.d_x ? launch<NC, true, false>(p, first, st) : launch<NC, false, false>(p, first, st);
+}
+
+}  // namespace
+
+cudaError_t launch_head_logits_few(const HeadArgs& p, bool first, cudaStream_t st) {
+  if (p.tokens <= 16) return launch_for<16>(p, first, st);
+  if (p.tokens <= 32) return launch_for<32>(p, first, st);
+  return launch_for<64>(p, first, st);
+}
+
+}  // namespace mixlora

@@ -94,6 +94,12 @@ __global__ void __launch_bounds__(kListThreads) head_lists_kernel(HeadArgs p) {
   }
 }
 
+// What a weight is multiplied by: one over the normalizer
+__device__ __forceinline__ float part_of_each(const HeadArgs& p, double weights) {
+  const double norm = p.normalizer ? (double)p.normalizer[0] : weights;
+  return norm == 0.0 ? 0.f : (float)(1.0 / norm);
+}
+
 // Numbers the counted rows and adds up their weights: one block, 8192 tokens a turn.  Rows that are left out get their
 // zeroes here, and the counters of the call are cleared.
 __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
@@ -112,7 +118,7 @@ __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
     for (int j = 0; j < kScanEach; ++j) {
       const int t = first + j;
       if (t >= p.tokens) break;
-      const bool ok = p.labels ? p.labels[t] >= 0 && p.labels[t] < p.vocab : p.list_n[t] > 0;
+      const bool ok = head_entries(p, t) > 0;
       in |= (unsigned)ok << j;
       if (ok) {
         weight += p.weights ? (double)p.weights[t] : 1.0;
@@ -153,12 +159,11 @@ __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
   if (threadIdx.x == 0) {
     double sum = 0.0;
     for (int i = 0; i < kScanThreads / 32; ++i) sum += warp_w[i];
-    const double norm = p.normalizer ? (double)p.normalizer[0] : sum;
     p.state->status = 0;
     p.state->counted = base;
     p.state->joined = 0;
     p.state->weight = (float)sum;
-    p.state->each = norm == 0.0 ? 0.f : (float)(1.0 / norm);
+    p.state->each = part_of_each(p, sum);
   }
 }
 
@@ -182,60 +187,69 @@ __global__ void __launch_bounds__(kRowThreads) head_gather_kernel(HeadArgs p, in
   for (int i = lane; i < p.d / kEach; i += 32) dst[i] = left_out ? make_uint4(0, 0, 0, 0) : src[i];
 }
 
-// One row's loss and, with a gradient, what its columns need, by one warp.  lr: log-sum-exp of the columns that are not
-// listed; r_others: their R (-inf where there is none).  `z` holds the listed logits and gets the places' values G_k / A.
+// In 64 bits, out of line: a row needs several, and their code would not stay in the instruction cache otherwise
+__device__ __noinline__ double exp64(double x) { return exp(x); }
+__device__ __noinline__ double log64(double x) { return log(x); }
+
+// One row's loss and, with a gradient, what its columns need, by one warp.  The columns that are not listed come as
+// s 2^r (s = 0: there is none).  `z` holds the listed logits and gets the places' values G_k / A.
 struct RowResult { double r, weighted; float scale; };
-__device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, int n, double lr, double r_others, float* z, bool rounds) {
+__device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, int n, double s, double r, float each, float* z,
+                                                bool rounds) {
   const int lane = threadIdx.x & 31;
-  const double* q = p.labels ? nullptr : p.list_q + (size_t)token * p.top;
-  const double rest = p.labels ? 0.0 : p.rest_q[token];
-  double most = -INFINITY;
-  for (int k = lane; k < n; k += 32) most = fmax(most, (double)z[k]);
-  most = warp_max(most);
-  const double from = fmax(most, lr);
-  double sum = 0.0;
-  for (int k = lane; k < n; k += 32) sum += exp((double)z[k] - from);
-  sum = warp_sum(sum);
-  const double lse = from + log(sum + exp(lr - from));
-  double loss = 0.0;
-  for (int k = lane; k < n; k += 32) {
-    const double zk = (double)z[k];
-    if (!q) {
-      const double gap = lr - zk;
-      loss = fmax(gap, 0.0) + log1p(exp(-fabs(gap)));
-    } else if (!(q[k] == 0.0)) {
-      loss += q[k] * (log(q[k]) - (zk - lse));
-    }
-  }
-  loss = warp_sum(loss);
-  if (!(rest == 0.0)) loss += rest * (log(rest) - (lr - lse));
-  loss += (double)p.z_loss * lse * lse;
-  // what the target sums up to: 1 but where a teacher's entries exceed it, or name every column and stay below
-  double mass = 1.0;
-  if (q) {
-    mass = 0.0;
-    for (int k = lane; k < n; k += 32) mass += q[k];
-    mass = warp_sum(mass) + rest;
-  }
-  const double curl = 2.0 * (double)p.z_loss * lse, share = mass + curl;
+  const double lr = s == 0.0 ? -INFINITY : r * kLn2d + log64(s);
   const double weight = p.weights ? (double)p.weights[token] : 1.0;
+  const double zeta = (double)p.z_loss;
+  double loss, lse, most, miss = 0.0, mass = 1.0, rest = 0.0;
+  const double* q = nullptr;
+  if (p.labels) {
+    // loss = ln(1 + e^gap) without a difference of two logarithms, and 1 - p without one from one
+    most = (double)__shfl_sync(0xffffffffu, lane == 0 ? z[0] : 0.f, 0);     // lane 0 writes it below
+    const double gap = lr - most, e = exp64(-fabs(gap));
+    loss = fmax(gap, 0.0) + log1p(e);
+    miss = (gap > 0.0 ? 1.0 : e) / (1.0 + e);
+    lse = most + loss;
+  } else {
+    q = p.list_q + (size_t)token * p.top;
+    rest = p.rest_q[token];
+    most = -INFINITY;
+    for (int k = lane; k < n; k += 32) most = fmax(most, (double)z[k]);
+    most = warp_max(most);
+    const double from = fmax(most, lr);
+    double sum = 0.0;
+    for (int k = lane; k < n; k += 32) sum += exp64((double)z[k] - from);
+    sum = warp_sum(sum) + exp64(lr - from);
+    lse = from + log64(sum);
+    loss = mass = 0.0;
+    for (int k = lane; k < n; k += 32) {
+      mass += q[k];
+      if (!(q[k] == 0.0)) loss += q[k] * (log64(q[k]) - ((double)z[k] - lse));
+    }
+    loss = warp_sum(loss);
+    // what the target sums up to: 1 but where a teacher's entries exceed it, or name every column and stay below
+    mass = warp_sum(mass) + rest;
+    if (!(rest == 0.0)) loss += rest * (log64(rest) - (lr - lse));
+  }
+  loss += zeta * lse * lse;
   if (lane == 0) {
     p.loss[token] = (float)loss;
     if (p.lse) p.lse[token] = (float)lse;
   }
-  RowResult out{0.0, weight * (double)(float)loss, 0.f};
+  RowResult out{r, weight * (double)(float)loss, 0.f};
   if (!p.d_x) return out;
-  const double r = fmax(r_others, 100.0 * rint(most * kLog2ed / 100.0));
-  const double u = exp(r * kLn2d - lse), s = exp(lr - r * kLn2d);
-  const double part = rest > 0.0 && s > 0x1p-100 ? rest / s : 0.0;
+  const double r_listed = 100.0 * rint(most * (kLog2ed / 100.0));
+  if (s == 0.0 || r_listed > r) out.r = r_listed;
+  const double u = exp64(out.r * kLn2d - lse), s_row = s == 0.0 ? 0.0 : exp64(lr - out.r * kLn2d);
+  const double part = rest > 0.0 && s_row > 0x1p-100 ? rest / s_row : 0.0;
+  const double curl = 2.0 * zeta * lse, share = mass + curl;
   double a = share * u - part;
   // nothing below what the 32-bit sums behind u and s can tell from zero, so that G_k / A stays in range
   const double least = 0x1p-30 * fmax(u, part);
   if (fabs(a) < least) a = a < 0.0 ? -least : least;
   double largest = 0.0;
   for (int k = lane; k < n; k += 32) {
-    const double zk = (double)z[k], pk = exp(zk - lse);
-    double g = q ? share * pk - q[k] : curl * pk - 1.0 / (1.0 + exp(zk - lr));
+    const double zk = (double)z[k], pk = exp64(zk - lse);
+    double g = q ? share * pk - q[k] : curl * pk - miss;
     if (p.softcap > 0.f) {
       const double tk = zk * (double)p.temperature / (double)p.softcap;
       g *= (1.0 - tk) * (1.0 + tk);
@@ -254,14 +268,14 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
     const double near = (double)__bfloat162float(__float2bfloat16((float)(largest / a)));
     if (fabs(near) > 0x1p-100 && fabs(near) < 0x1p120) a = largest / near;
   }
-  for (int k = lane; k < n; k += 32) z[k] = (float)((double)z[k] / a);
-  out.r = r;
-  out.scale = (float)(a * ((double)p.scale / (double)p.temperature) * weight * (double)p.state->each);
+  const double over = 1.0 / a;
+  for (int k = lane; k < n; k += 32) z[k] = (float)((double)z[k] * over);
+  out.scale = (float)(a * ((double)p.scale / (double)p.temperature) * weight * (double)each);
   return out;
 }
 
 // Sum of every block's weighted losses, by the block that comes last, in the blocks' order.
-__device__ __forceinline__ void add_totals(const HeadArgs& p, int block, double mine, double* warp_w) {
+__device__ __forceinline__ void add_totals(const HeadArgs& p, int block, double mine, float weights, double* warp_w) {
   __shared__ int last;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
@@ -281,7 +295,7 @@ __device__ __forceinline__ void add_totals(const HeadArgs& p, int block, double 
     sum = 0.0;
     for (int i = 0; i < kRowThreads / 32; ++i) sum += warp_w[i];
     p.totals[0] = (float)sum;
-    p.totals[1] = p.state->weight;
+    p.totals[1] = weights;
   }
 }
 
@@ -295,10 +309,31 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = blockIdx.x * kWarps + warp;
   double weighted = 0.0;
-  if (row < head_rows_here(p)) {
+  float weights, each;
+  if (p.few) {                                     // no kernel has been over the tokens before
+    double sum = 0.0;
+    for (int t = lane; t < p.tokens; t += 32)
+      if (head_entries(p, t) > 0) sum += p.weights ? (double)p.weights[t] : 1.0;
+    sum = warp_sum(sum);
+    weights = (float)sum;
+    each = part_of_each(p, sum);
+  } else {
+    weights = p.state->weight;
+    each = p.state->each;
+  }
+  const int token = row < head_rows_here(p) ? (p.few ? row : p.row_token[p.piece0 + row]) : -1;
+  const int n = token >= 0 ? head_entries(p, token) : 0;
+  if (p.few && token >= 0 && lane == 0) {
+    p.row_token[token] = token;
+    p.token_row[token] = n ? token : -1;
+    if (n == 0) {
+      p.loss[token] = 0.f;
+      if (p.lse) p.lse[token] = 0.f;
+      if (p.d_x) p.row_scale[row] = 0.f;
+    }
+  }
+  if (n) {
     const float2* stats = p.stats + (size_t)row * p.col_tiles;
-    const int token = p.row_token[p.piece0 + row];
-    const int n = p.labels ? 1 : p.list_n[token];
     float* z = p.z_listed + (size_t)row * p.top;
     float r = -INFINITY, s = 0.f;
     auto add = [&](float r2, float s2) {           // a sum of nothing has no say in R
@@ -318,8 +353,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
       const float r2 = __shfl_xor_sync(0xffffffffu, r, d), s2 = __shfl_xor_sync(0xffffffffu, s, d);
       add(r2, s2);
     }
-    const double lr = s == 0.f ? -INFINITY : (double)r * kLn2d + log((double)s);
-    const RowResult res = finish_row(p, token, n, lr, s == 0.f ? -INFINITY : (double)r, z, true);
+    const RowResult res = finish_row(p, token, n, (double)s, (double)r, each, z, true);
     if (lane == 0) weighted = res.weighted;
     if (p.d_x) {
       if (lane == 0) p.row_scale[row] = res.scale;
@@ -360,7 +394,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
   if (threadIdx.x == 0)
     for (int i = 0; i < kWarps; ++i) mine += warp_w[i];
   __syncthreads();
-  add_totals(p, p.piece0 / kWarps + blockIdx.x, mine, warp_w);
+  add_totals(p, p.piece0 / kWarps + blockIdx.x, mine, weights, warp_w);
 }
 
 // The fp32 mode's rows: a block a row, whose logits (x . w, as the product left them) become the gradient's factors.
@@ -418,8 +452,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_f32_kernel(HeadArgs p) 
       sum = 0.0;
       for (int i = 0; i < kWarps; ++i) sum += warp_w[i];
       // R of the others is their largest logit here (no tiles have to agree on one), as a power of two
-      const double lr = sum == 0.0 ? -INFINITY : (double)m + log(sum);
-      const RowResult res = finish_row(p, token, n, lr, sum == 0.0 ? -INFINITY : (double)m * kLog2ed, z, false);
+      const RowResult res = finish_row(p, token, n, sum, (double)m * kLog2ed, p.state->each, z, false);
       if (lane == 0) {
         weighted = res.weighted;
         row_r = res.r;
@@ -440,7 +473,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_f32_kernel(HeadArgs p) 
     }
   }
   __syncthreads();
-  add_totals(p, p.piece0 + blockIdx.x, weighted, warp_w);
+  add_totals(p, p.piece0 + blockIdx.x, weighted, p.state->weight, warp_w);
 }
 
 }  // namespace

@@ -181,7 +181,11 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
 }
 
 // 32 columns of one row of d_x
-__device__ __forceinline__ void grad_chunk(const HeadArgs& p, bf16* out, float by, int col, const uint32_t (&v)[32]) {
+__device__ __forceinline__ void grad_chunk(const HeadArgs& p, bf16* out, float by, bool none, int col, uint32_t (&v)[32]) {
+  if (none) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = 0u;
+  }
 #pragma unroll
   for (int j = 0; j < 32; j += 8)
     if (col + j < p.d)
@@ -347,10 +351,13 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
         tc_fence_after();
         const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile;
         float by = 0.f;
+        bool none = false;                               // a token that is left out, where the rows have such
         bf16* out = nullptr;
         if (live) {
+          const int token = p.row_token[p.piece0 + row];
           by = p.row_scale[row];
-          out = reinterpret_cast<bf16*>(p.d_x) + (size_t)p.row_token[p.piece0 + row] * p.dx_stride;
+          none = p.token_row[token] < 0;
+          out = reinterpret_cast<bf16*>(p.d_x) + (size_t)token * p.dx_stride;
         }
         if (t.tile >= 0) {
           // a share's partial sums, [chunk of 32 columns][4 columns][lane]: a warp's accesses cover 512 bytes at a time.
@@ -405,7 +412,7 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
                 v[4 * j] = __float_as_uint(sum[j].x); v[4 * j + 1] = __float_as_uint(sum[j].y);
                 v[4 * j + 2] = __float_as_uint(sum[j].z); v[4 * j + 3] = __float_as_uint(sum[j].w);
               }
-              if (live) grad_chunk(p, out, by, t.n0 + c, v);
+              if (live) grad_chunk(p, out, by, none, t.n0 + c, v);
             }
             if (lane == 0) *counter = 0;                 // ready for the next piece
           }
@@ -415,7 +422,7 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
           uint32_t v[32];
           tmem_ld32(acc + c, v);
           tmem_ld_wait();
-          if (live) grad_chunk(p, out, by, t.n0 + c, v);
+          if (live) grad_chunk(p, out, by, none, t.n0 + c, v);
         }
         tc_fence_before();
         __syncwarp();

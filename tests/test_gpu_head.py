@@ -244,3 +244,20 @@ def test_teacher_logits_at_the_edges(B):
     got = run(B, x, w, index, logit)
     torch.cuda.synchronize()
     assert got["loss"][5].isnan() and got["loss"].isnan().sum() == 1 and got["d_x"].isnan().any(1).sum() == 1
+
+
+@pytest.mark.parametrize("grad", [True, False], ids=["grad", "loss"])
+@pytest.mark.parametrize("t,v,d,top,softcap", [(16, 40001, 64, 0, 0.0), (17, 19300, 1096, 0, 8.0), (32, 700, 2056, 40, 0.0),
+                                               (33, 20011, 1032, 256, 5.0), (64, 40001, 136, 9, 0.0), (65, 20011, 1032, 33, 5.0),
+                                               (258, 38000, 1096, 3, 0.0)])
+def test_many_tiles_and_spans(B, t, v, d, top, softcap, grad):
+    # more tiles than a block takes at once, more reduction than one span, on both sides of the form for few tokens
+    g, x, w = rand(12, t, v, d, torch.bfloat16, 3.0)
+    opt = dict(softcap=softcap, z_loss=0.001)
+    if top:
+        index, logit = lists(g, t, v, top)
+        args = (index, logit, torch.logsumexp(logit, 1) + 0.2)
+    else:
+        args = (torch.randint(-v // 4, v, (t,), generator=g, device="cuda", dtype=torch.int32),)
+    weights = torch.rand(t, generator=g, device="cuda")
+    check(B, run(B, x, w, *args, weights=weights, grad=grad, **opt), want(x, w, *args, weights=weights, gradient=grad, **opt))
