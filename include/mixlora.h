@@ -409,15 +409,16 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
  *
  * x, d_x [T, d], w [vocab, d] of shape.dtype, 16-byte aligned, rows *_stride elements apart (0: dense); d_x must not
  * overlap an input.  d_model and the strides are multiples of 8.  Tokens that are left out cost nothing in the products.
- * Logits are sums in fp32.  Factors of the gradient's product are rounded once to shape.dtype (relatively, after all
+ * Logits are sums in fp32, and so are the gradients of the fp32 mode, where operands are taken apart into three bf16 values
+ * that hold their 24 bits (values below 2^-100 lose some).  Factors of the gradient's product are rounded once to shape.dtype (relatively, after all
  * differences have been taken, so that a confident token's small gradient keeps its precision); where a row's listed
  * columns hold more than 2^70 times the weight of all others, the others' part of the gradient may become zero.  Results
  * do not depend on the order in which blocks run.
  * An inf or NaN in a token's x makes its own loss and gradient NaN (and totals[0]), no other token's; one in w reaches every
  * token.  Tokens that are left out may hold anything.
- * The workspace (256-byte aligned, mixlora_head_workspace_bytes) is scratch of one call: whatever the batch, about 1.2 GB at
- * most beside a few numbers a token and the teacher's entries; calls that may run at the same time need one each;
- * mixlora_device_status works on it. */
+ * The workspace (256-byte aligned, mixlora_head_workspace_bytes) is scratch of one call: whatever the batch, about 1.2 GB (in
+ * fp32 mode 2.7 GB and 6 bytes for each value of w) at most beside a few numbers a token and the teacher's entries; calls
+ * that may run at the same time need one each; mixlora_device_status works on it. */
 #define MIXLORA_MAX_TEACHER_TOP 256
 typedef struct {
   uint32_t struct_size;       /* = sizeof(mixlora_head_shape_t) */

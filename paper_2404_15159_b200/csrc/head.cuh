@@ -24,8 +24,8 @@ constexpr int kHeadFewTokens = 64;
 constexpr int kHeadNone = 0x7fffffff;        // no column (ends a row's list)
 constexpr int kHeadMaxShares = 16;           // CTA pairs that share one tile's reduction
 constexpr int kHeadMaxItems = 222;           // shares under way: three rounds of 74 CTA pairs
-constexpr int kHeadCounters = 1024;          // one for each epilogue warp of a split tile (73 tiles of 8 warps at most)
-constexpr int kHeadSimtShares = 296;         // the same of the fp32 kernel's 128 x 128 tiles, two blocks an SM
+constexpr int kHeadMostPairs = 128;          // CTA pairs that a launch uses at most
+constexpr int kHeadCounters = 16 * kHeadMostPairs;   // one for each 32 x 128 corner of a shared tile
 constexpr int kHeadRowsPerBlock = 8;         // rows that a block of the joining kernel takes
 
 // What the kernels of a call leave for one another beside the arrays
@@ -60,10 +60,12 @@ struct HeadArgs {
   double *list_q, *rest_q;        // [tokens, top], [tokens] teacher probabilities, and what they leave over
   int32_t* list_n;                // [tokens] entries, 0: left out
   double* loss_part;              // sum of weight * loss for each block of the joining kernel
-  void* x_rows;                   // [piece, d] the counted rows of x, where some tokens are left out
+  void* x_rows;                   // [parts, piece, d] the counted rows of x, where some tokens are left out or in parts
+  bf16* w_parts;                  // [parts, vocab, d] fp32 mode: the head in parts
   float* z_listed;                // [piece, top] logits of the listed columns
   float2* stats;                  // [piece, col_tiles] (R, S)
-  void* e;                        // [piece, pitch]
+  void* e;                        // [parts, piece, pitch]
+  long long e_part;               // values from a part of E to the next
   float* row_scale;               // [piece]
   float* part;                    // partial tiles of a split reduction
   // the piece of counted rows that a launch works on
@@ -71,6 +73,7 @@ struct HeadArgs {
   int pitch, col_tiles;
   int join_blocks;                // of the joining kernel, over all pieces
   int part_items;                 // that `part` has room for
+  int parts;                      // bf16 values that hold an operand: 1, or 3 in the fp32 mode
   int few;                        // rows are tokens, those that are left out among them
 };
 
@@ -82,15 +85,26 @@ __device__ __forceinline__ int head_rows_here(const HeadArgs& p) {
   return min(max(p.state->counted - p.piece0, 0), p.piece);
 }
 
+// A value as the sum of three bf16 ones: the first is cut off (rounding could overflow), the others are rounded, which
+// leaves nothing of 24 bits.
+struct HeadParts { float v[3]; };
+__device__ __forceinline__ HeadParts head_parts(float x) {
+  HeadParts p;
+  p.v[0] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  const float rest = x - p.v[0];
+  p.v[1] = __bfloat162float(__float2bfloat16(rest));
+  p.v[2] = rest - p.v[1];
+  return p;
+}
+
 cudaError_t launch_head_lists(const HeadArgs& p, cudaStream_t st);        // a teacher's entries: list, list_q, rest_q, list_n
 cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st);   // row_token, token_row, state; clears counters
-cudaError_t launch_head_gather(const HeadArgs& p, bool bf16_mode, bool first_piece, cudaStream_t st);   // x_rows, zeroes of d_x
-cudaError_t launch_head_join(const HeadArgs& p, bool bf16_mode, cudaStream_t st);      // loss, lse, totals; E finished, row_scale
+cudaError_t launch_head_parts(const HeadArgs& p, cudaStream_t st);        // fp32 mode: w_parts
+cudaError_t launch_head_gather(const HeadArgs& p, bool first_piece, cudaStream_t st);   // x_rows, zeroes of d_x
 cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st);    // stats, z_listed, E
-cudaError_t launch_head_grad_tc(const HeadArgs& p, cudaStream_t st);      // d_x
 cudaError_t launch_head_logits_few(const HeadArgs& p, bool first, cudaStream_t st);   // the same for up to kHeadFewTokens; clears the state
-cudaError_t launch_head_logits_simt(const HeadArgs& p, cudaStream_t st);
-cudaError_t launch_head_grad_simt(const HeadArgs& p, cudaStream_t st);
+cudaError_t launch_head_join(const HeadArgs& p, cudaStream_t st);         // loss, lse, totals; E finished, row_scale
+cudaError_t launch_head_grad_tc(const HeadArgs& p, cudaStream_t st);      // d_x
 int head_pairs();                                                         // CTA pairs of this GPU
 
 }  // namespace mixlora

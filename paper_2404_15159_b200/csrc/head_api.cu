@@ -42,14 +42,13 @@ mixlora_status_t check_head(const mixlora_head_shape_t* s) {
   return MIXLORA_OK;
 }
 
-// Counted rows are worked on in pieces, as many as keep a piece's exponentials (fp32 mode: logits) within 512 MiB: enough
-// for whole rounds of tiles, and the same whatever the batch.  Without a gradient bf16 keeps two numbers for 128 columns,
-// and the copy of the rows of x is what counts.
-int piece_rows(const mixlora_head_shape_t& s, bool gradient) {
-  const bool bf16_mode = s.dtype == MIXLORA_DTYPE_BF16;
-  long long row = bf16_mode ? (gradient ? (long long)s.vocab * 2 : (long long)((s.vocab + kHeadCols - 1) / kHeadCols) * 8)
-                            : (long long)s.vocab * 4;
-  if (bf16_mode && row < 2LL * s.d_model) row = 2LL * s.d_model;
+// Counted rows are worked on in pieces, as many as keep a piece's exponentials within 512 MiB: enough for whole rounds of
+// tiles, and the same whatever the batch.  Without a gradient there are two numbers for 128 columns, and the copy of the
+// rows of x is what counts.
+int piece_rows(const mixlora_head_shape_t& s, bool gradient, int parts) {
+  long long row = 2LL * parts * s.d_model;
+  const long long wide = gradient ? 2LL * parts * s.vocab : (s.vocab + kHeadCols - 1) / kHeadCols * 8LL;
+  if (row < wide) row = wide;
   long long rows = (512LL << 20) / row / kHeadTile * kHeadTile;
   if (rows < kHeadTile) rows = kHeadTile;
   const long long all = ((long long)s.tokens + kHeadTile - 1) / kHeadTile * kHeadTile;
@@ -57,20 +56,19 @@ int piece_rows(const mixlora_head_shape_t& s, bool gradient) {
 }
 
 struct HeadLayout {
-  size_t state, counters, row_token, token_row, list, list_q, rest_q, list_n, loss_part, x_rows, z_listed, stats, e, row_scale,
-      part, total;
-  int piece, pieces, pitch, col_tiles, join_blocks, part_items;
+  size_t state, counters, row_token, token_row, list, list_q, rest_q, list_n, loss_part, x_rows, w_parts, z_listed, stats, e,
+      row_scale, part, total;
+  int parts, piece, pieces, pitch, col_tiles, join_blocks, part_items;
 };
 HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
-  const bool bf16_mode = s.dtype == MIXLORA_DTYPE_BF16;
   const size_t tokens = (size_t)s.tokens, top = s.teacher_top ? (size_t)s.teacher_top : 1;
   HeadLayout L;
-  L.piece = piece_rows(s, gradient);
+  L.parts = s.dtype == MIXLORA_DTYPE_BF16 ? 1 : 3;
+  L.piece = piece_rows(s, gradient, L.parts);
   L.pieces = (s.tokens + L.piece - 1) / L.piece;
   L.pitch = (s.vocab + 7) / 8 * 8;
   L.col_tiles = (s.vocab + kHeadCols - 1) / kHeadCols;
-  const int per_block = bf16_mode ? kHeadRowsPerBlock : 1;
-  L.join_blocks = L.pieces * (L.piece / per_block);
+  L.join_blocks = L.pieces * (L.piece / kHeadRowsPerBlock);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
   L.state = take(sizeof(HeadState));
@@ -84,18 +82,17 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   L.list_n = take(lists * 4);
   L.loss_part = take((size_t)L.join_blocks * 8);
   const size_t piece = (size_t)L.piece;
-  L.x_rows = take(bf16_mode ? piece * s.d_model * 2 : 0);
+  L.x_rows = take(piece * s.d_model * 2 * L.parts);
+  L.w_parts = take(L.parts == 3 ? (size_t)s.vocab * s.d_model * 6 : 0);
   L.z_listed = take(piece * top * 4);
-  L.stats = take(bf16_mode ? (size_t)L.col_tiles * piece * 8 : 0);
-  L.e = take(bf16_mode ? (gradient ? piece * L.pitch * 2 : 0) : piece * L.pitch * 4);
+  L.stats = take((size_t)L.col_tiles * piece * 8);
+  L.e = take(gradient ? piece * L.pitch * 2 * L.parts : 0);
   L.row_scale = take(gradient ? piece * 4 : 0);
   // shares of the second product's tiles: no more than its tiles can be split into
   const size_t tiles = piece / kHeadTile * ((size_t)(s.d_model + kHeadTile - 1) / kHeadTile);
   const size_t items = tiles * kHeadMaxShares;
   L.part_items = gradient ? (int)(items < kHeadMaxItems ? items : kHeadMaxItems) : 0;
-  // the fp32 kernel's tiles are a quarter as large, and there are at most 4 blocks a pair of SMs of them
-  L.part = take(gradient ? (bf16_mode ? (size_t)L.part_items * kHeadTile * kHeadTile * 4
-                                      : (size_t)kHeadSimtShares * (kHeadTile * kHeadTile / 4) * 4) : 0);
+  L.part = take((size_t)L.part_items * kHeadTile * kHeadTile * 4);
   L.total = off;
   return L;
 }
@@ -114,7 +111,7 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
       !aligned_or_null(c.lse, 4) || !aligned_or_null(c.totals, 4) || !aligned_or_null(c.weights, 4) ||
       !aligned_or_null(c.normalizer, 4) || c.d_x == c.x)
     return MIXLORA_ERR_INVALID_ARG;
-  const bool gradient = c.d_x != nullptr, bf16_mode = s->dtype == MIXLORA_DTYPE_BF16;
+  const bool gradient = c.d_x != nullptr;
   const HeadLayout L = head_layout(*s, gradient);
   if (!aligned(workspace, 256) || workspace_bytes < L.total) return MIXLORA_ERR_WORKSPACE;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -149,30 +146,34 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   a.rest_q = reinterpret_cast<double*>(ws + L.rest_q);
   a.list_n = reinterpret_cast<int32_t*>(ws + L.list_n);
   a.loss_part = reinterpret_cast<double*>(ws + L.loss_part);
-  a.x_rows = bf16_mode ? ws + L.x_rows : nullptr;
+  a.x_rows = ws + L.x_rows;
+  a.w_parts = reinterpret_cast<bf16*>(ws + L.w_parts);
   a.z_listed = reinterpret_cast<float*>(ws + L.z_listed);
   a.stats = reinterpret_cast<float2*>(ws + L.stats);
-  a.e = reinterpret_cast<float*>(ws + L.e);
+  a.e = ws + L.e;
+  a.e_part = (long long)L.piece * L.pitch;
+  a.parts = L.parts;
   a.row_scale = reinterpret_cast<float*>(ws + L.row_scale);
   a.part = reinterpret_cast<float*>(ws + L.part);
   a.piece = L.piece; a.pitch = L.pitch; a.col_tiles = L.col_tiles;
   a.join_blocks = L.join_blocks; a.part_items = L.part_items;
 
   if (!c.labels) MIXLORA_TRY(launch_head_lists(a, st));
-  if (bf16_mode && s->tokens <= kHeadFewTokens) {
+  if (L.parts == 1 && s->tokens <= kHeadFewTokens) {
     a.few = 1;
     MIXLORA_TRY(launch_head_logits_few(a, c.labels != nullptr, st));
-    MIXLORA_TRY(launch_head_join(a, true, st));
+    MIXLORA_TRY(launch_head_join(a, st));
     if (gradient) MIXLORA_TRY(launch_head_grad_tc(a, st));
     return MIXLORA_OK;
   }
   MIXLORA_TRY(launch_head_scan(a, c.labels != nullptr, st));
+  if (L.parts == 3) MIXLORA_TRY(launch_head_parts(a, st));
   for (int i = 0; i < L.pieces; ++i) {
     a.piece0 = i * L.piece;
-    if (bf16_mode || (gradient && i == 0)) MIXLORA_TRY(launch_head_gather(a, bf16_mode, i == 0, st));
-    MIXLORA_TRY(bf16_mode ? launch_head_logits_tc(a, st) : launch_head_logits_simt(a, st));
-    MIXLORA_TRY(launch_head_join(a, bf16_mode, st));
-    if (gradient) MIXLORA_TRY(bf16_mode ? launch_head_grad_tc(a, st) : launch_head_grad_simt(a, st));
+    MIXLORA_TRY(launch_head_gather(a, i == 0, st));
+    MIXLORA_TRY(launch_head_logits_tc(a, st));
+    MIXLORA_TRY(launch_head_join(a, st));
+    if (gradient) MIXLORA_TRY(launch_head_grad_tc(a, st));
   }
   return MIXLORA_OK;
 }

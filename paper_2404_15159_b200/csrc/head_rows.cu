@@ -25,6 +25,20 @@ __device__ __forceinline__ double warp_max(double v) {
   return v;
 }
 
+// A row of n fp32 values (a multiple of 8) into three rows of bf16, `apart` values from one to the next, by a warp
+__device__ __forceinline__ void take_apart(const float* src, bf16* dst, size_t apart, int n) {
+  for (int i = (threadIdx.x & 31) * 4; i < n; i += 128) {
+    const float4 v = *reinterpret_cast<const float4*>(src + i);
+    const HeadParts a = head_parts(v.x), b = head_parts(v.y), c = head_parts(v.z), d = head_parts(v.w);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(a.v[k], b.v[k]), up = __floats2bfloat162_rn(c.v[k], d.v[k]);
+      *reinterpret_cast<uint2*>(dst + k * apart + i) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&up));
+    }
+  }
+}
+
 // A teacher's entries of one token, a warp each: columns ascending, an entry outside the vocabulary dropped, entries of the
 // same column added up; their probabilities and what they leave over.  An entry's place is the number of entries before
 // it, counted by comparing it with all (at most 256 x 256 / 32 steps of a warp).
@@ -167,24 +181,43 @@ __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
   }
 }
 
-// Where tokens are left out: the counted rows of this piece side by side (the products then pass over nothing else), and
-// zeroes for the gradients of the others.  A warp a token.
-template <typename T>
+// The counted rows of this piece side by side, where tokens are left out (the products then pass over nothing else) or an
+// fp32 row is taken apart, and zeroes for the gradients of the tokens that are left out.  A warp a token.
+template <int PARTS>
 __global__ void __launch_bounds__(kRowThreads) head_gather_kernel(HeadArgs p, int zeroes) {
   let_next_start();
   wait_for_last();
-  if (p.state->counted == p.tokens) return;
+  if (PARTS == 1 && p.state->counted == p.tokens) return;
   const int lane = threadIdx.x & 31;
   const int t = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
   if (t >= p.tokens) return;
-  const int row = p.token_row[t] - p.piece0;
-  const bool left_out = row + p.piece0 < 0;
-  if (left_out ? !(zeroes && p.d_x) : (row < 0 || row >= p.piece || !p.x_rows)) return;
-  constexpr int kEach = 16 / sizeof(T);
-  const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(p.x) + (size_t)t * p.x_stride);
-  uint4* dst = left_out ? reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.d_x) + (size_t)t * p.dx_stride)
-                        : reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.x_rows) + (size_t)row * p.d);
-  for (int i = lane; i < p.d / kEach; i += 32) dst[i] = left_out ? make_uint4(0, 0, 0, 0) : src[i];
+  const int at = p.token_row[t], row = at - p.piece0;
+  if (at < 0) {
+    if (!zeroes || !p.d_x) return;
+    constexpr int kEach = PARTS == 1 ? 8 : 4;              // values of 16 bytes
+    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<char*>(p.d_x) + (size_t)t * p.dx_stride * (16 / kEach));
+    for (int i = lane; i < p.d / kEach; i += 32) dst[i] = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  if (row < 0 || row >= p.piece) return;
+  if (PARTS == 1) {
+    const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.x) + (size_t)t * p.x_stride);
+    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(p.x_rows) + (size_t)row * p.d);
+    for (int i = lane; i < p.d / 8; i += 32) dst[i] = src[i];
+  } else {
+    take_apart(reinterpret_cast<const float*>(p.x) + (size_t)t * p.x_stride,
+               reinterpret_cast<bf16*>(p.x_rows) + (size_t)row * p.d, (size_t)p.piece * p.d, p.d);
+  }
+}
+
+// The head in parts, a warp a row: memory's 10 bytes a value
+__global__ void __launch_bounds__(kRowThreads) head_parts_kernel(HeadArgs p) {
+  let_next_start();
+  wait_for_last();
+  const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
+  if (row >= p.vocab) return;
+  take_apart(reinterpret_cast<const float*>(p.w) + (size_t)row * p.w_stride, p.w_parts + (size_t)row * p.d,
+             (size_t)p.vocab * p.d, p.d);
 }
 
 // In 64 bits, out of line: a row needs several, and their code would not stay in the instruction cache otherwise
@@ -353,7 +386,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
       const float r2 = __shfl_xor_sync(0xffffffffu, r, d), s2 = __shfl_xor_sync(0xffffffffu, s, d);
       add(r2, s2);
     }
-    const RowResult res = finish_row(p, token, n, (double)s, (double)r, each, z, true);
+    const RowResult res = finish_row(p, token, n, (double)s, (double)r, each, z, p.parts == 1);
     if (lane == 0) weighted = res.weighted;
     if (p.d_x) {
       if (lane == 0) p.row_scale[row] = res.scale;
@@ -370,8 +403,9 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
           todo &= todo - 1;
           const float f = exp2f(__shfl_sync(0xffffffffu, by, l));
           const int c = (i0 + l) * kHeadCols + lane * 4;
-          if (c < p.pitch) {
-            uint2* at = reinterpret_cast<uint2*>(e + c);
+          if (c >= p.pitch) continue;
+          for (int k = 0; k < p.parts; ++k) {
+            uint2* at = reinterpret_cast<uint2*>(e + k * p.e_part + c);
             uint2 v = *at;
             __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
@@ -385,7 +419,15 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
       }
       __syncwarp();
       const int32_t* list = p.list + (size_t)token * p.top;
-      for (int k = lane; k < n; k += 32) e[list[k]] = __float2bfloat16(z[k]);
+      for (int k = lane; k < n; k += 32) {
+        if (p.parts == 1) {
+          e[list[k]] = __float2bfloat16(z[k]);
+        } else {
+          const HeadParts v = head_parts(z[k]);
+#pragma unroll
+          for (int j = 0; j < 3; ++j) e[j * p.e_part + list[k]] = __float2bfloat16(v.v[j]);
+        }
+      }
     }
   }
   if (lane == 0) warp_w[warp] = weighted;
@@ -395,85 +437,6 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
     for (int i = 0; i < kWarps; ++i) mine += warp_w[i];
   __syncthreads();
   add_totals(p, p.piece0 / kWarps + blockIdx.x, mine, weights, warp_w);
-}
-
-// The fp32 mode's rows: a block a row, whose logits (x . w, as the product left them) become the gradient's factors.
-__global__ void __launch_bounds__(kRowThreads) head_join_f32_kernel(HeadArgs p) {
-  constexpr int kWarps = kRowThreads / 32;
-  let_next_start();
-  wait_for_last();
-  __shared__ float warp_m[kWarps];
-  __shared__ double warp_w[kWarps], row_r;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x;
-  double weighted = 0.0;
-  if (row < head_rows_here(p)) {
-    float* e = reinterpret_cast<float*>(p.e) + (size_t)row * p.pitch;
-    float* z = p.z_listed + (size_t)row * p.top;
-    const int token = p.row_token[p.piece0 + row];
-    const int n = p.labels ? 1 : p.list_n[token];
-    const int32_t* list = p.list + (size_t)token * p.top;
-    // the listed logits leave the row
-    if (warp == 0) {
-      for (int k = lane; k < n; k += 32) {
-        const float raw = e[list[k]] * p.logit_factor;
-        z[k] = p.softcap > 0.f ? tanhf(raw) * p.cap_out : raw;
-        e[list[k]] = -INFINITY;
-      }
-    }
-    __syncthreads();
-    float m = -INFINITY;
-    for (int c = threadIdx.x; c < p.vocab; c += kRowThreads) m = fmaxf(m, e[c]);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if (lane == 0) warp_m[warp] = m;
-    __syncthreads();
-    m = warp_m[0];
-    for (int i = 1; i < kWarps; ++i) m = fmaxf(m, warp_m[i]);
-    m *= p.logit_factor;
-    if (p.softcap > 0.f) m = tanhf(m) * p.cap_out;
-    if (m == -INFINITY) m = 0.f;
-    double sum = 0.0;
-    for (int c = threadIdx.x; c < p.vocab; c += kRowThreads) {
-      float v = e[c] * p.logit_factor, slope = 1.f;
-      const bool gone = e[c] == -INFINITY;
-      if (p.softcap > 0.f) {
-        const float t = tanhf(v);
-        v = t * p.cap_out;
-        slope = (1.f - t) * (1.f + t);
-      }
-      const float ex = gone ? 0.f : expf(v - m);
-      sum += (double)ex;
-      if (p.d_x) e[c] = ex * slope;
-    }
-    sum = warp_sum(sum);
-    if (lane == 0) warp_w[warp] = sum;
-    __syncthreads();
-    if (warp == 0) {
-      sum = 0.0;
-      for (int i = 0; i < kWarps; ++i) sum += warp_w[i];
-      // R of the others is their largest logit here (no tiles have to agree on one), as a power of two
-      const RowResult res = finish_row(p, token, n, sum, (double)m * kLog2ed, p.state->each, z, false);
-      if (lane == 0) {
-        weighted = res.weighted;
-        row_r = res.r;
-        if (p.d_x) p.row_scale[row] = res.scale;
-      }
-    }
-    __syncthreads();
-    if (p.d_x) {
-      // e is over e^m, the row over 2^R
-      const double by = (double)m * kLog2ed - row_r;
-      if (by < 0.0) {
-        const float f = (float)exp2(by);
-        for (int c = threadIdx.x; c < p.vocab; c += kRowThreads) e[c] *= f;
-      }
-      __syncthreads();
-      if (warp == 0)
-        for (int k = lane; k < n; k += 32) e[list[k]] = z[k];
-    }
-  }
-  __syncthreads();
-  add_totals(p, p.piece0 + blockIdx.x, weighted, p.state->weight, warp_w);
 }
 
 }  // namespace
@@ -491,14 +454,18 @@ cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_head_gather(const HeadArgs& p, bool bf16_mode, bool first_piece, cudaStream_t st) {
-  const unsigned blocks = (unsigned)((p.tokens + kRowThreads / 32 - 1) / (kRowThreads / 32));
-  return bf16_mode ? launch_behind(head_gather_kernel<bf16>, blocks, kRowThreads, 0, st, p, first_piece ? 1 : 0)
-                   : launch_behind(head_gather_kernel<float>, blocks, kRowThreads, 0, st, p, first_piece ? 1 : 0);
+cudaError_t launch_head_parts(const HeadArgs& p, cudaStream_t st) {
+  const unsigned blocks = (unsigned)((p.vocab + kRowThreads / 32 - 1) / (kRowThreads / 32));
+  return launch_behind(head_parts_kernel, blocks, kRowThreads, 0, st, p);
 }
 
-cudaError_t launch_head_join(const HeadArgs& p, bool bf16_mode, cudaStream_t st) {
-  if (!bf16_mode) return launch_behind(head_join_f32_kernel, (unsigned)p.piece, kRowThreads, 0, st, p);
+cudaError_t launch_head_gather(const HeadArgs& p, bool first_piece, cudaStream_t st) {
+  const unsigned blocks = (unsigned)((p.tokens + kRowThreads / 32 - 1) / (kRowThreads / 32));
+  return p.parts == 1 ? launch_behind(head_gather_kernel<1>, blocks, kRowThreads, 0, st, p, first_piece ? 1 : 0)
+                      : launch_behind(head_gather_kernel<3>, blocks, kRowThreads, 0, st, p, first_piece ? 1 : 0);
+}
+
+cudaError_t launch_head_join(const HeadArgs& p, cudaStream_t st) {
   return launch_behind(head_join_kernel, (unsigned)((p.piece + kHeadRowsPerBlock - 1) / kHeadRowsPerBlock), kRowThreads, 0, st, p);
 }
 

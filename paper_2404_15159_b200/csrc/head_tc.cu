@@ -1,12 +1,20 @@
 // The two products of the head's losses on the tensor cores (tcgen05, TMEM, TMA; bf16 operands, fp32 accumulation).
 //
-//   logits   x [rows, d] . w [vocab, d]^T   per tile of 256 columns: R, S, the listed logits and, for a gradient, E
+//   logits   x [rows, d] . w [vocab, d]^T   per 128 columns: R, S, the listed logits and, for a gradient, E
 //   grad     E [rows, vocab] . w [vocab, d]  times the row's A scale / temperature weight / normalizer, to the row's token
 //
 // Pairs of CTAs work on 256 x 256 tiles (cta_group::2, 128 rows of the accumulator and half of B's columns each), one
-// persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the products, the other warps turn a finished
-// accumulator into its result while the second one is filled.  The number of rows is read on the device: tokens without a
-// label take no part.
+// persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the products, warps 2 to 9 take finished sums into
+// registers, 128 columns of one row a thread, and turn them into results while the next sums are under way.  The number of
+// rows is read on the device: tokens without a label take no part.
+//
+// The tensor core cuts off what a sum has behind its 24 bits, at every step of 16 products: over 4096 of them that is a few
+// 2^-20 of a logit, always towards zero.  So a sum starts anew every span of k-blocks, and the parts are added up in
+// registers, rounded to nearest.
+//
+// In the fp32 mode (PARTS = 3) an operand is the sum of three bf16 values that hold its 24 bits, and the six products of
+// parts that matter at 2^-24 are added up, the small ones first: exact to fp32's own rounding, at a sixth of the rate, which
+// is still three times that of the fp32 pipes.
 #include <cuda.h>
 #include <math.h>
 
@@ -18,18 +26,21 @@ namespace {
 
 using namespace tc;
 constexpr int kBK = 64, kUmmaK = 16, kTile = kHeadTile;
-constexpr int kStages = 6;
-// warps that take finished accumulators: the logits need two for each quarter of the rows, 128 columns a thread
-constexpr int result_warps(bool to_x) { return to_x ? 4 : 8; }
-constexpr int threads_of(bool to_x) { return 64 + 32 * result_warps(to_x); }
-// k-blocks of a logit that the tensor core adds up before the sum is taken on in registers (see logits_rows)
-constexpr int kSpan = 16;
-constexpr uint32_t kABytes = 128 * kBK * 2, kBBytes = 128 * kBK * 2, kStageBytes = kABytes + kBBytes;
-constexpr uint32_t kSmemBytes = kStages * kStageBytes + 1024 + 256;
+constexpr int kResultWarps = 8, kThreads = 64 + 32 * kResultWarps;
+constexpr uint32_t kHalf = 128 * kBK * 2;                 // bytes of one CTA's part of an operand, one k-block
 constexpr uint32_t kTmemCols = 512;
-// a share of a split reduction keeps at least this many k-blocks, and costs this many on top (fp32 partials out and in)
-constexpr int kShareMin = 16, kShareCost = 24;
-
+template <bool TO_X, int PARTS> struct Form {
+  static constexpr int kStages = PARTS == 1 ? 6 : 2;
+  static constexpr uint32_t kStage = PARTS * 2 * kHalf;
+  static constexpr uint32_t kSmem = kStages * kStage + 1024 + 256;
+  // k-blocks of a span: 64 steps of the tensor core (24 with parts).  The gradient's product is rounded to bf16 in the
+  // end, where 512 steps are nothing
+  static constexpr int kSpan = PARTS == 3 ? 1 : (TO_X ? 128 : 16);
+  // a share of a split reduction keeps at least this many k-blocks, and costs this many on top (partial sums out and in)
+  static constexpr int kShareMin = PARTS == 1 ? 16 : 3, kShareCost = PARTS == 1 ? 24 : 4;
+};
+// the six products of parts, small ones first
+__device__ constexpr int kPartOfA[6] = {2, 0, 1, 1, 0, 0}, kPartOfB[6] = {0, 2, 1, 0, 1, 0};
 struct alignas(64) HeadMaps { CUtensorMap a, a_rows, b; };
 
 // How the tiles are dealt out.  Whole rounds of pairs take a tile each, in groups of row tiles (rows fastest) whose
@@ -39,12 +50,13 @@ struct Plan {
   int m_tiles, n_tiles, group, k_blocks;
   int whole, shares, items;          // tiles taken whole, shares of each other tile, items altogether
 };
-__device__ __forceinline__ Plan make_plan(int rows, int n_tiles, int k_blocks, int pairs, int most_items, bool split) {
+template <bool TO_X, int PARTS>
+__device__ __forceinline__ Plan make_plan(int rows, int n_tiles, int k_blocks, int pairs, int most_items) {
   Plan t;
   t.m_tiles = (rows + kTile - 1) / kTile;
   t.n_tiles = n_tiles;
   t.k_blocks = k_blocks;
-  const long long slice = (long long)kTile * k_blocks * kBK * 2;
+  const long long slice = (long long)kTile * k_blocks * kBK * 2 * PARTS;
   const int fit = (int)((40ll << 20) / slice);
   if (fit >= t.m_tiles) t.group = max(t.m_tiles, 1);
   else if (fit >= 8) { const int groups = (t.m_tiles + fit - 1) / fit; t.group = (t.m_tiles + groups - 1) / groups; }
@@ -52,10 +64,10 @@ __device__ __forceinline__ Plan make_plan(int rows, int n_tiles, int k_blocks, i
   const int tiles = t.m_tiles * n_tiles, rest = tiles % pairs;
   t.whole = tiles;
   t.shares = 1;
-  if (split && rest) {
+  if (TO_X && rest) {
     int best = k_blocks;
-    for (int s = 2; s <= kHeadMaxShares && s * kShareMin <= k_blocks && s * rest <= most_items; ++s) {
-      const int cost = (rest * s + pairs - 1) / pairs * ((k_blocks + s - 1) / s + kShareCost);
+    for (int s = 2; s <= kHeadMaxShares && s * Form<TO_X, PARTS>::kShareMin <= k_blocks && s * rest <= most_items; ++s) {
+      const int cost = (rest * s + pairs - 1) / pairs * ((k_blocks + s - 1) / s + Form<TO_X, PARTS>::kShareCost);
       if (cost < best) { best = cost; t.shares = s; }
     }
     if (t.shares > 1) t.whole = tiles - rest;
@@ -96,7 +108,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // One row of 128 logits, in registers, by one thread: the listed ones are put aside, the others become exponentials.
-template <bool GRAD, bool CAP>
+template <bool GRAD, bool CAP, int PARTS>
 __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCols], int n0, int row, bool live) {
   constexpr int kChunks = kHeadCols / 32;
   const int token = live ? p.row_token[p.piece0 + row] : 0;
@@ -171,40 +183,100 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     if (GRAD && live) {
 #pragma unroll
       for (int j = 32 * c; j < 32 * c + 32; j += 8)
-        if (n0 + j < p.pitch)
-          *reinterpret_cast<uint4*>(e + j) = make_uint4(pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
-                                                        pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
+        if (n0 + j < p.pitch) {
+          if constexpr (PARTS == 1) {
+            *reinterpret_cast<uint4*>(e + j) = make_uint4(pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
+                                                          pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
+          } else {
+            uint32_t part[3][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const HeadParts lo = head_parts(x[j + 2 * i]), up = head_parts(x[j + 2 * i + 1]);
+#pragma unroll
+              for (int n = 0; n < 3; ++n) part[n][i] = pack_bf16(lo.v[n], up.v[n]);
+            }
+#pragma unroll
+            for (int n = 0; n < 3; ++n)
+              *reinterpret_cast<uint4*>(e + n * p.e_part + j) = make_uint4(part[n][0], part[n][1], part[n][2], part[n][3]);
+          }
+        }
     }
   }
   if (live && n0 < p.vocab)
     p.stats[(size_t)row * p.col_tiles + n0 / kHeadCols] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
 }
 
-// 32 columns of one row of d_x
-__device__ __forceinline__ void grad_chunk(const HeadArgs& p, bf16* out, float by, bool none, int col, uint32_t (&v)[32]) {
-  if (none) {
+// One row of 128 sums of the gradient's product.  Where a tile's reduction is shared, the sums go to `part`, [4 columns]
+// [lane] so that a warp's accesses cover 512 bytes, and the warp that completes its 32 x 128 corner of the tile adds the
+// shares up in their order, whoever it is.
+template <int PARTS>
+__device__ __forceinline__ void grad_row(const HeadArgs& p, float (&x)[kHeadCols], const Plan& plan, const Item& t, int corner,
+                                         int n0, int row, bool live) {
+  const int lane = threadIdx.x & 31;
+  if (t.tile >= 0) {
+    constexpr size_t kCorner = 32 * kHeadCols, kAll = 16 * kCorner;          // floats of a corner, of a tile
+    const float* first = p.part + (size_t)t.tile * plan.shares * kAll + corner * kCorner + lane * 4;
+    float* to = p.part + (size_t)(t.tile * plan.shares + t.share) * kAll + corner * kCorner + lane * 4;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = 0u;
+    for (int j = 0; j < kHeadCols; j += 4)
+      *reinterpret_cast<float4*>(to + j * 32) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+    __threadfence();
+    __syncwarp();
+    int seen = 0;
+    int* counter = p.counters + t.tile * 16 + corner;
+    if (lane == 0) seen = atomicAdd(counter, 1);
+    if (__shfl_sync(0xffffffffu, seen, 0) != plan.shares - 1) return;
+    __threadfence();
+#pragma unroll
+    for (int c = 0; c < kHeadCols; c += 32) {
+      float4 sum[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < plan.shares; ++s) {
+        float4 w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = __ldcg(reinterpret_cast<const float4*>(first + s * kAll + (c + 4 * j) * 32));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sum[j].x += w[j].x; sum[j].y += w[j].y; sum[j].z += w[j].z; sum[j].w += w[j].w;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[c + 4 * j] = sum[j].x; x[c + 4 * j + 1] = sum[j].y; x[c + 4 * j + 2] = sum[j].z; x[c + 4 * j + 3] = sum[j].w;
+      }
+    }
+    if (lane == 0) *counter = 0;                           // ready for the next piece
   }
+  if (!live) return;
+  const int token = p.row_token[p.piece0 + row];
+  const float by = p.row_scale[row];
+  const bool none = p.few && p.token_row[token] < 0;       // a token that is left out: its sums may be anything
 #pragma unroll
-  for (int j = 0; j < 32; j += 8)
-    if (col + j < p.d)
-      *reinterpret_cast<uint4*>(out + col + j) =
-          make_uint4(pack_bf16(by * __uint_as_float(v[j]), by * __uint_as_float(v[j + 1])),
-                     pack_bf16(by * __uint_as_float(v[j + 2]), by * __uint_as_float(v[j + 3])),
-                     pack_bf16(by * __uint_as_float(v[j + 4]), by * __uint_as_float(v[j + 5])),
-                     pack_bf16(by * __uint_as_float(v[j + 6]), by * __uint_as_float(v[j + 7])));
+  for (int j = 0; j < kHeadCols; ++j) x[j] = none ? 0.f : by * x[j];
+  if constexpr (PARTS == 1) {
+    bf16* out = reinterpret_cast<bf16*>(p.d_x) + (size_t)token * p.dx_stride + n0;
+#pragma unroll
+    for (int j = 0; j < kHeadCols; j += 8)
+      if (n0 + j < p.d)
+        *reinterpret_cast<uint4*>(out + j) = make_uint4(pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
+                                                        pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
+  } else {
+    float* out = reinterpret_cast<float*>(p.d_x) + (size_t)token * p.dx_stride + n0;
+#pragma unroll
+    for (int j = 0; j < kHeadCols; j += 4)
+      if (n0 + j < p.d) *reinterpret_cast<float4*>(out + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+  }
 }
 
-enum { kLogits = 0, kLogitsGrad = 1, kLogitsCap = 2, kLogitsCapGrad = 3, kGrad = 4 };
-
-template <int MODE>
-__global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(const __grid_constant__ HeadArgs p,
+template <bool TO_X, bool GRAD, bool CAP, int PARTS>
+__global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_constant__ HeadArgs p,
                                                               const __grid_constant__ HeadMaps maps) {
-  constexpr bool kToX = MODE == kGrad;                    // the second product: B is [K, N]
+  using F = Form<TO_X, PARTS>;
+  constexpr int kStages = F::kStages;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * F::kStage);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -219,7 +291,7 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
   let_next_start();
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * result_warps(kToX)); }
+    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * kResultWarps); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tmap(&maps.a); prefetch_tmap(&maps.a_rows); prefetch_tmap(&maps.b);
@@ -237,16 +309,16 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
 
   const int rows = head_rows_here(p);
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const Plan plan = kToX ? make_plan(rows, (p.d + kTile - 1) / kTile, (p.vocab + kBK - 1) / kBK, pairs, p.part_items, true)
-                         : make_plan(rows, (p.vocab + kTile - 1) / kTile, (p.d + kBK - 1) / kBK, pairs, 0, false);
+  const Plan plan = make_plan<TO_X, PARTS>(rows, ((TO_X ? p.d : p.vocab) + kTile - 1) / kTile,
+                                           ((TO_X ? p.vocab : p.d) + kBK - 1) / kBK, pairs, p.part_items);
 
   if (warp == 0) {
     // ---------------- loads (both CTAs, each its own halves) ----------------
     if (lane == 0) {
-      // where every token counts, x itself holds the rows
-      const bool direct = kToX || p.state->counted == p.tokens;
+      // where every token counts, x itself holds the rows (not its parts)
+      const bool direct = !TO_X && PARTS == 1 && p.state->counted == p.tokens;
       const CUtensorMap* am = direct ? &maps.a : &maps.a_rows;
-      const int row0 = kToX || !direct ? 0 : p.piece0;
+      const int row0 = direct ? p.piece0 : 0;
       uint32_t it = 0;
       bool ok = true;
       for (int i = pair; i < plan.items && ok; i += pairs) {
@@ -255,15 +327,18 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const int st = it % kStages;
           if (!mbar_wait(empty_bar(st), ((it / kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-          const uint32_t a_dst = smem_base + st * kStageBytes, b_dst = a_dst + kABytes;
+          const uint32_t a_dst = smem_base + st * F::kStage, b_dst = a_dst + PARTS * kHalf;
           const uint32_t bar = map_to_cta(full_bar(st), 0);
-          if (leader) mbar_expect_tx(full_bar(st), 2 * kStageBytes);
-          tma_load_2d_pair(a_dst, am, bar, kb * kBK, m0);
-          if (kToX) {
-            tma_load_2d_pair(b_dst, &maps.b, bar, n0, kb * kBK);
-            tma_load_2d_pair(b_dst + kBK * 128, &maps.b, bar, n0 + 64, kb * kBK);
-          } else {
-            tma_load_2d_pair(b_dst, &maps.b, bar, kb * kBK, n0);
+          if (leader) mbar_expect_tx(full_bar(st), 2 * F::kStage);
+#pragma unroll
+          for (int n = 0; n < PARTS; ++n) {
+            tma_load_2d_pair(a_dst + n * kHalf, am, bar, kb * kBK, m0 + n * p.piece);
+            if (TO_X) {
+              tma_load_2d_pair(b_dst + n * kHalf, &maps.b, bar, n0, kb * kBK + n * p.vocab);
+              tma_load_2d_pair(b_dst + n * kHalf + kHalf / 2, &maps.b, bar, n0 + 64, kb * kBK + n * p.vocab);
+            } else {
+              tma_load_2d_pair(b_dst + n * kHalf, &maps.b, bar, kb * kBK, n0 + n * p.vocab);
+            }
           }
         }
       }
@@ -275,28 +350,31 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
   } else if (warp == 1) {
     // ---------------- products (leader) ----------------
     if (lane == 0 && leader) {
-      const uint32_t idesc = make_idesc_m(256, kTile, 0, kToX ? 1 : 0);
+      const uint32_t idesc = make_idesc_m(256, kTile, 0, TO_X ? 1 : 0);
       uint32_t it = 0, count = 0;
       bool ok = true;
       for (int i = pair; i < plan.items && ok; i += pairs) {
         const Item t = item_at(plan, i);
-        for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += kToX ? plan.k_blocks : kSpan, ++count) {
-          const int k1 = kToX ? t.kb1 : min(k0 + kSpan, t.kb1);
+        for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += F::kSpan, ++count) {
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + buf * kTile;
-          for (int kb = k0; kb < k1; ++kb, ++it) {
+          for (int kb = k0; kb < min(k0 + F::kSpan, t.kb1); ++kb, ++it) {
             const int st = it % kStages;
             if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t a_addr = smem_base + st * kStageBytes, b_addr = a_addr + kABytes;
+            const uint32_t a_addr = smem_base + st * F::kStage, b_addr = a_addr + PARTS * kHalf;
 #pragma unroll
-            for (int k = 0; k < kBK / kUmmaK; ++k) {
-              const uint64_t ad = make_desc(a_addr + k * (kUmmaK * 2), 16, 1024);
-              const uint64_t bd = kToX ? make_desc(b_addr + k * (kUmmaK * 128), kBK * 128, 1024)
-                                       : make_desc(b_addr + k * (kUmmaK * 2), 16, 1024);
-              umma_bf16_pair(acc, ad, bd, idesc, kb > k0 || k > 0);
+            for (int c = PARTS == 1 ? 5 : 0; c < 6; ++c) {
+              const uint32_t a_part = a_addr + kPartOfA[c] * kHalf, b_part = b_addr + kPartOfB[c] * kHalf;
+#pragma unroll
+              for (int k = 0; k < kBK / kUmmaK; ++k) {
+                const uint64_t ad = make_desc(a_part + k * (kUmmaK * 2), 16, 1024);
+                const uint64_t bd = TO_X ? make_desc(b_part + k * (kUmmaK * 128), kBK * 128, 1024)
+                                         : make_desc(b_part + k * (kUmmaK * 2), 16, 1024);
+                umma_bf16_pair(acc, ad, bd, idesc, kb > k0 || k > 0 || c > (PARTS == 1 ? 5 : 0));
+              }
             }
             umma_commit_pair(empty_bar(st), 3);
           }
@@ -310,124 +388,37 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
     }
   } else {
     // ---------------- results (both CTAs, a row per thread) ----------------
-    const int q = warp & 3;
+    const int q = warp & 3, half = (warp - 2) >> 2;      // the TMEM lanes that a warp may read go by its number
     uint32_t count = 0;
     bool ok = true;
     for (int i = pair; i < plan.items && ok; i += pairs) {
       const Item t = item_at(plan, i);
       const int row = t.m0 + (int)rank * 128 + q * 32 + lane;
       const bool live = row < rows;
-      if constexpr (!kToX) {
-        // The tensor core cuts off what a sum has behind its 24 bits, at every step of 16 products: over a whole row that
-        // is a few 2^-20 of the logit, always towards zero.  So a sum starts anew every kSpan k-blocks, and the parts are
-        // added here, rounded to nearest.
-        const int half = (warp - 2) >> 2;
-        float x[kHeadCols];
+      float x[kHeadCols];
 #pragma unroll
-        for (int j = 0; j < kHeadCols; ++j) x[j] = 0.f;
-        for (int k0 = 0; k0 < plan.k_blocks; k0 += kSpan, ++count) {
-          const uint32_t buf = count & 1u, use = count >> 1;
-          if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile + half * kHeadCols;
-#pragma unroll
-          for (int c = 0; c < kHeadCols; c += 32) {
-            uint32_t v[32];
-            tmem_ld32(acc + c, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) x[c + j] += __uint_as_float(v[j]);
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(buf), 0));
-        }
-        if (!ok) break;
-        logits_row<(MODE & 1) != 0, (MODE & 2) != 0>(p, x, t.n0 + half * kHeadCols, row, live);
-      } else {
+      for (int j = 0; j < kHeadCols; ++j) x[j] = 0.f;
+      for (int k0 = t.kb0; k0 < t.kb1; k0 += F::kSpan, ++count) {
         const uint32_t buf = count & 1u, use = count >> 1;
-        ++count;
         if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
         tc_fence_after();
-        const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile;
-        float by = 0.f;
-        bool none = false;                               // a token that is left out, where the rows have such
-        bf16* out = nullptr;
-        if (live) {
-          const int token = p.row_token[p.piece0 + row];
-          by = p.row_scale[row];
-          none = p.token_row[token] < 0;
-          out = reinterpret_cast<bf16*>(p.d_x) + (size_t)token * p.dx_stride;
-        }
-        if (t.tile >= 0) {
-          // a share's partial sums, [chunk of 32 columns][4 columns][lane]: a warp's accesses cover 512 bytes at a time.
-          // The warp that completes the tile adds them up in the shares' order, whoever it is.
-          const size_t slab = (size_t)128 * kTile;
-          const size_t mine = (size_t)q * 32 * kTile + (size_t)lane * 4;
-          const float* first = p.part + ((size_t)t.tile * plan.shares * 2 + rank) * slab + mine;
-          float* to = p.part + ((size_t)(t.tile * plan.shares + t.share) * 2 + rank) * slab + mine;
-          for (int c = 0; c < kTile; c += 32) {
-            uint32_t v[32];
-            tmem_ld32(acc + c, v);
-            tmem_ld_wait();
+        const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile + half * kHeadCols;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              *reinterpret_cast<uint4*>(to + (c / 32 * 8 + j) * 128) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          }
-          tc_fence_before();
-          __threadfence();
-          __syncwarp();
-          int* counter = p.counters + (t.tile * 2 + (int)rank) * 4 + q;
-          int seen = 0;
-          if (lane == 0) {
-            mbar_arrive_cluster(map_to_cta(tempty_bar(buf), 0));
-            seen = atomicAdd(counter, 1);
-          }
-          seen = __shfl_sync(0xffffffffu, seen, 0);
-          if (seen == plan.shares - 1) {
-            __threadfence();
-            for (int c = 0; c < kTile; c += 32) {
-              float4 sum[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-              for (int s = 0; s < plan.shares; s += 2) {
-                float4 w[2][8];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                  for (int j = 0; j < 8; ++j)
-                    w[h][j] = s + h < plan.shares
-                                  ? __ldcg(reinterpret_cast<const float4*>(first + (size_t)(s + h) * 2 * slab + (c / 32 * 8 + j) * 128))
-                                  : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) {
-                    sum[j].x += w[h][j].x; sum[j].y += w[h][j].y; sum[j].z += w[h][j].z; sum[j].w += w[h][j].w;
-                  }
-              }
-              uint32_t v[32];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                v[4 * j] = __float_as_uint(sum[j].x); v[4 * j + 1] = __float_as_uint(sum[j].y);
-                v[4 * j + 2] = __float_as_uint(sum[j].z); v[4 * j + 3] = __float_as_uint(sum[j].w);
-              }
-              if (live) grad_chunk(p, out, by, none, t.n0 + c, v);
-            }
-            if (lane == 0) *counter = 0;                 // ready for the next piece
-          }
-          continue;
-        }
-        for (int c = 0; c < kTile; c += 32) {
+        for (int c = 0; c < kHeadCols; c += 32) {
           uint32_t v[32];
           tmem_ld32(acc + c, v);
           tmem_ld_wait();
-          if (live) grad_chunk(p, out, by, none, t.n0 + c, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) x[c + j] += __uint_as_float(v[j]);
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(buf), 0));
       }
+      if (!ok) break;
+      const int n0 = t.n0 + half * kHeadCols;
+      if constexpr (TO_X) grad_row<PARTS>(p, x, plan, t, (int)rank * 8 + q * 2 + half, n0, row, live);
+      else logits_row<GRAD, CAP, PARTS>(p, x, n0, row, live);
     }
     if (!ok && lane == 0) {
       *abort_flag = 1;
@@ -448,13 +439,15 @@ __global__ void __launch_bounds__(threads_of(MODE == kGrad), 1) head_tc_kernel(c
   }
 }
 
-template <int MODE>
+template <bool TO_X, bool GRAD, bool CAP, int PARTS>
 cudaError_t launch(const HeadArgs& p, const HeadMaps& maps, long long most_items, cudaStream_t st) {
   static bool done[64] = {false};
-  cudaError_t e = allow_smem(head_tc_kernel<MODE>, kSmemBytes, done);
+  constexpr auto kernel = head_tc_kernel<TO_X, GRAD, CAP, PARTS>;
+  constexpr uint32_t kSmem = Form<TO_X, PARTS>::kSmem;
+  cudaError_t e = allow_smem(kernel, kSmem, done);
   if (e != cudaSuccess) return e;
   const int pairs = (int)(most_items < head_pairs() ? (most_items > 0 ? most_items : 1) : head_pairs());
-  return launch_behind_in_clusters(2, head_tc_kernel<MODE>, (unsigned)(2 * pairs), threads_of(MODE == kGrad), kSmemBytes, st, p, maps);
+  return launch_behind_in_clusters(2, kernel, (unsigned)(2 * pairs), kThreads, kSmem, st, p, maps);
 }
 
 }  // namespace
@@ -467,27 +460,36 @@ int head_pairs() {
     int n = 0;
     sms[dev] = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 1 ? n : 148;
   }
-  return sms[dev] / 2;
+  return sms[dev] / 2 < kHeadMostPairs ? sms[dev] / 2 : kHeadMostPairs;
 }
 
 cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st) {
   HeadMaps m;
-  if (!tc_encode_2d(&m.a, p.x, p.tokens, p.d, p.x_stride, 128, kBK) ||
-      !tc_encode_2d(&m.a_rows, p.x_rows, p.piece, p.d, p.d, 128, kBK) ||
-      !tc_encode_2d(&m.b, p.w, p.vocab, p.d, p.w_stride, 128, kBK))
+  const bool parts = p.parts == 3;
+  if (!tc_encode_2d(&m.a_rows, p.x_rows, (long long)p.parts * p.piece, p.d, p.d, 128, kBK)) return cudaErrorInvalidValue;
+  if (parts ? !tc_encode_2d(&m.b, p.w_parts, 3LL * p.vocab, p.d, p.d, 128, kBK)
+            : !tc_encode_2d(&m.b, p.w, p.vocab, p.d, p.w_stride, 128, kBK) ||
+                  !tc_encode_2d(&m.a, p.x, p.tokens, p.d, p.x_stride, 128, kBK))
     return cudaErrorInvalidValue;
+  if (parts) m.a = m.a_rows;
   const long long items = (long long)((p.piece + kTile - 1) / kTile) * ((p.vocab + kTile - 1) / kTile);
-  if (p.softcap > 0.f) return p.d_x ? launch<kLogitsCapGrad>(p, m, items, st) : launch<kLogitsCap>(p, m, items, st);
-  return p.d_x ? launch<kLogitsGrad>(p, m, items, st) : launch<kLogits>(p, m, items, st);
+  const bool cap = p.softcap > 0.f, grad = p.d_x != nullptr;
+  if (parts) {
+    if (cap) return grad ? launch<false, true, true, 3>(p, m, items, st) : launch<false, false, true, 3>(p, m, items, st);
+    return grad ? launch<false, true, false, 3>(p, m, items, st) : launch<false, false, false, 3>(p, m, items, st);
+  }
+  if (cap) return grad ? launch<false, true, true, 1>(p, m, items, st) : launch<false, false, true, 1>(p, m, items, st);
+  return grad ? launch<false, true, false, 1>(p, m, items, st) : launch<false, false, false, 1>(p, m, items, st);
 }
 
 cudaError_t launch_head_grad_tc(const HeadArgs& p, cudaStream_t st) {
   HeadMaps m;
-  if (!tc_encode_2d(&m.a, p.e, p.piece, p.vocab, p.pitch, 128, kBK) ||
-      !tc_encode_2d(&m.b, p.w, p.vocab, p.d, p.w_stride, kBK, 64))
+  const bool parts = p.parts == 3;
+  if (!tc_encode_2d(&m.a_rows, p.e, (long long)p.parts * p.piece, p.vocab, p.pitch, 128, kBK) ||
+      !tc_encode_2d(&m.b, parts ? p.w_parts : p.w, (long long)p.parts * p.vocab, p.d, parts ? p.d : p.w_stride, kBK, 64))
     return cudaErrorInvalidValue;
-  m.a_rows = m.a;
-  return launch<kGrad>(p, m, head_pairs(), st);
+  m.a = m.a_rows;
+  return parts ? launch<true, true, false, 3>(p, m, head_pairs(), st) : launch<true, true, false, 1>(p, m, head_pairs(), st);
 }
 
 }  // namespace mixlora
