@@ -48,6 +48,7 @@ struct HeadArgs {
   const float *weights, *normalizer;   // or NULL
   float *loss, *lse, *totals;     // lse, totals: or NULL
   float scale, softcap, temperature, z_loss;
+  double z_per_xw, z_to_cap;      // a logit for x . w where no cap bends it; a logit to what the cap's tanh gave
   float logit_factor;             // logits, before a cap, are this times x . w; a cap's are cap_out tanh(this times x . w)
   float cap_out, to2;             // to2: from x . w (from the tanh) to log2(e) times the logit
   // workspace

@@ -136,6 +136,8 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   a.logit_factor = cap ? s->scale / s->softcap : s->scale / s->temperature;
   a.cap_out = cap ? s->softcap / s->temperature : 0.f;
   a.to2 = (float)(1.44269504088896340736 * (cap ? (double)s->softcap : (double)s->scale) / (double)s->temperature);
+  a.z_per_xw = (double)s->scale / (double)s->temperature;
+  a.z_to_cap = cap ? (double)s->temperature / (double)s->softcap : 0.0;
   a.state = reinterpret_cast<HeadState*>(ws + L.state);
   a.counters = reinterpret_cast<int32_t*>(ws + L.counters);
   a.row_token = reinterpret_cast<int32_t*>(ws + L.row_token);

@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kListThreads) head_lists_kernel(HeadArgs p) {
 // What a weight is multiplied by: one over the normalizer
 __device__ __forceinline__ float part_of_each(const HeadArgs& p, double weights) {
   const double norm = p.normalizer ? (double)p.normalizer[0] : weights;
-  return norm == 0.0 ? 0.f : (float)(1.0 / norm);
+  return norm == 0.0 ? 0.f : 1.f / (float)norm;
 }
 
 // Numbers the counted rows and adds up their weights: one block, 8192 tokens a turn.  Rows that are left out get their
@@ -220,9 +220,27 @@ __global__ void __launch_bounds__(kRowThreads) head_parts_kernel(HeadArgs p) {
              (size_t)p.vocab * p.d, p.d);
 }
 
-// In 64 bits, out of line: a row needs several, and their code would not stay in the instruction cache otherwise
-__device__ __noinline__ double exp64(double x) { return exp(x); }
-__device__ __noinline__ double log64(double x) { return log(x); }
+// What a row needs of the exponential and the logarithm: any 64-bit argument, a result good to fp32's relative rounding (the
+// logits behind it are no better).  The power of two goes by the exponent's bits, the rest through the fp32 function; the
+// 64-bit functions are ten times the code, and fetching that once a launch took longer than all of a row's work.
+__device__ __forceinline__ double exp64(double x) {
+  if (x < -690.0) return 0.0;
+  const double k = rint(fmin(x, 700.0) * kLog2ed);
+  return (double)expf((float)fma(-k, kLn2d, x)) * __hiloint2double((1023 + (int)k) << 20, 0);
+}
+__device__ __forceinline__ double log64(double x) {        // x > 0
+  if (x < 0x1p-1000) x = 0x1p-1000;
+  const int hi = __double2hiint(x);
+  double m = __hiloint2double((hi & 0x000fffff) | 0x3ff00000, __double2loint(x));
+  int e = (hi >> 20) - 1023;
+  if (m > 1.4142135623730951) { m *= 0.5; ++e; }
+  return e > 1023 ? x : (double)log1pf((float)(m - 1.0)) + e * kLn2d;
+}
+__device__ __forceinline__ double recip64(double x) {      // x in fp32's range
+  double r = (double)__fdividef(1.f, (float)x);
+  r = r * fma(-x, r, 2.0);
+  return r * fma(-x, r, 2.0);
+}
 
 // One row's loss and, with a gradient, what its columns need, by one warp.  The columns that are not listed come as
 // s 2^r (s = 0: there is none).  `z` holds the listed logits and gets the places' values G_k / A.
@@ -239,8 +257,8 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
     // loss = ln(1 + e^gap) without a difference of two logarithms, and 1 - p without one from one
     most = (double)__shfl_sync(0xffffffffu, lane == 0 ? z[0] : 0.f, 0);     // lane 0 writes it below
     const double gap = lr - most, e = exp64(-fabs(gap));
-    loss = fmax(gap, 0.0) + log1p(e);
-    miss = (gap > 0.0 ? 1.0 : e) / (1.0 + e);
+    loss = (gap < 0.0 ? 0.0 : gap) + (double)log1pf((float)e);
+    miss = (gap > 0.0 ? 1.0 : e) * recip64(1.0 + e);
     lse = most + loss;
   } else {
     q = p.list_q + (size_t)token * p.top;
@@ -273,7 +291,7 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
   const double r_listed = 100.0 * rint(most * (kLog2ed / 100.0));
   if (s == 0.0 || r_listed > r) out.r = r_listed;
   const double u = exp64(out.r * kLn2d - lse), s_row = s == 0.0 ? 0.0 : exp64(lr - out.r * kLn2d);
-  const double part = rest > 0.0 && s_row > 0x1p-100 ? rest / s_row : 0.0;
+  const double part = rest > 0.0 && s_row > 0x1p-100 ? rest * recip64(s_row) : 0.0;
   const double curl = 2.0 * zeta * lse, share = mass + curl;
   double a = share * u - part;
   // nothing below what the 32-bit sums behind u and s can tell from zero, so that G_k / A stays in range
@@ -284,7 +302,7 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
     const double zk = (double)z[k], pk = exp64(zk - lse);
     double g = q ? share * pk - q[k] : curl * pk - miss;
     if (p.softcap > 0.f) {
-      const double tk = zk * (double)p.temperature / (double)p.softcap;
+      const double tk = zk * p.z_to_cap;
       g *= (1.0 - tk) * (1.0 + tk);
     }
     z[k] = (float)g;
@@ -298,12 +316,12 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
       const double other = __shfl_xor_sync(0xffffffffu, largest, d);
       if (fabs(other) > fabs(largest) || (fabs(other) == fabs(largest) && other > largest)) largest = other;
     }
-    const double near = (double)__bfloat162float(__float2bfloat16((float)(largest / a)));
-    if (fabs(near) > 0x1p-100 && fabs(near) < 0x1p120) a = largest / near;
+    const double near = (double)__bfloat162float(__float2bfloat16((float)(largest * recip64(a))));
+    if (fabs(near) > 0x1p-100 && fabs(near) < 0x1p120) a = largest * recip64(near);
   }
-  const double over = 1.0 / a;
+  const double over = recip64(a);
   for (int k = lane; k < n; k += 32) z[k] = (float)((double)z[k] * over);
-  out.scale = (float)(a * ((double)p.scale / (double)p.temperature) * weight * (double)each);
+  out.scale = (float)(a * p.z_per_xw * weight * (double)each);
   return out;
 }
 
@@ -354,8 +372,10 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
     weights = p.state->weight;
     each = p.state->each;
   }
-  const int token = row < head_rows_here(p) ? (p.few ? row : p.row_token[p.piece0 + row]) : -1;
-  const int n = token >= 0 ? head_entries(p, token) : 0;
+  const int rows = head_rows_here(p);
+  int token = p.few ? row : (p.piece0 + row < p.tokens ? p.row_token[p.piece0 + row] : -1);      // asked for together
+  if (row >= rows) token = -1;
+  const int n = token < 0 ? 0 : (p.labels && !p.few ? 1 : head_entries(p, token));
   if (p.few && token >= 0 && lane == 0) {
     p.row_token[token] = token;
     p.token_row[token] = n ? token : -1;

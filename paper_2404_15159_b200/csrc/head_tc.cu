@@ -65,9 +65,14 @@ __device__ __forceinline__ Plan make_plan(int rows, int n_tiles, int k_blocks, i
   t.whole = tiles;
   t.shares = 1;
   if (TO_X && rest) {
-    int best = k_blocks;
-    for (int s = 2; s <= kHeadMaxShares && s * Form<TO_X, PARTS>::kShareMin <= k_blocks && s * rest <= most_items; ++s) {
-      const int cost = (rest * s + pairs - 1) / pairs * ((k_blocks + s - 1) / s + Form<TO_X, PARTS>::kShareCost);
+    // in fp32 without divisions, which would take a microsecond; whichever of two nearly equal costs is taken, every role of
+    // every CTA takes the same
+    const float per_pair = 1.f / pairs;
+    float best = k_blocks;
+#pragma unroll
+    for (int s = 2; s <= kHeadMaxShares; ++s) {
+      if (s * Form<TO_X, PARTS>::kShareMin > k_blocks || s * rest > most_items) continue;
+      const float cost = ceilf(rest * s * per_pair - 0x1p-10f) * (k_blocks * (1.f / s) + Form<TO_X, PARTS>::kShareCost);
       if (cost < best) { best = cost; t.shares = s; }
     }
     if (t.shares > 1) t.whole = tiles - rest;
