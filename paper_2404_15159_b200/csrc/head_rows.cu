@@ -3,6 +3,7 @@
 // All of it is small beside the products (8192 rows of 32000 columns: TODO us of TODO), so what can lose bits by
 // cancellation is done in 64 bits: probabilities of a teacher, log-sum-exps, gradients towards listed columns.
 #include <math.h>
+#include <string.h>
 
 #include "head.cuh"
 
@@ -242,18 +243,32 @@ __device__ __forceinline__ double recip64(double x) {      // x in fp32's range
   return r * fma(-x, r, 2.0);
 }
 
+// What a warp of the joining kernel works on
+struct RowJob {
+  const float2* stats;          // the row's tiles
+  int tiles, n;                 // n: listed columns
+  const int32_t* list;
+  const double* q;              // the teacher's probabilities, or NULL: a label
+  double rest, weight;
+  float each;
+  float* z;                     // the listed logits; gets the places' values G_k / A
+  float *loss, *lse, *scale;    // lse, scale: or NULL
+  bf16* e;
+  long long e_part;
+};
+
 // One row's loss and, with a gradient, what its columns need, by one warp.  The columns that are not listed come as
-// s 2^r (s = 0: there is none).  `z` holds the listed logits and gets the places' values G_k / A.
-struct RowResult { double r, weighted; float scale; };
-__device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, int n, double s, double r, float each, float* z,
-                                                bool rounds) {
-  const int lane = threadIdx.x & 31;
+// s 2^r (s = 0: there is none).
+struct RowResult { double r, weighted; };
+__device__ __forceinline__ RowResult finish_row(const HeadArgs& p, const RowJob& job, double s, double r) {
+  const int lane = threadIdx.x & 31, n = job.n;
   const double lr = s == 0.0 ? -INFINITY : r * kLn2d + log64(s);
-  const double weight = p.weights ? (double)p.weights[token] : 1.0;
   const double zeta = (double)p.z_loss;
-  double loss, lse, most, miss = 0.0, mass = 1.0, rest = 0.0;
-  const double* q = nullptr;
-  if (p.labels) {
+  double loss, lse, most, miss = 0.0, mass = 1.0;
+  const double* q = job.q;
+  float* z = job.z;
+  const double rest = job.rest;
+  if (!q) {
     // loss = ln(1 + e^gap) without a difference of two logarithms, and 1 - p without one from one
     most = (double)__shfl_sync(0xffffffffu, lane == 0 ? z[0] : 0.f, 0);     // lane 0 writes it below
     const double gap = lr - most, e = exp64(-fabs(gap));
@@ -261,8 +276,6 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
     miss = (gap > 0.0 ? 1.0 : e) * recip64(1.0 + e);
     lse = most + loss;
   } else {
-    q = p.list_q + (size_t)token * p.top;
-    rest = p.rest_q[token];
     most = -INFINITY;
     for (int k = lane; k < n; k += 32) most = fmax(most, (double)z[k]);
     most = warp_max(most);
@@ -283,11 +296,11 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
   }
   loss += zeta * lse * lse;
   if (lane == 0) {
-    p.loss[token] = (float)loss;
-    if (p.lse) p.lse[token] = (float)lse;
+    *job.loss = (float)loss;
+    if (job.lse) *job.lse = (float)lse;
   }
-  RowResult out{r, weight * (double)(float)loss, 0.f};
-  if (!p.d_x) return out;
+  RowResult out{r, job.weight * (double)(float)loss};
+  if (!job.scale) return out;
   const double r_listed = 100.0 * rint(most * (kLog2ed / 100.0));
   if (s == 0.0 || r_listed > r) out.r = r_listed;
   const double u = exp64(out.r * kLn2d - lse), s_row = s == 0.0 ? 0.0 : exp64(lr - out.r * kLn2d);
@@ -308,7 +321,7 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
     z[k] = (float)g;
     if (fabs(g) > fabs(largest)) largest = (double)(float)g;
   }
-  if (rounds) {
+  if (p.parts == 1) {
     // the largest listed factor, most of the gradient where the others' are spread out, is made one that rounding keeps: A
     // takes up the difference
 #pragma unroll
@@ -321,100 +334,137 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, int token, in
   }
   const double over = recip64(a);
   for (int k = lane; k < n; k += 32) z[k] = (float)((double)z[k] * over);
-  out.scale = (float)(a * p.z_per_xw * weight * (double)each);
+  if (lane == 0) *job.scale = (float)(a * p.z_per_xw * job.weight * (double)job.each);
   return out;
 }
 
-// Sum of every block's weighted losses, by the block that comes last, in the blocks' order.
-__device__ __forceinline__ void add_totals(const HeadArgs& p, int block, double mine, float weights, double* warp_w) {
-  __shared__ int last;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (threadIdx.x == 0) {
-    p.loss_part[block] = mine;
-    __threadfence();
-    last = atomicAdd(&p.state->joined, 1) == p.join_blocks - 1;
-  }
-  __syncthreads();
-  if (!last || !p.totals) return;
-  __threadfence();
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < p.join_blocks; i += kRowThreads) sum += __ldcg(p.loss_part + i);
-  sum = warp_sum(sum);
-  if (lane == 0) warp_w[warp] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    sum = 0.0;
-    for (int i = 0; i < kRowThreads / 32; ++i) sum += warp_w[i];
-    p.totals[0] = (float)sum;
-    p.totals[1] = weights;
-  }
-}
-
 // Joins a row's tiles, a warp a row: sums over the tiles' R and S, the row's loss, and for a gradient its exponentials at one
-// R with the listed columns' factors in their places.
-__global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
+// R with the listed columns' factors in their places.  A ninth warp adds up the blocks' weighted losses meanwhile: the block
+// that comes last does so, in the blocks' order.
+//
+// A block runs through its code once on a row of its own making while the kernel before it still runs: the instructions have
+// then been fetched when the sums arrive (they are 8 KB, and a launch of few rows waited longer for them than it computed).
+struct BlankRow { float2 stats; double q; float z, loss, lse, scale; int32_t list; bf16 e; };
+__global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p) {
   constexpr int kWarps = kRowThreads / 32, kAhead = 8;
   let_next_start();
-  wait_for_last();
   __shared__ double warp_w[kWarps];
+  __shared__ float weights;
+  __shared__ BlankRow blank[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row = blockIdx.x * kWarps + warp;
-  double weighted = 0.0;
-  float weights, each;
-  if (p.few) {                                     // no kernel has been over the tokens before
+  if (warp == kWarps) {
+    wait_for_last();
+    __syncthreads();
+    const int block = p.piece0 / kWarps + blockIdx.x;
+    int last = 0;
+    if (lane == 0) {
+      double mine = 0.0;
+      for (int i = 0; i < kWarps; ++i) mine += warp_w[i];
+      p.loss_part[block] = mine;
+      __threadfence();
+      last = atomicAdd(&p.state->joined, 1) == p.join_blocks - 1;
+    }
+    if (!__shfl_sync(0xffffffffu, last, 0) || !p.totals) return;
+    __threadfence();
     double sum = 0.0;
-    for (int t = lane; t < p.tokens; t += 32)
-      if (head_entries(p, t) > 0) sum += p.weights ? (double)p.weights[t] : 1.0;
+#pragma unroll 8
+    for (int i = lane; i < p.join_blocks; i += 32) sum += __ldcg(p.loss_part + i);
     sum = warp_sum(sum);
-    weights = (float)sum;
-    each = part_of_each(p, sum);
-  } else {
-    weights = p.state->weight;
-    each = p.state->each;
+    if (lane == 0) {
+      p.totals[0] = (float)sum;
+      p.totals[1] = weights;
+    }
+    return;
   }
-  const int rows = head_rows_here(p);
-  int token = p.few ? row : (p.piece0 + row < p.tokens ? p.row_token[p.piece0 + row] : -1);      // asked for together
-  if (row >= rows) token = -1;
-  const int n = token < 0 ? 0 : (p.labels && !p.few ? 1 : head_entries(p, token));
-  if (p.few && token >= 0 && lane == 0) {
-    p.row_token[token] = token;
-    p.token_row[token] = n ? token : -1;
-    if (n == 0) {
-      p.loss[token] = 0.f;
-      if (p.lse) p.lse[token] = 0.f;
-      if (p.d_x) p.row_scale[row] = 0.f;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    RowJob job;
+    memset(&job, 0, sizeof(job));
+    if (pass == 0) {
+      BlankRow& b = blank[warp];
+      if (lane == 0) {
+        b.stats = make_float2(0.f, 1.f);
+        b.q = 1.0;
+        b.z = 0.f;
+        b.list = 0;
+      }
+      __syncwarp();
+      job.stats = &b.stats; job.tiles = 1; job.n = 1;
+      job.list = &b.list; job.q = p.labels ? nullptr : &b.q;
+      job.z = &b.z; job.loss = &b.loss; job.lse = &b.lse; job.scale = p.d_x ? &b.scale : nullptr;
+      job.e = &b.e;
+    } else {
+      wait_for_last();
+      const int row = blockIdx.x * kWarps + warp, rows = head_rows_here(p);
+      if (p.few) {                                     // no kernel has been over the tokens before
+        double sum = 0.0;
+        for (int t = lane; t < p.tokens; t += 32)
+          if (head_entries(p, t) > 0) sum += p.weights ? (double)p.weights[t] : 1.0;
+        sum = warp_sum(sum);
+        if (threadIdx.x == 0) weights = (float)sum;
+        job.each = part_of_each(p, sum);
+      } else {
+        if (threadIdx.x == 0) weights = p.state->weight;
+        job.each = p.state->each;
+      }
+      int token = p.few ? row : (p.piece0 + row < p.tokens ? p.row_token[p.piece0 + row] : -1);      // asked for together
+      if (row >= rows) token = -1;
+      if (token >= 0) {
+        job.n = p.labels && !p.few ? 1 : head_entries(p, token);
+        job.stats = p.stats + (size_t)row * p.col_tiles; job.tiles = p.col_tiles;
+        job.list = p.list + (size_t)token * p.top;
+        job.weight = p.weights ? (double)p.weights[token] : 1.0;
+        if (!p.labels) {
+          job.q = p.list_q + (size_t)token * p.top;
+          job.rest = p.rest_q[token];
+        }
+        job.z = p.z_listed + (size_t)row * p.top;
+        job.loss = p.loss + token;
+        job.lse = p.lse ? p.lse + token : nullptr;
+        job.scale = p.d_x ? p.row_scale + row : nullptr;
+        job.e = reinterpret_cast<bf16*>(p.e) + (size_t)row * p.pitch; job.e_part = p.e_part;
+        if (p.few && lane == 0) {
+          p.row_token[token] = token;
+          p.token_row[token] = job.n ? token : -1;
+          if (job.n == 0) {
+            *job.loss = 0.f;
+            if (job.lse) *job.lse = 0.f;
+            if (job.scale) *job.scale = 0.f;
+          }
+        }
+      }
     }
-  }
-  if (n) {
-    const float2* stats = p.stats + (size_t)row * p.col_tiles;
-    float* z = p.z_listed + (size_t)row * p.top;
-    float r = -INFINITY, s = 0.f;
-    auto add = [&](float r2, float s2) {           // a sum of nothing has no say in R
-      const float most = s2 == 0.f ? r : (s == 0.f ? r2 : fmaxf(r, r2));
-      s = (s == 0.f ? 0.f : s * exp2f(r - most)) + (s2 == 0.f ? 0.f : s2 * exp2f(r2 - most));
-      r = most;
-    };
-    for (int i0 = lane; i0 < p.col_tiles; i0 += 32 * kAhead) {
-      float2 v[kAhead];
+    RowResult res{0.0, 0.0};
+    if (job.n) {
+      float r = -INFINITY, s = 0.f;
+      auto add = [&](float r2, float s2) {           // a sum of nothing has no say in R
+        const float most = s2 == 0.f ? r : (s == 0.f ? r2 : fmaxf(r, r2));
+        s = (s == 0.f ? 0.f : s * exp2f(r - most)) + (s2 == 0.f ? 0.f : s2 * exp2f(r2 - most));
+        r = most;
+      };
+      for (int i0 = lane; i0 < job.tiles; i0 += 32 * kAhead) {
+        float2 v[kAhead];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) v[j] = i0 + 32 * j < p.col_tiles ? stats[i0 + 32 * j] : make_float2(0.f, 0.f);
+        for (int j = 0; j < kAhead; ++j) v[j] = i0 + 32 * j < job.tiles ? job.stats[i0 + 32 * j] : make_float2(0.f, 0.f);
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) add(v[j].x, v[j].y);
+        for (int j = 0; j < kAhead; ++j) add(v[j].x, v[j].y);
+      }
+#pragma unroll
+      for (int d = 16; d; d >>= 1) {
+        const float r2 = __shfl_xor_sync(0xffffffffu, r, d), s2 = __shfl_xor_sync(0xffffffffu, s, d);
+        add(r2, s2);
+      }
+      res = finish_row(p, job, (double)s, (double)r);
     }
-#pragma unroll
-    for (int d = 16; d; d >>= 1) {
-      const float r2 = __shfl_xor_sync(0xffffffffu, r, d), s2 = __shfl_xor_sync(0xffffffffu, s, d);
-      add(r2, s2);
+    if (pass == 1) {
+      if (lane == 0) warp_w[warp] = res.weighted;
+      __syncthreads();                                 // the ninth warp goes on
     }
-    const RowResult res = finish_row(p, token, n, (double)s, (double)r, each, z, p.parts == 1);
-    if (lane == 0) weighted = res.weighted;
-    if (p.d_x) {
-      if (lane == 0) p.row_scale[row] = res.scale;
-      bf16* e = reinterpret_cast<bf16*>(p.e) + (size_t)row * p.pitch;
-      for (int i0 = 0; i0 < p.col_tiles; i0 += 32) {
+    if (job.n && job.scale) {
+      for (int i0 = 0; i0 < job.tiles; i0 += 32) {
         float by = 0.f;
-        if (i0 + lane < p.col_tiles) {
-          const float2 v = stats[i0 + lane];
+        if (i0 + lane < job.tiles) {
+          const float2 v = job.stats[i0 + lane];
           if (v.y != 0.f) by = v.x - (float)res.r;
         }
         unsigned todo = __ballot_sync(0xffffffffu, by < 0.f);
@@ -425,7 +475,7 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
           const int c = (i0 + l) * kHeadCols + lane * 4;
           if (c >= p.pitch) continue;
           for (int k = 0; k < p.parts; ++k) {
-            uint2* at = reinterpret_cast<uint2*>(e + k * p.e_part + c);
+            uint2* at = reinterpret_cast<uint2*>(job.e + k * job.e_part + c);
             uint2 v = *at;
             __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
 #pragma unroll
@@ -436,27 +486,20 @@ __global__ void __launch_bounds__(kRowThreads) head_join_kernel(HeadArgs p) {
             *at = v;
           }
         }
+        __syncwarp();
       }
-      __syncwarp();
-      const int32_t* list = p.list + (size_t)token * p.top;
-      for (int k = lane; k < n; k += 32) {
+      for (int k = lane; k < job.n; k += 32) {
+        bf16* at = job.e + job.list[k];
         if (p.parts == 1) {
-          e[list[k]] = __float2bfloat16(z[k]);
+          *at = __float2bfloat16(job.z[k]);
         } else {
-          const HeadParts v = head_parts(z[k]);
+          const HeadParts v = head_parts(job.z[k]);
 #pragma unroll
-          for (int j = 0; j < 3; ++j) e[j * p.e_part + list[k]] = __float2bfloat16(v.v[j]);
+          for (int j = 0; j < 3; ++j) at[j * job.e_part] = __float2bfloat16(v.v[j]);
         }
       }
     }
   }
-  if (lane == 0) warp_w[warp] = weighted;
-  __syncthreads();
-  double mine = 0.0;
-  if (threadIdx.x == 0)
-    for (int i = 0; i < kWarps; ++i) mine += warp_w[i];
-  __syncthreads();
-  add_totals(p, p.piece0 / kWarps + blockIdx.x, mine, weights, warp_w);
 }
 
 }  // namespace
@@ -486,7 +529,8 @@ cudaError_t launch_head_gather(const HeadArgs& p, bool first_piece, cudaStream_t
 }
 
 cudaError_t launch_head_join(const HeadArgs& p, cudaStream_t st) {
-  return launch_behind(head_join_kernel, (unsigned)((p.piece + kHeadRowsPerBlock - 1) / kHeadRowsPerBlock), kRowThreads, 0, st, p);
+  return launch_behind(head_join_kernel, (unsigned)((p.piece + kHeadRowsPerBlock - 1) / kHeadRowsPerBlock), kRowThreads + 32, 0,
+                       st, p);
 }
 
 }  // namespace mixlora
