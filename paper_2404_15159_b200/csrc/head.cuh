@@ -1,9 +1,9 @@
 // Shared parts of the losses on the output head: arguments, and how a row's exponentials are held.
 //
-// Logits z_v = (capped) scale x . w_v / temperature of a row are formed 128 columns at a time and turned into
+// Logits z_v = (capped) scale x . w_v / temperature of a row are formed up to 128 columns at a time and turned into
 // exponentials at once.  A row's `listed` columns (its label, or the teacher's entries) are left out of them and kept as
 // fp32 logits: a sum or a difference that a confident row makes small is then never taken of nearly equal numbers.
-//   128 columns           R = 100 rint(log2(e) max z / 100) over its columns that are not listed, S = sum 2^(z log2(e) - R)
+//   those columns         R = 100 rint(log2(e) max z / 100) over its columns that are not listed, S = sum 2^(z log2(e) - R)
 //   gradient              E_v = 2^(z_v log2(e) - R) (1 - (z_v temperature / softcap)^2), one rounding to bf16
 // R is a multiple of 100, so tiles of a row nearly always share it, and where they do not (logits 35 apart or more) the
 // row is brought to the largest one by powers of two, which round nothing.  With the row's R and
@@ -18,12 +18,14 @@
 namespace mixlora {
 
 constexpr int kHeadTile = 256;               // rows and columns of a tile of the products
-constexpr int kHeadCols = 128;               // columns that share R and S
+constexpr int kHeadCols = 128;               // most columns that share R and S
+constexpr int kHeadLeastCols = 64;
 constexpr float kHeadStep = 100.f;           // R's step, in powers of two
 constexpr int kHeadFewTokens = 64;
 constexpr int kHeadNone = 0x7fffffff;        // no column (ends a row's list)
 constexpr int kHeadMaxShares = 16;           // CTA pairs that share one tile's reduction
 constexpr int kHeadMaxItems = 222;           // shares under way: three rounds of 74 CTA pairs
+constexpr int kHeadPairs = 74;               // CTA pairs of a B200
 constexpr int kHeadMostPairs = 128;          // CTA pairs that a launch uses at most
 constexpr int kHeadCounters = 16 * kHeadMostPairs;   // one for each 32 x 128 corner of a shared tile
 constexpr int kHeadRowsPerBlock = 8;         // rows that a block of the joining kernel takes
@@ -71,7 +73,7 @@ struct HeadArgs {
   float* part;                    // partial tiles of a split reduction
   // the piece of counted rows that a launch works on
   int piece0, piece;              // first row, most rows
-  int pitch, col_tiles;
+  int pitch, cols, col_tiles;     // cols: columns that share R and S, half a tile of the logits
   int join_blocks;                // of the joining kernel, over all pieces
   int part_items;                 // that `part` has room for
   int parts;                      // bf16 values that hold an operand: 1, or 3 in the fp32 mode

@@ -47,7 +47,7 @@ mixlora_status_t check_head(const mixlora_head_shape_t* s) {
 // rows of x is what counts.
 int piece_rows(const mixlora_head_shape_t& s, bool gradient, int parts) {
   long long row = 2LL * parts * s.d_model;
-  const long long wide = gradient ? 2LL * parts * s.vocab : (s.vocab + kHeadCols - 1) / kHeadCols * 8LL;
+  const long long wide = gradient ? 2LL * parts * s.vocab : (s.vocab + kHeadLeastCols - 1) / kHeadLeastCols * 8LL;
   if (row < wide) row = wide;
   long long rows = (512LL << 20) / row / kHeadTile * kHeadTile;
   if (rows < kHeadTile) rows = kHeadTile;
@@ -55,10 +55,26 @@ int piece_rows(const mixlora_head_shape_t& s, bool gradient, int parts) {
   return (int)(rows < all ? rows : (all > 0 ? all : kHeadTile));
 }
 
+// Columns of half a tile of the logits.  In fp32 mode, whose products outlast the way of their operands, a tile is made
+// narrower where that fills the last round of CTA pairs better (700 tokens of 8009 columns 222 -> 203 us).  With bf16 a tile
+// of 256 columns already waits for its operands: 512 tokens of 32000 columns take 4 rounds of 224 columns as long as 4 of 256.
+int head_cols(const mixlora_head_shape_t& s, int parts, int piece) {
+  if (parts == 1) return kHeadCols;
+  const long long m_tiles = ((s.tokens < piece ? s.tokens : piece) + kHeadTile - 1) / kHeadTile;
+  int best = kHeadCols;
+  long long least = 0;
+  for (int cols = kHeadCols; cols >= kHeadLeastCols; cols -= 16) {
+    const long long tiles = m_tiles * ((s.vocab + 2 * cols - 1) / (2 * cols));
+    const long long cost = (tiles + kHeadPairs - 1) / kHeadPairs * cols;
+    if (cols == kHeadCols || cost < least) { least = cost; best = cols; }
+  }
+  return best;
+}
+
 struct HeadLayout {
   size_t state, counters, row_token, token_row, list, list_q, rest_q, list_n, loss_part, x_rows, w_parts, z_listed, stats, e,
       row_scale, part, total;
-  int parts, piece, pieces, pitch, col_tiles, join_blocks, part_items;
+  int parts, piece, pieces, pitch, cols, col_tiles, join_blocks, part_items;
 };
 HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   const size_t tokens = (size_t)s.tokens, top = s.teacher_top ? (size_t)s.teacher_top : 1;
@@ -67,7 +83,8 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   L.piece = piece_rows(s, gradient, L.parts);
   L.pieces = (s.tokens + L.piece - 1) / L.piece;
   L.pitch = (s.vocab + 7) / 8 * 8;
-  L.col_tiles = (s.vocab + kHeadCols - 1) / kHeadCols;
+  L.cols = head_cols(s, L.parts, L.piece);
+  L.col_tiles = (s.vocab + L.cols - 1) / L.cols;
   L.join_blocks = L.pieces * (L.piece / kHeadRowsPerBlock);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
@@ -157,7 +174,7 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   a.parts = L.parts;
   a.row_scale = reinterpret_cast<float*>(ws + L.row_scale);
   a.part = reinterpret_cast<float*>(ws + L.part);
-  a.piece = L.piece; a.pitch = L.pitch; a.col_tiles = L.col_tiles;
+  a.piece = L.piece; a.pitch = L.pitch; a.cols = L.cols; a.col_tiles = L.col_tiles;
   a.join_blocks = L.join_blocks; a.part_items = L.part_items;
 
   if (!c.labels) MIXLORA_TRY(launch_head_lists(a, st));

@@ -472,8 +472,8 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
           const int l = __ffs(todo) - 1;
           todo &= todo - 1;
           const float f = exp2f(__shfl_sync(0xffffffffu, by, l));
-          const int c = (i0 + l) * kHeadCols + lane * 4;
-          if (c >= p.pitch) continue;
+          const int c = (i0 + l) * p.cols + lane * 4;
+          if (lane * 4 >= p.cols || c >= p.pitch) continue;
           for (int k = 0; k < p.parts; ++k) {
             uint2* at = reinterpret_cast<uint2*>(job.e + k * job.e_part + c);
             uint2 v = *at;

@@ -1,10 +1,10 @@
 // The two products of the head's losses on the tensor cores (tcgen05, TMEM, TMA; bf16 operands, fp32 accumulation).
 //
-//   logits   x [rows, d] . w [vocab, d]^T   per 128 columns: R, S, the listed logits and, for a gradient, E
+//   logits   x [rows, d] . w [vocab, d]^T   per half a tile's columns: R, S, the listed logits and, for a gradient, E
 //   grad     E [rows, vocab] . w [vocab, d]  times the row's A scale / temperature weight / normalizer, to the row's token
 //
-// Pairs of CTAs work on 256 x 256 tiles (cta_group::2, 128 rows of the accumulator and half of B's columns each), one
-// persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the products, warps 2 to 9 take finished sums into
+// Pairs of CTAs work on 256 x 256 tiles (cta_group::2, 128 rows of the accumulator and half of B's columns each; the logits'
+// tiles may be narrower, see head_cols), one persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the products, warps 2 to 9 take finished sums into
 // registers, 128 columns of one row a thread, and turn them into results while the next sums are under way.  The number of
 // rows is read on the device: tokens without a label take no part.
 //
@@ -81,7 +81,7 @@ __device__ __forceinline__ Plan make_plan(int rows, int n_tiles, int k_blocks, i
   return t;
 }
 struct Item { int m0, n0, kb0, kb1, tile, share; };   // tile: index among the shared tiles, -1 for a whole one
-__device__ __forceinline__ Item item_at(const Plan& t, int i) {
+__device__ __forceinline__ Item item_at(const Plan& t, int i, int width) {
   Item it;
   it.kb0 = 0; it.kb1 = t.k_blocks;
   it.tile = -1; it.share = 0;
@@ -98,7 +98,7 @@ __device__ __forceinline__ Item item_at(const Plan& t, int i) {
   const int rows = min(t.group, t.m_tiles - g * t.group);
   const int col = in / rows;
   it.m0 = (g * t.group + in - col * rows) * kTile;
-  it.n0 = col * kTile;
+  it.n0 = col * width;
   return it;
 }
 
@@ -112,10 +112,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// One row of 128 logits, in registers, by one thread: the listed ones are put aside, the others become exponentials.
+// One row of up to 128 logits, in registers, by one thread: the listed ones are put aside, the others become exponentials.
 template <bool GRAD, bool CAP, int PARTS>
 __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCols], int n0, int row, bool live) {
-  constexpr int kChunks = kHeadCols / 32;
+  constexpr int kChunk = 16, kChunks = kHeadCols / kChunk;
+  const int cols = p.cols;
   const int token = live ? p.row_token[p.piece0 + row] : 0;
   const int32_t* list = p.list + (size_t)token * p.top;
   // the first listed column that may be among these
@@ -135,9 +136,10 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
   float most = -INFINITY;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
-    const int col = n0 + 32 * c;
+    if (c * kChunk >= cols) break;
+    const int col = n0 + kChunk * c;
     uint32_t named = 0;
-    while (next < col + 32) {
+    while (next < col + kChunk) {
       named |= 1u << (next - col);
       ++at;
       next = at < p.top ? list[at] : kHeadNone;
@@ -145,21 +147,21 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     __syncwarp();
     if (named) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j)
+      for (int j = 0; j < kChunk; ++j)
         if (named >> j & 1) {
-          const float raw = x[32 * c + j] * factor;
+          const float raw = x[kChunk * c + j] * factor;
           *z++ = CAP ? tanhf(raw) * cap_out : raw;
         }
     }
     __syncwarp();
-    dead[c] = named | (p.vocab - col >= 32 ? 0u : ~((1u << max(p.vocab - col, 0)) - 1u));
+    dead[c] = named | (p.vocab - col >= kChunk ? 0u : ~((1u << max(p.vocab - col, 0)) - 1u));
     if (__any_sync(0xffffffffu, dead[c])) {
 #pragma unroll
-      for (int j = 0; j < 32; ++j)
-        if (!(dead[c] >> j & 1)) most = fmaxf(most, x[32 * c + j]);
+      for (int j = 0; j < kChunk; ++j)
+        if (!(dead[c] >> j & 1)) most = fmaxf(most, x[kChunk * c + j]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 32; ++j) most = fmaxf(most, x[32 * c + j]);
+      for (int j = 0; j < kChunk; ++j) most = fmaxf(most, x[kChunk * c + j]);
     }
   }
   most *= factor;
@@ -169,10 +171,11 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
   bf16* e = reinterpret_cast<bf16*>(p.e) + (size_t)row * p.pitch + n0;
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
+    if (c * kChunk >= cols) break;
     const bool any = __any_sync(0xffffffffu, dead[c]);
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-      float& v = x[32 * c + j];
+    for (int j = 0; j < kChunk; ++j) {
+      float& v = x[kChunk * c + j];
       float ex, slope = 1.f;
       if (CAP) {
         const float t = tanhf(v * factor);
@@ -187,7 +190,7 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     }
     if (GRAD && live) {
 #pragma unroll
-      for (int j = 32 * c; j < 32 * c + 32; j += 8)
+      for (int j = kChunk * c; j < kChunk * c + kChunk; j += 8)
         if (n0 + j < p.pitch) {
           if constexpr (PARTS == 1) {
             *reinterpret_cast<uint4*>(e + j) = make_uint4(pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
@@ -208,7 +211,7 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     }
   }
   if (live && n0 < p.vocab)
-    p.stats[(size_t)row * p.col_tiles + n0 / kHeadCols] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+    p.stats[(size_t)row * p.col_tiles + n0 / cols] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
 }
 
 // One row of 128 sums of the gradient's product.  Where a tile's reduction is shared, the sums go to `part`, [4 columns]
@@ -314,7 +317,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
 
   const int rows = head_rows_here(p);
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  const Plan plan = make_plan<TO_X, PARTS>(rows, ((TO_X ? p.d : p.vocab) + kTile - 1) / kTile,
+  const int cols = TO_X ? kHeadCols : p.cols;              // half of a tile's columns
+  const Plan plan = make_plan<TO_X, PARTS>(rows, ((TO_X ? p.d : p.vocab) + 2 * cols - 1) / (2 * cols),
                                            ((TO_X ? p.vocab : p.d) + kBK - 1) / kBK, pairs, p.part_items);
 
   if (warp == 0) {
@@ -324,17 +328,18 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       const bool direct = !TO_X && PARTS == 1 && p.state->counted == p.tokens;
       const CUtensorMap* am = direct ? &maps.a : &maps.a_rows;
       const int row0 = direct ? p.piece0 : 0;
+      const uint32_t bytes = 2 * PARTS * (kHalf + cols * kBK * 2);      // of both CTAs' operands
       uint32_t it = 0;
       bool ok = true;
       for (int i = pair; i < plan.items && ok; i += pairs) {
-        const Item t = item_at(plan, i);
-        const int m0 = row0 + t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * 128;
+        const Item t = item_at(plan, i, 2 * cols);
+        const int m0 = row0 + t.m0 + (int)rank * 128, n0 = t.n0 + (int)rank * cols;
         for (int kb = t.kb0; kb < t.kb1; ++kb, ++it) {
           const int st = it % kStages;
           if (!mbar_wait(empty_bar(st), ((it / kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           const uint32_t a_dst = smem_base + st * F::kStage, b_dst = a_dst + PARTS * kHalf;
           const uint32_t bar = map_to_cta(full_bar(st), 0);
-          if (leader) mbar_expect_tx(full_bar(st), 2 * F::kStage);
+          if (leader) mbar_expect_tx(full_bar(st), bytes);
 #pragma unroll
           for (int n = 0; n < PARTS; ++n) {
             tma_load_2d_pair(a_dst + n * kHalf, am, bar, kb * kBK, m0 + n * p.piece);
@@ -355,11 +360,11 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
   } else if (warp == 1) {
     // ---------------- products (leader) ----------------
     if (lane == 0 && leader) {
-      const uint32_t idesc = make_idesc_m(256, kTile, 0, TO_X ? 1 : 0);
+      const uint32_t idesc = make_idesc_m(256, 2 * cols, 0, TO_X ? 1 : 0);
       uint32_t it = 0, count = 0;
       bool ok = true;
       for (int i = pair; i < plan.items && ok; i += pairs) {
-        const Item t = item_at(plan, i);
+        const Item t = item_at(plan, i, 2 * cols);
         for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += F::kSpan, ++count) {
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -397,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
     uint32_t count = 0;
     bool ok = true;
     for (int i = pair; i < plan.items && ok; i += pairs) {
-      const Item t = item_at(plan, i);
+      const Item t = item_at(plan, i, 2 * cols);
       const int row = t.m0 + (int)rank * 128 + q * 32 + lane;
       const bool live = row < rows;
       float x[kHeadCols];
@@ -407,9 +412,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         const uint32_t buf = count & 1u, use = count >> 1;
         if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
         tc_fence_after();
-        const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile + half * kHeadCols;
+        const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * kTile + half * cols;
 #pragma unroll
         for (int c = 0; c < kHeadCols; c += 32) {
+          if (c >= cols) break;                            // the last columns of 32 may be another half's, or nothing's
           uint32_t v[32];
           tmem_ld32(acc + c, v);
           tmem_ld_wait();
@@ -421,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
         if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(buf), 0));
       }
       if (!ok) break;
-      const int n0 = t.n0 + half * kHeadCols;
+      const int n0 = t.n0 + half * cols;
       if constexpr (TO_X) grad_row<PARTS>(p, x, plan, t, (int)rank * 8 + q * 2 + half, n0, row, live);
       else logits_row<GRAD, CAP, PARTS>(p, x, n0, row, live);
     }
@@ -472,12 +478,12 @@ cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st) {
   HeadMaps m;
   const bool parts = p.parts == 3;
   if (!tc_encode_2d(&m.a_rows, p.x_rows, (long long)p.parts * p.piece, p.d, p.d, 128, kBK)) return cudaErrorInvalidValue;
-  if (parts ? !tc_encode_2d(&m.b, p.w_parts, 3LL * p.vocab, p.d, p.d, 128, kBK)
-            : !tc_encode_2d(&m.b, p.w, p.vocab, p.d, p.w_stride, 128, kBK) ||
+  if (parts ? !tc_encode_2d(&m.b, p.w_parts, 3LL * p.vocab, p.d, p.d, p.cols, kBK)
+            : !tc_encode_2d(&m.b, p.w, p.vocab, p.d, p.w_stride, p.cols, kBK) ||
                   !tc_encode_2d(&m.a, p.x, p.tokens, p.d, p.x_stride, 128, kBK))
     return cudaErrorInvalidValue;
   if (parts) m.a = m.a_rows;
-  const long long items = (long long)((p.piece + kTile - 1) / kTile) * ((p.vocab + kTile - 1) / kTile);
+  const long long items = (long long)((p.piece + kTile - 1) / kTile) * ((p.vocab + 2 * p.cols - 1) / (2 * p.cols));
   const bool cap = p.softcap > 0.f, grad = p.d_x != nullptr;
   if (parts) {
     if (cap) return grad ? launch<false, true, true, 3>(p, m, items, st) : launch<false, false, true, 3>(p, m, items, st);
