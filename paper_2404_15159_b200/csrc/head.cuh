@@ -108,6 +108,8 @@ cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st);    // sta
 cudaError_t launch_head_logits_few(const HeadArgs& p, bool first, cudaStream_t st);   // the same for up to kHeadFewTokens; clears the state
 cudaError_t launch_head_join(const HeadArgs& p, cudaStream_t st);         // loss, lse, totals; E finished, row_scale
 cudaError_t launch_head_grad_tc(const HeadArgs& p, cudaStream_t st);      // d_x
+cudaError_t launch_head_grad_few(const HeadArgs& p, cudaStream_t st);
+int head_few_shares(int d, int vocab);                                    // arrays [tokens, d] of it in `part`
 int head_pairs();                                                         // CTA pairs of this GPU
 
 }  // namespace mixlora

@@ -42,6 +42,8 @@ mixlora_status_t check_head(const mixlora_head_shape_t* s) {
   return MIXLORA_OK;
 }
 
+bool few_tokens(const mixlora_head_shape_t& s) { return s.dtype == MIXLORA_DTYPE_BF16 && s.tokens <= kHeadFewTokens; }
+
 // Counted rows are worked on in pieces, as many as keep a piece's exponentials within 512 MiB: enough for whole rounds of
 // tiles, and the same whatever the batch.  Without a gradient there are two numbers for 128 columns, and the copy of the
 // rows of x is what counts.
@@ -109,7 +111,8 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   const size_t tiles = piece / kHeadTile * ((size_t)(s.d_model + kHeadTile - 1) / kHeadTile);
   const size_t items = tiles * kHeadMaxShares;
   L.part_items = gradient ? (int)(items < kHeadMaxItems ? items : kHeadMaxItems) : 0;
-  L.part = take((size_t)L.part_items * kHeadTile * kHeadTile * 4);
+  L.part = take(few_tokens(s) ? (gradient ? (size_t)head_few_shares(s.d_model, s.vocab) * tokens * s.d_model * 4 : 0)
+                             : (size_t)L.part_items * kHeadTile * kHeadTile * 4);
   L.total = off;
   return L;
 }
@@ -178,11 +181,11 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   a.join_blocks = L.join_blocks; a.part_items = L.part_items;
 
   if (!c.labels) MIXLORA_TRY(launch_head_lists(a, st));
-  if (L.parts == 1 && s->tokens <= kHeadFewTokens) {
+  if (few_tokens(*s)) {
     a.few = 1;
     MIXLORA_TRY(launch_head_logits_few(a, c.labels != nullptr, st));
     MIXLORA_TRY(launch_head_join(a, st));
-    if (gradient) MIXLORA_TRY(launch_head_grad_tc(a, st));
+    if (gradient) MIXLORA_TRY(launch_head_grad_few(a, st));
     return MIXLORA_OK;
   }
   MIXLORA_TRY(launch_head_scan(a, c.labels != nullptr, st));

@@ -1,11 +1,15 @@
-// Logits of a few tokens (up to 64; bf16): bound by reading the head once.
+// The two products for a few tokens (up to 64; bf16): bound by reading the head, once each.
 //
 // The roles of the operands are turned around: 128 columns of the vocabulary are the rows of a tensor-core tile, the tokens
 // its columns (16, 32 or 64), so that no part of a tile is empty and the head streams through shared memory at the rate of
 // the memory.  One persistent CTA an SM; warp 0 loads (128 reduction elements a stage, so that 256 bytes of each row are
 // asked for at once), warp 1 issues the products, warps 2 to 5 add up the spans (see the kernel for many tokens) and pass
 // the tile through shared memory, and warps 2 to 9 then work on a token each, four neighbouring columns a lane.
-// Rows are tokens here: those that are left out pass through the product too, and the joining kernel drops them.
+// Rows are tokens here: those that are left out pass through the products too, and the joining kernel drops them.
+//
+// The gradient's product goes the same way: 256 columns of d_x are the rows of two tiles, the tokens their columns, and the
+// vocabulary, which is the reduction, is shared out so that every SM has one item.  The shares' sums go to memory, and a
+// kernel of their own adds them up in their order (a few MB that L2 holds; one CTA a tile would read them for 10 us).
 #include <cuda.h>
 #include <math.h>
 
@@ -246,6 +250,184 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   }
 }
 
+// ---- the gradient's product ----
+constexpr int kOut = 256;                                 // columns of d_x of an item
+template <int NC> struct FewGrad {
+  static constexpr uint32_t kABytes = kOut * kBK * 2, kBBytes = NC * kBK * 2, kStage = kABytes + kBBytes;
+  static constexpr int kStages = NC == 64 ? 5 : 6;
+  static constexpr uint32_t kSmem = kStages * kStage + 1024 + 256;
+  static constexpr uint32_t kTmem = 2 * NC < 32 ? 32 : 2 * NC;
+};
+
+template <int NC>
+__global__ void __launch_bounds__(192, 1) head_few_grad_kernel(const __grid_constant__ HeadArgs p,
+                                                               const __grid_constant__ FewMaps maps, int shares) {
+  using F = FewGrad<NC>;
+  constexpr int kStages = F::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * F::kStage);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (kStages + s); };
+  const uint32_t done_bar = bar_base + 8u * (2 * kStages);
+
+  let_next_start();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    mbar_init(done_bar, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_tmap(&maps.w); prefetch_tmap(&maps.x);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), F::kTmem);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+
+  const int tile = blockIdx.x / shares, share = blockIdx.x - tile * shares, c0 = tile * kOut;
+  const int blocks = (p.vocab + kBK - 1) / kBK;
+  const int kb0 = (int)((long long)share * blocks / shares), kb1 = (int)((long long)(share + 1) * blocks / shares);
+  if (warp == 0) {
+    if (lane == 0) {
+      auto load_w = [&](int kb, int st) {
+        mbar_expect_tx(full_bar(st), F::kStage);
+        for (int j = 0; j < kOut / 64; ++j)
+          tma_load_2d(smem_base + st * F::kStage + j * (kBK * 128), &maps.w, full_bar(st), c0 + 64 * j, kb * kBK);
+      };
+      auto load_e = [&](int kb, int st) {
+        tma_load_2d(smem_base + st * F::kStage + F::kABytes, &maps.x, full_bar(st), kb * kBK, 0);
+      };
+      // the head is nobody's result: its first blocks come in while the rows are still being joined
+      const int early = min(kStages, kb1 - kb0);
+      for (int i = 0; i < early; ++i) load_w(kb0 + i, i);
+      wait_for_last();
+      for (int i = 0; i < early; ++i) load_e(kb0 + i, i);
+      bool ok = true;
+      for (int kb = kb0 + early, it = early; kb < kb1; ++kb, ++it) {
+        const int st = it % kStages;
+        if (!mbar_wait(empty_bar(st), ((it / kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        load_w(kb, st);
+        load_e(kb, st);
+      }
+      if (!ok) {
+        *abort_flag = 1;
+        atomicExch(&p.state->status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      wait_for_last();
+      const uint32_t idesc = make_idesc(NC, 1, 0);
+      bool ok = true;
+      for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+        const int st = it % kStages;
+        if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t a_addr = smem_base + st * F::kStage, b_addr = a_addr + F::kABytes;
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int k = 0; k < kBK / kUmmaK; ++k)
+            umma_bf16(tmem_base + sub * NC, make_desc(a_addr + sub * (2 * kBK * 128) + k * (kUmmaK * 128), kBK * 128, 1024),
+                      make_desc(b_addr + k * (kUmmaK * 2), 16, 1024), idesc, kb > kb0 || k > 0);
+        umma_commit(empty_bar(st));
+      }
+      if (ok) {
+        umma_commit(done_bar);
+      } else {
+        *abort_flag = 1;
+        atomicExch(&p.state->status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+      }
+    }
+  } else {
+    wait_for_last();
+    const int q = warp & 3;
+    if (__all_sync(0xffffffffu, mbar_wait(done_bar, 0, abort_flag))) {
+      tc_fence_after();
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const int c = c0 + sub * 128 + q * 32 + lane;
+        float* to = p.part + (size_t)share * p.tokens * p.d + c;
+#pragma unroll
+        for (int t = 0; t < NC; t += 16) {
+          uint32_t v[16];
+          tmem_ld16(tmem_base + ((uint32_t)(q * 32) << 16) + sub * NC + t, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (c < p.d && t + j < p.tokens) to[(size_t)(t + j) * p.d] = __uint_as_float(v[j]);
+        }
+      }
+      tc_fence_before();
+    } else if (lane == 0) {
+      *abort_flag = 1;
+      atomicExch(&p.state->status, (int)MIXLORA_ERR_DEVICE_TIMEOUT);
+    }
+  }
+  __syncthreads();
+  if (*abort_flag) {
+    for (int i = 0; i < 200; ++i) __nanosleep(5000);      // let copies that may still be in flight land
+  }
+  tc_fence_after();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem_base, F::kTmem);
+  }
+}
+
+// d_x from the shares, eight columns of a token a thread
+__global__ void __launch_bounds__(128) head_few_add_kernel(HeadArgs p, int shares) {
+  let_next_start();
+  wait_for_last();
+  const int each = p.d / 8;
+  const int i = blockIdx.x * 128 + threadIdx.x;
+  if (i >= p.tokens * each) return;
+  const int t = i / each, c = (i - t * each) * 8;
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (p.token_row[t] >= 0) {
+    const float* from = p.part + (size_t)t * p.d + c;
+    const size_t apart = (size_t)p.tokens * p.d;
+#pragma unroll 8
+    for (int s = 0; s < shares; ++s) {
+      const float4 a = __ldcg(reinterpret_cast<const float4*>(from + s * apart));
+      const float4 b = __ldcg(reinterpret_cast<const float4*>(from + s * apart + 4));
+      sum[0] += a.x; sum[1] += a.y; sum[2] += a.z; sum[3] += a.w;
+      sum[4] += b.x; sum[5] += b.y; sum[6] += b.z; sum[7] += b.w;
+    }
+    const float by = p.row_scale[t];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] *= by;
+  }
+  uint4 out;
+  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&out);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(sum[2 * j], sum[2 * j + 1]);
+  *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(p.d_x) + (size_t)t * p.dx_stride + c) = out;
+}
+
+template <int NC>
+cudaError_t launch_grad(const HeadArgs& p, cudaStream_t st) {
+  FewMaps m;
+  if (!tc_encode_2d(&m.w, p.w, p.vocab, p.d, p.w_stride, kBK, 64) || !tc_encode_2d(&m.x, p.e, p.piece, p.vocab, p.pitch, NC, kBK))
+    return cudaErrorInvalidValue;
+  static bool done[64] = {false};
+  cudaError_t e = allow_smem(head_few_grad_kernel<NC>, FewGrad<NC>::kSmem, done);
+  if (e != cudaSuccess) return e;
+  const int shares = head_few_shares(p.d, p.vocab), tiles = (p.d + kOut - 1) / kOut;
+  e = launch_behind(head_few_grad_kernel<NC>, (unsigned)(tiles * shares), 192, FewGrad<NC>::kSmem, st, p, m, shares);
+  if (e != cudaSuccess) return e;
+  const int threads = p.tokens * (p.d / 8);
+  return launch_behind(head_few_add_kernel, (unsigned)((threads + 127) / 128), 128, 0, st, p, shares);
+}
+
 template <int NC, bool GRAD, bool CAP>
 cudaError_t launch(const HeadArgs& p, bool first, cudaStream_t st) {
   FewMaps m;
@@ -272,6 +454,19 @@ cudaError_t launch_head_logits_few(const HeadArgs& p, bool first, cudaStream_t s
   if (p.tokens <= 16) return launch_for<16>(p, first, st);
   if (p.tokens <= 32) return launch_for<32>(p, first, st);
   return launch_for<64>(p, first, st);
+}
+
+int head_few_shares(int d, int vocab) {
+  const int tiles = (d + kOut - 1) / kOut, blocks = (vocab + kBK - 1) / kBK;
+  int shares = 2 * kHeadPairs / tiles;
+  if (shares > blocks / 4) shares = blocks / 4;           // no share of less than 4 blocks
+  return shares > 0 ? shares : 1;
+}
+
+cudaError_t launch_head_grad_few(const HeadArgs& p, cudaStream_t st) {
+  if (p.tokens <= 16) return launch_grad<16>(p, st);
+  if (p.tokens <= 32) return launch_grad<32>(p, st);
+  return launch_grad<64>(p, st);
 }
 
 }  // namespace mixlora

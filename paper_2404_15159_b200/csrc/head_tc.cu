@@ -259,9 +259,8 @@ __device__ __forceinline__ void grad_row(const HeadArgs& p, float (&x)[kHeadCols
   if (!live) return;
   const int token = p.row_token[p.piece0 + row];
   const float by = p.row_scale[row];
-  const bool none = p.few && p.token_row[token] < 0;       // a token that is left out: its sums may be anything
 #pragma unroll
-  for (int j = 0; j < kHeadCols; ++j) x[j] = none ? 0.f : by * x[j];
+  for (int j = 0; j < kHeadCols; ++j) x[j] *= by;
   if constexpr (PARTS == 1) {
     bf16* out = reinterpret_cast<bf16*>(p.d_x) + (size_t)token * p.dx_stride + n0;
 #pragma unroll
