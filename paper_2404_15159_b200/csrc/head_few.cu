@@ -73,7 +73,6 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  wait_for_last();
   // what the scan leaves for the later kernels of a call with many tokens
   if (blockIdx.x == 0) {
     for (int i = threadIdx.x; i < kHeadCounters; i += kThreads) p.counters[i] = 0;
@@ -140,6 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
       }
     }
   } else {
+    wait_for_last();                                      // for the lists: the products need the call's inputs alone
     const int q = warp & 3;
     const float factor = p.logit_factor, cap_out = p.cap_out, to2 = p.to2;
     uint32_t count = 0;

@@ -211,14 +211,14 @@ __global__ void __launch_bounds__(kRowThreads) head_gather_kernel(HeadArgs p, in
   }
 }
 
-// The head in parts, a warp a row: memory's 10 bytes a value
+// The head in parts, a warp a row: memory's 10 bytes a value.  It runs beside the scan, of which it needs nothing.
 __global__ void __launch_bounds__(kRowThreads) head_parts_kernel(HeadArgs p) {
   let_next_start();
-  wait_for_last();
   const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
-  if (row >= p.vocab) return;
-  take_apart(reinterpret_cast<const float*>(p.w) + (size_t)row * p.w_stride, p.w_parts + (size_t)row * p.d,
-             (size_t)p.vocab * p.d, p.d);
+  if (row < p.vocab)
+    take_apart(reinterpret_cast<const float*>(p.w) + (size_t)row * p.w_stride, p.w_parts + (size_t)row * p.d,
+               (size_t)p.vocab * p.d, p.d);
+  wait_for_last();
 }
 
 // What a row needs of the exponential and the logarithm: any 64-bit argument, a result good to fp32's relative rounding (the
@@ -380,6 +380,11 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
   for (int pass = 0; pass < 2; ++pass) {
     RowJob job;
     memset(&job, 0, sizeof(job));
+    float2 ahead[kAhead];                              // a lane's first tiles, asked for before anything else
+    auto ask = [&](int i0) {
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) ahead[j] = i0 + 32 * j < job.tiles ? job.stats[i0 + 32 * j] : make_float2(0.f, 0.f);
+    };
     if (pass == 0) {
       BlankRow& b = blank[warp];
       if (lane == 0) {
@@ -393,9 +398,13 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
       job.list = &b.list; job.q = p.labels ? nullptr : &b.q;
       job.z = &b.z; job.loss = &b.loss; job.lse = &b.lse; job.scale = p.d_x ? &b.scale : nullptr;
       job.e = &b.e;
+      ask(lane);
     } else {
       wait_for_last();
-      const int row = blockIdx.x * kWarps + warp, rows = head_rows_here(p);
+      const int row = blockIdx.x * kWarps + warp;
+      job.stats = p.stats + (size_t)row * p.col_tiles; job.tiles = p.col_tiles;
+      ask(lane);
+      const int rows = head_rows_here(p);
       if (p.few) {                                     // no kernel has been over the tokens before
         double sum = 0.0;
         for (int t = lane; t < p.tokens; t += 32)
@@ -411,7 +420,6 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
       if (row >= rows) token = -1;
       if (token >= 0) {
         job.n = p.labels && !p.few ? 1 : head_entries(p, token);
-        job.stats = p.stats + (size_t)row * p.col_tiles; job.tiles = p.col_tiles;
         job.list = p.list + (size_t)token * p.top;
         job.weight = p.weights ? (double)p.weights[token] : 1.0;
         if (!p.labels) {
@@ -442,12 +450,12 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
         s = (s == 0.f ? 0.f : s * exp2f(r - most)) + (s2 == 0.f ? 0.f : s2 * exp2f(r2 - most));
         r = most;
       };
-      for (int i0 = lane; i0 < job.tiles; i0 += 32 * kAhead) {
-        float2 v[kAhead];
+      for (int i0 = lane;;) {
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) v[j] = i0 + 32 * j < job.tiles ? job.stats[i0 + 32 * j] : make_float2(0.f, 0.f);
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) add(v[j].x, v[j].y);
+        for (int j = 0; j < kAhead; ++j) add(ahead[j].x, ahead[j].y);
+        i0 += 32 * kAhead;
+        if (i0 >= job.tiles) break;
+        ask(i0);
       }
 #pragma unroll
       for (int d = 16; d; d >>= 1) {
