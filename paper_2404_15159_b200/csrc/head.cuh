@@ -27,7 +27,6 @@ constexpr int kHeadMaxShares = 16;           // CTA pairs that share one tile's 
 constexpr int kHeadMaxItems = 222;           // shares under way: three rounds of 74 CTA pairs
 constexpr int kHeadPairs = 74;               // CTA pairs of a B200
 constexpr int kHeadMostPairs = 128;          // CTA pairs that a launch uses at most
-constexpr int kHeadCounters = 16 * kHeadMostPairs;   // one for each 32 x 128 corner of a shared tile
 constexpr int kHeadRowsPerBlock = 8;         // rows that a block of the joining kernel takes
 
 // What the kernels of a call leave for one another beside the arrays
@@ -55,7 +54,6 @@ struct HeadArgs {
   float cap_out, to2;             // to2: from x . w (from the tanh) to log2(e) times the logit
   // workspace
   HeadState* state;
-  int32_t* counters;              // arrivals at split tiles, zero between launches
   int32_t* row_token;             // [tokens] token of each counted row, ascending
   int32_t* token_row;             // [tokens] its inverse, -1 for a token that is left out
   const int32_t* list;            // [tokens, top] listed columns ascending, kHeadNone behind the last (labels: the labels)
@@ -101,7 +99,7 @@ __device__ __forceinline__ HeadParts head_parts(float x) {
 }
 
 cudaError_t launch_head_lists(const HeadArgs& p, cudaStream_t st);        // a teacher's entries: list, list_q, rest_q, list_n
-cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st);   // row_token, token_row, state; clears counters
+cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st);   // row_token, token_row, state
 cudaError_t launch_head_parts(const HeadArgs& p, cudaStream_t st);        // fp32 mode: w_parts
 cudaError_t launch_head_gather(const HeadArgs& p, bool first_piece, cudaStream_t st);   // x_rows, zeroes of d_x
 cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st);    // stats, z_listed, E

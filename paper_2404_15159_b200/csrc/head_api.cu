@@ -74,7 +74,7 @@ int head_cols(const mixlora_head_shape_t& s, int parts, int piece) {
 }
 
 struct HeadLayout {
-  size_t state, counters, row_token, token_row, list, list_q, rest_q, list_n, loss_part, x_rows, w_parts, z_listed, stats, e,
+  size_t state, row_token, token_row, list, list_q, rest_q, list_n, loss_part, x_rows, w_parts, z_listed, stats, e,
       row_scale, part, total;
   int parts, piece, pieces, pitch, cols, col_tiles, join_blocks, part_items;
 };
@@ -91,7 +91,6 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
   L.state = take(sizeof(HeadState));
-  L.counters = take(kHeadCounters * 4);
   L.row_token = take(tokens * 4);
   L.token_row = take(tokens * 4);
   const size_t lists = s.teacher_top ? tokens : 0;
@@ -159,7 +158,6 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   a.z_per_xw = (double)s->scale / (double)s->temperature;
   a.z_to_cap = cap ? (double)s->temperature / (double)s->softcap : 0.0;
   a.state = reinterpret_cast<HeadState*>(ws + L.state);
-  a.counters = reinterpret_cast<int32_t*>(ws + L.counters);
   a.row_token = reinterpret_cast<int32_t*>(ws + L.row_token);
   a.token_row = reinterpret_cast<int32_t*>(ws + L.token_row);
   a.list_out = reinterpret_cast<int32_t*>(ws + L.list);

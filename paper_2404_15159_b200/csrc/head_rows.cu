@@ -116,14 +116,13 @@ __device__ __forceinline__ float part_of_each(const HeadArgs& p, double weights)
 }
 
 // Numbers the counted rows and adds up their weights: one block, 8192 tokens a turn.  Rows that are left out get their
-// zeroes here, and the counters of the call are cleared.
+// zeroes here.
 __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
   let_next_start();
   wait_for_last();
   __shared__ int warp_n[32];
   __shared__ double warp_w[32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < kHeadCounters; i += kScanThreads) p.counters[i] = 0;
   int base = 0;
   double weight = 0.0;
   for (int t0 = 0; t0 < p.tokens; t0 += kScanThreads * kScanEach) {

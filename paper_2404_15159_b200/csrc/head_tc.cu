@@ -41,6 +41,7 @@ template <bool TO_X, int PARTS> struct Form {
 };
 // the six products of parts, small ones first
 __device__ constexpr int kPartOfA[6] = {2, 0, 1, 1, 0, 0}, kPartOfB[6] = {0, 2, 1, 0, 1, 0};
+constexpr int kCorners = 16, kCornerSums = 32 * kHeadCols, kTileSums = kCorners * kCornerSums, kAddThreads = 256;
 struct alignas(64) HeadMaps { CUtensorMap a, a_rows, b; };
 
 // How the tiles are dealt out.  Whole rounds of pairs take a tile each, in groups of row tiles (rows fastest) whose
@@ -214,47 +215,17 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     p.stats[(size_t)row * p.col_tiles + n0 / cols] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
 }
 
-// One row of 128 sums of the gradient's product.  Where a tile's reduction is shared, the sums go to `part`, [4 columns]
-// [lane] so that a warp's accesses cover 512 bytes, and the warp that completes its 32 x 128 corner of the tile adds the
-// shares up in their order, whoever it is.
+// One row of 128 sums of the gradient's product.  Where a tile's reduction is shared, the sums go to `part`, corner by corner
+// (32 rows x 128 columns) as [4 columns][row] so that a warp's accesses cover 512 bytes.
 template <int PARTS>
 __device__ __forceinline__ void grad_row(const HeadArgs& p, float (&x)[kHeadCols], const Plan& plan, const Item& t, int corner,
                                          int n0, int row, bool live) {
-  const int lane = threadIdx.x & 31;
   if (t.tile >= 0) {
-    constexpr size_t kCorner = 32 * kHeadCols, kAll = 16 * kCorner;          // floats of a corner, of a tile
-    const float* first = p.part + (size_t)t.tile * plan.shares * kAll + corner * kCorner + lane * 4;
-    float* to = p.part + (size_t)(t.tile * plan.shares + t.share) * kAll + corner * kCorner + lane * 4;
+    float* to = p.part + (size_t)(t.tile * plan.shares + t.share) * kTileSums + corner * kCornerSums + (threadIdx.x & 31) * 4;
 #pragma unroll
     for (int j = 0; j < kHeadCols; j += 4)
       *reinterpret_cast<float4*>(to + j * 32) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
-    __threadfence();
-    __syncwarp();
-    int seen = 0;
-    int* counter = p.counters + t.tile * 16 + corner;
-    if (lane == 0) seen = atomicAdd(counter, 1);
-    if (__shfl_sync(0xffffffffu, seen, 0) != plan.shares - 1) return;
-    __threadfence();
-#pragma unroll
-    for (int c = 0; c < kHeadCols; c += 32) {
-      float4 sum[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int s = 0; s < plan.shares; ++s) {
-        float4 w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = __ldcg(reinterpret_cast<const float4*>(first + s * kAll + (c + 4 * j) * 32));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          sum[j].x += w[j].x; sum[j].y += w[j].y; sum[j].z += w[j].z; sum[j].w += w[j].w;
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[c + 4 * j] = sum[j].x; x[c + 4 * j + 1] = sum[j].y; x[c + 4 * j + 2] = sum[j].z; x[c + 4 * j + 3] = sum[j].w;
-      }
-    }
-    if (lane == 0) *counter = 0;                           // ready for the next piece
+    return;
   }
   if (!live) return;
   const int token = p.row_token[p.piece0 + row];
@@ -273,6 +244,57 @@ __device__ __forceinline__ void grad_row(const HeadArgs& p, float (&x)[kHeadCols
 #pragma unroll
     for (int j = 0; j < kHeadCols; j += 4)
       if (n0 + j < p.d) *reinterpret_cast<float4*>(out + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+  }
+}
+
+// The shared tiles' rows of d_x: a block adds up the shares of one corner, in their order, and turns it for the way out.  In
+// a launch of its own all SMs take part; where the CTA that finished a tile last added it up, 12 shares of 2 MB took it 20 us.
+template <int PARTS>
+__global__ void __launch_bounds__(kAddThreads) head_add_kernel(HeadArgs p, int pairs) {
+  let_next_start();
+  wait_for_last();
+  __shared__ float turn[32][kHeadCols + 4];
+  const int rows = head_rows_here(p);
+  const Plan plan = make_plan<true, PARTS>(rows, (p.d + kTile - 1) / kTile, (p.vocab + kBK - 1) / kBK, pairs, p.part_items);
+  const int tile = blockIdx.x / kCorners, corner = blockIdx.x - tile * kCorners;
+  if (plan.shares == 1 || plan.whole + tile * plan.shares >= plan.items) return;
+  const Item t = item_at(plan, plan.whole + tile * plan.shares, kTile);
+  const int m0 = t.m0 + (corner >> 1) * 32, n0 = t.n0 + (corner & 1) * kHeadCols;
+  if (m0 >= rows || n0 >= p.d) return;
+  const float* from = p.part + (size_t)tile * plan.shares * kTileSums + corner * kCornerSums + threadIdx.x * 4;
+  constexpr int kEach = kCornerSums / 4 / kAddThreads;
+  float4 sum[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+  for (int s = 0; s < plan.shares; ++s) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(from + s * kTileSums + i * kAddThreads * 4));
+      sum[i].x += v.x; sum[i].y += v.y; sum[i].z += v.z; sum[i].w += v.w;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int at = threadIdx.x + i * kAddThreads;          // [4 columns][row]
+    *reinterpret_cast<float4*>(&turn[at & 31][(at >> 5) * 4]) = sum[i];
+  }
+  __syncthreads();
+  constexpr int kWide = PARTS == 1 ? 8 : 4;                // values of 16 bytes
+  for (int i = threadIdx.x; i < kCornerSums / kWide; i += kAddThreads) {
+    const int r = i / (kHeadCols / kWide), c = (i - r * (kHeadCols / kWide)) * kWide;
+    if (m0 + r >= rows || n0 + c >= p.d) continue;
+    const float by = p.row_scale[m0 + r];
+    const size_t at = (size_t)p.row_token[p.piece0 + m0 + r] * p.dx_stride + n0 + c;
+    const float4 lo = *reinterpret_cast<const float4*>(&turn[r][c]);
+    if constexpr (PARTS == 1) {
+      const float4 up = *reinterpret_cast<const float4*>(&turn[r][c + 4]);
+      *reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(p.d_x) + at) =
+          make_uint4(pack_bf16(by * lo.x, by * lo.y), pack_bf16(by * lo.z, by * lo.w), pack_bf16(by * up.x, by * up.y),
+                     pack_bf16(by * up.z, by * up.w));
+    } else {
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.d_x) + at) = make_float4(by * lo.x, by * lo.y, by * lo.z, by * lo.w);
+    }
   }
 }
 
@@ -499,7 +521,12 @@ cudaError_t launch_head_grad_tc(const HeadArgs& p, cudaStream_t st) {
       !tc_encode_2d(&m.b, parts ? p.w_parts : p.w, (long long)p.parts * p.vocab, p.d, parts ? p.d : p.w_stride, kBK, 64))
     return cudaErrorInvalidValue;
   m.a = m.a_rows;
-  return parts ? launch<true, true, false, 3>(p, m, head_pairs(), st) : launch<true, true, false, 1>(p, m, head_pairs(), st);
+  const int pairs = head_pairs();
+  const cudaError_t e = parts ? launch<true, true, false, 3>(p, m, pairs, st) : launch<true, true, false, 1>(p, m, pairs, st);
+  if (e != cudaSuccess) return e;
+  const unsigned blocks = (unsigned)((pairs - 1) * kCorners);     // less than a round of tiles is shared
+  return parts ? launch_behind(head_add_kernel<3>, blocks, kAddThreads, 0, st, p, pairs)
+               : launch_behind(head_add_kernel<1>, blocks, kAddThreads, 0, st, p, pairs);
 }
 
 }  // namespace mixlora
