@@ -430,7 +430,7 @@ typedef struct {
   float scale;                /* > 0 */
   float softcap;              /* 0: none */
   float temperature;          /* > 0 */
-  float z_loss;               /* >= 0 */
+  float z_loss;               /* 0 .. 2^20 */
   int32_t reserved;           /* 0 */
   int64_t x_stride, w_stride, d_x_stride;
 } mixlora_head_shape_t;

@@ -23,7 +23,7 @@ mixlora_status_t check_head(const mixlora_head_shape_t* s) {
   if (s->tokens < 0 || s->d_model <= 0 || s->vocab <= 0 || s->teacher_top < 0) return MIXLORA_ERR_INVALID_ARG;
   if (s->dtype != MIXLORA_DTYPE_BF16 && s->dtype != MIXLORA_DTYPE_FP32) return MIXLORA_ERR_INVALID_ARG;
   if (!isfinite(s->scale) || s->scale <= 0.f || !isfinite(s->temperature) || s->temperature <= 0.f ||
-      !isfinite(s->softcap) || s->softcap < 0.f || !isfinite(s->z_loss) || s->z_loss < 0.f)
+      !isfinite(s->softcap) || s->softcap < 0.f || !(s->z_loss >= 0.f && s->z_loss <= 0x1p20f))
     return MIXLORA_ERR_INVALID_ARG;
   // the factors that the kernels form of them, in fp32: none may leave the normal range
   if (!isnormal(s->scale / s->temperature) || !isnormal(s->scale / s->temperature * 1.4426950408889634f)) return MIXLORA_ERR_INVALID_ARG;

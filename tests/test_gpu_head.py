@@ -134,8 +134,9 @@ def test_order_and_repeats_of_a_list_are_free(B):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
-def test_strided_rows_and_garbage_where_nothing_counts(B, dtype):
-    t, v, d = 200, 900, 96
+@pytest.mark.parametrize("t", [200, 40])
+def test_strided_rows_and_garbage_where_nothing_counts(B, t, dtype):
+    v, d = 900, 96
     g, x, w = rand(5, t, v, d, dtype, 2.0)
     labels = torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
     labels[torch.rand(t, generator=g, device="cuda") < 0.5] = -1

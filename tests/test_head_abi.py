@@ -36,7 +36,7 @@ BAD = [
     (dict(vocab=-5), INVALID), (dict(dtype=2), INVALID), (dict(reserved=1), INVALID), (dict(scale=0.0), INVALID),
     (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID),
     (dict(softcap=-1.0), INVALID), (dict(softcap=float("inf")), INVALID), (dict(temperature=0.0), INVALID),
-    (dict(temperature=float("nan")), INVALID), (dict(z_loss=-1.0), INVALID), (dict(z_loss=float("inf")), INVALID),
+    (dict(temperature=float("nan")), INVALID), (dict(z_loss=-1.0), INVALID), (dict(z_loss=float("inf")), INVALID), (dict(z_loss=2e6), INVALID), (dict(z_loss=float("nan")), INVALID),
     (dict(scale=1e-30, temperature=1e20), INVALID), (dict(scale=1e30, temperature=1e-20), INVALID),
     (dict(softcap=1e-30, scale=1e20), INVALID), (dict(softcap=1e30, temperature=1e-20), INVALID),
     (dict(x_stride=32), INVALID), (dict(w_stride=-64), INVALID), (dict(d_x_stride=8), INVALID),
