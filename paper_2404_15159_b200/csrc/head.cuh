@@ -72,7 +72,6 @@ struct HeadArgs {
   // the piece of counted rows that a launch works on
   int piece0, piece;              // first row, most rows
   int pitch, cols, col_tiles;     // cols: columns that share R and S, half a tile of the logits
-  int join_blocks;                // of the joining kernel, over all pieces
   int part_items;                 // that `part` has room for
   int parts;                      // bf16 values that hold an operand: 1, or 3 in the fp32 mode
   int few;                        // rows are tokens, those that are left out among them

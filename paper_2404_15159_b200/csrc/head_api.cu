@@ -76,7 +76,7 @@ int head_cols(const mixlora_head_shape_t& s, int parts, int piece) {
 struct HeadLayout {
   size_t state, row_token, token_row, list, list_q, rest_q, list_n, loss_part, x_rows, w_parts, z_listed, stats, e,
       row_scale, part, total;
-  int parts, piece, pieces, pitch, cols, col_tiles, join_blocks, part_items;
+  int parts, piece, pieces, pitch, cols, col_tiles, part_items;
 };
 HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   const size_t tokens = (size_t)s.tokens, top = s.teacher_top ? (size_t)s.teacher_top : 1;
@@ -87,7 +87,6 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   L.pitch = (s.vocab + 7) / 8 * 8;
   L.cols = head_cols(s, L.parts, L.piece);
   L.col_tiles = (s.vocab + L.cols - 1) / L.cols;
-  L.join_blocks = L.pieces * (L.piece / kHeadRowsPerBlock);
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
   L.state = take(sizeof(HeadState));
@@ -98,7 +97,7 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   L.list_q = take(lists * top * 8);
   L.rest_q = take(lists * 8);
   L.list_n = take(lists * 4);
-  L.loss_part = take((size_t)L.join_blocks * 8);
+  L.loss_part = take((tokens / kHeadRowsPerBlock + 1) * 8);
   const size_t piece = (size_t)L.piece;
   L.x_rows = take(piece * s.d_model * 2 * L.parts);
   L.w_parts = take(L.parts == 3 ? (size_t)s.vocab * s.d_model * 6 : 0);
@@ -176,7 +175,7 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   a.row_scale = reinterpret_cast<float*>(ws + L.row_scale);
   a.part = reinterpret_cast<float*>(ws + L.part);
   a.piece = L.piece; a.pitch = L.pitch; a.cols = L.cols; a.col_tiles = L.col_tiles;
-  a.join_blocks = L.join_blocks; a.part_items = L.part_items;
+  a.part_items = L.part_items;
 
   if (!c.labels) MIXLORA_TRY(launch_head_lists(a, st));
   if (few_tokens(*s)) {

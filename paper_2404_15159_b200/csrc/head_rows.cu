@@ -115,56 +115,61 @@ __device__ __forceinline__ float part_of_each(const HeadArgs& p, double weights)
   return norm == 0.0 ? 0.f : 1.f / (float)norm;
 }
 
-// Numbers the counted rows and adds up their weights: one block, 8192 tokens a turn.  Rows that are left out get their
-// zeroes here.
+// Numbers the counted rows and adds up their weights: one block, 8192 tokens a turn, eight to a thread and a warp's 32 side
+// by side.  Rows that are left out get their zeroes here.
 __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
+  constexpr int kWarps = kScanThreads / 32, kCounts = kScanEach * kWarps;
   let_next_start();
   wait_for_last();
-  __shared__ int warp_n[32];
-  __shared__ double warp_w[32];
+  __shared__ int counts[kCounts], of_eight[32];            // counted tokens of each 32, then of those before them
+  __shared__ double warp_w[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int base = 0;
   double weight = 0.0;
   for (int t0 = 0; t0 < p.tokens; t0 += kScanThreads * kScanEach) {
-    const int first = t0 + threadIdx.x * kScanEach;
-    unsigned in = 0;
+    unsigned in[kScanEach];
 #pragma unroll
     for (int j = 0; j < kScanEach; ++j) {
-      const int t = first + j;
-      if (t >= p.tokens) break;
-      const bool ok = head_entries(p, t) > 0;
-      in |= (unsigned)ok << j;
+      const int t = t0 + j * kScanThreads + threadIdx.x;
+      const bool ok = t < p.tokens && head_entries(p, t) > 0;
+      in[j] = __ballot_sync(0xffffffffu, ok);
       if (ok) {
         weight += p.weights ? (double)p.weights[t] : 1.0;
-      } else {
+      } else if (t < p.tokens) {
         p.loss[t] = 0.f;
         if (p.lse) p.lse[t] = 0.f;
       }
+      if (lane == 0) counts[j * kWarps + warp] = __popc(in[j]);
     }
-    const int n = __popc(in);
-    int upto = n;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= d) upto += up;
-    }
-    if (lane == 31) warp_n[warp] = upto;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int i = 0; i < kScanThreads / 32; ++i) {
-      if (i < warp) before += warp_n[i];
-      all += warp_n[i];
+    // 256 counts: 32 threads add up eight each, and one of those 32
+    if (threadIdx.x < kCounts / 8) {
+      int sum = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int n = counts[threadIdx.x * 8 + j];
+        counts[threadIdx.x * 8 + j] = sum;
+        sum += n;
+      }
+      int upto = sum;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += up;
+      }
+      of_eight[lane] = upto;
     }
-    int row = base + before + upto - n;
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < kScanEach; ++j) {
-      const int t = first + j;
-      if (t >= p.tokens) break;
-      const bool ok = in >> j & 1;
+      const int t = t0 + j * kScanThreads + threadIdx.x, at = j * kWarps + warp;
+      if (t >= p.tokens) continue;
+      const int row = base + counts[at] + (at >= 8 ? of_eight[at / 8 - 1] : 0) + __popc(in[j] & ((1u << lane) - 1u));
+      const bool ok = in[j] >> lane & 1;
       p.token_row[t] = ok ? row : -1;
-      if (ok) p.row_token[row++] = t;
+      if (ok) p.row_token[row] = t;
     }
-    base += all;
+    base += of_eight[31];
     __syncthreads();
   }
   weight = warp_sum(weight);
@@ -172,7 +177,7 @@ __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
   __syncthreads();
   if (threadIdx.x == 0) {
     double sum = 0.0;
-    for (int i = 0; i < kScanThreads / 32; ++i) sum += warp_w[i];
+    for (int i = 0; i < kWarps; ++i) sum += warp_w[i];
     p.state->status = 0;
     p.state->counted = base;
     p.state->joined = 0;
@@ -180,6 +185,7 @@ __global__ void __launch_bounds__(kScanThreads) head_scan_kernel(HeadArgs p) {
     p.state->each = part_of_each(p, sum);
   }
 }
+static_assert(kScanEach * kScanThreads / 32 == 256, "the scan's counts are added up by one warp, eight a lane");
 
 // The counted rows of this piece side by side, where tokens are left out (the products then pass over nothing else) or an
 // fp32 row is taken apart, and zeroes for the gradients of the tokens that are left out.  A warp a token.
@@ -341,11 +347,12 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, const RowJob&
 // R with the listed columns' factors in their places.  A ninth warp adds up the blocks' weighted losses meanwhile: the block
 // that comes last does so, in the blocks' order.
 //
-// A block runs through its code once on a row of its own making while the kernel before it still runs: the instructions have
-// then been fetched when the sums arrive (they are 8 KB, and a launch of few rows waited longer for them than it computed).
+// The blocks that can be there early run through their code once on a row of their own making while the kernel before them
+// still runs: the instructions have then been fetched when the sums arrive (a launch of few rows waited longer for its 8 KB
+// of them than it computed).
 struct BlankRow { float2 stats; double q; float z, loss, lse, scale; int32_t list; bf16 e; };
 __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p) {
-  constexpr int kWarps = kRowThreads / 32, kAhead = 8;
+  constexpr int kWarps = kRowThreads / 32, kAhead = 8, kWarmBlocks = 3 * 148;
   let_next_start();
   __shared__ double warp_w[kWarps];
   __shared__ float weights;
@@ -353,21 +360,23 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (warp == kWarps) {
     wait_for_last();
+    // blocks that have rows, over all pieces; where none has, the first one is left to write the totals
+    const int block = p.piece0 / kWarps + blockIdx.x, blocks = max((p.state->counted + kWarps - 1) / kWarps, 1);
     __syncthreads();
-    const int block = p.piece0 / kWarps + blockIdx.x;
+    if (block >= blocks) return;
     int last = 0;
     if (lane == 0) {
       double mine = 0.0;
       for (int i = 0; i < kWarps; ++i) mine += warp_w[i];
       p.loss_part[block] = mine;
       __threadfence();
-      last = atomicAdd(&p.state->joined, 1) == p.join_blocks - 1;
+      last = atomicAdd(&p.state->joined, 1) == blocks - 1;
     }
     if (!__shfl_sync(0xffffffffu, last, 0) || !p.totals) return;
     __threadfence();
     double sum = 0.0;
 #pragma unroll 8
-    for (int i = lane; i < p.join_blocks; i += 32) sum += __ldcg(p.loss_part + i);
+    for (int i = lane; i < blocks; i += 32) sum += __ldcg(p.loss_part + i);
     sum = warp_sum(sum);
     if (lane == 0) {
       p.totals[0] = (float)sum;
@@ -376,7 +385,7 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
     return;
   }
 #pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {
+  for (int pass = blockIdx.x < kWarmBlocks ? 0 : 1; pass < 2; ++pass) {
     RowJob job;
     memset(&job, 0, sizeof(job));
     float2 ahead[kAhead];                              // a lane's first tiles, asked for before anything else
