@@ -226,13 +226,35 @@ __global__ void __launch_bounds__(kRowThreads) head_parts_kernel(HeadArgs p) {
   wait_for_last();
 }
 
-// What a row needs of the exponential and the logarithm: any 64-bit argument, a result good to fp32's relative rounding (the
-// logits behind it are no better).  The power of two goes by the exponent's bits, the rest through the fp32 function; the
-// 64-bit functions are ten times the code, and fetching that once a launch took longer than all of a row's work.
+// What a row needs of the exponential and the logarithm in 64 bits, good to about 2^-33: a divergence is a small difference
+// of logarithms.  Powers of two go by the exponent's bits, the rest by the series.  The library's functions are several times
+// the code, and fetching that once a launch took longer than all of a row's work.
+__device__ __forceinline__ double recip64(double x) {      // x in fp32's range
+  double r = (double)__fdividef(1.f, (float)x);
+  r = r * fma(-x, r, 2.0);
+  return r * fma(-x, r, 2.0);
+}
 __device__ __forceinline__ double exp64(double x) {
   if (x < -690.0) return 0.0;
-  const double k = rint(fmin(x, 700.0) * kLog2ed);
-  return (double)expf((float)fma(-k, kLn2d, x)) * __hiloint2double((1023 + (int)k) << 20, 0);
+  const double k = rint(fmin(x, 700.0) * kLog2ed), t = fma(-k, kLn2d, x);      // |t| <= 0.35
+  double y = 1.0 / 40320;                                  // t^n / n! up to the eighth: the ninth is 2e-10
+  y = fma(y, t, 1.0 / 5040);
+  y = fma(y, t, 1.0 / 720);
+  y = fma(y, t, 1.0 / 120);
+  y = fma(y, t, 1.0 / 24);
+  y = fma(y, t, 1.0 / 6);
+  y = fma(y, t, 0.5);
+  y = fma(y, t, 1.0);
+  y = fma(y, t, 1.0);
+  return y * __hiloint2double((1023 + (int)k) << 20, 0);
+}
+// ln((1 + t) / (1 - t)) = 2 (t + t^3 / 3 + ...), |t| <= 1/3: relatively, what is left out is 1e-10
+__device__ __forceinline__ double twice_artanh(double t) {
+  const double u = t * t;
+  double y = 1.0 / 17;
+#pragma unroll
+  for (int n = 15; n >= 1; n -= 2) y = fma(y, u, 1.0 / n);
+  return 2.0 * t * y;
 }
 __device__ __forceinline__ double log64(double x) {        // x > 0
   if (x < 0x1p-1000) x = 0x1p-1000;
@@ -240,13 +262,9 @@ __device__ __forceinline__ double log64(double x) {        // x > 0
   double m = __hiloint2double((hi & 0x000fffff) | 0x3ff00000, __double2loint(x));
   int e = (hi >> 20) - 1023;
   if (m > 1.4142135623730951) { m *= 0.5; ++e; }
-  return e > 1023 ? x : (double)log1pf((float)(m - 1.0)) + e * kLn2d;
+  return e > 1023 ? x : twice_artanh((m - 1.0) * recip64(m + 1.0)) + e * kLn2d;
 }
-__device__ __forceinline__ double recip64(double x) {      // x in fp32's range
-  double r = (double)__fdividef(1.f, (float)x);
-  r = r * fma(-x, r, 2.0);
-  return r * fma(-x, r, 2.0);
-}
+__device__ __forceinline__ double log1p64(double x) { return twice_artanh(x * recip64(2.0 + x)); }      // 0 <= x <= 1
 
 // What a warp of the joining kernel works on
 struct RowJob {
@@ -277,7 +295,7 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, const RowJob&
     // loss = ln(1 + e^gap) without a difference of two logarithms, and 1 - p without one from one
     most = (double)__shfl_sync(0xffffffffu, lane == 0 ? z[0] : 0.f, 0);     // lane 0 writes it below
     const double gap = lr - most, e = exp64(-fabs(gap));
-    loss = (gap < 0.0 ? 0.0 : gap) + (double)log1pf((float)e);
+    loss = (gap < 0.0 ? 0.0 : gap) + log1p64(e);
     miss = (gap > 0.0 ? 1.0 : e) * recip64(1.0 + e);
     lse = most + loss;
   } else {

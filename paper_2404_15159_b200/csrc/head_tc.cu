@@ -33,9 +33,11 @@ template <bool TO_X, int PARTS> struct Form {
   static constexpr int kStages = PARTS == 1 ? 6 : 2;
   static constexpr uint32_t kStage = PARTS * 2 * kHalf;
   static constexpr uint32_t kSmem = kStages * kStage + 1024 + 256;
-  // k-blocks of a span: 64 steps of the tensor core (24 with parts).  The gradient's product is rounded to bf16 in the
-  // end, where 512 steps are nothing
-  static constexpr int kSpan = PARTS == 3 ? 1 : (TO_X ? 128 : 16);
+  // k-blocks of the span that starts `done` k-blocks into a sum.  The logits' first two are long, since the warps that take
+  // the sums are then still busy with the tile before (its exponentials take about 20 k-blocks' time; with 8 k-blocks from the
+  // start 4096 tokens took 866 us, with 16 throughout 835).  The gradient's product is rounded to bf16 in the end, where 512
+  // steps are nothing, and with parts a k-block is 24 steps already.
+  static __device__ __forceinline__ int span(int done) { return PARTS == 3 ? 1 : (TO_X ? 128 : (done < 20 ? 10 : 4)); }
   // a share of a split reduction keeps at least this many k-blocks, and costs this many on top (partial sums out and in)
   static constexpr int kShareMin = PARTS == 1 ? 16 : 3, kShareCost = PARTS == 1 ? 24 : 4;
 };
@@ -386,12 +388,13 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       bool ok = true;
       for (int i = pair; i < plan.items && ok; i += pairs) {
         const Item t = item_at(plan, i, 2 * cols);
-        for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 += F::kSpan, ++count) {
+        for (int k0 = t.kb0, k1; k0 < t.kb1 && ok; k0 = k1, ++count) {
+          k1 = min(k0 + F::span(k0 - t.kb0), t.kb1);
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + buf * kTile;
-          for (int kb = k0; kb < min(k0 + F::kSpan, t.kb1); ++kb, ++it) {
+          for (int kb = k0; kb < k1; ++kb, ++it) {
             const int st = it % kStages;
             if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
             tc_fence_after();
@@ -429,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       float x[kHeadCols];
 #pragma unroll
       for (int j = 0; j < kHeadCols; ++j) x[j] = 0.f;
-      for (int k0 = t.kb0; k0 < t.kb1; k0 += F::kSpan, ++count) {
+      for (int k0 = t.kb0; k0 < t.kb1; k0 += F::span(k0 - t.kb0), ++count) {
         const uint32_t buf = count & 1u, use = count >> 1;
         if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
         tc_fence_after();
