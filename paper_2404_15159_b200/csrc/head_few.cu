@@ -21,8 +21,7 @@ namespace {
 
 using namespace tc;
 constexpr int kWarps = 8, kThreads = 64 + 32 * kWarps, kBK = 64, kUmmaK = 16;
-// stages of 128 reduction elements of the span that starts `done` stages into a sum (see the kernel for many tokens)
-__device__ __forceinline__ int span(int done) { return done < 8 ? 4 : 2; }
+constexpr int kSpan = 4;                                  // stages of 128 reduction elements
 constexpr uint32_t kABytes = 2 * 128 * kBK * 2;
 template <int NC> struct Few {
   static constexpr uint32_t kBBytes = 2 * NC * kBK * 2, kStage = kABytes + kBBytes;
@@ -110,12 +109,12 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
       uint32_t it = 0, count = 0;
       bool ok = true;
       for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
-        for (int s0 = 0; s0 < steps && ok; s0 += span(s0), ++count) {
+        for (int s0 = 0; s0 < steps && ok; s0 += kSpan, ++count) {
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + buf * NC;
-          for (int s = s0; s < min(s0 + span(s0), steps); ++s, ++it) {
+          for (int s = s0; s < min(s0 + kSpan, steps); ++s, ++it) {
             const int st = it % kStages;
             if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
             tc_fence_after();
@@ -147,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
       if (warp < 6) {
 #pragma unroll
         for (int j = 0; j < NC; ++j) x[j] = 0.f;
-        for (int s0 = 0; s0 < steps; s0 += span(s0), ++count) {
+        for (int s0 = 0; s0 < steps; s0 += kSpan, ++count) {
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
           tc_fence_after();

@@ -33,11 +33,11 @@ template <bool TO_X, int PARTS> struct Form {
   static constexpr int kStages = PARTS == 1 ? 6 : 2;
   static constexpr uint32_t kStage = PARTS * 2 * kHalf;
   static constexpr uint32_t kSmem = kStages * kStage + 1024 + 256;
-  // k-blocks of the span that starts `done` k-blocks into a sum.  The logits' first two are long, since the warps that take
-  // the sums are then still busy with the tile before (its exponentials take about 20 k-blocks' time; with 8 k-blocks from the
-  // start 4096 tokens took 866 us, with 16 throughout 835).  The gradient's product is rounded to bf16 in the end, where 512
-  // steps are nothing, and with parts a k-block is 24 steps already.
-  static __device__ __forceinline__ int span(int done) { return PARTS == 3 ? 1 : (TO_X ? 128 : (done < 20 ? 10 : 4)); }
+  // k-blocks of a span, 64 steps of the tensor core.  A span's end costs it about 360 cycles, since the sums are read from
+  // the memory that it works in: at width 4096 spans of 4 / 8 / 16 / 32 k-blocks took 926 / 866 / 835 / 825 us for 4096 tokens,
+  // with losses off by 1e-7 / 3e-7 / 6e-7 / 1.2e-6 (fp32's own products: 6e-7).  The gradient's product is rounded to bf16 in
+  // the end, where 512 steps are nothing, and with parts a k-block is 24 steps already.
+  static constexpr int kSpan = PARTS == 3 ? 1 : (TO_X ? 128 : 16);
   // a share of a split reduction keeps at least this many k-blocks, and costs this many on top (partial sums out and in)
   static constexpr int kShareMin = PARTS == 1 ? 16 : 3, kShareCost = PARTS == 1 ? 24 : 4;
 };
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       for (int i = pair; i < plan.items && ok; i += pairs) {
         const Item t = item_at(plan, i, 2 * cols);
         for (int k0 = t.kb0, k1; k0 < t.kb1 && ok; k0 = k1, ++count) {
-          k1 = min(k0 + F::span(k0 - t.kb0), t.kb1);
+          k1 = min(k0 + F::kSpan, t.kb1);
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       float x[kHeadCols];
 #pragma unroll
       for (int j = 0; j < kHeadCols; ++j) x[j] = 0.f;
-      for (int k0 = t.kb0; k0 < t.kb1; k0 += F::span(k0 - t.kb0), ++count) {
+      for (int k0 = t.kb0; k0 < t.kb1; k0 += F::kSpan, ++count) {
         const uint32_t buf = count & 1u, use = count >> 1;
         if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
         tc_fence_after();
