@@ -87,10 +87,11 @@ __device__ __forceinline__ int head_rows_here(const HeadArgs& p) {
 
 // A value as the sum of three bf16 ones: the first is cut off (rounding could overflow), the others are rounded, which
 // leaves nothing of 24 bits.
+__device__ __forceinline__ float head_cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 struct HeadParts { float v[3]; };
 __device__ __forceinline__ HeadParts head_parts(float x) {
   HeadParts p;
-  p.v[0] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  p.v[0] = head_cut(x);
   const float rest = x - p.v[0];
   p.v[1] = __bfloat162float(__float2bfloat16(rest));
   p.v[2] = rest - p.v[1];

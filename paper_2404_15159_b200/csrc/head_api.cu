@@ -84,7 +84,7 @@ HeadLayout head_layout(const mixlora_head_shape_t& s, bool gradient) {
   L.parts = s.dtype == MIXLORA_DTYPE_BF16 ? 1 : 3;
   L.piece = piece_rows(s, gradient, L.parts);
   L.pieces = (s.tokens + L.piece - 1) / L.piece;
-  L.pitch = (s.vocab + 7) / 8 * 8;
+  L.pitch = (s.vocab + 15) / 16 * 16;                      // rows of E start at 32 bytes
   L.cols = head_cols(s, L.parts, L.piece);
   L.col_tiles = (s.vocab + L.cols - 1) / L.cols;
   size_t off = 0;

@@ -46,6 +46,13 @@ __device__ constexpr int kPartOfA[6] = {2, 0, 1, 1, 0, 0}, kPartOfB[6] = {0, 2, 
 constexpr int kCorners = 16, kCornerSums = 32 * kHeadCols, kTileSums = kCorners * kCornerSums, kAddThreads = 256;
 struct alignas(64) HeadMaps { CUtensorMap a, a_rows, b; };
 
+// 32 bytes, at such a boundary, with one instruction: a warp's rows are far apart, and every instruction visits all of them
+__device__ __forceinline__ void store_32(void* to, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+               "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+
 // How the tiles are dealt out.  Whole rounds of pairs take a tile each, in groups of row tiles (rows fastest) whose
 // operands stay in L2 while the columns pass; the tiles of the last, partial round are shared out over their reduction,
 // so that no pair is idle in it: the number of shares with the least rounds x (k-blocks + what a share costs).
@@ -191,26 +198,30 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
       sum[j & 3] += ex;
       v = CAP ? ex * slope : ex;
     }
-    if (GRAD && live) {
+    if (GRAD && live && n0 + kChunk * c < p.pitch) {
 #pragma unroll
-      for (int j = kChunk * c; j < kChunk * c + kChunk; j += 8)
-        if (n0 + j < p.pitch) {
-          if constexpr (PARTS == 1) {
-            *reinterpret_cast<uint4*>(e + j) = make_uint4(pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]),
-                                                          pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
+      for (int n = 0; n < PARTS; ++n) {
+        uint32_t out[kChunk / 2];
+#pragma unroll
+        for (int j = 0; j < kChunk; j += 2) {
+          float &lo = x[kChunk * c + j], &up = x[kChunk * c + j + 1];
+          if (PARTS == 3 && n == 0) {                      // a part, and what it leaves for the next
+            const float a = head_cut(lo), b = head_cut(up);
+            out[j / 2] = pack_bf16(a, b);
+            lo -= a;
+            up -= b;
           } else {
-            uint32_t part[3][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const HeadParts lo = head_parts(x[j + 2 * i]), up = head_parts(x[j + 2 * i + 1]);
-#pragma unroll
-              for (int n = 0; n < 3; ++n) part[n][i] = pack_bf16(lo.v[n], up.v[n]);
+            const __nv_bfloat162 h = __floats2bfloat162_rn(lo, up);
+            out[j / 2] = *reinterpret_cast<const uint32_t*>(&h);
+            if (PARTS == 3 && n == 1) {
+              const float2 f = __bfloat1622float2(h);
+              lo -= f.x;
+              up -= f.y;
             }
-#pragma unroll
-            for (int n = 0; n < 3; ++n)
-              *reinterpret_cast<uint4*>(e + n * p.e_part + j) = make_uint4(part[n][0], part[n][1], part[n][2], part[n][3]);
           }
         }
+        store_32(e + n * p.e_part + kChunk * c, out);
+      }
     }
   }
   if (live && n0 < p.vocab)
