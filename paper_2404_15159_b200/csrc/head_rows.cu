@@ -1,7 +1,9 @@
 // What the head's losses do once a row: which rows count, a teacher's lists, and the join of a row's tiles.
 //
-// All of it is small beside the products (8192 rows of 32000 columns: TODO us of TODO), so what can lose bits by
-// cancellation is done in 64 bits: probabilities of a teacher, log-sum-exps, gradients towards listed columns.
+// All of it is small beside the products (8192 rows of 32000 columns: scan 10, join 27 of 3390 us; 4096 rows with 64 entries:
+// lists 10, scan 5, rows side by side 12, join 25 of 1660), so what can lose bits by cancellation is done in 64 bits:
+// probabilities of a teacher, log-sum-exps, gradients towards listed columns.  With few rows these kernels wait for one load
+// after another; each starts under its predecessor, and the join is 5 to 9 us of a call of 40.
 #include <math.h>
 #include <string.h>
 
@@ -26,16 +28,24 @@ __device__ __forceinline__ double warp_max(double v) {
   return v;
 }
 
+constexpr int kCopies = 4;      // 16-byte loads that a lane has under way
 // A row of n fp32 values (a multiple of 8) into three rows of bf16, `apart` values from one to the next, by a warp
 __device__ __forceinline__ void take_apart(const float* src, bf16* dst, size_t apart, int n) {
-  for (int i = (threadIdx.x & 31) * 4; i < n; i += 128) {
-    const float4 v = *reinterpret_cast<const float4*>(src + i);
-    const HeadParts a = head_parts(v.x), b = head_parts(v.y), c = head_parts(v.z), d = head_parts(v.w);
+  for (int i0 = (threadIdx.x & 31) * 4; i0 < n; i0 += 128 * kCopies) {
+    float4 v[kCopies];
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const __nv_bfloat162 lo = __floats2bfloat162_rn(a.v[k], b.v[k]), up = __floats2bfloat162_rn(c.v[k], d.v[k]);
-      *reinterpret_cast<uint2*>(dst + k * apart + i) =
-          make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&up));
+    for (int j = 0; j < kCopies; ++j)
+      if (i0 + 128 * j < n) v[j] = *reinterpret_cast<const float4*>(src + i0 + 128 * j);
+#pragma unroll
+    for (int j = 0; j < kCopies; ++j) {
+      if (i0 + 128 * j >= n) break;
+      const HeadParts a = head_parts(v[j].x), b = head_parts(v[j].y), c = head_parts(v[j].z), d = head_parts(v[j].w);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(a.v[k], b.v[k]), up = __floats2bfloat162_rn(c.v[k], d.v[k]);
+        *reinterpret_cast<uint2*>(dst + k * apart + i0 + 128 * j) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&up));
+      }
     }
   }
 }
@@ -209,7 +219,15 @@ __global__ void __launch_bounds__(kRowThreads) head_gather_kernel(HeadArgs p, in
   if (PARTS == 1) {
     const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(p.x) + (size_t)t * p.x_stride);
     uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(p.x_rows) + (size_t)row * p.d);
-    for (int i = lane; i < p.d / 8; i += 32) dst[i] = src[i];
+    for (int i = lane; i < p.d / 8; i += 32 * kCopies) {
+      uint4 v[kCopies];
+#pragma unroll
+      for (int j = 0; j < kCopies; ++j)
+        if (i + 32 * j < p.d / 8) v[j] = src[i + 32 * j];
+#pragma unroll
+      for (int j = 0; j < kCopies; ++j)
+        if (i + 32 * j < p.d / 8) dst[i + 32 * j] = v[j];
+    }
   } else {
     take_apart(reinterpret_cast<const float*>(p.x) + (size_t)t * p.x_stride,
                reinterpret_cast<bf16*>(p.x_rows) + (size_t)row * p.d, (size_t)p.piece * p.d, p.d);

@@ -12,6 +12,11 @@
 // 2^-20 of a logit, always towards zero.  So a sum starts anew every span of k-blocks, and the parts are added up in
 // registers, rounded to nearest.
 //
+// Measured on a B200, 8192 rows, 32000 columns, width 4096: logits 1.45 ms, gradient 1.41 ms in short runs (1.48 and
+// 1.52 PFLOP/s, tensor pipe 83 and 90 % active at 1.6 and 1.45 GHz under the power cap), 3.39 ms a call one after another
+// (1.27 PFLOP/s; the library's own dense product in such a loop: 1.38).  512 rows: 112 and 97 us (four rounds of tiles for
+// 3.4; tiles that are narrower wait for their operands as long).
+//
 // In the fp32 mode (PARTS = 3) an operand is the sum of three bf16 values that hold its 24 bits, and the six products of
 // parts that matter at 2^-24 are added up, the small ones first: exact to fp32's own rounding, at a sixth of the rate, which
 // is still three times that of the fp32 pipes.
