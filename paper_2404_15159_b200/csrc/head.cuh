@@ -21,7 +21,7 @@ constexpr int kHeadTile = 256;               // rows and columns of a tile of th
 constexpr int kHeadCols = 128;               // most columns that share R and S
 constexpr int kHeadLeastCols = 64;
 constexpr float kHeadStep = 100.f;           // R's step, in powers of two
-constexpr int kHeadFewTokens = 64;
+constexpr int kHeadFewTokens = 64;           // tokens up to which the head is streamed (bf16)
 constexpr int kHeadNone = 0x7fffffff;        // no column (ends a row's list)
 constexpr int kHeadMaxShares = 16;           // CTA pairs that share one tile's reduction
 constexpr int kHeadMaxItems = 222;           // shares under way: three rounds of 74 CTA pairs
@@ -74,7 +74,7 @@ struct HeadArgs {
   int pitch, cols, col_tiles;     // cols: columns that share R and S, half a tile of the logits
   int part_items;                 // that `part` has room for
   int parts;                      // bf16 values that hold an operand: 1, or 3 in the fp32 mode
-  int few;                        // rows are tokens, those that are left out among them
+  int few;                        // no more tokens than a tile has rows: rows are tokens, those that are left out among them
 };
 
 // Entries of a token's list, 0 where it is left out
@@ -82,8 +82,11 @@ __device__ __forceinline__ int head_entries(const HeadArgs& p, int token) {
   return p.labels ? (p.labels[token] >= 0 && p.labels[token] < p.vocab) : p.list_n[token];
 }
 __device__ __forceinline__ int head_rows_here(const HeadArgs& p) {
-  return min(max(p.state->counted - p.piece0, 0), p.piece);
+  return p.few ? p.tokens : min(max(p.state->counted - p.piece0, 0), p.piece);
 }
+__device__ __forceinline__ int head_token(const HeadArgs& p, int row) { return p.few ? row : p.row_token[p.piece0 + row]; }
+// Whether a token has no gradient, whatever its sums are
+__device__ __forceinline__ bool head_left_out(const HeadArgs& p, int token) { return p.few && p.token_row[token] < 0; }
 
 // A value as the sum of three bf16 ones: the first is cut off (rounding could overflow), the others are rounded, which
 // leaves nothing of 24 bits.
@@ -99,8 +102,8 @@ __device__ __forceinline__ HeadParts head_parts(float x) {
 }
 
 cudaError_t launch_head_lists(const HeadArgs& p, cudaStream_t st);        // a teacher's entries: list, list_q, rest_q, list_n
-cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st);   // row_token, token_row, state
-cudaError_t launch_head_parts(const HeadArgs& p, cudaStream_t st);        // fp32 mode: w_parts
+cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st);   // row_token, token_row, state (few tokens: none of it needed)
+cudaError_t launch_head_parts(const HeadArgs& p, bool first, cudaStream_t st);   // fp32 mode: w_parts; x_rows where rows are tokens
 cudaError_t launch_head_gather(const HeadArgs& p, bool first_piece, cudaStream_t st);   // x_rows, zeroes of d_x
 cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st);    // stats, z_listed, E
 cudaError_t launch_head_logits_few(const HeadArgs& p, bool first, cudaStream_t st);   // the same for up to kHeadFewTokens; clears the state

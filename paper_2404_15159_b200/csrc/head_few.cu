@@ -76,10 +76,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  // what the scan leaves for the later kernels of a call with many tokens
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     p.state->status = 0;
-    p.state->counted = p.tokens;
     p.state->joined = 0;
   }
 

@@ -234,13 +234,17 @@ __global__ void __launch_bounds__(kRowThreads) head_gather_kernel(HeadArgs p, in
   }
 }
 
-// The head in parts, a warp a row: memory's 10 bytes a value.  It runs beside the scan, of which it needs nothing.
+// The head in parts, a warp a row: memory's 10 bytes a value; behind it, where rows are tokens, those of x.  It runs beside
+// the scan or the lists, of which it needs nothing.
 __global__ void __launch_bounds__(kRowThreads) head_parts_kernel(HeadArgs p) {
   let_next_start();
   const int row = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);
   if (row < p.vocab)
     take_apart(reinterpret_cast<const float*>(p.w) + (size_t)row * p.w_stride, p.w_parts + (size_t)row * p.d,
                (size_t)p.vocab * p.d, p.d);
+  else if (p.few && row - p.vocab < p.tokens)
+    take_apart(reinterpret_cast<const float*>(p.x) + (size_t)(row - p.vocab) * p.x_stride,
+               reinterpret_cast<bf16*>(p.x_rows) + (size_t)(row - p.vocab) * p.d, (size_t)p.piece * p.d, p.d);
   wait_for_last();
 }
 
@@ -397,7 +401,8 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
   if (warp == kWarps) {
     wait_for_last();
     // blocks that have rows, over all pieces; where none has, the first one is left to write the totals
-    const int block = p.piece0 / kWarps + blockIdx.x, blocks = max((p.state->counted + kWarps - 1) / kWarps, 1);
+    const int block = p.piece0 / kWarps + blockIdx.x, counted = p.few ? p.tokens : p.state->counted,
+              blocks = max((counted + kWarps - 1) / kWarps, 1);
     __syncthreads();
     if (block >= blocks) return;
     int last = 0;
@@ -569,9 +574,12 @@ cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_head_parts(const HeadArgs& p, cudaStream_t st) {
-  const unsigned blocks = (unsigned)((p.vocab + kRowThreads / 32 - 1) / (kRowThreads / 32));
-  return launch_behind(head_parts_kernel, blocks, kRowThreads, 0, st, p);
+cudaError_t launch_head_parts(const HeadArgs& p, bool first, cudaStream_t st) {
+  const int rows = p.vocab + (p.few ? p.tokens : 0);
+  const unsigned blocks = (unsigned)((rows + kRowThreads / 32 - 1) / (kRowThreads / 32));
+  if (!first) return launch_behind(head_parts_kernel, blocks, kRowThreads, 0, st, p);
+  head_parts_kernel<<<blocks, kRowThreads, 0, st>>>(p);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_head_gather(const HeadArgs& p, bool first_piece, cudaStream_t st) {

@@ -132,7 +132,7 @@ template <bool GRAD, bool CAP, int PARTS>
 __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCols], int n0, int row, bool live) {
   constexpr int kChunk = 16, kChunks = kHeadCols / kChunk;
   const int cols = p.cols;
-  const int token = live ? p.row_token[p.piece0 + row] : 0;
+  const int token = live ? head_token(p, row) : 0;
   const int32_t* list = p.list + (size_t)token * p.top;
   // the first listed column that may be among these
   int at = 0;
@@ -246,10 +246,11 @@ __device__ __forceinline__ void grad_row(const HeadArgs& p, float (&x)[kHeadCols
     return;
   }
   if (!live) return;
-  const int token = p.row_token[p.piece0 + row];
+  const int token = head_token(p, row);
   const float by = p.row_scale[row];
+  const bool none = head_left_out(p, token);
 #pragma unroll
-  for (int j = 0; j < kHeadCols; ++j) x[j] *= by;
+  for (int j = 0; j < kHeadCols; ++j) x[j] = none ? 0.f : x[j] * by;
   if constexpr (PARTS == 1) {
     bf16* out = reinterpret_cast<bf16*>(p.d_x) + (size_t)token * p.dx_stride + n0;
 #pragma unroll
@@ -303,7 +304,14 @@ __global__ void __launch_bounds__(kAddThreads) head_add_kernel(HeadArgs p, int p
     const int r = i / (kHeadCols / kWide), c = (i - r * (kHeadCols / kWide)) * kWide;
     if (m0 + r >= rows || n0 + c >= p.d) continue;
     const float by = p.row_scale[m0 + r];
-    const size_t at = (size_t)p.row_token[p.piece0 + m0 + r] * p.dx_stride + n0 + c;
+    const int token = head_token(p, m0 + r);
+    const size_t at = (size_t)token * p.dx_stride + n0 + c;
+    if (head_left_out(p, token)) {
+      uint4* to = PARTS == 1 ? reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(p.d_x) + at)
+                             : reinterpret_cast<uint4*>(reinterpret_cast<float*>(p.d_x) + at);
+      *to = make_uint4(0, 0, 0, 0);
+      continue;
+    }
     const float4 lo = *reinterpret_cast<const float4*>(&turn[r][c]);
     if constexpr (PARTS == 1) {
       const float4 up = *reinterpret_cast<const float4*>(&turn[r][c + 4]);
@@ -354,6 +362,10 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
   const uint32_t tmem_base = *tmem_slot;
   wait_for_last();
 
+  if (!TO_X && p.few && blockIdx.x == 0 && threadIdx.x == 0) {
+    p.state->status = 0;
+    p.state->joined = 0;
+  }
   const int rows = head_rows_here(p);
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const int cols = TO_X ? kHeadCols : p.cols;              // half of a tile's columns
@@ -364,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
     // ---------------- loads (both CTAs, each its own halves) ----------------
     if (lane == 0) {
       // where every token counts, x itself holds the rows (not its parts)
-      const bool direct = !TO_X && PARTS == 1 && p.state->counted == p.tokens;
+      const bool direct = !TO_X && PARTS == 1 && (p.few || p.state->counted == p.tokens);
       const CUtensorMap* am = direct ? &maps.a : &maps.a_rows;
       const int row0 = direct ? p.piece0 : 0;
       const uint32_t bytes = 2 * PARTS * (kHalf + cols * kBK * 2);      // of both CTAs' operands

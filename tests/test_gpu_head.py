@@ -262,3 +262,30 @@ def test_many_tiles_and_spans(B, t, v, d, top, softcap, grad):
         args = (torch.randint(-v // 4, v, (t,), generator=g, device="cuda", dtype=torch.int32),)
     weights = torch.rand(t, generator=g, device="cuda")
     check(B, run(B, x, w, *args, weights=weights, grad=grad, **opt), want(x, w, *args, weights=weights, gradient=grad, **opt))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("top", [0, 5])
+@pytest.mark.parametrize("t", [64, 65, 200, 256, 257])
+def test_left_out_tokens_on_both_sides_of_a_tile(B, t, top, dtype):
+    # up to a tile's rows the tokens that are left out pass through the products, behind it they do not; labels just behind the
+    # vocabulary fall into its last tile
+    v, d = 700, 128
+    g, x, w = rand(13, t, v, d, dtype, 3.0)
+    out = torch.rand(t, generator=g, device="cuda") < 0.4
+    out[0] = False
+    x[out] = torch.tensor([float("nan"), float("inf")], device="cuda", dtype=dtype).repeat(d // 2)
+    weights = torch.rand(t, generator=g, device="cuda")
+    weights[out] = float("nan")
+    if top:
+        index, logit = lists(g, t, v, top, ragged=False)
+        index[out] = v + 1
+        args = (index, logit)
+    else:
+        labels = torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+        labels[out] = v + 3
+        args = (labels,)
+    got = run(B, x, w, *args, weights=weights)
+    ref = want(torch.where(out[:, None], torch.zeros_like(x), x), w, *args, weights=torch.where(out, torch.zeros_like(weights), weights))
+    check(B, got, ref)
+    assert (got["d_x"][out] == 0).all() and (got["loss"][out] == 0).all()
