@@ -51,6 +51,7 @@ int piece_rows(const mixlora_head_shape_t& s, bool gradient, int parts) {
   long long row = 2LL * parts * s.d_model;
   const long long wide = gradient ? 2LL * parts * s.vocab : (s.vocab + kHeadLeastCols - 1) / kHeadLeastCols * 8LL;
   if (row < wide) row = wide;
+  if (row < 4LL * s.teacher_top) row = 4LL * s.teacher_top;          // the listed logits
   long long rows = (512LL << 20) / row / kHeadTile * kHeadTile;
   if (rows < kHeadTile) rows = kHeadTile;
   const long long all = ((long long)s.tokens + kHeadTile - 1) / kHeadTile * kHeadTile;

@@ -201,3 +201,23 @@ def test_calls_of_different_shapes_share_a_workspace_in_turn(B):
     for t, top, grad in ((700, 0, True), (3, 0, False), (64, 9, True), (65, 256, True), (700, 3, False), (1, 0, True)):
         args = lists(g, t, 4001, top) if top else (torch.randint(0, 4001, (t,), generator=g, device="cuda", dtype=torch.int32),)
         check(B, run(B, x[:t], w, *args, ws=ws, grad=grad), want(x[:t], w, *args, gradient=grad))
+
+
+@pytest.mark.parametrize("t,top,dtype", CALLS)
+def test_outputs_that_nobody_wants(B, t, top, dtype):
+    g, x, w = rand(37, t, 2001, 128, dtype, 2.0)
+    args = lists(g, t, 2001, top) if top else (torch.randint(-900, 2001, (t,), generator=g, device="cuda", dtype=torch.int32),)
+    full = run(B, x, w, *args)
+    code = B.MIXLORA_DTYPE_BF16 if dtype == torch.bfloat16 else B.MIXLORA_DTYPE_FP32
+    shape = B.make_head_shape(t, 128, 2001, code, teacher_top=top)
+    loss, d_x, ws = torch.empty(t, device="cuda"), torch.empty_like(x), B.alloc_head_workspace(shape, True)
+    tail = (None, None, loss, None, None, d_x, ws)
+    if top:
+        B.mixlora_head_distill(shape, x, w, args[0], args[1], None, *tail)
+    else:
+        B.mixlora_head_loss(shape, x, w, args[0], *tail)
+    torch.cuda.synchronize()
+    assert torch.equal(loss, full["loss"]) and torch.equal(d_x, full["d_x"]) and B.mixlora_device_status(ws) == 0
+    # the loss alone takes the same sums; a gradient's workspace serves it too
+    alone = run(B, x, w, *args, grad=False, ws=ws)
+    assert all(torch.equal(alone[n], full[n]) for n in ("loss", "lse", "totals"))

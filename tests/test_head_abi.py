@@ -78,6 +78,9 @@ def test_workspace_is_bounded_by_the_piece(B):
             few, many = (size(B.make_head_shape(t, 1024, vocab, dtype), 1) for t in (1 << 19, 1 << 20))
             parts = 0 if dtype == B.MIXLORA_DTYPE_BF16 else 6 * vocab * 1024      # the fp32 head taken apart
             assert few - parts < 2.7e9 and many - few <= 32 * (1 << 19)      # a few numbers a token
+    # a teacher's entries and their probabilities, 12 bytes each, are what grows with them
+    lists = B.make_head_shape(1 << 20, 64, 2, teacher_top=256)
+    assert size(lists, 1) < 12.1 * (256 << 20) + 2e9
     assert size(B.make_head_shape(8192, 4096, 32000), 0) < size(B.make_head_shape(8192, 4096, 32000), 1)
 
 
