@@ -382,8 +382,8 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
                                             const float *lse, const void *d_o, void *workspace, size_t workspace_bytes,
                                             void *d_q, void *d_k, void *d_v, void *stream);
 
-/* Losses at the end of a MixLoRA model: from the last hidden states (after the final norm) and the frozen output head to a
- * loss and the gradient towards the hidden states, which mixlora_layer_backward of the last layer takes as dh (the paper
+/* Losses at the end of a MixLoRA model: from what enters the frozen output head to a loss and the gradient towards it, which
+ * mixlora_layer_backward of the last layer takes as dh (through the norm between them, where a model has one; the paper
  * trains with the language-model loss and prints no formula).  Logits are formed a tile at a time and never kept.
  *     z_tv = cap(scale x_t . w_v) / temperature,   cap(y) = softcap tanh(y / softcap), or y where softcap = 0
  *     lse_t = ln sum_v e^(z_tv),   p_tv = e^(z_tv - lse_t)
@@ -402,18 +402,19 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
  * Divergences carry no factor temperature^2; a caller that wants it puts it into the weights.
  *
  * Outputs: loss [T] and lse [T] (may be NULL), 0 for tokens that are left out; totals [2] (may be NULL) = {sum_t weight_t
- * loss_t, sum_t weight_t} over the others, in an order that does not change; d_x [T, d] (NULL: loss only, about a third of
- * the time) = the gradient of sum_t weight_t loss_t / normalizer, 0 for tokens that are left out.  weights [T] fp32 or NULL
+ * loss_t, sum_t weight_t} over the others, in an order that does not change; d_x [T, d] (NULL: loss only, about half of the
+ * time) = the gradient of sum_t weight_t loss_t / normalizer, 0 for tokens that are left out.  weights [T] fp32 or NULL
  * (all 1); `normalizer` is a device scalar, or NULL for this call's own sum of weights (data-parallel shards pass the sum
  * over all shards); where it is 0 the gradient is 0.  w gets no gradient.
  *
  * x, d_x [T, d], w [vocab, d] of shape.dtype, 16-byte aligned, rows *_stride elements apart (0: dense); d_x must not
  * overlap an input.  d_model and the strides are multiples of 8.  Tokens that are left out cost nothing in the products.
  * Logits are sums in fp32, and so are the gradients of the fp32 mode, where operands are taken apart into three bf16 values
- * that hold their 24 bits (values below 2^-100 lose some).  Factors of the gradient's product are rounded once to shape.dtype (relatively, after all
- * differences have been taken, so that a confident token's small gradient keeps its precision); where a row's listed
- * columns hold more than 2^70 times the weight of all others, the others' part of the gradient may become zero.  Results
- * do not depend on the order in which blocks run.
+ * that hold their 24 bits (values below 2^-100 lose some).  With bf16 the factors of the gradient's product are rounded to
+ * it, relatively and after all differences have been taken, so that a confident token's small gradient keeps its precision:
+ * within one half step for a listed column, within two for another.  Where a row's listed columns hold more than 2^70 times
+ * the weight of all others, the others' part of the gradient may become zero; logits beyond 2^20 promise no result.
+ * Results do not depend on the order in which blocks run.
  * An inf or NaN in a token's x makes its own loss and gradient NaN (and totals[0]), no other token's; one in w reaches every
  * token.  Tokens that are left out may hold anything.
  * The workspace (256-byte aligned, mixlora_head_workspace_bytes) is scratch of one call: whatever the batch, about 1.2 GB (in

@@ -4,9 +4,9 @@
 //   grad     E [rows, vocab] . w [vocab, d]  times the row's A scale / temperature weight / normalizer, to the row's token
 //
 // Pairs of CTAs work on 256 x 256 tiles (cta_group::2, 128 rows of the accumulator and half of B's columns each; the logits'
-// tiles may be narrower, see head_cols), one persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the products, warps 2 to 9 take finished sums into
-// registers, 128 columns of one row a thread, and turn them into results while the next sums are under way.  The number of
-// rows is read on the device: tokens without a label take no part.
+// tiles may be narrower, see head_cols), one persistent pair on two SMs; warp 0 loads, warp 1 of the leader issues the
+// products, warps 2 to 9 take finished sums into registers, 128 columns of one row a thread, and turn them into results
+// while the next sums are under way.  The number of rows is read on the device: tokens without a label take no part.
 //
 // The tensor core cuts off what a sum has behind its 24 bits, at every step of 16 products: over 4096 of them that is a few
 // 2^-20 of a logit, always towards zero.  So a sum starts anew every span of k-blocks, and the parts are added up in
