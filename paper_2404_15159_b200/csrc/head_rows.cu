@@ -278,13 +278,14 @@ __device__ __forceinline__ double twice_artanh(double t) {
   for (int n = 15; n >= 1; n -= 2) y = fma(y, u, 1.0 / n);
   return 2.0 * t * y;
 }
-__device__ __forceinline__ double log64(double x) {        // x > 0
+__device__ __forceinline__ double log64(double x) {        // x > 0, or no number of either sign
+  if (!(x <= 0x1.fffffffffffffp+1023)) return x;
   if (x < 0x1p-1000) x = 0x1p-1000;
   const int hi = __double2hiint(x);
   double m = __hiloint2double((hi & 0x000fffff) | 0x3ff00000, __double2loint(x));
   int e = (hi >> 20) - 1023;
   if (m > 1.4142135623730951) { m *= 0.5; ++e; }
-  return e > 1023 ? x : twice_artanh((m - 1.0) * recip64(m + 1.0)) + e * kLn2d;
+  return twice_artanh((m - 1.0) * recip64(m + 1.0)) + e * kLn2d;
 }
 __device__ __forceinline__ double log1p64(double x) { return twice_artanh(x * recip64(2.0 + x)); }      // 0 <= x <= 1
 
