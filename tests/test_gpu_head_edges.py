@@ -49,3 +49,46 @@ def test_the_lse_of_a_listed_logit_that_is_infinite_is_no_number(B, tail, t):
     got = run(B, x, w, index, logit, torch.logsumexp(logit, 1) + 0.3 if tail else None)
     torch.cuda.synchronize()
     assert got["lse"].isnan().all() and got["loss"].isnan().all()
+
+
+def exact_logits(z):
+    """fp32 states and head whose logits are the fp32 numbers z [t, v] themselves: a token picks its column of the head."""
+    t = z.shape[0]
+    d = (t + 7) // 8 * 8
+    x, w = torch.zeros(t, d, device="cuda"), torch.zeros(z.shape[1], d, device="cuda")
+    x[torch.arange(t), torch.arange(t)] = 1.0
+    w[:, :t] = z.T
+    return x, w
+
+
+def test_a_small_divergence_of_exact_logits_keeps_its_digits(B):
+    # every column is listed, so that no sum in 32 bits takes part: loss = sum q (ln q - z + lse) of logits and probabilities in 64.
+    # The exponential's series leaves out 1e-11 relatively, the logarithm's less, where |ln of a fraction| is largest, 0.49 ln 2;
+    # and the loss is rounded once.
+    g = torch.Generator(device="cuda").manual_seed(42)
+    t, v = 56, 64
+    z = -0.49 * 0.6931 * torch.randint(0, 2, (t, v), generator=g, device="cuda").float()
+    z[1::3] = 3 * torch.randn(t, v, generator=g, device="cuda")[1::3]
+    z[:, 0] = 0.0
+    u = z + 2.0 ** -8 * torch.randn(t, v, generator=g, device="cuda")
+    x, w = exact_logits(z)
+    index = torch.arange(v, dtype=torch.int32, device="cuda").repeat(t, 1)
+    got = run(B, x, w, index, u, grad=False)
+    log_q, log_p = torch.log_softmax(u.double(), 1), torch.log_softmax(z.double(), 1)
+    loss = (log_q.exp() * (log_q - log_p)).sum(1)
+    assert float(loss.max()) < 1e-3
+    assert bool(((got["loss"].double() - loss).abs() <= 2.0 ** -34 + 2.0 ** -24 * loss).all())
+    lse = torch.logsumexp(z.double(), 1)
+    assert bool(((got["lse"].double() - lse).abs() <= 2.0 ** -34 + 2.0 ** -24 * lse.abs()).all())
+
+
+def test_a_loss_of_two_exact_logits_is_rounded_once(B):
+    # one other column, of logit 0, whose sum is 1 without a rounding: loss = ln(1 + e^-z), its series good to 2^-32
+    z = torch.cat([torch.linspace(-85.0, 85.0, 171, device="cuda"), torch.linspace(-1.0, 1.0, 165, device="cuda")])
+    x, w = exact_logits(torch.stack([z, torch.zeros_like(z)], 1))
+    got = run(B, x, w, torch.zeros(z.numel(), dtype=torch.int32, device="cuda"), grad=False)
+    loss = torch.nn.functional.softplus(-z.double(), threshold=1000.0)
+    loss = torch.where(z > 0, torch.log1p(torch.exp(-z.double())), loss)
+    assert bool(((got["loss"].double() - loss).abs() <= (2.0 ** -24 + 2.0 ** -31) * loss + 2.0 ** -149).all())
+    lse = torch.nn.functional.softplus(z.double(), threshold=1000.0)
+    assert bool(((got["lse"].double() - lse).abs() <= (2.0 ** -24 + 2.0 ** -31) * lse + 2.0 ** -31 * z.double().abs()).all())
