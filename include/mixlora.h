@@ -415,8 +415,9 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
  * within one half step for a listed column, within two for another.  Where a row's listed columns hold more than 2^70 times
  * the weight of all others, the others' part of the gradient may become zero; logits beyond 2^20 promise no result.
  * Results do not depend on the order in which blocks run.
- * An inf or NaN in a token's x makes its own loss and gradient NaN (and totals[0]), no other token's; one in w reaches every
- * token.  Tokens that are left out may hold anything.
+ * An inf or NaN in a token's x makes its own loss, lse and gradient NaN (and totals[0]), no other token's; one in w reaches
+ * every token.  So does a product x . w beyond fp32's range, also where a cap would bend it to a number.  Tokens that are left
+ * out may hold anything.
  * The workspace (256-byte aligned, mixlora_head_workspace_bytes) is scratch of one call: whatever the batch, about 1.2 GB (in
  * fp32 mode 2.7 GB and 6 bytes for each value of w) at most beside a few numbers a token and the teacher's entries; calls
  * that may run at the same time need one each; mixlora_device_status works on it. */

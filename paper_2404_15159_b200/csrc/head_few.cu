@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
             if (at >> 2 == lane) {
               const int j = at & 3;
               const float raw = (j == 0 ? v[0] : j == 1 ? v[1] : j == 2 ? v[2] : v[3]) * factor;
-              p.z_listed[(size_t)t * p.top + k0 + l] = CAP ? tanhf(raw) * cap_out : raw;
+              p.z_listed[(size_t)t * p.top + k0 + l] = fmaf(raw, 0.f, CAP ? tanhf(raw) * cap_out : raw);
               dead |= 1u << j;
             }
           }
@@ -217,8 +217,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
           } else {
             ex = exp2_fast(fmaf(v[j], to2, -r));
           }
+          sum += dead >> j & 1 ? 0.f : fmaf(v[j], 0.f, ex);      // no number where the product is infinite
           if (dead >> j & 1) ex = 0.f;
-          sum += ex;
           v[j] = CAP ? ex * slope : ex;
         }
 #pragma unroll

@@ -129,6 +129,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // One row of up to 128 logits, in registers, by one thread: the listed ones are put aside, the others become exponentials.
+// A cap, or an exponential, would make a number of a product that is infinite: 0 times it is added to what the row leaves.
 template <bool GRAD, bool CAP, int PARTS>
 __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCols], int n0, int row, bool live) {
   constexpr int kChunk = 16, kChunks = kHeadCols / kChunk;
@@ -149,7 +150,7 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
   const float factor = p.logit_factor, cap_out = p.cap_out, to2 = p.to2;
   int next = live && at < p.top ? list[at] : kHeadNone;
   uint32_t dead[kChunks];       // a bit for each column that is listed or behind the vocabulary
-  float most = -INFINITY;
+  float most = -INFINITY, far = 0.f;       // far: the largest magnitude
 #pragma unroll
   for (int c = 0; c < kChunks; ++c) {
     if (c * kChunk >= cols) break;
@@ -166,7 +167,7 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
       for (int j = 0; j < kChunk; ++j)
         if (named >> j & 1) {
           const float raw = x[kChunk * c + j] * factor;
-          *z++ = CAP ? tanhf(raw) * cap_out : raw;
+          *z++ = fmaf(raw, 0.f, CAP ? tanhf(raw) * cap_out : raw);
         }
     }
     __syncwarp();
@@ -174,10 +175,16 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     if (__any_sync(0xffffffffu, dead[c])) {
 #pragma unroll
       for (int j = 0; j < kChunk; ++j)
-        if (!(dead[c] >> j & 1)) most = fmaxf(most, x[kChunk * c + j]);
+        if (!(dead[c] >> j & 1)) {
+          most = fmaxf(most, x[kChunk * c + j]);
+          far = fmaxf(far, fabsf(x[kChunk * c + j]));
+        }
     } else {
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) most = fmaxf(most, x[kChunk * c + j]);
+      for (int j = 0; j < kChunk; ++j) {
+        most = fmaxf(most, x[kChunk * c + j]);
+        far = fmaxf(far, fabsf(x[kChunk * c + j]));
+      }
     }
   }
   most *= factor;
@@ -231,7 +238,7 @@ __device__ __forceinline__ void logits_row(const HeadArgs& p, float (&x)[kHeadCo
     }
   }
   if (live && n0 < p.vocab)
-    p.stats[(size_t)row * p.col_tiles + n0 / cols] = make_float2(r, (sum[0] + sum[1]) + (sum[2] + sum[3]));
+    p.stats[(size_t)row * p.col_tiles + n0 / cols] = make_float2(r, fmaf(far, 0.f, (sum[0] + sum[1]) + (sum[2] + sum[3])));
 }
 
 // One row of 128 sums of the gradient's product.  Where a tile's reduction is shared, the sums go to `part`, corner by corner

@@ -92,3 +92,59 @@ def test_a_loss_of_two_exact_logits_is_rounded_once(B):
     assert bool(((got["loss"].double() - loss).abs() <= (2.0 ** -24 + 2.0 ** -31) * loss + 2.0 ** -149).all())
     lse = torch.nn.functional.softplus(z.double(), threshold=1000.0)
     assert bool(((got["lse"].double() - lse).abs() <= (2.0 ** -24 + 2.0 ** -31) * lse + 2.0 ** -31 * z.double().abs()).all())
+
+
+@TYPES
+@TOKENS
+@pytest.mark.parametrize("kind", ["labels", "listed", "tail"])
+@pytest.mark.parametrize("softcap", [0.0, 4.0])
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+def test_a_token_that_is_no_number_says_so_and_stays_alone(B, bad, softcap, kind, t, dtype):
+    # a cap makes numbers of infinite products, and an exponential a zero of those below: neither hides them
+    v = 300
+    g, x, w = rand(43, t, v, 64, dtype)
+    args = targets(kind, g, t, v)
+    x[7, 3], x[t - 1, 60] = bad, bad
+    out = torch.tensor([7, t - 1], device="cuda")
+    keep = torch.ones(t, dtype=torch.bool, device="cuda").index_fill(0, out, False)
+    norm = torch.full((1,), float(t), device="cuda")
+    got = run(B, x, w, *args, softcap=softcap, normalizer=norm)
+    torch.cuda.synchronize()
+    for n in ("loss", "lse", "d_x"):
+        assert got[n][out].isnan().all(), n
+    assert got["totals"][0].isnan() and got["totals"][1] == t
+    x[out] = 0
+    ref = want(x, w, *args, softcap=softcap, normalizer=float(t))
+    for n in ("loss", "lse", "d_x"):
+        off = (got[n].double() - ref[n]).abs()[keep]
+        assert bool((off <= ref["bound"][n][keep]).all()), n
+
+
+@TYPES
+@TOKENS
+@pytest.mark.parametrize("kind", ["labels", "listed", "tail"])
+@pytest.mark.parametrize("softcap", [0.0, 4.0])
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+def test_a_head_that_is_no_number_reaches_every_token(B, bad, softcap, kind, t, dtype):
+    v = 300
+    g, x, w = rand(44, t, v, 64, dtype)
+    args = targets(kind, g, t, v)
+    args[0][:2] = 17                       # listed for some, not for others
+    args[0][2] = -1                        # left out
+    w[17, 5] = bad
+    for grad in (True, False):
+        got = run(B, x, w, *args, softcap=softcap, grad=grad)
+        torch.cuda.synchronize()
+        for n in ("loss", "lse", "d_x")[: 3 if grad else 2]:
+            keep = torch.arange(t, device="cuda") != 2
+            assert got[n][keep].isnan().all() and (got[n][2] == 0).all(), n
+
+
+@TYPES
+@pytest.mark.parametrize("bad", [INF, -INF])
+def test_one_column_of_infinite_logits(B, bad, dtype):
+    g, x, w = rand(45, 3, 1, 64, dtype)
+    x[1] = torch.sign(w[0].float()).to(dtype) * bad
+    got = run(B, x, w, torch.zeros(3, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert got["loss"].isnan().tolist() == [False, True, False] and got["d_x"].isnan().any(1).tolist() == [False, True, False]
