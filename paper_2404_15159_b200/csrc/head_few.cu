@@ -3,8 +3,10 @@
 // The roles of the operands are turned around: 128 columns of the vocabulary are the rows of a tensor-core tile, the tokens
 // its columns (16, 32 or 64), so that no part of a tile is empty and the head streams through shared memory at the rate of
 // the memory.  One persistent CTA an SM; warp 0 loads (128 reduction elements a stage, so that 256 bytes of each row are
-// asked for at once), warp 1 issues the products, warps 2 to 5 add up the spans (see the kernel for many tokens) and pass
-// the tile through shared memory, and warps 2 to 9 then work on a token each, four neighbouring columns a lane.
+// asked for at once), warp 1 issues the products, warps 2 to 5 add up the stages' sums in registers, rounded to nearest (what the
+// tensor core cuts off in 8 steps is 1 unit of 2^-23 of a logit where a sum of 4096 products at once would lose 35; it
+// runs up to 8 stages ahead of them), and pass the tile through shared memory, and warps 2 to 9 then work on a token each, four
+// neighbouring columns a lane.
 // Rows are tokens here: those that are left out pass through the products too, and the joining kernel drops them.
 //
 // The gradient's product goes the same way: 256 columns of d_x are the rows of two tiles, the tokens their columns, and the
@@ -24,7 +26,7 @@ namespace {
 
 using namespace tc;
 constexpr int kWarps = 8, kThreads = 64 + 32 * kWarps, kBK = 64, kUmmaK = 16;
-constexpr int kSpan = 4;                                  // stages of 128 reduction elements
+constexpr int kBufs = 8;                                  // accumulators, one a stage
 constexpr uint32_t kABytes = 2 * 128 * kBK * 2;
 template <int NC> struct Few {
   static constexpr uint32_t kBBytes = 2 * NC * kBK * 2, kStage = kABytes + kBBytes;
@@ -49,7 +51,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* turn = reinterpret_cast<float*>(smem + kStages * F::kStage);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * F::kStage + F::kTurn);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 4);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 2 * kBufs);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* give_up = abort_flag + 1;                 // one of the result warps waited in vain
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -57,19 +59,19 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
   auto empty_bar = [&](int s) { return bar_base + 8u * (kStages + s); };
   auto tfull_bar = [&](int b) { return bar_base + 8u * (2 * kStages + b); };
-  auto tempty_bar = [&](int b) { return bar_base + 8u * (2 * kStages + 2 + b); };
+  auto tempty_bar = [&](int b) { return bar_base + 8u * (2 * kStages + kBufs + b); };
 
   let_next_start();
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 4); }
+    for (int b = 0; b < kBufs; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 4); }
     *abort_flag = 0;
     *give_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_tmap(&maps.w); prefetch_tmap(&maps.x);
   }
   if (warp == 1) {
-    tmem_alloc(smem_u32(tmem_slot), 2 * NC);
+    tmem_alloc(smem_u32(tmem_slot), kBufs * NC);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -107,28 +109,24 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   } else if (warp == 1) {
     if (lane == 0) {
       const uint32_t idesc = make_idesc(NC, 0, 0);
-      uint32_t it = 0, count = 0;
+      uint32_t it = 0;
       bool ok = true;
       for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
-        for (int s0 = 0; s0 < steps && ok; s0 += kSpan, ++count) {
-          const uint32_t buf = count & 1u, use = count >> 1;
-          if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        for (int s = 0; s < steps; ++s, ++it) {
+          const int st = it % kStages, buf = it % kBufs;
+          if (!mbar_wait(tempty_bar(buf), ((it / kBufs) & 1u) ^ 1u, abort_flag) ||
+              !mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + buf * NC;
-          for (int s = s0; s < min(s0 + kSpan, steps); ++s, ++it) {
-            const int st = it % kStages;
-            if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t a_addr = smem_base + st * F::kStage, b_addr = a_addr + kABytes;
+          const uint32_t a_addr = smem_base + st * F::kStage, b_addr = a_addr + kABytes;
 #pragma unroll
-            for (int k = 0; k < 2 * kBK / kUmmaK; ++k) {
-              const uint32_t half = k / (kBK / kUmmaK), in = k % (kBK / kUmmaK);
-              umma_bf16(acc, make_desc(a_addr + half * (kABytes / 2) + in * (kUmmaK * 2), 16, 1024),
-                        make_desc(b_addr + half * (F::kBBytes / 2) + in * (kUmmaK * 2), 16, 1024), idesc, s > s0 || k > 0);
-            }
-            umma_commit(empty_bar(st));
+          for (int k = 0; k < 2 * kBK / kUmmaK; ++k) {
+            const uint32_t half = k / (kBK / kUmmaK), in = k % (kBK / kUmmaK);
+            umma_bf16(acc, make_desc(a_addr + half * (kABytes / 2) + in * (kUmmaK * 2), 16, 1024),
+                      make_desc(b_addr + half * (F::kBBytes / 2) + in * (kUmmaK * 2), 16, 1024), idesc, k > 0);
           }
-          if (ok) umma_commit(tfull_bar(buf));
+          umma_commit(empty_bar(st));
+          umma_commit(tfull_bar(buf));
         }
       }
       if (!ok) {
@@ -147,8 +145,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
       if (warp < 6) {
 #pragma unroll
         for (int j = 0; j < NC; ++j) x[j] = 0.f;
-        for (int s0 = 0; s0 < steps; s0 += kSpan, ++count) {
-          const uint32_t buf = count & 1u, use = count >> 1;
+        for (int s = 0; s < steps; ++s, ++count) {
+          const uint32_t buf = count % kBufs, use = count / kBufs;
           if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * NC;
@@ -244,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   tc_fence_after();
   if (warp == 1) {
     __syncwarp();
-    tmem_dealloc(tmem_base, 2 * NC);
+    tmem_dealloc(tmem_base, kBufs * NC);
   }
 }
 

@@ -9,8 +9,8 @@
 // while the next sums are under way.  The number of rows is read on the device: tokens without a label take no part.
 //
 // The tensor core cuts off what a sum has behind its 24 bits, at every step of 16 products: over 4096 of them that is a few
-// 2^-20 of a logit, always towards zero.  So a sum starts anew every span of k-blocks, and the parts are added up in
-// registers, rounded to nearest.
+// 2^-20 of a logit, always towards zero.  So a sum starts anew every few spans of k-blocks, and the parts are added up in
+// registers, rounded to nearest; and every span of the logits has a partner that goes the other way (see Spans).
 //
 // Measured on a B200, 8192 rows, 32000 columns, width 4096: logits 1.45 ms, gradient 1.41 ms in short runs (1.48 and
 // 1.52 PFLOP/s, tensor pipe 83 and 90 % active at 1.6 and 1.45 GHz under the power cap), 3.39 ms a call one after another
@@ -38,15 +38,34 @@ template <bool TO_X, int PARTS> struct Form {
   static constexpr int kStages = PARTS == 1 ? 6 : 2;
   static constexpr uint32_t kStage = PARTS * 2 * kHalf;
   static constexpr uint32_t kSmem = kStages * kStage + 1024 + 256;
-  // k-blocks of a span, 64 steps of the tensor core.  A span's end costs it about 360 cycles, since the sums are read from
-  // the memory that it works in: at width 4096 spans of 4 / 8 / 16 / 32 k-blocks took 926 / 866 / 835 / 825 us for 4096 tokens,
-  // with losses off by 1e-7 / 3e-7 / 6e-7 / 1.2e-6 (fp32's own products: 6e-7).  The gradient's product is rounded to bf16 in
-  // the end, where 512 steps are nothing, and with parts a k-block is 24 steps already.
+  // k-blocks of a span.  Its end costs the tensor core about 360 cycles, since the sums are read from the memory that it works
+  // in: with spans of 4 / 8 / 16 k-blocks throughout 4096 tokens of width 4096 take 963 / 867 / 829 us.  The gradient's product is
+  // rounded to bf16 in the end, where 512 steps are nothing, and with parts a k-block is 24 steps already.
   static constexpr int kSpan = PARTS == 3 ? 1 : (TO_X ? 128 : 16);
+  static constexpr bool kTurns = !TO_X && PARTS == 1;
   // a share of a split reduction keeps at least this many k-blocks, and costs this many on top (partial sums out and in): with
   // a cost of 8 or 12, which takes nine shares where 24 takes four, 333 tokens of width 2048 took 135 us instead of 129
   static constexpr int kShareMin = PARTS == 1 ? 16 : 3, kShareCost = PARTS == 1 ? 24 : 4;
 };
+// The span that starts at k-block k0 of [kb0, kb1).
+//
+// Where spans turn around, up to four make a group: the first two, one in either accumulator, add their products up from
+// zero, and the other two go on in the same accumulators with their products subtracted, back to about zero where a row's
+// products lean one way.  On the way up the cut takes from the first sum a, on the way down from a - b, which adds it to
+// b: a + b = 2 a - (a - b) has lost on one way what it won on the other.  On logits whose products lean by 0.3 of their spread, as a
+// sure token's with its label, width 4096: too small by 8.9 units of 2^-23 with spans of 16 k-blocks that do not turn, by 2.0 with
+// spans of 4 (which take 15 % longer), by 0.3 with spans of 16 that do, with a spread of 0.9 (fp32's own products: 0.5).  A
+// span without a partner has 4 k-blocks at most.
+constexpr int kLeastSpan = 4;
+struct Span { int k1; bool back; float factor; };     // factor: of what the accumulator holds at its end
+template <bool TO_X, int PARTS>
+__device__ __forceinline__ Span span_at(int k0, int kb0, int kb1) {
+  using F = Form<TO_X, PARTS>;
+  if constexpr (!F::kTurns) return Span{min(k0 + F::kSpan, kb1), false, 1.f};
+  const int from = kb0 + (k0 - kb0) / (4 * F::kSpan) * (4 * F::kSpan), blocks = min(4 * F::kSpan, kb1 - from);
+  const int each = max((blocks + 3) / 4, kLeastSpan), i = (k0 - from) / each;
+  return Span{min(k0 + each, from + blocks), i >= 2, i >= 2 ? -1.f : ((i + 2) * each < blocks ? 2.f : 1.f)};
+}
 // the six products of parts, small ones first
 __device__ constexpr int kPartOfA[6] = {2, 0, 1, 1, 0, 0}, kPartOfB[6] = {0, 2, 1, 0, 1, 0};
 constexpr int kCorners = 16, kCornerSums = 32 * kHeadCols, kTileSums = kCorners * kCornerSums, kAddThreads = 256;
@@ -420,12 +439,14 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
     // ---------------- products (leader) ----------------
     if (lane == 0 && leader) {
       const uint32_t idesc = make_idesc_m(256, 2 * cols, 0, TO_X ? 1 : 0);
+      constexpr uint32_t kNegateA = 1u << 13;
       uint32_t it = 0, count = 0;
       bool ok = true;
       for (int i = pair; i < plan.items && ok; i += pairs) {
         const Item t = item_at(plan, i, 2 * cols);
         for (int k0 = t.kb0, k1; k0 < t.kb1 && ok; k0 = k1, ++count) {
-          k1 = min(k0 + F::kSpan, t.kb1);
+          const Span span = span_at<TO_X, PARTS>(k0, t.kb0, t.kb1);
+          k1 = span.k1;
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
@@ -443,7 +464,8 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
                 const uint64_t ad = make_desc(a_part + k * (kUmmaK * 2), 16, 1024);
                 const uint64_t bd = TO_X ? make_desc(b_part + k * (kUmmaK * 128), kBK * 128, 1024)
                                          : make_desc(b_part + k * (kUmmaK * 2), 16, 1024);
-                umma_bf16_pair(acc, ad, bd, idesc, kb > k0 || k > 0 || c > (PARTS == 1 ? 5 : 0));
+                umma_bf16_pair(acc, ad, bd, span.back ? idesc | kNegateA : idesc,
+                               span.back || kb > k0 || k > 0 || c > (PARTS == 1 ? 5 : 0));
               }
             }
             umma_commit_pair(empty_bar(st), 3);
@@ -468,7 +490,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       float x[kHeadCols];
 #pragma unroll
       for (int j = 0; j < kHeadCols; ++j) x[j] = 0.f;
-      for (int k0 = t.kb0; k0 < t.kb1; k0 += F::kSpan, ++count) {
+      for (int k0 = t.kb0; k0 < t.kb1; ++count) {
+        const Span span = span_at<TO_X, PARTS>(k0, t.kb0, t.kb1);
+        k0 = span.k1;
         const uint32_t buf = count & 1u, use = count >> 1;
         if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
         tc_fence_after();
@@ -480,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
           tmem_ld32(acc + c, v);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 32; ++j) x[c + j] += __uint_as_float(v[j]);
+          for (int j = 0; j < 32; ++j) x[c + j] = fmaf(__uint_as_float(v[j]), span.factor, x[c + j]);
         }
         tc_fence_before();
         __syncwarp();

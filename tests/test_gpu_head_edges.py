@@ -148,3 +148,55 @@ def test_one_column_of_infinite_logits(B, bad, dtype):
     got = run(B, x, w, torch.zeros(3, dtype=torch.int32, device="cuda"))
     torch.cuda.synchronize()
     assert got["loss"].isnan().tolist() == [False, True, False] and got["d_x"].isnan().any(1).tolist() == [False, True, False]
+
+
+# units of 2^-23 of a logit that the spans of its sum may cost it: a step of 16 products cuts off less than one unit of what has
+# been added up, half of one on the average, and over a span of n steps that has grown to (n + 1) / 2 steps' worth on the average.
+# Few tokens have spans of 128 products; tiles longer ones that go up and down in turns, or else 256
+SPANS = {40: 8, 300: 16}               # steps of a span
+
+
+def cut_off(t):
+    return 0.5 * (SPANS[t] + 1) / 2 * 2.0 ** -23
+
+
+@pytest.mark.parametrize("t", [40, 300])
+def test_a_logit_loses_less_than_its_spans_cut_off(B, t):
+    # one column: the log-sum-exp is the logit.  Its products lean one way, as those of a sure token with its label do, so that
+    # what is cut off adds up; what rounds either way goes down with the number of logits (4096 products: below 2 units each).
+    # Sums between two powers of two lose up to twice as much as those just below one: the widths take both
+    g = torch.Generator(device="cuda").manual_seed(46)
+    for d in (1024, 1104, 1536, 2560, 4096, 4416):
+        off, n = 0.0, 0
+        for _ in range(10):
+            w = torch.randn(1, d, generator=g, device="cuda")
+            x = (torch.randn(t, d, generator=g, device="cuda") + 0.3 * w).bfloat16()
+            w = w.bfloat16()
+            got = run(B, x, w, torch.zeros(t, dtype=torch.int32, device="cuda"), grad=False)
+            z = (x.double() @ w.double().T)[:, 0]
+            off += float(((got["lse"].double() - z) / z.mean()).sum())
+            n += t
+        assert abs(off / n) <= cut_off(t) + 2 * 2.0 ** -23 * n ** -0.5, (d, off / n * 2 ** 23)
+
+
+@pytest.mark.parametrize("t", [40, 300])
+def test_a_sure_token_at_a_models_width_keeps_its_loss(B, t):
+    # loss = e^(lse of the others - z): relatively it is off by what the logits are off by.  The label's logit is about 30, that
+    # of the columns that matter beside it about 4 (their spread is 2), with either sign of what is cut off; exponentials and
+    # sums add 2^-21
+    v, d = 32000, 4096
+    g, x, w = rand(47, t, v, d, torch.bfloat16, 2.0)
+    labels = torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+    wl = w[labels.long()].float()
+    x = (x.float() + 30.0 * wl / (wl * wl).sum(1, keepdim=True)).bfloat16()
+    got = run(B, x, w, labels, grad=False)
+    z = torch.empty(t, device="cuda", dtype=torch.float64)
+    ref = torch.empty_like(z)
+    for a in range(0, t, 50):
+        all_z = x[a:a + 50].double() @ w.double().T
+        z[a:a + 50] = torch.gather(all_z, 1, labels[a:a + 50].long()[:, None])[:, 0]
+        others = torch.logsumexp(all_z.scatter(1, labels[a:a + 50].long()[:, None], -INF), 1)
+        ref[a:a + 50] = torch.log1p(torch.exp(others - z[a:a + 50]))
+    off = (got["loss"].double() - ref) / ref
+    assert float(ref.max()) < 1e-2
+    assert abs(float(off.mean())) <= cut_off(t) * (float(z.mean()) + 4.0) + 2.0 ** -21, float(off.mean())
