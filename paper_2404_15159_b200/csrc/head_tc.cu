@@ -100,15 +100,15 @@ __device__ __forceinline__ Plan make_plan(int rows, int n_tiles, int k_blocks, i
   t.whole = tiles;
   t.shares = 1;
   if (TO_X && rest) {
-    // in fp32 without divisions, which would take a microsecond; whichever of two nearly equal costs is taken, every role of
-    // every CTA takes the same
-    const float per_pair = 1.f / pairs;
-    float best = k_blocks;
+    // in whole numbers, costs times shares compared crosswise: the kernel that adds the shares up has to come to the same plan
+    int best = k_blocks, rounds = 1, items = rest;
 #pragma unroll
     for (int s = 2; s <= kHeadMaxShares; ++s) {
-      if (s * Form<TO_X, PARTS>::kShareMin > k_blocks || s * rest > most_items) continue;
-      const float cost = ceilf(rest * s * per_pair - 0x1p-10f) * (k_blocks * (1.f / s) + Form<TO_X, PARTS>::kShareCost);
-      if (cost < best) { best = cost; t.shares = s; }
+      items += rest;
+      rounds += items > rounds * pairs;                    // of `pairs` items, rounded up: rest < pairs
+      if (s * Form<TO_X, PARTS>::kShareMin > k_blocks || items > most_items) continue;
+      const int cost = rounds * (k_blocks + s * Form<TO_X, PARTS>::kShareCost);
+      if (cost * t.shares < best * s) { best = cost; t.shares = s; }
     }
     if (t.shares > 1) t.whole = tiles - rest;
   }
