@@ -35,7 +35,7 @@ struct HeadState {
   int32_t counted;      // rows with a label (an entry), the only ones that are computed
   int32_t joined;       // blocks of the joining kernel that are done
   float weight;         // sum of the counted rows' weights
-  float each;           // 1 / normalizer
+  double each;          // 1 / normalizer
 };
 
 struct HeadArgs {

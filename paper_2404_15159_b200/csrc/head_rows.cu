@@ -119,10 +119,10 @@ __global__ void __launch_bounds__(kListThreads) head_lists_kernel(HeadArgs p) {
   }
 }
 
-// What a weight is multiplied by: one over the normalizer
-__device__ __forceinline__ float part_of_each(const HeadArgs& p, double weights) {
+// What a weight is multiplied by: one over the normalizer, in 64 bits, where that of the smallest fp32 weights has a value
+__device__ __forceinline__ double part_of_each(const HeadArgs& p, double weights) {
   const double norm = p.normalizer ? (double)p.normalizer[0] : weights;
-  return norm == 0.0 ? 0.f : 1.f / (float)norm;
+  return norm == 0.0 ? 0.0 : 1.0 / norm;
 }
 
 // Numbers the counted rows and adds up their weights: one block, 8192 tokens a turn, eight to a thread and a warp's 32 side
@@ -296,8 +296,7 @@ struct RowJob {
   int tiles, n;                 // n: listed columns
   const int32_t* list;
   const double* q;              // the teacher's probabilities, or NULL: a label
-  double rest, weight;
-  float each;
+  double rest, weight, each;
   float* z;                     // the listed logits; gets the places' values G_k / A
   float *loss, *lse, *scale;    // lse, scale: or NULL
   bf16* e;
@@ -381,7 +380,7 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, const RowJob&
   }
   const double over = recip64(a);
   for (int k = lane; k < n; k += 32) z[k] = (float)((double)z[k] * over);
-  if (lane == 0) *job.scale = (float)(a * p.z_per_xw * job.weight * (double)job.each);
+  if (lane == 0) *job.scale = (float)(a * p.z_per_xw * job.weight * job.each);
   return out;
 }
 

@@ -200,3 +200,18 @@ def test_a_sure_token_at_a_models_width_keeps_its_loss(B, t):
     off = (got["loss"].double() - ref) / ref
     assert float(ref.max()) < 1e-2
     assert abs(float(off.mean())) <= cut_off(t) * (float(z.mean()) + 4.0) + 2.0 ** -21, float(off.mean())
+
+
+@TYPES
+@TOKENS
+@pytest.mark.parametrize("given", [False, True], ids=["own", "given"])
+@pytest.mark.parametrize("size", [2.0 ** -140, 2.0 ** 120])
+def test_weights_of_any_size_divide_out(B, size, given, t, dtype):
+    # one over a sum of 2^-137 is no fp32 number, and one over 2^127 has few bits; weight / normalizer is a number like any other
+    g, x, w = rand(48, t, 300, 64, dtype)
+    labels = torch.randint(0, 300, (t,), generator=g, device="cuda", dtype=torch.int32)
+    weights = size * torch.randint(1, 4, (t,), generator=g, device="cuda").float() / (t if size > 1 else 1)
+    norm = torch.tensor([size * 5], device="cuda") if given else None
+    got = run(B, x, w, labels, weights=weights, normalizer=norm)
+    ref = want(x, w, labels, weights=weights, normalizer=size * 5 if given else None)
+    check(B, got, {n: ref[n] for n in ("loss", "lse", "d_x", "bound")})
