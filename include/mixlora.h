@@ -421,9 +421,9 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
  * An inf or NaN in a token's x makes its own loss, lse and gradient NaN (and totals[0]), no other token's; one in w reaches
  * every token.  So does a product x . w beyond fp32's range, also where a cap would bend it to a number.  Tokens that are left
  * out may hold anything.
- * The workspace (256-byte aligned, mixlora_head_workspace_bytes) is scratch of one call: whatever the batch, about 1.2 GB (in
- * fp32 mode 2.7 GB and 6 bytes for each value of w) at most beside a few numbers a token and the teacher's entries; calls
- * that may run at the same time need one each; mixlora_device_status works on it. */
+ * The workspace (256-byte aligned, mixlora_head_workspace_bytes) is scratch of one call: whatever the batch, at most 1.7 GB (in
+ * fp32 mode 1.8 GB and 6 bytes for each value of w) beside 9 bytes a token and 12 for each of the teacher's entries (and 12
+ * for their token); calls that may run at the same time need one each; mixlora_device_status works on it. */
 #define MIXLORA_MAX_TEACHER_TOP 256
 typedef struct {
   uint32_t struct_size;       /* = sizeof(mixlora_head_shape_t) */

@@ -44,9 +44,9 @@ mixlora_status_t check_head(const mixlora_head_shape_t* s) {
 
 bool few_tokens(const mixlora_head_shape_t& s) { return s.dtype == MIXLORA_DTYPE_BF16 && s.tokens <= kHeadFewTokens; }
 
-// Counted rows are worked on in pieces, as many as keep a piece's exponentials within 512 MiB: enough for whole rounds of
-// tiles, and the same whatever the batch.  Without a gradient there are two numbers for 128 columns, and the copy of the
-// rows of x is what counts.
+// Counted rows are worked on in pieces, as many as keep each of a piece's exponentials, rows of x and listed logits within 512
+// MiB: enough for whole rounds of tiles, and the same whatever the batch.  Without a gradient there are two numbers for 128
+// columns, and the copy of the rows of x is what counts.
 int piece_rows(const mixlora_head_shape_t& s, bool gradient, int parts) {
   long long row = 2LL * parts * s.d_model;
   const long long wide = gradient ? 2LL * parts * s.vocab : (s.vocab + kHeadLeastCols - 1) / kHeadLeastCols * 8LL;

@@ -84,6 +84,18 @@ def test_workspace_is_bounded_by_the_piece(B):
     assert size(B.make_head_shape(8192, 4096, 32000), 0) < size(B.make_head_shape(8192, 4096, 32000), 1)
 
 
+@pytest.mark.parametrize("d", [8, 512, 520, 4096, 65536])
+@pytest.mark.parametrize("vocab", [1, 512, 520, 2048, 32000, 1 << 20])
+@pytest.mark.parametrize("top", [0, 64, 256])
+def test_workspace_is_what_the_header_says(B, d, vocab, top):
+    # rows of x, exponentials and listed logits may each come to 512 MiB, where a row of each has about the same size
+    t = 1 << 22
+    for dtype, most in ((B.MIXLORA_DTYPE_BF16, 1.7e9), (B.MIXLORA_DTYPE_FP32, 1.8e9 + 6 * vocab * d)):
+        for grad in (0, 1):
+            got = B.lib.mixlora_head_workspace_bytes(C.byref(B.make_head_shape(t, d, vocab, dtype, teacher_top=top)), grad)
+            assert 0 < got <= most + 9 * t + (12 * top + 12 if top else 0) * t
+
+
 def test_the_binding_raises(B):
     import torch
     with pytest.raises(B.MixLoraError) as e:
