@@ -215,3 +215,103 @@ def test_weights_of_any_size_divide_out(B, size, given, t, dtype):
     got = run(B, x, w, labels, weights=weights, normalizer=norm)
     ref = want(x, w, labels, weights=weights, normalizer=size * 5 if given else None)
     check(B, got, {n: ref[n] for n in ("loss", "lse", "d_x", "bound")})
+
+
+MORE = pytest.mark.parametrize("t", [130, 300])            # the form for more than 64 tokens
+
+
+@TYPES
+@MORE
+def test_far_logits_in_every_place_of_a_tile(B, t, dtype):
+    v, d = 1500, 64
+    g, x, w = rand(49, t, v, d, dtype)
+    lift = torch.zeros(v, device="cuda")
+    lift[100], lift[300], lift[700:760], lift[1400] = 30.0, 80.0, -90.0, 55.0
+    x[:, 0] = torch.linspace(-3, 3, t, device="cuda").to(dtype)
+    w[:, 0] = lift.to(dtype)
+    labels = torch.tensor([100, 300, 701, 1400, 5], dtype=torch.int32, device="cuda").repeat(t)[:t].contiguous()
+    check(B, run(B, x, w, labels), want(x, w, labels))
+    index = torch.tensor([300, 5, 701, 1400], dtype=torch.int32, device="cuda").repeat(t, 1)
+    logit = 2 * torch.randn(t, 4, generator=g, device="cuda")
+    check(B, run(B, x, w, index, logit), want(x, w, index, logit))
+
+
+@TYPES
+@MORE
+def test_a_sure_token_in_a_tile_keeps_its_small_loss_and_gradient(B, t, dtype):
+    # relatively, row by row: logits of a few tens, sums of 64 products, are off by less than 2^-12 here, and what rounds the
+    # gradient's factors and itself comes to less than four half steps of bf16
+    v, d = 800, 64
+    g, x, w = rand(50, t, v, d, dtype)
+    labels = torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+    lean = torch.linspace(0, 40, t, device="cuda")[:, None]
+    wl = w[labels.long()].float()
+    x = (x.float() + lean * wl / (wl * wl).sum(1, keepdim=True)).to(dtype)
+    got, ref = run(B, x, w, labels), want(x, w, labels)
+    check(B, got, ref)
+    assert float(ref["loss"].min()) < 1e-10
+    rel = ((got["loss"].double() - ref["loss"]).abs() / ref["loss"]).max()
+    assert float(rel) < 2.0 ** -10
+    size = ref["d_x"].abs().max(1).values
+    assert float(((got["d_x"].double() - ref["d_x"]).abs().max(1).values / size).max()) < (2.0 ** -6 if dtype == torch.bfloat16 else 2.0 ** -10)
+
+
+@TYPES
+@MORE
+def test_teacher_logits_at_the_edges_of_a_tile(B, t, dtype):
+    g, x, w = rand(51, t, 300, 64, dtype)
+    index, logit = lists(g, t, 300, 4, ragged=False)
+    last = t - 7                          # the same edges among the first rows and the last
+    for a in (0, last):
+        logit[a + 1, 1:] = -INF
+        logit[a + 2] = -INF               # says nothing: left out
+        logit[a + 3] *= 1000
+    check(B, run(B, x, w, index, logit), want(x, w, index, logit))
+    t_lse = torch.logsumexp(logit, 1) + 0.1
+    for a in (0, last):
+        t_lse[a + 2] = 0.0                # the teacher chose none of these: everything is left over
+        t_lse[a + 4] = t_lse[a + 4] - 1.0  # listed entries above one: nothing is left over
+    check(B, run(B, x, w, index, logit, t_lse), want(x, w, index, logit, t_lse))
+    logit[last + 5, 2] = NAN
+    got = run(B, x, w, index, logit)
+    torch.cuda.synchronize()
+    assert got["loss"][last + 5].isnan() and got["loss"].isnan().sum() == 1 and got["d_x"].isnan().any(1).sum() == 1
+
+
+@TYPES
+@pytest.mark.parametrize("left_out", [False, True], ids=["all", "some"])
+@pytest.mark.parametrize("top", [0, 3])
+@pytest.mark.parametrize("shape,grad", [("wide", True), ("deep", True), ("deep", False)])
+def test_pieces_of_every_kind(B, shape, grad, top, left_out, dtype):
+    # a piece is 256 rows at the widest vocabulary, 4096 (in parts: 1280) at the greatest width; where no token is left out the rows
+    # are read in place, the last piece's tiles reaching beyond the last token
+    bf16 = dtype == torch.bfloat16
+    t, v, d = (601, 1 << 20, 16) if shape == "wide" else (4397 if bf16 else 1399, 300, 65536)
+    g, x, w = rand(52, t, v, d, dtype, 2.0)
+    weights = torch.rand(t, generator=g, device="cuda") + 0.1
+    out = torch.zeros(t, dtype=torch.bool, device="cuda")
+    if left_out:
+        out[1::3] = True
+    if top:
+        index = torch.randint(0, v, (t, top), generator=g, device="cuda", dtype=torch.int32)
+        index[:, 1:][torch.rand(t, top - 1, generator=g, device="cuda") < 0.3] = -1
+        index[out] = -1
+        args = [index, 3 * torch.randn(t, top, generator=g, device="cuda")]
+        args.append(torch.logsumexp(args[1], 1) + 0.4)
+    else:
+        labels = torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+        args = [torch.where(out, torch.full_like(labels, -1), labels)]
+    got = run(B, x, w, *args, weights=weights, grad=grad)
+    torch.cuda.synchronize()
+    assert B.mixlora_device_status(got["ws"]) == 0
+    norm = float(weights[~out].double().sum())
+    total = 0.0
+    step = 50 if shape == "wide" else 400
+    for a in range(0, t, step):
+        rows = slice(a, a + step)
+        ref = want(x[rows], w, *(v[rows] for v in args), weights=weights[rows], normalizer=norm, gradient=grad)
+        total += float(ref["totals"][0])
+        for n in ("loss", "lse", "d_x")[: 3 if grad else 2]:
+            off = (got[n][rows].double() - ref[n]).abs()
+            assert bool((off <= ref["bound"][n]).all()), (n, a)
+    assert abs(float(got["totals"][0]) - total) <= 1e-5 * abs(total) and abs(float(got["totals"][1]) - norm) <= 2.0 ** -23 * norm
