@@ -2,7 +2,8 @@
 //
 // Logits z_v = (capped) scale x . w_v / temperature of a row are formed up to 128 columns at a time and turned into
 // exponentials at once.  A row's `listed` columns (its label, or the teacher's entries) are left out of them and kept as
-// fp32 logits: a sum or a difference that a confident row makes small is then never taken of nearly equal numbers.
+// fp32 logits: a sum or a difference that a confident row makes small is then never taken of nearly equal numbers, and is as good
+// as the logits themselves.
 //   those columns         R = 100 rint(log2(e) max z / 100) over its columns that are not listed, S = sum 2^(z log2(e) - R)
 //   gradient              E_v = 2^(z_v log2(e) - R) (1 - (z_v temperature / softcap)^2), one rounding to bf16
 // R is a multiple of 100, so tiles of a row nearly always share it, and where they do not (logits 35 apart or more) the
@@ -87,6 +88,12 @@ __device__ __forceinline__ int head_rows_here(const HeadArgs& p) {
 __device__ __forceinline__ int head_token(const HeadArgs& p, int row) { return p.few ? row : p.row_token[p.piece0 + row]; }
 // Whether a token has no gradient, whatever its sums are
 __device__ __forceinline__ bool head_left_out(const HeadArgs& p, int token) { return p.few && p.token_row[token] < 0; }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // A value as the sum of three bf16 ones: the first is cut off (rounding could overflow), the others are rounded, which
 // leaves nothing of 24 bits.

@@ -36,12 +36,6 @@ template <int NC> struct Few {
 };
 struct alignas(64) FewMaps { CUtensorMap w, x; };
 
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 template <int NC, bool GRAD, bool CAP>
 __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_constant__ HeadArgs p,
                                                                const __grid_constant__ FewMaps maps) {
