@@ -347,10 +347,16 @@ __device__ __forceinline__ RowResult finish_row(const HeadArgs& p, const RowJob&
   }
   RowResult out{r, job.weight * (double)(float)loss};
   if (!job.scale) return out;
-  const double r_listed = 100.0 * rint(most * (kLog2ed / 100.0));
-  if (s == 0.0 || r_listed > r) out.r = r_listed;
-  const double u = exp64(out.r * kLn2d - lse), s_row = s == 0.0 ? 0.0 : exp64(lr - out.r * kLn2d);
-  const double part = rest > 0.0 && s_row > 0x1p-100 ? rest * recip64(s_row) : 0.0;
+  // The others' R, unless G_k / A could leave bf16's range there: then the next one that brings u above 2^-50.  What is left
+  // over keeps the others' where it counts, since the whole of it goes into their E, however small they are
+  if (s == 0.0) out.r = 100.0 * rint(most * (kLog2ed / 100.0));
+  double u = exp64(out.r * kLn2d - lse), part = rest > 0.0 && s > 0.0 ? rest * recip64(s) : 0.0;
+  if (s != 0.0 && fmax(u, part) < 0x1p-50) {
+    out.r = r + 100.0 * ceil((lse * kLog2ed - r - 50.0) * 0.01);
+    u = exp64(out.r * kLn2d - lse);
+    const double s_row = exp64(lr - out.r * kLn2d);
+    part = rest > 0.0 && s_row > 0x1p-100 ? rest * recip64(s_row) : 0.0;
+  }
   const double curl = 2.0 * zeta * lse, share = mass + curl;
   double a = share * u - part;
   // nothing below what the 32-bit sums behind u and s can tell from zero, so that G_k / A stays in range

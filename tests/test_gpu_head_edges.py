@@ -1,5 +1,7 @@
 """Where the head's losses can go wrong at the edges: numbers that are none, tokens that are sure at a model's own width, both
 on every side of the form for few tokens and of a tile."""
+import math
+
 import pytest
 import torch
 
@@ -315,3 +317,21 @@ def test_pieces_of_every_kind(B, shape, grad, top, left_out, dtype):
             off = (got[n][rows].double() - ref[n]).abs()
             assert bool((off <= ref["bound"][n]).all()), (n, a)
     assert abs(float(got["totals"][0]) - total) <= 1e-5 * abs(total) and abs(float(got["totals"][1]) - norm) <= 2.0 ** -23 * norm
+
+
+@TYPES
+@TOKENS
+@pytest.mark.parametrize("v", [5, 300])
+@pytest.mark.parametrize("left", [0.01, 0.9])
+def test_what_a_teacher_leaves_over_stays_beside_listed_columns_of_any_weight(B, left, v, t, dtype):
+    # one listed column holds up to 2^69 times the weight of all that are not listed, and still their share of the gradient is
+    # what the teacher leaves over, spread as they are
+    d = 64
+    g, x, w = rand(53, t, v, d, dtype)
+    w[:, 0] = 0.0
+    w[4, 0] = 1.0
+    x[:, 0] = torch.linspace(-10.0, 46.0, t, device="cuda").to(dtype)
+    index = torch.tensor([[4, 0, 2]], dtype=torch.int32, device="cuda").repeat(t, 1)
+    logit = torch.randn(t, 3, generator=g, device="cuda")
+    t_lse = torch.logsumexp(logit, 1) - math.log1p(-left)
+    check(B, run(B, x, w, index, logit, t_lse), want(x, w, index, logit, t_lse))
