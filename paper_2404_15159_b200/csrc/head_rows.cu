@@ -481,6 +481,7 @@ __global__ void __launch_bounds__(kRowThreads + 32) head_join_kernel(HeadArgs p)
         if (!p.labels) {
           job.q = p.list_q + (size_t)token * p.top;
           job.rest = p.rest_q[token];
+          if (job.n == 1 && job.rest == 0.0 && job.q[0] == 1.0) job.q = nullptr;      // one column takes all: a label
         }
         job.z = p.z_listed + (size_t)row * p.top;
         job.loss = p.loss + token;

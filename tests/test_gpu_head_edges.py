@@ -335,3 +335,21 @@ def test_what_a_teacher_leaves_over_stays_beside_listed_columns_of_any_weight(B,
     logit = torch.randn(t, 3, generator=g, device="cuda")
     t_lse = torch.logsumexp(logit, 1) - math.log1p(-left)
     check(B, run(B, x, w, index, logit, t_lse), want(x, w, index, logit, t_lse))
+
+
+@TYPES
+@TOKENS
+def test_a_list_of_one_entry_is_a_label(B, t, dtype):
+    # to the last bit, also where the token is so sure that its loss, e^-40 and less, is no difference of logarithms any more
+    v, d = 800, 64
+    g, x, w = rand(54, t, v, d, dtype)
+    labels = torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+    wl = w[labels.long()].float()
+    x = (x.float() + torch.linspace(0, 44, t, device="cuda")[:, None] * wl / (wl * wl).sum(1, keepdim=True)).to(dtype)
+    a = run(B, x, w, labels, z_loss=1e-3)
+    index = torch.full((t, 3), -1, dtype=torch.int32, device="cuda")
+    index[torch.arange(t), torch.arange(t) % 3] = labels
+    b = run(B, x, w, index, torch.randn(t, 3, generator=g, device="cuda"), z_loss=1e-3)
+    assert all(torch.equal(a[n], b[n]) for n in ("loss", "lse", "totals", "d_x"))
+    b = run(B, x, w, index, torch.randn(t, 3, generator=g, device="cuda"))
+    check(B, b, want(x, w, index, torch.zeros(t, 3, device="cuda")))
