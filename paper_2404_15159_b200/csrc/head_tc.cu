@@ -57,15 +57,26 @@ template <bool TO_X, int PARTS> struct Form {
 // spans of 4 (which take 15 % longer), by 0.3 with spans of 16 that do, with a spread of 0.9 (fp32's own products: 0.5).  A
 // span without a partner has 4 k-blocks at most.
 constexpr int kLeastSpan = 4;
-struct Span { int k1; bool back; float factor; };     // factor: of what the accumulator holds at its end
-template <bool TO_X, int PARTS>
-__device__ __forceinline__ Span span_at(int k0, int kb0, int kb1) {
+template <bool TO_X, int PARTS> struct Spans {
   using F = Form<TO_X, PARTS>;
-  if constexpr (!F::kTurns) return Span{min(k0 + F::kSpan, kb1), false, 1.f};
-  const int from = kb0 + (k0 - kb0) / (4 * F::kSpan) * (4 * F::kSpan), blocks = min(4 * F::kSpan, kb1 - from);
-  const int each = max((blocks + 3) / 4, kLeastSpan), i = (k0 - from) / each;
-  return Span{min(k0 + each, from + blocks), i >= 2, i >= 2 ? -1.f : ((i + 2) * each < blocks ? 2.f : 1.f)};
-}
+  int k1 = 0, end = 0, each = 0, turn = 0;
+  bool back = false;                  // the products are subtracted
+  float factor = 1.f;                 // of what the accumulator holds at the span's end
+  __device__ __forceinline__ void start(int k0, int kb1) {
+    if constexpr (!F::kTurns) {
+      k1 = min(k0 + F::kSpan, kb1);
+    } else {
+      if (k0 >= end) {
+        end = min(k0 + 4 * F::kSpan, kb1);
+        each = max((end - k0 + 3) / 4, kLeastSpan);
+        turn = k0 + 2 * each;
+      }
+      back = k0 >= turn;
+      factor = back ? -1.f : (k0 + 2 * each < end ? 2.f : 1.f);
+      k1 = min(k0 + each, end);
+    }
+  }
+};
 // the six products of parts, small ones first
 __device__ constexpr int kPartOfA[6] = {2, 0, 1, 1, 0, 0}, kPartOfB[6] = {0, 2, 1, 0, 1, 0};
 constexpr int kCorners = 16, kCornerSums = 32 * kHeadCols, kTileSums = kCorners * kCornerSums, kAddThreads = 256;
@@ -439,14 +450,14 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       bool ok = true;
       for (int i = pair; i < plan.items && ok; i += pairs) {
         const Item t = item_at(plan, i, 2 * cols);
-        for (int k0 = t.kb0, k1; k0 < t.kb1 && ok; k0 = k1, ++count) {
-          const Span span = span_at<TO_X, PARTS>(k0, t.kb0, t.kb1);
-          k1 = span.k1;
+        Spans<TO_X, PARTS> span;
+        for (int k0 = t.kb0; k0 < t.kb1 && ok; k0 = span.k1, ++count) {
+          span.start(k0, t.kb1);
           const uint32_t buf = count & 1u, use = count >> 1;
           if (!mbar_wait(tempty_bar(buf), (use & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + buf * kTile;
-          for (int kb = k0; kb < k1; ++kb, ++it) {
+          for (int kb = k0; kb < span.k1; ++kb, ++it) {
             const int st = it % kStages;
             if (!mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
             tc_fence_after();
@@ -485,9 +496,9 @@ __global__ void __launch_bounds__(kThreads, 1) head_tc_kernel(const __grid_const
       float x[kHeadCols];
 #pragma unroll
       for (int j = 0; j < kHeadCols; ++j) x[j] = 0.f;
-      for (int k0 = t.kb0; k0 < t.kb1; ++count) {
-        const Span span = span_at<TO_X, PARTS>(k0, t.kb0, t.kb1);
-        k0 = span.k1;
+      Spans<TO_X, PARTS> span;
+      for (int k0 = t.kb0; k0 < t.kb1; k0 = span.k1, ++count) {
+        span.start(k0, t.kb1);
         const uint32_t buf = count & 1u, use = count >> 1;
         if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
         tc_fence_after();
