@@ -411,11 +411,11 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
  * overlap an input.  d_model and the strides are multiples of 8.  Tokens that are left out cost nothing in the products.
  * Logits are sums in fp32, and so are the gradients of the fp32 mode, where operands are taken apart into three bf16 values
  * that hold their 24 bits (values below 2^-100 lose some).  The tensor core cuts off what its sums have behind 24 bits; it is
- * given so few of a logit's products at once, or every other part with the opposite sign, that a logit of a token that leans
- * towards a column is too small by about one 2^-23 of it up to 64 tokens, by half of that beyond and with fp32 (with products
- * of the one sign only, by up to ten of them beyond 64 tokens).  With bf16 the factors of the gradient's product are rounded to
- * it, relatively and after all differences have been taken, so that a confident token's small gradient keeps its precision:
- * within one half step for a listed column, within two for another.  Where a row's listed columns hold more than 2^70 times
+ * given so few of a logit's products at once, and every other part with the opposite sign, that a logit of a token that leans
+ * towards a column is too small by two 2^-23 of it at most, from width 2048 on by half of one (with products of the one sign
+ * only, by up to ten beyond 64 tokens).  With bf16 the factors of the gradient's product are rounded to it, relatively and
+ * after all differences have been taken, so that a confident token's small gradient keeps its precision: within one half
+ * step for a listed column, within two for another.  Where a row's listed columns hold more than 2^70 times
  * the weight of all others, the others' part of the gradient may become zero; logits beyond 2^20 promise no result.
  * Results do not depend on the order in which blocks run.
  * An inf or NaN in a token's x makes its own loss, lse and gradient NaN (and totals[0]), no other token's; one in w reaches

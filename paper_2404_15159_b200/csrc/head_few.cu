@@ -3,10 +3,9 @@
 // The roles of the operands are turned around: 128 columns of the vocabulary are the rows of a tensor-core tile, the tokens
 // its columns (16, 32 or 64), so that no part of a tile is empty and the head streams through shared memory at the rate of
 // the memory.  One persistent CTA an SM; warp 0 loads (128 reduction elements a stage, so that 256 bytes of each row are
-// asked for at once), warp 1 issues the products, warps 2 to 5 add up the stages' sums in registers, rounded to nearest (what the
-// tensor core cuts off in 8 steps is 1 unit of 2^-23 of a logit where a sum of 4096 products at once would lose 35; it
-// runs up to 8 stages ahead of them), and pass the tile through shared memory, and warps 2 to 9 then work on a token each, four
-// neighbouring columns a lane.
+// asked for at once), warp 1 issues the products, warps 2 to 5 add up the stages' sums in registers, rounded to nearest (the
+// tensor core, which cuts off what is behind 24 bits, runs up to 8 stages ahead of them), and pass the tile through shared
+// memory, and warps 2 to 9 then work on a token each, four neighbouring columns a lane.
 // Rows are tokens here: those that are left out pass through the products too, and the joining kernel drops them.
 //
 // The gradient's product goes the same way: 256 columns of d_x are the rows of two tiles, the tokens their columns, and the
@@ -26,7 +25,13 @@ namespace {
 
 using namespace tc;
 constexpr int kWarps = 8, kThreads = 64 + 32 * kWarps, kBK = 64, kUmmaK = 16;
+// A stage is a span of 128 products, and of the stages that take turns in an accumulator every second one goes on in it with its
+// products subtracted (see the kernel for many tokens).  In registers four stages are added up to one another before the tile's
+// sum, whose own roundings are kept for up to 16 tokens (with 32 that took 55.6 -> 57.2 us).  On logits whose products lean by
+// 0.3 of their spread, width 4096: too small by 0.15 units of 2^-23 with a spread of 0.3 (up to 16 tokens) and 0.5, where spans
+// of 512 that do not turn gave 4.4, and fp32's own products 0 and 1.1.
 constexpr int kBufs = 8;                                  // accumulators, one a stage
+__device__ __forceinline__ bool goes_back(int stage) { return (stage / kBufs) & 1; }
 constexpr uint32_t kABytes = 2 * 128 * kBK * 2;
 template <int NC> struct Few {
   static constexpr uint32_t kBBytes = 2 * NC * kBK * 2, kStage = kABytes + kBBytes;
@@ -45,19 +50,18 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float* turn = reinterpret_cast<float*>(smem + kStages * F::kStage);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * F::kStage + F::kTurn);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kStages + 2 * kBufs);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kStages + 2 * kBufs);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* give_up = abort_flag + 1;                 // one of the result warps waited in vain
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = smem_u32(smem), bar_base = smem_u32(bars);
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
-  auto empty_bar = [&](int s) { return bar_base + 8u * (kStages + s); };
-  auto tfull_bar = [&](int b) { return bar_base + 8u * (2 * kStages + b); };
-  auto tempty_bar = [&](int b) { return bar_base + 8u * (2 * kStages + kBufs + b); };
+  auto tfull_bar = [&](int b) { return bar_base + 8u * (kStages + b); };
+  auto tempty_bar = [&](int b) { return bar_base + 8u * (kStages + kBufs + b); };
 
   let_next_start();
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int s = 0; s < kStages; ++s) mbar_init(full_bar(s), 1);
     for (int b = 0; b < kBufs; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 4); }
     *abort_flag = 0;
     *give_up = 0;
@@ -85,7 +89,11 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
       for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
         for (int s = 0; s < steps; ++s, ++it) {
           const int st = it % kStages;
-          if (!mbar_wait(empty_bar(st), ((it / kStages) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          // a stage is free when the products that read it have arrived, `kStages` before these
+          if (it >= kStages && !mbar_wait(tfull_bar((it - kStages) % kBufs), ((it - kStages) / kBufs) & 1u, abort_flag)) {
+            ok = false;
+            break;
+          }
           const uint32_t a_dst = smem_base + st * F::kStage, b_dst = a_dst + kABytes;
           mbar_expect_tx(full_bar(st), F::kStage);
           const int k = s * 2 * kBK;
@@ -103,6 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
   } else if (warp == 1) {
     if (lane == 0) {
       const uint32_t idesc = make_idesc(NC, 0, 0);
+      constexpr uint32_t kNegateA = 1u << 13;
       uint32_t it = 0;
       bool ok = true;
       for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
@@ -112,14 +121,15 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
               !mbar_wait(full_bar(st), (it / kStages) & 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + buf * NC;
+          const bool back = goes_back(s);
           const uint32_t a_addr = smem_base + st * F::kStage, b_addr = a_addr + kABytes;
 #pragma unroll
           for (int k = 0; k < 2 * kBK / kUmmaK; ++k) {
             const uint32_t half = k / (kBK / kUmmaK), in = k % (kBK / kUmmaK);
             umma_bf16(acc, make_desc(a_addr + half * (kABytes / 2) + in * (kUmmaK * 2), 16, 1024),
-                      make_desc(b_addr + half * (F::kBBytes / 2) + in * (kUmmaK * 2), 16, 1024), idesc, k > 0);
+                      make_desc(b_addr + half * (F::kBBytes / 2) + in * (kUmmaK * 2), 16, 1024),
+                      back ? idesc | kNegateA : idesc, back || k > 0);
           }
-          umma_commit(empty_bar(st));
           umma_commit(tfull_bar(buf));
         }
       }
@@ -130,27 +140,39 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
     }
   } else {
     wait_for_last();                                      // for the lists: the products need the call's inputs alone
+    constexpr int kLow = NC == 16 ? NC : 1;
     const int q = warp & 3;
     const float factor = p.logit_factor, cap_out = p.cap_out, to2 = p.to2;
     uint32_t count = 0;
     bool ok = true;
     for (int tile = blockIdx.x; tile < p.col_tiles && ok; tile += gridDim.x) {
-      float x[NC];
+      float x[NC], some[NC];                              // the tile's sums, and those of the last four stages
+      float low[kLow];                                    // what the roundings of the tile's sums have left, up to 16 tokens
       if (warp < 6) {
 #pragma unroll
-        for (int j = 0; j < NC; ++j) x[j] = 0.f;
+        for (int j = 0; j < NC; ++j) x[j] = some[j] = low[j % kLow] = 0.f;
         for (int s = 0; s < steps; ++s, ++count) {
           const uint32_t buf = count % kBufs, use = count / kBufs;
           if (!__all_sync(0xffffffffu, mbar_wait(tfull_bar(buf), use & 1u, abort_flag))) { ok = false; break; }
           tc_fence_after();
           const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + buf * NC;
+          const float times = goes_back(s) ? -1.f : (s + kBufs < steps ? 2.f : 1.f);
 #pragma unroll
           for (int c = 0; c < NC; c += 16) {
             uint32_t v[16];
             tmem_ld16(acc + c, v);
             tmem_ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x[c + j] += __uint_as_float(v[j]);
+            for (int j = 0; j < 16; ++j) some[c + j] = fmaf(__uint_as_float(v[j]), times, some[c + j]);
+          }
+          if (s % 4 == 3 || s == steps - 1) {
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+              const float sum = x[j] + some[j], of_some = sum - x[j];
+              if (kLow == NC) low[j % kLow] += (x[j] - (sum - of_some)) + (some[j] - of_some);
+              x[j] = sum;
+              some[j] = 0.f;
+            }
           }
           tc_fence_before();
           __syncwarp();
@@ -163,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1) head_few_kernel(const __grid_cons
       ok = *give_up == 0;
       if (warp < 6) {
 #pragma unroll
-        for (int j = 0; j < NC; ++j) turn[j * kHeadCols + q * 32 + lane] = x[j];
+        for (int j = 0; j < NC; ++j) turn[j * kHeadCols + q * 32 + lane] = kLow == NC ? x[j] + low[j % kLow] : x[j];
       }
       named_barrier(1, 32 * kWarps);
       if (!ok) break;
