@@ -408,7 +408,8 @@ mixlora_status_t mixlora_attention_backward(const mixlora_attention_shape_t *sha
  * over all shards); where it is 0 the gradient is 0.  w gets no gradient.
  *
  * x, d_x [T, d], w [vocab, d] of shape.dtype, 16-byte aligned, rows *_stride elements apart (0: dense); d_x must not
- * overlap an input.  d_model and the strides are multiples of 8.  Tokens that are left out cost nothing in the products.
+ * overlap an input.  d_model and the strides are multiples of 8.  In batches of more than 256 tokens those that are left out
+ * cost nothing in the products.
  * Logits are sums in fp32, and so are the gradients of the fp32 mode, where operands are taken apart into three bf16 values
  * that hold their 24 bits (values below 2^-100 lose some).  The tensor core cuts off what its sums have behind 24 bits; it is
  * given so few of a logit's products at once, and every other part with the opposite sign, that a logit of a token that leans

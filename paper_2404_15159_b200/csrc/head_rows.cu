@@ -1,7 +1,7 @@
 // What the head's losses do once a row: which rows count, a teacher's lists, and the join of a row's tiles.
 //
-// All of it is small beside the products (8192 rows of 32000 columns: scan 10, join 27 of 3390 us; 4096 rows with 64 entries:
-// lists 10, scan 5, rows side by side 12, join 25 of 1660), so what can lose bits by cancellation is done in 64 bits:
+// All of it is small beside the products (8192 rows of 32000 columns: scan 9, join 27 of 3410 us; 4096 rows with 64 entries:
+// lists 10, scan 6, rows side by side 10, join 30 of 1670), so what can lose bits by cancellation is done in 64 bits:
 // probabilities of a teacher, log-sum-exps, gradients towards listed columns.  With few rows these kernels wait for one load
 // after another; each starts under its predecessor, and the join is 5 to 9 us of a call of 40.
 #include <math.h>

@@ -12,9 +12,9 @@
 // 2^-20 of a logit, always towards zero.  So a sum starts anew every few spans of k-blocks, and the parts are added up in
 // registers, rounded to nearest; and every span of the logits has a partner that goes the other way (see Spans).
 //
-// Measured on a B200, 8192 rows, 32000 columns, width 4096: logits 1.45 ms, gradient 1.41 ms in short runs (1.48 and
-// 1.52 PFLOP/s, tensor pipe 83 and 90 % active at 1.6 and 1.45 GHz under the power cap), 3.39 ms a call one after another
-// (1.27 PFLOP/s; the library's own dense product in such a loop: 1.38).  512 rows: 112 and 97 us (four rounds of tiles for
+// Measured on a B200, 8192 rows, 32000 columns, width 4096: logits 1.51 ms, gradient 1.45 ms in short runs (1.42 and
+// 1.48 PFLOP/s, tensor pipe 79 and 90 % active at 1.6 and 1.5 GHz under the power cap), 3.41 ms a call one after another
+// (1.26 PFLOP/s; the library's own dense product in such a loop: 1.38).  512 rows: 116 and 98 us (four rounds of tiles for
 // 3.4; tiles that are narrower wait for their operands as long).
 //
 // In the fp32 mode (PARTS = 3) an operand is the sum of three bf16 values that hold its 24 bits, and the six products of
@@ -54,8 +54,9 @@ template <bool TO_X, int PARTS> struct Form {
 // products lean one way.  On the way up the cut takes from the first sum a, on the way down from a - b, which adds it to
 // b: a + b = 2 a - (a - b) has lost on one way what it won on the other.  On logits whose products lean by 0.3 of their spread, as a
 // sure token's with its label, width 4096: too small by 8.9 units of 2^-23 with spans of 16 k-blocks that do not turn, by 2.0 with
-// spans of 4 (which take 15 % longer), by 0.3 with spans of 16 that do, with a spread of 0.9 (fp32's own products: 0.5).  A
-// span without a partner has 4 k-blocks at most.
+// spans of 4 (which take 15 % longer), by 0.3 with spans of 16 that do (which take 1 to 3 %: adding to what is there at a
+// span's start, and the change of sign), with a spread of 0.95 (fp32's own products: 0 and 0.5).  A span without a partner has 4
+// k-blocks at most.  Of products of one sign the cut at each product's own last bits remains: 9.8 units.
 constexpr int kLeastSpan = 4;
 template <bool TO_X, int PARTS> struct Spans {
   using F = Form<TO_X, PARTS>;
