@@ -111,7 +111,7 @@ __device__ __forceinline__ HeadParts head_parts(float x) {
 cudaError_t launch_head_lists(const HeadArgs& p, cudaStream_t st);        // a teacher's entries: list, list_q, rest_q, list_n
 cudaError_t launch_head_scan(const HeadArgs& p, bool first, cudaStream_t st);   // row_token, token_row, state (few tokens: none of it needed)
 cudaError_t launch_head_parts(const HeadArgs& p, bool first, cudaStream_t st);   // fp32 mode: w_parts; x_rows where rows are tokens
-cudaError_t launch_head_gather(const HeadArgs& p, bool first_piece, cudaStream_t st);   // x_rows, zeroes of d_x
+cudaError_t launch_head_gather(const HeadArgs& p, cudaStream_t st);       // x_rows; before the first piece zeroes of d_x
 cudaError_t launch_head_logits_tc(const HeadArgs& p, cudaStream_t st);    // stats, z_listed, E
 cudaError_t launch_head_logits_few(const HeadArgs& p, bool first, cudaStream_t st);   // the same for up to kHeadFewTokens; clears the state
 cudaError_t launch_head_join(const HeadArgs& p, cudaStream_t st);         // loss, lse, totals; E finished, row_scale

@@ -193,7 +193,7 @@ mixlora_status_t run_head(const mixlora_head_shape_t* s, const HeadCall& c, void
   if (L.parts == 3) MIXLORA_TRY(launch_head_parts(a, a.few && !lists, st));
   for (int i = 0; i < L.pieces; ++i) {
     a.piece0 = i * L.piece;
-    if (!a.few) MIXLORA_TRY(launch_head_gather(a, i == 0, st));
+    if (!a.few) MIXLORA_TRY(launch_head_gather(a, st));
     MIXLORA_TRY(launch_head_logits_tc(a, st));
     MIXLORA_TRY(launch_head_join(a, st));
     if (gradient) MIXLORA_TRY(launch_head_grad_tc(a, st));
