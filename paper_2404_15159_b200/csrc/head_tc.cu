@@ -47,7 +47,7 @@ template <bool TO_X, int PARTS> struct Form {
   // a cost of 8 or 12, which takes nine shares where 24 takes four, 333 tokens of width 2048 took 135 us instead of 129
   static constexpr int kShareMin = PARTS == 1 ? 16 : 3, kShareCost = PARTS == 1 ? 24 : 4;
 };
-// The span that starts at k-block k0 of [kb0, kb1).
+// The spans of a tile's sums, one after another: the one that starts at k-block k0 ends at k1.
 //
 // Where spans turn around, up to four make a group: the first two, one in either accumulator, add their products up from
 // zero, and the other two go on in the same accumulators with their products subtracted, back to about zero where a row's

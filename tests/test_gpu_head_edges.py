@@ -353,3 +353,20 @@ def test_a_list_of_one_entry_is_a_label(B, t, dtype):
     assert all(torch.equal(a[n], b[n]) for n in ("loss", "lse", "totals", "d_x"))
     b = run(B, x, w, index, torch.randn(t, 3, generator=g, device="cuda"))
     check(B, b, want(x, w, index, torch.zeros(t, 3, device="cuda")))
+
+
+@TOKENS
+@pytest.mark.parametrize("softcap", [0.0, 4.0])
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+def test_no_number_is_lost_in_a_sum_of_many_spans(B, bad, softcap, t):
+    # wherever in the reduction it stands: spans that go up, that go down, and the last one
+    v, d = 300, 2376
+    g, x, w = rand(55, t, v, d, torch.bfloat16)
+    labels = torch.randint(0, v, (t,), generator=g, device="cuda", dtype=torch.int32)
+    out = torch.arange(3, 3 + 12 * 3, 3, device="cuda")
+    x[out, torch.arange(12, device="cuda") * 215 + 7] = bad
+    got = run(B, x, w, labels, softcap=softcap, normalizer=torch.full((1,), float(t), device="cuda"))
+    torch.cuda.synchronize()
+    keep = torch.ones(t, dtype=torch.bool, device="cuda").index_fill(0, out, False)
+    for n in ("loss", "lse", "d_x"):
+        assert got[n][out].isnan().all() and not got[n][keep].isnan().any(), n
